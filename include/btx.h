@@ -217,6 +217,45 @@ btx_status btx_merge_ffn(int32_t n_models, int32_t dtype, int32_t layout, int32_
                          const void* const* w2_src, void* w1_dst, void* w3_dst, void* w2_dst,
                          void* workspace, size_t workspace_bytes, void* stream);
 
+/* Score routing: the choice of k experts per token from given logits[T,E] (rows `logits_stride` elements
+ * apart, desc.dtype), as later mixture-of-experts models do it (the paper's router is btx_moe_forward's).
+ *   s = softmax(z) or sigmoid(z) over the row;  c = s + bias (bias[E] fp32 or NULL; it takes part in the
+ *   choice only, never in the weights);  with NULL the experts are ordered by z itself.
+ *   Groups: the E experts are n_group runs of E/n_group; a group counts as much as its best c (MAX) or the
+ *   sum of its two best (SUM2; without a bias: of their scores); only the topk_group best groups take part.
+ *   (n_group = 1: no groups.)
+ *   topk_idx[T,k]: the k largest c, largest first; ties between groups and between experts go to the lower
+ *   index.  The order is that of the exact values: a row whose order fp32 cannot settle is settled in fp64.
+ *   gates[T,k] = scale * s, or with `renorm` scale * s / (sum of s over the row's choice).
+ *   An expert with a logit of -inf or NaN (or whose c is) is switched off in that row: score 0, never chosen.
+ *   Slots that find no expert, and all slots of rows with row_valid[t] == 0 (row_valid may be NULL), have
+ *   topk_idx -1 and gate 0.
+ * Optional outputs, NULL to skip: scores[T,E] fp32 (s; 0 in rows that are not valid), counts[E] (tokens per
+ * expert, from which a caller moves its bias).  E <= 512, k <= 32, n_group <= 32, k <= topk_group * E / n_group,
+ * scale > 0.  T may be 0.  Pointers need the alignment of their elements; rows that start on 16-byte boundaries
+ * and hold whole 16-byte vectors are read fastest.  No workspace: calls on different streams may overlap. */
+typedef enum { BTX_SCORE_SOFTMAX = 0, BTX_SCORE_SIGMOID = 1 } btx_score;
+typedef enum { BTX_GROUP_MAX = 0, BTX_GROUP_SUM2 = 1 } btx_group_score;
+typedef struct {
+  int32_t T, E, k;
+  int32_t dtype;              /* btx_dtype of logits and dlogits */
+  int32_t score;              /* btx_score */
+  int32_t n_group, topk_group;
+  int32_t group_score;        /* btx_group_score */
+  int32_t renorm;
+  float   scale;
+} btx_route_desc;
+btx_status btx_route(const btx_route_desc* desc, const void* logits, int64_t logits_stride, const float* bias,
+                     const uint8_t* row_valid, int32_t* topk_idx, float* gates, float* scores, int32_t* counts,
+                     void* stream);
+
+/* Gradient of btx_route's gates: dlogits[T,E] (desc.dtype, rows dlogits_stride elements apart, overwritten) from
+ * dgates[T,k] fp32, the same logits and the topk_idx that btx_route returned.  The choice is piecewise constant
+ * and has no gradient, nor has the bias.  Slots with an index outside 0..E-1 add nothing. */
+btx_status btx_route_backward(const btx_route_desc* desc, const void* logits, int64_t logits_stride,
+                              const int32_t* topk_idx, const float* dgates, void* dlogits, int64_t dlogits_stride,
+                              void* stream);
+
 /* Synchronises `stream` and reads the status word that kernels of earlier calls left in
  * `workspace`: *device_status (host) is BTX_OK or BTX_ERR_TIMEOUT. */
 btx_status btx_device_status(const void* workspace, void* stream, int32_t* device_status);

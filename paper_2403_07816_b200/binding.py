@@ -18,6 +18,8 @@ BTX_F32, BTX_BF16 = 0, 1
 ROUTE_TOPK, ROUTE_SWITCH, ROUTE_SOFT, ROUTE_SAMPLE1 = 0, 1, 2, 3
 PARAM_AVERAGE, PARAM_FFN = 0, 1
 FFN_STACK, FFN_SPLIT, FFN_BLEND = 0, 1, 2
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+GROUP_MAX, GROUP_SUM2 = 0, 1
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libbtx.so")
 _lib = None
@@ -47,8 +49,15 @@ class MergeItem(C.Structure):
                 ("src", C.POINTER(C.c_void_p)), ("dst", C.c_void_p)]
 
 
+class RouteDesc(C.Structure):
+    _fields_ = [("T", C.c_int32), ("E", C.c_int32), ("k", C.c_int32), ("dtype", C.c_int32), ("score", C.c_int32),
+                ("n_group", C.c_int32), ("topk_group", C.c_int32), ("group_score", C.c_int32), ("renorm", C.c_int32),
+                ("scale", C.c_float)]
+
+
 EXPORTS = ["btx_moe_sizes", "btx_moe_forward", "btx_moe_backward", "btx_moe_step_host",
            "btx_lb_loss_workspace_size", "btx_lb_loss", "btx_lb_loss_noalloc", "btx_merge_workspace_size", "btx_merge", "btx_merge_ffn_workspace_size", "btx_merge_ffn",
+           "btx_route", "btx_route_backward",
            "btx_device_status", "btx_selftest_wait_expiry", "btx_set_stage_events", "btx_status_string", "btx_version"]
 
 
@@ -75,6 +84,8 @@ def lib():
         L.btx_merge_ffn_workspace_size.argtypes = [i32, i32, C.POINTER(sz)]
         L.btx_merge_ffn.argtypes = [i32, i32, i32, i32, i32, i32, C.POINTER(vp), C.POINTER(vp), C.POINTER(vp), vp, vp, vp,
                                     vp, sz, vp]
+        L.btx_route.argtypes = [C.POINTER(RouteDesc), vp, C.c_int64, vp, vp, vp, vp, vp, vp, vp]
+        L.btx_route_backward.argtypes = [C.POINTER(RouteDesc), vp, C.c_int64, vp, vp, vp, C.c_int64, vp]
         L.btx_device_status.argtypes = [vp, vp, C.POINTER(i32)]
         L.btx_status_string.argtypes = [i32]
         L.btx_status_string.restype = C.c_char_p
@@ -313,6 +324,68 @@ def btx_merge_ffn(w1s, w3s, w2s, layout, chunks, w1_dst, w3_dst, w2_dst, workspa
     if s != BTX_OK:
         raise BtxError(s, "btx_merge_ffn")
     return workspace
+
+
+def _check(t, name, shape, dtype, device, optional=False):
+    """Shape, type and device of a tensor argument; the library sees only its address."""
+    if t is None:
+        if optional:
+            return
+        raise ValueError(f"btx: {name} is missing")
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device:
+        raise ValueError(f"btx: {name} must be {tuple(shape)} {dtype} on {device}, not {tuple(t.shape)} {t.dtype} on {t.device}")
+
+
+def _rows(t, name):
+    """Address and row stride of a matrix whose rows are contiguous (any row stride)."""
+    if not t.is_cuda:
+        raise RuntimeError("btx: tensors must live on a CUDA device (there is no CPU path)")
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise RuntimeError(f"btx: the rows of {name} must be contiguous and must not overlap")
+    return C.c_void_p(t.data_ptr()), max(t.stride(0), t.shape[1])
+
+
+def make_route_desc(T, E, k, dtype, score=SCORE_SOFTMAX, n_group=1, topk_group=1, group_score=GROUP_MAX, renorm=True,
+                    scale=1.0) -> RouteDesc:
+    code = _dtype_code(dtype) if isinstance(dtype, torch.dtype) else int(dtype)
+    return RouteDesc(T, E, k, code, score, n_group, topk_group, group_score, int(renorm), float(scale))
+
+
+def btx_route(desc, logits, bias, topk_idx, gates, scores=None, counts=None, row_valid=None):
+    """Expert choice and weights from router logits [T,E] (rows may be strided); see btx.h."""
+    T, E, k, dev = desc.T, desc.E, desc.k, logits.device
+    _check(logits, "logits", (T, E), torch.bfloat16 if desc.dtype == BTX_BF16 else torch.float32, dev)
+    _check(bias, "bias", (E,), torch.float32, dev, True)
+    _check(topk_idx, "topk_idx", (T, k), torch.int32, dev)
+    _check(gates, "gates", (T, k), torch.float32, dev)
+    _check(scores, "scores", (T, E), torch.float32, dev, True)
+    _check(counts, "counts", (E,), torch.int32, dev, True)
+    if row_valid is not None and row_valid.dtype == torch.bool:
+        row_valid = row_valid.view(torch.uint8)
+    _check(row_valid, "row_valid", (T,), torch.uint8, dev, True)
+    rows, stride = _rows(logits, "logits")
+    with _on(dev):
+        s = lib().btx_route(C.byref(desc), rows, stride, _ptr(bias), _ptr(row_valid), _ptr(topk_idx), _ptr(gates),
+                            _ptr(scores), _ptr(counts), _stream(dev))
+    if s != BTX_OK:
+        raise BtxError(s, "btx_route")
+
+
+def btx_route_backward(desc, logits, topk_idx, dgates, dlogits):
+    """d logits from d gates (fp32 [T,k]) and the choice btx_route made; see btx.h."""
+    T, E, k, dev = desc.T, desc.E, desc.k, logits.device
+    dt = torch.bfloat16 if desc.dtype == BTX_BF16 else torch.float32
+    _check(logits, "logits", (T, E), dt, dev)
+    _check(topk_idx, "topk_idx", (T, k), torch.int32, dev)
+    _check(dgates, "dgates", (T, k), torch.float32, dev)
+    _check(dlogits, "dlogits", (T, E), dt, dev)
+    rows, stride = _rows(logits, "logits")
+    out, out_stride = _rows(dlogits, "dlogits")
+    with _on(dev):
+        s = lib().btx_route_backward(C.byref(desc), rows, stride, _ptr(topk_idx), _ptr(dgates), out, out_stride,
+                                     _stream(dev))
+    if s != BTX_OK:
+        raise BtxError(s, "btx_route_backward")
 
 
 def btx_selftest_wait_expiry(workspace):

@@ -141,8 +141,6 @@ static EffectiveRouting effective_routing(const btx_moe_desc* desc) {
   return {BTX_ROUTE_TOPK, 1.0f};
 }
 
-static bool misaligned(const void* p) { return ((uintptr_t)p & 15) != 0; }
-
 // One helper stream per device, created on first use and kept for the life of the process: the
 // backward pass runs its memory-bound router kernels on it beside the tensor-bound weight-gradient
 // GEMMs.  nullptr when it cannot be had; the backward then runs on the caller's stream alone.
@@ -197,7 +195,7 @@ int btx::sm_count() {
 
 namespace btx {
 
-static btx_status check_device() {
+btx_status check_device() {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return BTX_ERR_CUDA;
   int major = 0;

@@ -68,6 +68,11 @@ void mark_stage(int i, cudaStream_t st);
 // Multiprocessor count of the current device (looked up once per device).
 int sm_count();
 
+// BTX_OK when the current device is of compute capability 10.x.
+btx_status check_device();
+
+inline bool misaligned(const void* p) { return ((uintptr_t)p & 15) != 0; }
+
 // ---------------------------------------------------------------------------------------------
 // Launchers (defined in the .cu files).
 // ---------------------------------------------------------------------------------------------
