@@ -256,6 +256,54 @@ btx_status btx_route_backward(const btx_route_desc* desc, const void* logits, in
                               const int32_t* topk_idx, const float* dgates, void* dlogits, int64_t dlogits_stride,
                               void* stream);
 
+/* MXFP4 (OCP Microscaling Formats v1.0: e2m1 elements, one power-of-two scale per 32 of them), for experts
+ * served in 4 bits: 17/32 bytes per weight.  A matrix of `rows` rows of K elements (K a multiple of 32), or a
+ * batch of them, is held as
+ *   codes   [batch][rows][K/2] bytes, two elements per byte, the even one in the low half; codes 0..7 are
+ *           0, 0.5, 1, 1.5, 2, 3, 4, 6, bit 3 is the sign;
+ *   scales  [batch][ceil(rows/128)][ceil(K/128)][512] bytes: byte (r % 32) * 16 + (r / 32 % 4) * 4 + j of a
+ *           tile is the scale 2^(b - 127) of elements 32 (4c + j) .. of row r (255: the block is NaN).
+ * btx_mx4_sizes gives the bytes of both (either pointer may be NULL); both are 16-byte aligned.
+ *
+ * btx_mx4_quantize casts src[batch][rows][K] (dtype, rows `row_stride` and matrices `batch_stride` elements
+ * apart, elements of a row contiguous): scale 2^(floor(log2 max|x|) - 2), not below 2^-127; elements to the
+ * nearest value, ties to the even code, at most 6 in size; a block that holds an infinity or NaN becomes NaN.
+ * Row r goes to row row_first + r * row_step of a matrix of out_rows rows (0, 1, rows: as it stands; W1 with
+ * (0, 2) and W3 with (1, 2) make the interleaved matrix of btx_mx4_moe_forward).  Bytes of rows that the call
+ * does not name are left as they were, and so are scale bytes past the last row; those past K are 0.
+ * btx_mx4_dequantize gives the values back, dst[batch][rows][K], exactly (contiguous). */
+btx_status btx_mx4_sizes(int32_t batch, int32_t rows, int32_t K, size_t* code_bytes, size_t* scale_bytes);
+btx_status btx_mx4_quantize(int32_t dtype, const void* src, int64_t row_stride, int64_t batch_stride, int32_t batch,
+                            int32_t rows, int32_t K, int32_t out_rows, int32_t row_first, int32_t row_step,
+                            void* codes, void* scales, void* stream);
+btx_status btx_mx4_dequantize(int32_t dtype, const void* codes, const void* scales, int32_t batch, int32_t rows,
+                              int32_t K, void* dst, void* stream);
+
+/* y[batch][M][N] (dtype, contiguous) = A B^T of A[batch][M][K] and B[batch][N][K], both MXFP4: products of the
+ * values, fp32 accumulation, one rounding.  K is a multiple of 32, M and N are any size (M or batch 0: nothing
+ * to do).  Inference: there is no gradient through the cast.  The workspace serves one call at a time. */
+btx_status btx_mx4_matmul_workspace_size(int32_t dtype, int32_t batch, int32_t M, int32_t N, int32_t K,
+                                         size_t* workspace_bytes);
+btx_status btx_mx4_matmul(int32_t dtype, int32_t batch, int32_t M, int32_t N, int32_t K, const void* a_codes,
+                          const void* a_scales, const void* b_codes, const void* b_scales, void* y, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/* The expert layer of btx_moe_forward (Section 3.2) on MXFP4 experts under a routing from elsewhere, e.g.
+ * btx_route:  y_t = sum over slots j of gates[t,j] * W2_e a,  a = mx4(silu(W1_e mx4(x_t)) * W3_e mx4(x_t)),
+ * e = topk_idx[t,j].  Activations are cast to MXFP4 in front of both products, silu and the products are
+ * formed in fp32, slots are added in fp32 in slot order, y is rounded once.
+ *   x[T,d], y[T,d] in dtype; topk_idx[T,k] int32 (an index outside 0..E-1 is an empty slot: it adds nothing);
+ *   gates[T,k] fp32; w13: E matrices of 2F rows of d, row 2i is row i of W1_e and row 2i + 1 row i of W3_e;
+ *   w2: E matrices of d rows of F.  d and F are multiples of 32, E <= 512, T may be 0. */
+typedef struct {
+  int32_t T, d_model, d_ff, E, k;
+  int32_t dtype;              /* btx_dtype of x and y */
+} btx_mx4_moe_desc;
+btx_status btx_mx4_moe_workspace_size(const btx_mx4_moe_desc* desc, size_t* workspace_bytes);
+btx_status btx_mx4_moe_forward(const btx_mx4_moe_desc* desc, const void* x, const int32_t* topk_idx, const float* gates,
+                               const void* w13_codes, const void* w13_scales, const void* w2_codes,
+                               const void* w2_scales, void* y, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Synchronises `stream` and reads the status word that kernels of earlier calls left in
  * `workspace`: *device_status (host) is BTX_OK or BTX_ERR_TIMEOUT. */
 btx_status btx_device_status(const void* workspace, void* stream, int32_t* device_status);

@@ -55,9 +55,16 @@ class RouteDesc(C.Structure):
                 ("scale", C.c_float)]
 
 
+class Mx4MoeDesc(C.Structure):
+    _fields_ = [("T", C.c_int32), ("d_model", C.c_int32), ("d_ff", C.c_int32), ("E", C.c_int32), ("k", C.c_int32),
+                ("dtype", C.c_int32)]
+
+
 EXPORTS = ["btx_moe_sizes", "btx_moe_forward", "btx_moe_backward", "btx_moe_step_host",
            "btx_lb_loss_workspace_size", "btx_lb_loss", "btx_lb_loss_noalloc", "btx_merge_workspace_size", "btx_merge", "btx_merge_ffn_workspace_size", "btx_merge_ffn",
            "btx_route", "btx_route_backward",
+           "btx_mx4_sizes", "btx_mx4_quantize", "btx_mx4_dequantize", "btx_mx4_matmul_workspace_size", "btx_mx4_matmul",
+           "btx_mx4_moe_workspace_size", "btx_mx4_moe_forward",
            "btx_device_status", "btx_selftest_wait_expiry", "btx_set_stage_events", "btx_status_string", "btx_version"]
 
 
@@ -86,6 +93,14 @@ def lib():
                                     vp, sz, vp]
         L.btx_route.argtypes = [C.POINTER(RouteDesc), vp, C.c_int64, vp, vp, vp, vp, vp, vp, vp]
         L.btx_route_backward.argtypes = [C.POINTER(RouteDesc), vp, C.c_int64, vp, vp, vp, C.c_int64, vp]
+        i64 = C.c_int64
+        L.btx_mx4_sizes.argtypes = [i32, i32, i32, C.POINTER(sz), C.POINTER(sz)]
+        L.btx_mx4_quantize.argtypes = [i32, vp, i64, i64, i32, i32, i32, i32, i32, i32, vp, vp, vp]
+        L.btx_mx4_dequantize.argtypes = [i32, vp, vp, i32, i32, i32, vp, vp]
+        L.btx_mx4_matmul_workspace_size.argtypes = [i32, i32, i32, i32, i32, C.POINTER(sz)]
+        L.btx_mx4_matmul.argtypes = [i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.btx_mx4_moe_workspace_size.argtypes = [C.POINTER(Mx4MoeDesc), C.POINTER(sz)]
+        L.btx_mx4_moe_forward.argtypes = [C.POINTER(Mx4MoeDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.btx_device_status.argtypes = [vp, vp, C.POINTER(i32)]
         L.btx_status_string.argtypes = [i32]
         L.btx_status_string.restype = C.c_char_p
@@ -386,6 +401,126 @@ def btx_route_backward(desc, logits, topk_idx, dgates, dlogits):
                                      _stream(dev))
     if s != BTX_OK:
         raise BtxError(s, "btx_route_backward")
+
+
+@dataclass
+class Mx4:
+    """A batch of matrices [batch, rows, K] held as MXFP4 codes and scale tiles (layout in btx.h)."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+
+    @staticmethod
+    def empty(batch, rows, K, device):
+        btx_mx4_sizes(batch, rows, K)
+        return Mx4(torch.empty((batch, rows, K // 2), dtype=torch.uint8, device=device),
+                   torch.empty((batch, (rows + 127) // 128, (K + 127) // 128, 512), dtype=torch.uint8, device=device))
+
+    @property
+    def shape(self):
+        b, r, c = self.codes.shape
+        return b, r, 2 * c
+
+
+def _mx4_ptrs(q, name, shape, device):
+    batch, rows, K = shape
+    _check(q.codes, name + ".codes", (batch, rows, K // 2), torch.uint8, device)
+    _check(q.scales, name + ".scales", (batch, (rows + 127) // 128, (K + 127) // 128, 512), torch.uint8, device)
+    return _ptr(q.codes), _ptr(q.scales)
+
+
+def btx_mx4_sizes(batch, rows, K):
+    """Bytes of the codes and of the scales of a batch of MXFP4 matrices."""
+    codes, scales = C.c_size_t(0), C.c_size_t(0)
+    s = lib().btx_mx4_sizes(batch, rows, K, C.byref(codes), C.byref(scales))
+    if s != BTX_OK:
+        raise BtxError(s, "btx_mx4_sizes")
+    return codes.value, scales.value
+
+
+def btx_mx4_quantize(src, out, row_first=0, row_step=1):
+    """src [batch, rows, K] or [rows, K] (contiguous rows, any row and batch stride) cast into the Mx4 `out`; row r
+    becomes row row_first + r * row_step."""
+    if not src.is_cuda:
+        raise RuntimeError("btx: tensors must live on a CUDA device (there is no CPU path)")
+    v = src if src.dim() == 3 else src.unsqueeze(0)
+    batch, rows, K = v.shape
+    if K > 1 and v.stride(2) != 1:
+        raise RuntimeError("btx: the rows of src must be contiguous")
+    ob, orows, oK = out.shape
+    if ob != batch or oK != K:
+        raise ValueError(f"btx: src is {tuple(v.shape)}, out is {out.shape}")
+    codes, scales = _mx4_ptrs(out, "out", out.shape, src.device)
+    with _on(src.device):
+        s = lib().btx_mx4_quantize(_dtype_code(src.dtype), C.c_void_p(src.data_ptr()), v.stride(1), v.stride(0), batch, rows, K,
+                                   orows, row_first, row_step, codes, scales, _stream(src.device))
+    if s != BTX_OK:
+        raise BtxError(s, "btx_mx4_quantize")
+
+
+def btx_mx4_dequantize(q, dst):
+    """The values of the Mx4 `q` into dst (contiguous, [batch, rows, K] or [rows, K] for one matrix)."""
+    batch, rows, K = q.shape
+    if dst.numel() != batch * rows * K or dst.shape[-1] != K:
+        raise ValueError(f"btx: dst is {tuple(dst.shape)}, q is {q.shape}")
+    codes, scales = _mx4_ptrs(q, "q", q.shape, dst.device)
+    with _on(dst.device):
+        s = lib().btx_mx4_dequantize(_dtype_code(dst.dtype), codes, scales, batch, rows, K, _ptr(dst), _stream(dst.device))
+    if s != BTX_OK:
+        raise BtxError(s, "btx_mx4_dequantize")
+
+
+def btx_mx4_matmul_workspace_size(M, N, K, dtype, batch=1):
+    sz = C.c_size_t(0)
+    s = lib().btx_mx4_matmul_workspace_size(_dtype_code(dtype), batch, M, N, K, C.byref(sz))
+    if s != BTX_OK:
+        raise BtxError(s, "btx_mx4_matmul_workspace_size")
+    return sz.value
+
+
+def btx_mx4_matmul(a, b, y, workspace):
+    """y = a b^T of two Mx4 of the same batch and K; y is [batch, M, N], or [M, N] for one matrix."""
+    batch, M, K = a.shape
+    bb, N, bK = b.shape
+    if bb != batch or bK != K:
+        raise ValueError(f"btx: a is {a.shape}, b is {b.shape}")
+    dev = y.device
+    _check(y, "y", (batch, M, N) if y.dim() == 3 or batch != 1 else (M, N), y.dtype, dev)
+    ac, asc = _mx4_ptrs(a, "a", a.shape, dev)
+    bc, bsc = _mx4_ptrs(b, "b", b.shape, dev)
+    with _on(dev):
+        s = lib().btx_mx4_matmul(_dtype_code(y.dtype), batch, M, N, K, ac, asc, bc, bsc, _ptr(y), _ptr(workspace),
+                                 workspace.numel(), _stream(dev))
+    if s != BTX_OK:
+        raise BtxError(s, "btx_mx4_matmul")
+
+
+def make_mx4_moe_desc(T, d_model, d_ff, E, k, dtype) -> Mx4MoeDesc:
+    return Mx4MoeDesc(T, d_model, d_ff, E, k, _dtype_code(dtype) if isinstance(dtype, torch.dtype) else int(dtype))
+
+
+def btx_mx4_moe_workspace_size(desc):
+    sz = C.c_size_t(0)
+    s = lib().btx_mx4_moe_workspace_size(C.byref(desc), C.byref(sz))
+    if s != BTX_OK:
+        raise BtxError(s, "btx_mx4_moe_workspace_size")
+    return sz.value
+
+
+def btx_mx4_moe_forward(desc, x, topk_idx, gates, w13, w2, y, workspace):
+    """The expert layer on MXFP4 experts under a given routing; w13 holds the rows of W1 and W3 in turn; see btx.h."""
+    T, d, F, E, k, dev = desc.T, desc.d_model, desc.d_ff, desc.E, desc.k, x.device
+    dt = torch.bfloat16 if desc.dtype == BTX_BF16 else torch.float32
+    _check(x, "x", (T, d), dt, dev)
+    _check(topk_idx, "topk_idx", (T, k), torch.int32, dev)
+    _check(gates, "gates", (T, k), torch.float32, dev)
+    _check(y, "y", (T, d), dt, dev)
+    c13, s13 = _mx4_ptrs(w13, "w13", (E, 2 * F, d), dev)
+    c2, s2 = _mx4_ptrs(w2, "w2", (E, d, F), dev)
+    with _on(dev):
+        s = lib().btx_mx4_moe_forward(C.byref(desc), _ptr(x), _ptr(topk_idx), _ptr(gates), c13, s13, c2, s2, _ptr(y),
+                                      _ptr(workspace), workspace.numel(), _stream(dev))
+    if s != BTX_OK:
+        raise BtxError(s, "btx_mx4_moe_forward")
 
 
 def btx_selftest_wait_expiry(workspace):

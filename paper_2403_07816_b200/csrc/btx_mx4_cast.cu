@@ -1,0 +1,474 @@
+// MXFP4 casts and the row dispatch of the expert layer on MXFP4 weights: the memory-bound steps around the products.
+//
+//   quantize     per 32 elements: scale 2^(floor(log2 max|x|) - 2), elements to the nearest e2m1 value (ties to the
+//                even code, at most 6).  Four lanes share a block, eight elements each: a warp reads 256 consecutive
+//                elements with 16-byte loads, the maximum takes two shuffles, a lane stores four bytes of codes and
+//                every sixteenth lane four scale bytes.  Bound by memory: 2 + 17/32 bytes per bf16 element.
+//   dequantize   the same mapping backwards
+//   dispatch     stable counting sort of the assignments by expert, padded to 128-row tiles
+//   quantize_rows  quantize of x with every row written to the k rows of its token: x is read once
+#include <cuda_fp4.h>
+
+#include "btx_mx4.cuh"
+#include "btx_route_dev.cuh"
+
+namespace btx {
+namespace mx4 {
+namespace {
+
+using routedev::Vec;
+
+constexpr unsigned kAll = 0xffffffffu;
+constexpr int kCastThreads = 256;
+constexpr int kCastUnroll = 4;             // 256-element chunks a warp has in flight
+constexpr int kSortThreads = 512;
+constexpr int kSortChunk = 2048;           // assignments per block of the dispatch kernels
+
+template <typename T> __device__ __forceinline__ void load8(const T* p, float (&v)[8], bool vec);
+template <> __device__ __forceinline__ void load8<float>(const float* p, float (&v)[8], bool vec) {
+  if (vec) {
+    const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = p[i];
+  }
+}
+template <> __device__ __forceinline__ void load8<__nv_bfloat16>(const __nv_bfloat16* p, float (&v)[8], bool vec) {
+  if (vec) {
+    Vec<__nv_bfloat16>::unpack(__ldcs(reinterpret_cast<const uint4*>(p)), v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __bfloat162float(p[i]);
+  }
+}
+
+__device__ __forceinline__ uint32_t e2m1_pair(float lo, float hi) {
+  return (uint32_t)__nv_cvt_float2_to_fp4x2(make_float2(lo, hi), __NV_E2M1, cudaRoundNearest);
+}
+
+// Eight elements of a block shared by four neighbouring lanes: four bytes of codes and the block's scale byte.
+__device__ __forceinline__ uint32_t cast8(const float (&v)[8], uint32_t& byte) {
+  uint32_t amax = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) amax = max(amax, __float_as_uint(v[i]) & 0x7fffffffu);
+  amax = max(amax, __shfl_xor_sync(kAll, amax, 1));
+  amax = max(amax, __shfl_xor_sync(kAll, amax, 2));
+  float inv;
+  byte = scale_byte(amax, inv);
+  if (byte == 255u) return 0u;
+  uint32_t q = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) q |= e2m1_pair(v[2 * i] * inv, v[2 * i + 1] * inv) << (8 * i);
+  return q;
+}
+// The scale bytes of the four blocks (128 elements) of sixteen lanes as one word, in all of them.
+__device__ __forceinline__ uint32_t scale_word(uint32_t byte, int lane) {
+  uint32_t w = byte << (8 * ((lane >> 2) & 3));
+  w |= __shfl_xor_sync(kAll, w, 4);
+  w |= __shfl_xor_sync(kAll, w, 8);
+  return w;
+}
+__device__ __forceinline__ size_t scale_offset(size_t tile_row0, int row, int kt, int chunk) {
+  return ((tile_row0 + row / kTileRows) * (size_t)kt + chunk) * kTileBytes + (row & 31) * 16 + ((row >> 5) & 3) * 4;
+}
+
+// A warp takes kCastUnroll chunks of 256 elements of one row at a time.
+template <typename T>
+__global__ void __launch_bounds__(kCastThreads)
+quantize_kernel(const CastParams p, int vec, long long items, int groups) {
+  const int lane = threadIdx.x & 31;
+  const int kt = (int)scale_tiles_k(p.K);
+  const size_t tiles = ((size_t)p.out_rows + kTileRows - 1) / kTileRows;
+  for (long long w = ((long long)blockIdx.x * kCastThreads + threadIdx.x) >> 5; w < items;
+       w += (long long)gridDim.x * (kCastThreads / 32)) {
+    const int g = (int)(w % groups);
+    const long long r = w / groups;
+    const int row = (int)(r % p.rows), b = (int)(r / p.rows);
+    const T* src = (const T*)p.src + b * p.batch_stride + row * p.row_stride;
+    const int out_row = p.first + row * p.step;
+    float v[kCastUnroll][8];
+#pragma unroll
+    for (int u = 0; u < kCastUnroll; ++u) {
+      const int c = (g * kCastUnroll + u) * 256 + lane * 8;
+      if (c < p.K) {
+        load8<T>(src + c, v[u], vec != 0);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[u][i] = 0.f;
+      }
+    }
+    uint8_t* codes = p.codes + ((size_t)b * p.out_rows + out_row) * (p.K / 2);
+#pragma unroll
+    for (int u = 0; u < kCastUnroll; ++u) {
+      const int c = (g * kCastUnroll + u) * 256 + lane * 8;
+      uint32_t byte;
+      const uint32_t q = cast8(v[u], byte);
+      const uint32_t word = scale_word(byte, lane);
+      if (c < p.K) *reinterpret_cast<uint32_t*>(codes + c / 2) = q;
+      const int chunk = c / 128;
+      if ((lane & 15) == 0 && chunk < kt)
+        *reinterpret_cast<uint32_t*>(p.scales + scale_offset(b * tiles, out_row, kt, chunk)) = word;
+    }
+  }
+}
+
+template <typename T> __device__ __forceinline__ void store8(T* p, const float (&v)[8]);
+template <> __device__ __forceinline__ void store8<float>(float* p, const float (&v)[8]) {
+  __stcs(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
+  __stcs(reinterpret_cast<float4*>(p) + 1, make_float4(v[4], v[5], v[6], v[7]));
+}
+template <> __device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16* p, const float (&v)[8]) {
+  __nv_bfloat162 h[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+  __stcs(reinterpret_cast<uint4*>(p), *reinterpret_cast<uint4*>(h));
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kCastThreads)
+dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int rows, int K, long long items,
+                  int groups, T* __restrict__ dst) {
+  const int lane = threadIdx.x & 31;
+  const int kt = (int)scale_tiles_k(K);
+  const size_t tiles = ((size_t)rows + kTileRows - 1) / kTileRows;
+  for (long long w = ((long long)blockIdx.x * kCastThreads + threadIdx.x) >> 5; w < items;
+       w += (long long)gridDim.x * (kCastThreads / 32)) {
+    const int g = (int)(w % groups);
+    const long long r = w / groups;
+    const int row = (int)(r % rows);
+    const size_t b = (size_t)(r / rows);
+    uint32_t q[kCastUnroll], byte[kCastUnroll];
+#pragma unroll
+    for (int u = 0; u < kCastUnroll; ++u) {
+      const int c = (g * kCastUnroll + u) * 256 + lane * 8;
+      q[u] = 0; byte[u] = 0;
+      if (c < K) {
+        q[u] = *reinterpret_cast<const uint32_t*>(codes + (size_t)r * (K / 2) + c / 2);
+        byte[u] = scales[scale_offset(b * tiles, row, kt, c / 128) + (c / kBlock & 3)];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kCastUnroll; ++u) {
+      const int c = (g * kCastUnroll + u) * 256 + lane * 8;
+      if (c >= K) break;
+      const float s = byte[u] == 255u ? __uint_as_float(0x7fffffffu)
+                                      : __uint_as_float(byte[u] == 0u ? 0x00400000u : byte[u] << 23);
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const __half2_raw h = __nv_cvt_fp4x2_to_halfraw2((__nv_fp4x2_storage_t)(q[u] >> (8 * i)), __NV_E2M1);
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+        v[2 * i] = f.x * s;                 // exact: at most two significant bits times a power of two
+        v[2 * i + 1] = f.y * s;
+      }
+      store8<T>(dst + (size_t)r * K + c, v);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Dispatch
+// ---------------------------------------------------------------------------------------------
+// Offsets of the experts' padded segments from their counts in shared memory (one block): pad[e], and the list of
+// the expert of every tile.
+__device__ __forceinline__ void place_experts(int E, int m_tiles_max, const int* cnt, int* pad, int* __restrict__ scan,
+                                              int32_t* __restrict__ tile_expert, int32_t* __restrict__ n_tiles,
+                                              int32_t* __restrict__ pad_offsets) {
+  const int tid = threadIdx.x;               // kSortThreads >= kMaxExperts4: a thread per expert
+  const int lane = tid & 31, warp = tid >> 5;
+  int tiles = tid < E ? (cnt[tid] + kTileRows - 1) / kTileRows : 0;
+  int incl = tiles;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int up = __shfl_up_sync(kAll, incl, o);
+    if (lane >= o) incl += up;
+  }
+  if (lane == 31) scan[warp] = incl;
+  __syncthreads();
+  int before = 0;
+  for (int w = 0; w < warp; ++w) before += scan[w];
+  const int first = before + incl - tiles;
+  if (tid < E) {
+    pad[tid] = first * kTileRows;
+    if (pad_offsets != nullptr) pad_offsets[tid] = first * kTileRows;
+    for (int j = 0; j < tiles; ++j) tile_expert[first + j] = tid;
+  }
+  if (tid == E - 1) {
+    n_tiles[0] = first + tiles;
+    if (pad_offsets != nullptr) pad_offsets[E] = (first + tiles) * kTileRows;
+  }
+  __syncthreads();
+}
+
+// Stable ranks of one block's assignments inside their experts, in rounds of kSortThreads; running[e] is the rank
+// the next one gets.  Bucket E takes assignments without an expert.
+__device__ __forceinline__ void scatter_rounds(int begin, int end, int E, const int32_t* __restrict__ topk_idx,
+                                               int* running, int (*wcnt)[kMaxExperts4 + 1], const int* pad,
+                                               int32_t* __restrict__ flat2row, int32_t* __restrict__ rowmap) {
+  constexpr int NW = kSortThreads / 32;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int r0 = begin; r0 < end; r0 += kSortThreads) {
+    for (int j = threadIdx.x; j <= E; j += kSortThreads)
+#pragma unroll
+      for (int w = 0; w < NW; ++w) wcnt[w][j] = 0;
+    __syncthreads();
+    const int i = r0 + threadIdx.x;
+    int e = E;
+    if (i < end) {
+      e = topk_idx[i];
+      if ((unsigned)e >= (unsigned)E) e = E;
+    }
+    const unsigned same = __match_any_sync(kAll, e);
+    const int rank = __popc(same & ((1u << lane) - 1u));
+    if (rank == 0) wcnt[warp][e] = __popc(same);
+    __syncthreads();
+    if (i < end) {
+      int row = -1;
+      if (e < E) {
+        int before = 0;
+        for (int w = 0; w < warp; ++w) before += wcnt[w][e];
+        row = pad[e] + running[e] + before + rank;
+        rowmap[row] = i;
+      }
+      flat2row[i] = row;
+    }
+    __syncthreads();
+    for (int q = threadIdx.x; q < E; q += kSortThreads) {
+      int s = 0;
+      for (int w = 0; w < NW; ++w) s += wcnt[w][q];
+      running[q] += s;
+    }
+    __syncthreads();
+  }
+}
+
+__device__ __forceinline__ void clear_padding(int E, const int* cnt, const int* pad, int32_t* __restrict__ rowmap) {
+  for (int e = threadIdx.x; e < E; e += blockDim.x)
+    for (int r = cnt[e]; r < (cnt[e] + kTileRows - 1) / kTileRows * kTileRows; ++r) rowmap[pad[e] + r] = -1;
+}
+
+struct SortShared {
+  int wcnt[kSortThreads / 32][kMaxExperts4 + 1];
+  int cnt[kMaxExperts4 + 1], running[kMaxExperts4 + 1], pad[kMaxExperts4 + 1], scan[kSortThreads / 32];
+};
+
+// The whole dispatch of a batch of at most kSortChunk assignments in one block.
+__global__ void __launch_bounds__(kSortThreads)
+dispatch_one_kernel(const Dispatch q) {
+  __shared__ SortShared s;
+  allow_dependents();
+  if (threadIdx.x < kStatusWords) q.status[threadIdx.x] = 0;
+  for (int i = threadIdx.x; i <= kMaxExperts4; i += kSortThreads) { s.cnt[i] = 0; s.running[i] = 0; }
+  __syncthreads();
+  for (int i = threadIdx.x; i < q.R; i += kSortThreads) {
+    const int e = q.topk_idx[i];
+    if ((unsigned)e < (unsigned)q.E) atomicAdd(&s.cnt[e], 1);
+  }
+  __syncthreads();
+  place_experts(q.E, q.m_tiles_max, s.cnt, s.pad, s.scan, q.tile_expert, q.n_tiles, nullptr);
+  clear_padding(q.E, s.cnt, s.pad, q.rowmap);
+  scatter_rounds(0, q.R, q.E, q.topk_idx, s.running, s.wcnt, s.pad, q.flat2row, q.rowmap);
+}
+
+__global__ void __launch_bounds__(kSortThreads)
+dispatch_count_kernel(const Dispatch q) {
+  __shared__ int hist[kMaxExperts4];
+  allow_dependents();
+  if (blockIdx.x == 0 && threadIdx.x < kStatusWords) q.status[threadIdx.x] = 0;
+  for (int i = threadIdx.x; i < q.E; i += kSortThreads) hist[i] = 0;
+  __syncthreads();
+  const int begin = blockIdx.x * kSortChunk, end = min(q.R, begin + kSortChunk);
+  for (int i = begin + threadIdx.x; i < end; i += kSortThreads) {
+    const int e = q.topk_idx[i];
+    if ((unsigned)e < (unsigned)q.E) atomicAdd(&hist[e], 1);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < q.E; i += kSortThreads) q.block_counts[(size_t)blockIdx.x * q.E + i] = hist[i];
+}
+
+// counts per block -> the rank each block starts at, in place; segments and tiles of the experts
+__global__ void __launch_bounds__(kSortThreads)
+dispatch_scan_kernel(const Dispatch q) {
+  __shared__ int cnt[kMaxExperts4 + 1], pad[kMaxExperts4 + 1], scan[kSortThreads / 32];
+  allow_dependents();
+  grid_dependency_wait();
+  const int e = threadIdx.x;
+  if (e < q.E) {
+    int run = 0;
+    for (int b0 = 0; b0 < q.blocks; b0 += 8) {
+      int v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = b0 + i < q.blocks ? q.block_counts[(size_t)(b0 + i) * q.E + e] : 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (b0 + i < q.blocks) q.block_counts[(size_t)(b0 + i) * q.E + e] = run;
+        run += v[i];
+      }
+    }
+    cnt[e] = run;
+  }
+  __syncthreads();
+  place_experts(q.E, q.m_tiles_max, cnt, pad, scan, q.tile_expert, q.n_tiles, q.pad_offsets);
+  clear_padding(q.E, cnt, pad, q.rowmap);
+}
+
+__global__ void __launch_bounds__(kSortThreads)
+dispatch_scatter_kernel(const Dispatch q) {
+  __shared__ SortShared s;
+  allow_dependents();
+  grid_dependency_wait();
+  for (int i = threadIdx.x; i < q.E; i += kSortThreads) {
+    s.running[i] = q.block_counts[(size_t)blockIdx.x * q.E + i];
+    s.pad[i] = q.pad_offsets[i];
+  }
+  __syncthreads();
+  const int begin = blockIdx.x * kSortChunk;
+  scatter_rounds(begin, min(q.R, begin + kSortChunk), q.E, q.topk_idx, s.running, s.wcnt, s.pad, q.flat2row, q.rowmap);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kCastThreads)
+quantize_rows_kernel(const Dispatch q, const T* __restrict__ x, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
+                     long long items, int groups) {
+  const int lane = threadIdx.x & 31;
+  const int kt = (int)scale_tiles_k(q.d);
+  allow_dependents();
+  grid_dependency_wait();
+  for (long long w = ((long long)blockIdx.x * kCastThreads + threadIdx.x) >> 5; w < items;
+       w += (long long)gridDim.x * (kCastThreads / 32)) {
+    const int g = (int)(w % groups);
+    const size_t t = (size_t)(w / groups);
+    float v[kCastUnroll][8];
+#pragma unroll
+    for (int u = 0; u < kCastUnroll; ++u) {
+      const int c = (g * kCastUnroll + u) * 256 + lane * 8;
+      if (c < q.d) {
+        load8<T>(x + t * q.d + c, v[u], true);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[u][i] = 0.f;
+      }
+    }
+    uint32_t code[kCastUnroll], word[kCastUnroll];
+#pragma unroll
+    for (int u = 0; u < kCastUnroll; ++u) {
+      uint32_t byte;
+      code[u] = cast8(v[u], byte);
+      word[u] = scale_word(byte, lane);
+    }
+    for (int j = 0; j < q.k; ++j) {
+      const int row = q.flat2row[t * q.k + j];
+      if (row < 0) continue;
+#pragma unroll
+      for (int u = 0; u < kCastUnroll; ++u) {
+        const int c = (g * kCastUnroll + u) * 256 + lane * 8;
+        if (c < q.d) *reinterpret_cast<uint32_t*>(codes + (size_t)row * (q.d / 2) + c / 2) = code[u];
+        if ((lane & 15) == 0 && c / 128 < kt)
+          *reinterpret_cast<uint32_t*>(scales + scale_offset(0, row, kt, c / 128)) = word[u];
+      }
+    }
+  }
+}
+
+// A thread owns 16 bytes of y; slots and splits are added in order, in fp32, and rounded once.
+template <typename T>
+__global__ void __launch_bounds__(256)
+combine_rows_kernel(int Tn, int d, int k, int splits, const float* __restrict__ rows, const int32_t* __restrict__ flat2row,
+                    T* __restrict__ y) {
+  constexpr int VN = Vec<T>::N;
+  const int vecs = d / VN;
+  const size_t split_stride = (size_t)Tn * k * d;
+  allow_dependents();
+  grid_dependency_wait();
+  for (size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x; i < (size_t)Tn * vecs; i += (size_t)gridDim.x * blockDim.x) {
+    const size_t t = i / vecs;
+    const int c = (int)(i - t * vecs) * VN;
+    float acc[VN];
+#pragma unroll
+    for (int j = 0; j < VN; ++j) acc[j] = 0.f;
+    for (int s = 0; s < k; ++s) {
+      if (flat2row[t * k + s] < 0) continue;               // its row was never written
+      for (int sp = 0; sp < splits; ++sp) {
+        const float* r = rows + sp * split_stride + (t * k + s) * d + c;
+#pragma unroll
+        for (int j = 0; j < VN; j += 4) {
+          const float4 q = __ldcs(reinterpret_cast<const float4*>(r + j));
+          acc[j] += q.x; acc[j + 1] += q.y; acc[j + 2] += q.z; acc[j + 3] += q.w;
+        }
+      }
+    }
+    __align__(16) T out[VN];
+#pragma unroll
+    for (int j = 0; j < VN; ++j) out[j] = from_f32<T>(acc[j]);
+    *reinterpret_cast<uint4*>(y + t * d + c) = *reinterpret_cast<const uint4*>(out);
+  }
+}
+
+int cast_blocks(long long items) {
+  const long long want = (items + kCastThreads / 32 - 1) / (kCastThreads / 32), most = 8ll * sm_count();
+  return (int)(want < most ? want : most);
+}
+int cast_groups(int K) { return (K + 256 * kCastUnroll - 1) / (256 * kCastUnroll); }
+
+}  // namespace
+
+cudaError_t launch_quantize(const CastParams& p, int dtype, cudaStream_t st) {
+  const int groups = cast_groups(p.K);
+  const long long items = (long long)p.batch * p.rows * groups;
+  const int esize = dtype == BTX_BF16 ? 2 : 4;
+  const int vec = ((uintptr_t)p.src & 15) == 0 && p.row_stride * esize % 16 == 0 && p.batch_stride * esize % 16 == 0;
+  if (dtype == BTX_BF16) quantize_kernel<__nv_bfloat16><<<cast_blocks(items), kCastThreads, 0, st>>>(p, vec, items, groups);
+  else quantize_kernel<float><<<cast_blocks(items), kCastThreads, 0, st>>>(p, vec, items, groups);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_dequantize(const uint8_t* codes, const uint8_t* scales, int batch, int rows, int K, int dtype, void* dst,
+                              cudaStream_t st) {
+  const int groups = cast_groups(K);
+  const long long items = (long long)batch * rows * groups;
+  if (dtype == BTX_BF16)
+    dequantize_kernel<__nv_bfloat16><<<cast_blocks(items), kCastThreads, 0, st>>>(codes, scales, rows, K, items, groups,
+                                                                                  (__nv_bfloat16*)dst);
+  else
+    dequantize_kernel<float><<<cast_blocks(items), kCastThreads, 0, st>>>(codes, scales, rows, K, items, groups, (float*)dst);
+  return cudaGetLastError();
+}
+
+int dispatch_blocks(long long R) { return (int)((R + kSortChunk - 1) / kSortChunk); }
+
+cudaError_t launch_dispatch(const Dispatch& q, cudaStream_t st) {
+  if (q.blocks <= 1) {
+    dispatch_one_kernel<<<1, kSortThreads, 0, st>>>(q);
+    return cudaGetLastError();
+  }
+  dispatch_count_kernel<<<q.blocks, kSortThreads, 0, st>>>(q);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  if ((e = launch_after_predecessor(dispatch_scan_kernel, dim3(1), dim3(kSortThreads), 0, st, true, q)) != cudaSuccess) return e;
+  return launch_after_predecessor(dispatch_scatter_kernel, dim3(q.blocks), dim3(kSortThreads), 0, st, true, q);
+}
+
+cudaError_t launch_quantize_rows(const Dispatch& q, int dtype, const void* x, uint8_t* codes, uint8_t* scales, cudaStream_t st) {
+  const int groups = cast_groups(q.d);
+  const long long items = (long long)q.T * groups;
+  if (dtype == BTX_BF16)
+    return launch_after_predecessor(quantize_rows_kernel<__nv_bfloat16>, dim3(cast_blocks(items)), dim3(kCastThreads), 0, st, true,
+                                    q, (const __nv_bfloat16*)x, codes, scales, items, groups);
+  return launch_after_predecessor(quantize_rows_kernel<float>, dim3(cast_blocks(items)), dim3(kCastThreads), 0, st, true, q,
+                                  (const float*)x, codes, scales, items, groups);
+}
+
+cudaError_t launch_combine_rows(const Dispatch& q, int dtype, const float* rows, int splits, void* y, cudaStream_t st) {
+  const size_t n = (size_t)q.T * (q.d / (dtype == BTX_BF16 ? 8 : 4));
+  const size_t want = (n + 255) / 256, most = (size_t)sm_count() * 32;
+  const dim3 grid((unsigned)(want < most ? want : most));
+  if (dtype == BTX_BF16)
+    return launch_after_predecessor(combine_rows_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, true, q.T, q.d, q.k, splits, rows,
+                                    (const int32_t*)q.flat2row, (__nv_bfloat16*)y);
+  return launch_after_predecessor(combine_rows_kernel<float>, grid, dim3(256), 0, st, true, q.T, q.d, q.k, splits, rows,
+                                  (const int32_t*)q.flat2row, (float*)y);
+}
+
+}  // namespace mx4
+}  // namespace btx

@@ -1,0 +1,406 @@
+// Products of MXFP4 matrices on the 5th-generation tensor cores (tcgen05.mma kind::mxf4.block_scale): codes straight
+// from memory to shared memory by TMA, scales by bulk copies and tcgen05.cp into tensor memory, fp32 accumulation in
+// tensor memory; nothing is decoded on the way.  y = A B^T with both operands K-major, per output element
+//   sum over blocks of 32:  2^(sa - 127) 2^(sb - 127) sum a_i b_i.
+//
+// One persistent kernel, a CTA per SM, a 128 x BN tile at a time:
+//   warp 0      TMA producer (one lane): ring of stages of 256 contraction elements (A 128 x 128 bytes, B BN x 128
+//               bytes, swizzled; the two 512-byte scale tiles of A and of every 128 rows of B)
+//   warp 1      allocates tensor memory; one lane copies a stage's scales into the stage's own tensor-memory columns
+//               (so a copy never meets an MMA that still reads them: the stage is free only after its commit) and
+//               issues up to four MMAs of 64 contraction elements
+//   warps 2-9   epilogue: a row per thread, two warps per 32-lane quarter, each half of the columns.  Two accumulators
+//               let the epilogue of a tile overlap the main loop of the next.
+// Modes:
+//   STORE    y, fp32 or bf16
+//   GATE_UP  B rows alternate between W1 and W3, so h1 and h3 of a hidden unit are neighbouring columns of one thread:
+//            silu(h1) * h3 in fp32, cast to MXFP4 in registers (32 neighbouring units are a block)
+//   DOWN     gate-scaled fp32 rows scattered to t*k+slot
+// Every wait is bounded (tcx::mbar_wait); a wait that runs out leaves BTX_ERR_TIMEOUT in the status word.
+#include <cuda_fp4.h>
+
+#include "btx_mx4.cuh"
+#include "btx_tc_ptx.cuh"
+
+namespace btx {
+namespace mx4 {
+namespace {
+
+using namespace tcx;
+
+constexpr int SK = 256;                                  // contraction elements per stage (128 bytes of codes)
+constexpr int BM = kTileRows;
+constexpr int EPI_WARPS = 8;
+constexpr int THREADS = 64 + EPI_WARPS * 32;
+constexpr int A_BYTES = BM * SK / 2;
+constexpr int SFA_BYTES = 2 * kTileBytes;
+constexpr int GROUP_N = 8;                               // column tiles per raster group
+
+enum Mode { STORE = 0, GATE_UP = 1, DOWN = 2 };
+
+template <int BN> struct Cfg {
+  static constexpr int B_BYTES = BN * SK / 2;
+  static constexpr int SFB_BYTES = (BN / kTileRows) * 2 * kTileBytes;
+  static constexpr int STAGE_BYTES = A_BYTES + B_BYTES + SFA_BYTES + SFB_BYTES;
+  static constexpr int STAGES = 220 * 1024 / STAGE_BYTES;
+  static constexpr int SF_COLS = 8 + (BN / kTileRows) * 8;          // tensor-memory columns of a stage's scales
+  static constexpr int SMEM = STAGES * STAGE_BYTES + 1024 + 256;
+  static_assert(2 * BN + STAGES * SF_COLS <= 512, "accumulators and scales fit in tensor memory");
+  static_assert(STAGES * 16 + 48 <= 256, "barriers fit behind the ring");
+};
+
+struct Params {
+  int M, N, K;                      // STORE: rows and columns of y; grouped: N = B rows per expert
+  int m_tiles, n_tiles, batch;
+  int grouped;
+  const int32_t* n_row_tiles;       // grouped: row tiles in use (device)
+  const int32_t* tile_expert;
+  const int32_t* rowmap;
+  const uint8_t* a_scales;
+  const uint8_t* b_scales;
+  long long a_scale_batch, b_scale_batch;   // bytes from one matrix to the next
+  int kt;                           // scale tiles along K
+  const float* gates;
+  void* y;
+  uint8_t* act_codes;
+  uint8_t* act_scales;
+  int out_bf16;
+  int wide;                         // output rows start on 32-byte boundaries
+  int32_t* status;
+};
+
+// ---- PTX of the one-CTA forms ----
+__device__ __forceinline__ void load_3d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+      ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void load_bulk(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void mma_mxf4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                         uint32_t accum) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accum) : "memory");
+}
+// 32 rows of 16 bytes (a 512-byte scale tile) to four tensor-memory columns, repeated in every 32-lane quarter
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint32_t smem) {
+  // no swizzle, eight-row core matrices of 128 bytes, 128 bytes apart
+  const uint64_t desc = (uint64_t)((smem & 0x3FFFFu) >> 4) | ((uint64_t)(128 >> 4) << 16) | ((uint64_t)(128 >> 4) << 32) |
+                        (1ull << 46);
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+struct Item { int mt, nt, b, e; };
+
+// Tile number -> (row tile, column tile): groups of GROUP_N column tiles, rows advance slowest inside a group.
+__device__ __forceinline__ Item get_item(const Params& p, int m_tiles, int t) {
+  Item it;
+  const int per = m_tiles * p.n_tiles;
+  it.b = t / per;
+  const int local = t - it.b * per;
+  const int full = p.n_tiles / GROUP_N, in_full = full * m_tiles * GROUP_N;
+  int g, width, rem;
+  if (local < in_full) { g = local / (m_tiles * GROUP_N); rem = local - g * m_tiles * GROUP_N; width = GROUP_N; }
+  else { g = full; rem = local - in_full; width = p.n_tiles - full * GROUP_N; }
+  it.mt = rem / width;
+  it.nt = g * GROUP_N + rem - it.mt * width;
+  it.e = p.grouped ? p.tile_expert[it.mt] : it.b;
+  return it;
+}
+
+template <int MODE, int BN>
+__global__ void __launch_bounds__(THREADS, 1)
+mx4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const Params p) {
+  using C = Cfg<BN>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t ring = (raw + 1023u) & ~1023u;
+  uint8_t* ctl = smem_raw + (ring - raw) + C::STAGES * C::STAGE_BYTES;
+  const uint32_t bar_full = smem_u32(ctl), bar_empty = bar_full + C::STAGES * 8;
+  const uint32_t bar_tfull = bar_empty + C::STAGES * 8, bar_tempty = bar_tfull + 16;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctl + C::STAGES * 16 + 32);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(ctl + C::STAGES * 16 + 40);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < C::STAGES; ++s) { mbar_init(bar_full + s * 8, 1); mbar_init(bar_empty + s * 8, 1); }
+    for (int a = 0; a < 2; ++a) { mbar_init(bar_tfull + a * 8, 1); mbar_init(bar_tempty + a * 8, EPI_WARPS * 32); }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512));
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  allow_dependents();
+  grid_dependency_wait();
+  // a product of its own clears its status word (a wait of another CTA cannot have run out yet)
+  if (MODE == STORE && blockIdx.x == 0 && threadIdx.x < kStatusWords) p.status[threadIdx.x] = 0;
+  const int m_tiles = p.grouped ? p.n_row_tiles[0] : p.m_tiles;
+  const int n_total = m_tiles * p.n_tiles * p.batch;
+  const int kb_total = (p.K + SK - 1) / SK;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      uint32_t stage = 0, phase = 0;
+      bool ok = true;
+      for (int t = blockIdx.x; t < n_total && ok; t += gridDim.x) {
+        const Item it = get_item(p, m_tiles, t);
+        const uint8_t* sfa = p.a_scales + it.b * p.a_scale_batch + (size_t)it.mt * p.kt * kTileBytes;
+        const uint8_t* sfb = p.b_scales + it.e * p.b_scale_batch + (size_t)it.nt * (BN / kTileRows) * p.kt * kTileBytes;
+        // the last row tiles of B may lie past its end: a tile of BN = 256 columns then has one row tile of scales
+        const int b_rows = min(BN / kTileRows, (p.N + kTileRows - 1) / kTileRows - it.nt * (BN / kTileRows));
+        for (int kb = 0; kb < kb_total; ++kb) {
+          if (!(ok = mbar_wait(bar_empty + stage * 8, phase ^ 1u, abort_flag, p.status))) break;
+          const uint32_t bar = bar_full + stage * 8;
+          const uint32_t sA = ring + stage * C::STAGE_BYTES, sB = sA + A_BYTES, sSA = sB + C::B_BYTES, sSB = sSA + SFA_BYTES;
+          const uint32_t sf = (uint32_t)min(2, p.kt - 2 * kb) * kTileBytes;
+          mbar_expect_tx(bar, A_BYTES + C::B_BYTES + sf * (1 + b_rows));
+          load_3d(sA, &tmA, kb * (SK / 2), it.mt * BM, it.b, bar);
+          load_3d(sB, &tmB, kb * (SK / 2), it.nt * BN, it.e, bar);
+          load_bulk(sSA, sfa + (size_t)kb * 2 * kTileBytes, sf, bar);
+          for (int r = 0; r < b_rows; ++r)
+            load_bulk(sSB + r * 2 * kTileBytes, sfb + ((size_t)r * p.kt + kb * 2) * kTileBytes, sf, bar);
+          if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+        }
+      }
+      for (int i = 0; i < C::STAGES && ok; ++i) {         // the MMAs that read the last stages have retired
+        ok = mbar_wait(bar_empty + stage * 8, phase ^ 1u, abort_flag, p.status);
+        if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      // e2m1 x e2m1 (type code 1), UE8M0 scales, both operands K-major, M 128, N BN; scale selectors per MMA below
+      constexpr uint32_t idesc0 = (1u << 7) | (1u << 10) | ((uint32_t)(BN >> 3) << 17) | (1u << 23) | ((uint32_t)(BM >> 4) << 24);
+      uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
+      bool ok = true;
+      for (int t = blockIdx.x; t < n_total && ok; t += gridDim.x) {
+        if (!(ok = mbar_wait(bar_tempty + acc * 8, acc_phase ^ 1u, abort_flag, p.status))) break;
+        tc_fence_after();
+        const uint32_t d = tmem + acc * BN;
+        for (int kb = 0; kb < kb_total; ++kb) {
+          if (!(ok = mbar_wait(bar_full + stage * 8, phase, abort_flag, p.status))) break;
+          tc_fence_after();
+          const uint32_t sA = ring + stage * C::STAGE_BYTES, sB = sA + A_BYTES, sSA = sB + C::B_BYTES, sSB = sSA + SFA_BYTES;
+          const uint32_t tA = tmem + 2 * BN + stage * C::SF_COLS, tB = tA + 8;
+          const int k64 = min(SK / 64, (p.K - kb * SK + 63) / 64);     // MMAs that hold elements
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            if (2 * c < k64) {
+              copy_scales(tA + c * 4, sSA + c * kTileBytes);
+#pragma unroll
+              for (int r = 0; r < BN / kTileRows; ++r)
+                copy_scales(tB + (c * (BN / kTileRows) + r) * 4, sSB + (r * 2 + c) * kTileBytes);
+            }
+          }
+          const uint64_t da = smem_desc(sA, false), db = smem_desc(sB, false);
+#pragma unroll
+          for (int j = 0; j < SK / 64; ++j) {
+            if (j < k64) {
+              const uint32_t id = (uint32_t)(j & 1) * 2;                 // which half of the four scale bytes of a word
+              mma_mxf4(d, da + (uint64_t)(2 * j), db + (uint64_t)(2 * j), idesc0 | (id << 4) | (id << 29), tA + (j >> 1) * 4,
+                       tB + (j >> 1) * (BN / kTileRows) * 4, (kb > 0 || j > 0) ? 1u : 0u);
+            }
+          }
+          commit(bar_empty + stage * 8);
+          if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+        }
+        if (!ok) break;
+        commit(bar_tfull + acc * 8);
+        acc ^= 1u;
+        if (acc == 0) acc_phase ^= 1u;
+      }
+    }
+  } else {
+    const int q = warp & 3, half = (warp - 2) >> 2;
+    const int row = q * 32 + lane;
+    const bool wide = p.wide != 0;
+    constexpr int HC = BN / 2;                            // columns of this warp
+    uint32_t acc = 0, acc_phase = 0;
+    bool ok = true;
+    for (int t = blockIdx.x; t < n_total && ok; t += gridDim.x) {
+      const Item it = get_item(p, m_tiles, t);
+      const int m = it.mt * BM + row;
+      const int flat = MODE == STORE ? (m < p.M ? m : -1) : p.rowmap[m];
+      const bool any = __any_sync(0xffffffffu, flat >= 0);
+      if (!(ok = mbar_wait(bar_tfull + acc * 8, acc_phase, abort_flag, p.status))) break;
+      tc_fence_after();
+      const uint32_t taddr = tmem + acc * BN + half * HC + ((uint32_t)(q * 32) << 16);
+      const int n0 = it.nt * BN + half * HC;
+      if (any) {
+        float v[32];
+        if constexpr (MODE == STORE) {
+          for (int c = 0; c < HC; c += 32) {
+            __syncwarp();                                 // the tensor-memory load needs the whole warp
+            tc_ld32(taddr + c, v);
+            const int col = n0 + c;
+            if (flat < 0 || col >= p.N) continue;
+            const size_t o = ((size_t)it.b * p.M + flat) * p.N + col;
+            if (p.out_bf16) {
+              __nv_bfloat16* y = (__nv_bfloat16*)p.y + o;
+              if (wide && col + 32 <= p.N) {
+                st32(y, pack8(v), pack8(v + 8), true);
+                st32(y + 16, pack8(v + 16), pack8(v + 24), true);
+              } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                  if (col + i < p.N) y[i] = __float2bfloat16_rn(v[i]);
+              }
+            } else {
+              float* y = (float*)p.y + o;
+              if (wide && col + 32 <= p.N) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) st32(y + 8 * i, f4(v + 8 * i), f4(v + 8 * i + 4), true);
+              } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                  if (col + i < p.N) y[i] = v[i];
+              }
+            }
+          }
+        } else if constexpr (MODE == DOWN) {
+          const float g = flat >= 0 ? p.gates[flat] : 0.f;
+          for (int c = 0; c < HC; c += 32) {
+            __syncwarp();                                 // the tensor-memory load needs the whole warp
+            tc_ld32(taddr + c, v);
+            const int col = n0 + c;
+            if (flat < 0 || col >= p.N) continue;         // N is a multiple of 32
+            float* y = (float*)p.y + (size_t)flat * p.N + col;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] *= g;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) st32(y + 8 * i, f4(v + 8 * i), f4(v + 8 * i + 4), wide);
+          }
+        } else {
+          const int F = p.N / 2;
+          const int akt = (int)scale_tiles_k(F);
+          for (int c = 0; c < HC; c += 64) {
+            const int f0 = (n0 + c) / 2;                  // 32 hidden units: one block
+            float a[32];
+            __syncwarp();
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              tc_ld32(taddr + c + 32 * h, v);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) a[16 * h + i] = fast_swiglu(v[2 * i], v[2 * i + 1]);
+            }
+            if (flat < 0) continue;
+            uint32_t amax = 0;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) amax = max(amax, __float_as_uint(a[i]) & 0x7fffffffu);
+            float inv;
+            uint32_t byte = scale_byte(amax, inv);
+            uint32_t w[4] = {0, 0, 0, 0};
+            if (byte != 255u) {
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                w[i / 4] |= (uint32_t)__nv_cvt_float2_to_fp4x2(make_float2(a[2 * i] * inv, a[2 * i + 1] * inv), __NV_E2M1,
+                                                               cudaRoundNearest) << (8 * (i & 3));
+            }
+            // past the last unit there is no block, but the other half of an MMA's 64 elements wants a finite scale
+            if (f0 >= F) byte = 0;
+            const int blk = f0 / kBlock;
+            if (blk < 4 * akt)
+              p.act_scales[((size_t)it.mt * akt + blk / 4) * kTileBytes + (row & 31) * 16 + (row >> 5) * 4 + (blk & 3)] =
+                  (uint8_t)byte;
+            if (f0 < F)
+              *reinterpret_cast<uint4*>(p.act_codes + (size_t)m * (F / 2) + f0 / 2) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        }
+      }
+      __syncwarp();
+      tc_fence_before();
+      arrive(bar_tempty + acc * 8);
+      acc ^= 1u;
+      if (acc == 0) acc_phase ^= 1u;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
+  }
+}
+
+// codes [batch][rows][K/2] as bytes, box of 128 bytes x box_rows
+bool make_codes_map(CUtensorMap* m, const void* base, long long K, long long rows, long long batch, uint32_t box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[3] = {(cuuint64_t)K / 2, (cuuint64_t)rows, (cuuint64_t)batch};
+  cuuint64_t strides[2] = {(cuuint64_t)K / 2, (cuuint64_t)(K / 2 * rows)};
+  cuuint32_t box[3] = {SK / 2, box_rows, 1};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int MODE, int BN>
+btx_status launch(const GemmArgs& g, Params p, int max_items, cudaStream_t st) {
+  CUtensorMap a, b;
+  if (!make_codes_map(&a, g.a_codes, g.K, g.M, g.batch, BM) || !make_codes_map(&b, g.b_codes, g.K, g.N, g.experts, BN))
+    return BTX_ERR_CUDA;
+  if (cudaFuncSetAttribute(mx4_gemm_kernel<MODE, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<BN>::SMEM) != cudaSuccess)
+    return BTX_ERR_CUDA;
+  int blocks = sm_count();
+  if (blocks > max_items) blocks = max_items;
+  return launch_after_predecessor(mx4_gemm_kernel<MODE, BN>, dim3(blocks), dim3(THREADS), Cfg<BN>::SMEM, st, MODE != STORE, a, b,
+                                  p) == cudaSuccess ? BTX_OK : BTX_ERR_CUDA;
+}
+
+Params base_params(const GemmArgs& g, int bn) {
+  Params p = {};
+  p.M = g.M; p.N = g.N; p.K = g.K; p.batch = g.batch; p.status = g.status;
+  p.m_tiles = (g.M + BM - 1) / BM; p.n_tiles = (g.N + bn - 1) / bn;
+  p.kt = (int)scale_tiles_k(g.K);
+  p.a_scales = g.a_scales; p.b_scales = g.b_scales;
+  p.a_scale_batch = (long long)p.m_tiles * p.kt * kTileBytes;
+  p.b_scale_batch = (long long)((g.N + kTileRows - 1) / kTileRows) * p.kt * kTileBytes;
+  return p;
+}
+
+}  // namespace
+
+btx_status launch_matmul(const GemmArgs& g, int dtype, void* y, cudaStream_t st) {
+  constexpr int BN = 128;
+  Params p = base_params(g, BN);
+  p.y = y; p.out_bf16 = dtype == BTX_BF16;
+  p.wide = aligned32(y) && (size_t)g.N * (p.out_bf16 ? 2 : 4) % 32 == 0;
+  return launch<STORE, BN>(g, p, (int)((long long)p.m_tiles * p.n_tiles * p.batch < 1 << 20 ? p.m_tiles * p.n_tiles * p.batch : 1 << 20), st);
+}
+
+btx_status launch_gate_up(const GemmArgs& g, const Dispatch& q, uint8_t* act_codes, uint8_t* act_scales, cudaStream_t st) {
+  constexpr int BN = 128;
+  Params p = base_params(g, BN);
+  p.grouped = 1; p.n_row_tiles = q.n_tiles; p.tile_expert = q.tile_expert; p.rowmap = q.rowmap;
+  p.act_codes = act_codes; p.act_scales = act_scales;
+  return launch<GATE_UP, BN>(g, p, p.m_tiles * p.n_tiles, st);
+}
+
+btx_status launch_down(const GemmArgs& g, const Dispatch& q, const float* gates, float* rows, cudaStream_t st) {
+  constexpr int BN = 128;
+  Params p = base_params(g, BN);
+  p.grouped = 1; p.n_row_tiles = q.n_tiles; p.tile_expert = q.tile_expert; p.rowmap = q.rowmap;
+  p.gates = gates; p.y = rows; p.wide = aligned32(rows);
+  return launch<DOWN, BN>(g, p, p.m_tiles * p.n_tiles, st);
+}
+
+}  // namespace mx4
+}  // namespace btx
