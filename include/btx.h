@@ -55,8 +55,14 @@ typedef enum { BTX_F32 = 0, BTX_BF16 = 1 } btx_dtype;
  *          one expert (k = 1).  gumbel_tau = 0 is hard sampling, the paper's inference rule: expert
  *          arg-max(W_l x + G) with gate 1 and no router gradient.  Defined here without the
  *          load-balancing loss (lb_alpha must be 0); `probs` then holds the perturbed softmax.
+ *   GIVEN  the caller's routing (e.g. btx_route's): routing->topk_idx[T,k] and routing->gates[T,k] are inputs of
+ *          btx_moe_forward.  An index outside 0..E-1 is an empty slot: it adds nothing and its gate has no
+ *          gradient.  There is no router here: w_router, router_bias, dw_router and dbias may be NULL and are not used,
+ *          lb_alpha must be 0, routing->logits, probs, u, p and lb_loss are left as they were, and `dlogits` of
+ *          btx_moe_backward receives d gates [T,k].  Not valid in btx_lb_loss and btx_moe_step_host.
  * Ties between equal logits go to the lower expert index; slot 0 holds the largest logit. */
-typedef enum { BTX_ROUTE_TOPK = 0, BTX_ROUTE_SWITCH = 1, BTX_ROUTE_SOFT = 2, BTX_ROUTE_SAMPLE1 = 3 } btx_routing;
+typedef enum { BTX_ROUTE_TOPK = 0, BTX_ROUTE_SWITCH = 1, BTX_ROUTE_SOFT = 2, BTX_ROUTE_SAMPLE1 = 3,
+               BTX_ROUTE_GIVEN = 4 } btx_routing;
 
 typedef struct {
   int32_t T, d_model, d_ff, E, k;

@@ -15,7 +15,7 @@ import torch
 BTX_OK = 0
 BTX_ERR_INVALID_ARG, BTX_ERR_UNSUPPORTED, BTX_ERR_WORKSPACE, BTX_ERR_ARCH, BTX_ERR_CUDA, BTX_ERR_TIMEOUT = 1, 2, 3, 4, 5, 6
 BTX_F32, BTX_BF16 = 0, 1
-ROUTE_TOPK, ROUTE_SWITCH, ROUTE_SOFT, ROUTE_SAMPLE1 = 0, 1, 2, 3
+ROUTE_TOPK, ROUTE_SWITCH, ROUTE_SOFT, ROUTE_SAMPLE1, ROUTE_GIVEN = 0, 1, 2, 3, 4
 PARAM_AVERAGE, PARAM_FFN = 0, 1
 FFN_STACK, FFN_SPLIT, FFN_BLEND = 0, 1, 2
 SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
@@ -181,8 +181,19 @@ class Routing:
                        torch.empty((T, E), **f), torch.empty(E, **i), torch.empty(E + 1, **i), torch.empty(R, **i),
                        torch.empty(R, **i), torch.empty(E, **f), torch.empty(E, **f), torch.empty(1, **f))
 
+    @staticmethod
+    def given(desc: MoeDesc, topk_idx, gates):
+        """The caller's choice [T,k] int32 and gates [T,k] fp32 for ROUTE_GIVEN, with room for the permutation."""
+        dev, R = topk_idx.device, desc.T * desc.k
+        _check(topk_idx, "topk_idx", (desc.T, desc.k), torch.int32, dev)
+        _check(gates, "gates", (desc.T, desc.k), torch.float32, dev)
+        _ptr(topk_idx), _ptr(gates)
+        i = dict(dtype=torch.int32, device=dev)
+        return Routing(None, topk_idx, gates, None, torch.empty(desc.E, **i), torch.empty(desc.E + 1, **i),
+                       torch.empty(R, **i), torch.empty(R, **i), None, None, None)
+
     def as_struct(self) -> RoutingOut:
-        return RoutingOut(*[t.data_ptr() for t in (self.logits, self.topk_idx, self.gates, self.probs, self.counts,
+        return RoutingOut(*[None if t is None else t.data_ptr() for t in (self.logits, self.topk_idx, self.gates, self.probs, self.counts,
                                                    self.offsets, self.perm, self.inv_perm, self.u, self.p,
                                                    self.lb_loss)])
 
@@ -207,6 +218,7 @@ def btx_moe_forward(desc, x, w_router, router_bias, w1, w3, w2, y, routing, save
 
 def btx_moe_backward(desc, x, w_router, router_bias, w1, w3, w2, dy, lb_grad_scale, saved, dx, dw_router, dbias,
                      dw1, dw3, dw2, accumulate, workspace, router_noise=None, dlogits=None):
+    """With ROUTE_GIVEN w_router, dw_router and dbias are None and dlogits receives d gates [T,k]."""
     with _on(x.device):
         s = lib().btx_moe_backward(C.byref(desc), _ptr(x), _ptr(w_router), _ptr(router_bias), _ptr(router_noise),
                                    _ptr(w1), _ptr(w3), _ptr(w2),

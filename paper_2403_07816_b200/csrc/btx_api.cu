@@ -16,11 +16,12 @@ btx_status make_plan(const btx_moe_desc* desc, Plan* pl, bool routing_only) {
   if (desc->T < 1 || desc->E < 1) return BTX_ERR_INVALID_ARG;
   if (!routing_only && (desc->d_model < 1 || desc->d_ff < 1)) return BTX_ERR_INVALID_ARG;
   if (desc->dtype != BTX_F32 && desc->dtype != BTX_BF16) return BTX_ERR_INVALID_ARG;
-  if (desc->routing < BTX_ROUTE_TOPK || desc->routing > BTX_ROUTE_SAMPLE1) return BTX_ERR_INVALID_ARG;
+  if (desc->routing < BTX_ROUTE_TOPK || desc->routing > BTX_ROUTE_GIVEN) return BTX_ERR_INVALID_ARG;
   int k = desc->routing == BTX_ROUTE_SOFT ? desc->E : desc->k;
   if (k < 1 || k > desc->E) return BTX_ERR_INVALID_ARG;
   if ((desc->routing == BTX_ROUTE_SWITCH || desc->routing == BTX_ROUTE_SAMPLE1) && k != 1) return BTX_ERR_INVALID_ARG;
   if (desc->routing == BTX_ROUTE_SAMPLE1 && (desc->gumbel_tau < 0.f || desc->lb_alpha != 0.f)) return BTX_ERR_UNSUPPORTED;
+  if (desc->routing == BTX_ROUTE_GIVEN && desc->lb_alpha != 0.f) return BTX_ERR_UNSUPPORTED;
   if (!(desc->capacity_factor >= 0.f)) return BTX_ERR_INVALID_ARG;
   if (desc->capacity_factor > 0.f && desc->routing == BTX_ROUTE_SOFT) return BTX_ERR_INVALID_ARG;
   if (desc->E > kMaxExperts) return BTX_ERR_UNSUPPORTED;
@@ -36,10 +37,12 @@ btx_status make_plan(const btx_moe_desc* desc, Plan* pl, bool routing_only) {
   p.esize = desc->dtype == BTX_BF16 ? 2 : 4;
   p.capped = desc->capacity_factor > 0.f;
   p.capacity = p.R;
+  p.given = desc->routing == BTX_ROUTE_GIVEN;
   if (p.capped) {     // ceil(CF * T * k / E) in double; never more than the R assignments there are
     const double c = ceil((double)desc->capacity_factor * (double)p.R / (double)p.E);
     if (c < (double)p.R) p.capacity = (int)c;
   }
+  if (p.given) p.capped = 1;                                // slots may be empty
   p.r_pad_max = (int)align_up((size_t)p.R + (size_t)p.E * (kRowTile - 1), kRowTile);
   p.mt_max = p.r_pad_max / kRowTile;
   p.nt_dact = desc->dtype == BTX_BF16 ? 2 * ((p.F + 255) / 256) : (p.F + 63) / 64;   // row-dot partials per row
@@ -56,7 +59,7 @@ btx_status make_plan(const btx_moe_desc* desc, Plan* pl, bool routing_only) {
     const int chunks = p.E < p.R ? p.E : p.R;             // typical: every expert holds one token chunk
     p.dec_s1 = pick_decode_splits(2 * chunks * ((p.F + 255) / 256), (p.d + 63) / 64);
     p.dec_s2 = pick_decode_splits(chunks * ((p.d + 255) / 256), (p.F + 63) / 64);
-    p.dense = dense_small_fits(p, desc->save_for_backward) ? 1 : 0;
+    p.dense = !p.given && dense_small_fits(p, desc->save_for_backward) ? 1 : 0;
     p.dense_n = (p.T + 15) & ~15;
   }
 
@@ -226,7 +229,8 @@ extern "C" btx_status btx_moe_forward(const btx_moe_desc* desc, const void* x, c
   Plan pl;
   btx_status s = make_plan(desc, &pl, false);
   if (s != BTX_OK) return s;
-  if (!x || !w_router || !w1 || !w3 || !w2 || !y || !workspace) return BTX_ERR_INVALID_ARG;
+  if (!x || (!w_router && !pl.given) || !w1 || !w3 || !w2 || !y || !workspace) return BTX_ERR_INVALID_ARG;
+  if (pl.given && (!routing || !routing->topk_idx || !routing->gates)) return BTX_ERR_INVALID_ARG;
   if (desc->save_for_backward && !saved) return BTX_ERR_INVALID_ARG;
   if (desc->routing == BTX_ROUTE_SAMPLE1 && !router_noise) return BTX_ERR_INVALID_ARG;
   const EffectiveRouting er = effective_routing(desc);
@@ -258,9 +262,12 @@ extern "C" btx_status btx_moe_forward(const btx_moe_desc* desc, const void* x, c
     const float* expert_rows = b.yp;
     int splits = 1;
     BTX_CUDA_OK(cudaMemsetAsync(b.status, 0, kStatusWords * 4, st));
-    if (!route_permute_small_fits(pl) && pl.capacity < pl.R)       // the tail of perm past the kept rows reads -1
+    if (pl.given || (!route_permute_small_fits(pl) && pl.capacity < pl.R))   // the tail of perm past the kept rows reads -1
       BTX_CUDA_OK(cudaMemsetAsync(b.perm, 0xFF, (size_t)pl.R * sizeof(int32_t), st));
-    if (route_permute_small_fits(pl)) {
+    if (pl.given) {
+      BTX_CUDA_OK(launch_given_routing(pl, routing->topk_idx, routing->gates, b, st));
+      BTX_CUDA_OK(launch_permute(pl, b, st));
+    } else if (route_permute_small_fits(pl)) {
       BTX_CUDA_OK(launch_route_permute_small(pl, desc->dtype, er.routing, desc->lb_alpha, x, w_router, router_bias, noise,
                                              er.inv_tau, b, st));
     } else {
@@ -288,17 +295,19 @@ extern "C" btx_status btx_moe_forward(const btx_moe_desc* desc, const void* x, c
     auto out = [&](void* dst, const void* src, size_t bytes) -> cudaError_t {
       return dst ? cudaMemcpyAsync(dst, src, bytes, cudaMemcpyDeviceToDevice, st) : cudaSuccess;
     };
-    BTX_CUDA_OK(out(routing->logits, b.logits, (size_t)pl.T * pl.E * 4));
-    BTX_CUDA_OK(out(routing->probs, b.probs, (size_t)pl.T * pl.E * 4));
-    BTX_CUDA_OK(out(routing->topk_idx, b.topk, (size_t)pl.R * 4));
-    BTX_CUDA_OK(out(routing->gates, b.gates, (size_t)pl.R * 4));
+    if (!pl.given) {
+      BTX_CUDA_OK(out(routing->logits, b.logits, (size_t)pl.T * pl.E * 4));
+      BTX_CUDA_OK(out(routing->probs, b.probs, (size_t)pl.T * pl.E * 4));
+      BTX_CUDA_OK(out(routing->topk_idx, b.topk, (size_t)pl.R * 4));
+      BTX_CUDA_OK(out(routing->gates, b.gates, (size_t)pl.R * 4));
+      BTX_CUDA_OK(out(routing->u, b.u, pl.E * 4));
+      BTX_CUDA_OK(out(routing->p, b.p, pl.E * 4));
+      BTX_CUDA_OK(out(routing->lb_loss, b.loss, 4));
+    }
     BTX_CUDA_OK(out(routing->counts, b.counts, pl.E * 4));
     BTX_CUDA_OK(out(routing->offsets, b.offsets, (pl.E + 1) * 4));
     BTX_CUDA_OK(out(routing->perm, b.perm, (size_t)pl.R * 4));
     BTX_CUDA_OK(out(routing->inv_perm, b.inv_perm, (size_t)pl.R * 4));
-    BTX_CUDA_OK(out(routing->u, b.u, pl.E * 4));
-    BTX_CUDA_OK(out(routing->p, b.p, pl.E * 4));
-    BTX_CUDA_OK(out(routing->lb_loss, b.loss, 4));
   }
   return BTX_OK;
 }
@@ -316,8 +325,8 @@ extern "C" btx_status btx_moe_backward(const btx_moe_desc* desc, const void* x, 
   btx_status s = make_plan(desc, &pl, false);
   if (s != BTX_OK) return s;
   const int skip_wgrad = desc->skip_wgrad != 0;
-  if (!x || !w_router || !w1 || !w3 || !w2 || !dy || !saved || !dx || !dw_router || !workspace)
-    return BTX_ERR_INVALID_ARG;
+  if (!x || !w1 || !w3 || !w2 || !dy || !saved || !dx || !workspace) return BTX_ERR_INVALID_ARG;
+  if (!pl.given && (!w_router || !dw_router)) return BTX_ERR_INVALID_ARG;
   if (!skip_wgrad && (!dw1 || !dw3 || !dw2)) return BTX_ERR_INVALID_ARG;
   if (misaligned(x) || misaligned(w_router) || misaligned(w1) || misaligned(w3) || misaligned(w2) ||
       misaligned(dy) || misaligned(saved) || misaligned(dx) || misaligned(dw_router) || misaligned(dlogits) ||
@@ -350,9 +359,12 @@ extern "C" btx_status btx_moe_backward(const btx_moe_desc* desc, const void* x, 
   const EffectiveRouting er = effective_routing(desc);
   cudaStream_t rst = side != nullptr ? side : st;
   if (side != nullptr) BTX_CUDA_OK(cudaStreamWaitEvent(side, after_dx, 0));
-  BTX_CUDA_OK(launch_router_backward(pl, desc->dtype, er.routing, desc->lb_alpha, lb_grad_scale,
-                                     desc->lb_stopgrad_u, 1, x, w_router, b, dx, dw_router, dbias, dlogits,
-                                     accumulate, er.inv_tau, desc->routing == BTX_ROUTE_SAMPLE1, rst));
+  if (pl.given)
+    BTX_CUDA_OK(launch_given_backward(pl, desc->dtype, b, dx, dlogits, rst));
+  else
+    BTX_CUDA_OK(launch_router_backward(pl, desc->dtype, er.routing, desc->lb_alpha, lb_grad_scale,
+                                       desc->lb_stopgrad_u, 1, x, w_router, b, dx, dw_router, dbias, dlogits,
+                                       accumulate, er.inv_tau, desc->routing == BTX_ROUTE_SAMPLE1, rst));
   if (side != nullptr) {
     BTX_CUDA_OK(cudaEventRecord(evs.e[1], side));
     BTX_CUDA_OK(cudaStreamWaitEvent(st, evs.e[1], 0));
@@ -374,6 +386,7 @@ extern "C" btx_status btx_moe_step_host(const btx_moe_desc* desc, const void* x_
   if (!x_host || !dy_host || !y_host || !dx_host || !loss_host || !x_dev || !dy_dev || !y_dev || !dx_dev || !saved)
     return BTX_ERR_INVALID_ARG;
   if (!desc->save_for_backward) return BTX_ERR_INVALID_ARG;
+  if (pl.given) return BTX_ERR_UNSUPPORTED;
   cudaStream_t st = (cudaStream_t)stream;
   cudaStream_t cs = (cudaStream_t)copy_stream;
   const bool overlap = copy_stream != nullptr && copy_stream != stream;
@@ -440,7 +453,7 @@ static btx_status lb_loss_validate(const btx_moe_desc* desc, const float* logits
                                    Plan* pl) {
   btx_status s = make_plan(desc, pl, true);
   if (s != BTX_OK) return s;
-  if (desc->routing == BTX_ROUTE_SAMPLE1) return BTX_ERR_UNSUPPORTED;
+  if (desc->routing == BTX_ROUTE_SAMPLE1 || desc->routing == BTX_ROUTE_GIVEN) return BTX_ERR_UNSUPPORTED;
   if (!logits || !loss || !u || !p) return BTX_ERR_INVALID_ARG;
   return BTX_OK;
 }

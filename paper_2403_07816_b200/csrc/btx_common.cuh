@@ -34,7 +34,8 @@ struct Plan {
   int dense;                         // a handful of tokens, nothing kept for backward: every expert meets all tokens
   int dense_n;                       // MMA N of that path: T rounded up to a multiple of 16
   int capacity;                      // rows one expert accepts (R when there is no limit)
-  int capped;                        // a capacity limit is set: assignments may be dropped
+  int capped;                        // assignments may be without a row: a capacity limit, or empty slots of a given routing
+  int given;                         // the caller's routing (BTX_ROUTE_GIVEN)
   // saved
   size_t s_topk, s_gates, s_probs, s_logits, s_u, s_p, s_up64, s_loss, s_counts, s_offsets, s_pad_offsets,
       s_tile_expert, s_rowmap, s_flat2row, s_perm, s_inv_perm, s_xs, s_h1, s_h3, saved_bytes;
@@ -83,6 +84,10 @@ cudaError_t launch_router(const Plan& pl, int dtype, int routing, float alpha, c
                           const Buffers& b, cudaStream_t st);
 cudaError_t launch_permute(const Plan& pl, const Buffers& b, cudaStream_t st);
 cudaError_t launch_wait_expiry_selftest(int32_t* status, cudaStream_t st);
+// BTX_ROUTE_GIVEN: the caller's choice and gates into `b` (a slot without an expert: -1, gate 0), and in the backward
+// d gates (when wanted) and dx from the expert rows.
+cudaError_t launch_given_routing(const Plan& pl, const int32_t* topk_idx, const float* gates, const Buffers& b, cudaStream_t st);
+cudaError_t launch_given_backward(const Plan& pl, int dtype, const Buffers& b, void* dx, float* dgates, cudaStream_t st);
 // Router + loss + permutation in one single-block launch, for batches with T*k <= 1024.
 bool route_permute_small_fits(const Plan& pl);
 cudaError_t launch_route_permute_small(const Plan& pl, int dtype, int routing, float alpha, const void* x,

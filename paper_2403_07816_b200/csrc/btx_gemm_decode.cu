@@ -297,8 +297,10 @@ btx_status launch_expert_forward_small_bf16(const Plan& pl, const void* w1, cons
   SwapParams p = {};
   p.E = pl.E; p.pad_offsets = b.pad_offsets; p.tile_expert = b.tile_expert; p.rowmap = b.rowmap; p.status = b.status;
   p.counts = b.counts;
-  // a chunk holds at most min(T, 256) tokens (a token meets an expert once): each CTA loads half of them
-  const int n_max = ((pl.T < CH ? pl.T : CH) + 15) & ~15;
+  // a chunk holds at most min(T, 256) tokens (a token meets an expert once, except that a given routing may name an
+  // expert in several of its slots): each CTA loads half of them
+  const int rows_max = pl.given ? pl.R : pl.T;
+  const int n_max = ((rows_max < CH ? rows_max : CH) + 15) & ~15;
   p.box_rows = n_max / 2 <= 32 ? 32 : (n_max / 2 <= 64 ? 64 : 128);
   p.stages = D_RING_BYTES / (DA_BYTES + p.box_rows * BK * 2);
   if (p.stages > D_MAX_STAGES) p.stages = D_MAX_STAGES;

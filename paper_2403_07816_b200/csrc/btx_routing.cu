@@ -318,7 +318,10 @@ perm_count_kernel(int R, int E, int nblocks, const int32_t* __restrict__ topk, i
   grid_dependency_wait();
   int base = blockIdx.x * kPermChunk;
   int end = min(R, base + kPermChunk);
-  for (int i = base + threadIdx.x; i < end; i += kPermThreads) atomicAdd(&hist[topk[i]], 1);
+  for (int i = base + threadIdx.x; i < end; i += kPermThreads) {
+    const int e = topk[i];
+    if (e >= 0) atomicAdd(&hist[e], 1);              // -1: an empty slot of a given routing
+  }
   __syncthreads();
   if (threadIdx.x < E) perm_counts[threadIdx.x * nblocks + blockIdx.x] = hist[threadIdx.x];
 }
@@ -392,7 +395,8 @@ perm_scatter_kernel(int R, int E, int nblocks, int cap, int r_pad_max, const int
     for (int j = threadIdx.x; j < NW * (kMaxExperts + 1); j += kPermThreads) (&wcnt[0][0])[j] = 0;
     __syncthreads();
     int i = r0 + threadIdx.x;
-    int e = (i < end) ? topk[i] : E;                 // E = dummy bucket for idle lanes
+    int e = (i < end) ? topk[i] : E;                 // E = dummy bucket for idle lanes and empty slots
+    if (e < 0) e = E;
     unsigned same = __match_any_sync(0xffffffffu, e);
     int rank = __popc(same & ((1u << lane) - 1u));
     if (rank == 0) wcnt[warp][e] = __popc(same);
@@ -400,15 +404,15 @@ perm_scatter_kernel(int R, int E, int nblocks, int cap, int r_pad_max, const int
     if (i < end) {
       int before = 0;
       for (int w = 0; w < warp; ++w) before += wcnt[w][e];
-      int within = running[e] + before + rank;       // stable rank inside the expert
-      if (within < cap) {
+      int within = (e < E ? running[e] : 0) + before + rank;         // stable rank inside the expert
+      if (e < E && within < cap) {
         int r = offsets[e] + within;                 // tight sorted row
         int rp = pad_offsets[e] + within;            // padded sorted row
         perm[r] = i;
         inv_perm[i] = r;
         rowmap[rp] = i;
         flat2row[i] = rp;
-      } else {                                       // beyond the expert's capacity: dropped
+      } else {                                       // beyond the expert's capacity, or no expert: dropped
         inv_perm[i] = -1;
         flat2row[i] = -1;
       }
@@ -420,6 +424,19 @@ perm_scatter_kernel(int R, int E, int nblocks, int cap, int r_pad_max, const int
       running[threadIdx.x] += s;
     }
     __syncthreads();
+  }
+}
+
+// Routing handed in by the caller: indexes outside 0..E-1 become -1 with gate 0.
+__global__ void __launch_bounds__(256)
+given_routing_kernel(int R, int E, const int32_t* __restrict__ topk_in, const float* __restrict__ gates_in,
+                     int32_t* __restrict__ topk, float* __restrict__ gates) {
+  allow_dependents();
+  for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < R; i += gridDim.x * blockDim.x) {
+    const int e = topk_in[i];
+    const bool ok = (unsigned)e < (unsigned)E;
+    topk[i] = ok ? e : -1;
+    gates[i] = ok ? gates_in[i] : 0.f;
   }
 }
 
@@ -591,6 +608,15 @@ dg_rowsum_kernel(int nt, int r_pad_max, int E, const int32_t* __restrict__ pad_o
 #pragma unroll 8
   for (int n = 0; n < nt; ++n) a += dg_part[(size_t)n * r_pad_max + rp];
   dg_part[rp] = a;
+}
+
+// d gate of every assignment of a given routing: the summed row-dot of its row, 0 without one.
+__global__ void __launch_bounds__(256)
+given_dgates_kernel(int R, const int32_t* __restrict__ flat2row, const float* __restrict__ dg_rows, float* __restrict__ dgates) {
+  for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < R; i += gridDim.x * blockDim.x) {
+    const int row = flat2row[i];
+    dgates[i] = row >= 0 ? dg_rows[row] : 0.f;
+  }
 }
 
 // One thread per token: d gate of every slot (the summed row-dot of its row plus the u-term of L_LB),
@@ -848,6 +874,28 @@ cudaError_t launch_router_backward(const Plan& pl, int dtype, int routing, float
   }
   router_dw_reduce_kernel<<<(pl.E * pl.d + 255) / 256, 256, 0, st>>>(pl.d, pl.E, pl.wr_chunks, b.dwr_part, bias_part,
                                                                      dw_router, dbias, accumulate);
+  return cudaGetLastError();
+}
+
+static int flat_blocks(int R) { return min((R + 255) / 256, sm_count() * 8); }
+
+cudaError_t launch_given_routing(const Plan& pl, const int32_t* topk_idx, const float* gates, const Buffers& b, cudaStream_t st) {
+  given_routing_kernel<<<flat_blocks(pl.R), 256, 0, st>>>(pl.R, pl.E, topk_idx, gates, b.topk, b.gates);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_given_backward(const Plan& pl, int dtype, const Buffers& b, void* dx, float* dgates, cudaStream_t st) {
+  if (dgates != nullptr) {
+    dg_rowsum_kernel<<<(pl.r_pad_max + 255) / 256, 256, 0, st>>>(pl.nt_dact, pl.r_pad_max, pl.E, b.pad_offsets, b.dg_part);
+    given_dgates_kernel<<<flat_blocks(pl.R), 256, 0, st>>>(pl.R, b.flat2row, b.dg_part, dgates);
+  }
+  const size_t n = (size_t)pl.T * (pl.d / (dtype == BTX_BF16 ? 8 : 4));
+  const int blocks = (int)min((n + 255) / 256, (size_t)sm_count() * 32);
+  if (dtype == BTX_BF16)
+    combine_kernel<__nv_bfloat16><<<blocks, 256, 0, st>>>(pl.T, pl.d, pl.k, pl.E, 1, b.dxp, nullptr, nullptr, b.flat2row,
+                                                          (__nv_bfloat16*)dx);
+  else
+    combine_kernel<float><<<blocks, 256, 0, st>>>(pl.T, pl.d, pl.k, pl.E, 1, b.dxp, nullptr, nullptr, b.flat2row, (float*)dx);
   return cudaGetLastError();
 }
 

@@ -84,3 +84,56 @@ def test_statement_route_properties():
     b[7] = 5.0
     i2, w2, s2, _ = o.route(z, 3, o.SIGMOID, b, renorm=False)
     assert (i2[:, 0] == 7).all() and np.allclose(w2[:, 0], s2[:, 7])
+
+
+def test_mx4_and_given_refusals(L):
+    sz = C.c_size_t(0)
+    assert L.btx_mx4_sizes(1, 8, 48, C.byref(sz), None) == 2                     # K not a multiple of 32
+    assert L.btx_mx4_sizes(-1, 8, 64, C.byref(sz), None) == 1
+    assert L.btx_mx4_sizes(2, 130, 160, None, C.byref(sz)) == 0 and sz.value == 2 * 2 * 2 * 512
+    q = lambda *a: L.btx_mx4_quantize(*a, None)
+    assert q(0, A, 64, 512, 1, 8, 64, 8, 1, 1, A, A) == 1                         # last row outside
+    assert q(0, A, 64, 512, 1, 8, 64, 8, 0, 0, A, A) == 1
+    assert q(2, A, 64, 512, 1, 8, 64, 8, 0, 1, A, A) == 1
+    assert q(0, C.c_void_p(4098), 64, 512, 1, 8, 64, 8, 0, 1, A, A) == 1
+    assert q(0, A, 64, 512, 1, 8, 64, 8, 0, 1, C.c_void_p(4104), A) == 1
+    assert q(0, None, 64, 512, 1, 0, 64, 0, 0, 1, None, None) == 0                # no rows: nothing to do
+    mm = lambda *a: L.btx_mx4_matmul(*a, None)
+    assert mm(0, 1, 8, 8, 48, A, A, A, A, A, A, 256) == 2
+    assert mm(0, 1, 8, 0, 64, A, A, A, A, A, A, 256) == 1
+    assert mm(0, 1, 8, 8, 64, A, A, A, A, A, A, 64) == 3
+    assert mm(0, 1, 8, 8, 64, A, None, A, A, A, A, 256) == 1
+    assert mm(0, 1, 1 << 30, 1 << 30, 64, A, A, A, A, A, A, 256) == 2
+    assert mm(0, 1, 0, 8, 64, None, None, None, None, None, None, 0) == 0
+    for bad, status in [(B.make_mx4_moe_desc(4, 64, 96, 4, 5, torch.float32), 1), (B.make_mx4_moe_desc(4, 48, 96, 4, 2, torch.float32), 2),
+                        (B.make_mx4_moe_desc(4, 64, 80, 4, 2, torch.float32), 2), (B.make_mx4_moe_desc(4, 64, 96, 513, 2, torch.float32), 2),
+                        (B.make_mx4_moe_desc(-1, 64, 96, 4, 2, torch.float32), 1), (B.make_mx4_moe_desc(4, 64, 96, 4, 2, 9), 1)]:
+        assert L.btx_mx4_moe_workspace_size(C.byref(bad), C.byref(sz)) == status
+        assert L.btx_mx4_moe_forward(C.byref(bad), A, A, A, A, A, A, A, A, A, 1 << 40, None) == status
+    ok = B.make_mx4_moe_desc(4, 64, 96, 4, 2, torch.float32)
+    assert L.btx_mx4_moe_forward(C.byref(ok), A, A, A, A, A, A, A, A, A, 16, None) == 3
+    assert L.btx_mx4_moe_forward(C.byref(ok), A, None, A, A, A, A, A, A, A, 1 << 40, None) == 1
+    # the caller's routing in the training layer
+    mk = lambda alpha: B.make_desc(8, 64, 64, 4, 2, torch.float32, B.ROUTE_GIVEN, alpha, save_for_backward=True)
+    with pytest.raises(B.BtxError) as ei:
+        B.btx_moe_sizes(mk(0.01))                                                # no router, no loss
+    assert ei.value.status == 2
+    d = mk(0.0)
+    assert L.btx_moe_forward(C.byref(d), A, None, None, None, A, A, A, A, None, A, A, 1 << 40, None) == 1
+    r = B.RoutingOut(topk_idx=4096)
+    assert L.btx_moe_forward(C.byref(d), A, None, None, None, A, A, A, A, C.byref(r), A, A, 1 << 40, None) == 1   # no gates
+    assert L.btx_lb_loss(C.byref(d), A, None, A, A, A, None, A, 1 << 40, None) == 2
+    assert L.btx_moe_step_host(C.byref(d), *([A] * 15), 1.0, *([A] * 5), 0, A, A, 1 << 40, None, None) == 2
+
+
+def test_statement_mx4_against_the_format():
+    """The statement's cast: nearest value of the grid, ties to the even code, saturation, scale of the block."""
+    x = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.9] + [0.0] * 24)
+    assert o.mx4_round(x)[:8].tolist() == [0.0, 1.0, 1.0, 2.0, 2.0, 4.0, 4.0, 6.0]
+    r = np.random.default_rng(0).normal(size=(4, 64))
+    v = o.mx4_round(r)
+    assert np.array_equal(o.mx4_round(v * 1.0), v) or np.abs(v - r).max() < np.abs(r).max() / 3
+    c, s = o.mx4_quantize(r)
+    assert np.array_equal(o.mx4_values(c, s), v)
+    t = o.mx4_tile_scales(s)
+    assert t.shape == (1, 1, 512) and t[0, 0, 3 * 16 + 1] == s[3, 1]
