@@ -187,7 +187,7 @@ class Routing:
         dev, R = topk_idx.device, desc.T * desc.k
         _check(topk_idx, "topk_idx", (desc.T, desc.k), torch.int32, dev)
         _check(gates, "gates", (desc.T, desc.k), torch.float32, dev)
-        _ptr(topk_idx), _ptr(gates)
+        _addr(topk_idx), _addr(gates)
         i = dict(dtype=torch.int32, device=dev)
         return Routing(None, topk_idx, gates, None, torch.empty(desc.E, **i), torch.empty(desc.E + 1, **i),
                        torch.empty(R, **i), torch.empty(R, **i), None, None, None)
@@ -359,17 +359,39 @@ def _check(t, name, shape, dtype, device, optional=False):
         if optional:
             return
         raise ValueError(f"btx: {name} is missing")
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device:
+    if t.shape != shape or t.dtype is not dtype or t.device != device:
         raise ValueError(f"btx: {name} must be {tuple(shape)} {dtype} on {device}, not {tuple(t.shape)} {t.dtype} on {t.device}")
+
+
+def _addr(t):
+    """Address of a contiguous tensor whose device has been checked (None: absent)."""
+    if t is None:
+        return None
+    if not t.is_contiguous():
+        raise RuntimeError("btx: tensors must be contiguous")
+    return t.data_ptr()
 
 
 def _rows(t, name):
     """Address and row stride of a matrix whose rows are contiguous (any row stride)."""
-    if not t.is_cuda:
-        raise RuntimeError("btx: tensors must live on a CUDA device (there is no CPU path)")
     if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
         raise RuntimeError(f"btx: the rows of {name} must be contiguous and must not overlap")
-    return C.c_void_p(t.data_ptr()), max(t.stride(0), t.shape[1])
+    return t.data_ptr(), max(t.stride(0), t.shape[1])
+
+
+def _launch(name, device, *args):
+    """Calls a library function that takes the current stream last, with the tensors' device current.  The usual case,
+    in which it is, costs no context switch: these calls run for a few microseconds on the device."""
+    if device.type != "cuda":
+        raise RuntimeError("btx: tensors must live on a CUDA device (there is no CPU path)")
+    fn = getattr(_lib or lib(), name)
+    if torch._C._cuda_getDevice() == device.index:
+        s = fn(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    else:
+        with torch.cuda.device(device):
+            s = fn(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    if s != BTX_OK:
+        raise BtxError(s, name)
 
 
 def make_route_desc(T, E, k, dtype, score=SCORE_SOFTMAX, n_group=1, topk_group=1, group_score=GROUP_MAX, renorm=True,
@@ -391,11 +413,8 @@ def btx_route(desc, logits, bias, topk_idx, gates, scores=None, counts=None, row
         row_valid = row_valid.view(torch.uint8)
     _check(row_valid, "row_valid", (T,), torch.uint8, dev, True)
     rows, stride = _rows(logits, "logits")
-    with _on(dev):
-        s = lib().btx_route(C.byref(desc), rows, stride, _ptr(bias), _ptr(row_valid), _ptr(topk_idx), _ptr(gates),
-                            _ptr(scores), _ptr(counts), _stream(dev))
-    if s != BTX_OK:
-        raise BtxError(s, "btx_route")
+    _launch("btx_route", dev, C.byref(desc), rows, stride, _addr(bias), _addr(row_valid), _addr(topk_idx), _addr(gates),
+            _addr(scores), _addr(counts))
 
 
 def btx_route_backward(desc, logits, topk_idx, dgates, dlogits):
@@ -408,11 +427,7 @@ def btx_route_backward(desc, logits, topk_idx, dgates, dlogits):
     _check(dlogits, "dlogits", (T, E), dt, dev)
     rows, stride = _rows(logits, "logits")
     out, out_stride = _rows(dlogits, "dlogits")
-    with _on(dev):
-        s = lib().btx_route_backward(C.byref(desc), rows, stride, _ptr(topk_idx), _ptr(dgates), out, out_stride,
-                                     _stream(dev))
-    if s != BTX_OK:
-        raise BtxError(s, "btx_route_backward")
+    _launch("btx_route_backward", dev, C.byref(desc), rows, stride, _addr(topk_idx), _addr(dgates), out, out_stride)
 
 
 @dataclass
@@ -437,7 +452,13 @@ def _mx4_ptrs(q, name, shape, device):
     batch, rows, K = shape
     _check(q.codes, name + ".codes", (batch, rows, K // 2), torch.uint8, device)
     _check(q.scales, name + ".scales", (batch, (rows + 127) // 128, (K + 127) // 128, 512), torch.uint8, device)
-    return _ptr(q.codes), _ptr(q.scales)
+    return _addr(q.codes), _addr(q.scales)
+
+
+def _workspace(ws, device):
+    if ws.device != device or ws.dtype is not torch.uint8:
+        raise ValueError(f"btx: workspace must be a uint8 tensor on {device}")
+    return _addr(ws), ws.numel()
 
 
 def btx_mx4_sizes(batch, rows, K):
@@ -452,8 +473,6 @@ def btx_mx4_sizes(batch, rows, K):
 def btx_mx4_quantize(src, out, row_first=0, row_step=1):
     """src [batch, rows, K] or [rows, K] (contiguous rows, any row and batch stride) cast into the Mx4 `out`; row r
     becomes row row_first + r * row_step."""
-    if not src.is_cuda:
-        raise RuntimeError("btx: tensors must live on a CUDA device (there is no CPU path)")
     v = src if src.dim() == 3 else src.unsqueeze(0)
     batch, rows, K = v.shape
     if K > 1 and v.stride(2) != 1:
@@ -462,11 +481,8 @@ def btx_mx4_quantize(src, out, row_first=0, row_step=1):
     if ob != batch or oK != K:
         raise ValueError(f"btx: src is {tuple(v.shape)}, out is {out.shape}")
     codes, scales = _mx4_ptrs(out, "out", out.shape, src.device)
-    with _on(src.device):
-        s = lib().btx_mx4_quantize(_dtype_code(src.dtype), C.c_void_p(src.data_ptr()), v.stride(1), v.stride(0), batch, rows, K,
-                                   orows, row_first, row_step, codes, scales, _stream(src.device))
-    if s != BTX_OK:
-        raise BtxError(s, "btx_mx4_quantize")
+    _launch("btx_mx4_quantize", src.device, _dtype_code(src.dtype), src.data_ptr(), v.stride(1), v.stride(0), batch, rows, K,
+            orows, row_first, row_step, codes, scales)
 
 
 def btx_mx4_dequantize(q, dst):
@@ -475,10 +491,7 @@ def btx_mx4_dequantize(q, dst):
     if dst.numel() != batch * rows * K or dst.shape[-1] != K:
         raise ValueError(f"btx: dst is {tuple(dst.shape)}, q is {q.shape}")
     codes, scales = _mx4_ptrs(q, "q", q.shape, dst.device)
-    with _on(dst.device):
-        s = lib().btx_mx4_dequantize(_dtype_code(dst.dtype), codes, scales, batch, rows, K, _ptr(dst), _stream(dst.device))
-    if s != BTX_OK:
-        raise BtxError(s, "btx_mx4_dequantize")
+    _launch("btx_mx4_dequantize", dst.device, _dtype_code(dst.dtype), codes, scales, batch, rows, K, _addr(dst))
 
 
 def btx_mx4_matmul_workspace_size(M, N, K, dtype, batch=1):
@@ -499,11 +512,8 @@ def btx_mx4_matmul(a, b, y, workspace):
     _check(y, "y", (batch, M, N) if y.dim() == 3 or batch != 1 else (M, N), y.dtype, dev)
     ac, asc = _mx4_ptrs(a, "a", a.shape, dev)
     bc, bsc = _mx4_ptrs(b, "b", b.shape, dev)
-    with _on(dev):
-        s = lib().btx_mx4_matmul(_dtype_code(y.dtype), batch, M, N, K, ac, asc, bc, bsc, _ptr(y), _ptr(workspace),
-                                 workspace.numel(), _stream(dev))
-    if s != BTX_OK:
-        raise BtxError(s, "btx_mx4_matmul")
+    ws, ws_bytes = _workspace(workspace, dev)
+    _launch("btx_mx4_matmul", dev, _dtype_code(y.dtype), batch, M, N, K, ac, asc, bc, bsc, _addr(y), ws, ws_bytes)
 
 
 def make_mx4_moe_desc(T, d_model, d_ff, E, k, dtype) -> Mx4MoeDesc:
@@ -528,11 +538,9 @@ def btx_mx4_moe_forward(desc, x, topk_idx, gates, w13, w2, y, workspace):
     _check(y, "y", (T, d), dt, dev)
     c13, s13 = _mx4_ptrs(w13, "w13", (E, 2 * F, d), dev)
     c2, s2 = _mx4_ptrs(w2, "w2", (E, d, F), dev)
-    with _on(dev):
-        s = lib().btx_mx4_moe_forward(C.byref(desc), _ptr(x), _ptr(topk_idx), _ptr(gates), c13, s13, c2, s2, _ptr(y),
-                                      _ptr(workspace), workspace.numel(), _stream(dev))
-    if s != BTX_OK:
-        raise BtxError(s, "btx_mx4_moe_forward")
+    ws, ws_bytes = _workspace(workspace, dev)
+    _launch("btx_mx4_moe_forward", dev, C.byref(desc), _addr(x), _addr(topk_idx), _addr(gates), c13, s13, c2, s2, _addr(y), ws,
+            ws_bytes)
 
 
 def btx_selftest_wait_expiry(workspace):

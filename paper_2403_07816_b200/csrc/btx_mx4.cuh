@@ -33,9 +33,10 @@ cudaError_t launch_dequantize(const uint8_t* codes, const uint8_t* scales, int b
                               cudaStream_t st);
 
 // Row dispatch of the expert layer: rows of an expert are consecutive, in the order of t*k+slot, and padded to whole
-// 128-row tiles.
+// tiles of 128 rows or pairs of them.
 struct Dispatch {
   int T, k, R, E, d;                       // R = T*k
+  int pad_tiles;                           // an expert's rows are padded to this many row tiles (2: products by CTA pairs)
   int m_tiles_max;                         // upper bound of the padded row tiles
   const int32_t* topk_idx;                 // an index outside 0..E-1: no expert
   int32_t* flat2row;                       // [R] padded row of an assignment, -1 without an expert
@@ -61,6 +62,8 @@ struct GemmArgs {
   int experts;                             // B matrices
   int32_t* status;
 };
+// Whether the expert layer's products run on CTA pairs (256-row tiles): enough rows per expert to fill them.
+bool pairs_fit(long long rows, long long experts, long long d, long long F);
 btx_status launch_matmul(const GemmArgs& g, int dtype, void* y, cudaStream_t st);
 // W1/W3 product (rows interleaved) with silu(h1) * h3 cast to MXFP4
 btx_status launch_gate_up(const GemmArgs& g, const Dispatch& q, uint8_t* act_codes, uint8_t* act_scales, cudaStream_t st);

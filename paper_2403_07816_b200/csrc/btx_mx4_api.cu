@@ -31,12 +31,15 @@ btx_status make_moe_plan(const btx_mx4_moe_desc* d, MoePlan* pl) {
   const long long R = (long long)d->T * d->k;
   if (R > (1ll << 28)) return BTX_ERR_UNSUPPORTED;
   const long long used = R < d->E ? R : d->E;        // experts that can hold a row
-  const long long tiles = (R + used * (kTileRows - 1)) / kTileRows;
+  const int pad_tiles = pairs_fit(R, used, d->d_model, d->d_ff) ? 2 : 1;
+  const long long unit = pad_tiles * kTileRows;
+  const long long tiles = (R + used * (unit - 1)) / unit * pad_tiles;
   const long long widest = d->d_model > 2 * (long long)d->d_ff ? d->d_model : 2 * (long long)d->d_ff;
   if (tiles * row_tiles(widest) > kMaxItems) return BTX_ERR_UNSUPPORTED;
   *pl = MoePlan();
   Dispatch& q = pl->q;
   q.T = d->T; q.k = d->k; q.R = (int)R; q.E = d->E; q.d = d->d_model;
+  q.pad_tiles = pad_tiles;
   q.m_tiles_max = (int)tiles;
   q.blocks = dispatch_blocks(R);
   size_t o = 0;

@@ -172,12 +172,13 @@ dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__
 // ---------------------------------------------------------------------------------------------
 // Offsets of the experts' padded segments from their counts in shared memory (one block): pad[e], and the list of
 // the expert of every tile.
-__device__ __forceinline__ void place_experts(int E, int m_tiles_max, const int* cnt, int* pad, int* __restrict__ scan,
+__device__ __forceinline__ void place_experts(int E, int pad_tiles, const int* cnt, int* pad, int* __restrict__ scan,
                                               int32_t* __restrict__ tile_expert, int32_t* __restrict__ n_tiles,
                                               int32_t* __restrict__ pad_offsets) {
   const int tid = threadIdx.x;               // kSortThreads >= kMaxExperts4: a thread per expert
   const int lane = tid & 31, warp = tid >> 5;
-  int tiles = tid < E ? (cnt[tid] + kTileRows - 1) / kTileRows : 0;
+  const int unit = pad_tiles * kTileRows;
+  const int tiles = tid < E ? (cnt[tid] + unit - 1) / unit * pad_tiles : 0;
   int incl = tiles;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -243,9 +244,11 @@ __device__ __forceinline__ void scatter_rounds(int begin, int end, int E, const 
   }
 }
 
-__device__ __forceinline__ void clear_padding(int E, const int* cnt, const int* pad, int32_t* __restrict__ rowmap) {
-  for (int e = threadIdx.x; e < E; e += blockDim.x)
-    for (int r = cnt[e]; r < (cnt[e] + kTileRows - 1) / kTileRows * kTileRows; ++r) rowmap[pad[e] + r] = -1;
+// padding rows of all experts: a warp per expert
+__device__ __forceinline__ void clear_padding(int E, int pad_tiles, const int* cnt, const int* pad, int32_t* __restrict__ rowmap) {
+  const int unit = pad_tiles * kTileRows;
+  for (int e = threadIdx.x >> 5; e < E; e += blockDim.x >> 5)
+    for (int r = cnt[e] + (threadIdx.x & 31); r < (cnt[e] + unit - 1) / unit * unit; r += 32) rowmap[pad[e] + r] = -1;
 }
 
 struct SortShared {
@@ -266,8 +269,8 @@ dispatch_one_kernel(const Dispatch q) {
     if ((unsigned)e < (unsigned)q.E) atomicAdd(&s.cnt[e], 1);
   }
   __syncthreads();
-  place_experts(q.E, q.m_tiles_max, s.cnt, s.pad, s.scan, q.tile_expert, q.n_tiles, nullptr);
-  clear_padding(q.E, s.cnt, s.pad, q.rowmap);
+  place_experts(q.E, q.pad_tiles, s.cnt, s.pad, s.scan, q.tile_expert, q.n_tiles, nullptr);
+  clear_padding(q.E, q.pad_tiles, s.cnt, s.pad, q.rowmap);
   scatter_rounds(0, q.R, q.E, q.topk_idx, s.running, s.wcnt, s.pad, q.flat2row, q.rowmap);
 }
 
@@ -309,8 +312,8 @@ dispatch_scan_kernel(const Dispatch q) {
     cnt[e] = run;
   }
   __syncthreads();
-  place_experts(q.E, q.m_tiles_max, cnt, pad, scan, q.tile_expert, q.n_tiles, q.pad_offsets);
-  clear_padding(q.E, cnt, pad, q.rowmap);
+  place_experts(q.E, q.pad_tiles, cnt, pad, scan, q.tile_expert, q.n_tiles, q.pad_offsets);
+  clear_padding(q.E, q.pad_tiles, cnt, pad, q.rowmap);
 }
 
 __global__ void __launch_bounds__(kSortThreads)

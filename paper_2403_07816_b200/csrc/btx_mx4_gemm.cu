@@ -19,6 +19,8 @@
 // Every wait is bounded (tcx::mbar_wait); a wait that runs out leaves BTX_ERR_TIMEOUT in the status word.
 #include <cuda_fp4.h>
 
+#include <atomic>
+
 #include "btx_mx4.cuh"
 #include "btx_tc_ptx.cuh"
 
@@ -53,6 +55,7 @@ struct Params {
   int M, N, K;                      // STORE: rows and columns of y; grouped: N = B rows per expert
   int m_tiles, n_tiles, batch;
   int grouped;
+  int tile_step;                    // 128-row tiles per row tile of this launch (1, or 2 for CTA pairs)
   const int32_t* n_row_tiles;       // grouped: row tiles in use (device)
   const int32_t* tile_expert;
   const int32_t* rowmap;
@@ -60,6 +63,7 @@ struct Params {
   const uint8_t* b_scales;
   long long a_scale_batch, b_scale_batch;   // bytes from one matrix to the next
   int kt;                           // scale tiles along K
+  int a_row_tiles, b_row_tiles;     // scale row tiles of one matrix
   const float* gates;
   void* y;
   uint8_t* act_codes;
@@ -115,8 +119,82 @@ __device__ __forceinline__ Item get_item(const Params& p, int m_tiles, int t) {
   else { g = full; rem = local - in_full; width = p.n_tiles - full * GROUP_N; }
   it.mt = rem / width;
   it.nt = g * GROUP_N + rem - it.mt * width;
-  it.e = p.grouped ? p.tile_expert[it.mt] : it.b;
+  it.e = p.grouped ? p.tile_expert[it.mt * p.tile_step] : it.b;
   return it;
+}
+
+// 64 accumulator columns of one row per thread (columns n0 .. n0 + 63 of the product), by a whole warp.  m: the row of
+// A; flat: its row of y (STORE) or its assignment, -1 for a row that nobody asked for.
+template <int MODE>
+__device__ __forceinline__ void epilogue_chunk(const Params& p, const Item& it, uint32_t taddr, int n0, int m, int flat) {
+  const bool wide = p.wide != 0;
+  float v[32];
+  if constexpr (MODE == GATE_UP) {
+    const int F = p.N / 2;
+    const int f0 = n0 / 2;                                // 32 hidden units: one block
+    float a[32];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      __syncwarp();                                       // the tensor-memory load needs the whole warp
+      tc_ld32(taddr + 32 * h, v);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) a[16 * h + i] = fast_swiglu(v[2 * i], v[2 * i + 1]);
+    }
+    if (flat < 0) return;
+    uint32_t amax = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) amax = max(amax, __float_as_uint(a[i]) & 0x7fffffffu);
+    float inv;
+    uint32_t byte = scale_byte(amax, inv);
+    uint32_t w[4] = {0, 0, 0, 0};
+    if (byte != 255u) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        w[i / 4] |= (uint32_t)__nv_cvt_float2_to_fp4x2(make_float2(a[2 * i] * inv, a[2 * i + 1] * inv), __NV_E2M1,
+                                                       cudaRoundNearest) << (8 * (i & 3));
+    }
+    // past the last unit there is no block, but the other half of an MMA's 64 elements wants a finite scale
+    if (f0 >= F) byte = 0;
+    const int blk = f0 / kBlock, akt = (int)scale_tiles_k(F);
+    if (blk < 4 * akt)
+      p.act_scales[((size_t)(m / kTileRows) * akt + blk / 4) * kTileBytes + (m & 31) * 16 + (m >> 5 & 3) * 4 + (blk & 3)] = (uint8_t)byte;
+    if (f0 < F) *reinterpret_cast<uint4*>(p.act_codes + (size_t)m * (F / 2) + f0 / 2) = make_uint4(w[0], w[1], w[2], w[3]);
+  } else {
+    const float g = MODE == DOWN && flat >= 0 ? p.gates[flat] : 1.f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      __syncwarp();
+      tc_ld32(taddr + 32 * h, v);
+      const int col = n0 + 32 * h;
+      if (flat < 0 || col >= p.N) continue;
+      const size_t o = MODE == STORE ? ((size_t)it.b * p.M + flat) * p.N + col : (size_t)flat * p.N + col;
+      if (MODE == STORE && p.out_bf16) {
+        __nv_bfloat16* y = (__nv_bfloat16*)p.y + o;
+        if (wide && col + 32 <= p.N) {
+          st32(y, pack8(v), pack8(v + 8), true);
+          st32(y + 16, pack8(v + 16), pack8(v + 24), true);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (col + i < p.N) y[i] = __float2bfloat16_rn(v[i]);
+        }
+      } else {
+        float* y = (float*)p.y + o;
+        if (MODE == DOWN) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] *= g;
+        }
+        if (MODE == DOWN || (wide && col + 32 <= p.N)) {  // DOWN: rows of a multiple of 32 columns
+#pragma unroll
+          for (int i = 0; i < 4; ++i) st32(y + 8 * i, f4(v + 8 * i), f4(v + 8 * i + 4), wide);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (col + i < p.N) y[i] = v[i];
+        }
+      }
+    }
+  }
 }
 
 template <int MODE, int BN>
@@ -231,7 +309,6 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
   } else {
     const int q = warp & 3, half = (warp - 2) >> 2;
     const int row = q * 32 + lane;
-    const bool wide = p.wide != 0;
     constexpr int HC = BN / 2;                            // columns of this warp
     uint32_t acc = 0, acc_phase = 0;
     bool ok = true;
@@ -245,85 +322,8 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
       const uint32_t taddr = tmem + acc * BN + half * HC + ((uint32_t)(q * 32) << 16);
       const int n0 = it.nt * BN + half * HC;
       if (any) {
-        float v[32];
-        if constexpr (MODE == STORE) {
-          for (int c = 0; c < HC; c += 32) {
-            __syncwarp();                                 // the tensor-memory load needs the whole warp
-            tc_ld32(taddr + c, v);
-            const int col = n0 + c;
-            if (flat < 0 || col >= p.N) continue;
-            const size_t o = ((size_t)it.b * p.M + flat) * p.N + col;
-            if (p.out_bf16) {
-              __nv_bfloat16* y = (__nv_bfloat16*)p.y + o;
-              if (wide && col + 32 <= p.N) {
-                st32(y, pack8(v), pack8(v + 8), true);
-                st32(y + 16, pack8(v + 16), pack8(v + 24), true);
-              } else {
-#pragma unroll
-                for (int i = 0; i < 32; ++i)
-                  if (col + i < p.N) y[i] = __float2bfloat16_rn(v[i]);
-              }
-            } else {
-              float* y = (float*)p.y + o;
-              if (wide && col + 32 <= p.N) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) st32(y + 8 * i, f4(v + 8 * i), f4(v + 8 * i + 4), true);
-              } else {
-#pragma unroll
-                for (int i = 0; i < 32; ++i)
-                  if (col + i < p.N) y[i] = v[i];
-              }
-            }
-          }
-        } else if constexpr (MODE == DOWN) {
-          const float g = flat >= 0 ? p.gates[flat] : 0.f;
-          for (int c = 0; c < HC; c += 32) {
-            __syncwarp();                                 // the tensor-memory load needs the whole warp
-            tc_ld32(taddr + c, v);
-            const int col = n0 + c;
-            if (flat < 0 || col >= p.N) continue;         // N is a multiple of 32
-            float* y = (float*)p.y + (size_t)flat * p.N + col;
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] *= g;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) st32(y + 8 * i, f4(v + 8 * i), f4(v + 8 * i + 4), wide);
-          }
-        } else {
-          const int F = p.N / 2;
-          const int akt = (int)scale_tiles_k(F);
-          for (int c = 0; c < HC; c += 64) {
-            const int f0 = (n0 + c) / 2;                  // 32 hidden units: one block
-            float a[32];
-            __syncwarp();
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              tc_ld32(taddr + c + 32 * h, v);
-#pragma unroll
-              for (int i = 0; i < 16; ++i) a[16 * h + i] = fast_swiglu(v[2 * i], v[2 * i + 1]);
-            }
-            if (flat < 0) continue;
-            uint32_t amax = 0;
-#pragma unroll
-            for (int i = 0; i < 32; ++i) amax = max(amax, __float_as_uint(a[i]) & 0x7fffffffu);
-            float inv;
-            uint32_t byte = scale_byte(amax, inv);
-            uint32_t w[4] = {0, 0, 0, 0};
-            if (byte != 255u) {
-#pragma unroll
-              for (int i = 0; i < 16; ++i)
-                w[i / 4] |= (uint32_t)__nv_cvt_float2_to_fp4x2(make_float2(a[2 * i] * inv, a[2 * i + 1] * inv), __NV_E2M1,
-                                                               cudaRoundNearest) << (8 * (i & 3));
-            }
-            // past the last unit there is no block, but the other half of an MMA's 64 elements wants a finite scale
-            if (f0 >= F) byte = 0;
-            const int blk = f0 / kBlock;
-            if (blk < 4 * akt)
-              p.act_scales[((size_t)it.mt * akt + blk / 4) * kTileBytes + (row & 31) * 16 + (row >> 5) * 4 + (blk & 3)] =
-                  (uint8_t)byte;
-            if (f0 < F)
-              *reinterpret_cast<uint4*>(p.act_codes + (size_t)m * (F / 2) + f0 / 2) = make_uint4(w[0], w[1], w[2], w[3]);
-          }
-        }
+#pragma unroll 1
+        for (int c = 0; c < HC; c += 64) epilogue_chunk<MODE>(p, it, taddr + c, n0 + c, m, flat);
       }
       __syncwarp();
       tc_fence_before();
@@ -340,6 +340,206 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
   }
 }
 
+// ---------------------------------------------------------------------------------------------
+// Two CTAs on one 256 x 256 tile (cta_group::2)
+// ---------------------------------------------------------------------------------------------
+// A stage brings 128 rows of A and 128 of the 256 rows of B per CTA, half of what two CTAs with tiles of their own
+// would fetch for the same products: the 128 x 128 tiles above fetch 15.6 bytes per 1000 products and stop at the L2's
+// bandwidth (2.5 PFLOP/s at M = 8192, N = 11008, K = 4096).
+// Tensor memory: an accumulator takes 256 of the 512 columns, so two do not fit beside the scales whole.  They
+// overlap in 64 columns: 0..255 and 192..447.  The epilogue reads the shared columns of a tile first and then hands
+// them over, so the next tile starts after a quarter of it.  The remaining columns hold the scales of two stages; a
+// stage's scales are copied once the MMAs of the stage before the last have retired.
+//   warp 0   TMA of A and its scales   warp 10  TMA of B and its scales (two threads: an operation costs its thread
+//   about 80 ns, four of them more than the 270 ns that the MMAs of a stage take)
+//   warp 1   MMAs (one lane of the leader CTA)   warps 2-9  epilogue, 64-column chunks: of the two warps of a lane
+//   quarter the first takes the shared chunk and the one at the other end, the second the two between
+constexpr int P_STAGES = 6;
+constexpr int P_B_BYTES = 128 * SK / 2, P_SFB_BYTES = 2 * 2 * kTileBytes;
+constexpr int P_STAGE_BYTES = A_BYTES + P_B_BYTES + SFA_BYTES + P_SFB_BYTES;
+constexpr int P_SMEM = P_STAGES * P_STAGE_BYTES + 1024 + 256;
+constexpr int P_THREADS = THREADS + 32;
+constexpr int P_ACC1 = 192, P_SF0 = 448, P_SF_COLS = 24;
+static_assert(P_SF0 + 2 * P_SF_COLS <= 512 && P_ACC1 + 256 <= P_SF0, "tensor memory");
+
+__device__ __forceinline__ void mma_mxf4_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                              uint32_t accum) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accum) : "memory");
+}
+// in both CTAs, each from its own shared memory to its own tensor memory
+__device__ __forceinline__ void copy_scales_pair(uint32_t tmem, uint32_t smem) {
+  const uint64_t desc = (uint64_t)((smem & 0x3FFFFu) >> 4) | ((uint64_t)(128 >> 4) << 16) | ((uint64_t)(128 >> 4) << 32) |
+                        (1ull << 46);
+  asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+
+template <int MODE>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
+mx4_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                     const __grid_constant__ CUtensorMap tmSA, const __grid_constant__ CUtensorMap tmSB, const Params p) {
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t ring = (raw + 1023u) & ~1023u;
+  uint8_t* ctl = smem_raw + (ring - raw) + P_STAGES * P_STAGE_BYTES;
+  const uint32_t bar_full = smem_u32(ctl), bar_empty = bar_full + P_STAGES * 8;
+  const uint32_t bar_tfull = bar_empty + P_STAGES * 8, bar_handed = bar_tfull + 16;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctl + P_STAGES * 16 + 32);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(ctl + P_STAGES * 16 + 40);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < P_STAGES; ++s) { mbar_init(bar_full + s * 8, 1); mbar_init(bar_empty + s * 8, 1); }
+    for (int a = 0; a < 2; ++a) mbar_init(bar_tfull + a * 8, 1);
+    mbar_init(bar_handed, 2 * EPI_WARPS);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512));
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  allow_dependents();
+  grid_dependency_wait();
+  if (MODE == STORE && blockIdx.x == 0 && threadIdx.x < kStatusWords) p.status[threadIdx.x] = 0;
+  const int m_tiles = p.grouped ? p.n_row_tiles[0] / 2 : p.m_tiles;       // of 256 rows
+  const int n_total = m_tiles * p.n_tiles * p.batch;
+  const int kb_total = (p.K + SK - 1) / SK;
+
+  if (warp == 0 || warp == 10) {
+    if (lane == 0) {
+      const bool a_side = warp == 0;
+      uint32_t stage = 0, phase = 0;
+      bool ok = true;
+      for (int t = pair; t < n_total && ok; t += n_pairs) {
+        const Item it = get_item(p, m_tiles, t);
+        const int row0 = it.mt * 256 + (int)rank * 128;
+        const int sfa_row = it.b * p.a_row_tiles + it.mt * 2 + (int)rank, sfb_row = it.e * p.b_row_tiles + it.nt * 2;
+        for (int kb = 0; kb < kb_total; ++kb) {
+          if (!(ok = mbar_wait(bar_empty + stage * 8, phase ^ 1u, abort_flag, p.status))) break;
+          const uint32_t full_local = bar_full + stage * 8;
+          const uint32_t full = map_to_cta(full_local, 0);
+          const uint32_t sA = ring + stage * P_STAGE_BYTES, sB = sA + A_BYTES, sSA = sB + P_B_BYTES, sSB = sSA + SFA_BYTES;
+          if (a_side) {
+            if (rank == 0) mbar_expect_tx(full_local, 2 * P_STAGE_BYTES);
+            tma_load_3d(sA, &tmA, kb * (SK / 2), row0, it.b, full);
+            tma_load_3d(sSA, &tmSA, 0, kb * 2, sfa_row, full);
+          } else {
+            tma_load_3d(sB, &tmB, kb * (SK / 2), it.nt * 256 + (int)rank * 128, it.e, full);
+            tma_load_3d(sSB, &tmSB, 0, kb * 2, sfb_row, full);
+          }
+          if (++stage == P_STAGES) { stage = 0; phase ^= 1u; }
+        }
+      }
+      for (int i = 0; i < P_STAGES && ok; ++i) {
+        ok = mbar_wait(bar_empty + stage * 8, phase ^ 1u, abort_flag, p.status);
+        if (++stage == P_STAGES) { stage = 0; phase ^= 1u; }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
+      constexpr uint32_t idesc0 = (1u << 7) | (1u << 10) | ((uint32_t)(256 >> 3) << 17) | (1u << 23) | ((uint32_t)(256 >> 4) << 24);
+      uint32_t stage = 0, phase = 0, acc = 0, tile = 0, slot = 0;
+      uint32_t ret_stage = 0, ret_phase = 0, steps = 0;   // the step whose scale columns are taken over next
+      bool ok = true;
+      for (int t = pair; t < n_total && ok; t += n_pairs, ++tile) {
+        // the tile before has handed over the shared columns (and the one before that everything)
+        if (tile > 0 && !(ok = mbar_wait(bar_handed, (tile - 1) & 1u, abort_flag, p.status))) break;
+        tc_fence_after();
+        const uint32_t d = tmem + (acc ? P_ACC1 : 0);
+        for (int kb = 0; kb < kb_total; ++kb) {
+          if (!(ok = mbar_wait(bar_full + stage * 8, phase, abort_flag, p.status))) break;
+          if (steps >= 2) {
+            if (!(ok = mbar_wait(bar_empty + ret_stage * 8, ret_phase, abort_flag, p.status))) break;
+            if (++ret_stage == P_STAGES) { ret_stage = 0; ret_phase ^= 1u; }
+          }
+          ++steps;
+          tc_fence_after();
+          const uint32_t sA = ring + stage * P_STAGE_BYTES, sB = sA + A_BYTES, sSA = sB + P_B_BYTES, sSB = sSA + SFA_BYTES;
+          const uint32_t tA = tmem + P_SF0 + slot * P_SF_COLS, tB = tA + 8;
+          slot ^= 1u;
+          const int k64 = min(SK / 64, (p.K - kb * SK + 63) / 64);
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            if (2 * c < k64) {
+              copy_scales_pair(tA + c * 4, sSA + c * kTileBytes);
+              copy_scales_pair(tB + c * 8, sSB + c * kTileBytes);
+              copy_scales_pair(tB + c * 8 + 4, sSB + (2 + c) * kTileBytes);
+            }
+          }
+          const uint64_t da = smem_desc(sA, false), db = smem_desc(sB, false);
+#pragma unroll
+          for (int j = 0; j < SK / 64; ++j) {
+            if (j < k64) {
+              const uint32_t id = (uint32_t)(j & 1) * 2;
+              mma_mxf4_pair(d, da + (uint64_t)(2 * j), db + (uint64_t)(2 * j), idesc0 | (id << 4) | (id << 29), tA + (j >> 1) * 4,
+                            tB + (j >> 1) * 8, (kb > 0 || j > 0) ? 1u : 0u);
+            }
+          }
+          tc_commit_pair(bar_empty + stage * 8);
+          if (++stage == P_STAGES) { stage = 0; phase ^= 1u; }
+        }
+        if (!ok) break;
+        tc_commit_pair(bar_tfull + acc * 8);
+        acc ^= 1u;
+      }
+    }
+  } else {
+    const int q = warp & 3, half = (warp - 2) >> 2;
+    const int row = q * 32 + lane;
+    const uint32_t handed = map_to_cta(bar_handed, 0);
+    uint32_t acc = 0, acc_phase = 0;
+    bool ok = true;
+    for (int t = pair; t < n_total && ok; t += n_pairs) {
+      const Item it = get_item(p, m_tiles, t);
+      const int m = it.mt * 256 + (int)rank * 128 + row;
+      const int flat = MODE == STORE ? (m < p.M ? m : -1) : p.rowmap[m];
+      const bool any = __any_sync(0xffffffffu, flat >= 0);
+      if (!(ok = mbar_wait(bar_tfull + acc * 8, acc_phase, abort_flag, p.status))) break;
+      tc_fence_after();
+      const uint32_t taddr = tmem + (acc ? P_ACC1 : 0) + ((uint32_t)(q * 32) << 16);
+      const int n0 = it.nt * 256;
+      // chunk 3 of the accumulator at 0 and chunk 0 of the one at 192 are the same columns
+      const int shared_chunk = acc ? 0 : 3;
+      if (half == 1) {                                    // everything of the tile before is read
+        if (lane == 0) mbar_arrive_cluster(handed);
+        if (any) {
+          epilogue_chunk<MODE>(p, it, taddr + 64, n0 + 64, m, flat);
+          epilogue_chunk<MODE>(p, it, taddr + 128, n0 + 128, m, flat);
+        }
+      } else {
+        if (any) epilogue_chunk<MODE>(p, it, taddr + shared_chunk * 64, n0 + shared_chunk * 64, m, flat);
+        __syncwarp();
+        tc_fence_before();
+        if (lane == 0) mbar_arrive_cluster(handed);
+        if (any) epilogue_chunk<MODE>(p, it, taddr + (3 - shared_chunk) * 64, n0 + (3 - shared_chunk) * 64, m, flat);
+      }
+      __syncwarp();
+      tc_fence_before();
+      acc ^= 1u;
+      if (acc == 0) acc_phase ^= 1u;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
+  }
+}
+
 // codes [batch][rows][K/2] as bytes, box of 128 bytes x box_rows
 bool make_codes_map(CUtensorMap* m, const void* base, long long K, long long rows, long long batch, uint32_t box_rows) {
   EncodeTiledFn fn = encode_fn();
@@ -352,38 +552,86 @@ bool make_codes_map(CUtensorMap* m, const void* base, long long K, long long row
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// scale tiles [row tiles][kt][512 bytes] of all matrices, box of two tiles along K x box_tiles row tiles
+bool make_scales_map(CUtensorMap* m, const void* base, long long kt, long long row_tiles, uint32_t box_tiles) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[3] = {kTileBytes / 4, (cuuint64_t)kt, (cuuint64_t)row_tiles};
+  cuuint64_t strides[2] = {kTileBytes, (cuuint64_t)(kt * kTileBytes)};
+  cuuint32_t box[3] = {kTileBytes / 4, 2, box_tiles};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_INT32, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// once per device and kernel: the attribute outlives the call
+bool allow_smem(const void* kernel, int bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0ull;
+  if (bit != 0 && (done.load(std::memory_order_relaxed) & bit)) return true;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+  done.fetch_or(bit, std::memory_order_relaxed);
+  return true;
+}
+
 template <int MODE, int BN>
-btx_status launch(const GemmArgs& g, Params p, int max_items, cudaStream_t st) {
+btx_status launch(const GemmArgs& g, Params p, long long max_items, cudaStream_t st) {
+  static std::atomic<uint64_t> done{0};
   CUtensorMap a, b;
-  if (!make_codes_map(&a, g.a_codes, g.K, g.M, g.batch, BM) || !make_codes_map(&b, g.b_codes, g.K, g.N, g.experts, BN))
+  if (!make_codes_map(&a, g.a_codes, g.K, g.M, g.batch, BM) || !make_codes_map(&b, g.b_codes, g.K, g.N, g.experts, BN) ||
+      !allow_smem((const void*)mx4_gemm_kernel<MODE, BN>, Cfg<BN>::SMEM, done))
     return BTX_ERR_CUDA;
-  if (cudaFuncSetAttribute(mx4_gemm_kernel<MODE, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<BN>::SMEM) != cudaSuccess)
-    return BTX_ERR_CUDA;
-  int blocks = sm_count();
-  if (blocks > max_items) blocks = max_items;
+  const int blocks = max_items < sm_count() ? (int)max_items : sm_count();
   return launch_after_predecessor(mx4_gemm_kernel<MODE, BN>, dim3(blocks), dim3(THREADS), Cfg<BN>::SMEM, st, MODE != STORE, a, b,
                                   p) == cudaSuccess ? BTX_OK : BTX_ERR_CUDA;
+}
+
+template <int MODE>
+btx_status launch_pair(const GemmArgs& g, Params p, cudaStream_t st) {
+  static std::atomic<uint64_t> done{0};
+  CUtensorMap a, b, sa, sb;
+  p.m_tiles = (g.M + 255) / 256; p.n_tiles = (g.N + 255) / 256; p.tile_step = 2;
+  if (!make_codes_map(&a, g.a_codes, g.K, g.M, g.batch, 128) || !make_codes_map(&b, g.b_codes, g.K, g.N, g.experts, 128) ||
+      !make_scales_map(&sa, g.a_scales, p.kt, (long long)p.a_row_tiles * g.batch, 1) ||
+      !make_scales_map(&sb, g.b_scales, p.kt, (long long)p.b_row_tiles * g.experts, 2) ||
+      !allow_smem((const void*)mx4_gemm_pair_kernel<MODE>, P_SMEM, done))
+    return BTX_ERR_CUDA;
+  const long long items = (long long)p.m_tiles * p.n_tiles * p.batch;
+  int pairs = sm_count() / 2;
+  if (items < pairs) pairs = (int)items;
+  return launch_after_predecessor(mx4_gemm_pair_kernel<MODE>, dim3(2 * pairs), dim3(P_THREADS), P_SMEM, st, MODE != STORE, a, b, sa,
+                                  sb, p) == cudaSuccess ? BTX_OK : BTX_ERR_CUDA;
 }
 
 Params base_params(const GemmArgs& g, int bn) {
   Params p = {};
   p.M = g.M; p.N = g.N; p.K = g.K; p.batch = g.batch; p.status = g.status;
   p.m_tiles = (g.M + BM - 1) / BM; p.n_tiles = (g.N + bn - 1) / bn;
-  p.kt = (int)scale_tiles_k(g.K);
+  p.kt = (int)scale_tiles_k(g.K); p.tile_step = 1;
+  p.a_row_tiles = (g.M + kTileRows - 1) / kTileRows; p.b_row_tiles = (g.N + kTileRows - 1) / kTileRows;
   p.a_scales = g.a_scales; p.b_scales = g.b_scales;
   p.a_scale_batch = (long long)p.m_tiles * p.kt * kTileBytes;
   p.b_scale_batch = (long long)((g.N + kTileRows - 1) / kTileRows) * p.kt * kTileBytes;
   return p;
 }
 
+// CTA pairs want whole tiles of 256 rows and enough of them
+bool use_pairs(long long pair_tiles, long long rows) { return rows > 128 && pair_tiles >= sm_count() / 2; }
+
 }  // namespace
+
+bool pairs_fit(long long rows, long long experts, long long d, long long F) {
+  return rows >= 256 * experts && use_pairs(rows / 256 * ((d + 255) / 256), rows) && F > 0;
+}
 
 btx_status launch_matmul(const GemmArgs& g, int dtype, void* y, cudaStream_t st) {
   constexpr int BN = 128;
   Params p = base_params(g, BN);
   p.y = y; p.out_bf16 = dtype == BTX_BF16;
   p.wide = aligned32(y) && (size_t)g.N * (p.out_bf16 ? 2 : 4) % 32 == 0;
-  return launch<STORE, BN>(g, p, (int)((long long)p.m_tiles * p.n_tiles * p.batch < 1 << 20 ? p.m_tiles * p.n_tiles * p.batch : 1 << 20), st);
+  if (use_pairs((long long)g.batch * ((g.M + 255) / 256) * ((g.N + 255) / 256), g.M)) return launch_pair<STORE>(g, p, st);
+  return launch<STORE, BN>(g, p, (long long)p.m_tiles * p.n_tiles * p.batch, st);
 }
 
 btx_status launch_gate_up(const GemmArgs& g, const Dispatch& q, uint8_t* act_codes, uint8_t* act_scales, cudaStream_t st) {
@@ -391,7 +639,8 @@ btx_status launch_gate_up(const GemmArgs& g, const Dispatch& q, uint8_t* act_cod
   Params p = base_params(g, BN);
   p.grouped = 1; p.n_row_tiles = q.n_tiles; p.tile_expert = q.tile_expert; p.rowmap = q.rowmap;
   p.act_codes = act_codes; p.act_scales = act_scales;
-  return launch<GATE_UP, BN>(g, p, p.m_tiles * p.n_tiles, st);
+  if (q.pad_tiles == 2) return launch_pair<GATE_UP>(g, p, st);
+  return launch<GATE_UP, BN>(g, p, (long long)p.m_tiles * p.n_tiles, st);
 }
 
 btx_status launch_down(const GemmArgs& g, const Dispatch& q, const float* gates, float* rows, cudaStream_t st) {
@@ -399,7 +648,8 @@ btx_status launch_down(const GemmArgs& g, const Dispatch& q, const float* gates,
   Params p = base_params(g, BN);
   p.grouped = 1; p.n_row_tiles = q.n_tiles; p.tile_expert = q.tile_expert; p.rowmap = q.rowmap;
   p.gates = gates; p.y = rows; p.wide = aligned32(rows);
-  return launch<DOWN, BN>(g, p, p.m_tiles * p.n_tiles, st);
+  if (q.pad_tiles == 2) return launch_pair<DOWN>(g, p, st);
+  return launch<DOWN, BN>(g, p, (long long)p.m_tiles * p.n_tiles, st);
 }
 
 }  // namespace mx4

@@ -24,7 +24,10 @@ namespace {
 using routedev::Vec;
 
 constexpr unsigned kAll = 0xffffffffu;
-constexpr int kRsWarps = 8;
+// Rows in flight per block.  Every block adds its counts to E addresses, so fewer, larger blocks: T = 16384, E = 64 with
+// 1184 blocks of 8 warps spent 10 of 14 us on the additions.
+template <int EPL> struct RouteWarps { static constexpr int n = EPL <= 8 ? 16 : 8; };
+constexpr int kRsWarps = 8;                 // backward
 constexpr int kMaxScoredExperts = 512;
 constexpr int kMaxScoredK = 32;             // lane j keeps slot j
 constexpr int kMaxScoredGroups = 32;
@@ -45,16 +48,12 @@ struct RouteParams {
 // fp32 to integers of the same order, never 0 (0 marks "no candidate"); -0 and +0 are one value
 __device__ __forceinline__ uint32_t order_key(float v) {
   const uint32_t b = __float_as_uint(v + 0.0f);
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
+  return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
+__device__ __forceinline__ float order_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
-  return v;
-}
-__device__ __forceinline__ float warp_max(float v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kAll, v, o));
   return v;
 }
 __device__ __forceinline__ float sigmoid_rn(float z) { return 1.0f / (1.0f + expf(-z)); }
@@ -84,17 +83,45 @@ __device__ __forceinline__ void load_row(const T* __restrict__ row, int E, int l
 
 // Two-best merge: (a, b) with a >= b
 template <typename F> __device__ __forceinline__ void push2(F v, F& a, F& b) {
-  if (v > a) { b = a; a = v; } else if (v > b) { b = v; }
+  const F low = a < v ? a : v;
+  a = a < v ? v : a;
+  b = b < low ? low : b;
 }
 // Group key from its two best members' keys.  A group without a candidate has -inf, a missing second adds nothing.
 template <typename F> __device__ __forceinline__ F group_value(F a, F b, int sum2) {
   return sum2 && b > (F)-CUDART_INF ? a + b : a;
 }
+__device__ __forceinline__ float warp_max_of(float v) { return order_value(__reduce_max_sync(kAll, order_key(v))); }
+__device__ __forceinline__ float warp_min_of(float v) { return order_value(__reduce_min_sync(kAll, order_key(v))); }
+__device__ __forceinline__ double warp_max_of(double v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = fmax(v, __shfl_xor_sync(kAll, v, o));
+  return v;
+}
+__device__ __forceinline__ double warp_min_of(double v) { return -warp_max_of(-v); }
 
-// Which groups stay, as a bit mask, from the keys in the warp's shared memory (expert e at e + (e / size) * P, so
-// that the lanes of different groups read different banks).  P lanes share a group.  `margin` receives the
-// difference between the worst group that stays and the best that does not, `reach` the largest
-// sum of magnitudes behind a group's key (for the caller's error bound).
+// Whether this lane's group g stays: v is its key, the same in the P lanes g * P .. g * P + P - 1, which share the
+// comparisons with the G groups; `size` bounds the magnitudes behind v.  `margin` receives the difference between the
+// worst group that stays and the best that does not, `reach` the largest size (for the caller's error bound).
+template <typename F>
+__device__ __forceinline__ bool rank_groups(F v, F size, int g, int G, int P, int lane, int topk_group, F& margin, F& reach) {
+  const F low = (F)-CUDART_INF;
+  int rank = 0;
+  for (int q0 = 0; q0 < G; q0 += P) {
+    const int q = q0 + (lane & (P - 1));
+    const F o = __shfl_sync(kAll, v, (q * P) & 31);
+    rank += q < G && (o > v || (o == v && q < g));
+  }
+  for (int o = 1; o < P; o <<= 1) rank += __shfl_xor_sync(kAll, rank, o);
+  const bool stays = g < G && rank < topk_group;
+  const F worst = warp_min_of(stays ? v : (F)CUDART_INF), best = warp_max_of(g < G && !stays ? v : low);
+  reach = warp_max_of(g < G && v > low ? size : (F)0);
+  margin = best > low ? worst - best : (F)CUDART_INF;
+  return stays;
+}
+
+// The groups that stay, as a bit mask, from keys in the warp's shared memory (expert e at e + (e / size) * P, so that the lanes of different
+// groups read different banks); P lanes share a group.
 template <typename F>
 __device__ __forceinline__ uint32_t choose_groups(const F* key, int G, int size, int P, int topk_group, int sum2,
                                                   int lane, F& margin, F& reach) {
@@ -109,28 +136,9 @@ __device__ __forceinline__ uint32_t choose_groups(const F* key, int G, int size,
     push2(ob, a, b);
   }
   const F v = g < G ? group_value(a, b, sum2) : low;
-  int rank = 0;
-  for (int q = 0; q < G; ++q) {
-    const F o = __shfl_sync(kAll, v, q * P);
-    rank += o > v || (o == v && q < g);
-  }
-  const bool leader = g < G && p == 0;
-  F worst = (F)CUDART_INF, best = low;
-  if (leader && rank < topk_group) worst = v;
-  if (leader && rank >= topk_group) best = v;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const F ow = __shfl_xor_sync(kAll, worst, o), ob = __shfl_xor_sync(kAll, best, o);
-    worst = ow < worst ? ow : worst;
-    best = ob > best ? ob : best;
-  }
-  F size_ab = (F)0;
-  if (leader && v > low) size_ab = fabs(a) + (v != a ? fabs(b) : (F)0);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) size_ab = fmax(size_ab, __shfl_xor_sync(kAll, size_ab, o));
-  margin = best > low ? worst - best : (F)CUDART_INF;
-  reach = size_ab;
-  const uint32_t lanes = __ballot_sync(kAll, leader && rank < topk_group && v > low);
+  const F reach_g = fabs(a) + (sum2 && b > low ? fabs(b) : (F)0);
+  const bool stays = rank_groups(v, reach_g, g, G, P, lane, topk_group, margin, reach);
+  const uint32_t lanes = __ballot_sync(kAll, stays && p == 0);
   uint32_t mask = 0;
   for (int q = 0; q < G; ++q) mask |= ((lanes >> (q * P)) & 1u) << q;
   return mask;
@@ -201,146 +209,233 @@ __device__ __noinline__ int choose_in_double(const T* __restrict__ row, const Ro
   return mine;
 }
 
+// Scores for the choice, from the approximate base-2 exponential and reciprocal of the hardware; the weights and the
+// `scores` output are formed again to full accuracy.  Errors (exp(x) as 2^(x log2 e): within 2 + 1.173 |x| ulp, the
+// reciprocal within 1; flushed subnormals are far below 2^-23):
+//   sigmoid  s (1 - s) (2 + 1.173 |z|) 2^-23 + 4 * 2^-24 s <= 2^-22 s + 2^-23
+//   softmax  each exponential carries the rounded difference x = max - z as well, (2 + 1.7 x) 2^-23; s x < 0.4, the
+//            mean of x under s is below 7 for E <= 512, the sum rounds 21 times: below 2^-18 s + 2^-23
+__device__ __forceinline__ float exp2_fast(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float rcp_fast(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+constexpr float kLog2e = 1.4426950408889634f;
+__device__ __forceinline__ float sigmoid_key(float z) { return rcp_fast(1.0f + exp2_fast(-kLog2e * z)); }
+
 template <typename T, int EPL, bool SIGMOID>
-__global__ void __launch_bounds__(kRsWarps * 32)
+__global__ void __launch_bounds__(RouteWarps<EPL>::n * 32, EPL <= 8 ? 2 : 3)
 route_scored_kernel(const T* __restrict__ logits, const RouteParams p, int sum2, int vec) {
+  constexpr int W = RouteWarps<EPL>::n;
   // per warp: 32-bit keys for the groups, or 64-bit keys of a row that is decided again (never both at once)
-  __shared__ double keys_s[kRsWarps][EPL * 32 + 32];
+  __shared__ double keys_s[W][EPL * 32 + 32];
   __shared__ int hist[EPL * 32];
+  // A packed key is the ordered key with its lowest bits replaced by the index, larger for lower experts: one warp
+  // maximum finds the next expert, its place and the lower index of a tie.
+  constexpr uint32_t IDX = EPL * 32 - 1;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const bool grouped = p.n_group > 1;
-  const int P = p.lanes_per_group;
+  const bool grouped = p.n_group > 1, biased = p.bias != nullptr;
   const int e0 = lane * EPL;
   const float low = -CUDART_INF_F;
   if (p.counts != nullptr) {
     for (int i = threadIdx.x; i < p.E; i += blockDim.x) hist[i] = 0;
     __syncthreads();
   }
-  // Error bounds of a 32-bit key, relative to its score and to itself (expf is within 1 ulp, division and sums
-  // round to nearest): sigmoid 2^-22 s; softmax also carries the rounded differences z - max, |z - max| 2^-24 each,
-  // and a sum of 21 roundings, together below 2^-19 (s + 0.02) for E <= 512.
-  const float err_s = SIGMOID ? 0x1p-22f : 0x1p-19f, err_0 = SIGMOID ? 0.f : 0x1p-24f, err_c = 0x1p-24f;
-  const bool need_scores = p.scores != nullptr || p.bias != nullptr || (grouped && sum2);
-  const bool need_total = !SIGMOID && (need_scores || !p.renorm);
+  const float err_s = SIGMOID ? 0x1p-22f : 0x1p-18f, err_0 = 0x1p-23f, err_c = 0x1p-24f;
+  const bool need_total = !SIGMOID && (p.scores != nullptr || biased || (grouped && sum2) || !p.renorm);
+  const bool exact_keys = !biased && sizeof(T) == 2;               // 16-bit logits keep every bit in a packed key
+  // groups of whole lanes (a power of two of them) are compared in registers, others through shared memory
+  const int lanes_per = p.group_size / EPL;
+  const bool by_lanes = grouped && lanes_per * EPL == p.group_size && (lanes_per & (lanes_per - 1)) == 0;
+  float bias[EPL];                          // the same for every row
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) bias[i] = biased && e0 + i < p.E ? p.bias[e0 + i] : 0.f;
+  int half_k = 1;                           // reductions over the chosen: lanes 0 .. 2 * half_k - 1 cover k
+  while (2 * half_k < p.k) half_k *= 2;
 
-  for (int t = blockIdx.x * kRsWarps + warp; t < p.T; t += gridDim.x * kRsWarps) {
+  for (int t = blockIdx.x * W + warp; t < p.T; t += gridDim.x * W) {
     const T* row = logits + (long long)t * p.stride;
     int sel = -1;                           // lane j: the expert of slot j
     float total = 1.f, zmax = 0.f;
     if (p.row_valid == nullptr || p.row_valid[t] != 0) {
-      float z[EPL], c[EPL], s[EPL];
+      float z[EPL];
       load_row<T, EPL>(row, p.E, lane, vec != 0, z);
       if (need_total) {
         float m = low;
 #pragma unroll
         for (int i = 0; i < EPL; ++i) m = fmaxf(m, z[i]);          // (fmaxf passes over NaN)
-        zmax = warp_max(m);
+        zmax = warp_max_of(m);
         float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < EPL; ++i) {
-          s[i] = z[i] > low ? exp_below(z[i], zmax) : 0.f;
-          sum += s[i];
-        }
+        for (int i = 0; i < EPL; ++i) sum += z[i] > low ? exp_below(z[i], zmax) : 0.f;
         total = warp_sum(sum);
-#pragma unroll
-        for (int i = 0; i < EPL; ++i) s[i] = total > 0.f ? s[i] / total : 0.f;
-      } else {
-#pragma unroll
-        for (int i = 0; i < EPL; ++i) s[i] = SIGMOID && need_scores && z[i] > low ? sigmoid_rn(z[i]) : 0.f;
+        if (!(total > 0.f)) total = 1.f;                           // nothing is on
       }
+      const float inv_total = 1.0f / total;
+      auto score_key = [&](float v) {                              // v > -inf
+        if (SIGMOID) return sigmoid_key(v);
+        return (v == zmax ? 1.0f : exp2_fast((v - zmax) * kLog2e)) * inv_total;
+      };
       if (p.scores != nullptr) {
 #pragma unroll
         for (int i = 0; i < EPL; ++i)
-          if (e0 + i < p.E) p.scores[(size_t)t * p.E + e0 + i] = s[i];
+          if (e0 + i < p.E)
+            p.scores[(size_t)t * p.E + e0 + i] = !(z[i] > low) ? 0.f : SIGMOID ? sigmoid_rn(z[i]) : exp_below(z[i], zmax) / total;
       }
+      float c[EPL];                                                // -inf: not a candidate
 #pragma unroll
       for (int i = 0; i < EPL; ++i) {
-        c[i] = p.bias == nullptr ? z[i] : (z[i] > low && e0 + i < p.E ? s[i] + p.bias[e0 + i] : low);
-        if (!(c[i] > low)) c[i] = low;
+        c[i] = biased ? score_key(z[i]) + bias[i] : z[i];
+        if (!(z[i] > low && c[i] > low)) c[i] = low;
       }
-      bool doubt = false;
+      const float smax = SIGMOID ? 1.0f : inv_total;               // no score is larger
+      bool unsure = false;                                         // the choice of groups is within its error
       if (grouped) {
-        float* key = reinterpret_cast<float*>(keys_s[warp]);
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < EPL; ++i) {
-          const int e = e0 + i;
-          if (e < p.E)
-            key[e + e / p.group_size * P] = p.bias == nullptr && sum2 ? (z[i] > low ? s[i] : low) : c[i];
-        }
-        __syncwarp();
         float margin, reach;
-        const uint32_t stay = choose_groups<float>(key, p.n_group, p.group_size, P, p.topk_group, sum2, lane, margin, reach);
-        // scores are at most 1 (two at most 2); keys compared as they stand (logits) are exact
-        if (p.bias != nullptr || sum2)
-          doubt = margin <= 2.f * ((sum2 ? 2.f : 1.f) * (err_s + err_0) + 3.f * err_c * reach);
+        if (by_lanes) {
+          float a = low, b = low;
 #pragma unroll
-        for (int i = 0; i < EPL; ++i)
-          if (e0 + i < p.E && !((stay >> ((e0 + i) / p.group_size)) & 1u)) c[i] = low;
-      }
-      // k rounds of a warp maximum, one more to see how far the last chosen is from the next
-      uint32_t u[EPL];
-      uint32_t lm = 0;
-      int li = 0;
+          for (int i = 0; i < EPL; ++i) push2(c[i], a, b);
+          for (int o = 1; o < lanes_per; o <<= 1) {
+            const float oa = __shfl_xor_sync(kAll, a, o), ob = __shfl_xor_sync(kAll, b, o);
+            push2(oa, a, b);
+            push2(ob, a, b);
+          }
+          if (!biased && sum2) {                                   // the best logits have the best scores
+            a = a > low ? score_key(a) : low;
+            b = b > low ? score_key(b) : low;
+          }
+          const bool stays = rank_groups(group_value(a, b, sum2), fabsf(a) + (sum2 && b > low ? fabsf(b) : 0.f),
+                                         lane / lanes_per, p.n_group, lanes_per, lane, p.topk_group, margin, reach);
+          if (!stays) {
 #pragma unroll
-      for (int i = 0; i < EPL; ++i) {
-        u[i] = c[i] > low ? order_key(c[i]) : 0u;
-        if (u[i] > lm) { lm = u[i]; li = i; }
-      }
-      const int rounds = p.bias != nullptr ? min(p.k + 1, 32) : p.k;
-      for (int j = 0; j < rounds; ++j) {
-        const uint32_t m = __reduce_max_sync(kAll, lm);
-        if (m == 0u) break;
-        const int w = __ffs(__ballot_sync(kAll, lm == m)) - 1;
-        const int e = __shfl_sync(kAll, e0 + li, w);
-        if (lane == j) sel = e;
-        if (lane == w) {
-          lm = 0;
-          int ni = 0;
+            for (int i = 0; i < EPL; ++i) c[i] = low;
+          }
+        } else {
+          float* key = reinterpret_cast<float*>(keys_s[warp]);
+          const int P = p.lanes_per_group;
+          __syncwarp();
 #pragma unroll
           for (int i = 0; i < EPL; ++i) {
-            if (i == li) u[i] = 0u;
-            if (u[i] > lm) { lm = u[i]; ni = i; }
+            const int e = e0 + i;
+            if (e < p.E) key[e + e / p.group_size * P] = !biased && sum2 && c[i] > low ? score_key(z[i]) : c[i];
           }
-          li = ni;
+          __syncwarp();
+          const uint32_t stay = choose_groups<float>(key, p.n_group, p.group_size, P, p.topk_group, sum2, lane, margin, reach);
+#pragma unroll
+          for (int i = 0; i < EPL; ++i)
+            if (e0 + i < p.E && !((stay >> ((e0 + i) / p.group_size)) & 1u)) c[i] = low;
+        }
+        // keys compared as they stand (logits) are exact
+        if (biased || sum2) unsure = margin <= 2.f * (sum2 ? 2.f : 1.f) * (err_s * smax + err_0) + 6.f * err_c * reach;
+      }
+      // k rounds: the largest packed key of the warp goes to the next slot.  A lane holds its two best (0: none) and
+      // looks through its experts again when both are taken.
+      uint32_t u[EPL], a = 0, b = 0;
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) {
+        u[i] = c[i] > low ? (order_key(c[i]) & ~IDX) | (IDX - (uint32_t)(e0 + i)) : 0u;
+        push2(u[i], a, b);
+      }
+      uint32_t mine = 0;                                           // key of slot `lane`
+      int n = 0;
+      uint32_t next = __reduce_max_sync(kAll, a);
+      auto pick = [&]() {
+        if (lane == n) mine = next;
+        if (a == next) {
+          a = b;
+          b = 0;
+          if (a == 0u) {
+#pragma unroll
+            for (int i = 0; i < EPL; ++i) push2(u[i] < next ? u[i] : 0u, a, b);
+          }
+        }
+        ++n;
+        next = __reduce_max_sync(kAll, a);
+      };
+      while (n < p.k && next != 0u) pick();
+      if (!exact_keys && n > 0 && !unsure) {
+        // Neighbours that lie within what a packed key leaves out and the error of the keys: take what else lies as
+        // close, and order all of it in 64 bits.  The bound holds for every key from the first to the one compared.
+        const float c0 = fabsf(order_value(__shfl_sync(kAll, mine, 0) & ~IDX));
+        const float fixed = biased ? 2.f * (err_s * smax + err_0) : 0.f, rel = biased ? 2.f * err_c : 0.f;
+        auto close = [&](uint32_t hi, uint32_t lo) {
+          const float l = order_value(lo | IDX);
+          return !(order_value(hi & ~IDX) - l > fixed + rel * 1.01f * fmaxf(c0, fabsf(l)));
+        };
+        const uint32_t after = __shfl_down_sync(kAll, mine, 1);
+        const uint32_t last0 = __shfl_sync(kAll, mine, n - 1);
+        const bool tail = next != 0u && close(last0, next);
+        if (__any_sync(kAll, lane + 1 < n && close(mine, after)) || tail) {
+          uint32_t last = last0;
+          while (n < 32 && next != 0u && close(last, next)) {
+            last = next;
+            pick();
+          }
+          if (next != 0u && close(last, next)) unsure = true;
+          if (!unsure) {
+            const double top = (double)zmax;
+            double sum = 1.0;
+            if (!SIGMOID && biased) {
+              sum = 0.0;
+#pragma unroll
+              for (int i = 0; i < EPL; ++i)
+                if (z[i] > low) sum += z[i] == zmax ? 1.0 : exp((double)z[i] - top);
+#pragma unroll
+              for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kAll, sum, o);
+            }
+            const int e = (int)(IDX - (mine & IDX));
+            double cd = 0.0;
+            if (lane < n) {
+              const float zf = to_f32(row[e]);
+              cd = (double)zf;
+              if (biased)
+                cd = (SIGMOID ? 1.0 / (1.0 + exp(-cd)) : (zf == zmax ? 1.0 : exp(cd - top)) / sum) + (double)p.bias[e];
+            }
+            int rank = 0;
+            for (int j = 0; j < n; ++j) {
+              const double oc = __shfl_sync(kAll, cd, j);
+              const int oe = __shfl_sync(kAll, e, j);
+              rank += oc > cd || (oc == cd && oe < e);
+            }
+            uint32_t* order = reinterpret_cast<uint32_t*>(keys_s[warp]);
+            __syncwarp();
+            if (lane < n) order[rank] = mine;
+            __syncwarp();
+            if (lane < n) mine = order[lane];
+            __syncwarp();
+          }
         }
       }
-      if (p.bias != nullptr) {
-        // neighbours in the order whose distance is within the error bound, and that are not equal by their inputs
-        const float zs = sel >= 0 ? to_f32(row[sel]) : low, bs = sel >= 0 ? p.bias[sel] : 0.f;
-        const float ss = sel >= 0 ? (SIGMOID ? sigmoid_rn(zs) : exp_below(zs, zmax) / total) : 0.f;
-        const float cs = ss + bs;
-        const float zn = __shfl_down_sync(kAll, zs, 1), bn = __shfl_down_sync(kAll, bs, 1);
-        const float sn = __shfl_down_sync(kAll, ss, 1), cn = __shfl_down_sync(kAll, cs, 1);
-        const int en = __shfl_down_sync(kAll, sel, 1);
-        if (lane < 31 && sel >= 0 && en >= 0 && !(zs == zn && bs == bn))
-          doubt |= !(cs - cn > err_s * (ss + sn) + 2.f * err_0 + err_c * (fabsf(cs) + fabsf(cn)));
-        // a 33rd neighbour is not compared: with k = 32 the last place is always settled in 64 bits
-        doubt |= p.k == 32 && p.E > 32;
-      }
-      if (__any_sync(kAll, doubt)) {
+      if (unsure) {
         __syncwarp();
         sel = choose_in_double<T, SIGMOID>(row, p, sum2, keys_s[warp], lane);
         __syncwarp();
+      } else if (lane < n && lane < p.k) {
+        sel = (int)(IDX - (mine & IDX));
       }
     } else if (p.scores != nullptr) {
       for (int e = lane; e < p.E; e += 32) p.scores[(size_t)t * p.E + e] = 0.f;
     }
-    // weights: lane j has slot j.  Renormalised weights are formed from exponentials shifted by the largest chosen
-    // logit, so they are a number even where every score underflows.
-    if (lane >= p.k) sel = -1;
+    // Weights: lane j has slot j.  Renormalised weights are formed from exponentials shifted by the largest chosen
+    // logit where their sum could underflow, so they are a number even where every score is 0.
     const bool have = sel >= 0;
     const float zs = have ? to_f32(row[sel]) : low;
     float w = 0.f;
     if (p.renorm) {
-      const float m = warp_max(zs);
-      if (SIGMOID) {
-        const float shift = fminf(m, 0.f);
-        if (have) w = zs > 0.f ? sigmoid_rn(zs) : expf(zs - shift) / (1.0f + expf(zs));
-      } else if (have) {
-        w = exp_below(zs, m);
+      if (SIGMOID && __any_sync(kAll, zs > -10.f)) {
+        if (have) w = sigmoid_rn(zs);
+      } else {
+        const float m = warp_max_of(zs);
+        if (have) w = SIGMOID ? expf(zs - m) / (1.0f + expf(zs)) : exp_below(zs, m);
       }
-      const float sum = warp_sum(w);
+      float sum = w;
+      for (int o = half_k; o > 0; o >>= 1) sum += __shfl_xor_sync(kAll, sum, o);
       if (have) w = w / sum * p.scale;
     } else if (have) {
       w = (SIGMOID ? sigmoid_rn(zs) : exp_below(zs, zmax) / total) * p.scale;
@@ -372,6 +467,10 @@ route_scored_backward_kernel(int Tn, int E, int k, int renorm, float scale, long
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int e0 = lane * EPL;
   const float low = -CUDART_INF_F;
+  __shared__ __align__(16) float add_s[kRsWarps][EPL * 32];
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) add_s[warp][i * 32 + lane] = 0.f;
+  __syncwarp();
   for (int t = blockIdx.x * kRsWarps + warp; t < Tn; t += gridDim.x * kRsWarps) {
     const T* row = logits + (long long)t * stride;
     int sel = -1;
@@ -388,7 +487,7 @@ route_scored_backward_kernel(int Tn, int E, int k, int renorm, float scale, long
     for (int i = 0; i < EPL; ++i) dz[i] = 0.f;
     float v = 0.f;
     if (renorm) {
-      const float m = warp_max(zs);
+      const float m = warp_max_of(zs);
       float pj = 0.f;
       if (SIGMOID) {
         if (have) pj = zs > 0.f ? sigmoid_rn(zs) : expf(zs - fminf(m, 0.f)) / (1.0f + expf(zs));
@@ -408,7 +507,7 @@ route_scored_backward_kernel(int Tn, int E, int k, int renorm, float scale, long
       float m = low;
 #pragma unroll
       for (int i = 0; i < EPL; ++i) m = fmaxf(m, z[i]);
-      m = warp_max(m);
+      m = warp_max_of(m);
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < EPL; ++i) {
@@ -417,18 +516,28 @@ route_scored_backward_kernel(int Tn, int E, int k, int renorm, float scale, long
       }
       sum = warp_sum(sum);
       const float s = have && sum > 0.f ? exp_below(zs, m) / sum : 0.f;
-      const float inner = scale * warp_sum(s * dw);
+      const float factor = sum > 0.f ? -scale * warp_sum(s * dw) / sum : 0.f;
 #pragma unroll
-      for (int i = 0; i < EPL; ++i) dz[i] = sum > 0.f ? -(dz[i] / sum) * inner : 0.f;
+      for (int i = 0; i < EPL; ++i) dz[i] *= factor;
       v = scale * s * dw;
     }
-    for (int j = 0; j < k; ++j) {
-      const int i0 = __shfl_sync(kAll, sel, j) - e0;
-      const float vj = __shfl_sync(kAll, v, j);
-#pragma unroll
-      for (int i = 0; i < EPL; ++i)
-        if (i == i0) dz[i] += vj;
+    // the chosen slots' values reach the lanes that own their experts through shared memory; an expert named in
+    // several slots gets their sum, in slot order
+    const unsigned same = __match_any_sync(kAll, sel);
+    if (__any_sync(kAll, have && __popc(same) > 1)) {
+      float acc = 0.f;
+      for (int j = 0; j < k; ++j) {
+        const float vj = __shfl_sync(kAll, v, j);
+        if ((same >> j) & 1u) acc += vj;
+      }
+      v = acc;
     }
+    if (have) add_s[warp][sel] = v;
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) dz[i] += add_s[warp][e0 + i];
+    __syncwarp();
+    if (have) add_s[warp][sel] = 0.f;
     T* out = dlogits + (long long)t * out_stride;
     constexpr int VN = Vec<T>::N;
     if (EPL >= VN && vec_out) {
@@ -468,18 +577,19 @@ bool row_vectors(const void* base, long long stride, int E, int esize) {
   return ((uintptr_t)base & 15) == 0 && stride * esize % 16 == 0 && E * esize % 16 == 0;
 }
 
-int row_blocks(int T) {
-  const int want = (T + kRsWarps - 1) / kRsWarps, most = 8 * sm_count();
+int row_blocks(int T, int warps, int per_sm) {
+  const int want = (T + warps - 1) / warps, most = per_sm * sm_count();
   return want < most ? want : most;
 }
 
 template <typename T, int EPL>
 cudaError_t launch_route_t(const btx_route_desc* d, const void* logits, RouteParams p, cudaStream_t st) {
   const int vec = row_vectors(logits, p.stride, p.E, sizeof(T)) ? 1 : 0;
-  int blocks = row_blocks(p.T);
-  // Counting: one block writes its own counts; more add theirs to zeros.  A block of 8 warps takes up to 16 rows
-  // on its own, which costs less than a second launch to clear the counts.
-  p.single_block = p.counts != nullptr && p.T <= 2 * kRsWarps;
+  constexpr int W = RouteWarps<EPL>::n;
+  int blocks = row_blocks(p.T, W, EPL <= 8 ? 2 : 4);
+  // Counting: one block writes its own counts; more add theirs to zeros.  One block takes up to 16 rows on
+  // its own, which costs less than a second launch to clear the counts.
+  p.single_block = p.counts != nullptr && p.T <= 16;
   if (p.single_block) blocks = 1;
   else if (p.counts != nullptr) {
     cudaError_t e = cudaMemsetAsync(p.counts, 0, (size_t)p.E * sizeof(int32_t), st);
@@ -487,9 +597,9 @@ cudaError_t launch_route_t(const btx_route_desc* d, const void* logits, RoutePar
   }
   const int sum2 = d->group_score == BTX_GROUP_SUM2;
   if (d->score == BTX_SCORE_SIGMOID)
-    route_scored_kernel<T, EPL, true><<<blocks, kRsWarps * 32, 0, st>>>((const T*)logits, p, sum2, vec);
+    route_scored_kernel<T, EPL, true><<<blocks, W * 32, 0, st>>>((const T*)logits, p, sum2, vec);
   else
-    route_scored_kernel<T, EPL, false><<<blocks, kRsWarps * 32, 0, st>>>((const T*)logits, p, sum2, vec);
+    route_scored_kernel<T, EPL, false><<<blocks, W * 32, 0, st>>>((const T*)logits, p, sum2, vec);
   return cudaGetLastError();
 }
 
@@ -498,10 +608,10 @@ cudaError_t launch_route_backward_t(const btx_route_desc* d, const void* logits,
                                     const float* dgates, void* dlogits, long long out_stride, cudaStream_t st) {
   const int vi = row_vectors(logits, stride, d->E, sizeof(T)), vo = row_vectors(dlogits, out_stride, d->E, sizeof(T));
   if (d->score == BTX_SCORE_SIGMOID)
-    route_scored_backward_kernel<T, EPL, true><<<row_blocks(d->T), kRsWarps * 32, 0, st>>>(
+    route_scored_backward_kernel<T, EPL, true><<<row_blocks(d->T, kRsWarps, 8), kRsWarps * 32, 0, st>>>(
         d->T, d->E, d->k, d->renorm != 0, d->scale, stride, vi, vo, (const T*)logits, topk_idx, dgates, (T*)dlogits, out_stride);
   else
-    route_scored_backward_kernel<T, EPL, false><<<row_blocks(d->T), kRsWarps * 32, 0, st>>>(
+    route_scored_backward_kernel<T, EPL, false><<<row_blocks(d->T, kRsWarps, 8), kRsWarps * 32, 0, st>>>(
         d->T, d->E, d->k, d->renorm != 0, d->scale, stride, vi, vo, (const T*)logits, topk_idx, dgates, (T*)dlogits, out_stride);
   return cudaGetLastError();
 }

@@ -147,7 +147,8 @@ def check_product(y, qa, qb):
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("shape", [(1, 1, 1, 32), (1, 1, 128, 64), (1, 128, 128, 256), (1, 5, 200, 96), (1, 129, 255, 160),
                                    (1, 300, 64, 1056), (2, 130, 136, 288), (3, 1, 1000, 512), (1, 1000, 17, 2048),
-                                   (1, 64, 4096, 4096), (1, 520, 2056, 544)], ids=lambda s: "x".join(map(str, s)))
+                                   (1, 64, 4096, 4096), (1, 520, 2056, 544),
+                                   (1, 2100, 2300, 320), (3, 1100, 1300, 96), (1, 4100, 1290, 2080)], ids=lambda s: "x".join(map(str, s)))
 def test_product(shape, dtype):
     batch, M, N, K = shape
     y, qa, qb = matmul(randn(batch, M, K, seed=M + K), randn(batch, N, K, seed=N + K + 1, std=0.02), dtype)
@@ -198,15 +199,19 @@ def moe_reference(x, idx, gates, w1, w3, w2):
     y, tol = np.zeros((T, d)), np.zeros((T, d))
     xq = o.mx4_round(x)
     F = w1.shape[1]
+    rounded = {}
     for t in range(T):
         for j in range(idx.shape[1]):
             e = idx[t, j]
             if e < 0 or e >= w1.shape[0]:
                 continue
-            u1, u3, u2 = o.mx4_round(w1[e]), o.mx4_round(w3[e]), o.mx4_round(w2[e])
+            if e not in rounded:
+                rounded[e] = o.mx4_round(w1[e]), o.mx4_round(w3[e]), o.mx4_round(w2[e])
+                rounded[e] += tuple(np.abs(u) for u in rounded[e])
+            u1, u3, u2, v1, v3, v2 = rounded[e]
             step = (d / 64 + 4) * 2.0 ** -22
             h1, h3 = u1 @ xq[t], u3 @ xq[t]
-            d1, d3 = step * (np.abs(u1) @ np.abs(xq[t])), step * (np.abs(u3) @ np.abs(xq[t]))
+            d1, d3 = step * (v1 @ np.abs(xq[t])), step * (v3 @ np.abs(xq[t]))
             silu = h1 / (1 + np.exp(-h1))
             a = silu * h3
             da = 1.1 * d1 * (np.abs(h3) + d3) + np.abs(silu) * d3 + 2.0 ** -19 * np.abs(a)   # |silu'| <= 1.1
@@ -223,9 +228,9 @@ def moe_reference(x, idx, gates, w1, w3, w2):
             casts = np.stack(casts)
             spread = (casts.max(0) - casts.min(0)).reshape(-1)
             act = o.mx4_round(a)
-            size = np.abs(u2) @ np.abs(act)
+            size = v2 @ np.abs(act)
             y[t] += gates[t, j] * (u2 @ act)
-            tol[t] += np.abs(gates[t, j]) * (np.abs(u2) @ spread + (F / 64 + 8) * 2.0 ** -22 * size)
+            tol[t] += np.abs(gates[t, j]) * (v2 @ spread + (F / 64 + 8) * 2.0 ** -22 * size)
     return y, tol
 
 
@@ -248,7 +253,8 @@ def moe(x, idx, gates, w1, w3, w2, dst=None):
 
 # (T, d, F, E, k, empty)
 LAYERS = [(1, 128, 160, 4, 2, 0.0), (5, 64, 32, 3, 1, 0.0), (33, 96, 224, 4, 2, 0.3), (150, 256, 288, 2, 2, 0.0),
-          (40, 160, 96, 40, 6, 0.0), (7, 32, 64, 512, 8, 0.0), (300, 64, 96, 1, 1, 0.1), (1100, 32, 64, 7, 3, 0.05)]
+          (40, 160, 96, 40, 6, 0.0), (7, 32, 64, 512, 8, 0.0), (300, 64, 96, 1, 1, 0.1), (1100, 32, 64, 7, 3, 0.05),
+          (3000, 1056, 160, 2, 2, 0.05), (2500, 544, 1184, 5, 3, 0.0)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
@@ -295,6 +301,18 @@ def test_layer_is_the_same_whatever_shares_its_batch():
         assert torch.equal(part, big[a:b])
     again, _ = moe(x, idx, gates, w1, w3, w2)
     assert torch.equal(again, big)
+
+
+def test_large_tiles_give_the_rows_of_small_ones():
+    # enough rows per expert for products by CTA pairs; the parts are too small for them
+    T, d, F, E, k = 4000, 1280, 320, 3, 2
+    x = randn(T, d, seed=2, dtype=torch.bfloat16)
+    w1, w3, w2 = (randn(E, *s, seed=i, std=0.2) for i, s in enumerate([(F, d), (F, d), (d, F)]))
+    idx, gates = random_routing(T, E, k, 8, 0.1)
+    big, _ = moe(x, idx, gates, w1, w3, w2)
+    for a, b in ((0, 1), (100, 300), (3990, 4000)):
+        part, _ = moe(x[a:b].contiguous(), idx[a:b].contiguous(), gates[a:b].contiguous(), w1, w3, w2)
+        assert torch.equal(part, big[a:b])
 
 
 def test_route_then_layer_on_a_stream_and_in_a_graph():
