@@ -105,6 +105,11 @@ __device__ __forceinline__ void arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
+// A bounded wait of a whole warp: it gives up for all lanes or for none.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* status) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, status));
+}
+
 struct Item { int mt, nt, b, e; };
 
 // Tile number -> (row tile, column tile): groups of GROUP_N column tiles, rows advance slowest inside a group.
@@ -123,27 +128,45 @@ __device__ __forceinline__ Item get_item(const Params& p, int m_tiles, int t) {
   return it;
 }
 
-// 64 accumulator columns of one row per thread (columns n0 .. n0 + 63 of the product), by a whole warp.  m: the row of
-// A; flat: its row of y (STORE) or its assignment, -1 for a row that nobody asked for.
+// 64 accumulator columns of one row per thread, by a whole warp
+__device__ __forceinline__ void load_chunk(uint32_t taddr, float (&v)[64]) {
+  uint32_t r[64];
+  __syncwarp();                                           // the tensor-memory load needs the whole warp
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[32 * h + 0]), "=r"(r[32 * h + 1]), "=r"(r[32 * h + 2]), "=r"(r[32 * h + 3]), "=r"(r[32 * h + 4]),
+          "=r"(r[32 * h + 5]), "=r"(r[32 * h + 6]), "=r"(r[32 * h + 7]), "=r"(r[32 * h + 8]), "=r"(r[32 * h + 9]),
+          "=r"(r[32 * h + 10]), "=r"(r[32 * h + 11]), "=r"(r[32 * h + 12]), "=r"(r[32 * h + 13]), "=r"(r[32 * h + 14]),
+          "=r"(r[32 * h + 15]), "=r"(r[32 * h + 16]), "=r"(r[32 * h + 17]), "=r"(r[32 * h + 18]), "=r"(r[32 * h + 19]),
+          "=r"(r[32 * h + 20]), "=r"(r[32 * h + 21]), "=r"(r[32 * h + 22]), "=r"(r[32 * h + 23]), "=r"(r[32 * h + 24]),
+          "=r"(r[32 * h + 25]), "=r"(r[32 * h + 26]), "=r"(r[32 * h + 27]), "=r"(r[32 * h + 28]), "=r"(r[32 * h + 29]),
+          "=r"(r[32 * h + 30]), "=r"(r[32 * h + 31])
+        : "r"(taddr + 32 * h));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 64; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+// What becomes of them (columns n0 .. n0 + 63 of the product).  m: the row of A; flat: its row of y (STORE) or its
+// assignment, -1 for a row that nobody asked for.
 template <int MODE>
-__device__ __forceinline__ void epilogue_chunk(const Params& p, const Item& it, uint32_t taddr, int n0, int m, int flat) {
+__device__ __forceinline__ void finish_chunk(const Params& p, const Item& it, float (&v)[64], int n0, int m, int flat) {
+  if (flat < 0 || n0 >= (MODE == GATE_UP ? (p.N + 255) / 256 * 256 : p.N)) return;
   const bool wide = p.wide != 0;
-  float v[32];
   if constexpr (MODE == GATE_UP) {
     const int F = p.N / 2;
     const int f0 = n0 / 2;                                // 32 hidden units: one block
     float a[32];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      __syncwarp();                                       // the tensor-memory load needs the whole warp
-      tc_ld32(taddr + 32 * h, v);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) a[16 * h + i] = fast_swiglu(v[2 * i], v[2 * i + 1]);
-    }
-    if (flat < 0) return;
     uint32_t amax = 0;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) amax = max(amax, __float_as_uint(a[i]) & 0x7fffffffu);
+    for (int i = 0; i < 32; ++i) {
+      a[i] = fast_swiglu(v[2 * i], v[2 * i + 1]);
+      amax = max(amax, __float_as_uint(a[i]) & 0x7fffffffu);
+    }
     float inv;
     uint32_t byte = scale_byte(amax, inv);
     uint32_t w[4] = {0, 0, 0, 0};
@@ -160,38 +183,31 @@ __device__ __forceinline__ void epilogue_chunk(const Params& p, const Item& it, 
       p.act_scales[((size_t)(m / kTileRows) * akt + blk / 4) * kTileBytes + (m & 31) * 16 + (m >> 5 & 3) * 4 + (blk & 3)] = (uint8_t)byte;
     if (f0 < F) *reinterpret_cast<uint4*>(p.act_codes + (size_t)m * (F / 2) + f0 / 2) = make_uint4(w[0], w[1], w[2], w[3]);
   } else {
-    const float g = MODE == DOWN && flat >= 0 ? p.gates[flat] : 1.f;
+    const size_t o = MODE == STORE ? ((size_t)it.b * p.M + flat) * p.N + n0 : (size_t)flat * p.N + n0;
+    if (MODE == DOWN) {
+      const float g = p.gates[flat];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      __syncwarp();
-      tc_ld32(taddr + 32 * h, v);
-      const int col = n0 + 32 * h;
-      if (flat < 0 || col >= p.N) continue;
-      const size_t o = MODE == STORE ? ((size_t)it.b * p.M + flat) * p.N + col : (size_t)flat * p.N + col;
-      if (MODE == STORE && p.out_bf16) {
-        __nv_bfloat16* y = (__nv_bfloat16*)p.y + o;
-        if (wide && col + 32 <= p.N) {
-          st32(y, pack8(v), pack8(v + 8), true);
-          st32(y + 16, pack8(v + 16), pack8(v + 24), true);
-        } else {
+      for (int i = 0; i < 64; ++i) v[i] *= g;
+    }
+    if (MODE == STORE && p.out_bf16) {
+      __nv_bfloat16* y = (__nv_bfloat16*)p.y + o;
+      if (wide && n0 + 64 <= p.N) {
 #pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if (col + i < p.N) y[i] = __float2bfloat16_rn(v[i]);
-        }
+        for (int i = 0; i < 64; i += 16) st32(y + i, pack8(v + i), pack8(v + i + 8), true);
       } else {
-        float* y = (float*)p.y + o;
-        if (MODE == DOWN) {
 #pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] *= g;
-        }
-        if (MODE == DOWN || (wide && col + 32 <= p.N)) {  // DOWN: rows of a multiple of 32 columns
+        for (int i = 0; i < 64; ++i)
+          if (n0 + i < p.N) y[i] = __float2bfloat16_rn(v[i]);
+      }
+    } else {
+      float* y = (float*)p.y + o;
+      if (wide && n0 + 64 <= p.N) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) st32(y + 8 * i, f4(v + 8 * i), f4(v + 8 * i + 4), wide);
-        } else {
+        for (int i = 0; i < 64; i += 8) st32(y + i, f4(v + i), f4(v + i + 4), true);
+      } else {
 #pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if (col + i < p.N) y[i] = v[i];
-        }
+        for (int i = 0; i < 64; ++i)
+          if (n0 + i < p.N) y[i] = v[i];
       }
     }
   }
@@ -317,17 +333,16 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
       const int m = it.mt * BM + row;
       const int flat = MODE == STORE ? (m < p.M ? m : -1) : p.rowmap[m];
       const bool any = __any_sync(0xffffffffu, flat >= 0);
-      if (!(ok = mbar_wait(bar_tfull + acc * 8, acc_phase, abort_flag, p.status))) break;
+      if (!(ok = warp_wait(bar_tfull + acc * 8, acc_phase, abort_flag, p.status))) break;
       tc_fence_after();
       const uint32_t taddr = tmem + acc * BN + half * HC + ((uint32_t)(q * 32) << 16);
       const int n0 = it.nt * BN + half * HC;
-      if (any) {
-#pragma unroll 1
-        for (int c = 0; c < HC; c += 64) epilogue_chunk<MODE>(p, it, taddr + c, n0 + c, m, flat);
-      }
-      __syncwarp();
+      static_assert(HC == 64, "one chunk per warp");
+      float v[64];
+      if (any) load_chunk(taddr, v);
       tc_fence_before();
-      arrive(bar_tempty + acc * 8);
+      arrive(bar_tempty + acc * 8);                       // the accumulator is read: the next tile may have it
+      if (any) finish_chunk<MODE>(p, it, v, n0, m, flat);
       acc ^= 1u;
       if (acc == 0) acc_phase ^= 1u;
     }
@@ -344,23 +359,24 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
 // Two CTAs on one 256 x 256 tile (cta_group::2)
 // ---------------------------------------------------------------------------------------------
 // A stage brings 128 rows of A and 128 of the 256 rows of B per CTA, half of what two CTAs with tiles of their own
-// would fetch for the same products: the 128 x 128 tiles above fetch 15.6 bytes per 1000 products and stop at the L2's
-// bandwidth (2.5 PFLOP/s at M = 8192, N = 11008, K = 4096).
+// would fetch for the same products.
+// Scales: tcgen05.cp runs in the pipe of the MMAs and took 37 ns a tile of 512 bytes, six of them 220 ns beside the
+// 384 ns of a stage's MMAs.  Four warps store the scales instead (tcgen05.st, a warp per 32-lane quarter): they read
+// the stored tiles from global memory, 16 bytes per lane and tile, two stages ahead, and keep up to five stages of
+// scales in tensor memory.  M = 8192, N = 11008, K = 11008: 519 us with the copies.
 // Tensor memory: an accumulator takes 256 of the 512 columns, so two do not fit beside the scales whole.  They
-// overlap in 64 columns: 0..255 and 192..447.  The epilogue reads the shared columns of a tile first and then hands
-// them over, so the next tile starts after a quarter of it.  The remaining columns hold the scales of two stages; a
-// stage's scales are copied once the MMAs of the stage before the last have retired.
-//   warp 0   TMA of A and its scales   warp 10  TMA of B and its scales (two threads: an operation costs its thread
-//   about 80 ns, four of them more than the 270 ns that the MMAs of a stage take)
-//   warp 1   MMAs (one lane of the leader CTA)   warps 2-9  epilogue, 64-column chunks: of the two warps of a lane
-//   quarter the first takes the shared chunk and the one at the other end, the second the two between
-constexpr int P_STAGES = 6;
-constexpr int P_B_BYTES = 128 * SK / 2, P_SFB_BYTES = 2 * 2 * kTileBytes;
-constexpr int P_STAGE_BYTES = A_BYTES + P_B_BYTES + SFA_BYTES + P_SFB_BYTES;
+// overlap in 128 columns: 0..255 and 128..383.  The epilogue reads the shared columns of a tile into registers first
+// and hands them over, so the next tile starts before anything is computed or stored.
+//   warp 0  TMA   warp 1  MMAs (one lane of the leader CTA)   warps 2-9  epilogue, two 64-column chunks each
+//   warps 10-13  scales
+constexpr int P_STAGES = 7;
+constexpr int P_B_BYTES = 128 * SK / 2;
+constexpr int P_STAGE_BYTES = A_BYTES + P_B_BYTES;
 constexpr int P_SMEM = P_STAGES * P_STAGE_BYTES + 1024 + 256;
-constexpr int P_THREADS = THREADS + 32;
-constexpr int P_ACC1 = 192, P_SF0 = 448, P_SF_COLS = 24;
-static_assert(P_SF0 + 2 * P_SF_COLS <= 512 && P_ACC1 + 256 <= P_SF0, "tensor memory");
+constexpr int P_THREADS = THREADS + 128;
+constexpr int P_ACC1 = 128, P_SF0 = 384, P_SF_COLS = 24, P_SF_SLOTS = 5;
+static_assert(P_SF0 + P_SF_SLOTS * P_SF_COLS <= 512 && P_ACC1 + 256 <= P_SF0, "tensor memory");
+static_assert(P_STAGES * 16 + P_SF_SLOTS * 8 + 40 <= 256, "barriers fit behind the ring");
 
 __device__ __forceinline__ void mma_mxf4_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
                                               uint32_t accum) {
@@ -370,31 +386,38 @@ __device__ __forceinline__ void mma_mxf4_pair(uint32_t d, uint64_t a, uint64_t b
       "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
       ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accum) : "memory");
 }
-// in both CTAs, each from its own shared memory to its own tensor memory
-__device__ __forceinline__ void copy_scales_pair(uint32_t tmem, uint32_t smem) {
-  const uint64_t desc = (uint64_t)((smem & 0x3FFFFu) >> 4) | ((uint64_t)(128 >> 4) << 16) | ((uint64_t)(128 >> 4) << 32) |
-                        (1ull << 46);
-  asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+__device__ __forceinline__ void store_scales(uint32_t taddr, const uint4& lo, const uint4& hi) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"r"(taddr), "r"(lo.x), "r"(lo.y), "r"(lo.z), "r"(lo.w), "r"(hi.x), "r"(hi.y), "r"(hi.z), "r"(hi.w) : "memory");
 }
+
+// The steps (tile, K stage) of a CTA pair in order, for the warps that bring the scales.
+struct ScaleCursor {
+  const uint8_t *a, *b;             // this lane's 16 bytes of the first tile along K
+  int t, kb;
+  bool second_b;                    // columns 128 .. 255 of the tile have scales
+  bool live;
+};
 
 template <int MODE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
-mx4_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
-                     const __grid_constant__ CUtensorMap tmSA, const __grid_constant__ CUtensorMap tmSB, const Params p) {
+mx4_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const Params p) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t ring = (raw + 1023u) & ~1023u;
   uint8_t* ctl = smem_raw + (ring - raw) + P_STAGES * P_STAGE_BYTES;
   const uint32_t bar_full = smem_u32(ctl), bar_empty = bar_full + P_STAGES * 8;
-  const uint32_t bar_tfull = bar_empty + P_STAGES * 8, bar_handed = bar_tfull + 16;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctl + P_STAGES * 16 + 32);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(ctl + P_STAGES * 16 + 40);
+  const uint32_t bar_scales = bar_empty + P_STAGES * 8;                 // used in the leader
+  const uint32_t bar_tfull = bar_scales + P_SF_SLOTS * 8, bar_handed = bar_tfull + 16;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctl + P_STAGES * 16 + P_SF_SLOTS * 8 + 24);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < P_STAGES; ++s) { mbar_init(bar_full + s * 8, 1); mbar_init(bar_empty + s * 8, 1); }
+    for (int s = 0; s < P_SF_SLOTS; ++s) mbar_init(bar_scales + s * 8, 8);
     for (int a = 0; a < 2; ++a) mbar_init(bar_tfull + a * 8, 1);
     mbar_init(bar_handed, 2 * EPI_WARPS);
     *abort_flag = 0;
@@ -417,28 +440,21 @@ mx4_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
   const int n_total = m_tiles * p.n_tiles * p.batch;
   const int kb_total = (p.K + SK - 1) / SK;
 
-  if (warp == 0 || warp == 10) {
+  if (warp == 0) {
     if (lane == 0) {
-      const bool a_side = warp == 0;
       uint32_t stage = 0, phase = 0;
       bool ok = true;
       for (int t = pair; t < n_total && ok; t += n_pairs) {
         const Item it = get_item(p, m_tiles, t);
-        const int row0 = it.mt * 256 + (int)rank * 128;
-        const int sfa_row = it.b * p.a_row_tiles + it.mt * 2 + (int)rank, sfb_row = it.e * p.b_row_tiles + it.nt * 2;
+        const int row0 = it.mt * 256 + (int)rank * 128, col0 = it.nt * 256 + (int)rank * 128;
         for (int kb = 0; kb < kb_total; ++kb) {
           if (!(ok = mbar_wait(bar_empty + stage * 8, phase ^ 1u, abort_flag, p.status))) break;
           const uint32_t full_local = bar_full + stage * 8;
           const uint32_t full = map_to_cta(full_local, 0);
-          const uint32_t sA = ring + stage * P_STAGE_BYTES, sB = sA + A_BYTES, sSA = sB + P_B_BYTES, sSB = sSA + SFA_BYTES;
-          if (a_side) {
-            if (rank == 0) mbar_expect_tx(full_local, 2 * P_STAGE_BYTES);
-            tma_load_3d(sA, &tmA, kb * (SK / 2), row0, it.b, full);
-            tma_load_3d(sSA, &tmSA, 0, kb * 2, sfa_row, full);
-          } else {
-            tma_load_3d(sB, &tmB, kb * (SK / 2), it.nt * 256 + (int)rank * 128, it.e, full);
-            tma_load_3d(sSB, &tmSB, 0, kb * 2, sfb_row, full);
-          }
+          const uint32_t sA = ring + stage * P_STAGE_BYTES, sB = sA + A_BYTES;
+          if (rank == 0) mbar_expect_tx(full_local, 2 * P_STAGE_BYTES);
+          tma_load_3d(sA, &tmA, kb * (SK / 2), row0, it.b, full);
+          tma_load_3d(sB, &tmB, kb * (SK / 2), col0, it.e, full);
           if (++stage == P_STAGES) { stage = 0; phase ^= 1u; }
         }
       }
@@ -450,34 +466,21 @@ mx4_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
       constexpr uint32_t idesc0 = (1u << 7) | (1u << 10) | ((uint32_t)(256 >> 3) << 17) | (1u << 23) | ((uint32_t)(256 >> 4) << 24);
-      uint32_t stage = 0, phase = 0, acc = 0, tile = 0, slot = 0;
-      uint32_t ret_stage = 0, ret_phase = 0, steps = 0;   // the step whose scale columns are taken over next
+      uint32_t stage = 0, phase = 0, acc = 0, tile = 0, slot = 0, slot_phase = 0;
       bool ok = true;
       for (int t = pair; t < n_total && ok; t += n_pairs, ++tile) {
-        // the tile before has handed over the shared columns (and the one before that everything)
+        // the tile before has handed over the shared columns
         if (tile > 0 && !(ok = mbar_wait(bar_handed, (tile - 1) & 1u, abort_flag, p.status))) break;
         tc_fence_after();
         const uint32_t d = tmem + (acc ? P_ACC1 : 0);
         for (int kb = 0; kb < kb_total; ++kb) {
+          if (!(ok = mbar_wait(bar_scales + slot * 8, slot_phase, abort_flag, p.status))) break;
           if (!(ok = mbar_wait(bar_full + stage * 8, phase, abort_flag, p.status))) break;
-          if (steps >= 2) {
-            if (!(ok = mbar_wait(bar_empty + ret_stage * 8, ret_phase, abort_flag, p.status))) break;
-            if (++ret_stage == P_STAGES) { ret_stage = 0; ret_phase ^= 1u; }
-          }
-          ++steps;
           tc_fence_after();
-          const uint32_t sA = ring + stage * P_STAGE_BYTES, sB = sA + A_BYTES, sSA = sB + P_B_BYTES, sSB = sSA + SFA_BYTES;
+          const uint32_t sA = ring + stage * P_STAGE_BYTES, sB = sA + A_BYTES;
           const uint32_t tA = tmem + P_SF0 + slot * P_SF_COLS, tB = tA + 8;
-          slot ^= 1u;
+          if (++slot == P_SF_SLOTS) { slot = 0; slot_phase ^= 1u; }
           const int k64 = min(SK / 64, (p.K - kb * SK + 63) / 64);
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            if (2 * c < k64) {
-              copy_scales_pair(tA + c * 4, sSA + c * kTileBytes);
-              copy_scales_pair(tB + c * 8, sSB + c * kTileBytes);
-              copy_scales_pair(tB + c * 8 + 4, sSB + (2 + c) * kTileBytes);
-            }
-          }
           const uint64_t da = smem_desc(sA, false), db = smem_desc(sB, false);
 #pragma unroll
           for (int j = 0; j < SK / 64; ++j) {
@@ -495,6 +498,69 @@ mx4_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
         acc ^= 1u;
       }
     }
+  } else if (warp >= 2 + EPI_WARPS) {
+    // ---- scales: rows c * 32 + lane of a tile are word c of the lane's 16 bytes, and column c of tensor memory ----
+    const uint32_t taddr = tmem + P_SF0 + ((uint32_t)((warp & 3) * 32) << 16);
+    const uint32_t ready = map_to_cta(bar_scales, 0);
+    ScaleCursor cur = {};
+    auto seek = [&]() {
+      cur.live = cur.t < n_total;
+      if (!cur.live) return;
+      const Item it = get_item(p, m_tiles, cur.t);
+      cur.a = p.a_scales + ((size_t)(it.b * p.a_row_tiles + it.mt * 2 + (int)rank) * p.kt) * kTileBytes + lane * 16;
+      cur.b = p.b_scales + ((size_t)((size_t)it.e * p.b_row_tiles + it.nt * 2) * p.kt) * kTileBytes + lane * 16;
+      // the tile's second half may hold no row of A (its outputs are dropped) or lie past the last column
+      if (it.mt * 2 + (int)rank >= p.a_row_tiles) cur.a = nullptr;
+      cur.second_b = it.nt * 2 + 1 < p.b_row_tiles;
+      cur.kb = 0;
+    };
+    cur.t = pair;
+    seek();
+    auto fetch = [&](uint4 (&r)[6]) {                    // the current step's scales, and on to the next step
+      const bool live = cur.live;
+#pragma unroll
+      for (int i = 0; i < 6; ++i) r[i] = make_uint4(0, 0, 0, 0);
+      if (live) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const size_t o = (size_t)(cur.kb * 2 + c) * kTileBytes;
+          if (cur.kb * 2 + c < p.kt) {
+            if (cur.a != nullptr) r[c] = *reinterpret_cast<const uint4*>(cur.a + o);
+            r[2 + 2 * c] = *reinterpret_cast<const uint4*>(cur.b + o);
+            if (cur.second_b) r[3 + 2 * c] = *reinterpret_cast<const uint4*>(cur.b + (size_t)p.kt * kTileBytes + o);
+          }
+        }
+        if (++cur.kb == kb_total) { cur.t += n_pairs; seek(); }
+      }
+      return live;
+    };
+    uint32_t slot = 0, steps = 0, ret_stage = 0, ret_phase = 0;
+    auto put = [&](const uint4 (&r)[6]) {
+      if (steps >= P_SF_SLOTS) {                         // the MMAs that read this slot's last scales have retired
+        if (!warp_wait(bar_empty + ret_stage * 8, ret_phase, abort_flag, p.status)) return false;
+        if (++ret_stage == P_STAGES) { ret_stage = 0; ret_phase ^= 1u; }
+        tc_fence_after();
+      }
+      ++steps;
+      __syncwarp();
+      const uint32_t to = taddr + slot * P_SF_COLS;
+      store_scales(to, r[0], r[1]);
+      store_scales(to + 8, r[2], r[3]);
+      store_scales(to + 16, r[4], r[5]);
+      asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+      tc_fence_before();
+      if (lane == 0) mbar_arrive_cluster(ready + slot * 8);
+      if (++slot == P_SF_SLOTS) slot = 0;
+      return true;
+    };
+    uint4 r0[6], r1[6];
+    bool live0 = fetch(r0), live1 = fetch(r1);
+    while (live0) {
+      if (!put(r0)) break;
+      live0 = fetch(r0);
+      if (!live1 || !put(r1)) break;
+      live1 = fetch(r1);
+    }
   } else {
     const int q = warp & 3, half = (warp - 2) >> 2;
     const int row = q * 32 + lane;
@@ -506,24 +572,20 @@ mx4_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
       const int m = it.mt * 256 + (int)rank * 128 + row;
       const int flat = MODE == STORE ? (m < p.M ? m : -1) : p.rowmap[m];
       const bool any = __any_sync(0xffffffffu, flat >= 0);
-      if (!(ok = mbar_wait(bar_tfull + acc * 8, acc_phase, abort_flag, p.status))) break;
+      if (!(ok = warp_wait(bar_tfull + acc * 8, acc_phase, abort_flag, p.status))) break;
       tc_fence_after();
       const uint32_t taddr = tmem + (acc ? P_ACC1 : 0) + ((uint32_t)(q * 32) << 16);
       const int n0 = it.nt * 256;
-      // chunk 3 of the accumulator at 0 and chunk 0 of the one at 192 are the same columns
-      const int shared_chunk = acc ? 0 : 3;
-      if (half == 1) {                                    // everything of the tile before is read
-        if (lane == 0) mbar_arrive_cluster(handed);
-        if (any) {
-          epilogue_chunk<MODE>(p, it, taddr + 64, n0 + 64, m, flat);
-          epilogue_chunk<MODE>(p, it, taddr + 128, n0 + 128, m, flat);
-        }
-      } else {
-        if (any) epilogue_chunk<MODE>(p, it, taddr + shared_chunk * 64, n0 + shared_chunk * 64, m, flat);
-        __syncwarp();
-        tc_fence_before();
-        if (lane == 0) mbar_arrive_cluster(handed);
-        if (any) epilogue_chunk<MODE>(p, it, taddr + (3 - shared_chunk) * 64, n0 + (3 - shared_chunk) * 64, m, flat);
+      // columns 128 .. 255 of tensor memory belong to both accumulators: chunks 2, 3 of the one at 0 and 0, 1 of the other
+      const int c0 = (acc ? 0 : 2) + half, c1 = (acc ? 2 : 0) + half;
+      float v[64];
+      if (any) load_chunk(taddr + c0 * 64, v);
+      tc_fence_before();
+      if (lane == 0) mbar_arrive_cluster(handed);         // (and all of the tile before has been read)
+      if (any) finish_chunk<MODE>(p, it, v, n0 + c0 * 64, m, flat);
+      if (any) {
+        load_chunk(taddr + c1 * 64, v);
+        finish_chunk<MODE>(p, it, v, n0 + c1 * 64, m, flat);
       }
       __syncwarp();
       tc_fence_before();
@@ -552,18 +614,6 @@ bool make_codes_map(CUtensorMap* m, const void* base, long long K, long long row
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// scale tiles [row tiles][kt][512 bytes] of all matrices, box of two tiles along K x box_tiles row tiles
-bool make_scales_map(CUtensorMap* m, const void* base, long long kt, long long row_tiles, uint32_t box_tiles) {
-  EncodeTiledFn fn = encode_fn();
-  if (!fn) return false;
-  cuuint64_t dims[3] = {kTileBytes / 4, (cuuint64_t)kt, (cuuint64_t)row_tiles};
-  cuuint64_t strides[2] = {kTileBytes, (cuuint64_t)(kt * kTileBytes)};
-  cuuint32_t box[3] = {kTileBytes / 4, 2, box_tiles};
-  cuuint32_t estr[3] = {1, 1, 1};
-  return fn(m, CU_TENSOR_MAP_DATA_TYPE_INT32, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 // once per device and kernel: the attribute outlives the call
 bool allow_smem(const void* kernel, int bytes, std::atomic<uint64_t>& done) {
   int dev = 0;
@@ -590,18 +640,16 @@ btx_status launch(const GemmArgs& g, Params p, long long max_items, cudaStream_t
 template <int MODE>
 btx_status launch_pair(const GemmArgs& g, Params p, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
-  CUtensorMap a, b, sa, sb;
+  CUtensorMap a, b;
   p.m_tiles = (g.M + 255) / 256; p.n_tiles = (g.N + 255) / 256; p.tile_step = 2;
   if (!make_codes_map(&a, g.a_codes, g.K, g.M, g.batch, 128) || !make_codes_map(&b, g.b_codes, g.K, g.N, g.experts, 128) ||
-      !make_scales_map(&sa, g.a_scales, p.kt, (long long)p.a_row_tiles * g.batch, 1) ||
-      !make_scales_map(&sb, g.b_scales, p.kt, (long long)p.b_row_tiles * g.experts, 2) ||
       !allow_smem((const void*)mx4_gemm_pair_kernel<MODE>, P_SMEM, done))
     return BTX_ERR_CUDA;
   const long long items = (long long)p.m_tiles * p.n_tiles * p.batch;
   int pairs = sm_count() / 2;
   if (items < pairs) pairs = (int)items;
-  return launch_after_predecessor(mx4_gemm_pair_kernel<MODE>, dim3(2 * pairs), dim3(P_THREADS), P_SMEM, st, MODE != STORE, a, b, sa,
-                                  sb, p) == cudaSuccess ? BTX_OK : BTX_ERR_CUDA;
+  return launch_after_predecessor(mx4_gemm_pair_kernel<MODE>, dim3(2 * pairs), dim3(P_THREADS), P_SMEM, st, MODE != STORE, a, b,
+                                  p) == cudaSuccess ? BTX_OK : BTX_ERR_CUDA;
 }
 
 Params base_params(const GemmArgs& g, int bn) {
