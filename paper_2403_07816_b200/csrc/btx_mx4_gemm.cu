@@ -110,6 +110,12 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, status));
 }
 
+__device__ __forceinline__ uint4 ld_shared_v4(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared::cta.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+
 struct Item { int mt, nt, b, e; };
 
 // Tile number -> (row tile, column tile): groups of GROUP_N column tiles, rows advance slowest inside a group.
@@ -361,22 +367,24 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
 // A stage brings 128 rows of A and 128 of the 256 rows of B per CTA, half of what two CTAs with tiles of their own
 // would fetch for the same products.
 // Scales: tcgen05.cp runs in the pipe of the MMAs and took 37 ns a tile of 512 bytes, six of them 220 ns beside the
-// 384 ns of a stage's MMAs.  Four warps store the scales instead (tcgen05.st, a warp per 32-lane quarter): they read
-// the stored tiles from global memory, 16 bytes per lane and tile, two stages ahead, and keep up to five stages of
-// scales in tensor memory.  M = 8192, N = 11008, K = 11008: 519 us with the copies.
+// 384 ns of a stage's MMAs.  Four warps store the scales instead (tcgen05.st, a warp per 32-lane quarter) from a ring
+// of their own in shared memory, and keep up to five stages of scales in tensor memory.  M = 8192, N = 11008,
+// K = 11008: 519 us with the copies, 415 us with the four warps reading the tiles from global memory four stages
+// ahead (every warp its own copy: a third more traffic from L2), 386 us with the ring.
 // Tensor memory: an accumulator takes 256 of the 512 columns, so two do not fit beside the scales whole.  They
 // overlap in 128 columns: 0..255 and 128..383.  The epilogue reads the shared columns of a tile into registers first
 // and hands them over, so the next tile starts before anything is computed or stored.
 //   warp 0  TMA   warp 1  MMAs (one lane of the leader CTA)   warps 2-9  epilogue, two 64-column chunks each
-//   warps 10-13  scales
-constexpr int P_STAGES = 7;
+//   warps 10-13  scales   warp 14  TMA of the scales
+constexpr int P_STAGES = 6, P_RING = 8;                  // stages of codes, of scales
 constexpr int P_B_BYTES = 128 * SK / 2;
 constexpr int P_STAGE_BYTES = A_BYTES + P_B_BYTES;
-constexpr int P_SMEM = P_STAGES * P_STAGE_BYTES + 1024 + 256;
-constexpr int P_THREADS = THREADS + 128;
+constexpr int P_SCALE_BYTES = 6 * kTileBytes;            // of a stage and CTA: two tiles of A, two of each half of B
+constexpr int P_SMEM = P_STAGES * P_STAGE_BYTES + P_RING * P_SCALE_BYTES + 1024 + 384;
+constexpr int P_THREADS = THREADS + 160;
 constexpr int P_ACC1 = 128, P_SF0 = 384, P_SF_COLS = 24, P_SF_SLOTS = 5;
 static_assert(P_SF0 + P_SF_SLOTS * P_SF_COLS <= 512 && P_ACC1 + 256 <= P_SF0, "tensor memory");
-static_assert(P_STAGES * 16 + P_SF_SLOTS * 8 + 40 <= 256, "barriers fit behind the ring");
+static_assert(P_STAGES * 16 + P_SF_SLOTS * 8 + P_RING * 16 + 40 <= 384 && P_SMEM <= 227 * 1024, "shared memory");
 
 __device__ __forceinline__ void mma_mxf4_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
                                               uint32_t accum) {
@@ -391,25 +399,20 @@ __device__ __forceinline__ void store_scales(uint32_t taddr, const uint4& lo, co
                ::"r"(taddr), "r"(lo.x), "r"(lo.y), "r"(lo.z), "r"(lo.w), "r"(hi.x), "r"(hi.y), "r"(hi.z), "r"(hi.w) : "memory");
 }
 
-// The steps (tile, K stage) of a CTA pair in order, for the warps that bring the scales.
-struct ScaleCursor {
-  const uint8_t *a, *b;             // this lane's 16 bytes of the first tile along K
-  int t, kb;
-  bool second_b;                    // columns 128 .. 255 of the tile have scales
-  bool live;
-};
-
 template <int MODE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
-mx4_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const Params p) {
+mx4_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                     const __grid_constant__ CUtensorMap tmSA, const __grid_constant__ CUtensorMap tmSB, const Params p) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t ring = (raw + 1023u) & ~1023u;
-  uint8_t* ctl = smem_raw + (ring - raw) + P_STAGES * P_STAGE_BYTES;
+  const uint32_t sf_ring = ring + P_STAGES * P_STAGE_BYTES;
+  uint8_t* ctl = smem_raw + (sf_ring - raw) + P_RING * P_SCALE_BYTES;
   const uint32_t bar_full = smem_u32(ctl), bar_empty = bar_full + P_STAGES * 8;
   const uint32_t bar_scales = bar_empty + P_STAGES * 8;                 // used in the leader
   const uint32_t bar_tfull = bar_scales + P_SF_SLOTS * 8, bar_handed = bar_tfull + 16;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctl + P_STAGES * 16 + P_SF_SLOTS * 8 + 24);
+  const uint32_t bar_sfull = bar_handed + 8, bar_sempty = bar_sfull + P_RING * 8;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctl + P_STAGES * 16 + P_SF_SLOTS * 8 + 24 + P_RING * 16);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
@@ -418,6 +421,7 @@ mx4_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
   if (threadIdx.x == 0) {
     for (int s = 0; s < P_STAGES; ++s) { mbar_init(bar_full + s * 8, 1); mbar_init(bar_empty + s * 8, 1); }
     for (int s = 0; s < P_SF_SLOTS; ++s) mbar_init(bar_scales + s * 8, 8);
+    for (int s = 0; s < P_RING; ++s) { mbar_init(bar_sfull + s * 8, 1); mbar_init(bar_sempty + s * 8, 4); }
     for (int a = 0; a < 2; ++a) mbar_init(bar_tfull + a * 8, 1);
     mbar_init(bar_handed, 2 * EPI_WARPS);
     *abort_flag = 0;
@@ -498,68 +502,59 @@ mx4_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
         acc ^= 1u;
       }
     }
+  } else if (warp == 14) {
+    // ---- TMA of the scales; tiles past the end of either matrix arrive as zeros ----
+    if (lane == 0) {
+      uint32_t slot = 0, phase = 0;
+      bool ok = true;
+      for (int t = pair; t < n_total && ok; t += n_pairs) {
+        const Item it = get_item(p, m_tiles, t);
+        const int a_tile = it.b * p.a_row_tiles + it.mt * 2 + (int)rank, b_tile = it.e * p.b_row_tiles + it.nt * 2;
+        for (int kb = 0; kb < kb_total; ++kb) {
+          if (!(ok = mbar_wait(bar_sempty + slot * 8, phase ^ 1u, abort_flag, p.status))) break;
+          const uint32_t bar = bar_sfull + slot * 8, to = sf_ring + slot * P_SCALE_BYTES;
+          mbar_expect_tx(bar, P_SCALE_BYTES);
+          load_3d(to, &tmSA, 0, kb * 2, a_tile, bar);
+          load_3d(to + 2 * kTileBytes, &tmSB, 0, kb * 2, b_tile, bar);
+          if (++slot == P_RING) { slot = 0; phase ^= 1u; }
+        }
+      }
+      for (int i = 0; i < P_RING && ok; ++i) {            // every copy has landed and has been read
+        ok = mbar_wait(bar_sempty + slot * 8, phase ^ 1u, abort_flag, p.status);
+        if (++slot == P_RING) { slot = 0; phase ^= 1u; }
+      }
+    }
   } else if (warp >= 2 + EPI_WARPS) {
-    // ---- scales: rows c * 32 + lane of a tile are word c of the lane's 16 bytes, and column c of tensor memory ----
+    // ---- scales: word c of a lane's 16 bytes is row c * 32 + lane of a tile, and column c of tensor memory ----
     const uint32_t taddr = tmem + P_SF0 + ((uint32_t)((warp & 3) * 32) << 16);
     const uint32_t ready = map_to_cta(bar_scales, 0);
-    ScaleCursor cur = {};
-    auto seek = [&]() {
-      cur.live = cur.t < n_total;
-      if (!cur.live) return;
-      const Item it = get_item(p, m_tiles, cur.t);
-      cur.a = p.a_scales + ((size_t)(it.b * p.a_row_tiles + it.mt * 2 + (int)rank) * p.kt) * kTileBytes + lane * 16;
-      cur.b = p.b_scales + ((size_t)((size_t)it.e * p.b_row_tiles + it.nt * 2) * p.kt) * kTileBytes + lane * 16;
-      // the tile's second half may hold no row of A (its outputs are dropped) or lie past the last column
-      if (it.mt * 2 + (int)rank >= p.a_row_tiles) cur.a = nullptr;
-      cur.second_b = it.nt * 2 + 1 < p.b_row_tiles;
-      cur.kb = 0;
-    };
-    cur.t = pair;
-    seek();
-    auto fetch = [&](uint4 (&r)[6]) {                    // the current step's scales, and on to the next step
-      const bool live = cur.live;
+    uint32_t slot = 0, steps = 0, ret_stage = 0, ret_phase = 0, in = 0, in_phase = 0;
+    bool ok = true;
+    for (int t = pair; t < n_total && ok; t += n_pairs) {
+      for (int kb = 0; kb < kb_total; ++kb) {
+        if (!(ok = warp_wait(bar_sfull + in * 8, in_phase, abort_flag, p.status))) break;
+        uint4 r[6];                                       // A: two tiles along K; B: two of the first half, two of the second
 #pragma unroll
-      for (int i = 0; i < 6; ++i) r[i] = make_uint4(0, 0, 0, 0);
-      if (live) {
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const size_t o = (size_t)(cur.kb * 2 + c) * kTileBytes;
-          if (cur.kb * 2 + c < p.kt) {
-            if (cur.a != nullptr) r[c] = *reinterpret_cast<const uint4*>(cur.a + o);
-            r[2 + 2 * c] = *reinterpret_cast<const uint4*>(cur.b + o);
-            if (cur.second_b) r[3 + 2 * c] = *reinterpret_cast<const uint4*>(cur.b + (size_t)p.kt * kTileBytes + o);
-          }
+        for (int i = 0; i < 6; ++i) r[i] = ld_shared_v4(sf_ring + in * P_SCALE_BYTES + i * kTileBytes + lane * 16);
+        if (steps >= P_SF_SLOTS) {                        // the MMAs that read this slot's last scales have retired
+          if (!(ok = warp_wait(bar_empty + ret_stage * 8, ret_phase, abort_flag, p.status))) break;
+          if (++ret_stage == P_STAGES) { ret_stage = 0; ret_phase ^= 1u; }
+          tc_fence_after();
         }
-        if (++cur.kb == kb_total) { cur.t += n_pairs; seek(); }
+        ++steps;
+        const uint32_t to = taddr + slot * P_SF_COLS;
+        store_scales(to, r[0], r[1]);
+        store_scales(to + 8, r[2], r[4]);
+        store_scales(to + 16, r[3], r[5]);
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        tc_fence_before();
+        if (lane == 0) {
+          mbar_arrive_cluster(ready + slot * 8);
+          arrive(bar_sempty + in * 8);
+        }
+        if (++slot == P_SF_SLOTS) slot = 0;
+        if (++in == P_RING) { in = 0; in_phase ^= 1u; }
       }
-      return live;
-    };
-    uint32_t slot = 0, steps = 0, ret_stage = 0, ret_phase = 0;
-    auto put = [&](const uint4 (&r)[6]) {
-      if (steps >= P_SF_SLOTS) {                         // the MMAs that read this slot's last scales have retired
-        if (!warp_wait(bar_empty + ret_stage * 8, ret_phase, abort_flag, p.status)) return false;
-        if (++ret_stage == P_STAGES) { ret_stage = 0; ret_phase ^= 1u; }
-        tc_fence_after();
-      }
-      ++steps;
-      __syncwarp();
-      const uint32_t to = taddr + slot * P_SF_COLS;
-      store_scales(to, r[0], r[1]);
-      store_scales(to + 8, r[2], r[3]);
-      store_scales(to + 16, r[4], r[5]);
-      asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-      tc_fence_before();
-      if (lane == 0) mbar_arrive_cluster(ready + slot * 8);
-      if (++slot == P_SF_SLOTS) slot = 0;
-      return true;
-    };
-    uint4 r0[6], r1[6];
-    bool live0 = fetch(r0), live1 = fetch(r1);
-    while (live0) {
-      if (!put(r0)) break;
-      live0 = fetch(r0);
-      if (!live1 || !put(r1)) break;
-      live1 = fetch(r1);
     }
   } else {
     const int q = warp & 3, half = (warp - 2) >> 2;
@@ -614,6 +609,18 @@ bool make_codes_map(CUtensorMap* m, const void* base, long long K, long long row
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// scale tiles [row tiles][kt][512 bytes] of all matrices, box of two tiles along K x box_tiles row tiles
+bool make_scales_map(CUtensorMap* m, const void* base, long long kt, long long row_tiles, uint32_t box_tiles) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[3] = {kTileBytes / 4, (cuuint64_t)kt, (cuuint64_t)row_tiles};
+  cuuint64_t strides[2] = {kTileBytes, (cuuint64_t)(kt * kTileBytes)};
+  cuuint32_t box[3] = {kTileBytes / 4, 2, box_tiles};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_INT32, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // once per device and kernel: the attribute outlives the call
 bool allow_smem(const void* kernel, int bytes, std::atomic<uint64_t>& done) {
   int dev = 0;
@@ -640,16 +647,18 @@ btx_status launch(const GemmArgs& g, Params p, long long max_items, cudaStream_t
 template <int MODE>
 btx_status launch_pair(const GemmArgs& g, Params p, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
-  CUtensorMap a, b;
+  CUtensorMap a, b, sa, sb;
   p.m_tiles = (g.M + 255) / 256; p.n_tiles = (g.N + 255) / 256; p.tile_step = 2;
   if (!make_codes_map(&a, g.a_codes, g.K, g.M, g.batch, 128) || !make_codes_map(&b, g.b_codes, g.K, g.N, g.experts, 128) ||
+      !make_scales_map(&sa, g.a_scales, p.kt, (long long)p.a_row_tiles * g.batch, 1) ||
+      !make_scales_map(&sb, g.b_scales, p.kt, (long long)p.b_row_tiles * g.experts, 2) ||
       !allow_smem((const void*)mx4_gemm_pair_kernel<MODE>, P_SMEM, done))
     return BTX_ERR_CUDA;
   const long long items = (long long)p.m_tiles * p.n_tiles * p.batch;
   int pairs = sm_count() / 2;
   if (items < pairs) pairs = (int)items;
-  return launch_after_predecessor(mx4_gemm_pair_kernel<MODE>, dim3(2 * pairs), dim3(P_THREADS), P_SMEM, st, MODE != STORE, a, b,
-                                  p) == cudaSuccess ? BTX_OK : BTX_ERR_CUDA;
+  return launch_after_predecessor(mx4_gemm_pair_kernel<MODE>, dim3(2 * pairs), dim3(P_THREADS), P_SMEM, st, MODE != STORE, a, b, sa,
+                                  sb, p) == cudaSuccess ? BTX_OK : BTX_ERR_CUDA;
 }
 
 Params base_params(const GemmArgs& g, int bn) {
