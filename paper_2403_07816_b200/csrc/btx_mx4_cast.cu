@@ -3,7 +3,7 @@
 //   quantize     per 32 elements: scale 2^(floor(log2 max|x|) - 2), elements to the nearest e2m1 value (ties to the
 //                even code, at most 6).  Four lanes share a block, eight elements each: a warp reads 256 consecutive
 //                elements with 16-byte loads, the maximum takes two shuffles, a lane stores four bytes of codes and
-//                every sixteenth lane four scale bytes.  Bound by memory: 2 + 17/32 bytes per bf16 element.
+//                every fourth the scale byte.  Bound by memory: 2 + 17/32 bytes per bf16 element.
 //   dequantize   the same mapping backwards
 //   dispatch     stable counting sort of the assignments by expert, padded to 128-row tiles
 //   quantize_rows  quantize of x with every row written to the k rows of its token: x is read once
@@ -24,91 +24,111 @@ constexpr int kCastUnroll = 4;             // 256-element chunks a warp has in f
 constexpr int kSortThreads = 512;
 constexpr int kSortChunk = 2048;           // assignments per block of the dispatch kernels
 
-template <typename T> __device__ __forceinline__ void load8(const T* p, float (&v)[8], bool vec);
-template <> __device__ __forceinline__ void load8<float>(const float* p, float (&v)[8], bool vec) {
-  if (vec) {
-    const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = p[i];
+// Eight elements of a lane as they were loaded: their largest magnitude as the bits of a float (NaN and infinities
+// compare above every number), and their values.
+template <typename T> struct Eight;
+template <> struct Eight<float> {
+  uint4 a, b;
+  __device__ __forceinline__ void zero() { a = b = make_uint4(0, 0, 0, 0); }
+  __device__ __forceinline__ void load(const float* p, bool vec) {
+    if (vec) {
+      a = __ldcs(reinterpret_cast<const uint4*>(p));
+      b = __ldcs(reinterpret_cast<const uint4*>(p) + 1);
+    } else {
+      const uint32_t* w = reinterpret_cast<const uint32_t*>(p);
+      a = make_uint4(w[0], w[1], w[2], w[3]);
+      b = make_uint4(w[4], w[5], w[6], w[7]);
+    }
   }
-}
-template <> __device__ __forceinline__ void load8<__nv_bfloat16>(const __nv_bfloat16* p, float (&v)[8], bool vec) {
-  if (vec) {
-    Vec<__nv_bfloat16>::unpack(__ldcs(reinterpret_cast<const uint4*>(p)), v);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __bfloat162float(p[i]);
+  __device__ __forceinline__ uint32_t block_max() const {
+    constexpr uint32_t M = 0x7fffffffu;
+    uint32_t m = max(max(max(a.x & M, a.y & M), max(a.z & M, a.w & M)), max(max(b.x & M, b.y & M), max(b.z & M, b.w & M)));
+    m = max(m, __shfl_xor_sync(kAll, m, 1));
+    return max(m, __shfl_xor_sync(kAll, m, 2));
   }
-}
+  __device__ __forceinline__ void values(float (&v)[8]) const {
+    v[0] = __uint_as_float(a.x); v[1] = __uint_as_float(a.y); v[2] = __uint_as_float(a.z); v[3] = __uint_as_float(a.w);
+    v[4] = __uint_as_float(b.x); v[5] = __uint_as_float(b.y); v[6] = __uint_as_float(b.z); v[7] = __uint_as_float(b.w);
+  }
+};
+template <> struct Eight<__nv_bfloat16> {
+  uint4 a;
+  __device__ __forceinline__ void zero() { a = make_uint4(0, 0, 0, 0); }
+  __device__ __forceinline__ void load(const __nv_bfloat16* p, bool vec) {
+    if (vec) {
+      a = __ldcs(reinterpret_cast<const uint4*>(p));
+    } else {
+      const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
+      a = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
+    }
+  }
+  // two 16-bit maxima per instruction: half the comparisons of the widened values
+  __device__ __forceinline__ uint32_t block_max() const {
+    constexpr uint32_t M = 0x7fff7fffu;
+    uint32_t m = __vimax3_u16x2(a.x & M, a.y & M, a.z & M);
+    m = __vimax3_u16x2(m, a.w & M, __shfl_xor_sync(kAll, __vimax3_u16x2(m, a.w & M, 0u), 1));
+    m = __vimax3_u16x2(m, __shfl_xor_sync(kAll, m, 2), 0u);
+    return max(m & 0xffff0000u, m << 16);
+  }
+  __device__ __forceinline__ void values(float (&v)[8]) const { Vec<__nv_bfloat16>::unpack(a, v); }
+};
 
-__device__ __forceinline__ uint32_t e2m1_pair(float lo, float hi) {
-  return (uint32_t)__nv_cvt_float2_to_fp4x2(make_float2(lo, hi), __NV_E2M1, cudaRoundNearest);
+// Four bytes of codes of eight elements times `inv`.
+__device__ __forceinline__ uint32_t pack_e2m1(const float (&v)[8], float inv) {
+  uint32_t q;
+  asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n\t"
+      "mov.b32 %0, {b0, b1, b2, b3};\n\t}"
+      : "=r"(q)
+      : "f"(v[0] * inv), "f"(v[1] * inv), "f"(v[2] * inv), "f"(v[3] * inv), "f"(v[4] * inv), "f"(v[5] * inv), "f"(v[6] * inv),
+        "f"(v[7] * inv));
+  return q;
 }
 
 // Eight elements of a block shared by four neighbouring lanes: four bytes of codes and the block's scale byte.
-__device__ __forceinline__ uint32_t cast8(const float (&v)[8], uint32_t& byte) {
-  uint32_t amax = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) amax = max(amax, __float_as_uint(v[i]) & 0x7fffffffu);
-  amax = max(amax, __shfl_xor_sync(kAll, amax, 1));
-  amax = max(amax, __shfl_xor_sync(kAll, amax, 2));
-  float inv;
-  byte = scale_byte(amax, inv);
-  if (byte == 255u) return 0u;
-  uint32_t q = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) q |= e2m1_pair(v[2 * i] * inv, v[2 * i + 1] * inv) << (8 * i);
-  return q;
-}
-// The scale bytes of the four blocks (128 elements) of sixteen lanes as one word, in all of them.
-__device__ __forceinline__ uint32_t scale_word(uint32_t byte, int lane) {
-  uint32_t w = byte << (8 * ((lane >> 2) & 3));
-  w |= __shfl_xor_sync(kAll, w, 4);
-  w |= __shfl_xor_sync(kAll, w, 8);
-  return w;
+template <typename T> __device__ __forceinline__ uint32_t cast8(const Eight<T>& x, uint32_t& byte) {
+  float inv, v[8];
+  byte = scale_byte(x.block_max(), inv);
+  x.values(v);
+  const uint32_t q = pack_e2m1(v, inv);
+  return byte == 255u ? 0u : q;
 }
 __device__ __forceinline__ size_t scale_offset(size_t tile_row0, int row, int kt, int chunk) {
   return ((tile_row0 + row / kTileRows) * (size_t)kt + chunk) * kTileBytes + (row & 31) * 16 + ((row >> 5) & 3) * 4;
 }
 
-// A warp takes kCastUnroll chunks of 256 elements of one row at a time.
-template <typename T>
+// A warp takes kCastUnroll chunks of 256 elements of one row at a time.  I: the type that numbers them; the two divisions
+// in 64 bits cost as many instructions as the cast of the chunks.
+template <typename T, typename I>
 __global__ void __launch_bounds__(kCastThreads)
-quantize_kernel(const CastParams p, int vec, long long items, int groups) {
+quantize_kernel(const CastParams p, int vec, I items, int groups) {
   const int lane = threadIdx.x & 31;
   const int kt = (int)scale_tiles_k(p.K);
   const size_t tiles = ((size_t)p.out_rows + kTileRows - 1) / kTileRows;
-  for (long long w = ((long long)blockIdx.x * kCastThreads + threadIdx.x) >> 5; w < items;
-       w += (long long)gridDim.x * (kCastThreads / 32)) {
-    const int g = (int)(w % groups);
-    const long long r = w / groups;
-    const int row = (int)(r % p.rows), b = (int)(r / p.rows);
+  for (I w = ((I)blockIdx.x * kCastThreads + threadIdx.x) >> 5; w < items; w += (I)gridDim.x * (kCastThreads / 32)) {
+    const I r = w / (I)groups;
+    const int g = (int)(w - r * (I)groups);
+    const int b = (int)(r / (I)p.rows), row = (int)(r - (I)b * (I)p.rows);
     const T* src = (const T*)p.src + b * p.batch_stride + row * p.row_stride;
     const int out_row = p.first + row * p.step;
-    float v[kCastUnroll][8];
+    const int c0 = g * kCastUnroll * 256 + lane * 8;
+    Eight<T> x[kCastUnroll];
 #pragma unroll
     for (int u = 0; u < kCastUnroll; ++u) {
-      const int c = (g * kCastUnroll + u) * 256 + lane * 8;
-      if (c < p.K) {
-        load8<T>(src + c, v[u], vec != 0);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[u][i] = 0.f;
-      }
+      if (c0 + u * 256 < p.K) x[u].load(src + c0 + u * 256, vec != 0);
+      else x[u].zero();
     }
-    uint8_t* codes = p.codes + ((size_t)b * p.out_rows + out_row) * (p.K / 2);
+    uint8_t* codes = p.codes + ((size_t)b * p.out_rows + out_row) * (p.K / 2) + c0 / 2;
+    uint8_t* scales = p.scales + scale_offset(b * tiles, out_row, kt, c0 / 128) + (c0 / kBlock & 3);
 #pragma unroll
     for (int u = 0; u < kCastUnroll; ++u) {
-      const int c = (g * kCastUnroll + u) * 256 + lane * 8;
       uint32_t byte;
-      const uint32_t q = cast8(v[u], byte);
-      const uint32_t word = scale_word(byte, lane);
-      if (c < p.K) *reinterpret_cast<uint32_t*>(codes + c / 2) = q;
-      const int chunk = c / 128;
-      if ((lane & 15) == 0 && chunk < kt)
-        *reinterpret_cast<uint32_t*>(p.scales + scale_offset(b * tiles, out_row, kt, chunk)) = word;
+      const uint32_t q = cast8(x[u], byte);
+      if (c0 + u * 256 < p.K) *reinterpret_cast<uint32_t*>(codes + u * 128) = q;
+      if ((lane & 3) == 0 && c0 + u * 256 < kt * 128) scales[u * 2 * kTileBytes] = (uint8_t)byte;
     }
   }
 }
@@ -125,19 +145,18 @@ template <> __device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16*
   __stcs(reinterpret_cast<uint4*>(p), *reinterpret_cast<uint4*>(h));
 }
 
-template <typename T>
+template <typename T, typename I>
 __global__ void __launch_bounds__(kCastThreads)
-dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int rows, int K, long long items,
-                  int groups, T* __restrict__ dst) {
+dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int rows, int K, I items, int groups,
+                  T* __restrict__ dst) {
   const int lane = threadIdx.x & 31;
   const int kt = (int)scale_tiles_k(K);
   const size_t tiles = ((size_t)rows + kTileRows - 1) / kTileRows;
-  for (long long w = ((long long)blockIdx.x * kCastThreads + threadIdx.x) >> 5; w < items;
-       w += (long long)gridDim.x * (kCastThreads / 32)) {
-    const int g = (int)(w % groups);
-    const long long r = w / groups;
-    const int row = (int)(r % rows);
-    const size_t b = (size_t)(r / rows);
+  for (I w = ((I)blockIdx.x * kCastThreads + threadIdx.x) >> 5; w < items; w += (I)gridDim.x * (kCastThreads / 32)) {
+    const I r = w / (I)groups;
+    const int g = (int)(w - r * (I)groups);
+    const size_t b = (size_t)(r / (I)rows);
+    const int row = (int)(r - (I)b * (I)rows);
     uint32_t q[kCastUnroll], byte[kCastUnroll];
 #pragma unroll
     for (int u = 0; u < kCastUnroll; ++u) {
@@ -330,45 +349,36 @@ dispatch_scatter_kernel(const Dispatch q) {
   scatter_rounds(begin, min(q.R, begin + kSortChunk), q.E, q.topk_idx, s.running, s.wcnt, s.pad, q.flat2row, q.rowmap);
 }
 
-template <typename T>
+template <typename T, typename I>
 __global__ void __launch_bounds__(kCastThreads)
 quantize_rows_kernel(const Dispatch q, const T* __restrict__ x, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
-                     long long items, int groups) {
+                     I items, int groups) {
   const int lane = threadIdx.x & 31;
   const int kt = (int)scale_tiles_k(q.d);
   allow_dependents();
   grid_dependency_wait();
-  for (long long w = ((long long)blockIdx.x * kCastThreads + threadIdx.x) >> 5; w < items;
-       w += (long long)gridDim.x * (kCastThreads / 32)) {
-    const int g = (int)(w % groups);
-    const size_t t = (size_t)(w / groups);
-    float v[kCastUnroll][8];
+  for (I w = ((I)blockIdx.x * kCastThreads + threadIdx.x) >> 5; w < items; w += (I)gridDim.x * (kCastThreads / 32)) {
+    const size_t t = (size_t)(w / (I)groups);
+    const int g = (int)(w - (I)t * (I)groups);
+    const int c0 = g * kCastUnroll * 256 + lane * 8;
+    Eight<T> v[kCastUnroll];
 #pragma unroll
     for (int u = 0; u < kCastUnroll; ++u) {
-      const int c = (g * kCastUnroll + u) * 256 + lane * 8;
-      if (c < q.d) {
-        load8<T>(x + t * q.d + c, v[u], true);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[u][i] = 0.f;
-      }
+      if (c0 + u * 256 < q.d) v[u].load(x + t * q.d + c0 + u * 256, true);
+      else v[u].zero();
     }
-    uint32_t code[kCastUnroll], word[kCastUnroll];
+    uint32_t code[kCastUnroll], byte[kCastUnroll];
 #pragma unroll
-    for (int u = 0; u < kCastUnroll; ++u) {
-      uint32_t byte;
-      code[u] = cast8(v[u], byte);
-      word[u] = scale_word(byte, lane);
-    }
+    for (int u = 0; u < kCastUnroll; ++u) code[u] = cast8(v[u], byte[u]);
     for (int j = 0; j < q.k; ++j) {
       const int row = q.flat2row[t * q.k + j];
       if (row < 0) continue;
+      uint8_t* to = codes + (size_t)row * (q.d / 2) + c0 / 2;
+      uint8_t* sc = scales + scale_offset(0, row, kt, c0 / 128) + (c0 / kBlock & 3);
 #pragma unroll
       for (int u = 0; u < kCastUnroll; ++u) {
-        const int c = (g * kCastUnroll + u) * 256 + lane * 8;
-        if (c < q.d) *reinterpret_cast<uint32_t*>(codes + (size_t)row * (q.d / 2) + c / 2) = code[u];
-        if ((lane & 15) == 0 && c / 128 < kt)
-          *reinterpret_cast<uint32_t*>(scales + scale_offset(0, row, kt, c / 128)) = word[u];
+        if (c0 + u * 256 < q.d) *reinterpret_cast<uint32_t*>(to + u * 128) = code[u];
+        if ((lane & 3) == 0 && c0 + u * 256 < kt * 128) sc[u * 2 * kTileBytes] = (uint8_t)byte[u];
       }
     }
   }
@@ -416,26 +426,34 @@ int cast_groups(int K) { return (K + 256 * kCastUnroll - 1) / (256 * kCastUnroll
 
 }  // namespace
 
+template <typename F> static cudaError_t by_index(long long items, F&& f) {
+  // numbers reach items plus one round of the grid
+  return items < (1ll << 31) ? f((uint32_t)items) : f((uint64_t)items);
+}
+
 cudaError_t launch_quantize(const CastParams& p, int dtype, cudaStream_t st) {
   const int groups = cast_groups(p.K);
   const long long items = (long long)p.batch * p.rows * groups;
   const int esize = dtype == BTX_BF16 ? 2 : 4;
   const int vec = ((uintptr_t)p.src & 15) == 0 && p.row_stride * esize % 16 == 0 && p.batch_stride * esize % 16 == 0;
-  if (dtype == BTX_BF16) quantize_kernel<__nv_bfloat16><<<cast_blocks(items), kCastThreads, 0, st>>>(p, vec, items, groups);
-  else quantize_kernel<float><<<cast_blocks(items), kCastThreads, 0, st>>>(p, vec, items, groups);
-  return cudaGetLastError();
+  return by_index(items, [&](auto n) {
+    if (dtype == BTX_BF16) quantize_kernel<__nv_bfloat16><<<cast_blocks(items), kCastThreads, 0, st>>>(p, vec, n, groups);
+    else quantize_kernel<float><<<cast_blocks(items), kCastThreads, 0, st>>>(p, vec, n, groups);
+    return cudaGetLastError();
+  });
 }
 
 cudaError_t launch_dequantize(const uint8_t* codes, const uint8_t* scales, int batch, int rows, int K, int dtype, void* dst,
                               cudaStream_t st) {
   const int groups = cast_groups(K);
   const long long items = (long long)batch * rows * groups;
-  if (dtype == BTX_BF16)
-    dequantize_kernel<__nv_bfloat16><<<cast_blocks(items), kCastThreads, 0, st>>>(codes, scales, rows, K, items, groups,
-                                                                                  (__nv_bfloat16*)dst);
-  else
-    dequantize_kernel<float><<<cast_blocks(items), kCastThreads, 0, st>>>(codes, scales, rows, K, items, groups, (float*)dst);
-  return cudaGetLastError();
+  return by_index(items, [&](auto n) {
+    if (dtype == BTX_BF16)
+      dequantize_kernel<<<cast_blocks(items), kCastThreads, 0, st>>>(codes, scales, rows, K, n, groups, (__nv_bfloat16*)dst);
+    else
+      dequantize_kernel<<<cast_blocks(items), kCastThreads, 0, st>>>(codes, scales, rows, K, n, groups, (float*)dst);
+    return cudaGetLastError();
+  });
 }
 
 int dispatch_blocks(long long R) { return (int)((R + kSortChunk - 1) / kSortChunk); }
@@ -455,11 +473,14 @@ cudaError_t launch_dispatch(const Dispatch& q, cudaStream_t st) {
 cudaError_t launch_quantize_rows(const Dispatch& q, int dtype, const void* x, uint8_t* codes, uint8_t* scales, cudaStream_t st) {
   const int groups = cast_groups(q.d);
   const long long items = (long long)q.T * groups;
-  if (dtype == BTX_BF16)
-    return launch_after_predecessor(quantize_rows_kernel<__nv_bfloat16>, dim3(cast_blocks(items)), dim3(kCastThreads), 0, st, true,
-                                    q, (const __nv_bfloat16*)x, codes, scales, items, groups);
-  return launch_after_predecessor(quantize_rows_kernel<float>, dim3(cast_blocks(items)), dim3(kCastThreads), 0, st, true, q,
-                                  (const float*)x, codes, scales, items, groups);
+  return by_index(items, [&](auto n) {
+    using I = decltype(n);
+    if (dtype == BTX_BF16)
+      return launch_after_predecessor(quantize_rows_kernel<__nv_bfloat16, I>, dim3(cast_blocks(items)), dim3(kCastThreads), 0, st,
+                                      true, q, (const __nv_bfloat16*)x, codes, scales, n, groups);
+    return launch_after_predecessor(quantize_rows_kernel<float, I>, dim3(cast_blocks(items)), dim3(kCastThreads), 0, st, true, q,
+                                    (const float*)x, codes, scales, n, groups);
+  });
 }
 
 cudaError_t launch_combine_rows(const Dispatch& q, int dtype, const float* rows, int splits, void* y, cudaStream_t st) {
