@@ -42,6 +42,7 @@ struct Dispatch {
   int32_t* flat2row;                       // [R] padded row of an assignment, -1 without an expert
   int32_t* rowmap;                         // [m_tiles_max * 128] assignment of a padded row, -1 for padding
   int32_t* tile_expert;                    // [m_tiles_max]
+  int32_t* tile_rows;                      // [m_tiles_max] rows of a tile with an assignment
   int32_t* n_tiles;                        // [1] padded row tiles in use
   int32_t* block_counts;                   // [blocks * E] (batches of more than one block)
   int32_t* pad_offsets;                    // [E + 1] first padded row of every expert

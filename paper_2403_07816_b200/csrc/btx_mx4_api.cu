@@ -19,7 +19,7 @@ btx_status check_shape(int batch, int rows, int K) {
 
 struct MoePlan {
   Dispatch q;
-  size_t w_status, w_flat2row, w_rowmap, w_tile_expert, w_n_tiles, w_block_counts, w_pad_offsets, w_xs, w_xs_scales, w_act,
+  size_t w_status, w_flat2row, w_rowmap, w_tile_expert, w_tile_rows, w_n_tiles, w_block_counts, w_pad_offsets, w_xs, w_xs_scales, w_act,
       w_act_scales, w_rows, bytes;
 };
 
@@ -49,6 +49,7 @@ btx_status make_moe_plan(const btx_mx4_moe_desc* d, MoePlan* pl) {
   pl->w_flat2row = take((size_t)R * 4);
   pl->w_rowmap = take(rp * 4);
   pl->w_tile_expert = take((size_t)tiles * 4);
+  pl->w_tile_rows = take((size_t)tiles * 4);
   pl->w_n_tiles = take(4);
   pl->w_block_counts = take((size_t)q.blocks * d->E * 4);
   pl->w_pad_offsets = take((size_t)(d->E + 1) * 4);
@@ -175,7 +176,7 @@ extern "C" btx_status btx_mx4_moe_forward(const btx_mx4_moe_desc* desc, const vo
   q.topk_idx = topk_idx;
   q.status = (int32_t*)(ws + pl.w_status);
   q.flat2row = (int32_t*)(ws + pl.w_flat2row); q.rowmap = (int32_t*)(ws + pl.w_rowmap);
-  q.tile_expert = (int32_t*)(ws + pl.w_tile_expert); q.n_tiles = (int32_t*)(ws + pl.w_n_tiles);
+  q.tile_expert = (int32_t*)(ws + pl.w_tile_expert); q.tile_rows = (int32_t*)(ws + pl.w_tile_rows); q.n_tiles = (int32_t*)(ws + pl.w_n_tiles);
   q.block_counts = (int32_t*)(ws + pl.w_block_counts); q.pad_offsets = (int32_t*)(ws + pl.w_pad_offsets);
   uint8_t *xs = (uint8_t*)ws + pl.w_xs, *xs_scales = (uint8_t*)ws + pl.w_xs_scales;
   uint8_t *act = (uint8_t*)ws + pl.w_act, *act_scales = (uint8_t*)ws + pl.w_act_scales;

@@ -192,8 +192,8 @@ dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__
 // Offsets of the experts' padded segments from their counts in shared memory (one block): pad[e], and the list of
 // the expert of every tile.
 __device__ __forceinline__ void place_experts(int E, int pad_tiles, const int* cnt, int* pad, int* __restrict__ scan,
-                                              int32_t* __restrict__ tile_expert, int32_t* __restrict__ n_tiles,
-                                              int32_t* __restrict__ pad_offsets) {
+                                              int32_t* __restrict__ tile_expert, int32_t* __restrict__ tile_rows,
+                                              int32_t* __restrict__ n_tiles, int32_t* __restrict__ pad_offsets) {
   const int tid = threadIdx.x;               // kSortThreads >= kMaxExperts4: a thread per expert
   const int lane = tid & 31, warp = tid >> 5;
   const int unit = pad_tiles * kTileRows;
@@ -212,7 +212,10 @@ __device__ __forceinline__ void place_experts(int E, int pad_tiles, const int* c
   if (tid < E) {
     pad[tid] = first * kTileRows;
     if (pad_offsets != nullptr) pad_offsets[tid] = first * kTileRows;
-    for (int j = 0; j < tiles; ++j) tile_expert[first + j] = tid;
+    for (int j = 0; j < tiles; ++j) {
+      tile_expert[first + j] = tid;
+      tile_rows[first + j] = max(0, min(kTileRows, cnt[tid] - j * kTileRows));
+    }
   }
   if (tid == E - 1) {
     n_tiles[0] = first + tiles;
@@ -288,7 +291,7 @@ dispatch_one_kernel(const Dispatch q) {
     if ((unsigned)e < (unsigned)q.E) atomicAdd(&s.cnt[e], 1);
   }
   __syncthreads();
-  place_experts(q.E, q.pad_tiles, s.cnt, s.pad, s.scan, q.tile_expert, q.n_tiles, nullptr);
+  place_experts(q.E, q.pad_tiles, s.cnt, s.pad, s.scan, q.tile_expert, q.tile_rows, q.n_tiles, nullptr);
   clear_padding(q.E, q.pad_tiles, s.cnt, s.pad, q.rowmap);
   scatter_rounds(0, q.R, q.E, q.topk_idx, s.running, s.wcnt, s.pad, q.flat2row, q.rowmap);
 }
@@ -331,7 +334,7 @@ dispatch_scan_kernel(const Dispatch q) {
     cnt[e] = run;
   }
   __syncthreads();
-  place_experts(q.E, q.pad_tiles, cnt, pad, scan, q.tile_expert, q.n_tiles, q.pad_offsets);
+  place_experts(q.E, q.pad_tiles, cnt, pad, scan, q.tile_expert, q.tile_rows, q.n_tiles, q.pad_offsets);
   clear_padding(q.E, q.pad_tiles, cnt, pad, q.rowmap);
 }
 

@@ -3,14 +3,21 @@
 // tensor memory; nothing is decoded on the way.  y = A B^T with both operands K-major, per output element
 //   sum over blocks of 32:  2^(sa - 127) 2^(sb - 127) sum a_i b_i.
 //
-// One persistent kernel, a CTA per SM, a 128 x BN tile at a time:
-//   warp 0      TMA producer (one lane): ring of stages of 256 contraction elements (A 128 x 128 bytes, B BN x 128
-//               bytes, swizzled; the two 512-byte scale tiles of A and of every 128 rows of B)
-//   warp 1      allocates tensor memory; one lane copies a stage's scales into the stage's own tensor-memory columns
-//               (so a copy never meets an MMA that still reads them: the stage is free only after its commit) and
-//               issues up to four MMAs of 64 contraction elements
-//   warps 2-9   epilogue: a row per thread, two warps per 32-lane quarter, each half of the columns.  Two accumulators
-//               let the epilogue of a tile overlap the main loop of the next.
+// Two kernels: mx4_gemm_kernel, a CTA per 128 x 128 tile, for few rows (bound by reading B), and below it
+// mx4_gemm_pair_kernel, two CTAs per 256 x 256 tile, for many (bound by the tensor cores and their power).
+//
+// mx4_gemm_kernel:
+//   warp 0, 10  TMA producers (one lane each: an operation costs its thread about 80 ns) of A and of B with their
+//               scales: ring of stages of 256 contraction elements (codes in swizzled rows of 128 bytes, two 512-byte
+//               scale tiles of each).  Of A a stage holds only as many rows as a tile can have (a multiple of 32),
+//               which leaves room for more stages: with 32 rows 10 instead of 6
+//   warp 1      allocates tensor memory; one lane issues up to four MMAs of 64 contraction elements per stage
+//   warps 11-14 scales, from shared memory into the stage's own tensor-memory columns, a warp per 32-lane quarter (the
+//               columns are free: the stage is filled again only after the MMAs that read them have retired).
+//               tcgen05.cp would do the same in the pipe of the MMAs, 37 ns a tile: 46 instead of 40 us for 190 MB of B
+//   warps 2-9   epilogue: a row per thread, two warps per 32-lane quarter, each half of the columns
+// Persistent, two accumulators; or SPLIT: a cluster of 2 to 8 CTAs shares a tile's contraction, each leaves its
+// partial sums in its shared memory and then adds up a slice of the columns over the cluster, in CTA order.
 // Modes:
 //   STORE    y, fp32 or bf16
 //   GATE_UP  B rows alternate between W1 and W3, so h1 and h3 of a hidden unit are neighbouring columns of one thread:
@@ -32,24 +39,27 @@ using namespace tcx;
 
 constexpr int SK = 256;                                  // contraction elements per stage (128 bytes of codes)
 constexpr int BM = kTileRows;
+constexpr int BN = 128;
 constexpr int EPI_WARPS = 8;
-constexpr int THREADS = 64 + EPI_WARPS * 32;
-constexpr int A_BYTES = BM * SK / 2;
-constexpr int SFA_BYTES = 2 * kTileBytes;
+constexpr int THREADS = 96 + EPI_WARPS * 32 + 128;
+constexpr int A_BYTES = BM * SK / 2, B_BYTES = BN * SK / 2;
+constexpr int SF_BYTES = 2 * kTileBytes;                 // scales of a stage, of A or of B
+constexpr int MAX_STAGES = 10, SF_COLS = 16;             // tensor-memory columns of a stage's scales
+constexpr int RING_BYTES = 220 * 1024;
+constexpr int SMEM_BYTES = RING_BYTES + 1024 + 320;
+constexpr int PART_PITCH = BN + 4;                       // SPLIT: floats per row of a partial tile (a quad apart: no bank conflicts)
+static_assert(2 * BN + MAX_STAGES * SF_COLS <= 512, "accumulators and scales fit in tensor memory");
+static_assert(MAX_STAGES * 24 + 48 <= 320 && BM * PART_PITCH * 4 <= RING_BYTES, "shared memory");
 constexpr int GROUP_N = 8;                               // column tiles per raster group
 
 enum Mode { STORE = 0, GATE_UP = 1, DOWN = 2 };
 
-template <int BN> struct Cfg {
-  static constexpr int B_BYTES = BN * SK / 2;
-  static constexpr int SFB_BYTES = (BN / kTileRows) * 2 * kTileBytes;
-  static constexpr int STAGE_BYTES = A_BYTES + B_BYTES + SFA_BYTES + SFB_BYTES;
-  static constexpr int STAGES = 220 * 1024 / STAGE_BYTES;
-  static constexpr int SF_COLS = 8 + (BN / kTileRows) * 8;          // tensor-memory columns of a stage's scales
-  static constexpr int SMEM = STAGES * STAGE_BYTES + 1024 + 256;
-  static_assert(2 * BN + STAGES * SF_COLS <= 512, "accumulators and scales fit in tensor memory");
-  static_assert(STAGES * 16 + 48 <= 256, "barriers fit behind the ring");
-};
+// bytes of a ring stage whose A part has `rows` rows, and how many fit
+inline __host__ __device__ int stage_bytes(int rows) { return rows * (SK / 2) + 2 * SF_BYTES + B_BYTES; }
+inline __host__ __device__ int stage_count(int rows) {
+  const int n = RING_BYTES / stage_bytes(rows);
+  return n < MAX_STAGES ? n : MAX_STAGES;
+}
 
 struct Params {
   int M, N, K;                      // STORE: rows and columns of y; grouped: N = B rows per expert
@@ -58,7 +68,10 @@ struct Params {
   int tile_step;                    // 128-row tiles per row tile of this launch (1, or 2 for CTA pairs)
   const int32_t* n_row_tiles;       // grouped: row tiles in use (device)
   const int32_t* tile_expert;
+  const int32_t* tile_rows;         // grouped: rows of a tile that hold an assignment
   const int32_t* rowmap;
+  int a_rows, a_box;                // rows of A per stage, rows per TMA operation
+  int split;                        // CTAs that share a tile's contraction
   const uint8_t* a_scales;
   const uint8_t* b_scales;
   long long a_scale_batch, b_scale_batch;   // bytes from one matrix to the next
@@ -94,12 +107,11 @@ __device__ __forceinline__ void mma_mxf4(uint32_t d, uint64_t a, uint64_t b, uin
       "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
       ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accum) : "memory");
 }
-// 32 rows of 16 bytes (a 512-byte scale tile) to four tensor-memory columns, repeated in every 32-lane quarter
-__device__ __forceinline__ void copy_scales(uint32_t tmem, uint32_t smem) {
-  // no swizzle, eight-row core matrices of 128 bytes, 128 bytes apart
-  const uint64_t desc = (uint64_t)((smem & 0x3FFFFu) >> 4) | ((uint64_t)(128 >> 4) << 16) | ((uint64_t)(128 >> 4) << 32) |
-                        (1ull << 46);
-  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+// This lane's 16 bytes of two 512-byte scale tiles to eight tensor-memory columns of the warp's 32-lane quarter.  Word
+// c of a lane's 16 bytes belongs to row c * 32 + lane of a tile: it goes to column c, the same in all four quarters.
+__device__ __forceinline__ void store_scales(uint32_t taddr, const uint4& lo, const uint4& hi) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"r"(taddr), "r"(lo.x), "r"(lo.y), "r"(lo.z), "r"(lo.w), "r"(hi.x), "r"(hi.y), "r"(hi.z), "r"(hi.w) : "memory");
 }
 __device__ __forceinline__ void arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
@@ -219,23 +231,36 @@ __device__ __forceinline__ void finish_chunk(const Params& p, const Item& it, fl
   }
 }
 
-template <int MODE, int BN>
+// SPLIT: one quad or one element of the sum over the cluster's partial tiles, in CTA order.
+__device__ __forceinline__ float4 ld_cluster_v4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ float ld_cluster(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+template <int MODE, bool SPLIT>
 __global__ void __launch_bounds__(THREADS, 1)
 mx4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const Params p) {
-  using C = Cfg<BN>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t ring = (raw + 1023u) & ~1023u;
-  uint8_t* ctl = smem_raw + (ring - raw) + C::STAGES * C::STAGE_BYTES;
-  const uint32_t bar_full = smem_u32(ctl), bar_empty = bar_full + C::STAGES * 8;
-  const uint32_t bar_tfull = bar_empty + C::STAGES * 8, bar_tempty = bar_tfull + 16;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctl + C::STAGES * 16 + 32);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(ctl + C::STAGES * 16 + 40);
+  uint8_t* ctl = smem_raw + (ring - raw) + RING_BYTES;
+  const uint32_t bar_full = smem_u32(ctl), bar_empty = bar_full + MAX_STAGES * 8;
+  const uint32_t bar_tfull = bar_empty + MAX_STAGES * 8, bar_tempty = bar_tfull + 16;
+  const uint32_t bar_scales = bar_tempty + 16;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctl + MAX_STAGES * 24 + 32);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(ctl + MAX_STAGES * 24 + 40);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int n_stages = stage_count(p.a_rows), s_bytes = stage_bytes(p.a_rows);
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < C::STAGES; ++s) { mbar_init(bar_full + s * 8, 1); mbar_init(bar_empty + s * 8, 1); }
-    for (int a = 0; a < 2; ++a) { mbar_init(bar_tfull + a * 8, 1); mbar_init(bar_tempty + a * 8, EPI_WARPS * 32); }
+    for (int s = 0; s < n_stages; ++s) { mbar_init(bar_full + s * 8, 2); mbar_init(bar_empty + s * 8, 1); mbar_init(bar_scales + s * 8, 4); }
+    for (int a = 0; a < 2; ++a) { mbar_init(bar_tfull + a * 8, 1); mbar_init(bar_tempty + a * 8, EPI_WARPS); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -254,73 +279,75 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
   if (MODE == STORE && blockIdx.x == 0 && threadIdx.x < kStatusWords) p.status[threadIdx.x] = 0;
   const int m_tiles = p.grouped ? p.n_row_tiles[0] : p.m_tiles;
   const int n_total = m_tiles * p.n_tiles * p.batch;
-  const int kb_total = (p.K + SK - 1) / SK;
+  // SPLIT: one tile per cluster, an even share of its stages per CTA
+  const int part = SPLIT ? (int)cluster_ctarank() : 0;
+  const int t0 = SPLIT ? (int)blockIdx.x / p.split : (int)blockIdx.x, t_step = SPLIT ? n_total : (int)gridDim.x;
+  const int kb_all = (p.K + SK - 1) / SK;
+  const int kb0 = SPLIT ? (int)((long long)part * kb_all / p.split) : 0;
+  const int kb1 = SPLIT ? (int)((long long)(part + 1) * kb_all / p.split) : kb_all;
 
-  if (warp == 0) {
+  if (warp == 0 || warp == 10) {
     if (lane == 0) {
       uint32_t stage = 0, phase = 0;
       bool ok = true;
-      for (int t = blockIdx.x; t < n_total && ok; t += gridDim.x) {
+      for (int t = t0; t < n_total && ok; t += t_step) {
         const Item it = get_item(p, m_tiles, t);
         const uint8_t* sfa = p.a_scales + it.b * p.a_scale_batch + (size_t)it.mt * p.kt * kTileBytes;
-        const uint8_t* sfb = p.b_scales + it.e * p.b_scale_batch + (size_t)it.nt * (BN / kTileRows) * p.kt * kTileBytes;
-        // the last row tiles of B may lie past its end: a tile of BN = 256 columns then has one row tile of scales
-        const int b_rows = min(BN / kTileRows, (p.N + kTileRows - 1) / kTileRows - it.nt * (BN / kTileRows));
-        for (int kb = 0; kb < kb_total; ++kb) {
+        const uint8_t* sfb = p.b_scales + it.e * p.b_scale_batch + (size_t)it.nt * p.kt * kTileBytes;
+        const int rows = min(p.grouped ? p.tile_rows[it.mt] : p.M - it.mt * BM, p.a_rows);
+        const int boxes = (rows + p.a_box - 1) / p.a_box;
+        for (int kb = kb0; kb < kb1; ++kb) {
           if (!(ok = mbar_wait(bar_empty + stage * 8, phase ^ 1u, abort_flag, p.status))) break;
           const uint32_t bar = bar_full + stage * 8;
-          const uint32_t sA = ring + stage * C::STAGE_BYTES, sB = sA + A_BYTES, sSA = sB + C::B_BYTES, sSB = sSA + SFA_BYTES;
+          const uint32_t sA = ring + stage * s_bytes, sSA = sA + p.a_rows * (SK / 2), sSB = sSA + SF_BYTES, sB = sSB + SF_BYTES;
           const uint32_t sf = (uint32_t)min(2, p.kt - 2 * kb) * kTileBytes;
-          mbar_expect_tx(bar, A_BYTES + C::B_BYTES + sf * (1 + b_rows));
-          load_3d(sA, &tmA, kb * (SK / 2), it.mt * BM, it.b, bar);
-          load_3d(sB, &tmB, kb * (SK / 2), it.nt * BN, it.e, bar);
-          load_bulk(sSA, sfa + (size_t)kb * 2 * kTileBytes, sf, bar);
-          for (int r = 0; r < b_rows; ++r)
-            load_bulk(sSB + r * 2 * kTileBytes, sfb + ((size_t)r * p.kt + kb * 2) * kTileBytes, sf, bar);
-          if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+          if (warp == 0) {
+            mbar_expect_tx(bar, boxes * p.a_box * (SK / 2) + sf);
+            for (int i = 0; i < boxes; ++i)
+              load_3d(sA + i * p.a_box * (SK / 2), &tmA, kb * (SK / 2), it.mt * BM + i * p.a_box, it.b, bar);
+            load_bulk(sSA, sfa + (size_t)kb * 2 * kTileBytes, sf, bar);
+          } else {
+            mbar_expect_tx(bar, B_BYTES + sf);
+            load_3d(sB, &tmB, kb * (SK / 2), it.nt * BN, it.e, bar);
+            load_bulk(sSB, sfb + (size_t)kb * 2 * kTileBytes, sf, bar);
+          }
+          if (++stage == n_stages) { stage = 0; phase ^= 1u; }
         }
       }
-      for (int i = 0; i < C::STAGES && ok; ++i) {         // the MMAs that read the last stages have retired
+      for (int i = 0; i < n_stages && ok; ++i) {          // the MMAs that read the last stages have retired
         ok = mbar_wait(bar_empty + stage * 8, phase ^ 1u, abort_flag, p.status);
-        if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+        if (++stage == n_stages) { stage = 0; phase ^= 1u; }
       }
     }
   } else if (warp == 1) {
     if (lane == 0) {
-      // e2m1 x e2m1 (type code 1), UE8M0 scales, both operands K-major, M 128, N BN; scale selectors per MMA below
+      // e2m1 x e2m1 (type code 1), UE8M0 scales, both operands K-major, M 128, N 128; scale selectors per MMA below.
+      // The MMA reads 128 rows of A: those past the stage's A part (other bytes of the stage) give rows nobody reads.
       constexpr uint32_t idesc0 = (1u << 7) | (1u << 10) | ((uint32_t)(BN >> 3) << 17) | (1u << 23) | ((uint32_t)(BM >> 4) << 24);
       uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
       bool ok = true;
-      for (int t = blockIdx.x; t < n_total && ok; t += gridDim.x) {
+      for (int t = t0; t < n_total && ok; t += t_step) {
         if (!(ok = mbar_wait(bar_tempty + acc * 8, acc_phase ^ 1u, abort_flag, p.status))) break;
         tc_fence_after();
         const uint32_t d = tmem + acc * BN;
-        for (int kb = 0; kb < kb_total; ++kb) {
+        for (int kb = kb0; kb < kb1; ++kb) {
           if (!(ok = mbar_wait(bar_full + stage * 8, phase, abort_flag, p.status))) break;
+          if (!(ok = mbar_wait(bar_scales + stage * 8, phase, abort_flag, p.status))) break;
           tc_fence_after();
-          const uint32_t sA = ring + stage * C::STAGE_BYTES, sB = sA + A_BYTES, sSA = sB + C::B_BYTES, sSB = sSA + SFA_BYTES;
-          const uint32_t tA = tmem + 2 * BN + stage * C::SF_COLS, tB = tA + 8;
+          const uint32_t sA = ring + stage * s_bytes, sB = sA + p.a_rows * (SK / 2) + 2 * SF_BYTES;
+          const uint32_t tA = tmem + 2 * BN + stage * SF_COLS, tB = tA + 8;
           const int k64 = min(SK / 64, (p.K - kb * SK + 63) / 64);     // MMAs that hold elements
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            if (2 * c < k64) {
-              copy_scales(tA + c * 4, sSA + c * kTileBytes);
-#pragma unroll
-              for (int r = 0; r < BN / kTileRows; ++r)
-                copy_scales(tB + (c * (BN / kTileRows) + r) * 4, sSB + (r * 2 + c) * kTileBytes);
-            }
-          }
           const uint64_t da = smem_desc(sA, false), db = smem_desc(sB, false);
 #pragma unroll
           for (int j = 0; j < SK / 64; ++j) {
             if (j < k64) {
               const uint32_t id = (uint32_t)(j & 1) * 2;                 // which half of the four scale bytes of a word
               mma_mxf4(d, da + (uint64_t)(2 * j), db + (uint64_t)(2 * j), idesc0 | (id << 4) | (id << 29), tA + (j >> 1) * 4,
-                       tB + (j >> 1) * (BN / kTileRows) * 4, (kb > 0 || j > 0) ? 1u : 0u);
+                       tB + (j >> 1) * 4, (kb > kb0 || j > 0) ? 1u : 0u);
             }
           }
           commit(bar_empty + stage * 8);
-          if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+          if (++stage == n_stages) { stage = 0; phase ^= 1u; }
         }
         if (!ok) break;
         commit(bar_tfull + acc * 8);
@@ -328,27 +355,50 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         if (acc == 0) acc_phase ^= 1u;
       }
     }
+  } else if (warp > 10) {
+    uint32_t stage = 0, phase = 0;
+    bool ok = true;
+    for (int t = t0; t < n_total && ok; t += t_step) {
+      for (int kb = kb0; kb < kb1; ++kb) {
+        if (!(ok = warp_wait(bar_full + stage * 8, phase, abort_flag, p.status))) break;
+        const uint32_t from = ring + stage * s_bytes + p.a_rows * (SK / 2) + lane * 16;
+        const uint32_t to = tmem + 2 * BN + stage * SF_COLS + ((uint32_t)((warp & 3) * 32) << 16);
+        store_scales(to, ld_shared_v4(from), ld_shared_v4(from + kTileBytes));
+        store_scales(to + 8, ld_shared_v4(from + SF_BYTES), ld_shared_v4(from + SF_BYTES + kTileBytes));
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        tc_fence_before();
+        if (lane == 0) arrive(bar_scales + stage * 8);
+        if (++stage == n_stages) { stage = 0; phase ^= 1u; }
+      }
+    }
   } else {
     const int q = warp & 3, half = (warp - 2) >> 2;
     const int row = q * 32 + lane;
-    constexpr int HC = BN / 2;                            // columns of this warp
     uint32_t acc = 0, acc_phase = 0;
     bool ok = true;
-    for (int t = blockIdx.x; t < n_total && ok; t += gridDim.x) {
+    for (int t = t0; t < n_total && ok; t += t_step) {
       const Item it = get_item(p, m_tiles, t);
       const int m = it.mt * BM + row;
       const int flat = MODE == STORE ? (m < p.M ? m : -1) : p.rowmap[m];
       const bool any = __any_sync(0xffffffffu, flat >= 0);
       if (!(ok = warp_wait(bar_tfull + acc * 8, acc_phase, abort_flag, p.status))) break;
       tc_fence_after();
-      const uint32_t taddr = tmem + acc * BN + half * HC + ((uint32_t)(q * 32) << 16);
-      const int n0 = it.nt * BN + half * HC;
-      static_assert(HC == 64, "one chunk per warp");
       float v[64];
-      if (any) load_chunk(taddr, v);
+      if (any) load_chunk(tmem + acc * BN + half * 64 + ((uint32_t)(q * 32) << 16), v);
       tc_fence_before();
-      arrive(bar_tempty + acc * 8);                       // the accumulator is read: the next tile may have it
-      if (any) finish_chunk<MODE>(p, it, v, n0, m, flat);
+      if (lane == 0) arrive(bar_tempty + acc * 8);        // the accumulator is read: the next tile may have it
+      if (SPLIT) {
+        // every MMA of this CTA has retired and every copy has landed: its ring is free for the partial tile
+        if (flat >= 0) {
+          const uint32_t to = ring + (uint32_t)(row * PART_PITCH + half * 64) * 4;
+#pragma unroll
+          for (int i = 0; i < 64; i += 4)
+            asm volatile("st.shared::cta.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to + i * 4), "f"(v[i]), "f"(v[i + 1]), "f"(v[i + 2]),
+                         "f"(v[i + 3]) : "memory");
+        }
+      } else if (any) {
+        finish_chunk<MODE>(p, it, v, it.nt * BN + half * 64, m, flat);
+      }
       acc ^= 1u;
       if (acc == 0) acc_phase ^= 1u;
     }
@@ -358,6 +408,51 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
   if (warp == 1) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
+  }
+  if constexpr (SPLIT) {
+    cluster_sync_all();
+    if (t0 < n_total && !*abort_flag) {
+      const Item it = get_item(p, m_tiles, t0);
+      const int rows = p.grouped ? p.tile_rows[it.mt] : min(BM, p.M - it.mt * BM);
+      const int width = BN / p.split, c0 = part * width, n0 = it.nt * BN + c0;
+      const int cols = min(width, p.N - n0);
+      if (p.wide && cols > 0) {                           // whole quads on 16-byte boundaries
+        const int quads = cols / 4;
+        for (int i = threadIdx.x; i < rows * quads; i += THREADS) {
+          const int r = i / quads, c = (i - r * quads) * 4;
+          const uint32_t at = ring + (uint32_t)(r * PART_PITCH + c0 + c) * 4;
+          float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int s = 0; s < p.split; ++s) {
+            const float4 x = ld_cluster_v4(map_to_cta(at, s));
+            a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
+          }
+          if (MODE == DOWN) {
+            const int flat = p.rowmap[it.mt * BM + r];
+            const float g = p.gates[flat];
+            *reinterpret_cast<float4*>((float*)p.y + (size_t)flat * p.N + n0 + c) = make_float4(a.x * g, a.y * g, a.z * g, a.w * g);
+          } else {
+            const size_t o = ((size_t)it.b * p.M + it.mt * BM + r) * p.N + n0 + c;
+            if (p.out_bf16) {
+              __nv_bfloat162 h[2] = {__floats2bfloat162_rn(a.x, a.y), __floats2bfloat162_rn(a.z, a.w)};
+              *reinterpret_cast<uint2*>((__nv_bfloat16*)p.y + o) = *reinterpret_cast<const uint2*>(h);
+            } else {
+              *reinterpret_cast<float4*>((float*)p.y + o) = a;
+            }
+          }
+        }
+      } else if (cols > 0) {
+        for (int i = threadIdx.x; i < rows * cols; i += THREADS) {
+          const int r = i / cols, c = i - r * cols;
+          const uint32_t at = ring + (uint32_t)(r * PART_PITCH + c0 + c) * 4;
+          float a = 0.f;
+          for (int s = 0; s < p.split; ++s) a += ld_cluster(map_to_cta(at, s));
+          const size_t o = ((size_t)it.b * p.M + it.mt * BM + r) * p.N + n0 + c;     // STORE (DOWN's rows are wide)
+          if (p.out_bf16) ((__nv_bfloat16*)p.y)[o] = __float2bfloat16_rn(a);
+          else ((float*)p.y)[o] = a;
+        }
+      }
+    }
+    cluster_sync_all();                                   // nobody leaves while its partial tile is being read
   }
 }
 
@@ -377,11 +472,10 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
 //   warp 0  TMA   warp 1  MMAs (one lane of the leader CTA)   warps 2-9  epilogue, two 64-column chunks each
 //   warps 10-13  scales   warp 14  TMA of the scales
 constexpr int P_STAGES = 6, P_RING = 8;                  // stages of codes, of scales
-constexpr int P_B_BYTES = 128 * SK / 2;
-constexpr int P_STAGE_BYTES = A_BYTES + P_B_BYTES;
+constexpr int P_STAGE_BYTES = A_BYTES + B_BYTES;
 constexpr int P_SCALE_BYTES = 6 * kTileBytes;            // of a stage and CTA: two tiles of A, two of each half of B
 constexpr int P_SMEM = P_STAGES * P_STAGE_BYTES + P_RING * P_SCALE_BYTES + 1024 + 384;
-constexpr int P_THREADS = THREADS + 160;
+constexpr int P_THREADS = 64 + EPI_WARPS * 32 + 160;
 constexpr int P_ACC1 = 128, P_SF0 = 384, P_SF_COLS = 24, P_SF_SLOTS = 5;
 static_assert(P_SF0 + P_SF_SLOTS * P_SF_COLS <= 512 && P_ACC1 + 256 <= P_SF0, "tensor memory");
 static_assert(P_STAGES * 16 + P_SF_SLOTS * 8 + P_RING * 16 + 40 <= 384 && P_SMEM <= 227 * 1024, "shared memory");
@@ -393,10 +487,6 @@ __device__ __forceinline__ void mma_mxf4_pair(uint32_t d, uint64_t a, uint64_t b
       "setp.ne.b32 p, %6, 0;\n\t"
       "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
       ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accum) : "memory");
-}
-__device__ __forceinline__ void store_scales(uint32_t taddr, const uint4& lo, const uint4& hi) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-               ::"r"(taddr), "r"(lo.x), "r"(lo.y), "r"(lo.z), "r"(lo.w), "r"(hi.x), "r"(hi.y), "r"(hi.z), "r"(hi.w) : "memory");
 }
 
 template <int MODE>
@@ -632,16 +722,35 @@ bool allow_smem(const void* kernel, int bytes, std::atomic<uint64_t>& done) {
   return true;
 }
 
-template <int MODE, int BN>
-btx_status launch(const GemmArgs& g, Params p, long long max_items, cudaStream_t st) {
+template <int MODE, bool SPLIT>
+btx_status launch(const GemmArgs& g, const Params& p, long long max_tiles, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
   CUtensorMap a, b;
-  if (!make_codes_map(&a, g.a_codes, g.K, g.M, g.batch, BM) || !make_codes_map(&b, g.b_codes, g.K, g.N, g.experts, BN) ||
-      !allow_smem((const void*)mx4_gemm_kernel<MODE, BN>, Cfg<BN>::SMEM, done))
+  if (!make_codes_map(&a, g.a_codes, g.K, g.M, g.batch, p.a_box) || !make_codes_map(&b, g.b_codes, g.K, g.N, g.experts, BN) ||
+      !allow_smem((const void*)mx4_gemm_kernel<MODE, SPLIT>, SMEM_BYTES, done))
     return BTX_ERR_CUDA;
-  const int blocks = max_items < sm_count() ? (int)max_items : sm_count();
-  return launch_after_predecessor(mx4_gemm_kernel<MODE, BN>, dim3(blocks), dim3(THREADS), Cfg<BN>::SMEM, st, MODE != STORE, a, b,
-                                  p) == cudaSuccess ? BTX_OK : BTX_ERR_CUDA;
+  cudaLaunchConfig_t cfg = {};
+  const long long blocks = SPLIT ? max_tiles * p.split : (max_tiles < sm_count() ? max_tiles : sm_count());
+  cfg.gridDim = dim3((unsigned)blocks); cfg.blockDim = dim3(THREADS); cfg.dynamicSmemBytes = SMEM_BYTES; cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  int n = 0;
+  if (MODE != STORE) {                                    // a programmatic dependent of the kernel before it
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  if (SPLIT) {
+    attr[n].id = cudaLaunchAttributeClusterDimension;
+    attr[n].val.clusterDim.x = p.split; attr[n].val.clusterDim.y = 1; attr[n++].val.clusterDim.z = 1;
+  }
+  cfg.attrs = attr; cfg.numAttrs = n;
+  return cudaLaunchKernelEx(&cfg, mx4_gemm_kernel<MODE, SPLIT>, a, b, p) == cudaSuccess ? BTX_OK : BTX_ERR_CUDA;
+}
+
+// CTAs per tile: as many as keep every multiprocessor busy at most once, with two stages each at least
+int split_of(long long tiles, long long K) {
+  int s = 1;
+  while (s < 8 && 2 * s * tiles <= sm_count() && 4 * s <= (K + SK - 1) / SK) s *= 2;
+  return s;
 }
 
 template <int MODE>
@@ -661,10 +770,10 @@ btx_status launch_pair(const GemmArgs& g, Params p, cudaStream_t st) {
                                   sb, p) == cudaSuccess ? BTX_OK : BTX_ERR_CUDA;
 }
 
-Params base_params(const GemmArgs& g, int bn) {
+Params base_params(const GemmArgs& g) {
   Params p = {};
   p.M = g.M; p.N = g.N; p.K = g.K; p.batch = g.batch; p.status = g.status;
-  p.m_tiles = (g.M + BM - 1) / BM; p.n_tiles = (g.N + bn - 1) / bn;
+  p.m_tiles = (g.M + BM - 1) / BM; p.n_tiles = (g.N + BN - 1) / BN; p.split = 1;
   p.kt = (int)scale_tiles_k(g.K); p.tile_step = 1;
   p.a_row_tiles = (g.M + kTileRows - 1) / kTileRows; p.b_row_tiles = (g.N + kTileRows - 1) / kTileRows;
   p.a_scales = g.a_scales; p.b_scales = g.b_scales;
@@ -683,30 +792,39 @@ bool pairs_fit(long long rows, long long experts, long long d, long long F) {
 }
 
 btx_status launch_matmul(const GemmArgs& g, int dtype, void* y, cudaStream_t st) {
-  constexpr int BN = 128;
-  Params p = base_params(g, BN);
+  Params p = base_params(g);
   p.y = y; p.out_bf16 = dtype == BTX_BF16;
   p.wide = aligned32(y) && (size_t)g.N * (p.out_bf16 ? 2 : 4) % 32 == 0;
   if (use_pairs((long long)g.batch * ((g.M + 255) / 256) * ((g.N + 255) / 256), g.M)) return launch_pair<STORE>(g, p, st);
-  return launch<STORE, BN>(g, p, (long long)p.m_tiles * p.n_tiles * p.batch, st);
+  const long long tiles = (long long)p.m_tiles * p.n_tiles * p.batch;
+  p.a_rows = p.a_box = g.M < BM ? (g.M + 31) / 32 * 32 : BM;
+  p.split = split_of(tiles, g.K);
+  return p.split > 1 ? launch<STORE, true>(g, p, tiles, st) : launch<STORE, false>(g, p, tiles, st);
+}
+
+static Params grouped_params(const GemmArgs& g, const Dispatch& q) {
+  Params p = base_params(g);
+  p.grouped = 1; p.n_row_tiles = q.n_tiles; p.tile_expert = q.tile_expert; p.tile_rows = q.tile_rows; p.rowmap = q.rowmap;
+  // a tile holds at most R rows; in small batches few of its rows are used, and only those are fetched
+  p.a_rows = q.R < BM ? (q.R + 31) / 32 * 32 : BM;
+  p.a_box = q.R <= 16 * BM ? 32 : BM;
+  return p;
 }
 
 btx_status launch_gate_up(const GemmArgs& g, const Dispatch& q, uint8_t* act_codes, uint8_t* act_scales, cudaStream_t st) {
-  constexpr int BN = 128;
-  Params p = base_params(g, BN);
-  p.grouped = 1; p.n_row_tiles = q.n_tiles; p.tile_expert = q.tile_expert; p.rowmap = q.rowmap;
+  Params p = grouped_params(g, q);
   p.act_codes = act_codes; p.act_scales = act_scales;
   if (q.pad_tiles == 2) return launch_pair<GATE_UP>(g, p, st);
-  return launch<GATE_UP, BN>(g, p, (long long)p.m_tiles * p.n_tiles, st);
+  return launch<GATE_UP, false>(g, p, (long long)p.m_tiles * p.n_tiles, st);
 }
 
 btx_status launch_down(const GemmArgs& g, const Dispatch& q, const float* gates, float* rows, cudaStream_t st) {
-  constexpr int BN = 128;
-  Params p = base_params(g, BN);
-  p.grouped = 1; p.n_row_tiles = q.n_tiles; p.tile_expert = q.tile_expert; p.rowmap = q.rowmap;
-  p.gates = gates; p.y = rows; p.wide = aligned32(rows);
+  Params p = grouped_params(g, q);
+  p.gates = gates; p.y = rows; p.wide = 1;                // rows of a multiple of 32 columns in a workspace region
   if (q.pad_tiles == 2) return launch_pair<DOWN>(g, p, st);
-  return launch<DOWN, BN>(g, p, (long long)p.m_tiles * p.n_tiles, st);
+  const long long tiles = (long long)p.m_tiles * p.n_tiles;
+  p.split = split_of(tiles, g.K);
+  return p.split > 1 ? launch<DOWN, true>(g, p, tiles, st) : launch<DOWN, false>(g, p, tiles, st);
 }
 
 }  // namespace mx4
