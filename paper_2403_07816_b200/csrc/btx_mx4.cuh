@@ -53,6 +53,9 @@ int dispatch_blocks(long long R);
 cudaError_t launch_dispatch(const Dispatch& q, cudaStream_t st);
 // x [T, d] cast to MXFP4 and written to the k padded rows of every token
 cudaError_t launch_quantize_rows(const Dispatch& q, int dtype, const void* x, uint8_t* codes, uint8_t* scales, cudaStream_t st);
+// both in one launch, for small batches
+bool dispatch_cast_fits(const Dispatch& q);
+cudaError_t launch_dispatch_cast(const Dispatch& q, int dtype, const void* x, uint8_t* codes, uint8_t* scales, cudaStream_t st);
 // y[t] = sum over slots with an expert, and over `splits` partial copies, of rows[split][t*k+slot]
 cudaError_t launch_combine_rows(const Dispatch& q, int dtype, const float* rows, int splits, void* y, cudaStream_t st);
 

@@ -181,9 +181,13 @@ extern "C" btx_status btx_mx4_moe_forward(const btx_mx4_moe_desc* desc, const vo
   uint8_t *xs = (uint8_t*)ws + pl.w_xs, *xs_scales = (uint8_t*)ws + pl.w_xs_scales;
   uint8_t *act = (uint8_t*)ws + pl.w_act, *act_scales = (uint8_t*)ws + pl.w_act_scales;
   float* rows = (float*)(ws + pl.w_rows);
-  // every kernel after the first is a programmatic dependent of the one before it
-  if (launch_dispatch(q, st) != cudaSuccess) return BTX_ERR_CUDA;
-  if (launch_quantize_rows(q, desc->dtype, x, xs, xs_scales, st) != cudaSuccess) return BTX_ERR_CUDA;
+  // every kernel is a programmatic dependent of the one before it
+  if (dispatch_cast_fits(q)) {
+    if (launch_dispatch_cast(q, desc->dtype, x, xs, xs_scales, st) != cudaSuccess) return BTX_ERR_CUDA;
+  } else {
+    if (launch_dispatch(q, st) != cudaSuccess) return BTX_ERR_CUDA;
+    if (launch_quantize_rows(q, desc->dtype, x, xs, xs_scales, st) != cudaSuccess) return BTX_ERR_CUDA;
+  }
   GemmArgs g = {};
   g.batch = 1; g.M = q.m_tiles_max * kTileRows; g.experts = desc->E; g.status = q.status;
   g.a_codes = xs; g.a_scales = xs_scales; g.b_codes = (const uint8_t*)w13_codes; g.b_scales = (const uint8_t*)w13_scales;

@@ -21,6 +21,7 @@ using routedev::Vec;
 constexpr unsigned kAll = 0xffffffffu;
 constexpr int kCastThreads = 256;
 constexpr int kCastUnroll = 4;             // 256-element chunks a warp has in flight
+constexpr int kFusedMaxR = 1024;           // assignments of a batch that is dispatched and cast in one launch
 constexpr int kSortThreads = 512;
 constexpr int kSortChunk = 2048;           // assignments per block of the dispatch kernels
 
@@ -107,6 +108,8 @@ __global__ void __launch_bounds__(kCastThreads)
 quantize_kernel(const CastParams p, int vec, I items, int groups) {
   const int lane = threadIdx.x & 31;
   const int kt = (int)scale_tiles_k(p.K);
+  allow_dependents();
+  grid_dependency_wait();
   const size_t tiles = ((size_t)p.out_rows + kTileRows - 1) / kTileRows;
   for (I w = ((I)blockIdx.x * kCastThreads + threadIdx.x) >> 5; w < items; w += (I)gridDim.x * (kCastThreads / 32)) {
     const I r = w / (I)groups;
@@ -151,6 +154,8 @@ dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__
                   T* __restrict__ dst) {
   const int lane = threadIdx.x & 31;
   const int kt = (int)scale_tiles_k(K);
+  allow_dependents();
+  grid_dependency_wait();
   const size_t tiles = ((size_t)rows + kTileRows - 1) / kTileRows;
   for (I w = ((I)blockIdx.x * kCastThreads + threadIdx.x) >> 5; w < items; w += (I)gridDim.x * (kCastThreads / 32)) {
     const I r = w / (I)groups;
@@ -283,6 +288,7 @@ __global__ void __launch_bounds__(kSortThreads)
 dispatch_one_kernel(const Dispatch q) {
   __shared__ SortShared s;
   allow_dependents();
+  grid_dependency_wait();
   if (threadIdx.x < kStatusWords) q.status[threadIdx.x] = 0;
   for (int i = threadIdx.x; i <= kMaxExperts4; i += kSortThreads) { s.cnt[i] = 0; s.running[i] = 0; }
   __syncthreads();
@@ -300,6 +306,7 @@ __global__ void __launch_bounds__(kSortThreads)
 dispatch_count_kernel(const Dispatch q) {
   __shared__ int hist[kMaxExperts4];
   allow_dependents();
+  grid_dependency_wait();
   if (blockIdx.x == 0 && threadIdx.x < kStatusWords) q.status[threadIdx.x] = 0;
   for (int i = threadIdx.x; i < q.E; i += kSortThreads) hist[i] = 0;
   __syncthreads();
@@ -352,39 +359,114 @@ dispatch_scatter_kernel(const Dispatch q) {
   scatter_rounds(begin, min(q.R, begin + kSortChunk), q.E, q.topk_idx, s.running, s.wcnt, s.pad, q.flat2row, q.rowmap);
 }
 
+// kCastUnroll chunks of 256 elements of a token, cast once and written to the rows of its slots.
+template <typename T>
+__device__ __forceinline__ void cast_token_rows(const T* __restrict__ x, int d, int g, int lane, int k, const int* rows,
+                                                uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+  const int kt = (int)scale_tiles_k(d);
+  const int c0 = g * kCastUnroll * 256 + lane * 8;
+  Eight<T> v[kCastUnroll];
+#pragma unroll
+  for (int u = 0; u < kCastUnroll; ++u) {
+    if (c0 + u * 256 < d) v[u].load(x + c0 + u * 256, true);
+    else v[u].zero();
+  }
+  uint32_t code[kCastUnroll], byte[kCastUnroll];
+#pragma unroll
+  for (int u = 0; u < kCastUnroll; ++u) code[u] = cast8(v[u], byte[u]);
+  for (int j = 0; j < k; ++j) {
+    const int row = rows[j];
+    if (row < 0) continue;
+    uint8_t* to = codes + (size_t)row * (d / 2) + c0 / 2;
+    uint8_t* sc = scales + scale_offset(0, row, kt, c0 / 128) + (c0 / kBlock & 3);
+#pragma unroll
+    for (int u = 0; u < kCastUnroll; ++u) {
+      if (c0 + u * 256 < d) *reinterpret_cast<uint32_t*>(to + u * 128) = code[u];
+      if ((lane & 3) == 0 && c0 + u * 256 < kt * 128) sc[u * 2 * kTileBytes] = (uint8_t)byte[u];
+    }
+  }
+}
+
 template <typename T, typename I>
 __global__ void __launch_bounds__(kCastThreads)
 quantize_rows_kernel(const Dispatch q, const T* __restrict__ x, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
                      I items, int groups) {
   const int lane = threadIdx.x & 31;
-  const int kt = (int)scale_tiles_k(q.d);
   allow_dependents();
   grid_dependency_wait();
   for (I w = ((I)blockIdx.x * kCastThreads + threadIdx.x) >> 5; w < items; w += (I)gridDim.x * (kCastThreads / 32)) {
     const size_t t = (size_t)(w / (I)groups);
     const int g = (int)(w - (I)t * (I)groups);
-    const int c0 = g * kCastUnroll * 256 + lane * 8;
-    Eight<T> v[kCastUnroll];
+    cast_token_rows<T>(x + t * q.d, q.d, g, lane, q.k, q.flat2row + t * q.k, codes, scales);
+  }
+}
+
+// The dispatch of a small batch in the same launch as the cast: a block per token counts all assignments (a few
+// thousand at most) for itself, so nothing has to wait for a first kernel.  Block 0 also writes the tile lists.
+template <typename T>
+__global__ void __launch_bounds__(kCastThreads)
+dispatch_cast_kernel(const Dispatch q, const T* __restrict__ x, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+  __shared__ int idx[kFusedMaxR];
+  __shared__ int cnt[kMaxExperts4], pad[kMaxExperts4], row_of[kFusedMaxR];
+  __shared__ int n_tiles;
+  constexpr int NW = kCastThreads / 32;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const size_t t = blockIdx.x;
+  for (int e = tid; e < q.E; e += kCastThreads) cnt[e] = 0;
+  allow_dependents();
+  grid_dependency_wait();
+  __syncthreads();
+  for (int i = tid; i < q.R; i += kCastThreads) {
+    int e = q.topk_idx[i];
+    if ((unsigned)e >= (unsigned)q.E) e = -1;
+    idx[i] = e;
+    if (e >= 0) atomicAdd(&cnt[e], 1);
+  }
+  __syncthreads();
+  if (warp == 0) {                                         // first padded row of every expert
+    int before = 0;
+    for (int e0 = 0; e0 < q.E; e0 += 32) {
+      const int e = e0 + lane, unit = q.pad_tiles * kTileRows;
+      const int tiles = e < q.E ? (cnt[e] + unit - 1) / unit * q.pad_tiles : 0;
+      int incl = tiles;
 #pragma unroll
-    for (int u = 0; u < kCastUnroll; ++u) {
-      if (c0 + u * 256 < q.d) v[u].load(x + t * q.d + c0 + u * 256, true);
-      else v[u].zero();
+      for (int o = 1; o < 32; o <<= 1) {
+        const int up = __shfl_up_sync(kAll, incl, o);
+        if (lane >= o) incl += up;
+      }
+      if (e < q.E) pad[e] = (before + incl - tiles) * kTileRows;
+      before += __shfl_sync(kAll, incl, 31);
     }
-    uint32_t code[kCastUnroll], byte[kCastUnroll];
-#pragma unroll
-    for (int u = 0; u < kCastUnroll; ++u) code[u] = cast8(v[u], byte[u]);
-    for (int j = 0; j < q.k; ++j) {
-      const int row = q.flat2row[t * q.k + j];
-      if (row < 0) continue;
-      uint8_t* to = codes + (size_t)row * (q.d / 2) + c0 / 2;
-      uint8_t* sc = scales + scale_offset(0, row, kt, c0 / 128) + (c0 / kBlock & 3);
-#pragma unroll
-      for (int u = 0; u < kCastUnroll; ++u) {
-        if (c0 + u * 256 < q.d) *reinterpret_cast<uint32_t*>(to + u * 128) = code[u];
-        if ((lane & 3) == 0 && c0 + u * 256 < kt * 128) sc[u * 2 * kTileBytes] = (uint8_t)byte[u];
+    if (lane == 0) n_tiles = before;
+  }
+  __syncthreads();
+  // rows of this token's assignments: rank among the earlier assignments of the same expert
+  for (int j = warp; j < q.k; j += NW) {
+    const int i = (int)t * q.k + j, e = idx[i];
+    int rank = 0;
+    if (e >= 0)
+      for (int b = 0; b < i; b += 32) rank += __popc(__ballot_sync(kAll, b + lane < i && idx[b + lane] == e));
+    const int row = e >= 0 ? pad[e] + rank : -1;
+    if (lane == 0) {
+      row_of[j] = row;
+      q.flat2row[i] = row;
+      if (row >= 0) q.rowmap[row] = i;
+    }
+  }
+  if (t == 0) {
+    if (tid < kStatusWords) q.status[tid] = 0;
+    if (tid == 0) q.n_tiles[0] = n_tiles;
+    for (int e = warp; e < q.E; e += NW) {
+      const int c = cnt[e], unit = q.pad_tiles * kTileRows, end = (c + unit - 1) / unit * unit, first = pad[e];
+      for (int r = c + lane; r < end; r += 32) q.rowmap[first + r] = -1;
+      for (int j = lane; j < end / kTileRows; j += 32) {
+        q.tile_expert[first / kTileRows + j] = e;
+        q.tile_rows[first / kTileRows + j] = max(0, min(kTileRows, c - j * kTileRows));
       }
     }
   }
+  __syncthreads();
+  for (int g = warp; g * kCastUnroll * 256 < q.d; g += NW) cast_token_rows<T>(x + t * q.d, q.d, g, lane, q.k, row_of, codes, scales);
 }
 
 // A thread owns 16 bytes of y; slots and splits are added in order, in fp32, and rounded once.
@@ -440,9 +522,12 @@ cudaError_t launch_quantize(const CastParams& p, int dtype, cudaStream_t st) {
   const int esize = dtype == BTX_BF16 ? 2 : 4;
   const int vec = ((uintptr_t)p.src & 15) == 0 && p.row_stride * esize % 16 == 0 && p.batch_stride * esize % 16 == 0;
   return by_index(items, [&](auto n) {
-    if (dtype == BTX_BF16) quantize_kernel<__nv_bfloat16><<<cast_blocks(items), kCastThreads, 0, st>>>(p, vec, n, groups);
-    else quantize_kernel<float><<<cast_blocks(items), kCastThreads, 0, st>>>(p, vec, n, groups);
-    return cudaGetLastError();
+    using I = decltype(n);
+    if (dtype == BTX_BF16)
+      return launch_after_predecessor(quantize_kernel<__nv_bfloat16, I>, dim3(cast_blocks(items)), dim3(kCastThreads), 0, st, true, p,
+                                      vec, n, groups);
+    return launch_after_predecessor(quantize_kernel<float, I>, dim3(cast_blocks(items)), dim3(kCastThreads), 0, st, true, p, vec, n,
+                                    groups);
   });
 }
 
@@ -451,11 +536,12 @@ cudaError_t launch_dequantize(const uint8_t* codes, const uint8_t* scales, int b
   const int groups = cast_groups(K);
   const long long items = (long long)batch * rows * groups;
   return by_index(items, [&](auto n) {
+    using I = decltype(n);
     if (dtype == BTX_BF16)
-      dequantize_kernel<<<cast_blocks(items), kCastThreads, 0, st>>>(codes, scales, rows, K, n, groups, (__nv_bfloat16*)dst);
-    else
-      dequantize_kernel<<<cast_blocks(items), kCastThreads, 0, st>>>(codes, scales, rows, K, n, groups, (float*)dst);
-    return cudaGetLastError();
+      return launch_after_predecessor(dequantize_kernel<__nv_bfloat16, I>, dim3(cast_blocks(items)), dim3(kCastThreads), 0, st, true,
+                                      codes, scales, rows, K, n, groups, (__nv_bfloat16*)dst);
+    return launch_after_predecessor(dequantize_kernel<float, I>, dim3(cast_blocks(items)), dim3(kCastThreads), 0, st, true, codes,
+                                    scales, rows, K, n, groups, (float*)dst);
   });
 }
 
@@ -463,14 +549,22 @@ int dispatch_blocks(long long R) { return (int)((R + kSortChunk - 1) / kSortChun
 
 cudaError_t launch_dispatch(const Dispatch& q, cudaStream_t st) {
   if (q.blocks <= 1) {
-    dispatch_one_kernel<<<1, kSortThreads, 0, st>>>(q);
-    return cudaGetLastError();
+    return launch_after_predecessor(dispatch_one_kernel, dim3(1), dim3(kSortThreads), 0, st, true, q);
   }
-  dispatch_count_kernel<<<q.blocks, kSortThreads, 0, st>>>(q);
-  cudaError_t e = cudaGetLastError();
+  cudaError_t e = launch_after_predecessor(dispatch_count_kernel, dim3(q.blocks), dim3(kSortThreads), 0, st, true, q);
   if (e != cudaSuccess) return e;
   if ((e = launch_after_predecessor(dispatch_scan_kernel, dim3(1), dim3(kSortThreads), 0, st, true, q)) != cudaSuccess) return e;
   return launch_after_predecessor(dispatch_scatter_kernel, dim3(q.blocks), dim3(kSortThreads), 0, st, true, q);
+}
+
+bool dispatch_cast_fits(const Dispatch& q) { return q.R <= kFusedMaxR && q.T <= 2 * sm_count(); }
+
+cudaError_t launch_dispatch_cast(const Dispatch& q, int dtype, const void* x, uint8_t* codes, uint8_t* scales, cudaStream_t st) {
+  if (dtype == BTX_BF16)
+    return launch_after_predecessor(dispatch_cast_kernel<__nv_bfloat16>, dim3(q.T), dim3(kCastThreads), 0, st, true, q,
+                                    (const __nv_bfloat16*)x, codes, scales);
+  return launch_after_predecessor(dispatch_cast_kernel<float>, dim3(q.T), dim3(kCastThreads), 0, st, true, q, (const float*)x, codes,
+                                  scales);
 }
 
 cudaError_t launch_quantize_rows(const Dispatch& q, int dtype, const void* x, uint8_t* codes, uint8_t* scales, cudaStream_t st) {

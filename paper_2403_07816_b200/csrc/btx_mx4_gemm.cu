@@ -734,10 +734,8 @@ btx_status launch(const GemmArgs& g, const Params& p, long long max_tiles, cudaS
   cfg.gridDim = dim3((unsigned)blocks); cfg.blockDim = dim3(THREADS); cfg.dynamicSmemBytes = SMEM_BYTES; cfg.stream = st;
   cudaLaunchAttribute attr[2];
   int n = 0;
-  if (MODE != STORE) {                                    // a programmatic dependent of the kernel before it
-    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[n++].val.programmaticStreamSerializationAllowed = 1;
-  }
+  attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;      // a programmatic dependent of the kernel before it
+  attr[n++].val.programmaticStreamSerializationAllowed = 1;
   if (SPLIT) {
     attr[n].id = cudaLaunchAttributeClusterDimension;
     attr[n].val.clusterDim.x = p.split; attr[n].val.clusterDim.y = 1; attr[n++].val.clusterDim.z = 1;
@@ -766,7 +764,7 @@ btx_status launch_pair(const GemmArgs& g, Params p, cudaStream_t st) {
   const long long items = (long long)p.m_tiles * p.n_tiles * p.batch;
   int pairs = sm_count() / 2;
   if (items < pairs) pairs = (int)items;
-  return launch_after_predecessor(mx4_gemm_pair_kernel<MODE>, dim3(2 * pairs), dim3(P_THREADS), P_SMEM, st, MODE != STORE, a, b, sa,
+  return launch_after_predecessor(mx4_gemm_pair_kernel<MODE>, dim3(2 * pairs), dim3(P_THREADS), P_SMEM, st, true, a, b, sa,
                                   sb, p) == cudaSuccess ? BTX_OK : BTX_ERR_CUDA;
 }
 

@@ -246,6 +246,8 @@ route_scored_kernel(const T* __restrict__ logits, const RouteParams p, int sum2,
     for (int i = threadIdx.x; i < p.E; i += blockDim.x) hist[i] = 0;
     __syncthreads();
   }
+  allow_dependents();
+  grid_dependency_wait();
   const float err_s = SIGMOID ? 0x1p-22f : 0x1p-18f, err_0 = 0x1p-23f, err_c = 0x1p-24f;
   const bool need_total = !SIGMOID && (p.scores != nullptr || biased || (grouped && sum2) || !p.renorm);
   const bool exact_keys = !biased && sizeof(T) == 2;               // 16-bit logits keep every bit in a packed key
@@ -471,6 +473,8 @@ route_scored_backward_kernel(int Tn, int E, int k, int renorm, float scale, long
 #pragma unroll
   for (int i = 0; i < EPL; ++i) add_s[warp][i * 32 + lane] = 0.f;
   __syncwarp();
+  allow_dependents();
+  grid_dependency_wait();
   for (int t = blockIdx.x * kRsWarps + warp; t < Tn; t += gridDim.x * kRsWarps) {
     const T* row = logits + (long long)t * stride;
     int sel = -1;
@@ -596,24 +600,18 @@ cudaError_t launch_route_t(const btx_route_desc* d, const void* logits, RoutePar
     if (e != cudaSuccess) return e;
   }
   const int sum2 = d->group_score == BTX_GROUP_SUM2;
-  if (d->score == BTX_SCORE_SIGMOID)
-    route_scored_kernel<T, EPL, true><<<blocks, W * 32, 0, st>>>((const T*)logits, p, sum2, vec);
-  else
-    route_scored_kernel<T, EPL, false><<<blocks, W * 32, 0, st>>>((const T*)logits, p, sum2, vec);
-  return cudaGetLastError();
+  return launch_after_predecessor(d->score == BTX_SCORE_SIGMOID ? route_scored_kernel<T, EPL, true> : route_scored_kernel<T, EPL, false>,
+                                  dim3(blocks), dim3(W * 32), 0, st, true, (const T*)logits, p, sum2, vec);
 }
 
 template <typename T, int EPL>
 cudaError_t launch_route_backward_t(const btx_route_desc* d, const void* logits, long long stride, const int32_t* topk_idx,
                                     const float* dgates, void* dlogits, long long out_stride, cudaStream_t st) {
   const int vi = row_vectors(logits, stride, d->E, sizeof(T)), vo = row_vectors(dlogits, out_stride, d->E, sizeof(T));
-  if (d->score == BTX_SCORE_SIGMOID)
-    route_scored_backward_kernel<T, EPL, true><<<row_blocks(d->T, kRsWarps, 8), kRsWarps * 32, 0, st>>>(
-        d->T, d->E, d->k, d->renorm != 0, d->scale, stride, vi, vo, (const T*)logits, topk_idx, dgates, (T*)dlogits, out_stride);
-  else
-    route_scored_backward_kernel<T, EPL, false><<<row_blocks(d->T, kRsWarps, 8), kRsWarps * 32, 0, st>>>(
-        d->T, d->E, d->k, d->renorm != 0, d->scale, stride, vi, vo, (const T*)logits, topk_idx, dgates, (T*)dlogits, out_stride);
-  return cudaGetLastError();
+  return launch_after_predecessor(
+      d->score == BTX_SCORE_SIGMOID ? route_scored_backward_kernel<T, EPL, true> : route_scored_backward_kernel<T, EPL, false>,
+      dim3(row_blocks(d->T, kRsWarps, 8)), dim3(kRsWarps * 32), 0, st, true, d->T, d->E, d->k, (int)(d->renorm != 0), d->scale, stride,
+      vi, vo, (const T*)logits, topk_idx, dgates, (T*)dlogits, out_stride);
 }
 
 // experts per lane: the power of two that covers E with 32 lanes
