@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libbtx.so")
 SOURCES = ["btx_api.cu", "btx_routing.cu", "btx_merge.cu", "btx_gemm_simt.cu", "btx_gemm_tc.cu", "btx_gemm_decode.cu",
            "btx_gemm_fused.cu", "btx_route_scored.cu", "btx_mx4_cast.cu", "btx_mx4_gemm.cu",
-           "btx_mx4_api.cu"]
+           "btx_mx4_layer.cu", "btx_mx4_api.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC"]
 

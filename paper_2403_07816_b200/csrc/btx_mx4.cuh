@@ -53,9 +53,6 @@ int dispatch_blocks(long long R);
 cudaError_t launch_dispatch(const Dispatch& q, cudaStream_t st);
 // x [T, d] cast to MXFP4 and written to the k padded rows of every token
 cudaError_t launch_quantize_rows(const Dispatch& q, int dtype, const void* x, uint8_t* codes, uint8_t* scales, cudaStream_t st);
-// both in one launch, for small batches
-bool dispatch_cast_fits(const Dispatch& q);
-cudaError_t launch_dispatch_cast(const Dispatch& q, int dtype, const void* x, uint8_t* codes, uint8_t* scales, cudaStream_t st);
 // y[t] = sum over slots with an expert, and over `splits` partial copies, of rows[split][t*k+slot]
 cudaError_t launch_combine_rows(const Dispatch& q, int dtype, const float* rows, int splits, void* y, cudaStream_t st);
 
@@ -73,6 +70,13 @@ btx_status launch_matmul(const GemmArgs& g, int dtype, void* y, cudaStream_t st)
 btx_status launch_gate_up(const GemmArgs& g, const Dispatch& q, uint8_t* act_codes, uint8_t* act_scales, cudaStream_t st);
 // W2 product, gate-scaled fp32 rows at [t*k+slot]
 btx_status launch_down(const GemmArgs& g, const Dispatch& q, const float* gates, float* rows, cudaStream_t st);
+
+// The whole layer of a small batch as one cooperative kernel; refused (BTX_ERR_CUDA, nothing launched) where not every
+// block can be resident.  `rows` holds layer_rows_floats floats.
+bool layer_fits(const Dispatch& q);
+size_t layer_rows_floats(const Dispatch& q);
+btx_status launch_layer(const GemmArgs& up, const GemmArgs& down, const Dispatch& q, int dtype, const void* x, const float* gates,
+                        float* rows, uint8_t* act_codes, uint8_t* act_scales, void* y, cudaStream_t st);
 
 // 32 values of a lane group are cast with one scale: the byte is floor(log2 max) - 2 (bias 127, not below 0), 255
 // when the block holds an infinity or NaN; `inv` is the exact reciprocal of the scale.

@@ -57,7 +57,7 @@ btx_status make_moe_plan(const btx_mx4_moe_desc* d, MoePlan* pl) {
   pl->w_xs_scales = take((size_t)tiles * scale_tiles_k(d->d_model) * kTileBytes);
   pl->w_act = take(rp * (d->d_ff / 2));
   pl->w_act_scales = take((size_t)tiles * scale_tiles_k(d->d_ff) * kTileBytes);
-  pl->w_rows = take((size_t)R * d->d_model * 4);
+  pl->w_rows = take((layer_fits(q) ? layer_rows_floats(q) : (size_t)R * d->d_model) * 4);
   pl->bytes = o;
   return BTX_OK;
 }
@@ -181,20 +181,21 @@ extern "C" btx_status btx_mx4_moe_forward(const btx_mx4_moe_desc* desc, const vo
   uint8_t *xs = (uint8_t*)ws + pl.w_xs, *xs_scales = (uint8_t*)ws + pl.w_xs_scales;
   uint8_t *act = (uint8_t*)ws + pl.w_act, *act_scales = (uint8_t*)ws + pl.w_act_scales;
   float* rows = (float*)(ws + pl.w_rows);
-  // every kernel is a programmatic dependent of the one before it
-  if (dispatch_cast_fits(q)) {
-    if (launch_dispatch_cast(q, desc->dtype, x, xs, xs_scales, st) != cudaSuccess) return BTX_ERR_CUDA;
-  } else {
-    if (launch_dispatch(q, st) != cudaSuccess) return BTX_ERR_CUDA;
-    if (launch_quantize_rows(q, desc->dtype, x, xs, xs_scales, st) != cudaSuccess) return BTX_ERR_CUDA;
+  GemmArgs up = {}, down = {};
+  up.batch = 1; up.M = q.m_tiles_max * kTileRows; up.experts = desc->E; up.status = q.status;
+  up.a_codes = xs; up.a_scales = xs_scales; up.b_codes = (const uint8_t*)w13_codes; up.b_scales = (const uint8_t*)w13_scales;
+  up.N = 2 * desc->d_ff; up.K = desc->d_model;
+  down = up;
+  down.a_codes = act; down.a_scales = act_scales; down.b_codes = (const uint8_t*)w2_codes; down.b_scales = (const uint8_t*)w2_scales;
+  down.N = desc->d_model; down.K = desc->d_ff;
+  if (layer_fits(q)) {
+    if (launch_layer(up, down, q, desc->dtype, x, gates, rows, act, act_scales, y, st) == BTX_OK) return BTX_OK;
+    cudaGetLastError();                      // not every block can be resident: the launches below do the same work
   }
-  GemmArgs g = {};
-  g.batch = 1; g.M = q.m_tiles_max * kTileRows; g.experts = desc->E; g.status = q.status;
-  g.a_codes = xs; g.a_scales = xs_scales; g.b_codes = (const uint8_t*)w13_codes; g.b_scales = (const uint8_t*)w13_scales;
-  g.N = 2 * desc->d_ff; g.K = desc->d_model;
-  if ((s = launch_gate_up(g, q, act, act_scales, st)) != BTX_OK) return s;
-  g.a_codes = act; g.a_scales = act_scales; g.b_codes = (const uint8_t*)w2_codes; g.b_scales = (const uint8_t*)w2_scales;
-  g.N = desc->d_model; g.K = desc->d_ff;
-  if ((s = launch_down(g, q, gates, rows, st)) != BTX_OK) return s;
+  // every kernel is a programmatic dependent of the one before it
+  if (launch_dispatch(q, st) != cudaSuccess) return BTX_ERR_CUDA;
+  if (launch_quantize_rows(q, desc->dtype, x, xs, xs_scales, st) != cudaSuccess) return BTX_ERR_CUDA;
+  if ((s = launch_gate_up(up, q, act, act_scales, st)) != BTX_OK) return s;
+  if ((s = launch_down(down, q, gates, rows, st)) != BTX_OK) return s;
   return launch_combine_rows(q, desc->dtype, rows, 1, y, st) == cudaSuccess ? BTX_OK : BTX_ERR_CUDA;
 }

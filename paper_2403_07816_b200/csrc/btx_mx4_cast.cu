@@ -7,99 +7,15 @@
 //   dequantize   the same mapping backwards
 //   dispatch     stable counting sort of the assignments by expert, padded to 128-row tiles
 //   quantize_rows  quantize of x with every row written to the k rows of its token: x is read once
-#include <cuda_fp4.h>
-
-#include "btx_mx4.cuh"
-#include "btx_route_dev.cuh"
+#include "btx_mx4_dev.cuh"
 
 namespace btx {
 namespace mx4 {
 namespace {
 
-using routedev::Vec;
-
-constexpr unsigned kAll = 0xffffffffu;
 constexpr int kCastThreads = 256;
-constexpr int kCastUnroll = 4;             // 256-element chunks a warp has in flight
-constexpr int kFusedMaxR = 1024;           // assignments of a batch that is dispatched and cast in one launch
 constexpr int kSortThreads = 512;
 constexpr int kSortChunk = 2048;           // assignments per block of the dispatch kernels
-
-// Eight elements of a lane as they were loaded: their largest magnitude as the bits of a float (NaN and infinities
-// compare above every number), and their values.
-template <typename T> struct Eight;
-template <> struct Eight<float> {
-  uint4 a, b;
-  __device__ __forceinline__ void zero() { a = b = make_uint4(0, 0, 0, 0); }
-  __device__ __forceinline__ void load(const float* p, bool vec) {
-    if (vec) {
-      a = __ldcs(reinterpret_cast<const uint4*>(p));
-      b = __ldcs(reinterpret_cast<const uint4*>(p) + 1);
-    } else {
-      const uint32_t* w = reinterpret_cast<const uint32_t*>(p);
-      a = make_uint4(w[0], w[1], w[2], w[3]);
-      b = make_uint4(w[4], w[5], w[6], w[7]);
-    }
-  }
-  __device__ __forceinline__ uint32_t block_max() const {
-    constexpr uint32_t M = 0x7fffffffu;
-    uint32_t m = max(max(max(a.x & M, a.y & M), max(a.z & M, a.w & M)), max(max(b.x & M, b.y & M), max(b.z & M, b.w & M)));
-    m = max(m, __shfl_xor_sync(kAll, m, 1));
-    return max(m, __shfl_xor_sync(kAll, m, 2));
-  }
-  __device__ __forceinline__ void values(float (&v)[8]) const {
-    v[0] = __uint_as_float(a.x); v[1] = __uint_as_float(a.y); v[2] = __uint_as_float(a.z); v[3] = __uint_as_float(a.w);
-    v[4] = __uint_as_float(b.x); v[5] = __uint_as_float(b.y); v[6] = __uint_as_float(b.z); v[7] = __uint_as_float(b.w);
-  }
-};
-template <> struct Eight<__nv_bfloat16> {
-  uint4 a;
-  __device__ __forceinline__ void zero() { a = make_uint4(0, 0, 0, 0); }
-  __device__ __forceinline__ void load(const __nv_bfloat16* p, bool vec) {
-    if (vec) {
-      a = __ldcs(reinterpret_cast<const uint4*>(p));
-    } else {
-      const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
-      a = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
-    }
-  }
-  // two 16-bit maxima per instruction: half the comparisons of the widened values
-  __device__ __forceinline__ uint32_t block_max() const {
-    constexpr uint32_t M = 0x7fff7fffu;
-    uint32_t m = __vimax3_u16x2(a.x & M, a.y & M, a.z & M);
-    m = __vimax3_u16x2(m, a.w & M, __shfl_xor_sync(kAll, __vimax3_u16x2(m, a.w & M, 0u), 1));
-    m = __vimax3_u16x2(m, __shfl_xor_sync(kAll, m, 2), 0u);
-    return max(m & 0xffff0000u, m << 16);
-  }
-  __device__ __forceinline__ void values(float (&v)[8]) const { Vec<__nv_bfloat16>::unpack(a, v); }
-};
-
-// Four bytes of codes of eight elements times `inv`.
-__device__ __forceinline__ uint32_t pack_e2m1(const float (&v)[8], float inv) {
-  uint32_t q;
-  asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
-      "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n\t"
-      "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n\t"
-      "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n\t"
-      "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n\t"
-      "mov.b32 %0, {b0, b1, b2, b3};\n\t}"
-      : "=r"(q)
-      : "f"(v[0] * inv), "f"(v[1] * inv), "f"(v[2] * inv), "f"(v[3] * inv), "f"(v[4] * inv), "f"(v[5] * inv), "f"(v[6] * inv),
-        "f"(v[7] * inv));
-  return q;
-}
-
-// Eight elements of a block shared by four neighbouring lanes: four bytes of codes and the block's scale byte.
-template <typename T> __device__ __forceinline__ uint32_t cast8(const Eight<T>& x, uint32_t& byte) {
-  float inv, v[8];
-  byte = scale_byte(x.block_max(), inv);
-  x.values(v);
-  const uint32_t q = pack_e2m1(v, inv);
-  return byte == 255u ? 0u : q;
-}
-__device__ __forceinline__ size_t scale_offset(size_t tile_row0, int row, int kt, int chunk) {
-  return ((tile_row0 + row / kTileRows) * (size_t)kt + chunk) * kTileBytes + (row & 31) * 16 + ((row >> 5) & 3) * 4;
-}
 
 // A warp takes kCastUnroll chunks of 256 elements of one row at a time.  I: the type that numbers them; the two divisions
 // in 64 bits cost as many instructions as the cast of the chunks.
@@ -359,34 +275,6 @@ dispatch_scatter_kernel(const Dispatch q) {
   scatter_rounds(begin, min(q.R, begin + kSortChunk), q.E, q.topk_idx, s.running, s.wcnt, s.pad, q.flat2row, q.rowmap);
 }
 
-// kCastUnroll chunks of 256 elements of a token, cast once and written to the rows of its slots.
-template <typename T>
-__device__ __forceinline__ void cast_token_rows(const T* __restrict__ x, int d, int g, int lane, int k, const int* rows,
-                                                uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
-  const int kt = (int)scale_tiles_k(d);
-  const int c0 = g * kCastUnroll * 256 + lane * 8;
-  Eight<T> v[kCastUnroll];
-#pragma unroll
-  for (int u = 0; u < kCastUnroll; ++u) {
-    if (c0 + u * 256 < d) v[u].load(x + c0 + u * 256, true);
-    else v[u].zero();
-  }
-  uint32_t code[kCastUnroll], byte[kCastUnroll];
-#pragma unroll
-  for (int u = 0; u < kCastUnroll; ++u) code[u] = cast8(v[u], byte[u]);
-  for (int j = 0; j < k; ++j) {
-    const int row = rows[j];
-    if (row < 0) continue;
-    uint8_t* to = codes + (size_t)row * (d / 2) + c0 / 2;
-    uint8_t* sc = scales + scale_offset(0, row, kt, c0 / 128) + (c0 / kBlock & 3);
-#pragma unroll
-    for (int u = 0; u < kCastUnroll; ++u) {
-      if (c0 + u * 256 < d) *reinterpret_cast<uint32_t*>(to + u * 128) = code[u];
-      if ((lane & 3) == 0 && c0 + u * 256 < kt * 128) sc[u * 2 * kTileBytes] = (uint8_t)byte[u];
-    }
-  }
-}
-
 template <typename T, typename I>
 __global__ void __launch_bounds__(kCastThreads)
 quantize_rows_kernel(const Dispatch q, const T* __restrict__ x, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
@@ -399,74 +287,6 @@ quantize_rows_kernel(const Dispatch q, const T* __restrict__ x, uint8_t* __restr
     const int g = (int)(w - (I)t * (I)groups);
     cast_token_rows<T>(x + t * q.d, q.d, g, lane, q.k, q.flat2row + t * q.k, codes, scales);
   }
-}
-
-// The dispatch of a small batch in the same launch as the cast: a block per token counts all assignments (a few
-// thousand at most) for itself, so nothing has to wait for a first kernel.  Block 0 also writes the tile lists.
-template <typename T>
-__global__ void __launch_bounds__(kCastThreads)
-dispatch_cast_kernel(const Dispatch q, const T* __restrict__ x, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
-  __shared__ int idx[kFusedMaxR];
-  __shared__ int cnt[kMaxExperts4], pad[kMaxExperts4], row_of[kFusedMaxR];
-  __shared__ int n_tiles;
-  constexpr int NW = kCastThreads / 32;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const size_t t = blockIdx.x;
-  for (int e = tid; e < q.E; e += kCastThreads) cnt[e] = 0;
-  allow_dependents();
-  grid_dependency_wait();
-  __syncthreads();
-  for (int i = tid; i < q.R; i += kCastThreads) {
-    int e = q.topk_idx[i];
-    if ((unsigned)e >= (unsigned)q.E) e = -1;
-    idx[i] = e;
-    if (e >= 0) atomicAdd(&cnt[e], 1);
-  }
-  __syncthreads();
-  if (warp == 0) {                                         // first padded row of every expert
-    int before = 0;
-    for (int e0 = 0; e0 < q.E; e0 += 32) {
-      const int e = e0 + lane, unit = q.pad_tiles * kTileRows;
-      const int tiles = e < q.E ? (cnt[e] + unit - 1) / unit * q.pad_tiles : 0;
-      int incl = tiles;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int up = __shfl_up_sync(kAll, incl, o);
-        if (lane >= o) incl += up;
-      }
-      if (e < q.E) pad[e] = (before + incl - tiles) * kTileRows;
-      before += __shfl_sync(kAll, incl, 31);
-    }
-    if (lane == 0) n_tiles = before;
-  }
-  __syncthreads();
-  // rows of this token's assignments: rank among the earlier assignments of the same expert
-  for (int j = warp; j < q.k; j += NW) {
-    const int i = (int)t * q.k + j, e = idx[i];
-    int rank = 0;
-    if (e >= 0)
-      for (int b = 0; b < i; b += 32) rank += __popc(__ballot_sync(kAll, b + lane < i && idx[b + lane] == e));
-    const int row = e >= 0 ? pad[e] + rank : -1;
-    if (lane == 0) {
-      row_of[j] = row;
-      q.flat2row[i] = row;
-      if (row >= 0) q.rowmap[row] = i;
-    }
-  }
-  if (t == 0) {
-    if (tid < kStatusWords) q.status[tid] = 0;
-    if (tid == 0) q.n_tiles[0] = n_tiles;
-    for (int e = warp; e < q.E; e += NW) {
-      const int c = cnt[e], unit = q.pad_tiles * kTileRows, end = (c + unit - 1) / unit * unit, first = pad[e];
-      for (int r = c + lane; r < end; r += 32) q.rowmap[first + r] = -1;
-      for (int j = lane; j < end / kTileRows; j += 32) {
-        q.tile_expert[first / kTileRows + j] = e;
-        q.tile_rows[first / kTileRows + j] = max(0, min(kTileRows, c - j * kTileRows));
-      }
-    }
-  }
-  __syncthreads();
-  for (int g = warp; g * kCastUnroll * 256 < q.d; g += NW) cast_token_rows<T>(x + t * q.d, q.d, g, lane, q.k, row_of, codes, scales);
 }
 
 // A thread owns 16 bytes of y; slots and splits are added in order, in fp32, and rounded once.
@@ -555,16 +375,6 @@ cudaError_t launch_dispatch(const Dispatch& q, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   if ((e = launch_after_predecessor(dispatch_scan_kernel, dim3(1), dim3(kSortThreads), 0, st, true, q)) != cudaSuccess) return e;
   return launch_after_predecessor(dispatch_scatter_kernel, dim3(q.blocks), dim3(kSortThreads), 0, st, true, q);
-}
-
-bool dispatch_cast_fits(const Dispatch& q) { return q.R <= kFusedMaxR && q.T <= 2 * sm_count(); }
-
-cudaError_t launch_dispatch_cast(const Dispatch& q, int dtype, const void* x, uint8_t* codes, uint8_t* scales, cudaStream_t st) {
-  if (dtype == BTX_BF16)
-    return launch_after_predecessor(dispatch_cast_kernel<__nv_bfloat16>, dim3(q.T), dim3(kCastThreads), 0, st, true, q,
-                                    (const __nv_bfloat16*)x, codes, scales);
-  return launch_after_predecessor(dispatch_cast_kernel<float>, dim3(q.T), dim3(kCastThreads), 0, st, true, q, (const float*)x, codes,
-                                  scales);
 }
 
 cudaError_t launch_quantize_rows(const Dispatch& q, int dtype, const void* x, uint8_t* codes, uint8_t* scales, cudaStream_t st) {

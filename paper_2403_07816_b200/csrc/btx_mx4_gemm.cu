@@ -1,5 +1,5 @@
 // Products of MXFP4 matrices on the 5th-generation tensor cores (tcgen05.mma kind::mxf4.block_scale): codes straight
-// from memory to shared memory by TMA, scales by bulk copies and tcgen05.cp into tensor memory, fp32 accumulation in
+// from memory to shared memory by TMA, scales through shared memory and tcgen05.st into tensor memory, fp32 sums in
 // tensor memory; nothing is decoded on the way.  y = A B^T with both operands K-major, per output element
 //   sum over blocks of 32:  2^(sa - 127) 2^(sb - 127) sum a_i b_i.
 //
@@ -24,212 +24,17 @@
 //            silu(h1) * h3 in fp32, cast to MXFP4 in registers (32 neighbouring units are a block)
 //   DOWN     gate-scaled fp32 rows scattered to t*k+slot
 // Every wait is bounded (tcx::mbar_wait); a wait that runs out leaves BTX_ERR_TIMEOUT in the status word.
-#include <cuda_fp4.h>
-
-#include <atomic>
-
-#include "btx_mx4.cuh"
-#include "btx_tc_ptx.cuh"
+#include "btx_mx4_dev.cuh"
 
 namespace btx {
 namespace mx4 {
 namespace {
 
-using namespace tcx;
-
-constexpr int SK = 256;                                  // contraction elements per stage (128 bytes of codes)
-constexpr int BM = kTileRows;
-constexpr int BN = 128;
-constexpr int EPI_WARPS = 8;
 constexpr int THREADS = 96 + EPI_WARPS * 32 + 128;
-constexpr int A_BYTES = BM * SK / 2, B_BYTES = BN * SK / 2;
-constexpr int SF_BYTES = 2 * kTileBytes;                 // scales of a stage, of A or of B
-constexpr int MAX_STAGES = 10, SF_COLS = 16;             // tensor-memory columns of a stage's scales
 constexpr int RING_BYTES = 220 * 1024;
 constexpr int SMEM_BYTES = RING_BYTES + 1024 + 320;
 constexpr int PART_PITCH = BN + 4;                       // SPLIT: floats per row of a partial tile (a quad apart: no bank conflicts)
-static_assert(2 * BN + MAX_STAGES * SF_COLS <= 512, "accumulators and scales fit in tensor memory");
 static_assert(MAX_STAGES * 24 + 48 <= 320 && BM * PART_PITCH * 4 <= RING_BYTES, "shared memory");
-constexpr int GROUP_N = 8;                               // column tiles per raster group
-
-enum Mode { STORE = 0, GATE_UP = 1, DOWN = 2 };
-
-// bytes of a ring stage whose A part has `rows` rows, and how many fit
-inline __host__ __device__ int stage_bytes(int rows) { return rows * (SK / 2) + 2 * SF_BYTES + B_BYTES; }
-inline __host__ __device__ int stage_count(int rows) {
-  const int n = RING_BYTES / stage_bytes(rows);
-  return n < MAX_STAGES ? n : MAX_STAGES;
-}
-
-struct Params {
-  int M, N, K;                      // STORE: rows and columns of y; grouped: N = B rows per expert
-  int m_tiles, n_tiles, batch;
-  int grouped;
-  int tile_step;                    // 128-row tiles per row tile of this launch (1, or 2 for CTA pairs)
-  const int32_t* n_row_tiles;       // grouped: row tiles in use (device)
-  const int32_t* tile_expert;
-  const int32_t* tile_rows;         // grouped: rows of a tile that hold an assignment
-  const int32_t* rowmap;
-  int a_rows, a_box;                // rows of A per stage, rows per TMA operation
-  int split;                        // CTAs that share a tile's contraction
-  const uint8_t* a_scales;
-  const uint8_t* b_scales;
-  long long a_scale_batch, b_scale_batch;   // bytes from one matrix to the next
-  int kt;                           // scale tiles along K
-  int a_row_tiles, b_row_tiles;     // scale row tiles of one matrix
-  const float* gates;
-  void* y;
-  uint8_t* act_codes;
-  uint8_t* act_scales;
-  int out_bf16;
-  int wide;                         // output rows start on 32-byte boundaries
-  int32_t* status;
-};
-
-// ---- PTX of the one-CTA forms ----
-__device__ __forceinline__ void load_3d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-      ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar) : "memory");
-}
-__device__ __forceinline__ void load_bulk(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
-}
-__device__ __forceinline__ void commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void mma_mxf4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
-                                         uint32_t accum) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %6, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accum) : "memory");
-}
-// This lane's 16 bytes of two 512-byte scale tiles to eight tensor-memory columns of the warp's 32-lane quarter.  Word
-// c of a lane's 16 bytes belongs to row c * 32 + lane of a tile: it goes to column c, the same in all four quarters.
-__device__ __forceinline__ void store_scales(uint32_t taddr, const uint4& lo, const uint4& hi) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-               ::"r"(taddr), "r"(lo.x), "r"(lo.y), "r"(lo.z), "r"(lo.w), "r"(hi.x), "r"(hi.y), "r"(hi.z), "r"(hi.w) : "memory");
-}
-__device__ __forceinline__ void arrive(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-
-// A bounded wait of a whole warp: it gives up for all lanes or for none.
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* status) {
-  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, status));
-}
-
-__device__ __forceinline__ uint4 ld_shared_v4(uint32_t addr) {
-  uint4 v;
-  asm volatile("ld.shared::cta.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
-  return v;
-}
-
-struct Item { int mt, nt, b, e; };
-
-// Tile number -> (row tile, column tile): groups of GROUP_N column tiles, rows advance slowest inside a group.
-__device__ __forceinline__ Item get_item(const Params& p, int m_tiles, int t) {
-  Item it;
-  const int per = m_tiles * p.n_tiles;
-  it.b = t / per;
-  const int local = t - it.b * per;
-  const int full = p.n_tiles / GROUP_N, in_full = full * m_tiles * GROUP_N;
-  int g, width, rem;
-  if (local < in_full) { g = local / (m_tiles * GROUP_N); rem = local - g * m_tiles * GROUP_N; width = GROUP_N; }
-  else { g = full; rem = local - in_full; width = p.n_tiles - full * GROUP_N; }
-  it.mt = rem / width;
-  it.nt = g * GROUP_N + rem - it.mt * width;
-  it.e = p.grouped ? p.tile_expert[it.mt * p.tile_step] : it.b;
-  return it;
-}
-
-// 64 accumulator columns of one row per thread, by a whole warp
-__device__ __forceinline__ void load_chunk(uint32_t taddr, float (&v)[64]) {
-  uint32_t r[64];
-  __syncwarp();                                           // the tensor-memory load needs the whole warp
-#pragma unroll
-  for (int h = 0; h < 2; ++h)
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-        : "=r"(r[32 * h + 0]), "=r"(r[32 * h + 1]), "=r"(r[32 * h + 2]), "=r"(r[32 * h + 3]), "=r"(r[32 * h + 4]),
-          "=r"(r[32 * h + 5]), "=r"(r[32 * h + 6]), "=r"(r[32 * h + 7]), "=r"(r[32 * h + 8]), "=r"(r[32 * h + 9]),
-          "=r"(r[32 * h + 10]), "=r"(r[32 * h + 11]), "=r"(r[32 * h + 12]), "=r"(r[32 * h + 13]), "=r"(r[32 * h + 14]),
-          "=r"(r[32 * h + 15]), "=r"(r[32 * h + 16]), "=r"(r[32 * h + 17]), "=r"(r[32 * h + 18]), "=r"(r[32 * h + 19]),
-          "=r"(r[32 * h + 20]), "=r"(r[32 * h + 21]), "=r"(r[32 * h + 22]), "=r"(r[32 * h + 23]), "=r"(r[32 * h + 24]),
-          "=r"(r[32 * h + 25]), "=r"(r[32 * h + 26]), "=r"(r[32 * h + 27]), "=r"(r[32 * h + 28]), "=r"(r[32 * h + 29]),
-          "=r"(r[32 * h + 30]), "=r"(r[32 * h + 31])
-        : "r"(taddr + 32 * h));
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-  for (int i = 0; i < 64; ++i) v[i] = __uint_as_float(r[i]);
-}
-
-// What becomes of them (columns n0 .. n0 + 63 of the product).  m: the row of A; flat: its row of y (STORE) or its
-// assignment, -1 for a row that nobody asked for.
-template <int MODE>
-__device__ __forceinline__ void finish_chunk(const Params& p, const Item& it, float (&v)[64], int n0, int m, int flat) {
-  if (flat < 0 || n0 >= (MODE == GATE_UP ? (p.N + 255) / 256 * 256 : p.N)) return;
-  const bool wide = p.wide != 0;
-  if constexpr (MODE == GATE_UP) {
-    const int F = p.N / 2;
-    const int f0 = n0 / 2;                                // 32 hidden units: one block
-    float a[32];
-    uint32_t amax = 0;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      a[i] = fast_swiglu(v[2 * i], v[2 * i + 1]);
-      amax = max(amax, __float_as_uint(a[i]) & 0x7fffffffu);
-    }
-    float inv;
-    uint32_t byte = scale_byte(amax, inv);
-    uint32_t w[4] = {0, 0, 0, 0};
-    if (byte != 255u) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        w[i / 4] |= (uint32_t)__nv_cvt_float2_to_fp4x2(make_float2(a[2 * i] * inv, a[2 * i + 1] * inv), __NV_E2M1,
-                                                       cudaRoundNearest) << (8 * (i & 3));
-    }
-    // past the last unit there is no block, but the other half of an MMA's 64 elements wants a finite scale
-    if (f0 >= F) byte = 0;
-    const int blk = f0 / kBlock, akt = (int)scale_tiles_k(F);
-    if (blk < 4 * akt)
-      p.act_scales[((size_t)(m / kTileRows) * akt + blk / 4) * kTileBytes + (m & 31) * 16 + (m >> 5 & 3) * 4 + (blk & 3)] = (uint8_t)byte;
-    if (f0 < F) *reinterpret_cast<uint4*>(p.act_codes + (size_t)m * (F / 2) + f0 / 2) = make_uint4(w[0], w[1], w[2], w[3]);
-  } else {
-    const size_t o = MODE == STORE ? ((size_t)it.b * p.M + flat) * p.N + n0 : (size_t)flat * p.N + n0;
-    if (MODE == DOWN) {
-      const float g = p.gates[flat];
-#pragma unroll
-      for (int i = 0; i < 64; ++i) v[i] *= g;
-    }
-    if (MODE == STORE && p.out_bf16) {
-      __nv_bfloat16* y = (__nv_bfloat16*)p.y + o;
-      if (wide && n0 + 64 <= p.N) {
-#pragma unroll
-        for (int i = 0; i < 64; i += 16) st32(y + i, pack8(v + i), pack8(v + i + 8), true);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 64; ++i)
-          if (n0 + i < p.N) y[i] = __float2bfloat16_rn(v[i]);
-      }
-    } else {
-      float* y = (float*)p.y + o;
-      if (wide && n0 + 64 <= p.N) {
-#pragma unroll
-        for (int i = 0; i < 64; i += 8) st32(y + i, f4(v + i), f4(v + i + 4), true);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 64; ++i)
-          if (n0 + i < p.N) y[i] = v[i];
-      }
-    }
-  }
-}
 
 // SPLIT: one quad or one element of the sum over the cluster's partial tiles, in CTA order.
 __device__ __forceinline__ float4 ld_cluster_v4(uint32_t addr) {
@@ -256,7 +61,7 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctl + MAX_STAGES * 24 + 32);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(ctl + MAX_STAGES * 24 + 40);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int n_stages = stage_count(p.a_rows), s_bytes = stage_bytes(p.a_rows);
+  const int n_stages = stage_count(p.a_rows, RING_BYTES), s_bytes = stage_bytes(p.a_rows);
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < n_stages; ++s) { mbar_init(bar_full + s * 8, 2); mbar_init(bar_empty + s * 8, 1); mbar_init(bar_scales + s * 8, 4); }
@@ -687,18 +492,6 @@ mx4_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
   }
 }
 
-// codes [batch][rows][K/2] as bytes, box of 128 bytes x box_rows
-bool make_codes_map(CUtensorMap* m, const void* base, long long K, long long rows, long long batch, uint32_t box_rows) {
-  EncodeTiledFn fn = encode_fn();
-  if (!fn) return false;
-  cuuint64_t dims[3] = {(cuuint64_t)K / 2, (cuuint64_t)rows, (cuuint64_t)batch};
-  cuuint64_t strides[2] = {(cuuint64_t)K / 2, (cuuint64_t)(K / 2 * rows)};
-  cuuint32_t box[3] = {SK / 2, box_rows, 1};
-  cuuint32_t estr[3] = {1, 1, 1};
-  return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 // scale tiles [row tiles][kt][512 bytes] of all matrices, box of two tiles along K x box_tiles row tiles
 bool make_scales_map(CUtensorMap* m, const void* base, long long kt, long long row_tiles, uint32_t box_tiles) {
   EncodeTiledFn fn = encode_fn();
@@ -709,17 +502,6 @@ bool make_scales_map(CUtensorMap* m, const void* base, long long kt, long long r
   cuuint32_t estr[3] = {1, 1, 1};
   return fn(m, CU_TENSOR_MAP_DATA_TYPE_INT32, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
             CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-// once per device and kernel: the attribute outlives the call
-bool allow_smem(const void* kernel, int bytes, std::atomic<uint64_t>& done) {
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return false;
-  const uint64_t bit = dev < 64 ? 1ull << dev : 0ull;
-  if (bit != 0 && (done.load(std::memory_order_relaxed) & bit)) return true;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
-  done.fetch_or(bit, std::memory_order_relaxed);
-  return true;
 }
 
 template <int MODE, bool SPLIT>

@@ -254,7 +254,8 @@ def moe(x, idx, gates, w1, w3, w2, dst=None):
 # (T, d, F, E, k, empty)
 LAYERS = [(1, 128, 160, 4, 2, 0.0), (5, 64, 32, 3, 1, 0.0), (33, 96, 224, 4, 2, 0.3), (150, 256, 288, 2, 2, 0.0),
           (40, 160, 96, 40, 6, 0.0), (7, 32, 64, 512, 8, 0.0), (300, 64, 96, 1, 1, 0.1), (1100, 32, 64, 7, 3, 0.05),
-          (3000, 1056, 160, 2, 2, 0.05), (2500, 544, 1184, 5, 3, 0.0)]
+          (3000, 1056, 160, 2, 2, 0.05), (2500, 544, 1184, 5, 3, 0.0),
+          (520, 96, 1056, 3, 3, 0.1), (200, 1184, 96, 6, 5, 0.0), (290, 2080, 64, 9, 3, 0.2), (2, 320, 4128, 8, 1, 0.0)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
@@ -349,6 +350,27 @@ def test_route_then_layer_on_a_stream_and_in_a_graph():
         y.fill_(7)
         graph.replay()
         assert torch.equal(y, ref.roll(shift, 0))
+
+
+def test_layers_on_two_streams_at_once():
+    # small batches run as cooperative kernels that want the whole device: neither may keep the other from finishing
+    T, d, F, E, k = 24, 512, 1024, 6, 2
+    w1, w3, w2 = (randn(E, *s, seed=i, std=0.1) for i, s in enumerate([(F, d), (F, d), (d, F)]))
+    runs = []
+    for i in range(2):
+        x = randn(T, d, seed=20 + i, dtype=torch.bfloat16)
+        idx, gates = random_routing(T, E, k, 30 + i)
+        ref, (desc, w13, w2q) = moe(x, idx, gates, w1, w3, w2)
+        ws = torch.empty(B.btx_mx4_moe_workspace_size(desc), dtype=torch.uint8, device=DEV)
+        runs.append((x, idx, gates, ref, desc, w13, w2q, torch.empty_like(x), ws, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for x, idx, gates, ref, desc, w13, w2q, y, ws, stream in runs:
+            with torch.cuda.stream(stream):
+                B.btx_mx4_moe_forward(desc, x, idx, gates, w13, w2q, y, ws)
+    torch.cuda.synchronize()
+    for x, idx, gates, ref, desc, w13, w2q, y, ws, stream in runs:
+        assert torch.equal(y, ref) and B.btx_device_status(ws) == B.BTX_OK
 
 
 def test_binding_refuses_wrong_tensors():
