@@ -184,11 +184,10 @@ class Routing:
     @staticmethod
     def given(desc: MoeDesc, topk_idx, gates):
         """The caller's choice [T,k] int32 and gates [T,k] fp32 for ROUTE_GIVEN, with room for the permutation."""
-        dev, R = topk_idx.device, desc.T * desc.k
-        _check(topk_idx, "topk_idx", (desc.T, desc.k), torch.int32, dev)
-        _check(gates, "gates", (desc.T, desc.k), torch.float32, dev)
-        _addr(topk_idx), _addr(gates)
-        i = dict(dtype=torch.int32, device=dev)
+        dev, R = _device(topk_idx), desc.T * desc.k
+        _arg(topk_idx, "topk_idx", (desc.T, desc.k), torch.int32, dev)
+        _arg(gates, "gates", (desc.T, desc.k), torch.float32, dev)
+        i = dict(dtype=torch.int32, device=topk_idx.device)
         return Routing(None, topk_idx, gates, None, torch.empty(desc.E, **i), torch.empty(desc.E + 1, **i),
                        torch.empty(R, **i), torch.empty(R, **i), None, None, None)
 
@@ -353,45 +352,58 @@ def btx_merge_ffn(w1s, w3s, w2s, layout, chunks, w1_dst, w3_dst, w2_dst, workspa
     return workspace
 
 
-def _check(t, name, shape, dtype, device, optional=False):
-    """Shape, type and device of a tensor argument; the library sees only its address."""
+def _bad(t, name, shape, dtype, dev):
     if t is None:
-        if optional:
-            return
         raise ValueError(f"btx: {name} is missing")
-    if t.shape != shape or t.dtype is not dtype or t.device != device:
-        raise ValueError(f"btx: {name} must be {tuple(shape)} {dtype} on {device}, not {tuple(t.shape)} {t.dtype} on {t.device}")
+    if tuple(t.shape) == tuple(shape) and t.dtype is dtype and t.get_device() == dev:
+        raise RuntimeError(f"btx: {name} must be contiguous")
+    raise ValueError(f"btx: {name} must be {tuple(shape)} {dtype} on device {dev}, not {tuple(t.shape)} {t.dtype} on {t.device}")
 
 
-def _addr(t):
-    """Address of a contiguous tensor whose device has been checked (None: absent)."""
-    if t is None:
-        return None
-    if not t.is_contiguous():
-        raise RuntimeError("btx: tensors must be contiguous")
+def _arg(t, name, shape, dtype, dev):
+    """Address of a contiguous tensor argument of the given shape and type on device number `dev`: the library sees
+    only the address."""
+    if t is None or t.shape != shape or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
+        _bad(t, name, shape, dtype, dev)
     return t.data_ptr()
 
 
-def _rows(t, name):
-    """Address and row stride of a matrix whose rows are contiguous (any row stride)."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+def _opt(t, name, shape, dtype, dev):
+    return None if t is None else _arg(t, name, shape, dtype, dev)
+
+
+def _rows(t, name, shape, dtype, dev):
+    """Address and row stride of a matrix argument whose rows are contiguous (any row stride)."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev:
+        _bad(t, name, shape, dtype, dev)
+    rs, cs = t.stride()
+    if (cs != 1 and shape[1] > 1) or (rs < shape[1] and shape[0] > 1):
         raise RuntimeError(f"btx: the rows of {name} must be contiguous and must not overlap")
-    return t.data_ptr(), max(t.stride(0), t.shape[1])
+    return t.data_ptr(), max(rs, shape[1])
 
 
-def _launch(name, device, *args):
+def _device(t):
+    """Number of the CUDA device that a tensor lives on."""
+    dev = t.get_device()
+    if dev < 0:
+        raise RuntimeError("btx: tensors must live on a CUDA device (there is no CPU path)")
+    return dev
+
+
+def _launch(name, dev, *args):
     """Calls a library function that takes the current stream last, with the tensors' device current.  The usual case,
     in which it is, costs no context switch: these calls run for a few microseconds on the device."""
-    if device.type != "cuda":
-        raise RuntimeError("btx: tensors must live on a CUDA device (there is no CPU path)")
     fn = getattr(_lib or lib(), name)
-    if torch._C._cuda_getDevice() == device.index:
-        s = fn(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    if torch._C._cuda_getDevice() == dev:
+        s = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
     else:
-        with torch.cuda.device(device):
-            s = fn(*args, torch._C._cuda_getCurrentRawStream(device.index))
+        with torch.cuda.device(dev):
+            s = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
     if s != BTX_OK:
         raise BtxError(s, name)
+
+
+_DTYPE = {BTX_F32: torch.float32, BTX_BF16: torch.bfloat16}
 
 
 def make_route_desc(T, E, k, dtype, score=SCORE_SOFTMAX, n_group=1, topk_group=1, group_score=GROUP_MAX, renorm=True,
@@ -402,32 +414,23 @@ def make_route_desc(T, E, k, dtype, score=SCORE_SOFTMAX, n_group=1, topk_group=1
 
 def btx_route(desc, logits, bias, topk_idx, gates, scores=None, counts=None, row_valid=None):
     """Expert choice and weights from router logits [T,E] (rows may be strided); see btx.h."""
-    T, E, k, dev = desc.T, desc.E, desc.k, logits.device
-    _check(logits, "logits", (T, E), torch.bfloat16 if desc.dtype == BTX_BF16 else torch.float32, dev)
-    _check(bias, "bias", (E,), torch.float32, dev, True)
-    _check(topk_idx, "topk_idx", (T, k), torch.int32, dev)
-    _check(gates, "gates", (T, k), torch.float32, dev)
-    _check(scores, "scores", (T, E), torch.float32, dev, True)
-    _check(counts, "counts", (E,), torch.int32, dev, True)
-    if row_valid is not None and row_valid.dtype == torch.bool:
+    T, E, k, dev = desc.T, desc.E, desc.k, _device(logits)
+    rows, stride = _rows(logits, "logits", (T, E), _DTYPE.get(desc.dtype), dev)
+    if row_valid is not None and row_valid.dtype is torch.bool:
         row_valid = row_valid.view(torch.uint8)
-    _check(row_valid, "row_valid", (T,), torch.uint8, dev, True)
-    rows, stride = _rows(logits, "logits")
-    _launch("btx_route", dev, C.byref(desc), rows, stride, _addr(bias), _addr(row_valid), _addr(topk_idx), _addr(gates),
-            _addr(scores), _addr(counts))
+    _launch("btx_route", dev, C.byref(desc), rows, stride, _opt(bias, "bias", (E,), torch.float32, dev),
+            _opt(row_valid, "row_valid", (T,), torch.uint8, dev), _arg(topk_idx, "topk_idx", (T, k), torch.int32, dev),
+            _arg(gates, "gates", (T, k), torch.float32, dev), _opt(scores, "scores", (T, E), torch.float32, dev),
+            _opt(counts, "counts", (E,), torch.int32, dev))
 
 
 def btx_route_backward(desc, logits, topk_idx, dgates, dlogits):
     """d logits from d gates (fp32 [T,k]) and the choice btx_route made; see btx.h."""
-    T, E, k, dev = desc.T, desc.E, desc.k, logits.device
-    dt = torch.bfloat16 if desc.dtype == BTX_BF16 else torch.float32
-    _check(logits, "logits", (T, E), dt, dev)
-    _check(topk_idx, "topk_idx", (T, k), torch.int32, dev)
-    _check(dgates, "dgates", (T, k), torch.float32, dev)
-    _check(dlogits, "dlogits", (T, E), dt, dev)
-    rows, stride = _rows(logits, "logits")
-    out, out_stride = _rows(dlogits, "dlogits")
-    _launch("btx_route_backward", dev, C.byref(desc), rows, stride, _addr(topk_idx), _addr(dgates), out, out_stride)
+    T, E, k, dev = desc.T, desc.E, desc.k, _device(logits)
+    rows, stride = _rows(logits, "logits", (T, E), _DTYPE.get(desc.dtype), dev)
+    out, out_stride = _rows(dlogits, "dlogits", (T, E), _DTYPE.get(desc.dtype), dev)
+    _launch("btx_route_backward", dev, C.byref(desc), rows, stride, _arg(topk_idx, "topk_idx", (T, k), torch.int32, dev),
+            _arg(dgates, "dgates", (T, k), torch.float32, dev), out, out_stride)
 
 
 @dataclass
@@ -448,17 +451,17 @@ class Mx4:
         return b, r, 2 * c
 
 
-def _mx4_ptrs(q, name, shape, device):
-    batch, rows, K = shape
-    _check(q.codes, name + ".codes", (batch, rows, K // 2), torch.uint8, device)
-    _check(q.scales, name + ".scales", (batch, (rows + 127) // 128, (K + 127) // 128, 512), torch.uint8, device)
-    return _addr(q.codes), _addr(q.scales)
+def _mx4(q, name, dev):
+    """Shape and addresses of an Mx4 argument."""
+    codes, scales = q.codes, q.scales
+    batch, rows, half = codes.shape
+    return ((batch, rows, 2 * half), _arg(codes, name + ".codes", (batch, rows, half), torch.uint8, dev),
+            _arg(scales, name + ".scales", (batch, (rows + 127) // 128, (half + 63) // 64, 512), torch.uint8, dev))
 
 
-def _workspace(ws, device):
-    if ws.device != device or ws.dtype is not torch.uint8:
-        raise ValueError(f"btx: workspace must be a uint8 tensor on {device}")
-    return _addr(ws), ws.numel()
+def _workspace(ws, dev):
+    n = ws.numel()
+    return _arg(ws, "workspace", (n,), torch.uint8, dev), n
 
 
 def btx_mx4_sizes(batch, rows, K):
@@ -473,25 +476,26 @@ def btx_mx4_sizes(batch, rows, K):
 def btx_mx4_quantize(src, out, row_first=0, row_step=1):
     """src [batch, rows, K] or [rows, K] (contiguous rows, any row and batch stride) cast into the Mx4 `out`; row r
     becomes row row_first + r * row_step."""
-    v = src if src.dim() == 3 else src.unsqueeze(0)
-    batch, rows, K = v.shape
-    if K > 1 and v.stride(2) != 1:
-        raise RuntimeError("btx: the rows of src must be contiguous")
-    ob, orows, oK = out.shape
+    dev = _device(src)
+    if src.dim() == 2:
+        (rows, K), (row_stride, col), batch, batch_stride = src.shape, src.stride(), 1, 0
+    else:
+        (batch, rows, K), (batch_stride, row_stride, col) = src.shape, src.stride()
+    (ob, out_rows, oK), codes, scales = _mx4(out, "out", dev)
     if ob != batch or oK != K:
-        raise ValueError(f"btx: src is {tuple(v.shape)}, out is {out.shape}")
-    codes, scales = _mx4_ptrs(out, "out", out.shape, src.device)
-    _launch("btx_mx4_quantize", src.device, _dtype_code(src.dtype), src.data_ptr(), v.stride(1), v.stride(0), batch, rows, K,
-            orows, row_first, row_step, codes, scales)
+        raise ValueError(f"btx: src is {tuple(src.shape)}, out is {out.shape}")
+    if col != 1 and K > 1:
+        raise RuntimeError("btx: the rows of src must be contiguous")
+    _launch("btx_mx4_quantize", dev, _dtype_code(src.dtype), src.data_ptr(), row_stride, batch_stride, batch, rows, K, out_rows,
+            row_first, row_step, codes, scales)
 
 
 def btx_mx4_dequantize(q, dst):
     """The values of the Mx4 `q` into dst (contiguous, [batch, rows, K] or [rows, K] for one matrix)."""
-    batch, rows, K = q.shape
-    if dst.numel() != batch * rows * K or dst.shape[-1] != K:
-        raise ValueError(f"btx: dst is {tuple(dst.shape)}, q is {q.shape}")
-    codes, scales = _mx4_ptrs(q, "q", q.shape, dst.device)
-    _launch("btx_mx4_dequantize", dst.device, _dtype_code(dst.dtype), codes, scales, batch, rows, K, _addr(dst))
+    dev = _device(dst)
+    (batch, rows, K), codes, scales = _mx4(q, "q", dev)
+    shape = (rows, K) if batch == 1 and dst.dim() == 2 else (batch, rows, K)
+    _launch("btx_mx4_dequantize", dev, _dtype_code(dst.dtype), codes, scales, batch, rows, K, _arg(dst, "dst", shape, dst.dtype, dev))
 
 
 def btx_mx4_matmul_workspace_size(M, N, K, dtype, batch=1):
@@ -504,16 +508,15 @@ def btx_mx4_matmul_workspace_size(M, N, K, dtype, batch=1):
 
 def btx_mx4_matmul(a, b, y, workspace):
     """y = a b^T of two Mx4 of the same batch and K; y is [batch, M, N], or [M, N] for one matrix."""
-    batch, M, K = a.shape
-    bb, N, bK = b.shape
+    dev = _device(y)
+    (batch, M, K), ac, asc = _mx4(a, "a", dev)
+    (bb, N, bK), bc, bsc = _mx4(b, "b", dev)
     if bb != batch or bK != K:
         raise ValueError(f"btx: a is {a.shape}, b is {b.shape}")
-    dev = y.device
-    _check(y, "y", (batch, M, N) if y.dim() == 3 or batch != 1 else (M, N), y.dtype, dev)
-    ac, asc = _mx4_ptrs(a, "a", a.shape, dev)
-    bc, bsc = _mx4_ptrs(b, "b", b.shape, dev)
+    shape = (M, N) if batch == 1 and y.dim() == 2 else (batch, M, N)
     ws, ws_bytes = _workspace(workspace, dev)
-    _launch("btx_mx4_matmul", dev, _dtype_code(y.dtype), batch, M, N, K, ac, asc, bc, bsc, _addr(y), ws, ws_bytes)
+    _launch("btx_mx4_matmul", dev, _dtype_code(y.dtype), batch, M, N, K, ac, asc, bc, bsc, _arg(y, "y", shape, y.dtype, dev), ws,
+            ws_bytes)
 
 
 def make_mx4_moe_desc(T, d_model, d_ff, E, k, dtype) -> Mx4MoeDesc:
@@ -530,17 +533,16 @@ def btx_mx4_moe_workspace_size(desc):
 
 def btx_mx4_moe_forward(desc, x, topk_idx, gates, w13, w2, y, workspace):
     """The expert layer on MXFP4 experts under a given routing; w13 holds the rows of W1 and W3 in turn; see btx.h."""
-    T, d, F, E, k, dev = desc.T, desc.d_model, desc.d_ff, desc.E, desc.k, x.device
-    dt = torch.bfloat16 if desc.dtype == BTX_BF16 else torch.float32
-    _check(x, "x", (T, d), dt, dev)
-    _check(topk_idx, "topk_idx", (T, k), torch.int32, dev)
-    _check(gates, "gates", (T, k), torch.float32, dev)
-    _check(y, "y", (T, d), dt, dev)
-    c13, s13 = _mx4_ptrs(w13, "w13", (E, 2 * F, d), dev)
-    c2, s2 = _mx4_ptrs(w2, "w2", (E, d, F), dev)
+    T, d, F, E, k, dev = desc.T, desc.d_model, desc.d_ff, desc.E, desc.k, _device(x)
+    dt = _DTYPE.get(desc.dtype)
+    s13, c13, sc13 = _mx4(w13, "w13", dev)
+    s2, c2, sc2 = _mx4(w2, "w2", dev)
+    if s13 != (E, 2 * F, d) or s2 != (E, d, F):
+        raise ValueError(f"btx: w13 is {s13}, w2 is {s2}; the layer has E, d_ff, d_model = {E}, {F}, {d}")
     ws, ws_bytes = _workspace(workspace, dev)
-    _launch("btx_mx4_moe_forward", dev, C.byref(desc), _addr(x), _addr(topk_idx), _addr(gates), c13, s13, c2, s2, _addr(y), ws,
-            ws_bytes)
+    _launch("btx_mx4_moe_forward", dev, C.byref(desc), _arg(x, "x", (T, d), dt, dev),
+            _arg(topk_idx, "topk_idx", (T, k), torch.int32, dev), _arg(gates, "gates", (T, k), torch.float32, dev), c13, sc13, c2, sc2,
+            _arg(y, "y", (T, d), dt, dev), ws, ws_bytes)
 
 
 def btx_selftest_wait_expiry(workspace):
