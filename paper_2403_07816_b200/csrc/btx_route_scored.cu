@@ -8,10 +8,9 @@
 //   the k largest c of the groups that stay; ties go to the lower index
 //   w_j = scale * s_j, or scale * s_j / sum_i s_i over the chosen
 //
-// A warp owns a row and keeps its keys in registers, lane l the experts l*EPL .. l*EPL+EPL-1, so that the lowest
-// lane of a tie holds the lowest index and a round of the selection is one integer warp maximum, one vote and one
-// shuffle.  The memory traffic is the logits once; at T = 16384, E = 256 the kernel is bound by instruction issue
-// of the k rounds and by latency, not by memory (the logits stay in L2).
+// 8 to 32 lanes share a row and keep its keys in registers; a round of the selection is one integer maximum over the
+// row.  The memory traffic is the logits once; at T = 16384, E = 256 the kernel is bound by instruction issue of the k
+// rounds and by latency, not by memory.
 #include <math_constants.h>
 
 #include <type_traits>
@@ -24,10 +23,7 @@ namespace {
 using routedev::Vec;
 
 constexpr unsigned kAll = 0xffffffffu;
-// Rows in flight per block.  Every block adds its counts to E addresses, so fewer, larger blocks: T = 16384, E = 64 with
-// 1184 blocks of 8 warps spent 10 of 14 us on the additions.
-template <int EPL> struct RouteWarps { static constexpr int n = EPL <= 8 ? 16 : 8; };
-constexpr int kRsWarps = 8;                 // backward
+constexpr int kRsWarps = 8;
 constexpr int kMaxScoredExperts = 512;
 constexpr int kMaxScoredK = 32;             // lane j keeps slot j
 constexpr int kMaxScoredGroups = 32;
@@ -51,10 +47,47 @@ __device__ __forceinline__ uint32_t order_key(float v) {
   return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float order_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
-__device__ __forceinline__ float warp_sum(float v) {
+// Reductions over the L lanes that share a row (every lane gets the result).
+template <int L> __device__ __forceinline__ float row_sum(float v) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
+  for (int o = 1; o < L; o *= 2) v += __shfl_xor_sync(kAll, v, o);
   return v;
+}
+// Sum over a row of EPL values per lane as one binary tree over the experts: the result does not depend on how many
+// lanes share the row.
+template <int L, int EPL> __device__ __forceinline__ float row_sum(float (&v)[EPL]) {
+#pragma unroll
+  for (int w = 1; w < EPL; w *= 2)
+#pragma unroll
+    for (int i = 0; i + w < EPL; i += 2 * w) v[i] += v[i + w];
+  return row_sum<L>(v[0]);
+}
+template <int L> __device__ __forceinline__ uint32_t row_max(uint32_t v) {
+  if constexpr (L == 32) {
+    return __reduce_max_sync(kAll, v);
+  } else {
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(kAll, v, o));
+    return v;
+  }
+}
+template <int L> __device__ __forceinline__ float row_max(float v) {
+  if constexpr (L == 32) {
+    return order_value(__reduce_max_sync(kAll, order_key(v)));
+  } else {
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kAll, v, o));
+    return v;
+  }
+}
+template <int L> __device__ __forceinline__ double row_max(double v) {
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) v = fmax(v, __shfl_xor_sync(kAll, v, o));
+  return v;
+}
+template <int L> __device__ __forceinline__ bool row_any(bool v, int lane) {
+  const uint32_t m = __ballot_sync(kAll, v);
+  return L == 32 ? m != 0u : ((m >> (lane & ~(L - 1))) & ((1u << (L & 31)) - 1u)) != 0u;
 }
 __device__ __forceinline__ float sigmoid_rn(float z) { return 1.0f / (1.0f + expf(-z)); }
 // exp(z - m) for z <= m, with exp(0) = 1 where both are +inf
@@ -91,42 +124,34 @@ template <typename F> __device__ __forceinline__ void push2(F v, F& a, F& b) {
 template <typename F> __device__ __forceinline__ F group_value(F a, F b, int sum2) {
   return sum2 && b > (F)-CUDART_INF ? a + b : a;
 }
-__device__ __forceinline__ float warp_max_of(float v) { return order_value(__reduce_max_sync(kAll, order_key(v))); }
-__device__ __forceinline__ float warp_min_of(float v) { return order_value(__reduce_min_sync(kAll, order_key(v))); }
-__device__ __forceinline__ double warp_max_of(double v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = fmax(v, __shfl_xor_sync(kAll, v, o));
-  return v;
-}
-__device__ __forceinline__ double warp_min_of(double v) { return -warp_max_of(-v); }
-
-// Whether this lane's group g stays: v is its key, the same in the P lanes g * P .. g * P + P - 1, which share the
-// comparisons with the G groups; `size` bounds the magnitudes behind v.  `margin` receives the difference between the
-// worst group that stays and the best that does not, `reach` the largest size (for the caller's error bound).
-template <typename F>
+// Whether this lane's group g stays: v is its key, the same in the P lanes g * P .. g * P + P - 1 of the row's L, which
+// share the comparisons with the G groups; `size` bounds the magnitudes behind v.  `margin` receives the difference
+// between the worst group that stays and the best that does not, `reach` the largest size (for the caller's error
+// bound).
+template <int L, typename F>
 __device__ __forceinline__ bool rank_groups(F v, F size, int g, int G, int P, int lane, int topk_group, F& margin, F& reach) {
   const F low = (F)-CUDART_INF;
   int rank = 0;
   for (int q0 = 0; q0 < G; q0 += P) {
     const int q = q0 + (lane & (P - 1));
-    const F o = __shfl_sync(kAll, v, (q * P) & 31);
+    const F o = __shfl_sync(kAll, v, (q * P) & (L - 1), L);
     rank += q < G && (o > v || (o == v && q < g));
   }
   for (int o = 1; o < P; o <<= 1) rank += __shfl_xor_sync(kAll, rank, o);
   const bool stays = g < G && rank < topk_group;
-  const F worst = warp_min_of(stays ? v : (F)CUDART_INF), best = warp_max_of(g < G && !stays ? v : low);
-  reach = warp_max_of(g < G && v > low ? size : (F)0);
+  const F worst = -row_max<L>(stays ? -v : low), best = row_max<L>(g < G && !stays ? v : low);
+  reach = row_max<L>(g < G && v > low ? size : (F)0);
   margin = best > low ? worst - best : (F)CUDART_INF;
   return stays;
 }
 
-// The groups that stay, as a bit mask, from keys in the warp's shared memory (expert e at e + (e / size) * P, so that the lanes of different
-// groups read different banks); P lanes share a group.
-template <typename F>
-__device__ __forceinline__ uint32_t choose_groups(const F* key, int G, int size, int P, int topk_group, int sum2,
-                                                  int lane, F& margin, F& reach) {
+// The groups that stay, as a bit mask, from the row's keys in shared memory (expert e at e + (e / size) * P, so that the
+// lanes of different groups read different banks); P lanes share a group.
+template <int L, typename F>
+__device__ __forceinline__ uint32_t choose_groups(const F* key, int G, int size, int P, int topk_group, int sum2, int lane,
+                                                  F& margin, F& reach) {
   const F low = (F)-CUDART_INF;
-  const int g = lane / P, p = lane - g * P;
+  const int sl = lane & (L - 1), g = sl / P, p = sl - g * P;
   F a = low, b = low;
   if (g < G)
     for (int j = p; j < size; j += P) push2(key[g * (size + P) + j], a, b);
@@ -137,8 +162,8 @@ __device__ __forceinline__ uint32_t choose_groups(const F* key, int G, int size,
   }
   const F v = g < G ? group_value(a, b, sum2) : low;
   const F reach_g = fabs(a) + (sum2 && b > low ? fabs(b) : (F)0);
-  const bool stays = rank_groups(v, reach_g, g, G, P, lane, topk_group, margin, reach);
-  const uint32_t lanes = __ballot_sync(kAll, stays && p == 0);
+  const bool stays = rank_groups<L, F>(v, reach_g, g, G, P, lane, topk_group, margin, reach);
+  const uint32_t lanes = __ballot_sync(kAll, stays && p == 0) >> (lane & ~(L - 1));
   uint32_t mask = 0;
   for (int q = 0; q < G; ++q) mask |= ((lanes >> (q * P)) & 1u) << q;
   return mask;
@@ -148,7 +173,9 @@ __device__ __forceinline__ uint32_t choose_groups(const F* key, int G, int size,
 // doubles of the warp's shared memory.  Returns the expert of slot `lane` (-1: none).
 template <typename T, bool SIGMOID>
 __device__ __noinline__ int choose_in_double(const T* __restrict__ row, const RouteParams& p, int sum2, double* keys, int lane) {
-  const int P = p.n_group > 1 ? p.lanes_per_group : 0;
+  int P = 0;                                // lanes of the whole warp that share a group
+  if (p.n_group > 1)
+    for (P = 1; 2 * P * p.n_group <= 32;) P *= 2;
   const double low = -CUDART_INF;
   double zmax = low, total = 0.0;
   if (!SIGMOID) {
@@ -182,7 +209,7 @@ __device__ __noinline__ int choose_in_double(const T* __restrict__ row, const Ro
   place(true);
   if (p.n_group > 1) {
     double margin, reach;
-    stay = choose_groups<double>(keys, p.n_group, p.group_size, P, p.topk_group, sum2, lane, margin, reach);
+    stay = choose_groups<32, double>(keys, p.n_group, p.group_size, P, p.topk_group, sum2, lane, margin, reach);
     __syncwarp();
     if (!p.bias && sum2) place(false);
   }
@@ -228,223 +255,269 @@ __device__ __forceinline__ float rcp_fast(float x) {
 constexpr float kLog2e = 1.4426950408889634f;
 __device__ __forceinline__ float sigmoid_key(float z) { return rcp_fast(1.0f + exp2_fast(-kLog2e * z)); }
 
-template <typename T, int EPL, bool SIGMOID>
-__global__ void __launch_bounds__(RouteWarps<EPL>::n * 32, EPL <= 8 ? 2 : 3)
+// L lanes share a row, EPL experts each: 32 / L rows per warp share the instructions of a round.
+// Warps per block: every block adds its counts to E addresses, so few large blocks.  14 for 256 experts: with 12 the
+// registers allow more per thread, but T = 16384 takes a third pass over the grid (24.8 instead of 21.4 us); 16 spill.
+template <int E> struct RouteWarps { static constexpr int n = E <= 128 ? 16 : E <= 256 ? 14 : 8, per_sm = E <= 256 ? 2 : 3; };
+
+template <typename T, int L, int EPL, bool SIGMOID>
+__global__ void __launch_bounds__(RouteWarps<L * EPL>::n * 32, RouteWarps<L * EPL>::per_sm)
 route_scored_kernel(const T* __restrict__ logits, const RouteParams p, int sum2, int vec) {
-  constexpr int W = RouteWarps<EPL>::n;
-  // per warp: 32-bit keys for the groups, or 64-bit keys of a row that is decided again (never both at once)
-  __shared__ double keys_s[W][EPL * 32 + 32];
-  __shared__ int hist[EPL * 32];
-  // A packed key is the ordered key with its lowest bits replaced by the index, larger for lower experts: one warp
-  // maximum finds the next expert, its place and the lower index of a tie.
-  constexpr uint32_t IDX = EPL * 32 - 1;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr int ROWS = 32 / L, W = RouteWarps<L * EPL>::n;
+  constexpr int KEYS = EPL * L + 32;
+  // per warp: 32-bit keys of its rows for the groups, or 64-bit keys of a row that is decided again (never both at once)
+  __shared__ double keys_s[W][ROWS * KEYS / 2 > KEYS ? ROWS * KEYS / 2 : KEYS];
+  __shared__ float bias_s[EPL * L];
+  __shared__ int hist[EPL * L];
+  // A packed key is the ordered key with its lowest bits replaced by the index, larger for lower experts: one maximum
+  // over the row finds the next expert, its place and the lower index of a tie.
+  constexpr uint32_t IDX = EPL * L - 1;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sl = lane & (L - 1), seg0 = lane & ~(L - 1);
   const bool grouped = p.n_group > 1, biased = p.bias != nullptr;
-  const int e0 = lane * EPL;
+  const int e0 = sl * EPL;
   const float low = -CUDART_INF_F;
-  if (p.counts != nullptr) {
-    for (int i = threadIdx.x; i < p.E; i += blockDim.x) hist[i] = 0;
-    __syncthreads();
-  }
+  for (int i = threadIdx.x; i < EPL * L; i += W * 32) hist[i] = 0;
   allow_dependents();
   grid_dependency_wait();
+  if (biased)
+    for (int i = threadIdx.x; i < EPL * L; i += W * 32) bias_s[i] = i < p.E ? p.bias[i] : 0.f;
+  __syncthreads();
   const float err_s = SIGMOID ? 0x1p-22f : 0x1p-18f, err_0 = 0x1p-23f, err_c = 0x1p-24f;
   const bool need_total = !SIGMOID && (p.scores != nullptr || biased || (grouped && sum2) || !p.renorm);
   const bool exact_keys = !biased && sizeof(T) == 2;               // 16-bit logits keep every bit in a packed key
   // groups of whole lanes (a power of two of them) are compared in registers, others through shared memory
   const int lanes_per = p.group_size / EPL;
   const bool by_lanes = grouped && lanes_per * EPL == p.group_size && (lanes_per & (lanes_per - 1)) == 0;
-  float bias[EPL];                          // the same for every row
-#pragma unroll
-  for (int i = 0; i < EPL; ++i) bias[i] = biased && e0 + i < p.E ? p.bias[e0 + i] : 0.f;
   int half_k = 1;                           // reductions over the chosen: lanes 0 .. 2 * half_k - 1 cover k
   while (2 * half_k < p.k) half_k *= 2;
 
-  for (int t = blockIdx.x * W + warp; t < p.T; t += gridDim.x * W) {
-    const T* row = logits + (long long)t * p.stride;
-    int sel = -1;                           // lane j: the expert of slot j
+  for (int t0 = (blockIdx.x * W + warp) * ROWS; t0 < p.T; t0 += gridDim.x * W * ROWS) {
+    const int t = t0 + lane / L;
+    const bool there = t < p.T, on = there && (p.row_valid == nullptr || p.row_valid[t] != 0);
+    const T* row = logits + (long long)(there ? t : t0) * p.stride;
+    float z[EPL];                                                  // a row that is off has no candidate
+    if (on) {
+      load_row<T, EPL>(row, p.E, sl, vec != 0, z);
+    } else {
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) z[i] = low;
+    }
+    __syncwarp();
     float total = 1.f, zmax = 0.f;
-    if (p.row_valid == nullptr || p.row_valid[t] != 0) {
-      float z[EPL];
-      load_row<T, EPL>(row, p.E, lane, vec != 0, z);
-      if (need_total) {
-        float m = low;
+    if (need_total) {
+      float m = low;
 #pragma unroll
-        for (int i = 0; i < EPL; ++i) m = fmaxf(m, z[i]);          // (fmaxf passes over NaN)
-        zmax = warp_max_of(m);
-        float sum = 0.f;
+      for (int i = 0; i < EPL; ++i) m = fmaxf(m, z[i]);            // (fmaxf passes over NaN)
+      zmax = row_max<L>(m);
+      float ex[EPL];
 #pragma unroll
-        for (int i = 0; i < EPL; ++i) sum += z[i] > low ? exp_below(z[i], zmax) : 0.f;
-        total = warp_sum(sum);
-        if (!(total > 0.f)) total = 1.f;                           // nothing is on
-      }
-      const float inv_total = 1.0f / total;
-      auto score_key = [&](float v) {                              // v > -inf
-        if (SIGMOID) return sigmoid_key(v);
-        return (v == zmax ? 1.0f : exp2_fast((v - zmax) * kLog2e)) * inv_total;
-      };
-      if (p.scores != nullptr) {
+      for (int i = 0; i < EPL; ++i) ex[i] = z[i] > low ? exp_below(z[i], zmax) : 0.f;
+      total = row_sum<L, EPL>(ex);
+      if (!(total > 0.f)) total = 1.f;                             // nothing is on
+    }
+    const float inv_total = 1.0f / total;
+    auto score_key = [&](float v) {                                // v > -inf
+      if (SIGMOID) return sigmoid_key(v);
+      return (v == zmax ? 1.0f : exp2_fast((v - zmax) * kLog2e)) * inv_total;
+    };
+    if (p.scores != nullptr && there) {
 #pragma unroll
-        for (int i = 0; i < EPL; ++i)
-          if (e0 + i < p.E)
-            p.scores[(size_t)t * p.E + e0 + i] = !(z[i] > low) ? 0.f : SIGMOID ? sigmoid_rn(z[i]) : exp_below(z[i], zmax) / total;
-      }
-      float c[EPL];                                                // -inf: not a candidate
+      for (int i = 0; i < EPL; ++i)
+        if (e0 + i < p.E)
+          p.scores[(size_t)t * p.E + e0 + i] = !(z[i] > low) ? 0.f : SIGMOID ? sigmoid_rn(z[i]) : exp_below(z[i], zmax) / total;
+    }
+    float c[EPL];                                                  // -inf: not a candidate
 #pragma unroll
-      for (int i = 0; i < EPL; ++i) {
-        c[i] = biased ? score_key(z[i]) + bias[i] : z[i];
-        if (!(z[i] > low && c[i] > low)) c[i] = low;
-      }
-      const float smax = SIGMOID ? 1.0f : inv_total;               // no score is larger
-      bool unsure = false;                                         // the choice of groups is within its error
-      if (grouped) {
-        float margin, reach;
-        if (by_lanes) {
-          float a = low, b = low;
+    for (int i = 0; i < EPL; ++i) {
+      c[i] = biased ? score_key(z[i]) + bias_s[e0 + i] : z[i];
+      if (!(z[i] > low && c[i] > low)) c[i] = low;
+    }
+    const float smax = SIGMOID ? 1.0f : inv_total;                 // no score is larger
+    bool unsure = false;                                           // not settled in registers
+    auto group_error = [&](float reach) { return 2.f * (sum2 ? 2.f : 1.f) * (err_s * smax + err_0) + 6.f * err_c * reach; };
+    if (grouped) {
+      float margin, reach;
+      if (by_lanes) {
+        float a = low, b = low;
 #pragma unroll
-          for (int i = 0; i < EPL; ++i) push2(c[i], a, b);
-          for (int o = 1; o < lanes_per; o <<= 1) {
-            const float oa = __shfl_xor_sync(kAll, a, o), ob = __shfl_xor_sync(kAll, b, o);
-            push2(oa, a, b);
-            push2(ob, a, b);
+        for (int i = 0; i < EPL; ++i) push2(c[i], a, b);
+        for (int o = 1; o < lanes_per; o <<= 1) {
+          const float oa = __shfl_xor_sync(kAll, a, o), ob = __shfl_xor_sync(kAll, b, o);
+          push2(oa, a, b);
+          push2(ob, a, b);
+        }
+        if (!biased && sum2) {                                     // the best logits have the best scores
+          a = a > low ? score_key(a) : low;
+          b = b > low ? score_key(b) : low;
+        }
+        bool stays = rank_groups<L, float>(group_value(a, b, sum2), fabsf(a) + (sum2 && b > low ? fabsf(b) : 0.f), sl / lanes_per,
+                                           p.n_group, lanes_per, lane, p.topk_group, margin, reach);
+        // keys compared as they stand (logits) are exact; others are formed again in 64 bits where their order is in doubt
+        // (a few rows of a batch, but one of them holds up its block: the whole choice in 64 bits took 12 us)
+        if ((biased || sum2) && __any_sync(kAll, margin <= group_error(reach))) {
+          double da = low, db = low, top = zmax, sum = 1.0;
+          if (!SIGMOID) {
+            sum = 0.0;
+#pragma unroll
+            for (int i = 0; i < EPL; ++i)
+              if (z[i] > low) sum += z[i] == zmax ? 1.0 : exp((double)z[i] - top);
+#pragma unroll
+            for (int o = L / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(kAll, sum, o);
           }
-          if (!biased && sum2) {                                   // the best logits have the best scores
-            a = a > low ? score_key(a) : low;
-            b = b > low ? score_key(b) : low;
-          }
-          const bool stays = rank_groups(group_value(a, b, sum2), fabsf(a) + (sum2 && b > low ? fabsf(b) : 0.f),
-                                         lane / lanes_per, p.n_group, lanes_per, lane, p.topk_group, margin, reach);
-          if (!stays) {
-#pragma unroll
-            for (int i = 0; i < EPL; ++i) c[i] = low;
-          }
-        } else {
-          float* key = reinterpret_cast<float*>(keys_s[warp]);
-          const int P = p.lanes_per_group;
-          __syncwarp();
 #pragma unroll
           for (int i = 0; i < EPL; ++i) {
-            const int e = e0 + i;
-            if (e < p.E) key[e + e / p.group_size * P] = !biased && sum2 && c[i] > low ? score_key(z[i]) : c[i];
+            if (c[i] > low) {
+              const double zd = z[i];
+              const double sc = SIGMOID ? 1.0 / (1.0 + exp(-zd)) : (z[i] == zmax ? 1.0 : exp(zd - top)) / sum;
+              push2(sc + (biased ? (double)bias_s[e0 + i] : 0.0), da, db);
+            }
           }
-          __syncwarp();
-          const uint32_t stay = choose_groups<float>(key, p.n_group, p.group_size, P, p.topk_group, sum2, lane, margin, reach);
+          for (int o = 1; o < lanes_per; o <<= 1) {
+            const double oa = __shfl_xor_sync(kAll, da, o), ob = __shfl_xor_sync(kAll, db, o);
+            push2(oa, da, db);
+            push2(ob, da, db);
+          }
+          double dm, dr;
+          stays = rank_groups<L, double>(group_value(da, db, sum2), 0.0, sl / lanes_per, p.n_group, lanes_per, lane, p.topk_group, dm, dr);
+        }
+        if (!stays) {
+#pragma unroll
+          for (int i = 0; i < EPL; ++i) c[i] = low;
+        }
+      } else {
+        float* key = reinterpret_cast<float*>(keys_s[warp]) + lane / L * KEYS;
+        const int P = p.lanes_per_group;
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) {
+          const int e = e0 + i;
+          if (e < p.E) key[e + e / p.group_size * P] = !biased && sum2 && c[i] > low ? score_key(z[i]) : c[i];
+        }
+        __syncwarp();
+        const uint32_t stay = choose_groups<L, float>(key, p.n_group, p.group_size, P, p.topk_group, sum2, lane, margin, reach);
+#pragma unroll
+        for (int i = 0; i < EPL; ++i)
+          if (e0 + i < p.E && !((stay >> ((e0 + i) / p.group_size)) & 1u)) c[i] = low;
+        if (biased || sum2) unsure = margin <= group_error(reach);
+      }
+    }
+    // k rounds: the largest packed key of the row goes to the next slot.  A lane holds its three best (0: none) and looks
+    // through its experts again when all are taken.
+    uint32_t u[EPL], best0 = 0, best1 = 0, best2 = 0;
+    auto push3 = [&](uint32_t v) {
+      const uint32_t d0 = min(best0, v);
+      best0 = max(best0, v);
+      const uint32_t d1 = min(best1, d0);
+      best1 = max(best1, d0);
+      best2 = max(best2, d1);
+    };
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+      u[i] = c[i] > low ? (order_key(c[i]) & ~IDX) | (IDX - (uint32_t)(e0 + i)) : 0u;
+      push3(u[i]);
+    }
+    uint32_t mine = 0;                                             // key of slot `sl`
+    int n = 0;                                                     // slots taken (of this lane's row)
+    uint32_t next = row_max<L>(best0);
+    auto pick = [&](bool take) {                                   // `take`: the same in all lanes of a row
+      if (take) {
+        if (sl == n) mine = next;
+        ++n;
+        if (best0 == next) {
+          best0 = best1; best1 = best2; best2 = 0;
+          if (best0 == 0u) {
+#pragma unroll
+            for (int i = 0; i < EPL; ++i) push3(u[i] < next ? u[i] : 0u);
+          }
+        }
+      }
+      __syncwarp();
+      next = row_max<L>(best0);
+    };
+    for (int j = 0; j < p.k; ++j) pick(next != 0u);
+    if (!exact_keys) {
+      // Neighbours that lie within what a packed key leaves out and the error of the keys: take what else lies as close,
+      // and order all of it in 64 bits.  The bound holds for every key from the first to the one compared.
+      const uint32_t first = __shfl_sync(kAll, mine, 0, L);
+      const float c0 = fabsf(order_value(first & ~IDX));
+      const float fixed = biased ? 2.f * (err_s * smax + err_0) : 0.f, rel = biased ? 2.f * err_c : 0.f;
+      auto close = [&](uint32_t hi, uint32_t lo) {
+        const float l = order_value(lo | IDX);
+        return !(order_value(hi & ~IDX) - l > fixed + rel * 1.01f * fmaxf(c0, fabsf(l)));
+      };
+      const uint32_t after = __shfl_down_sync(kAll, mine, 1, L);
+      uint32_t last = __shfl_sync(kAll, mine, n > 0 ? n - 1 : 0, L);
+      const bool tail = n > 0 && next != 0u && close(last, next);
+      const bool near = row_any<L>(sl + 1 < n && close(mine, after), lane);     // (a vote of the whole warp: never behind a condition of a row)
+      const bool redo = !unsure && (near || tail);
+      if (__any_sync(kAll, redo)) {
+        for (;;) {
+          const bool more = redo && n < L && next != 0u && close(last, next);
+          if (!__any_sync(kAll, more)) break;
+          if (more) last = next;
+          pick(more);
+        }
+        if (redo && next != 0u && close(last, next)) unsure = true;
+        const double top = (double)zmax;
+        double sum = 1.0;
+        if (!SIGMOID && biased) {
+          sum = 0.0;
 #pragma unroll
           for (int i = 0; i < EPL; ++i)
-            if (e0 + i < p.E && !((stay >> ((e0 + i) / p.group_size)) & 1u)) c[i] = low;
+            if (z[i] > low) sum += z[i] == zmax ? 1.0 : exp((double)z[i] - top);
+#pragma unroll
+          for (int o = L / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(kAll, sum, o);
         }
-        // keys compared as they stand (logits) are exact
-        if (biased || sum2) unsure = margin <= 2.f * (sum2 ? 2.f : 1.f) * (err_s * smax + err_0) + 6.f * err_c * reach;
-      }
-      // k rounds: the largest packed key of the warp goes to the next slot.  A lane holds its two best (0: none) and
-      // looks through its experts again when both are taken.
-      uint32_t u[EPL], a = 0, b = 0;
-#pragma unroll
-      for (int i = 0; i < EPL; ++i) {
-        u[i] = c[i] > low ? (order_key(c[i]) & ~IDX) | (IDX - (uint32_t)(e0 + i)) : 0u;
-        push2(u[i], a, b);
-      }
-      uint32_t mine = 0;                                           // key of slot `lane`
-      int n = 0;
-      uint32_t next = __reduce_max_sync(kAll, a);
-      auto pick = [&]() {
-        if (lane == n) mine = next;
-        if (a == next) {
-          a = b;
-          b = 0;
-          if (a == 0u) {
-#pragma unroll
-            for (int i = 0; i < EPL; ++i) push2(u[i] < next ? u[i] : 0u, a, b);
-          }
+        const int e = (int)(IDX - (mine & IDX));
+        double cd = 0.0;
+        if (redo && sl < n) {
+          const float zf = to_f32(row[e]);
+          cd = (double)zf;
+          if (biased) cd = (SIGMOID ? 1.0 / (1.0 + exp(-cd)) : (zf == zmax ? 1.0 : exp(cd - top)) / sum) + (double)p.bias[e];
         }
-        ++n;
-        next = __reduce_max_sync(kAll, a);
-      };
-      while (n < p.k && next != 0u) pick();
-      if (!exact_keys && n > 0 && !unsure) {
-        // Neighbours that lie within what a packed key leaves out and the error of the keys: take what else lies as
-        // close, and order all of it in 64 bits.  The bound holds for every key from the first to the one compared.
-        const float c0 = fabsf(order_value(__shfl_sync(kAll, mine, 0) & ~IDX));
-        const float fixed = biased ? 2.f * (err_s * smax + err_0) : 0.f, rel = biased ? 2.f * err_c : 0.f;
-        auto close = [&](uint32_t hi, uint32_t lo) {
-          const float l = order_value(lo | IDX);
-          return !(order_value(hi & ~IDX) - l > fixed + rel * 1.01f * fmaxf(c0, fabsf(l)));
-        };
-        const uint32_t after = __shfl_down_sync(kAll, mine, 1);
-        const uint32_t last0 = __shfl_sync(kAll, mine, n - 1);
-        const bool tail = next != 0u && close(last0, next);
-        if (__any_sync(kAll, lane + 1 < n && close(mine, after)) || tail) {
-          uint32_t last = last0;
-          while (n < 32 && next != 0u && close(last, next)) {
-            last = next;
-            pick();
-          }
-          if (next != 0u && close(last, next)) unsure = true;
-          if (!unsure) {
-            const double top = (double)zmax;
-            double sum = 1.0;
-            if (!SIGMOID && biased) {
-              sum = 0.0;
-#pragma unroll
-              for (int i = 0; i < EPL; ++i)
-                if (z[i] > low) sum += z[i] == zmax ? 1.0 : exp((double)z[i] - top);
-#pragma unroll
-              for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kAll, sum, o);
-            }
-            const int e = (int)(IDX - (mine & IDX));
-            double cd = 0.0;
-            if (lane < n) {
-              const float zf = to_f32(row[e]);
-              cd = (double)zf;
-              if (biased)
-                cd = (SIGMOID ? 1.0 / (1.0 + exp(-cd)) : (zf == zmax ? 1.0 : exp(cd - top)) / sum) + (double)p.bias[e];
-            }
-            int rank = 0;
-            for (int j = 0; j < n; ++j) {
-              const double oc = __shfl_sync(kAll, cd, j);
-              const int oe = __shfl_sync(kAll, e, j);
-              rank += oc > cd || (oc == cd && oe < e);
-            }
-            uint32_t* order = reinterpret_cast<uint32_t*>(keys_s[warp]);
-            __syncwarp();
-            if (lane < n) order[rank] = mine;
-            __syncwarp();
-            if (lane < n) mine = order[lane];
-            __syncwarp();
-          }
+        int rank = 0;
+        const int longest = __reduce_max_sync(kAll, n);
+        for (int j = 0; j < longest; ++j) {
+          const double oc = __shfl_sync(kAll, cd, j, L);
+          const int oe = __shfl_sync(kAll, e, j, L);
+          rank += j < n && (oc > cd || (oc == cd && oe < e));
         }
-      }
-      if (unsure) {
+        uint32_t* order = reinterpret_cast<uint32_t*>(keys_s[warp]) + seg0;
         __syncwarp();
-        sel = choose_in_double<T, SIGMOID>(row, p, sum2, keys_s[warp], lane);
+        if (redo && sl < n) order[rank] = mine;
         __syncwarp();
-      } else if (lane < n && lane < p.k) {
-        sel = (int)(IDX - (mine & IDX));
+        if (redo && sl < n) mine = order[sl];
+        __syncwarp();
       }
-    } else if (p.scores != nullptr) {
-      for (int e = lane; e < p.E; e += 32) p.scores[(size_t)t * p.E + e] = 0.f;
     }
-    // Weights: lane j has slot j.  Renormalised weights are formed from exponentials shifted by the largest chosen
-    // logit where their sum could underflow, so they are a number even where every score is 0.
+    int sel = sl < n && sl < p.k ? (int)(IDX - (mine & IDX)) : -1;  // lane j of a row: the expert of slot j
+    for (uint32_t rows = __ballot_sync(kAll, unsure && sl == 0); rows != 0u; rows &= rows - 1u) {
+      const int src = __ffs(rows) - 1;                             // the whole warp decides the row again
+      __syncwarp();
+      const int got = choose_in_double<T, SIGMOID>(logits + (long long)(t0 + src / L) * p.stride, p, sum2, keys_s[warp], lane);
+      const int mine_now = __shfl_sync(kAll, got, sl);
+      if (seg0 == src) sel = sl < p.k ? mine_now : -1;
+      __syncwarp();
+    }
+    // Weights: lane j has slot j.  Renormalised weights are formed from exponentials shifted by the largest chosen logit
+    // where their sum could underflow, so they are a number even where every score is 0.
     const bool have = sel >= 0;
     const float zs = have ? to_f32(row[sel]) : low;
     float w = 0.f;
     if (p.renorm) {
-      if (SIGMOID && __any_sync(kAll, zs > -10.f)) {
-        if (have) w = sigmoid_rn(zs);
-      } else {
-        const float m = warp_max_of(zs);
-        if (have) w = SIGMOID ? expf(zs - m) / (1.0f + expf(zs)) : exp_below(zs, m);
-      }
+      const bool large = row_any<L>(zs > -10.f, lane);
+      const bool shift = !SIGMOID || __any_sync(kAll, !large);      // the same in the whole warp
+      const float m = shift ? row_max<L>(zs) : 0.f;
+      if (have) w = !SIGMOID ? exp_below(zs, m) : m > -10.f ? sigmoid_rn(zs) : expf(zs - m) / (1.0f + expf(zs));
       float sum = w;
       for (int o = half_k; o > 0; o >>= 1) sum += __shfl_xor_sync(kAll, sum, o);
       if (have) w = w / sum * p.scale;
     } else if (have) {
       w = (SIGMOID ? sigmoid_rn(zs) : exp_below(zs, zmax) / total) * p.scale;
     }
-    if (lane < p.k) {
-      p.topk_idx[(size_t)t * p.k + lane] = sel;
-      p.gates[(size_t)t * p.k + lane] = w;
+    if (there && sl < p.k) {
+      p.topk_idx[(size_t)t * p.k + sl] = sel;
+      p.gates[(size_t)t * p.k + sl] = w;
       if (have && p.counts != nullptr) atomicAdd(&hist[sel], 1);
     }
   }
@@ -491,16 +564,16 @@ route_scored_backward_kernel(int Tn, int E, int k, int renorm, float scale, long
     for (int i = 0; i < EPL; ++i) dz[i] = 0.f;
     float v = 0.f;
     if (renorm) {
-      const float m = warp_max_of(zs);
+      const float m = row_max<32>(zs);
       float pj = 0.f;
       if (SIGMOID) {
         if (have) pj = zs > 0.f ? sigmoid_rn(zs) : expf(zs - fminf(m, 0.f)) / (1.0f + expf(zs));
       } else if (have) {
         pj = exp_below(zs, m);
       }
-      const float sum = warp_sum(pj);
+      const float sum = row_sum<32>(pj);
       if (have) pj /= sum;
-      const float inner = warp_sum(pj * dw);
+      const float inner = row_sum<32>(pj * dw);
       if (have) v = scale * pj * (dw - inner);
       if (SIGMOID && have) v *= 1.0f / (1.0f + expf(zs));            // 1 - s without cancellation
     } else if (SIGMOID) {
@@ -511,16 +584,16 @@ route_scored_backward_kernel(int Tn, int E, int k, int renorm, float scale, long
       float m = low;
 #pragma unroll
       for (int i = 0; i < EPL; ++i) m = fmaxf(m, z[i]);
-      m = warp_max_of(m);
+      m = row_max<32>(m);
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < EPL; ++i) {
         dz[i] = z[i] > low ? exp_below(z[i], m) : 0.f;
         sum += dz[i];
       }
-      sum = warp_sum(sum);
+      sum = row_sum<32>(sum);
       const float s = have && sum > 0.f ? exp_below(zs, m) / sum : 0.f;
-      const float factor = sum > 0.f ? -scale * warp_sum(s * dw) / sum : 0.f;
+      const float factor = sum > 0.f ? -scale * row_sum<32>(s * dw) / sum : 0.f;
 #pragma unroll
       for (int i = 0; i < EPL; ++i) dz[i] *= factor;
       v = scale * s * dw;
@@ -586,22 +659,50 @@ int row_blocks(int T, int warps, int per_sm) {
   return want < most ? want : most;
 }
 
-template <typename T, int EPL>
+// A kernel, not a copy-engine memset: the kernel behind it can start as its dependent.
+__global__ void zero_counts_kernel(int E, int32_t* __restrict__ counts) {
+  allow_dependents();
+  grid_dependency_wait();
+  for (int i = threadIdx.x; i < E; i += blockDim.x) counts[i] = 0;
+}
+
+template <typename T, int L, int EPL>
 cudaError_t launch_route_t(const btx_route_desc* d, const void* logits, RouteParams p, cudaStream_t st) {
   const int vec = row_vectors(logits, p.stride, p.E, sizeof(T)) ? 1 : 0;
-  constexpr int W = RouteWarps<EPL>::n;
-  int blocks = row_blocks(p.T, W, EPL <= 8 ? 2 : 4);
-  // Counting: one block writes its own counts; more add theirs to zeros.  One block takes up to 16 rows on
-  // its own, which costs less than a second launch to clear the counts.
+  constexpr int W = RouteWarps<L * EPL>::n;
+  int blocks = row_blocks(p.T, W * (32 / L), RouteWarps<L * EPL>::per_sm);
+  // Counting: one block writes its own counts; more add theirs to zeros.  One block takes up to 16 rows on its own, which
+  // costs less than a second launch to clear the counts.
   p.single_block = p.counts != nullptr && p.T <= 16;
   if (p.single_block) blocks = 1;
   else if (p.counts != nullptr) {
-    cudaError_t e = cudaMemsetAsync(p.counts, 0, (size_t)p.E * sizeof(int32_t), st);
+    cudaError_t e = launch_after_predecessor(zero_counts_kernel, dim3(1), dim3(256), 0, st, true, p.E, p.counts);
     if (e != cudaSuccess) return e;
   }
+  p.lanes_per_group = 1;
+  while (2 * p.lanes_per_group * p.n_group <= L) p.lanes_per_group *= 2;
   const int sum2 = d->group_score == BTX_GROUP_SUM2;
-  return launch_after_predecessor(d->score == BTX_SCORE_SIGMOID ? route_scored_kernel<T, EPL, true> : route_scored_kernel<T, EPL, false>,
-                                  dim3(blocks), dim3(W * 32), 0, st, true, (const T*)logits, p, sum2, vec);
+  return launch_after_predecessor(
+      d->score == BTX_SCORE_SIGMOID ? route_scored_kernel<T, L, EPL, true> : route_scored_kernel<T, L, EPL, false>, dim3(blocks),
+      dim3(W * 32), 0, st, true, (const T*)logits, p, sum2, vec);
+}
+
+// Lanes of a row: enough for E experts at up to 16 each, for the k slots (one per lane) and for the groups.  Fewer lanes
+// per row mean more rows per warp instruction and a longer way through a row, so large batches take them and others get a
+// warp per row: E = 256, 8 of 8 groups, k = 8 takes 21.4 us with 16 lanes and 23.8 with 32 at T = 16384, 10.2 and 9.5 at
+// T = 4096, 8.0 and 5.3 at T = 512; E = 64, k = 2, softmax, T = 16384: 6.6 us with 8 lanes, 12.4 with 32.
+template <typename T>
+cudaError_t launch_route(const btx_route_desc* d, const void* logits, const RouteParams& p, cudaStream_t st) {
+  const int need = p.k > p.n_group ? p.k : p.n_group;
+  if (p.T > 8192) {
+    if (p.E <= 32 && need <= 8) return launch_route_t<T, 8, 4>(d, logits, p, st);
+    if (p.E <= 64 && need <= 8) return launch_route_t<T, 8, 8>(d, logits, p, st);
+    if (p.E <= 128 && need <= 16) return launch_route_t<T, 16, 8>(d, logits, p, st);
+    if (p.E <= 256 && need <= 16) return launch_route_t<T, 16, 16>(d, logits, p, st);
+  }
+  if (p.E <= 64) return launch_route_t<T, 32, 2>(d, logits, p, st);
+  if (p.E <= 256) return launch_route_t<T, 32, 8>(d, logits, p, st);
+  return launch_route_t<T, 32, 16>(d, logits, p, st);
 }
 
 template <typename T, int EPL>
@@ -649,12 +750,8 @@ extern "C" btx_status btx_route(const btx_route_desc* desc, const void* logits, 
   p.T = desc->T; p.E = desc->E; p.k = desc->k; p.n_group = desc->n_group; p.group_size = desc->E / desc->n_group;
   p.topk_group = desc->topk_group; p.renorm = desc->renorm != 0; p.scale = desc->scale; p.stride = logits_stride;
   p.bias = bias; p.row_valid = row_valid; p.topk_idx = topk_idx; p.gates = gates; p.scores = scores; p.counts = counts;
-  p.lanes_per_group = 1;
-  while (2 * p.lanes_per_group * p.n_group <= 32) p.lanes_per_group *= 2;
   if (p.topk_group == p.n_group) p.n_group = 1;                // every group stays: nothing to choose
-  const cudaError_t e = desc->dtype == BTX_BF16
-      ? by_width<__nv_bfloat16>(p.E, [&](auto w) { return launch_route_t<__nv_bfloat16, w.value>(desc, logits, p, st); })
-      : by_width<float>(p.E, [&](auto w) { return launch_route_t<float, w.value>(desc, logits, p, st); });
+  const cudaError_t e = desc->dtype == BTX_BF16 ? launch_route<__nv_bfloat16>(desc, logits, p, st) : launch_route<float>(desc, logits, p, st);
   return e == cudaSuccess ? BTX_OK : BTX_ERR_CUDA;
 }
 

@@ -216,6 +216,38 @@ def test_large_batch_matches_in_every_row():
     assert torch.equal(got["counts"].long(), torch.bincount(want.flatten(), minlength=256))
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("score", [0, 1], ids=["softmax", "sigmoid"])
+@pytest.mark.parametrize("shape", [(33, 5, 1, 1), (30, 6, 5, 3), (64, 8, 8, 4), (120, 12, 10, 3), (128, 16, 4, 2), (165, 6, 3, 2),
+                                   (256, 8, 8, 4), (256, 16, 16, 9), (256, 20, 2, 1), (512, 8, 8, 4)], ids=lambda s: "x".join(map(str, s)))
+def test_large_batches_share_a_warp_between_rows(shape, score, dtype):
+    # several rows per warp: ordinary rows beside rows that are masked, tied, or not settled by fp32
+    E, k, G, tg = shape
+    T = 8200
+    z, b = logits_of(T, E, dtype, E + k)
+    z[5:5000:7] *= 1e-6                                    # scores plus bias within a few fp32 steps where b is
+    z[11:5000:13] = 0
+    z[17:5000:19] = float("-inf")
+    z[23:5000:29, ::3] = float("nan")
+    z[31, :] = float("inf")
+    valid = torch.ones(T, dtype=torch.uint8, device=DEV)
+    valid[3::11] = 0
+    rows = np.r_[0:60, 2000:2030, T - 30:T]
+    for bias in (None, b, b * 1e-6):
+        for gs in (0, 1):
+            kw = dict(n_group=G, topk_group=tg, group_score=gs, renorm=bool(gs), scale=1.5)
+            _, got = run(z, k, score, bias, valid=valid, scores=False, **kw)
+            want = o.route(z[rows].double().cpu().numpy(), k, score, None if bias is None else bias.double().cpu().numpy(),
+                           valid=valid.cpu().numpy()[rows] != 0, **kw)
+            assert np.array_equal(got["topk_idx"].cpu().numpy()[rows], want[0])
+            np.testing.assert_allclose(got["gates"].double().cpu().numpy()[rows], want[1], rtol=REL, atol=1e-36)
+            # a batch below the limit runs a warp per row: the same choice
+            _, part = run(z[:4000].contiguous(), k, score, bias, valid=valid[:4000].contiguous(), scores=False, **kw)
+            assert torch.equal(part["topk_idx"], got["topk_idx"][:4000]) and torch.equal(part["gates"], got["gates"][:4000])
+            flat = got["topk_idx"].flatten()
+            assert torch.equal(got["counts"].long(), torch.bincount(flat[flat >= 0], minlength=E))
+
+
 def test_binding_refuses_wrong_tensors():
     z = torch.randn(4, 16, device=DEV)
     desc = B.make_route_desc(4, 16, 2, torch.float32)
