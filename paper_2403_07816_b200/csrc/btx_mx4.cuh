@@ -46,10 +46,10 @@ struct Dispatch {
   int32_t* n_tiles;                        // [1] padded row tiles in use
   int32_t* block_counts;                   // [blocks * E] (batches of more than one block)
   int32_t* pad_offsets;                    // [E + 1] first padded row of every expert
-  int blocks;
+  int chunk, blocks;                       // assignments per block of the dispatch kernels, blocks
   int32_t* status;                         // cleared by the first kernel
 };
-int dispatch_blocks(long long R);
+int dispatch_chunk(long long R);
 cudaError_t launch_dispatch(const Dispatch& q, cudaStream_t st);
 // x [T, d] cast to MXFP4 and written to the k padded rows of every token
 cudaError_t launch_quantize_rows(const Dispatch& q, int dtype, const void* x, uint8_t* codes, uint8_t* scales, cudaStream_t st);

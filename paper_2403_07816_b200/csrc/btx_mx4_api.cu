@@ -41,7 +41,8 @@ btx_status make_moe_plan(const btx_mx4_moe_desc* d, MoePlan* pl) {
   q.T = d->T; q.k = d->k; q.R = (int)R; q.E = d->E; q.d = d->d_model;
   q.pad_tiles = pad_tiles;
   q.m_tiles_max = (int)tiles;
-  q.blocks = dispatch_blocks(R);
+  q.chunk = dispatch_chunk(R);
+  q.blocks = (int)((R + q.chunk - 1) / q.chunk);
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t at = o; o = align_up(o + bytes, 256); return at; };
   const size_t rp = (size_t)tiles * kTileRows;

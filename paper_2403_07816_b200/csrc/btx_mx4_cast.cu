@@ -15,7 +15,7 @@ namespace {
 
 constexpr int kCastThreads = 256;
 constexpr int kSortThreads = 512;
-constexpr int kSortChunk = 2048;           // assignments per block of the dispatch kernels
+constexpr int kSortOne = 2048;             // assignments that one block dispatches on its own
 
 // A warp takes kCastUnroll chunks of 256 elements of one row at a time.  I: the type that numbers them; the two divisions
 // in 64 bits cost as many instructions as the cast of the chunks.
@@ -199,7 +199,7 @@ struct SortShared {
   int cnt[kMaxExperts4 + 1], running[kMaxExperts4 + 1], pad[kMaxExperts4 + 1], scan[kSortThreads / 32];
 };
 
-// The whole dispatch of a batch of at most kSortChunk assignments in one block.
+// The whole dispatch of a batch of at most kSortOne assignments in one block.
 __global__ void __launch_bounds__(kSortThreads)
 dispatch_one_kernel(const Dispatch q) {
   __shared__ SortShared s;
@@ -226,7 +226,7 @@ dispatch_count_kernel(const Dispatch q) {
   if (blockIdx.x == 0 && threadIdx.x < kStatusWords) q.status[threadIdx.x] = 0;
   for (int i = threadIdx.x; i < q.E; i += kSortThreads) hist[i] = 0;
   __syncthreads();
-  const int begin = blockIdx.x * kSortChunk, end = min(q.R, begin + kSortChunk);
+  const int begin = blockIdx.x * q.chunk, end = min(q.R, begin + q.chunk);
   for (int i = begin + threadIdx.x; i < end; i += kSortThreads) {
     const int e = q.topk_idx[i];
     if ((unsigned)e < (unsigned)q.E) atomicAdd(&hist[e], 1);
@@ -271,8 +271,8 @@ dispatch_scatter_kernel(const Dispatch q) {
     s.pad[i] = q.pad_offsets[i];
   }
   __syncthreads();
-  const int begin = blockIdx.x * kSortChunk;
-  scatter_rounds(begin, min(q.R, begin + kSortChunk), q.E, q.topk_idx, s.running, s.wcnt, s.pad, q.flat2row, q.rowmap);
+  const int begin = blockIdx.x * q.chunk;
+  scatter_rounds(begin, min(q.R, begin + q.chunk), q.E, q.topk_idx, s.running, s.wcnt, s.pad, q.flat2row, q.rowmap);
 }
 
 template <typename T, typename I>
@@ -365,7 +365,13 @@ cudaError_t launch_dequantize(const uint8_t* codes, const uint8_t* scales, int b
   });
 }
 
-int dispatch_blocks(long long R) { return (int)((R + kSortChunk - 1) / kSortChunk); }
+// Assignments per block: whole rounds of the block's threads, few enough rounds that at most 592 blocks share a batch (the
+// scan walks over the blocks).
+int dispatch_chunk(long long R) {
+  if (R <= kSortOne) return kSortOne;
+  const long long rounds = (R + kSortThreads * 592ll - 1) / (kSortThreads * 592ll);
+  return (int)(rounds * kSortThreads);
+}
 
 cudaError_t launch_dispatch(const Dispatch& q, cudaStream_t st) {
   if (q.blocks <= 1) {

@@ -24,6 +24,8 @@
 //            silu(h1) * h3 in fp32, cast to MXFP4 in registers (32 neighbouring units are a block)
 //   DOWN     gate-scaled fp32 rows scattered to t*k+slot
 // Every wait is bounded (tcx::mbar_wait); a wait that runs out leaves BTX_ERR_TIMEOUT in the status word.
+#include <cmath>
+
 #include "btx_mx4_dev.cuh"
 
 namespace btx {
@@ -562,21 +564,42 @@ Params base_params(const GemmArgs& g) {
   return p;
 }
 
-// CTA pairs want whole tiles of 256 rows and enough of them
-bool use_pairs(long long pair_tiles, long long rows) { return rows > 128 && pair_tiles >= sm_count() / 2; }
+// Which kernel a product takes: rounds of tiles over the multiprocessors times the time of a tile, in measured us: 0.38 a
+// stage of a 128 x 128 tile (its contraction split over a cluster where that keeps CTAs busy) and 0.47 of a 256 x 256 tile,
+// or the epilogue `epi` of the larger tile (the smaller one's takes half) where that is longer, and what a tile costs
+// beside them.  E.g. N = 4096, K = 4096: 512 rows 10.1 and 11.3 us, 768 rows 16.0 and 12.0 us; N = 4096, K = 11008: 256
+// rows 14.6 and 21.4, 768 rows 35.7 and 22.8; N = 11008, K = 4096: 192 rows 15.6 and 11.8, 384 rows 16.4 and 18.4.
+double single_us(double tiles, long long K, double epi) {
+  const double split = split_of((long long)(tiles + 0.5), K), kb = (double)((K + SK - 1) / SK);
+  return ceil(tiles * split / sm_count()) * (fmax(ceil(kb / split) * 0.38, epi / 2) + 0.4);
+}
+double pair_us(double tiles, long long K, double epi) {
+  return ceil(tiles / (sm_count() / 2)) * (fmax((double)((K + SK - 1) / SK) * 0.47, epi) + 0.85);
+}
+constexpr double kStoreUs = 2.0, kGateUpUs = 5.5, kDownUs = 3.5;       // epilogues of a 256 x 256 tile
 
 }  // namespace
 
+// The expert layer's two products, for experts with about rows / experts rows each (a tile more than they fill for
+// every second).  d = 4096, F = 11008, 4 experts, top-2: 128 tokens take 73 us on single CTAs and 82 on pairs, 256 tokens
+// 106 and 86, 1024 tokens 253 and 180.  d = 2048, F = 1024, 64 experts, top-8: 1024 tokens 113 and 126.
 bool pairs_fit(long long rows, long long experts, long long d, long long F) {
-  return rows >= 256 * experts && use_pairs(rows / 256 * ((d + 255) / 256), rows) && F > 0;
+  if (rows == 0) return false;
+  const double each = (double)rows / (double)experts;
+  const double t1 = experts * fmax(1.0, each / 128 + 0.5), t2 = experts * fmax(1.0, each / 256 + 0.5);
+  const double n1 = (double)((2 * F + 127) / 128), m1 = (double)((d + 127) / 128);
+  const double n2 = (double)((2 * F + 255) / 256), m2 = (double)((d + 255) / 256);
+  return pair_us(t2 * n2, d, kGateUpUs) + pair_us(t2 * m2, F, kDownUs) <
+         single_us(t1 * n1, d, kGateUpUs) + single_us(t1 * m1, F, kDownUs);
 }
 
 btx_status launch_matmul(const GemmArgs& g, int dtype, void* y, cudaStream_t st) {
   Params p = base_params(g);
   p.y = y; p.out_bf16 = dtype == BTX_BF16;
   p.wide = aligned32(y) && (size_t)g.N * (p.out_bf16 ? 2 : 4) % 32 == 0;
-  if (use_pairs((long long)g.batch * ((g.M + 255) / 256) * ((g.N + 255) / 256), g.M)) return launch_pair<STORE>(g, p, st);
   const long long tiles = (long long)p.m_tiles * p.n_tiles * p.batch;
+  if (pair_us((double)g.batch * ((g.M + 255) / 256) * ((g.N + 255) / 256), g.K, kStoreUs) < single_us((double)tiles, g.K, kStoreUs))
+    return launch_pair<STORE>(g, p, st);
   p.a_rows = p.a_box = g.M < BM ? (g.M + 31) / 32 * 32 : BM;
   p.split = split_of(tiles, g.K);
   return p.split > 1 ? launch<STORE, true>(g, p, tiles, st) : launch<STORE, false>(g, p, tiles, st);
