@@ -228,11 +228,14 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         for (int i = threadIdx.x; i < rows * quads; i += THREADS) {
           const int r = i / quads, c = (i - r * quads) * 4;
           const uint32_t at = ring + (uint32_t)(r * PART_PITCH + c0 + c) * 4;
-          float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-          for (int s = 0; s < p.split; ++s) {
-            const float4 x = ld_cluster_v4(map_to_cta(at, s));
-            a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
-          }
+          float4 x[8];                                    // all CTAs' loads on their way at once
+#pragma unroll
+          for (int s = 0; s < 8; ++s)
+            if (s < p.split) x[s] = ld_cluster_v4(map_to_cta(at, s));
+          float4 a = x[0];
+#pragma unroll
+          for (int s = 1; s < 8; ++s)
+            if (s < p.split) { a.x += x[s].x; a.y += x[s].y; a.z += x[s].z; a.w += x[s].w; }
           if (MODE == DOWN) {
             const int flat = p.rowmap[it.mt * BM + r];
             const float g = p.gates[flat];
@@ -251,8 +254,14 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         for (int i = threadIdx.x; i < rows * cols; i += THREADS) {
           const int r = i / cols, c = i - r * cols;
           const uint32_t at = ring + (uint32_t)(r * PART_PITCH + c0 + c) * 4;
-          float a = 0.f;
-          for (int s = 0; s < p.split; ++s) a += ld_cluster(map_to_cta(at, s));
+          float x[8];
+#pragma unroll
+          for (int s = 0; s < 8; ++s)
+            if (s < p.split) x[s] = ld_cluster(map_to_cta(at, s));
+          float a = x[0];
+#pragma unroll
+          for (int s = 1; s < 8; ++s)
+            if (s < p.split) a += x[s];
           const size_t o = ((size_t)it.b * p.M + it.mt * BM + r) * p.N + n0 + c;     // STORE (DOWN's rows are wide)
           if (p.out_bf16) ((__nv_bfloat16*)p.y)[o] = __float2bfloat16_rn(a);
           else ((float*)p.y)[o] = a;
