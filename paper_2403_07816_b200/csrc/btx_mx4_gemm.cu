@@ -38,18 +38,12 @@ constexpr int SMEM_BYTES = RING_BYTES + 1024 + 320;
 constexpr int PART_PITCH = BN + 4;                       // SPLIT: floats per row of a partial tile (a quad apart: no bank conflicts)
 static_assert(MAX_STAGES * 24 + 48 <= 320 && BM * PART_PITCH * 4 <= RING_BYTES, "shared memory");
 
-// SPLIT: one quad or one element of the sum over the cluster's partial tiles, in CTA order.
+// SPLIT: a quad of a CTA's partial tile.
 __device__ __forceinline__ float4 ld_cluster_v4(uint32_t addr) {
   float4 v;
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
   return v;
 }
-__device__ __forceinline__ float ld_cluster(uint32_t addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-  return v;
-}
-
 template <int MODE, bool SPLIT>
 __global__ void __launch_bounds__(THREADS, 1)
 mx4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const Params p) {
@@ -223,48 +217,40 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
       const int rows = p.grouped ? p.tile_rows[it.mt] : min(BM, p.M - it.mt * BM);
       const int width = BN / p.split, c0 = part * width, n0 = it.nt * BN + c0;
       const int cols = min(width, p.N - n0);
-      if (p.wide && cols > 0) {                           // whole quads on 16-byte boundaries
-        const int quads = cols / 4;
-        for (int i = threadIdx.x; i < rows * quads; i += THREADS) {
-          const int r = i / quads, c = (i - r * quads) * 4;
-          const uint32_t at = ring + (uint32_t)(r * PART_PITCH + c0 + c) * 4;
-          float4 x[8];                                    // all CTAs' loads on their way at once
+      const int quads = (cols + 3) / 4;                   // (none where cols is negative: the slice lies past the last column)
+      for (int i = threadIdx.x; i < rows * quads; i += THREADS) {
+        const int r = i / quads, c = (i - r * quads) * 4;
+        const uint32_t at = ring + (uint32_t)(r * PART_PITCH + c0 + c) * 4;
+        float4 x[8];                                      // all CTAs' loads on their way at once
 #pragma unroll
-          for (int s = 0; s < 8; ++s)
-            if (s < p.split) x[s] = ld_cluster_v4(map_to_cta(at, s));
-          float4 a = x[0];
+        for (int s = 0; s < 8; ++s)
+          if (s < p.split) x[s] = ld_cluster_v4(map_to_cta(at, s));
+        float4 a = x[0];
 #pragma unroll
-          for (int s = 1; s < 8; ++s)
-            if (s < p.split) { a.x += x[s].x; a.y += x[s].y; a.z += x[s].z; a.w += x[s].w; }
-          if (MODE == DOWN) {
-            const int flat = p.rowmap[it.mt * BM + r];
-            const float g = p.gates[flat];
-            *reinterpret_cast<float4*>((float*)p.y + (size_t)flat * p.N + n0 + c) = make_float4(a.x * g, a.y * g, a.z * g, a.w * g);
-          } else {
-            const size_t o = ((size_t)it.b * p.M + it.mt * BM + r) * p.N + n0 + c;
+        for (int s = 1; s < 8; ++s)
+          if (s < p.split) { a.x += x[s].x; a.y += x[s].y; a.z += x[s].z; a.w += x[s].w; }
+        if (MODE == DOWN) {
+          const int flat = p.rowmap[it.mt * BM + r];
+          const float g = p.gates[flat];
+          *reinterpret_cast<float4*>((float*)p.y + (size_t)flat * p.N + n0 + c) = make_float4(a.x * g, a.y * g, a.z * g, a.w * g);
+        } else {
+          const size_t o = ((size_t)it.b * p.M + it.mt * BM + r) * p.N + n0 + c;
+          const float f[4] = {a.x, a.y, a.z, a.w};
+          if (p.wide) {                                   // whole quads on 16-byte (bf16: 8-byte) boundaries
             if (p.out_bf16) {
               __nv_bfloat162 h[2] = {__floats2bfloat162_rn(a.x, a.y), __floats2bfloat162_rn(a.z, a.w)};
               *reinterpret_cast<uint2*>((__nv_bfloat16*)p.y + o) = *reinterpret_cast<const uint2*>(h);
             } else {
               *reinterpret_cast<float4*>((float*)p.y + o) = a;
             }
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (c + j < cols) {
+                if (p.out_bf16) ((__nv_bfloat16*)p.y)[o + j] = __float2bfloat16_rn(f[j]);
+                else ((float*)p.y)[o + j] = f[j];
+              }
           }
-        }
-      } else if (cols > 0) {
-        for (int i = threadIdx.x; i < rows * cols; i += THREADS) {
-          const int r = i / cols, c = i - r * cols;
-          const uint32_t at = ring + (uint32_t)(r * PART_PITCH + c0 + c) * 4;
-          float x[8];
-#pragma unroll
-          for (int s = 0; s < 8; ++s)
-            if (s < p.split) x[s] = ld_cluster(map_to_cta(at, s));
-          float a = x[0];
-#pragma unroll
-          for (int s = 1; s < 8; ++s)
-            if (s < p.split) a += x[s];
-          const size_t o = ((size_t)it.b * p.M + it.mt * BM + r) * p.N + n0 + c;     // STORE (DOWN's rows are wide)
-          if (p.out_bf16) ((__nv_bfloat16*)p.y)[o] = __float2bfloat16_rn(a);
-          else ((float*)p.y)[o] = a;
         }
       }
     }
