@@ -57,7 +57,9 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctl + MAX_STAGES * 24 + 32);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(ctl + MAX_STAGES * 24 + 40);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int n_stages = stage_count(p.a_rows, RING_BYTES), s_bytes = stage_bytes(p.a_rows);
+  const bool turn = MODE == STORE && !SPLIT && !p.wide;   // a piece of the ring turns tiles around
+  const int ring_bytes = RING_BYTES - (turn ? EPI_WARPS * TURN_BYTES : 0);
+  const int n_stages = stage_count(p.a_rows, ring_bytes), s_bytes = stage_bytes(p.a_rows);
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < n_stages; ++s) { mbar_init(bar_full + s * 8, 2); mbar_init(bar_empty + s * 8, 1); mbar_init(bar_scales + s * 8, 4); }
@@ -198,7 +200,11 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                          "f"(v[i + 3]) : "memory");
         }
       } else if (any) {
-        finish_chunk<MODE>(p, it, v, it.nt * BN + half * 64, m, flat);
+        if (turn)
+          store_turned(p, it, v, it.nt * BN + half * 64, it.mt * BM + q * 32, lane,
+                       reinterpret_cast<uint32_t*>(smem_raw + (ring - raw) + ring_bytes + (warp - 2) * TURN_BYTES));
+        else
+          finish_chunk<MODE>(p, it, v, it.nt * BN + half * 64, m, flat);
       }
       acc ^= 1u;
       if (acc == 0) acc_phase ^= 1u;
@@ -273,10 +279,11 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
 // and hands them over, so the next tile starts before anything is computed or stored.
 //   warp 0  TMA   warp 1  MMAs (one lane of the leader CTA)   warps 2-9  epilogue, two 64-column chunks each
 //   warps 10-13  scales   warp 14  TMA of the scales
-constexpr int P_STAGES = 6, P_RING = 8;                  // stages of codes, of scales
+constexpr int P_STAGES = 6, P_RING = 8;                  // stages of codes, of scales (half of them where tiles are turned around)
 constexpr int P_STAGE_BYTES = A_BYTES + B_BYTES;
 constexpr int P_SCALE_BYTES = 6 * kTileBytes;            // of a stage and CTA: two tiles of A, two of each half of B
-constexpr int P_SMEM = P_STAGES * P_STAGE_BYTES + P_RING * P_SCALE_BYTES + 1024 + 384;
+constexpr int P_TURN_MORE = EPI_WARPS * TURN_BYTES - P_RING / 2 * P_SCALE_BYTES;       // beyond the freed half
+constexpr int P_SMEM = P_STAGES * P_STAGE_BYTES + P_RING * P_SCALE_BYTES + P_TURN_MORE + 1024 + 384;
 constexpr int P_THREADS = 64 + EPI_WARPS * 32 + 160;
 constexpr int P_ACC1 = 128, P_SF0 = 384, P_SF_COLS = 24, P_SF_SLOTS = 5;
 static_assert(P_SF0 + P_SF_SLOTS * P_SF_COLS <= 512 && P_ACC1 + 256 <= P_SF0, "tensor memory");
@@ -299,7 +306,9 @@ mx4_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t ring = (raw + 1023u) & ~1023u;
   const uint32_t sf_ring = ring + P_STAGES * P_STAGE_BYTES;
-  uint8_t* ctl = smem_raw + (sf_ring - raw) + P_RING * P_SCALE_BYTES;
+  const bool turn = MODE == STORE && !p.wide;
+  const uint32_t ring_slots = turn ? P_RING / 2 : P_RING;
+  uint8_t* ctl = smem_raw + (sf_ring - raw) + P_RING * P_SCALE_BYTES + P_TURN_MORE;
   const uint32_t bar_full = smem_u32(ctl), bar_empty = bar_full + P_STAGES * 8;
   const uint32_t bar_scales = bar_empty + P_STAGES * 8;                 // used in the leader
   const uint32_t bar_tfull = bar_scales + P_SF_SLOTS * 8, bar_handed = bar_tfull + 16;
@@ -408,12 +417,12 @@ mx4_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
           mbar_expect_tx(bar, P_SCALE_BYTES);
           load_3d(to, &tmSA, 0, kb * 2, a_tile, bar);
           load_3d(to + 2 * kTileBytes, &tmSB, 0, kb * 2, b_tile, bar);
-          if (++slot == P_RING) { slot = 0; phase ^= 1u; }
+          if (++slot == ring_slots) { slot = 0; phase ^= 1u; }
         }
       }
-      for (int i = 0; i < P_RING && ok; ++i) {            // every copy has landed and has been read
+      for (uint32_t i = 0; i < ring_slots && ok; ++i) {            // every copy has landed and has been read
         ok = mbar_wait(bar_sempty + slot * 8, phase ^ 1u, abort_flag, p.status);
-        if (++slot == P_RING) { slot = 0; phase ^= 1u; }
+        if (++slot == ring_slots) { slot = 0; phase ^= 1u; }
       }
     }
   } else if (warp >= 2 + EPI_WARPS) {
@@ -445,7 +454,7 @@ mx4_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
           arrive(bar_sempty + in * 8);
         }
         if (++slot == P_SF_SLOTS) slot = 0;
-        if (++in == P_RING) { in = 0; in_phase ^= 1u; }
+        if (++in == ring_slots) { in = 0; in_phase ^= 1u; }
       }
     }
   } else {
@@ -469,10 +478,17 @@ mx4_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
       if (any) load_chunk(taddr + c0 * 64, v);
       tc_fence_before();
       if (lane == 0) mbar_arrive_cluster(handed);         // (and all of the tile before has been read)
-      if (any) finish_chunk<MODE>(p, it, v, n0 + c0 * 64, m, flat);
+      auto finish = [&](int c) {
+        if (turn)
+          store_turned(p, it, v, n0 + c * 64, it.mt * 256 + (int)rank * 128 + q * 32, lane,
+                       reinterpret_cast<uint32_t*>(smem_raw + (sf_ring - raw) + P_RING / 2 * P_SCALE_BYTES + (warp - 2) * TURN_BYTES));
+        else
+          finish_chunk<MODE>(p, it, v, n0 + c * 64, m, flat);
+      };
       if (any) {
+        finish(c0);
         load_chunk(taddr + c1 * 64, v);
-        finish_chunk<MODE>(p, it, v, n0 + c1 * 64, m, flat);
+        finish(c1);
       }
       __syncwarp();
       tc_fence_before();

@@ -148,7 +148,7 @@ def check_product(y, qa, qb):
 @pytest.mark.parametrize("shape", [(1, 1, 1, 32), (1, 1, 128, 64), (1, 128, 128, 256), (1, 5, 200, 96), (1, 129, 255, 160),
                                    (1, 300, 64, 1056), (2, 130, 136, 288), (3, 1, 1000, 512), (1, 1000, 17, 2048),
                                    (1, 64, 4096, 4096), (1, 520, 2056, 544),
-                                   (1, 2100, 2300, 320), (3, 1100, 1300, 96), (1, 4100, 1290, 2080)], ids=lambda s: "x".join(map(str, s)))
+                                   (1, 2100, 2300, 320), (3, 1100, 1300, 96), (1, 4100, 1290, 2080), (1, 1500, 3331, 128), (1, 1500, 3334, 128)], ids=lambda s: "x".join(map(str, s)))
 def test_product(shape, dtype):
     batch, M, N, K = shape
     y, qa, qb = matmul(randn(batch, M, K, seed=M + K), randn(batch, N, K, seed=N + K + 1, std=0.02), dtype)
