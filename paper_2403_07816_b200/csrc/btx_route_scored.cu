@@ -93,25 +93,36 @@ __device__ __forceinline__ float sigmoid_rn(float z) { return 1.0f / (1.0f + exp
 // exp(z - m) for z <= m, with exp(0) = 1 where both are +inf
 __device__ __forceinline__ float exp_below(float z, float m) { return z == m ? 1.0f : expf(z - m); }
 
-// The lane's EPL logits of one row.  `vec`: rows start on 16-byte boundaries and E is a multiple of a vector.
-template <typename T, int EPL>
-__device__ __forceinline__ void load_row(const T* __restrict__ row, int E, int lane, bool vec, float (&z)[EPL]) {
+// The lane's EPL logits of one row shared by L lanes (all 32 lanes of the warp call it, each with its row; on = false: no
+// candidate).  VEC: rows start on 16-byte boundaries and E is a multiple of a vector; other rows are read with
+// neighbouring lanes on neighbouring logits and turned through `st` (EPL * L floats of the row).
+template <typename T, int L, int EPL, bool VEC>
+__device__ __forceinline__ void load_row(const T* __restrict__ row, int E, int sl, bool on, float* st, float (&z)[EPL]) {
   constexpr int VN = Vec<T>::N;
-  const int e0 = lane * EPL;
-  if constexpr (EPL >= VN) {
-    if (vec) {
+  const int e0 = sl * EPL;
+  if constexpr (VEC && EPL >= VN) {
 #pragma unroll
-      for (int i = 0; i < EPL; i += VN) {
-        float v[VN];
-        if (e0 + i < E) Vec<T>::load(row + e0 + i, v);
+    for (int i = 0; i < EPL; i += VN) {
+      float v[VN];
+      if (on && e0 + i < E) Vec<T>::load(row + e0 + i, v);
 #pragma unroll
-        for (int j = 0; j < VN; ++j) z[i + j] = e0 + i < E ? v[j] : -CUDART_INF_F;
-      }
-      return;
+      for (int j = 0; j < VN; ++j) z[i + j] = on && e0 + i < E ? v[j] : -CUDART_INF_F;
     }
-  }
+  } else if constexpr (EPL <= 2) {
 #pragma unroll
-  for (int i = 0; i < EPL; ++i) z[i] = e0 + i < E ? to_f32(row[e0 + i]) : -CUDART_INF_F;
+    for (int i = 0; i < EPL; ++i) z[i] = on && e0 + i < E ? to_f32(row[e0 + i]) : -CUDART_INF_F;
+  } else {
+    float v[EPL];
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) v[i] = on && i * L + sl < E ? to_f32(row[i * L + sl]) : -CUDART_INF_F;
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) st[i * L + sl] = v[i];
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) z[i] = st[e0 + i];
+    __syncwarp();
+  }
 }
 
 // Two-best merge: (a, b) with a >= b
@@ -169,59 +180,88 @@ __device__ __forceinline__ uint32_t choose_groups(const F* key, int G, int size,
   return mask;
 }
 
-// The same choice with 64-bit scores, for the few rows whose order 32 bits do not settle.  keys: E + n_group * P
-// doubles of the warp's shared memory.  Returns the expert of slot `lane` (-1: none).
+// f(i, group of expert i of the lane) for the lane's EPL experts, the first being member r0 of group g0.
+template <int EPL, typename F> __device__ __forceinline__ void for_each_group(int g0, int r0, int size, F&& f) {
+  int g = g0, r = r0;
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) {
+    f(i, g);
+    if (++r == size) { r = 0; ++g; }
+  }
+}
+
+// The choice with 64-bit scores, for the few rows whose order 32 bits do not settle, by the whole warp.  `keys`: E + 32
+// doubles of the warp's shared memory, expert e at e + (e / group_size) * P.
+struct RowScore {                           // exact scores of one row
+  double zmax, total;
+  template <bool SIGMOID> __device__ __forceinline__ double of(double z) const {
+    return SIGMOID ? 1.0 / (1.0 + exp(-z)) : (z == zmax ? 1.0 : exp(z - zmax)) / total;
+  }
+};
+template <typename T, bool SIGMOID>
+__device__ __forceinline__ RowScore row_score(const T* __restrict__ row, int E, int lane) {
+  const double low = -CUDART_INF;
+  RowScore s = {low, 0.0};
+  if (!SIGMOID) {
+    for (int e = lane; e < E; e += 32) {
+      const double z = (double)to_f32(row[e]);
+      if (z > s.zmax) s.zmax = z;
+    }
+    s.zmax = row_max<32>(s.zmax);
+    for (int e = lane; e < E; e += 32) {
+      const double z = (double)to_f32(row[e]);
+      if (z > low) s.total += z == s.zmax ? 1.0 : exp(z - s.zmax);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s.total += __shfl_xor_sync(kAll, s.total, o);
+  }
+  return s;
+}
+// lanes of the whole warp that share a group
+__device__ __forceinline__ int warp_lanes_per_group(const RouteParams& p) {
+  int P = 1;
+  while (2 * P * p.n_group <= 32) P *= 2;
+  return P;
+}
+
+// The groups that stay.
+template <typename T, bool SIGMOID>
+__device__ __noinline__ uint32_t groups_in_double(const T* __restrict__ row, const RouteParams& p, int sum2, double* keys, int lane) {
+  const int P = warp_lanes_per_group(p);
+  const double low = -CUDART_INF;
+  const RowScore s = row_score<T, SIGMOID>(row, p.E, lane);
+  for (int e = lane; e < p.E; e += 32) {
+    const double z = (double)to_f32(row[e]);
+    double c = low;
+    if (z > low) c = p.bias ? s.of<SIGMOID>(z) + (double)p.bias[e] : sum2 ? s.of<SIGMOID>(z) : z;
+    keys[e + e / p.group_size * P] = c > low ? c : low;
+  }
+  __syncwarp();
+  double margin, reach;
+  const uint32_t stay = choose_groups<32, double>(keys, p.n_group, p.group_size, P, p.topk_group, sum2, lane, margin, reach);
+  __syncwarp();
+  return stay;
+}
+
+// The expert of slot `lane` (-1: none).
 template <typename T, bool SIGMOID>
 __device__ __noinline__ int choose_in_double(const T* __restrict__ row, const RouteParams& p, int sum2, double* keys, int lane) {
-  int P = 0;                                // lanes of the whole warp that share a group
-  if (p.n_group > 1)
-    for (P = 1; 2 * P * p.n_group <= 32;) P *= 2;
   const double low = -CUDART_INF;
-  double zmax = low, total = 0.0;
-  if (!SIGMOID) {
-    for (int e = lane; e < p.E; e += 32) {
-      const double z = (double)to_f32(row[e]);
-      if (z > zmax) zmax = z;
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) zmax = fmax(zmax, __shfl_xor_sync(kAll, zmax, o));
-    for (int e = lane; e < p.E; e += 32) {
-      const double z = (double)to_f32(row[e]);
-      if (z > low) total += z == zmax ? 1.0 : exp(z - zmax);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(kAll, total, o);
+  const uint32_t stay = p.n_group > 1 ? groups_in_double<T, SIGMOID>(row, p, sum2, keys, lane) : kAll;
+  const RowScore s = row_score<T, SIGMOID>(row, p.E, lane);
+  for (int e = lane; e < p.E; e += 32) {
+    const double z = (double)to_f32(row[e]);
+    double c = low;
+    if (z > low && ((stay >> (p.n_group > 1 ? e / p.group_size : 0)) & 1u)) c = p.bias ? s.of<SIGMOID>(z) + (double)p.bias[e] : z;
+    keys[e] = c > low ? c : low;
   }
-  auto score = [&](double z) {
-    return SIGMOID ? 1.0 / (1.0 + exp(-z)) : (z == zmax ? 1.0 : exp(z - zmax)) / total;
-  };
-  // the key that orders experts; without a bias it is the logit, and only a group's sum needs scores
-  auto place = [&](bool for_groups) {
-    for (int e = lane; e < p.E; e += 32) {
-      const double z = (double)to_f32(row[e]);
-      double c = low;
-      if (z > low) c = p.bias ? score(z) + (double)p.bias[e] : (for_groups && sum2 ? score(z) : z);
-      keys[e + (P ? e / p.group_size * P : 0)] = c > low ? c : low;
-    }
-    __syncwarp();
-  };
-  uint32_t stay = kAll;
-  place(true);
-  if (p.n_group > 1) {
-    double margin, reach;
-    stay = choose_groups<32, double>(keys, p.n_group, p.group_size, P, p.topk_group, sum2, lane, margin, reach);
-    __syncwarp();
-    if (!p.bias && sum2) place(false);
-  }
+  __syncwarp();
   int mine = -1;
   for (int j = 0; j < p.k; ++j) {
     double bv = low;
     int bi = -1;
-    for (int e = lane; e < p.E; e += 32) {
-      const int g = p.n_group > 1 ? e / p.group_size : 0;
-      const double c = keys[e + g * P];
-      if (((stay >> g) & 1u) && c > bv) { bv = c; bi = e; }
-    }
+    for (int e = lane; e < p.E; e += 32)
+      if (keys[e] > bv) { bv = keys[e]; bi = e; }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
       const double ov = __shfl_xor_sync(kAll, bv, o);
@@ -230,7 +270,7 @@ __device__ __noinline__ int choose_in_double(const T* __restrict__ row, const Ro
     }
     if (bi < 0) break;
     if (lane == j) mine = bi;
-    if (lane == 0) keys[bi + (P ? bi / p.group_size * P : 0)] = low;
+    if (lane == 0) keys[bi] = low;
     __syncwarp();
   }
   return mine;
@@ -260,9 +300,9 @@ __device__ __forceinline__ float sigmoid_key(float z) { return rcp_fast(1.0f + e
 // registers allow more per thread, but T = 16384 takes a third pass over the grid (24.8 instead of 21.4 us); 16 spill.
 template <int E> struct RouteWarps { static constexpr int n = E <= 128 ? 16 : E <= 256 ? 14 : 8, per_sm = E <= 256 ? 2 : 3; };
 
-template <typename T, int L, int EPL, bool SIGMOID>
+template <typename T, int L, int EPL, bool SIGMOID, bool VEC>
 __global__ void __launch_bounds__(RouteWarps<L * EPL>::n * 32, RouteWarps<L * EPL>::per_sm)
-route_scored_kernel(const T* __restrict__ logits, const RouteParams p, int sum2, int vec) {
+route_scored_kernel(const T* __restrict__ logits, const RouteParams p, int sum2) {
   constexpr int ROWS = 32 / L, W = RouteWarps<L * EPL>::n;
   constexpr int KEYS = EPL * L + 32;
   // per warp: 32-bit keys of its rows for the groups, or 64-bit keys of a row that is decided again (never both at once)
@@ -295,14 +335,9 @@ route_scored_kernel(const T* __restrict__ logits, const RouteParams p, int sum2,
     const int t = t0 + lane / L;
     const bool there = t < p.T, on = there && (p.row_valid == nullptr || p.row_valid[t] != 0);
     const T* row = logits + (long long)(there ? t : t0) * p.stride;
+    float* row_s = reinterpret_cast<float*>(keys_s[warp]) + lane / L * KEYS;
     float z[EPL];                                                  // a row that is off has no candidate
-    if (on) {
-      load_row<T, EPL>(row, p.E, sl, vec != 0, z);
-    } else {
-#pragma unroll
-      for (int i = 0; i < EPL; ++i) z[i] = low;
-    }
-    __syncwarp();
+    load_row<T, L, EPL, VEC>(row, p.E, sl, on, row_s, z);
     float total = 1.f, zmax = 0.f;
     if (need_total) {
       float m = low;
@@ -334,9 +369,23 @@ route_scored_kernel(const T* __restrict__ logits, const RouteParams p, int sum2,
     }
     const float smax = SIGMOID ? 1.0f : inv_total;                 // no score is larger
     bool unsure = false;                                           // not settled in registers
-    auto group_error = [&](float reach) { return 2.f * (sum2 ? 2.f : 1.f) * (err_s * smax + err_0) + 6.f * err_c * reach; };
     if (grouped) {
       float margin, reach;
+      uint32_t stay = 0;
+      // The groups of the rows whose choice is within its error, in 64 bits (a few rows of a batch, but one of them holds up
+      // its block: deciding all of such a row in 64 bits took 12 us); other rows keep `as_is`.  Keys compared as they stand
+      // (logits) are exact.
+      auto redo_groups = [&](float margin_, float reach_, uint32_t as_is) {
+        const float error = 2.f * (sum2 ? 2.f : 1.f) * (err_s * smax + err_0) + 6.f * err_c * reach_;
+        for (uint32_t rows = __ballot_sync(kAll, (biased || sum2) && sl == 0 && margin_ <= error); rows != 0u; rows &= rows - 1u) {
+          const int src = __ffs(rows) - 1;
+          __syncwarp();
+          const uint32_t exact = groups_in_double<T, SIGMOID>(logits + (long long)(t0 + src / L) * p.stride, p, sum2, keys_s[warp], lane);
+          if (seg0 == src) as_is = exact;
+          __syncwarp();
+        }
+        return as_is;
+      };
       if (by_lanes) {
         float a = low, b = low;
 #pragma unroll
@@ -352,53 +401,25 @@ route_scored_kernel(const T* __restrict__ logits, const RouteParams p, int sum2,
         }
         bool stays = rank_groups<L, float>(group_value(a, b, sum2), fabsf(a) + (sum2 && b > low ? fabsf(b) : 0.f), sl / lanes_per,
                                            p.n_group, lanes_per, lane, p.topk_group, margin, reach);
-        // keys compared as they stand (logits) are exact; others are formed again in 64 bits where their order is in doubt
-        // (a few rows of a batch, but one of them holds up its block: the whole choice in 64 bits took 12 us)
-        if ((biased || sum2) && __any_sync(kAll, margin <= group_error(reach))) {
-          double da = low, db = low, top = zmax, sum = 1.0;
-          if (!SIGMOID) {
-            sum = 0.0;
-#pragma unroll
-            for (int i = 0; i < EPL; ++i)
-              if (z[i] > low) sum += z[i] == zmax ? 1.0 : exp((double)z[i] - top);
-#pragma unroll
-            for (int o = L / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(kAll, sum, o);
-          }
-#pragma unroll
-          for (int i = 0; i < EPL; ++i) {
-            if (c[i] > low) {
-              const double zd = z[i];
-              const double sc = SIGMOID ? 1.0 / (1.0 + exp(-zd)) : (z[i] == zmax ? 1.0 : exp(zd - top)) / sum;
-              push2(sc + (biased ? (double)bias_s[e0 + i] : 0.0), da, db);
-            }
-          }
-          for (int o = 1; o < lanes_per; o <<= 1) {
-            const double oa = __shfl_xor_sync(kAll, da, o), ob = __shfl_xor_sync(kAll, db, o);
-            push2(oa, da, db);
-            push2(ob, da, db);
-          }
-          double dm, dr;
-          stays = rank_groups<L, double>(group_value(da, db, sum2), 0.0, sl / lanes_per, p.n_group, lanes_per, lane, p.topk_group, dm, dr);
-        }
+        stay = redo_groups(margin, reach, 0u);
+        if (stay != 0u) stays = (stay >> (sl / lanes_per)) & 1u;
         if (!stays) {
 #pragma unroll
           for (int i = 0; i < EPL; ++i) c[i] = low;
         }
       } else {
-        float* key = reinterpret_cast<float*>(keys_s[warp]) + lane / L * KEYS;
         const int P = p.lanes_per_group;
+        const int g_first = e0 / p.group_size, r_first = e0 - g_first * p.group_size;
         __syncwarp();
-#pragma unroll
-        for (int i = 0; i < EPL; ++i) {
-          const int e = e0 + i;
-          if (e < p.E) key[e + e / p.group_size * P] = !biased && sum2 && c[i] > low ? score_key(z[i]) : c[i];
-        }
+        for_each_group<EPL>(g_first, r_first, p.group_size, [&](int i, int g) {
+          if (e0 + i < p.E) row_s[e0 + i + g * P] = !biased && sum2 && c[i] > low ? score_key(z[i]) : c[i];
+        });
         __syncwarp();
-        const uint32_t stay = choose_groups<L, float>(key, p.n_group, p.group_size, P, p.topk_group, sum2, lane, margin, reach);
-#pragma unroll
-        for (int i = 0; i < EPL; ++i)
-          if (e0 + i < p.E && !((stay >> ((e0 + i) / p.group_size)) & 1u)) c[i] = low;
-        if (biased || sum2) unsure = margin <= group_error(reach);
+        stay = choose_groups<L, float>(row_s, p.n_group, p.group_size, P, p.topk_group, sum2, lane, margin, reach);
+        stay = redo_groups(margin, reach, stay);
+        for_each_group<EPL>(g_first, r_first, p.group_size, [&](int i, int g) {
+          if (!((stay >> (g & 31)) & 1u)) c[i] = low;              // (past the last expert there is no candidate anyway)
+        });
       }
     }
     // k rounds: the largest packed key of the row goes to the next slot.  A lane holds its three best (0: none) and looks
@@ -534,9 +555,9 @@ route_scored_kernel(const T* __restrict__ logits, const RouteParams p, int sum2,
 // t_j = dw_j - sum_i p_i dw_i, softmax dz_j = scale p_j t_j and sigmoid dz_j = scale p_j (1 - s_j) t_j; without,
 // sigmoid dz_j = scale dw_j s_j (1 - s_j); all other logits zero.  Softmax without renormalisation reaches every
 // logit: dz_e = s_e (scale dw_e [e chosen] - scale sum_j dw_j s_j).  Bound by the store of the row.
-template <typename T, int EPL, bool SIGMOID>
+template <typename T, int EPL, bool SIGMOID, bool VEC>
 __global__ void __launch_bounds__(kRsWarps * 32)
-route_scored_backward_kernel(int Tn, int E, int k, int renorm, float scale, long long stride, int vec_in, int vec_out,
+route_scored_backward_kernel(int Tn, int E, int k, int renorm, float scale, long long stride,
                              const T* __restrict__ logits, const int32_t* __restrict__ topk_idx,
                              const float* __restrict__ dgates, T* __restrict__ dlogits, long long out_stride) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -580,7 +601,12 @@ route_scored_backward_kernel(int Tn, int E, int k, int renorm, float scale, long
       if (have) v = scale * dw * sigmoid_rn(zs) * (1.0f / (1.0f + expf(zs)));
     } else {
       float z[EPL];
-      load_row<T, EPL>(row, E, lane, vec_in != 0, z);
+      load_row<T, 32, EPL, VEC>(row, E, lane, true, add_s[warp], z);
+      if (EPL > 2 && !(VEC && EPL >= Vec<T>::N)) {                   // the row was turned through it
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) add_s[warp][i * 32 + lane] = 0.f;
+        __syncwarp();
+      }
       float m = low;
 #pragma unroll
       for (int i = 0; i < EPL; ++i) m = fmaxf(m, z[i]);
@@ -615,9 +641,10 @@ route_scored_backward_kernel(int Tn, int E, int k, int renorm, float scale, long
     for (int i = 0; i < EPL; ++i) dz[i] += add_s[warp][e0 + i];
     __syncwarp();
     if (have) add_s[warp][sel] = 0.f;
+    __syncwarp();
     T* out = dlogits + (long long)t * out_stride;
     constexpr int VN = Vec<T>::N;
-    if (EPL >= VN && vec_out) {
+    if (EPL >= VN && VEC) {
 #pragma unroll
       for (int i = 0; i + VN <= EPL; i += VN) {
         if (e0 + i < E) {
@@ -627,10 +654,23 @@ route_scored_backward_kernel(int Tn, int E, int k, int renorm, float scale, long
           *reinterpret_cast<uint4*>(out + e0 + i) = *reinterpret_cast<const uint4*>(q);
         }
       }
-    } else {
+    } else if (EPL <= 2) {
 #pragma unroll
       for (int i = 0; i < EPL; ++i)
         if (e0 + i < E) out[e0 + i] = from_f32<T>(dz[i]);
+    } else {
+      // neighbouring lanes write neighbouring gradients, turned through shared memory (cleared for the next row again)
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) add_s[warp][e0 + i] = dz[i];
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < EPL; ++i)
+        if (i * 32 + lane < E) out[i * 32 + lane] = from_f32<T>(add_s[warp][i * 32 + lane]);
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) add_s[warp][i * 32 + lane] = 0.f;
+      __syncwarp();
     }
   }
 }
@@ -668,7 +708,6 @@ __global__ void zero_counts_kernel(int E, int32_t* __restrict__ counts) {
 
 template <typename T, int L, int EPL>
 cudaError_t launch_route_t(const btx_route_desc* d, const void* logits, RouteParams p, cudaStream_t st) {
-  const int vec = row_vectors(logits, p.stride, p.E, sizeof(T)) ? 1 : 0;
   constexpr int W = RouteWarps<L * EPL>::n;
   int blocks = row_blocks(p.T, W * (32 / L), RouteWarps<L * EPL>::per_sm);
   // Counting: one block writes its own counts; more add theirs to zeros.  One block takes up to 16 rows on its own, which
@@ -682,9 +721,13 @@ cudaError_t launch_route_t(const btx_route_desc* d, const void* logits, RoutePar
   p.lanes_per_group = 1;
   while (2 * p.lanes_per_group * p.n_group <= L) p.lanes_per_group *= 2;
   const int sum2 = d->group_score == BTX_GROUP_SUM2;
-  return launch_after_predecessor(
-      d->score == BTX_SCORE_SIGMOID ? route_scored_kernel<T, L, EPL, true> : route_scored_kernel<T, L, EPL, false>, dim3(blocks),
-      dim3(W * 32), 0, st, true, (const T*)logits, p, sum2, vec);
+  auto kernel = route_scored_kernel<T, L, EPL, false, false>;
+  const bool sigmoid = d->score == BTX_SCORE_SIGMOID;
+  if (row_vectors(logits, p.stride, p.E, sizeof(T)))
+    kernel = sigmoid ? route_scored_kernel<T, L, EPL, true, true> : route_scored_kernel<T, L, EPL, false, true>;
+  else if (sigmoid)
+    kernel = route_scored_kernel<T, L, EPL, true, false>;
+  return launch_after_predecessor(kernel, dim3(blocks), dim3(W * 32), 0, st, true, (const T*)logits, p, sum2);
 }
 
 // Lanes of a row: enough for E experts at up to 16 each, for the k slots (one per lane) and for the groups.  Fewer lanes
@@ -708,11 +751,14 @@ cudaError_t launch_route(const btx_route_desc* d, const void* logits, const Rout
 template <typename T, int EPL>
 cudaError_t launch_route_backward_t(const btx_route_desc* d, const void* logits, long long stride, const int32_t* topk_idx,
                                     const float* dgates, void* dlogits, long long out_stride, cudaStream_t st) {
-  const int vi = row_vectors(logits, stride, d->E, sizeof(T)), vo = row_vectors(dlogits, out_stride, d->E, sizeof(T));
-  return launch_after_predecessor(
-      d->score == BTX_SCORE_SIGMOID ? route_scored_backward_kernel<T, EPL, true> : route_scored_backward_kernel<T, EPL, false>,
-      dim3(row_blocks(d->T, kRsWarps, 8)), dim3(kRsWarps * 32), 0, st, true, d->T, d->E, d->k, (int)(d->renorm != 0), d->scale, stride,
-      vi, vo, (const T*)logits, topk_idx, dgates, (T*)dlogits, out_stride);
+  auto kernel = route_scored_backward_kernel<T, EPL, false, false>;
+  const bool sigmoid = d->score == BTX_SCORE_SIGMOID;
+  if (row_vectors(logits, stride, d->E, sizeof(T)) && row_vectors(dlogits, out_stride, d->E, sizeof(T)))
+    kernel = sigmoid ? route_scored_backward_kernel<T, EPL, true, true> : route_scored_backward_kernel<T, EPL, false, true>;
+  else if (sigmoid)
+    kernel = route_scored_backward_kernel<T, EPL, true, false>;
+  return launch_after_predecessor(kernel, dim3(row_blocks(d->T, kRsWarps, 8)), dim3(kRsWarps * 32), 0, st, true, d->T, d->E, d->k,
+                                  (int)(d->renorm != 0), d->scale, stride, (const T*)logits, topk_idx, dgates, (T*)dlogits, out_stride);
 }
 
 // experts per lane: the power of two that covers E with 32 lanes
