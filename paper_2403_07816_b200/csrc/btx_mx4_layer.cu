@@ -53,7 +53,8 @@ struct LayerParams {
   Params up, down;
 };
 
-// Parts of the contraction of pass 2: as many CTAs as keep every one busy at most once, two stages each at least.
+// Parts of the contraction of pass 2: as many CTAs as keep every one busy at most once, two stages each at least.  Every
+// part has room for the rows of all R assignments, so a batch of mostly empty slots counts as many row tiles as R fills.
 __device__ __forceinline__ int parts_of(int tiles, int ctas, int kb) {
   int s = 1;
   while (s < 8 && 2 * s * tiles <= ctas && 4 * s <= kb) s *= 2;
@@ -141,7 +142,7 @@ mx4_layer_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
   const int n_stages = stage_count(a_rows, L_RING), s_bytes = stage_bytes(a_rows);
   const int tiles1 = m_tiles * p.up.n_tiles, tiles2 = m_tiles * p.down.n_tiles;
   const int kb1 = (p.up.K + SK - 1) / SK, kb2 = (p.down.K + SK - 1) / SK;
-  const int parts = parts_of(tiles2, ctas, kb2);
+  const int parts = parts_of(max(m_tiles, (p.R + kTileRows - 1) / kTileRows) * p.down.n_tiles, ctas, kb2);
 
   // The work items of a pass for this CTA: item i -> tile, stages [k0, k1), rows of the part.
   struct Work { Item it; int k0, k1, part; };
@@ -364,10 +365,12 @@ mx4_layer_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
 }  // namespace
 
 bool layer_fits(const Dispatch& q) {
-  return q.pad_tiles == 1 && q.R <= L_MAX_R && q.T <= 2 * sm_count() && q.m_tiles_max <= L_MAX_TILES;
+  return q.pad_tiles == 1 && q.R <= L_MAX_R && q.T <= 2 * sm_count() && q.m_tiles_max <= L_MAX_TILES &&
+         (long long)q.T * q.d < (1ll << 31);                // (vectors of y are numbered in 32 bits)
 }
 
-// Rows of all parts: s > 1 parts of t tiles (s * t at most the CTAs) hold at most s * t * 128 * 128 floats.
+// Rows of all parts: s > 1 parts of t tiles (s * t at most the CTAs, t at least what R rows of d fill) are at most
+// s * t * 128 * 128 floats.
 size_t layer_rows_floats(const Dispatch& q) {
   const size_t one = (size_t)q.R * q.d, split = (size_t)sm_count() * kTileRows * BN;
   const size_t most = one > split ? one : split;

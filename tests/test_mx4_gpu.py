@@ -290,6 +290,24 @@ def test_expert_layer_empty_slots_only_and_out_of_range():
     assert float((both - one).abs().max()) <= 2.0 ** -21 * float(one.abs().max())
 
 
+def test_padded_batch_of_few_tokens_leaves_the_workspace():
+    # the few tokens' tiles alone would let every part of the contraction have rows of its own, more than there is room for
+    T, d, F, E, k = 128, 1024, 2048, 8, 8
+    x = randn(T, d, seed=3, dtype=torch.bfloat16)
+    w1, w3, w2 = (randn(E, *s, seed=i, std=0.05) for i, s in enumerate([(F, d), (F, d), (d, F)]))
+    idx, gates = random_routing(T, E, k, 11)
+    for kept in ([0, 127], [64]):
+        few = torch.full_like(idx, -1)
+        few[kept, :2] = 5
+        y, _ = moe(x, few, gates, w1, w3, w2)             # (looks at the guards around the workspace)
+        off = torch.ones(T, dtype=torch.bool)
+        off[kept] = False
+        assert bool((y[off.to(DEV)] == 0).all())
+        one = np.where(few.cpu().numpy()[kept] == 5, 0, -1)
+        want, tol = moe_reference(np64(x)[kept], one, np64(gates)[kept], np64(w1[5:6]), np64(w3[5:6]), np64(w2[5:6]))
+        assert (np.abs(np64(y)[kept] - want) <= tol + 2.0 ** -8 * np.abs(want)).all()
+
+
 def test_layer_is_the_same_whatever_shares_its_batch():
     # a row's result does not depend on the rows around it (tiles of 128, one or several dispatch blocks)
     T, d, F, E, k = 3000, 96, 160, 5, 2
