@@ -231,6 +231,7 @@ extern "C" btx_status btx_moe_forward(const btx_moe_desc* desc, const void* x, c
   if (s != BTX_OK) return s;
   if (!x || (!w_router && !pl.given) || !w1 || !w3 || !w2 || !y || !workspace) return BTX_ERR_INVALID_ARG;
   if (pl.given && (!routing || !routing->topk_idx || !routing->gates)) return BTX_ERR_INVALID_ARG;
+  if (pl.given && (((uintptr_t)routing->topk_idx | (uintptr_t)routing->gates) & 3)) return BTX_ERR_INVALID_ARG;
   if (desc->save_for_backward && !saved) return BTX_ERR_INVALID_ARG;
   if (desc->routing == BTX_ROUTE_SAMPLE1 && !router_noise) return BTX_ERR_INVALID_ARG;
   const EffectiveRouting er = effective_routing(desc);

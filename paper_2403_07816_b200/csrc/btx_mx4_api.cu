@@ -6,6 +6,7 @@ namespace mx4 {
 namespace {
 
 constexpr long long kMaxItems = 1ll << 30;           // output tiles of a product are numbered in 32 bits
+constexpr int kMaxSide = 1 << 30;                    // so are rows and columns, and the ends of the tiles past the last one
 
 size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
@@ -13,7 +14,7 @@ long long row_tiles(long long rows) { return (rows + kTileRows - 1) / kTileRows;
 
 btx_status check_shape(int batch, int rows, int K) {
   if (batch < 0 || rows < 0 || K < 1) return BTX_ERR_INVALID_ARG;
-  if (K % kBlock != 0) return BTX_ERR_UNSUPPORTED;
+  if (K % kBlock != 0 || rows > kMaxSide || K > kMaxSide) return BTX_ERR_UNSUPPORTED;
   return BTX_OK;
 }
 
@@ -27,7 +28,8 @@ btx_status make_moe_plan(const btx_mx4_moe_desc* d, MoePlan* pl) {
   if (!d || !pl) return BTX_ERR_INVALID_ARG;
   if (d->T < 0 || d->d_model < 1 || d->d_ff < 1 || d->E < 1 || d->k < 1 || d->k > d->E) return BTX_ERR_INVALID_ARG;
   if (d->dtype != BTX_F32 && d->dtype != BTX_BF16) return BTX_ERR_INVALID_ARG;
-  if (d->E > kMaxExperts4 || d->d_model % kBlock || d->d_ff % kBlock || d->d_ff > (1 << 29)) return BTX_ERR_UNSUPPORTED;
+  if (d->E > kMaxExperts4 || d->d_model % kBlock || d->d_ff % kBlock || d->d_model > kMaxSide || d->d_ff > kMaxSide / 2)
+    return BTX_ERR_UNSUPPORTED;
   const long long R = (long long)d->T * d->k;
   if (R > (1ll << 28)) return BTX_ERR_UNSUPPORTED;
   const long long used = R < d->E ? R : d->E;        // experts that can hold a row
@@ -68,7 +70,7 @@ btx_status check_matmul(int dtype, int batch, int M, int N, int K) {
   if (batch < 0 || M < 0 || N < 1) return BTX_ERR_INVALID_ARG;
   btx_status s = check_shape(batch, M, K);
   if (s != BTX_OK) return s;
-  if (row_tiles(M) * row_tiles(N) > kMaxItems || row_tiles(M) * row_tiles(N) * batch > kMaxItems) return BTX_ERR_UNSUPPORTED;
+  if (N > kMaxSide || row_tiles(M) * row_tiles(N) > kMaxItems || row_tiles(M) * row_tiles(N) * batch > kMaxItems) return BTX_ERR_UNSUPPORTED;
   return BTX_OK;
 }
 
@@ -94,6 +96,7 @@ extern "C" btx_status btx_mx4_quantize(int32_t dtype, const void* src, int64_t r
   if (s != BTX_OK) return s;
   if (dtype != BTX_F32 && dtype != BTX_BF16) return BTX_ERR_INVALID_ARG;
   if (row_first < 0 || row_step < 1 || out_rows < 0) return BTX_ERR_INVALID_ARG;
+  if (out_rows > kMaxSide) return BTX_ERR_UNSUPPORTED;
   if (rows > 0 && (long long)row_first + (long long)(rows - 1) * row_step >= out_rows) return BTX_ERR_INVALID_ARG;
   if (batch == 0 || rows == 0) return BTX_OK;
   if (!src || !codes || !scales) return BTX_ERR_INVALID_ARG;

@@ -126,6 +126,21 @@ def test_mx4_and_given_refusals(L):
     assert L.btx_moe_step_host(C.byref(d), *([A] * 15), 1.0, *([A] * 5), 0, A, A, 1 << 40, None, None) == 2
 
 
+def test_sizes_past_32_bit_arithmetic_are_refused(L):
+    sz, big = C.c_size_t(0), (1 << 31) - 32
+    assert L.btx_mx4_sizes(1, 1, 1 << 30, C.byref(sz), None) == 0 and sz.value == 1 << 29
+    assert L.btx_mx4_sizes(1, 1, big, C.byref(sz), None) == 2
+    assert L.btx_mx4_sizes(1, big, 32, C.byref(sz), None) == 2
+    assert L.btx_mx4_quantize(0, A, 32, 32, 1, 1, 32, big, 0, 1, A, A, None) == 2
+    for M, N, K in ((big, 1, 32), (1, big, 32), (1, 1, big)):
+        assert L.btx_mx4_matmul(0, 1, M, N, K, A, A, A, A, A, A, 256, None) == 2
+    for d, f in ((big, 32), (32, 1 << 30)):
+        assert L.btx_mx4_moe_workspace_size(C.byref(B.make_mx4_moe_desc(1, d, f, 1, 1, torch.float32)), C.byref(sz)) == 2
+    r = B.RoutingOut(topk_idx=4098, gates=4096)
+    d = B.make_desc(8, 64, 64, 4, 2, torch.float32, B.ROUTE_GIVEN, 0.0)
+    assert L.btx_moe_forward(C.byref(d), A, None, None, None, A, A, A, A, C.byref(r), None, A, 1 << 40, None) == 1
+
+
 def test_statement_mx4_against_the_format():
     """The statement's cast: nearest value of the grid, ties to the even code, saturation, scale of the block."""
     x = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.9] + [0.0] * 24)
