@@ -3,7 +3,7 @@
 //   quantize     per 32 elements: scale 2^(floor(log2 max|x|) - 2), elements to the nearest e2m1 value (ties to the
 //                even code, at most 6).  Four lanes share a block, eight elements each: a warp reads 256 consecutive
 //                elements with 16-byte loads, the maximum takes two shuffles, a lane stores four bytes of codes and
-//                every fourth the scale byte.  Bound by memory: 2 + 17/32 bytes per bf16 element.
+//                every fourth the scale byte.  Bound by memory: 2 + 17/32 bytes per bf16 element, 6.0 TB/s for large matrices.
 //   dequantize   the same mapping backwards
 //   dispatch     stable counting sort of the assignments by expert, padded to 128-row tiles
 //   quantize_rows  quantize of x with every row written to the k rows of its token: x is read once
@@ -323,8 +323,10 @@ combine_rows_kernel(int Tn, int d, int k, int splits, const float* __restrict__ 
   }
 }
 
+// More blocks than fit at once: with 32 for every multiprocessor the cast of four 11008 x 4096 matrices (bf16) takes 76 us
+// and the way back 74, with 8 86 and 86 (all blocks walk through memory in step), with 64 78 and 76.
 int cast_blocks(long long items) {
-  const long long want = (items + kCastThreads / 32 - 1) / (kCastThreads / 32), most = 8ll * sm_count();
+  const long long want = (items + kCastThreads / 32 - 1) / (kCastThreads / 32), most = 32ll * sm_count();
   return (int)(want < most ? want : most);
 }
 int cast_groups(int K) { return (K + 256 * kCastUnroll - 1) / (256 * kCastUnroll); }
