@@ -49,11 +49,11 @@ E2E_STEPS = 50
 # step at T=16384, from the one-pass ncu capture summarised in profiles/tc_gemm_kernel_fwd_bwd_T16384_dram.txt
 # (the traffic does not grow in proportion to T, so the T=4096 capture is not scaled).  The figure belongs to the
 # kernel sources whose hash is recorded with it; with any other sources the bench reports traffic = null.
-TC_GEMM_TRAFFIC = {"bytes_per_step_T16384": 33.68e9, "sources_sha256_16": "4b5584b3b2e0e287"}
+TC_GEMM_TRAFFIC = {"bytes_per_step_T16384": 36.54e9, "sources_sha256_16": "61f65534dad2e7eb"}
 TC_GEMM_SOURCES = ("btx_gemm_tc.cu", "btx_tc_ptx.cuh", "btx_common.cuh")
 # The same for one launch (one layer) of the one-kernel decode-shaped forward, from the capture summarised in
-# profiles/tc_small_forward_kernel_decode_T32_full.txt (1.0864 GB read + 0.0070 GB written).
-SMALL_FWD_TRAFFIC = {"bytes_per_layer_T32": 1.0934e9, "sources_sha256_16": "59f3acb607798dbb"}
+# profiles/tc_small_forward_kernel_decode_T32_full.txt (1.0864 GB read + 0.0052 GB written, mean of two launches).
+SMALL_FWD_TRAFFIC = {"bytes_per_layer_T32": 1.0916e9, "sources_sha256_16": "031cd7ec9517d630"}
 SMALL_FWD_SOURCES = ("btx_gemm_fused.cu", "btx_tc_ptx.cuh", "btx_route_dev.cuh", "btx_common.cuh")
 FALLBACK_PEAKS = {"hbm_gbs": 6650.0, "bf16_tflops": 1590.0, "bf16_tflops_sustained": 1400.0}
 
