@@ -106,12 +106,12 @@ def route_backward(z, idx, dgates, score, renorm=True, scale=1.0):
             v = p * (dw - (p * dw).sum())
             if score == SIGMOID:
                 v = v * _sigmoid(-z[t][sel])
-            dz[t, sel] += v
+            np.add.at(dz[t], sel, v)
         elif score == SIGMOID:
-            dz[t, sel] += dw * s[sel] * _sigmoid(-z[t][sel])
+            np.add.at(dz[t], sel, dw * s[sel] * _sigmoid(-z[t][sel]))
         else:
             ds = np.zeros(E)
-            ds[sel] = dw
+            np.add.at(ds, sel, dw)
             dz[t] = s * (ds - (s * ds).sum())
     return dz
 

@@ -13,8 +13,6 @@
 // rounds and by latency, not by memory.
 #include <math_constants.h>
 
-#include <type_traits>
-
 #include "btx_route_dev.cuh"
 
 namespace btx {
@@ -555,13 +553,16 @@ route_scored_kernel(const T* __restrict__ logits, const RouteParams p, int sum2)
 // t_j = dw_j - sum_i p_i dw_i, softmax dz_j = scale p_j t_j and sigmoid dz_j = scale p_j (1 - s_j) t_j; without,
 // sigmoid dz_j = scale dw_j s_j (1 - s_j); all other logits zero.  Softmax without renormalisation reaches every
 // logit: dz_e = s_e (scale dw_e [e chosen] - scale sum_j dw_j s_j).  Bound by the store of the row.
+// A warp per row.  Neighbouring lanes hold neighbouring experts, by the vector (VEC: rows start on 16-byte boundaries and
+// hold whole vectors) or one by one, so that every load and store of the warp is contiguous: 8 experts in a row per lane,
+// as in the choice above, took 9.0 instead of 7.9 us for T = 16384, E = 256, k = 8 (softmax, not renormalised).
 template <typename T, int EPL, bool SIGMOID, bool VEC>
 __global__ void __launch_bounds__(kRsWarps * 32)
 route_scored_backward_kernel(int Tn, int E, int k, int renorm, float scale, long long stride,
                              const T* __restrict__ logits, const int32_t* __restrict__ topk_idx,
                              const float* __restrict__ dgates, T* __restrict__ dlogits, long long out_stride) {
+  constexpr int VN = VEC && EPL >= Vec<T>::N ? Vec<T>::N : 1;        // experts side by side in a lane
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int e0 = lane * EPL;
   const float low = -CUDART_INF_F;
   __shared__ __align__(16) float add_s[kRsWarps][EPL * 32];
 #pragma unroll
@@ -600,26 +601,34 @@ route_scored_backward_kernel(int Tn, int E, int k, int renorm, float scale, long
     } else if (SIGMOID) {
       if (have) v = scale * dw * sigmoid_rn(zs) * (1.0f / (1.0f + expf(zs)));
     } else {
-      float z[EPL];
-      load_row<T, 32, EPL, VEC>(row, E, lane, true, add_s[warp], z);
-      if (EPL > 2 && !(VEC && EPL >= Vec<T>::N)) {                   // the row was turned through it
+      float z[EPL], m = low;
 #pragma unroll
-        for (int i = 0; i < EPL; ++i) add_s[warp][i * 32 + lane] = 0.f;
-        __syncwarp();
+      for (int i = 0; i < EPL; i += VN) {
+        const int e = i * 32 + lane * VN;
+        float q[VN];
+        if constexpr (VN > 1) {
+          if (e < E) Vec<T>::load(row + e, q);
+        } else {
+          if (e < E) q[0] = to_f32(row[e]);
+        }
+#pragma unroll
+        for (int j = 0; j < VN; ++j) {
+          z[i + j] = e < E ? fmaxf(q[j], low) : low;                 // NaN: no candidate
+          m = fmaxf(m, z[i + j]);
+        }
       }
-      float m = low;
-#pragma unroll
-      for (int i = 0; i < EPL; ++i) m = fmaxf(m, z[i]);
       m = row_max<32>(m);
+      const float shift = fabsf(m) < CUDART_INF_F ? m : 0.f;         // (-inf: nothing is on)
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < EPL; ++i) {
-        dz[i] = z[i] > low ? exp_below(z[i], m) : 0.f;
+        dz[i] = m < CUDART_INF_F ? expf(z[i] - shift) : z[i] == m ? 1.f : 0.f;
         sum += dz[i];
       }
       sum = row_sum<32>(sum);
       const float s = have && sum > 0.f ? exp_below(zs, m) / sum : 0.f;
-      const float factor = sum > 0.f ? -scale * row_sum<32>(s * dw) / sum : 0.f;
+      const float inner = row_sum<32>(s * dw);
+      const float factor = sum > 0.f ? -scale * inner / sum : 0.f;
 #pragma unroll
       for (int i = 0; i < EPL; ++i) dz[i] *= factor;
       v = scale * s * dw;
@@ -638,39 +647,23 @@ route_scored_backward_kernel(int Tn, int E, int k, int renorm, float scale, long
     if (have) add_s[warp][sel] = v;
     __syncwarp();
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) dz[i] += add_s[warp][e0 + i];
+    for (int i = 0; i < EPL; ++i) dz[i] += add_s[warp][i / VN * VN * 32 + lane * VN + i % VN];
     __syncwarp();
     if (have) add_s[warp][sel] = 0.f;
     __syncwarp();
     T* out = dlogits + (long long)t * out_stride;
-    constexpr int VN = Vec<T>::N;
-    if (EPL >= VN && VEC) {
 #pragma unroll
-      for (int i = 0; i + VN <= EPL; i += VN) {
-        if (e0 + i < E) {
-          __align__(16) T q[VN];
+    for (int i = 0; i < EPL; i += VN) {
+      const int e = i * 32 + lane * VN;
+      if (e >= E) continue;
+      if constexpr (VN > 1) {
+        __align__(16) T q[VN];
 #pragma unroll
-          for (int j = 0; j < VN; ++j) q[j] = from_f32<T>(dz[(i + j) % EPL]);
-          *reinterpret_cast<uint4*>(out + e0 + i) = *reinterpret_cast<const uint4*>(q);
-        }
+        for (int j = 0; j < VN; ++j) q[j] = from_f32<T>(dz[i + j]);
+        *reinterpret_cast<uint4*>(out + e) = *reinterpret_cast<const uint4*>(q);
+      } else {
+        out[e] = from_f32<T>(dz[i]);
       }
-    } else if (EPL <= 2) {
-#pragma unroll
-      for (int i = 0; i < EPL; ++i)
-        if (e0 + i < E) out[e0 + i] = from_f32<T>(dz[i]);
-    } else {
-      // neighbouring lanes write neighbouring gradients, turned through shared memory (cleared for the next row again)
-      __syncwarp();
-#pragma unroll
-      for (int i = 0; i < EPL; ++i) add_s[warp][e0 + i] = dz[i];
-      __syncwarp();
-#pragma unroll
-      for (int i = 0; i < EPL; ++i)
-        if (i * 32 + lane < E) out[i * 32 + lane] = from_f32<T>(add_s[warp][i * 32 + lane]);
-      __syncwarp();
-#pragma unroll
-      for (int i = 0; i < EPL; ++i) add_s[warp][i * 32 + lane] = 0.f;
-      __syncwarp();
     }
   }
 }
@@ -749,26 +742,26 @@ cudaError_t launch_route(const btx_route_desc* d, const void* logits, const Rout
 }
 
 template <typename T, int EPL>
-cudaError_t launch_route_backward_t(const btx_route_desc* d, const void* logits, long long stride, const int32_t* topk_idx,
-                                    const float* dgates, void* dlogits, long long out_stride, cudaStream_t st) {
+cudaError_t launch_backward_t(const btx_route_desc* d, const void* logits, long long stride, const int32_t* topk_idx,
+                              const float* dgates, void* dlogits, long long out_stride, cudaStream_t st) {
   auto kernel = route_scored_backward_kernel<T, EPL, false, false>;
   const bool sigmoid = d->score == BTX_SCORE_SIGMOID;
   if (row_vectors(logits, stride, d->E, sizeof(T)) && row_vectors(dlogits, out_stride, d->E, sizeof(T)))
     kernel = sigmoid ? route_scored_backward_kernel<T, EPL, true, true> : route_scored_backward_kernel<T, EPL, false, true>;
   else if (sigmoid)
     kernel = route_scored_backward_kernel<T, EPL, true, false>;
-  return launch_after_predecessor(kernel, dim3(row_blocks(d->T, kRsWarps, 8)), dim3(kRsWarps * 32), 0, st, true, d->T, d->E, d->k,
+  return launch_after_predecessor(kernel, dim3(row_blocks(d->T, kRsWarps, 16)), dim3(kRsWarps * 32), 0, st, true, d->T, d->E, d->k,
                                   (int)(d->renorm != 0), d->scale, stride, (const T*)logits, topk_idx, dgates, (T*)dlogits, out_stride);
 }
 
 // experts per lane: the power of two that covers E with 32 lanes
-template <typename T, typename F>
-cudaError_t by_width(int E, F&& f) {
-  if (E <= 32) return f(std::integral_constant<int, 1>());
-  if (E <= 64) return f(std::integral_constant<int, 2>());
-  if (E <= 128) return f(std::integral_constant<int, 4>());
-  if (E <= 256) return f(std::integral_constant<int, 8>());
-  return f(std::integral_constant<int, 16>());
+template <typename T, typename... Args>
+cudaError_t launch_backward(const btx_route_desc* d, Args... args) {
+  if (d->E <= 32) return launch_backward_t<T, 1>(d, args...);
+  if (d->E <= 64) return launch_backward_t<T, 2>(d, args...);
+  if (d->E <= 128) return launch_backward_t<T, 4>(d, args...);
+  if (d->E <= 256) return launch_backward_t<T, 8>(d, args...);
+  return launch_backward_t<T, 16>(d, args...);
 }
 
 }  // namespace
@@ -815,9 +808,7 @@ extern "C" btx_status btx_route_backward(const btx_route_desc* desc, const void*
   if ((s = check_device()) != BTX_OK) return s;
   cudaStream_t st = (cudaStream_t)stream;
   const cudaError_t e = desc->dtype == BTX_BF16
-      ? by_width<__nv_bfloat16>(desc->E, [&](auto w) {
-          return launch_route_backward_t<__nv_bfloat16, w.value>(desc, logits, logits_stride, topk_idx, dgates, dlogits, dlogits_stride, st); })
-      : by_width<float>(desc->E, [&](auto w) {
-          return launch_route_backward_t<float, w.value>(desc, logits, logits_stride, topk_idx, dgates, dlogits, dlogits_stride, st); });
+      ? launch_backward<__nv_bfloat16>(desc, logits, logits_stride, topk_idx, dgates, dlogits, dlogits_stride, st)
+      : launch_backward<float>(desc, logits, logits_stride, topk_idx, dgates, dlogits, dlogits_stride, st);
   return e == cudaSuccess ? BTX_OK : BTX_ERR_CUDA;
 }

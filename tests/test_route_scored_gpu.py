@@ -248,6 +248,39 @@ def test_large_batches_share_a_warp_between_rows(shape, score, dtype):
             assert torch.equal(got["counts"].long(), torch.bincount(flat[flat >= 0], minlength=E))
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("score,renorm", [(0, True), (0, False), (1, True), (1, False)])
+@pytest.mark.parametrize("shape", [(40, 8), (63, 3), (64, 8), (65, 2), (100, 16), (128, 9), (165, 7), (256, 8), (256, 16), (200, 20)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_gradient_of_large_batches(shape, score, renorm, dtype):
+    # several rows per warp: masked rows, rows without a choice, the same expert twice
+    E, k = shape
+    T = 8201
+    z, _ = logits_of(T, E, dtype, 2 * E + k)
+    z[17:5000:19, ::3] = float("-inf")
+    z[23:5000:29, ::5] = float("nan")
+    _, got = run(z, k, score, None, scores=False, renorm=renorm)
+    idx = got["topk_idx"].clone()
+    idx[3::13] = -1
+    idx[5::7, 0] = E
+    idx[6::5, 1] = idx[6::5, 0]
+    dw = torch.randn(T, k, generator=torch.Generator().manual_seed(9)).to(DEV)
+    mk = lambda n: B.make_route_desc(n, E, k, dtype, score, renorm=renorm, scale=1.75)
+    out = Guarded((T, E), dtype, DEV)
+    B.btx_route_backward(mk(T), z, idx, dw, out.t)
+    check_guards({"dlogits": out}, "btx_route_backward")
+    rows = np.r_[0:60, 2000:2040, T - 30:T]
+    z64 = z[rows].double().cpu().numpy()
+    want = o.route_backward(z64, idx.cpu().numpy()[rows], dw.cpu().numpy()[rows], score, renorm, 1.75)
+    atol = 2 * REL * 1.75 * float(dw.abs().max()) * 2          # the same expert in two slots adds two weights
+    err = np.abs(out.t.double().cpu().numpy()[rows] - want)
+    assert (err <= atol + torch.finfo(dtype).eps / 2 * np.abs(want)).all(), err.max()
+    # a batch below the limit runs a warp per row: the same gradient
+    part = torch.empty(4000, E, dtype=dtype, device=DEV)
+    B.btx_route_backward(mk(4000), z[:4000].contiguous(), idx[:4000].contiguous(), dw[:4000].contiguous(), part)
+    assert torch.equal(part, out.t[:4000])
+
+
 def test_binding_refuses_wrong_tensors():
     z = torch.randn(4, 16, device=DEV)
     desc = B.make_route_desc(4, 16, 2, torch.float32)
