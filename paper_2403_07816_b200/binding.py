@@ -404,6 +404,7 @@ def _launch(name, dev, *args):
 
 
 _DTYPE = {BTX_F32: torch.float32, BTX_BF16: torch.bfloat16}
+_U8, _I32, _F32 = torch.uint8, torch.int32, torch.float32
 
 
 def make_route_desc(T, E, k, dtype, score=SCORE_SOFTMAX, n_group=1, topk_group=1, group_score=GROUP_MAX, renorm=True,
@@ -418,10 +419,10 @@ def btx_route(desc, logits, bias, topk_idx, gates, scores=None, counts=None, row
     rows, stride = _rows(logits, "logits", (T, E), _DTYPE.get(desc.dtype), dev)
     if row_valid is not None and row_valid.dtype is torch.bool:
         row_valid = row_valid.view(torch.uint8)
-    _launch("btx_route", dev, C.byref(desc), rows, stride, _opt(bias, "bias", (E,), torch.float32, dev),
-            _opt(row_valid, "row_valid", (T,), torch.uint8, dev), _arg(topk_idx, "topk_idx", (T, k), torch.int32, dev),
-            _arg(gates, "gates", (T, k), torch.float32, dev), _opt(scores, "scores", (T, E), torch.float32, dev),
-            _opt(counts, "counts", (E,), torch.int32, dev))
+    _launch("btx_route", dev, C.byref(desc), rows, stride, _opt(bias, "bias", (E,), _F32, dev),
+            _opt(row_valid, "row_valid", (T,), _U8, dev), _arg(topk_idx, "topk_idx", (T, k), _I32, dev),
+            _arg(gates, "gates", (T, k), _F32, dev), _opt(scores, "scores", (T, E), _F32, dev),
+            _opt(counts, "counts", (E,), _I32, dev))
 
 
 def btx_route_backward(desc, logits, topk_idx, dgates, dlogits):
@@ -429,8 +430,8 @@ def btx_route_backward(desc, logits, topk_idx, dgates, dlogits):
     T, E, k, dev = desc.T, desc.E, desc.k, _device(logits)
     rows, stride = _rows(logits, "logits", (T, E), _DTYPE.get(desc.dtype), dev)
     out, out_stride = _rows(dlogits, "dlogits", (T, E), _DTYPE.get(desc.dtype), dev)
-    _launch("btx_route_backward", dev, C.byref(desc), rows, stride, _arg(topk_idx, "topk_idx", (T, k), torch.int32, dev),
-            _arg(dgates, "dgates", (T, k), torch.float32, dev), out, out_stride)
+    _launch("btx_route_backward", dev, C.byref(desc), rows, stride, _arg(topk_idx, "topk_idx", (T, k), _I32, dev),
+            _arg(dgates, "dgates", (T, k), _F32, dev), out, out_stride)
 
 
 @dataclass
@@ -442,8 +443,8 @@ class Mx4:
     @staticmethod
     def empty(batch, rows, K, device):
         btx_mx4_sizes(batch, rows, K)
-        return Mx4(torch.empty((batch, rows, K // 2), dtype=torch.uint8, device=device),
-                   torch.empty((batch, (rows + 127) // 128, (K + 127) // 128, 512), dtype=torch.uint8, device=device))
+        return Mx4(torch.empty((batch, rows, K // 2), dtype=_U8, device=device),
+                   torch.empty((batch, (rows + 127) // 128, (K + 127) // 128, 512), dtype=_U8, device=device))
 
     @property
     def shape(self):
@@ -452,16 +453,22 @@ class Mx4:
 
 
 def _mx4(q, name, dev):
-    """Shape and addresses of an Mx4 argument."""
+    """Shape (batch, rows, K) and addresses of an Mx4 argument."""
     codes, scales = q.codes, q.scales
     batch, rows, half = codes.shape
-    return ((batch, rows, 2 * half), _arg(codes, name + ".codes", (batch, rows, half), torch.uint8, dev),
-            _arg(scales, name + ".scales", (batch, (rows + 127) // 128, (half + 63) // 64, 512), torch.uint8, dev))
+    if (codes.dtype is not _U8 or codes.get_device() != dev or not codes.is_contiguous() or scales.dtype is not _U8
+            or scales.get_device() != dev or not scales.is_contiguous()
+            or scales.shape != (batch, (rows + 127) // 128, (half + 63) // 64, 512)):
+        _arg(codes, name + ".codes", (batch, rows, half), _U8, dev)
+        _arg(scales, name + ".scales", (batch, (rows + 127) // 128, (half + 63) // 64, 512), _U8, dev)
+    return batch, rows, 2 * half, codes.data_ptr(), scales.data_ptr()
 
 
 def _workspace(ws, dev):
     n = ws.numel()
-    return _arg(ws, "workspace", (n,), torch.uint8, dev), n
+    if ws.dtype is not _U8 or ws.dim() != 1 or ws.get_device() != dev or not ws.is_contiguous():
+        _bad(ws, "workspace", (n,), _U8, dev)
+    return ws.data_ptr(), n
 
 
 def btx_mx4_sizes(batch, rows, K):
@@ -477,13 +484,14 @@ def btx_mx4_quantize(src, out, row_first=0, row_step=1):
     """src [batch, rows, K] or [rows, K] (contiguous rows, any row and batch stride) cast into the Mx4 `out`; row r
     becomes row row_first + r * row_step."""
     dev = _device(src)
-    if src.dim() == 2:
-        (rows, K), (row_stride, col), batch, batch_stride = src.shape, src.stride(), 1, 0
+    shape, stride = src.shape, src.stride()
+    if len(shape) == 2:
+        (rows, K), (row_stride, col), batch, batch_stride = shape, stride, 1, 0
     else:
-        (batch, rows, K), (batch_stride, row_stride, col) = src.shape, src.stride()
-    (ob, out_rows, oK), codes, scales = _mx4(out, "out", dev)
+        (batch, rows, K), (batch_stride, row_stride, col) = shape, stride
+    ob, out_rows, oK, codes, scales = _mx4(out, "out", dev)
     if ob != batch or oK != K:
-        raise ValueError(f"btx: src is {tuple(src.shape)}, out is {out.shape}")
+        raise ValueError(f"btx: src is {tuple(shape)}, out is {out.shape}")
     if col != 1 and K > 1:
         raise RuntimeError("btx: the rows of src must be contiguous")
     _launch("btx_mx4_quantize", dev, _dtype_code(src.dtype), src.data_ptr(), row_stride, batch_stride, batch, rows, K, out_rows,
@@ -493,7 +501,7 @@ def btx_mx4_quantize(src, out, row_first=0, row_step=1):
 def btx_mx4_dequantize(q, dst):
     """The values of the Mx4 `q` into dst (contiguous, [batch, rows, K] or [rows, K] for one matrix)."""
     dev = _device(dst)
-    (batch, rows, K), codes, scales = _mx4(q, "q", dev)
+    batch, rows, K, codes, scales = _mx4(q, "q", dev)
     shape = (rows, K) if batch == 1 and dst.dim() == 2 else (batch, rows, K)
     _launch("btx_mx4_dequantize", dev, _dtype_code(dst.dtype), codes, scales, batch, rows, K, _arg(dst, "dst", shape, dst.dtype, dev))
 
@@ -509,8 +517,8 @@ def btx_mx4_matmul_workspace_size(M, N, K, dtype, batch=1):
 def btx_mx4_matmul(a, b, y, workspace):
     """y = a b^T of two Mx4 of the same batch and K; y is [batch, M, N], or [M, N] for one matrix."""
     dev = _device(y)
-    (batch, M, K), ac, asc = _mx4(a, "a", dev)
-    (bb, N, bK), bc, bsc = _mx4(b, "b", dev)
+    batch, M, K, ac, asc = _mx4(a, "a", dev)
+    bb, N, bK, bc, bsc = _mx4(b, "b", dev)
     if bb != batch or bK != K:
         raise ValueError(f"btx: a is {a.shape}, b is {b.shape}")
     shape = (M, N) if batch == 1 and y.dim() == 2 else (batch, M, N)
@@ -535,13 +543,13 @@ def btx_mx4_moe_forward(desc, x, topk_idx, gates, w13, w2, y, workspace):
     """The expert layer on MXFP4 experts under a given routing; w13 holds the rows of W1 and W3 in turn; see btx.h."""
     T, d, F, E, k, dev = desc.T, desc.d_model, desc.d_ff, desc.E, desc.k, _device(x)
     dt = _DTYPE.get(desc.dtype)
-    s13, c13, sc13 = _mx4(w13, "w13", dev)
-    s2, c2, sc2 = _mx4(w2, "w2", dev)
-    if s13 != (E, 2 * F, d) or s2 != (E, d, F):
-        raise ValueError(f"btx: w13 is {s13}, w2 is {s2}; the layer has E, d_ff, d_model = {E}, {F}, {d}")
+    *s13, c13, sc13 = _mx4(w13, "w13", dev)
+    *s2, c2, sc2 = _mx4(w2, "w2", dev)
+    if s13 != [E, 2 * F, d] or s2 != [E, d, F]:
+        raise ValueError(f"btx: w13 is {w13.shape}, w2 is {w2.shape}; the layer has E, d_ff, d_model = {E}, {F}, {d}")
     ws, ws_bytes = _workspace(workspace, dev)
     _launch("btx_mx4_moe_forward", dev, C.byref(desc), _arg(x, "x", (T, d), dt, dev),
-            _arg(topk_idx, "topk_idx", (T, k), torch.int32, dev), _arg(gates, "gates", (T, k), torch.float32, dev), c13, sc13, c2, sc2,
+            _arg(topk_idx, "topk_idx", (T, k), _I32, dev), _arg(gates, "gates", (T, k), _F32, dev), c13, sc13, c2, sc2,
             _arg(y, "y", (T, d), dt, dev), ws, ws_bytes)
 
 
