@@ -124,6 +124,26 @@ def test_agrees_with_the_layers_own_router(dtype):
             assert torch.equal(got[n], ref[n])
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T", [60, 900])
+def test_rows_without_an_expert_are_not_read(T, dtype):
+    # padding tokens may hold anything: it reaches no output and no gradient
+    inp = synth.moe_inputs(T, 64, 96, 4, 7, dtype, DEV)
+    idx, gates = routing(T, 4, 2, T, "all")
+    idx[1::5] = -1
+    idx[2, 1] = 9
+    clean = run(inp, idx, gates)
+    clean = {n: clean[n].clone() for n in ("y", "dx", "dgates", "dw1", "dw3", "dw2")}
+    inp["x"][1::5] = float("nan")
+    inp["dy"][1::5] = float("inf")
+    gates[1::5] = float("nan")
+    gates[2, 1] = float("inf")
+    got = run(inp, idx, gates)
+    for n, ref in clean.items():
+        assert torch.equal(got[n], ref), n
+    assert bool((got["y"][1::5] == 0).all()) and bool((got["dx"][1::5] == 0).all()) and bool((got["dgates"][1::5] == 0).all())
+
+
 def test_capacity_limit_applies_to_a_given_routing():
     inp = synth.moe_inputs(64, 64, 96, 4, 3, torch.float32, DEV)
     idx, gates = routing(64, 4, 1, 1, "one")

@@ -308,6 +308,26 @@ def test_padded_batch_of_few_tokens_leaves_the_workspace():
         assert (np.abs(np64(y)[kept] - want) <= tol + 2.0 ** -8 * np.abs(want)).all()
 
 
+@pytest.mark.parametrize("layer", [(33, 96, 224, 4, 2), (600, 96, 160, 4, 2), (3000, 1056, 160, 2, 2)], ids=lambda s: "x".join(map(str, s)))
+def test_rows_that_are_not_numbers_stay_by_themselves(layer):
+    # NaN in rows without an expert (and in the gates of empty slots) is not read; in other rows it reaches that row alone
+    T, d, F, E, k = layer
+    x = randn(T, d, seed=T, dtype=torch.bfloat16)
+    w1, w3, w2 = (randn(E, *s, seed=i, std=0.2) for i, s in enumerate([(F, d), (F, d), (d, F)]))
+    idx, gates = random_routing(T, E, k, T)
+    idx[2::9] = -1
+    idx[3, 0] = -1
+    clean, _ = moe(x, idx, gates, w1, w3, w2)
+    x[2::9] = float("nan")
+    gates[2::9] = float("inf")
+    gates[3, 0] = float("nan")
+    x[5, 40], x[7, 33] = float("inf"), float("nan")
+    y, _ = moe(x, idx, gates, w1, w3, w2)
+    bad = torch.zeros(T, dtype=torch.bool, device=DEV)
+    bad[[5, 7]] = True
+    assert bool(torch.isnan(y[bad]).all()) and torch.equal(y[~bad], clean[~bad]) and bool((y[2::9] == 0).all())
+
+
 def test_layer_is_the_same_whatever_shares_its_batch():
     # a row's result does not depend on the rows around it (tiles of 128, one or several dispatch blocks)
     T, d, F, E, k = 3000, 96, 160, 5, 2
