@@ -1,7 +1,7 @@
 // The expert layer on MXFP4 experts for a small batch as one cooperative kernel: dispatch and cast, W1/W3 product with
 // SwiGLU and cast, W2 product, sum over the slots.  The layer reads every used expert's weights once (287 MB, 45 us at
 // the copy rate, for 32 tokens, d = 4096, F = 11008, 4 experts, top-2) and does little else.  The thread that loads
-// weights fills the ring of the next pass before each grid barrier.  That batch takes 66.6 us, a launch of its own for
+// weights starts on the next pass before each grid barrier.  That batch takes 66.3 us, a launch of its own for
 // each step 66.9 us on the device and 10 us more of the host's time.  Stamps show where it goes: 7.7 us until the first
 // barrier is passed, 38 us for the 688 tiles of pass 1 (4.65 a CTA at 6.7 us; the slowest CTA sets the end), 18 us for
 // pass 2, 3 us behind it.  Weights on the M side of the MMAs and tokens on the N side measured 73 us.
@@ -29,6 +29,10 @@ namespace cg = cooperative_groups;
 constexpr int L_THREADS = 96 + EPI_WARPS * 32 + 128;
 constexpr int L_RING = 214 * 1024;
 constexpr int L_MAX_R = 1024;
+// Stages of weights on their way before the first barrier: a whole ring of every CTA holds up the cast and the barrier behind
+// it (68.4 us for that batch; 1 to 3 stages 66.6, 5 stages 66.8).  Before the second barrier the whole ring pays: 66.6 us,
+// 69 to 70 with 2 to 8 stages.
+constexpr int kFirstStages = 2;
 constexpr int L_MAX_TILES = kMaxExperts4 + L_MAX_R / kTileRows;      // min(R, E) + R / 128 bounds the row tiles
 
 struct Lists {
@@ -190,7 +194,7 @@ mx4_layer_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
 
   // ---- cast ----
   if (warp == 10) {
-    if (lane == 0) ahead = load_weights(false, 0, n_stages);
+    if (lane == 0) ahead = load_weights(false, 0, min(n_stages, kFirstStages));
     __syncwarp();
   } else if (warp >= 2 && warp < 10) {
     for (int t = blockIdx.x; t < p.T; t += ctas) {
