@@ -411,6 +411,46 @@ def test_layers_on_two_streams_at_once():
         assert torch.equal(y, ref) and B.btx_device_status(ws) == B.BTX_OK
 
 
+def test_offsets_past_32_bits():
+    # 2.4 G elements in x, in y and in the layer's rows: the last rows are those of a small call
+    M, K, N = 600_001, 4096, 4096
+    x = torch.empty(M, K, dtype=torch.bfloat16, device=DEV)
+    tail = randn(200, K, seed=1, dtype=torch.bfloat16)
+    x[:-200] = tail[0]
+    x[-200:] = tail
+    q, qt, w = B.Mx4.empty(1, M, K, DEV), B.Mx4.empty(1, 200, K, DEV), B.Mx4.empty(1, N, K, DEV)
+    B.btx_mx4_quantize(x, q)
+    B.btx_mx4_quantize(tail, qt)
+    B.btx_mx4_quantize(randn(N, K, seed=2, dtype=torch.bfloat16), w)
+    assert torch.equal(q.codes[0, -200:], qt.codes[0])
+    B.btx_mx4_dequantize(q, x)
+    back = torch.empty_like(tail)
+    B.btx_mx4_dequantize(qt, back)
+    assert torch.equal(x[-200:], back)
+    ws, small = torch.empty(256, dtype=torch.uint8, device=DEV), torch.empty(200, N, dtype=torch.bfloat16, device=DEV)
+    B.btx_mx4_matmul(qt, w, small, ws)
+    B.btx_mx4_matmul(q, w, x, ws)
+    # sums of another split of the contraction: within the error of K products in fp32
+    scale = float(back.float().norm(dim=1).max())
+    assert float((x[-200:].float() - small.float()).abs().max()) <= 2.0 ** -8 * float(small.abs().max()) + 2.0 ** -20 * scale ** 2
+    del x, q
+    T, d, F, E, k = 300_001, 4096, 64, 3, 2
+    xs = tail[torch.arange(T, device=DEV) % 200].contiguous()
+    w13, w2 = B.Mx4.empty(E, 2 * F, d, DEV), B.Mx4.empty(E, d, F, DEV)
+    B.btx_mx4_quantize(randn(E, 2 * F, d, seed=3, std=0.02), w13)
+    B.btx_mx4_quantize(randn(E, d, F, seed=4, std=0.2), w2)
+    idx, gates = random_routing(200, E, k, 5)
+    big = [t[torch.arange(T, device=DEV) % 200].contiguous() for t in (idx, gates)]
+    ys = []
+    for n, xi, ii, gi in ((T, xs, *big), (200, tail, idx, gates)):
+        desc = B.make_mx4_moe_desc(n, d, F, E, k, torch.bfloat16)
+        ws = torch.empty(B.btx_mx4_moe_workspace_size(desc), dtype=torch.uint8, device=DEV)
+        ys.append(torch.empty_like(xi))
+        B.btx_mx4_moe_forward(desc, xi, ii, gi, w13, w2, ys[-1], ws)
+    assert torch.equal(ys[0][:200], ys[1]) and torch.equal(ys[0][T // 200 * 200 - 200:T // 200 * 200], ys[1])
+    assert torch.equal(ys[0][-1], ys[1][(T - 1) % 200])
+
+
 def test_binding_refuses_wrong_tensors():
     q = B.Mx4.empty(1, 8, 64, DEV)
     x = randn(8, 64)

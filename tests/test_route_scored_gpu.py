@@ -281,6 +281,25 @@ def test_gradient_of_large_batches(shape, score, renorm, dtype):
     assert torch.equal(part, out.t[:4000])
 
 
+def test_offsets_past_32_bits():
+    T, E, k = 4_300_001, 512, 4
+    z = torch.empty(T, E, dtype=torch.bfloat16, device=DEV)
+    part, b = logits_of(1000, E, torch.bfloat16, 3)
+    z[:-1000] = part[0]
+    z[-1000:] = part
+    _, big = run(z, k, 1, b, scores=False)
+    _, small = run(part, k, 1, b, scores=False)
+    assert torch.equal(big["topk_idx"][-1000:], small["topk_idx"]) and torch.equal(big["gates"][-1000:], small["gates"])
+    assert int(big["counts"].sum()) == T * k
+    dw = torch.ones(T, k, device=DEV) * torch.arange(k, device=DEV)
+    desc = B.make_route_desc(T, E, k, torch.bfloat16, 1)
+    dz = torch.empty_like(z)
+    B.btx_route_backward(desc, z, big["topk_idx"], dw, dz)
+    dp = torch.empty_like(part)
+    B.btx_route_backward(B.make_route_desc(1000, E, k, torch.bfloat16, 1), part, small["topk_idx"], dw[:1000].contiguous(), dp)
+    assert torch.equal(dz[-1000:], dp)
+
+
 def test_binding_refuses_wrong_tensors():
     z = torch.randn(4, 16, device=DEV)
     desc = B.make_route_desc(4, 16, 2, torch.float32)
