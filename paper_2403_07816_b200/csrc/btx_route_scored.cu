@@ -60,9 +60,15 @@ template <int L, int EPL> __device__ __forceinline__ float row_sum(float (&v)[EP
     for (int i = 0; i + w < EPL; i += 2 * w) v[i] += v[i + w];
   return row_sum<L>(v[0]);
 }
+// 16 lanes: a reduction of the whole warp per row is a shorter chain than four exchanges (E = 256, 8 groups, k = 8,
+// T = 16384: 20.0 instead of 20.7 us); with 8 lanes four of them are not (E = 64, k = 2: 6.7 and 6.4 us).
 template <int L> __device__ __forceinline__ uint32_t row_max(uint32_t v) {
   if constexpr (L == 32) {
     return __reduce_max_sync(kAll, v);
+  } else if constexpr (L == 16) {
+    const bool upper = (threadIdx.x & 16) != 0;
+    const uint32_t a = __reduce_max_sync(kAll, upper ? 0u : v), b = __reduce_max_sync(kAll, upper ? v : 0u);
+    return upper ? b : a;
   } else {
 #pragma unroll
     for (int o = L / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(kAll, v, o));
@@ -71,7 +77,9 @@ template <int L> __device__ __forceinline__ uint32_t row_max(uint32_t v) {
 }
 template <int L> __device__ __forceinline__ float row_max(float v) {
   if constexpr (L == 32) {
-    return order_value(__reduce_max_sync(kAll, order_key(v)));
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
   } else {
 #pragma unroll
     for (int o = L / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kAll, v, o));
@@ -555,7 +563,7 @@ route_scored_kernel(const T* __restrict__ logits, const RouteParams p, int sum2)
 // logit: dz_e = s_e (scale dw_e [e chosen] - scale sum_j dw_j s_j).  Bound by the store of the row.
 // A warp per row.  Neighbouring lanes hold neighbouring experts, by the vector (VEC: rows start on 16-byte boundaries and
 // hold whole vectors) or one by one, so that every load and store of the warp is contiguous: 8 experts in a row per lane,
-// as in the choice above, took 9.0 instead of 7.9 us for T = 16384, E = 256, k = 8 (softmax, not renormalised).
+// as in the choice above, took 9.0 instead of 7.8 us for T = 16384, E = 256, k = 8 (softmax, not renormalised).
 template <typename T, int EPL, bool SIGMOID, bool VEC>
 __global__ void __launch_bounds__(kRsWarps * 32)
 route_scored_backward_kernel(int Tn, int E, int k, int renorm, float scale, long long stride,
@@ -725,7 +733,7 @@ cudaError_t launch_route_t(const btx_route_desc* d, const void* logits, RoutePar
 
 // Lanes of a row: enough for E experts at up to 16 each, for the k slots (one per lane) and for the groups.  Fewer lanes
 // per row mean more rows per warp instruction and a longer way through a row, so large batches take them and others get a
-// warp per row: E = 256, 8 of 8 groups, k = 8 takes 21.4 us with 16 lanes and 23.8 with 32 at T = 16384, 10.2 and 9.5 at
+// warp per row: E = 256, 8 of 8 groups, k = 8 takes 20.0 us with 16 lanes and 23.8 with 32 at T = 16384, 10.2 and 9.5 at
 // T = 4096, 8.0 and 5.3 at T = 512; E = 64, k = 2, softmax, T = 16384: 6.6 us with 8 lanes, 12.4 with 32.
 template <typename T>
 cudaError_t launch_route(const btx_route_desc* d, const void* logits, const RouteParams& p, cudaStream_t st) {
