@@ -137,9 +137,15 @@ template <typename F> __device__ __forceinline__ void push2(F v, F& a, F& b) {
   a = a < v ? v : a;
   b = b < low ? low : b;
 }
-// Group key from its two best members' keys.  A group without a candidate has -inf, a missing second adds nothing.
+// Group key from its two best members' keys: the best, or the sum; in fp32 half of it, since two finite keys may add up
+// past the largest float.  A group without a candidate has -inf, a missing second adds nothing.
 template <typename F> __device__ __forceinline__ F group_value(F a, F b, int sum2) {
-  return sum2 && b > (F)-CUDART_INF ? a + b : a;
+  const F part = sizeof(F) == 4 ? (F)0.5 : (F)1;
+  return !sum2 ? a : b > (F)-CUDART_INF ? part * a + part * b : part * a;
+}
+// Bound of the magnitudes behind the key of a group with a candidate.
+template <typename F> __device__ __forceinline__ F group_size(F a, F b, int sum2) {
+  return group_value((F)fabs(a), b > (F)-CUDART_INF ? (F)fabs(b) : b, sum2);
 }
 // Whether this lane's group g stays: v is its key, the same in the P lanes g * P .. g * P + P - 1 of the row's L, which
 // share the comparisons with the G groups; `size` bounds the magnitudes behind v.  `margin` receives the difference
@@ -178,8 +184,7 @@ __device__ __forceinline__ uint32_t choose_groups(const F* key, int G, int size,
     push2(ob, a, b);
   }
   const F v = g < G ? group_value(a, b, sum2) : low;
-  const F reach_g = fabs(a) + (sum2 && b > low ? fabs(b) : (F)0);
-  const bool stays = rank_groups<L, F>(v, reach_g, g, G, P, lane, topk_group, margin, reach);
+  const bool stays = rank_groups<L, F>(v, group_size(a, b, sum2), g, G, P, lane, topk_group, margin, reach);
   const uint32_t lanes = __ballot_sync(kAll, stays && p == 0) >> (lane & ~(L - 1));
   uint32_t mask = 0;
   for (int q = 0; q < G; ++q) mask |= ((lanes >> (q * P)) & 1u) << q;
@@ -380,9 +385,9 @@ route_scored_kernel(const T* __restrict__ logits, const RouteParams p, int sum2)
       uint32_t stay = 0;
       // The groups of the rows whose choice is within its error, in 64 bits (a few rows of a batch, but one of them holds up
       // its block: deciding all of such a row in 64 bits took 12 us); other rows keep `as_is`.  Keys compared as they stand
-      // (logits) are exact.
+      // (logits) are exact.  A key's error is that of one member, or half that of two: err_s, err_0 and its roundings.
       auto redo_groups = [&](float margin_, float reach_, uint32_t as_is) {
-        const float error = 2.f * (sum2 ? 2.f : 1.f) * (err_s * smax + err_0) + 6.f * err_c * reach_;
+        const float error = 2.f * (err_s * smax + err_0) + 6.f * err_c * reach_;
         for (uint32_t rows = __ballot_sync(kAll, (biased || sum2) && sl == 0 && margin_ <= error); rows != 0u; rows &= rows - 1u) {
           const int src = __ffs(rows) - 1;
           __syncwarp();
@@ -405,8 +410,8 @@ route_scored_kernel(const T* __restrict__ logits, const RouteParams p, int sum2)
           a = a > low ? score_key(a) : low;
           b = b > low ? score_key(b) : low;
         }
-        bool stays = rank_groups<L, float>(group_value(a, b, sum2), fabsf(a) + (sum2 && b > low ? fabsf(b) : 0.f), sl / lanes_per,
-                                           p.n_group, lanes_per, lane, p.topk_group, margin, reach);
+        bool stays = rank_groups<L, float>(group_value(a, b, sum2), group_size(a, b, sum2), sl / lanes_per, p.n_group,
+                                           lanes_per, lane, p.topk_group, margin, reach);
         stay = redo_groups(margin, reach, 0u);
         if (stay != 0u) stays = (stay >> (sl / lanes_per)) & 1u;
         if (!stays) {
