@@ -270,7 +270,7 @@ btx_status btx_route_backward(const btx_route_desc* desc, const void* logits, in
  *   scales  [batch][ceil(rows/128)][ceil(K/128)][512] bytes: byte (r % 32) * 16 + (r / 32 % 4) * 4 + j of a
  *           tile is the scale 2^(b - 127) of elements 32 (4c + j) .. of row r (255: the block is NaN).
  * btx_mx4_sizes gives the bytes of both (either pointer may be NULL); both are 16-byte aligned.  Rows and K are at
- * most 2^30.
+ * most 2^30, the codes of a matrix less than 2^40 bytes.
  *
  * btx_mx4_quantize casts src[batch][rows][K] (dtype, rows `row_stride` and matrices `batch_stride` elements
  * apart, elements of a row contiguous): scale 2^(floor(log2 max|x|) - 2), not below 2^-127; elements to the

@@ -7,6 +7,7 @@ namespace {
 
 constexpr long long kMaxItems = 1ll << 30;           // output tiles of a product are numbered in 32 bits
 constexpr int kMaxSide = 1 << 30;                    // so are rows and columns, and the ends of the tiles past the last one
+constexpr long long kMaxCodes = 1ll << 40;           // bytes of a matrix of codes: a tensor map's stride is below this
 
 size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
@@ -15,6 +16,8 @@ long long row_tiles(long long rows) { return (rows + kTileRows - 1) / kTileRows;
 btx_status check_shape(int batch, int rows, int K) {
   if (batch < 0 || rows < 0 || K < 1) return BTX_ERR_INVALID_ARG;
   if (K % kBlock != 0 || rows > kMaxSide || K > kMaxSide) return BTX_ERR_UNSUPPORTED;
+  const long long codes = rows * (long long)(K / 2), scales = row_tiles(rows) * scale_tiles_k(K) * kTileBytes;
+  if (codes >= kMaxCodes || (batch > 0 && (codes > scales ? codes : scales) > (1ll << 62) / batch)) return BTX_ERR_UNSUPPORTED;
   return BTX_OK;
 }
 
@@ -36,6 +39,8 @@ btx_status make_moe_plan(const btx_mx4_moe_desc* d, MoePlan* pl) {
   const int pad_tiles = pairs_fit(R, used, d->d_model, d->d_ff) ? 2 : 1;
   const long long unit = pad_tiles * kTileRows;
   const long long tiles = (R + used * (unit - 1)) / unit * pad_tiles;
+  const long long wide = d->d_model > d->d_ff ? d->d_model : d->d_ff;       // codes of the rows, of W1 and W3, of W2
+  if (tiles * kTileRows * (wide / 2) >= kMaxCodes || (long long)d->d_ff * d->d_model >= kMaxCodes) return BTX_ERR_UNSUPPORTED;
   const long long widest = d->d_model > 2 * (long long)d->d_ff ? d->d_model : 2 * (long long)d->d_ff;
   if (tiles * row_tiles(widest) > kMaxItems) return BTX_ERR_UNSUPPORTED;
   *pl = MoePlan();
@@ -70,7 +75,8 @@ btx_status check_matmul(int dtype, int batch, int M, int N, int K) {
   if (batch < 0 || M < 0 || N < 1) return BTX_ERR_INVALID_ARG;
   btx_status s = check_shape(batch, M, K);
   if (s != BTX_OK) return s;
-  if (N > kMaxSide || row_tiles(M) * row_tiles(N) > kMaxItems || row_tiles(M) * row_tiles(N) * batch > kMaxItems) return BTX_ERR_UNSUPPORTED;
+  if ((s = check_shape(batch, N, K)) != BTX_OK) return s;
+  if (row_tiles(M) * row_tiles(N) > kMaxItems || row_tiles(M) * row_tiles(N) * batch > kMaxItems) return BTX_ERR_UNSUPPORTED;
   return BTX_OK;
 }
 
@@ -96,7 +102,7 @@ extern "C" btx_status btx_mx4_quantize(int32_t dtype, const void* src, int64_t r
   if (s != BTX_OK) return s;
   if (dtype != BTX_F32 && dtype != BTX_BF16) return BTX_ERR_INVALID_ARG;
   if (row_first < 0 || row_step < 1 || out_rows < 0) return BTX_ERR_INVALID_ARG;
-  if (out_rows > kMaxSide) return BTX_ERR_UNSUPPORTED;
+  if ((s = check_shape(batch, out_rows, K)) != BTX_OK) return s;
   if (rows > 0 && (long long)row_first + (long long)(rows - 1) * row_step >= out_rows) return BTX_ERR_INVALID_ARG;
   if (batch == 0 || rows == 0) return BTX_OK;
   if (!src || !codes || !scales) return BTX_ERR_INVALID_ARG;
