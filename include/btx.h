@@ -8,7 +8,8 @@
  *     frees device memory and keeps no pointer after a call returns.  What it does keep, per
  *     process: one helper stream per device (btx_moe_backward), the multiprocessor count per
  *     device, the address of one static scratch array per device (btx_lb_loss_noalloc), and the
- *     calling thread's stage-timing hook (btx_set_stage_events).
+ *     calling thread's stage-timing hook (btx_set_stage_events) and self-test switch
+ *     (btx_selftest_separate_launches).
  *   - The current device must be the one the buffers and `stream` belong to.
  *   - `stream` is a cudaStream_t passed as void*.  Calls enqueue work on it and return without
  *     synchronising; arguments are validated on the host before anything is launched.
@@ -322,6 +323,11 @@ btx_status btx_device_status(const void* workspace, void* stream, int32_t* devic
  * seconds) if a copy or a partner CTA never signals.  btx_device_status then reports BTX_ERR_TIMEOUT; the
  * CUDA context stays usable and the next call that uses the workspace clears the word again. */
 btx_status btx_selftest_wait_expiry(void* workspace, size_t workspace_bytes, void* stream);
+
+/* Self-test of the launches that stand in for the one-kernel form of btx_mx4_moe_forward (taken by themselves only where
+ * the device refuses to hold all blocks of that kernel at once, e.g. in a partition of it): while set, calls of the
+ * calling host thread take them for every batch.  Same work and workspace; a row may differ in its last bits. */
+btx_status btx_selftest_separate_launches(int32_t on);
 
 /* Optional stage timing for the calling host thread.  `events` is a host array of n
  * cudaEvent_t (as void*), or NULL to switch the hook off.  While set, btx_moe_forward records

@@ -65,7 +65,7 @@ EXPORTS = ["btx_moe_sizes", "btx_moe_forward", "btx_moe_backward", "btx_moe_step
            "btx_route", "btx_route_backward",
            "btx_mx4_sizes", "btx_mx4_quantize", "btx_mx4_dequantize", "btx_mx4_matmul_workspace_size", "btx_mx4_matmul",
            "btx_mx4_moe_workspace_size", "btx_mx4_moe_forward",
-           "btx_device_status", "btx_selftest_wait_expiry", "btx_set_stage_events", "btx_status_string", "btx_version"]
+           "btx_device_status", "btx_selftest_wait_expiry", "btx_selftest_separate_launches", "btx_set_stage_events", "btx_status_string", "btx_version"]
 
 
 def lib():
@@ -83,6 +83,7 @@ def lib():
         L.btx_moe_step_host.argtypes = [C.POINTER(MoeDesc)] + [vp] * 15 + [f32] + [vp] * 5 + [i32, vp, vp, sz, vp, vp]
         L.btx_set_stage_events.argtypes = [C.POINTER(vp), i32]
         L.btx_selftest_wait_expiry.argtypes = [vp, sz, vp]
+        L.btx_selftest_separate_launches.argtypes = [i32]
         L.btx_lb_loss_workspace_size.argtypes = [C.POINTER(MoeDesc), C.POINTER(sz)]
         L.btx_lb_loss.argtypes = [C.POINTER(MoeDesc), vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.btx_lb_loss_noalloc.argtypes = [C.POINTER(MoeDesc), vp, vp, vp, vp, vp, vp, vp]
@@ -560,6 +561,13 @@ def btx_selftest_wait_expiry(workspace):
                                            _stream(workspace.device))
     if s != BTX_OK:
         raise BtxError(s, "btx_selftest_wait_expiry")
+
+
+def btx_selftest_separate_launches(on):
+    """Takes the separate launches of btx_mx4_moe_forward for every batch of this thread; see btx.h."""
+    s = lib().btx_selftest_separate_launches(int(on))
+    if s != BTX_OK:
+        raise BtxError(s, "btx_selftest_separate_launches")
 
 
 def btx_device_status(workspace):

@@ -71,7 +71,7 @@ btx_status launch_gate_up(const GemmArgs& g, const Dispatch& q, uint8_t* act_cod
 // W2 product, gate-scaled fp32 rows at [t*k+slot]
 btx_status launch_down(const GemmArgs& g, const Dispatch& q, const float* gates, float* rows, cudaStream_t st);
 
-// The whole layer of a small batch as one cooperative kernel; refused (BTX_ERR_CUDA, nothing launched) where not every
+// The whole layer of a small batch as one cooperative kernel; BTX_ERR_UNSUPPORTED, nothing launched, where not every
 // block can be resident.  `rows` holds layer_rows_floats floats.
 bool layer_fits(const Dispatch& q);
 size_t layer_rows_floats(const Dispatch& q);

@@ -9,6 +9,8 @@ constexpr long long kMaxItems = 1ll << 30;           // output tiles of a produc
 constexpr int kMaxSide = 1 << 30;                    // so are rows and columns, and the ends of the tiles past the last one
 constexpr long long kMaxCodes = 1ll << 40;           // bytes of a matrix of codes: a tensor map's stride is below this
 
+thread_local bool g_separate = false;                // btx_selftest_separate_launches
+
 size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 long long row_tiles(long long rows) { return (rows + kTileRows - 1) / kTileRows; }
@@ -198,9 +200,9 @@ extern "C" btx_status btx_mx4_moe_forward(const btx_mx4_moe_desc* desc, const vo
   down = up;
   down.a_codes = act; down.a_scales = act_scales; down.b_codes = (const uint8_t*)w2_codes; down.b_scales = (const uint8_t*)w2_scales;
   down.N = desc->d_model; down.K = desc->d_ff;
-  if (layer_fits(q)) {
-    if (launch_layer(up, down, q, desc->dtype, x, gates, rows, act, act_scales, y, st) == BTX_OK) return BTX_OK;
-    cudaGetLastError();                      // not every block can be resident: the launches below do the same work
+  if (layer_fits(q) && !g_separate) {
+    s = launch_layer(up, down, q, desc->dtype, x, gates, rows, act, act_scales, y, st);
+    if (s != BTX_ERR_UNSUPPORTED) return s;  // else not every block can be resident: the launches below do the same work
   }
   // every kernel is a programmatic dependent of the one before it
   if (launch_dispatch(q, st) != cudaSuccess) return BTX_ERR_CUDA;
@@ -208,4 +210,9 @@ extern "C" btx_status btx_mx4_moe_forward(const btx_mx4_moe_desc* desc, const vo
   if ((s = launch_gate_up(up, q, act, act_scales, st)) != BTX_OK) return s;
   if ((s = launch_down(down, q, gates, rows, st)) != BTX_OK) return s;
   return launch_combine_rows(q, desc->dtype, rows, 1, y, st) == cudaSuccess ? BTX_OK : BTX_ERR_CUDA;
+}
+
+extern "C" btx_status btx_selftest_separate_launches(int32_t on) {
+  g_separate = on != 0;
+  return BTX_OK;
 }

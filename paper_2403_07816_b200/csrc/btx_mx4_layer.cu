@@ -408,11 +408,14 @@ btx_status launch_layer(const GemmArgs& up, const GemmArgs& down, const Dispatch
   attr[0].id = cudaLaunchAttributeCooperative;
   attr[0].val.cooperative = 1;
   cfg.attrs = attr; cfg.numAttrs = 1;
-  if (dtype == BTX_BF16)
-    return allow_smem((const void*)mx4_layer_kernel<__nv_bfloat16>, L_SMEM, done[0]) &&
-                   cudaLaunchKernelEx(&cfg, mx4_layer_kernel<__nv_bfloat16>, mx, mw13, ma, mw2, p) == cudaSuccess ? BTX_OK : BTX_ERR_CUDA;
-  return allow_smem((const void*)mx4_layer_kernel<float>, L_SMEM, done[1]) &&
-                 cudaLaunchKernelEx(&cfg, mx4_layer_kernel<float>, mx, mw13, ma, mw2, p) == cudaSuccess ? BTX_OK : BTX_ERR_CUDA;
+  const bool bf16 = dtype == BTX_BF16;
+  const void* kernel = bf16 ? (const void*)mx4_layer_kernel<__nv_bfloat16> : (const void*)mx4_layer_kernel<float>;
+  if (!allow_smem(kernel, L_SMEM, done[bf16])) return BTX_ERR_CUDA;
+  const cudaError_t e = bf16 ? cudaLaunchKernelEx(&cfg, mx4_layer_kernel<__nv_bfloat16>, mx, mw13, ma, mw2, p)
+                             : cudaLaunchKernelEx(&cfg, mx4_layer_kernel<float>, mx, mw13, ma, mw2, p);
+  if (e != cudaErrorCooperativeLaunchTooLarge) return e == cudaSuccess ? BTX_OK : BTX_ERR_CUDA;
+  cudaGetLastError();                                      // answered by the caller, not an error of this thread any more
+  return BTX_ERR_UNSUPPORTED;
 }
 
 }  // namespace mx4
