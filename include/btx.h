@@ -234,7 +234,8 @@ btx_status btx_merge_ffn(int32_t n_models, int32_t dtype, int32_t layout, int32_
  *   topk_idx[T,k]: the k largest c, largest first; ties between groups and between experts go to the lower
  *   index.  The order is that of the exact values: a row whose order fp32 cannot settle is settled in fp64.
  *   gates[T,k] = scale * s, or with `renorm` scale * s / (sum of s over the row's choice).
- *   An expert with a logit of -inf or NaN (or whose c is) is switched off in that row: score 0, never chosen.
+ *   An expert with a logit of -inf or NaN is switched off in that row: score 0, never chosen.  A bias of -inf or NaN
+ *   only bars its expert from the choice: the expert keeps its score, in `scores` and in the sum of the softmax.
  *   Slots that find no expert, and all slots of rows with row_valid[t] == 0 (row_valid may be NULL), have
  *   topk_idx -1 and gate 0.
  * Optional outputs, NULL to skip: scores[T,E] fp32 (s; 0 in rows that are not valid), counts[E] (tokens per

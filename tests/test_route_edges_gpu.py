@@ -47,3 +47,26 @@ def test_keys_at_both_ends_of_the_type():
     z[3, 24:28] = float("-inf")
     for tg in (1, 3, 7):
         compare(z, 3, 1, b.to(DEV), n_group=8, topk_group=tg, group_score=1)
+
+
+@pytest.mark.parametrize("T", [2, 8200], ids=["few", "many"])
+@pytest.mark.parametrize("bar", [float("-inf"), float("nan")], ids=["-inf", "nan"])
+def test_a_bias_that_bars_an_expert_leaves_its_score(bar, T):
+    # values worked out by hand: the barred expert stays in the sum of the softmax, a logit of -inf does not
+    z = torch.tensor([[1.0, 2.0, 3.0, 4.0]]).repeat(T, 1).to(DEV)
+    b = torch.tensor([0.0, 0.0, 0.0, bar], device=DEV)
+    e = np.exp([1.0, 2.0, 3.0, 4.0])
+    sig = 1 / (1 + np.exp([-1.0, -2.0, -3.0, -4.0]))
+    off = z.clone()
+    off[:, 3] = float("-inf")
+    for score, scores in ((0, e / e.sum()), (1, sig)):
+        for renorm in (False, True):
+            _, got = compare(z, 2, score, b, renorm=renorm, scale=1.5)
+            w = 1.5 * scores[[2, 1]] / (scores[[2, 1]].sum() if renorm else 1)
+            for t in (0, T - 1):
+                assert got["topk_idx"][t].tolist() == [2, 1]
+                np.testing.assert_allclose(got["scores"][t].cpu().numpy(), scores, rtol=2.0 ** -17)
+                np.testing.assert_allclose(got["gates"][t].cpu().numpy(), w, rtol=2.0 ** -17)
+    _, got = compare(off, 2, 0, None, renorm=False)
+    np.testing.assert_allclose(got["scores"][0].cpu().numpy(), np.r_[e[:3] / e[:3].sum(), 0.0], rtol=2.0 ** -17)
+    np.testing.assert_allclose(got["gates"][0].cpu().numpy(), (e / e[:3].sum())[[2, 1]], rtol=2.0 ** -17)
