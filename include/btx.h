@@ -290,7 +290,9 @@ btx_status btx_mx4_dequantize(int32_t dtype, const void* codes, const void* scal
 
 /* y[batch][M][N] (dtype, contiguous) = A B^T of A[batch][M][K] and B[batch][N][K], both MXFP4: products of the
  * values, fp32 accumulation, one rounding.  K is a multiple of 32, M and N are any size (M or batch 0: nothing
- * to do).  Inference: there is no gradient through the cast.  The workspace serves one call at a time. */
+ * to do).  Inference: there is no gradient through the cast.  The workspace serves one call at a time.
+ * Results repeat from run to run.  How many parts the contraction is split into, and so the order in which an element's
+ * fp32 sum is formed, depends on batch, M, N and K: rows of calls of other sizes agree within that rounding only. */
 btx_status btx_mx4_matmul_workspace_size(int32_t dtype, int32_t batch, int32_t M, int32_t N, int32_t K,
                                          size_t* workspace_bytes);
 btx_status btx_mx4_matmul(int32_t dtype, int32_t batch, int32_t M, int32_t N, int32_t K, const void* a_codes,
@@ -303,7 +305,10 @@ btx_status btx_mx4_matmul(int32_t dtype, int32_t batch, int32_t M, int32_t N, in
  * formed in fp32, slots are added in fp32 in slot order, y is rounded once.
  *   x[T,d], y[T,d] in dtype; topk_idx[T,k] int32 (an index outside 0..E-1 is an empty slot: it adds nothing);
  *   gates[T,k] fp32; w13: E matrices of 2F rows of d, row 2i is row i of W1_e and row 2i + 1 row i of W3_e;
- *   w2: E matrices of d rows of F.  d and F are multiples of 32, E <= 512, T may be 0. */
+ *   w2: E matrices of d rows of F.  d and F are multiples of 32, E <= 512, T may be 0.
+ * Results repeat from run to run.  The W2 product of a small batch is split into parts whose number depends on how many
+ * tiles of 128 rows the experts fill: a token's y may differ in its last bits, by the rounding of fp32 sums formed in
+ * another order, when the tokens beside it are others (its activations in MXFP4 are the same). */
 typedef struct {
   int32_t T, d_model, d_ff, E, k;
   int32_t dtype;              /* btx_dtype of x and y */

@@ -54,3 +54,50 @@ def test_the_switch_is_the_threads_own():
     finally:
         B.btx_selftest_separate_launches(False)
     assert torch.equal(here, there)                        # one stage of F: nothing is split in either form
+
+
+def test_a_row_among_others():
+    # d = 1024: eight column tiles of W2, F = 2048: eight stages; one or two row tiles split them into 4 parts, five into 2,
+    # ten into 1.  The parts' sums are fp32 and added in fp32: both orders are within (F/64 + 8) 2^-22 of the sum of
+    # |w2| |a| from the exact sum of the same activations (an activation that 64 bits cast the other way changes that
+    # size by less than a quarter), and each y is rounded once to fp32.
+    d, F, E = 1024, 2048, 10
+    w = [randn(E, *s, seed=i, std=0.05) for i, s in enumerate([(F, d), (F, d), (d, F)])]
+    x = randn(200, d, seed=5)
+    x[1:] = x[1:].roll(1, 0)
+    gates = torch.full((200, 1), 0.75, device=DEV)
+
+    def row0(T, experts):
+        idx = (torch.arange(T, device=DEV, dtype=torch.int32) % experts)[:, None].contiguous()
+        return moe(x[:T].contiguous(), idx, gates[:T].contiguous(), *w)[0][0]
+    alone = row0(1, 1)
+    assert torch.equal(row0(1, 1), alone)                                   # again
+    assert torch.equal(row0(100, 1), alone) and torch.equal(row0(200, 1), alone) and torch.equal(row0(30, 2), alone)
+    from oracle import experts_oracle as o
+    xq, w1, w3, w2 = o.mx4_round(np64(x)[0]), *(o.mx4_round(np64(u)[0]) for u in w)
+    h1, h3 = w1 @ xq, w3 @ xq
+    size = 0.75 * np.abs(w2) @ np.abs(o.mx4_round(h1 / (1 + np.exp(-h1)) * h3))
+    for T, experts in ((5, 5), (10, 10), (200, 10)):
+        err = np.abs(np64(row0(T, experts)) - np64(alone))
+        assert (err <= 2 * 1.25 * (F / 64 + 8) * 2.0 ** -22 * size + 2.0 ** -23 * np.abs(np64(alone))).all()
+
+
+def test_a_row_of_a_product_among_others():
+    # the contraction of one row tile is shared by eight CTAs, that of eight row tiles by two
+    N, K = 1024, 4096
+    x, wt = randn(1000, K, seed=1), randn(1, N, K, seed=2, std=0.02)
+    wq = B.Mx4.empty(1, N, K, DEV)
+    B.btx_mx4_quantize(wt, wq)
+    ws = torch.empty(256, dtype=torch.uint8, device=DEV)
+
+    def rows(M):
+        q, y = B.Mx4.empty(1, M, K, DEV), torch.empty(M, N, device=DEV)
+        B.btx_mx4_quantize(x[:M], q)
+        B.btx_mx4_matmul(q, wq, y, ws)
+        return y
+    one = rows(1)
+    assert torch.equal(rows(1), one) and torch.equal(rows(100)[:1], one)    # the same split
+    from oracle import experts_oracle as o
+    size = np.abs(o.mx4_round(np64(x[:1]))) @ np.abs(o.mx4_round(np64(wt)[0])).T
+    err = np.abs(np64(rows(1000)[:1]) - np64(one))
+    assert (err <= 2 * (K / 64 + 4) * 2.0 ** -22 * size + 2.0 ** -23 * np.abs(np64(one))).all()
