@@ -1,4 +1,4 @@
-"""CPU statements in 64 bits of score routing, the MXFP4 format and the expert layer on MXFP4 weights.
+"""CPU statements in 64 bits of score routing and the MXFP4 format.
 
 Test infrastructure only: plain numpy from the definitions, one row or block at a time where that is clearest, and
 nothing shared with the CUDA path.  MXFP4 follows the OCP Microscaling Formats (MX) specification v1.0.
@@ -173,17 +173,3 @@ def mx4_tile_scales(scales, fill=0):
         for b in range(nb):
             out[r // 128, b // 4, (r % 32) * 16 + (r % 128 // 32) * 4 + b % 4] = scales[r, b]
     return out
-
-
-def mx4_moe(x, topk_idx, gates, w1, w3, w2, act_round=mx4_round):
-    """y[t] = sum over slots of gate * W2_e mx4(silu(W1_e x) * W3_e x), x and the weights given as MXFP4 values."""
-    y = np.zeros_like(x, dtype=np.float64)
-    E = w1.shape[0]
-    for t in range(x.shape[0]):
-        for j in range(topk_idx.shape[1]):
-            e = topk_idx[t, j]
-            if 0 <= e < E:
-                h1, h3 = w1[e] @ x[t], w3[e] @ x[t]
-                act = act_round(h1 * _sigmoid(h1) * h3)
-                y[t] += gates[t, j] * (w2[e] @ act)
-    return y
