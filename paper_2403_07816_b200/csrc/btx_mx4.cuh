@@ -3,8 +3,8 @@
 //
 // Format (include/btx.h): e2m1 codes, two per byte along K, rows of K/2 bytes; one scale byte (2^(b-127)) per 32
 // elements, stored in tiles of 128 rows x 4 blocks = 512 bytes, [row tile][K/128][512], byte (r % 32) * 16 +
-// (r / 32 % 4) * 4 + j for block 4c + j of row r: the order in which tcgen05.cp.32x128b puts a tile into tensor
-// memory, so no kernel rearranges scales.
+// (r / 32 % 4) * 4 + j for block 4c + j of row r: lane r % 32 of a warp takes 16 neighbouring bytes, whose four words are
+// the four columns of tensor memory that the MMAs read (tcgen05.st), so no kernel rearranges scales.
 #pragma once
 
 #include "btx_common.cuh"
@@ -53,8 +53,8 @@ int dispatch_chunk(long long R);
 cudaError_t launch_dispatch(const Dispatch& q, cudaStream_t st);
 // x [T, d] cast to MXFP4 and written to the k padded rows of every token
 cudaError_t launch_quantize_rows(const Dispatch& q, int dtype, const void* x, uint8_t* codes, uint8_t* scales, cudaStream_t st);
-// y[t] = sum over slots with an expert, and over `splits` partial copies, of rows[split][t*k+slot]
-cudaError_t launch_combine_rows(const Dispatch& q, int dtype, const float* rows, int splits, void* y, cudaStream_t st);
+// y[t] = sum over slots with an expert of rows[t*k+slot]
+cudaError_t launch_combine_rows(const Dispatch& q, int dtype, const float* rows, void* y, cudaStream_t st);
 
 // Products.  A: codes [batch, M, K] (grouped: the padded rows), B: codes [batch or experts, N, K].
 struct GemmArgs {

@@ -209,7 +209,7 @@ extern "C" btx_status btx_mx4_moe_forward(const btx_mx4_moe_desc* desc, const vo
   if (launch_quantize_rows(q, desc->dtype, x, xs, xs_scales, st) != cudaSuccess) return BTX_ERR_CUDA;
   if ((s = launch_gate_up(up, q, act, act_scales, st)) != BTX_OK) return s;
   if ((s = launch_down(down, q, gates, rows, st)) != BTX_OK) return s;
-  return launch_combine_rows(q, desc->dtype, rows, 1, y, st) == cudaSuccess ? BTX_OK : BTX_ERR_CUDA;
+  return launch_combine_rows(q, desc->dtype, rows, y, st) == cudaSuccess ? BTX_OK : BTX_ERR_CUDA;
 }
 
 extern "C" btx_status btx_selftest_separate_launches(int32_t on) {

@@ -289,14 +289,13 @@ quantize_rows_kernel(const Dispatch q, const T* __restrict__ x, uint8_t* __restr
   }
 }
 
-// A thread owns 16 bytes of y; slots and splits are added in order, in fp32, and rounded once.
+// A thread owns 16 bytes of y; slots are added in order, in fp32, and rounded once.
 template <typename T>
 __global__ void __launch_bounds__(256)
-combine_rows_kernel(int Tn, int d, int k, int splits, const float* __restrict__ rows, const int32_t* __restrict__ flat2row,
+combine_rows_kernel(int Tn, int d, int k, const float* __restrict__ rows, const int32_t* __restrict__ flat2row,
                     T* __restrict__ y) {
   constexpr int VN = Vec<T>::N;
   const int vecs = d / VN;
-  const size_t split_stride = (size_t)Tn * k * d;
   allow_dependents();
   grid_dependency_wait();
   for (size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x; i < (size_t)Tn * vecs; i += (size_t)gridDim.x * blockDim.x) {
@@ -307,13 +306,11 @@ combine_rows_kernel(int Tn, int d, int k, int splits, const float* __restrict__ 
     for (int j = 0; j < VN; ++j) acc[j] = 0.f;
     for (int s = 0; s < k; ++s) {
       if (flat2row[t * k + s] < 0) continue;               // its row was never written
-      for (int sp = 0; sp < splits; ++sp) {
-        const float* r = rows + sp * split_stride + (t * k + s) * d + c;
+      const float* r = rows + (t * k + s) * d + c;
 #pragma unroll
-        for (int j = 0; j < VN; j += 4) {
-          const float4 q = __ldcs(reinterpret_cast<const float4*>(r + j));
-          acc[j] += q.x; acc[j + 1] += q.y; acc[j + 2] += q.z; acc[j + 3] += q.w;
-        }
+      for (int j = 0; j < VN; j += 4) {
+        const float4 q = __ldcs(reinterpret_cast<const float4*>(r + j));
+        acc[j] += q.x; acc[j + 1] += q.y; acc[j + 2] += q.z; acc[j + 3] += q.w;
       }
     }
     __align__(16) T out[VN];
@@ -398,14 +395,14 @@ cudaError_t launch_quantize_rows(const Dispatch& q, int dtype, const void* x, ui
   });
 }
 
-cudaError_t launch_combine_rows(const Dispatch& q, int dtype, const float* rows, int splits, void* y, cudaStream_t st) {
+cudaError_t launch_combine_rows(const Dispatch& q, int dtype, const float* rows, void* y, cudaStream_t st) {
   const size_t n = (size_t)q.T * (q.d / (dtype == BTX_BF16 ? 8 : 4));
   const size_t want = (n + 255) / 256, most = (size_t)sm_count() * 32;
   const dim3 grid((unsigned)(want < most ? want : most));
   if (dtype == BTX_BF16)
-    return launch_after_predecessor(combine_rows_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, true, q.T, q.d, q.k, splits, rows,
+    return launch_after_predecessor(combine_rows_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, true, q.T, q.d, q.k, rows,
                                     (const int32_t*)q.flat2row, (__nv_bfloat16*)y);
-  return launch_after_predecessor(combine_rows_kernel<float>, grid, dim3(256), 0, st, true, q.T, q.d, q.k, splits, rows,
+  return launch_after_predecessor(combine_rows_kernel<float>, grid, dim3(256), 0, st, true, q.T, q.d, q.k, rows,
                                   (const int32_t*)q.flat2row, (float*)y);
 }
 

@@ -379,7 +379,6 @@ route_scored_kernel(const T* __restrict__ logits, const RouteParams p, int sum2)
       if (!(z[i] > low && c[i] > low)) c[i] = low;
     }
     const float smax = SIGMOID ? 1.0f : inv_total;                 // no score is larger
-    bool unsure = false;                                           // not settled in registers
     if (grouped) {
       float margin, reach;
       uint32_t stay = 0;
@@ -467,6 +466,7 @@ route_scored_kernel(const T* __restrict__ logits, const RouteParams p, int sum2)
       next = row_max<L>(best0);
     };
     for (int j = 0; j < p.k; ++j) pick(next != 0u);
+    bool unsure = false;                                           // not settled in registers
     if (!exact_keys) {
       // Neighbours that lie within what a packed key leaves out and the error of the keys: take what else lies as close,
       // and order all of it in 64 bits.  The bound holds for every key from the first to the one compared.
@@ -481,7 +481,7 @@ route_scored_kernel(const T* __restrict__ logits, const RouteParams p, int sum2)
       uint32_t last = __shfl_sync(kAll, mine, n > 0 ? n - 1 : 0, L);
       const bool tail = n > 0 && next != 0u && close(last, next);
       const bool near = row_any<L>(sl + 1 < n && close(mine, after), lane);     // (a vote of the whole warp: never behind a condition of a row)
-      const bool redo = !unsure && (near || tail);
+      const bool redo = near || tail;
       if (__any_sync(kAll, redo)) {
         for (;;) {
           const bool more = redo && n < L && next != 0u && close(last, next);
