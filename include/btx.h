@@ -10,6 +10,7 @@
  *     device, the address of one static scratch array per device (btx_lb_loss_noalloc), and the
  *     calling thread's stage-timing hook (btx_set_stage_events) and self-test switch
  *     (btx_selftest_separate_launches).
+ *   - Outputs overlap neither inputs nor one another unless a call says so.
  *   - The current device must be the one the buffers and `stream` belong to.
  *   - `stream` is a cudaStream_t passed as void*.  Calls enqueue work on it and return without
  *     synchronising; arguments are validated on the host before anything is launched.
@@ -232,7 +233,8 @@ btx_status btx_merge_ffn(int32_t n_models, int32_t dtype, int32_t layout, int32_
  *   sum of its two best (SUM2; without a bias: of their scores); only the topk_group best groups take part.
  *   (n_group = 1: no groups.)
  *   topk_idx[T,k]: the k largest c, largest first; ties between groups and between experts go to the lower
- *   index.  The order is that of the exact values: a row whose order fp32 cannot settle is settled in fp64.
+ *   index.  The order is that of the exact values, to the rounding of fp64: a row whose order fp32 cannot settle is
+ *   settled in fp64, which takes longer (a batch whose rows all are, e.g. of equal scores: 3 to 7 times as long).
  *   gates[T,k] = scale * s, or with `renorm` scale * s / (sum of s over the row's choice).
  *   An expert with a logit of -inf or NaN is switched off in that row: score 0, never chosen.  A bias of -inf or NaN
  *   only bars its expert from the choice: the expert keeps its score, in `scores` and in the sum of the softmax.
@@ -240,7 +242,8 @@ btx_status btx_merge_ffn(int32_t n_models, int32_t dtype, int32_t layout, int32_
  *   topk_idx -1 and gate 0.
  * Optional outputs, NULL to skip: scores[T,E] fp32 (s; 0 in rows that are not valid), counts[E] (tokens per
  * expert, from which a caller moves its bias).  E <= 512, k <= 32, n_group <= 32, k <= topk_group * E / n_group,
- * scale > 0.  T may be 0.  Pointers need the alignment of their elements; rows that start on 16-byte boundaries
+ * scale > 0.  T may be 0.  btx_moe_forward takes such a choice of up to 64 experts, btx_mx4_moe_forward (inference) of up
+ * to 512.  Pointers need the alignment of their elements; rows that start on 16-byte boundaries
  * and hold whole 16-byte vectors are read fastest.  No workspace: calls on different streams may overlap. */
 typedef enum { BTX_SCORE_SOFTMAX = 0, BTX_SCORE_SIGMOID = 1 } btx_score;
 typedef enum { BTX_GROUP_MAX = 0, BTX_GROUP_SUM2 = 1 } btx_group_score;
@@ -301,8 +304,9 @@ btx_status btx_mx4_matmul(int32_t dtype, int32_t batch, int32_t M, int32_t N, in
 
 /* The expert layer of btx_moe_forward (Section 3.2) on MXFP4 experts under a routing from elsewhere, e.g.
  * btx_route:  y_t = sum over slots j of gates[t,j] * W2_e a,  a = mx4(silu(W1_e mx4(x_t)) * W3_e mx4(x_t)),
- * e = topk_idx[t,j].  Activations are cast to MXFP4 in front of both products, silu and the products are
- * formed in fp32, slots are added in fp32 in slot order, y is rounded once.
+ * e = topk_idx[t,j].  Activations are cast to MXFP4 in front of both products, products are formed in fp32, silu in
+ * fp32 from the fast exponential (for x in fp32 too: within (4 + 1.2 |h|) 2^-23 of silu(h)), slots are added in
+ * fp32 in slot order, y is rounded once.
  *   x[T,d], y[T,d] in dtype; topk_idx[T,k] int32 (an index outside 0..E-1 is an empty slot: it adds nothing);
  *   gates[T,k] fp32; w13: E matrices of 2F rows of d, row 2i is row i of W1_e and row 2i + 1 row i of W3_e;
  *   w2: E matrices of d rows of F.  d and F are multiples of 32, E <= 512, T may be 0.

@@ -3,7 +3,8 @@
 //   quantize     per 32 elements: scale 2^(floor(log2 max|x|) - 2), elements to the nearest e2m1 value (ties to the
 //                even code, at most 6).  Four lanes share a block, eight elements each: a warp reads 256 consecutive
 //                elements with 16-byte loads, the maximum takes two shuffles, a lane stores four bytes of codes and
-//                every fourth the scale byte.  Bound by memory: 2 + 17/32 bytes per bf16 element, 6.0 TB/s for large matrices.
+//                every fourth the scale byte.  2 + 17/32 bytes per bf16 element, 6.0 TB/s for large matrices, 0.93 of the
+//                measured copy rate, at 88 % of the issue slots.
 //   dequantize   the same mapping backwards
 //   dispatch     stable counting sort of the assignments by expert, padded to 128-row tiles
 //   quantize_rows  quantize of x with every row written to the k rows of its token: x is read once

@@ -1,8 +1,8 @@
 // The expert layer on MXFP4 experts for a small batch as one cooperative kernel: dispatch and cast, W1/W3 product with
 // SwiGLU and cast, W2 product, sum over the slots.  The layer reads every used expert's weights once (287 MB, 45 us at
 // the copy rate, for 32 tokens, d = 4096, F = 11008, 4 experts, top-2) and does little else.  The thread that loads
-// weights starts on the next pass before each grid barrier.  That batch takes 66.3 us, a launch of its own for
-// each step 66.9 us on the device and 10 us more of the host's time.  Stamps show where it goes: 7.7 us until the first
+// weights starts on the next pass before each grid barrier.  That batch takes 66.7 us, a launch of its own for
+// each step 69.6 us on the device and 10 us more of the host's time.  Stamps show where it goes: 7.7 us until the first
 // barrier is passed, 38 us for the 688 tiles of pass 1 (4.65 a CTA at 6.7 us; the slowest CTA sets the end), 18 us for
 // pass 2, 3 us behind it.  Weights on the M side of the MMAs and tokens on the N side measured 73 us.
 //
@@ -28,6 +28,11 @@ namespace cg = cooperative_groups;
 
 constexpr int L_THREADS = 96 + EPI_WARPS * 32 + 128;
 constexpr int L_RING = 214 * 1024;
+// Batches of more assignments, or of more than two tokens for every multiprocessor (each ranks its assignments by a walk over
+// the list), take separate launches, which are as fast there on the device: 296 tokens on 3 of 16 experts (d = 2048,
+// F = 1024) 34.6 us in one kernel and 33.8, 290 tokens on one of 8 (4096 x 4096) 62.0 and 59.9.  Below, one kernel
+// is ahead: 32 tokens of the batch above 66.7 and 69.6, 128 of them 70.7 and 73.1, 128 tokens on 8 of 64 experts 63.7 and
+// 69.3 (d = 2048, F = 1024), on 8 of 256 179 and 202.
 constexpr int L_MAX_R = 1024;
 // Stages of weights on their way before the first barrier: a whole ring of every CTA holds up the cast and the barrier behind
 // it (68.4 us for that batch; 1 to 3 stages 66.6, 5 stages 66.8).  Before the second barrier the whole ring pays: 66.6 us,
