@@ -322,6 +322,64 @@ btx_status btx_mx4_moe_forward(const btx_mx4_moe_desc* desc, const void* x, cons
                                const void* w13_codes, const void* w13_scales, const void* w2_codes,
                                const void* w2_scales, void* y, void* workspace, size_t workspace_bytes, void* stream);
 
+/* FP8 (OCP e4m3: a sign, four bits of exponent, three of significand, at most 448, no infinities) with one power-of-two
+ * scale for 128 elements: activations, gradients and 8-bit weights of the products below.  A matrix of `rows` rows of K elements
+ * (any numbers), or a batch of them, is held as
+ *   codes   [batch][rows][P] bytes, P = K rounded up to a multiple of 16; those past K are 0;
+ *   scales  [batch][ceil(rows/128)][ceil(K/512)][512] bytes: byte (r % 32) * 16 + (r / 32 % 4) * 4 + j of a tile is the
+ *           scale 2^(b - 127) of elements 128 (4c + j) .. of row r (255: the block is NaN).  Square blocks (below) repeat
+ *           theirs in each of their rows.  Bytes past the last row and the last block are not read.
+ * btx_fp8_sizes gives the bytes of both (either pointer may be NULL); both are 16-byte aligned.  Rows and K are at
+ * most 2^30, the codes of a matrix less than 2^40 bytes.
+ *
+ * btx_fp8_quantize casts src[batch][rows][K] (dtype, rows `row_stride` and matrices `batch_stride` elements apart, elements of a
+ * row contiguous): the scale is the smallest 2^e, e >= -127, with max|x| / 2^e <= 448 over the block; elements go to the
+ * nearest value, ties to the even code; a block that holds an infinity or NaN becomes NaN.  Two outputs, either may be NULL:
+ *   codes, scales      the matrix as it stands; row r goes to row row_first + r * row_step of a matrix of out_rows rows, as in
+ *                      btx_mx4_quantize.  block_rows = 1: a block is 128 elements of a row; 128: 128 x 128 elements (fewer
+ *                      at the ends), rows counted in src.
+ *   codes_t, scales_t  [batch][K][rows], the transpose: block_rows = 1: a block is 128 elements of a column of src, for
+ *                      products that sum over rows; 128: the transpose of the square-block cast, value for value.
+ * Bytes of rows that the call does not name are left as they were, and so are scale bytes past the last row and block.
+ * btx_fp8_dequantize gives the values, dst[batch][rows][K] (contiguous): exactly, but where dtype has no such numbers
+ * (2^128, to which elements above 1.9375 * 2^127 go, is read as infinity; in BF16 values below 2^-133 are rounded). */
+btx_status btx_fp8_sizes(int32_t batch, int32_t rows, int32_t K, size_t* code_bytes, size_t* scale_bytes);
+btx_status btx_fp8_quantize(int32_t dtype, const void* src, int64_t row_stride, int64_t batch_stride, int32_t batch,
+                            int32_t rows, int32_t K, int32_t block_rows, int32_t out_rows, int32_t row_first,
+                            int32_t row_step, void* codes, void* scales, void* codes_t, void* scales_t, void* stream);
+btx_status btx_fp8_dequantize(int32_t dtype, const void* codes, const void* scales, int32_t batch, int32_t rows,
+                              int32_t K, void* dst, void* stream);
+
+/* Root-mean-square norm in front of the sublayer, with the residual's addition:
+ *   h = x + residual, rounded to dtype (residual NULL: h = x);   y = h / sqrt(mean(h^2) + eps) * weight,
+ * formed in fp32 and rounded once.  weight[d] in dtype, NULL: ones.  Outputs, each NULL to skip, one at least: h and y in
+ * dtype; codes and scales: y in FP8 (block_rows = 1) from its fp32 values, for the products of FP8 matrices.
+ * Rows are `*_stride` elements apart (at least d_model, the elements of a row contiguous) and need the alignment of their
+ * elements; rows on 16-byte boundaries are moved fastest.  h may be x or residual itself (same address and stride: the
+ * residual stream is updated in place), y may be x where h is not.  A row has at most 64 KB (32768 elements in BF16, 16384
+ * in F32); eps >= 0, T may be 0.  No workspace.  A row whose sum of squares passes the largest fp32 number has y = 0; rows
+ * do not affect one another. */
+typedef struct {
+  int32_t T, d_model;
+  int32_t dtype;              /* btx_dtype */
+  float   eps;
+} btx_norm_desc;
+btx_status btx_rms_norm(const btx_norm_desc* desc, const void* x, int64_t x_stride, const void* residual,
+                        int64_t residual_stride, const void* weight, void* h, int64_t h_stride, void* y, int64_t y_stride,
+                        void* codes, void* scales, void* stream);
+
+/* Gradients of btx_rms_norm from dy (with respect to y; the cast to FP8 is passed over) and dh (what reaches h from
+ * elsewhere; NULL: nothing):  with s = 1 / sqrt(mean(h^2) + eps), g = dy * weight,
+ *   dx[T,d] = dh + s (g - h s^2 mean(g h)), in dtype: the gradient of x and of residual alike;
+ *   dweight[d] = sum over rows of dy * h * s, fp32 (NULL: not wanted); accumulate = 1 adds to it.
+ * h is the h of the forward call (x where there was no residual).  Sums are fp32, in an order that repeats from run to
+ * run.  dx may be dy, dh or h itself (same address and stride).  T = 0 leaves dweight 0 (accumulate: as it was). */
+btx_status btx_rms_norm_backward_workspace_size(const btx_norm_desc* desc, size_t* workspace_bytes);
+btx_status btx_rms_norm_backward(const btx_norm_desc* desc, const void* h, int64_t h_stride, const void* weight,
+                                 const void* dy, int64_t dy_stride, const void* dh, int64_t dh_stride, void* dx,
+                                 int64_t dx_stride, float* dweight, int32_t accumulate, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
 /* Synchronises `stream` and reads the status word that kernels of earlier calls left in
  * `workspace`: *device_status (host) is BTX_OK or BTX_ERR_TIMEOUT. */
 btx_status btx_device_status(const void* workspace, void* stream, int32_t* device_status);

@@ -60,11 +60,17 @@ class Mx4MoeDesc(C.Structure):
                 ("dtype", C.c_int32)]
 
 
+class NormDesc(C.Structure):
+    _fields_ = [("T", C.c_int32), ("d_model", C.c_int32), ("dtype", C.c_int32), ("eps", C.c_float)]
+
+
 EXPORTS = ["btx_moe_sizes", "btx_moe_forward", "btx_moe_backward", "btx_moe_step_host",
            "btx_lb_loss_workspace_size", "btx_lb_loss", "btx_lb_loss_noalloc", "btx_merge_workspace_size", "btx_merge", "btx_merge_ffn_workspace_size", "btx_merge_ffn",
            "btx_route", "btx_route_backward",
            "btx_mx4_sizes", "btx_mx4_quantize", "btx_mx4_dequantize", "btx_mx4_matmul_workspace_size", "btx_mx4_matmul",
            "btx_mx4_moe_workspace_size", "btx_mx4_moe_forward",
+           "btx_fp8_sizes", "btx_fp8_quantize", "btx_fp8_dequantize",
+           "btx_rms_norm", "btx_rms_norm_backward_workspace_size", "btx_rms_norm_backward",
            "btx_device_status", "btx_selftest_wait_expiry", "btx_selftest_separate_launches", "btx_set_stage_events", "btx_status_string", "btx_version"]
 
 
@@ -102,6 +108,12 @@ def lib():
         L.btx_mx4_matmul.argtypes = [i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]
         L.btx_mx4_moe_workspace_size.argtypes = [C.POINTER(Mx4MoeDesc), C.POINTER(sz)]
         L.btx_mx4_moe_forward.argtypes = [C.POINTER(Mx4MoeDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.btx_fp8_sizes.argtypes = [i32, i32, i32, C.POINTER(sz), C.POINTER(sz)]
+        L.btx_fp8_quantize.argtypes = [i32, vp, i64, i64] + [i32] * 7 + [vp] * 5
+        L.btx_fp8_dequantize.argtypes = [i32, vp, vp, i32, i32, i32, vp, vp]
+        L.btx_rms_norm.argtypes = [C.POINTER(NormDesc), vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, vp]
+        L.btx_rms_norm_backward_workspace_size.argtypes = [C.POINTER(NormDesc), C.POINTER(sz)]
+        L.btx_rms_norm_backward.argtypes = [C.POINTER(NormDesc), vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, i32, vp, sz, vp]
         L.btx_device_status.argtypes = [vp, vp, C.POINTER(i32)]
         L.btx_status_string.argtypes = [i32]
         L.btx_status_string.restype = C.c_char_p
@@ -552,6 +564,116 @@ def btx_mx4_moe_forward(desc, x, topk_idx, gates, w13, w2, y, workspace):
     _launch("btx_mx4_moe_forward", dev, C.byref(desc), _arg(x, "x", (T, d), dt, dev),
             _arg(topk_idx, "topk_idx", (T, k), _I32, dev), _arg(gates, "gates", (T, k), _F32, dev), c13, sc13, c2, sc2,
             _arg(y, "y", (T, d), dt, dev), ws, ws_bytes)
+
+
+@dataclass
+class Fp8:
+    """A batch of matrices [batch, rows, K] held as FP8 codes and scale tiles (layout in btx.h)."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    K: int
+
+    @staticmethod
+    def empty(batch, rows, K, device):
+        btx_fp8_sizes(batch, rows, K)
+        return Fp8(torch.empty((batch, rows, (K + 15) // 16 * 16), dtype=_U8, device=device),
+                   torch.empty((batch, (rows + 127) // 128, (K + 511) // 512, 512), dtype=_U8, device=device), K)
+
+    @property
+    def shape(self):
+        b, r, _ = self.codes.shape
+        return b, r, self.K
+
+
+def _fp8(q, name, dev):
+    """Shape (batch, rows, K) and addresses of an Fp8 argument."""
+    codes, scales, K = q.codes, q.scales, q.K
+    batch, rows, pitch = codes.shape
+    if (pitch != (K + 15) // 16 * 16 or codes.dtype is not _U8 or codes.get_device() != dev or not codes.is_contiguous()
+            or scales.dtype is not _U8 or scales.get_device() != dev or not scales.is_contiguous()
+            or scales.shape != (batch, (rows + 127) // 128, (K + 511) // 512, 512)):
+        _arg(codes, name + ".codes", (batch, rows, (K + 15) // 16 * 16), _U8, dev)
+        _arg(scales, name + ".scales", (batch, (rows + 127) // 128, (K + 511) // 512, 512), _U8, dev)
+    return batch, rows, K, codes.data_ptr(), scales.data_ptr()
+
+
+def btx_fp8_sizes(batch, rows, K):
+    """Bytes of the codes and of the scales of a batch of FP8 matrices."""
+    codes, scales = C.c_size_t(0), C.c_size_t(0)
+    s = lib().btx_fp8_sizes(batch, rows, K, C.byref(codes), C.byref(scales))
+    if s != BTX_OK:
+        raise BtxError(s, "btx_fp8_sizes")
+    return codes.value, scales.value
+
+
+def btx_fp8_quantize(src, out, block_rows=1, row_first=0, row_step=1, out_t=None):
+    """src [batch, rows, K] or [rows, K] (contiguous rows, any row and batch stride) cast into the Fp8 `out` (row r becomes row
+    row_first + r * row_step) and, transposed, into the Fp8 `out_t` [batch, K, rows]; either may be None; see btx.h."""
+    dev = _device(src)
+    shape, stride = src.shape, src.stride()
+    if len(shape) == 2:
+        (rows, K), (row_stride, col), batch, batch_stride = shape, stride, 1, 0
+    else:
+        (batch, rows, K), (batch_stride, row_stride, col) = shape, stride
+    out_rows, codes, scales, codes_t, scales_t = rows, None, None, None, None
+    if out is not None:
+        ob, out_rows, oK, codes, scales = _fp8(out, "out", dev)
+        if ob != batch or oK != K:
+            raise ValueError(f"btx: src is {tuple(shape)}, out is {out.shape}")
+    if out_t is not None:
+        *st, codes_t, scales_t = _fp8(out_t, "out_t", dev)
+        if st != [batch, K, rows]:
+            raise ValueError(f"btx: src is {tuple(shape)}, out_t is {out_t.shape}")
+    if col != 1 and K > 1:
+        raise RuntimeError("btx: the rows of src must be contiguous")
+    _launch("btx_fp8_quantize", dev, _dtype_code(src.dtype), src.data_ptr(), row_stride, batch_stride, batch, rows, K, block_rows,
+            out_rows, row_first, row_step, codes, scales, codes_t, scales_t)
+
+
+def btx_fp8_dequantize(q, dst):
+    """The values of the Fp8 `q` into dst (contiguous, [batch, rows, K] or [rows, K] for one matrix)."""
+    dev = _device(dst)
+    batch, rows, K, codes, scales = _fp8(q, "q", dev)
+    shape = (rows, K) if batch == 1 and dst.dim() == 2 else (batch, rows, K)
+    _launch("btx_fp8_dequantize", dev, _dtype_code(dst.dtype), codes, scales, batch, rows, K, _arg(dst, "dst", shape, dst.dtype, dev))
+
+
+def make_norm_desc(T, d_model, dtype, eps=1e-5) -> NormDesc:
+    return NormDesc(T, d_model, _dtype_code(dtype) if isinstance(dtype, torch.dtype) else int(dtype), float(eps))
+
+
+def _opt_rows(t, name, shape, dtype, dev):
+    return (None, 0) if t is None else _rows(t, name, shape, dtype, dev)
+
+
+def btx_rms_norm(desc, x, weight, residual=None, h=None, y=None, q=None):
+    """h = x + residual and its norm, into y and the Fp8 `q` (each None to skip); rows may be strided; see btx.h."""
+    T, d, dt, dev = desc.T, desc.d_model, _DTYPE.get(desc.dtype), _device(x)
+    codes = scales = None
+    if q is not None:
+        *sq, codes, scales = _fp8(q, "q", dev)
+        if sq != [1, T, d]:
+            raise ValueError(f"btx: x is {tuple(x.shape)}, q is {q.shape}")
+    _launch("btx_rms_norm", dev, C.byref(desc), *_rows(x, "x", (T, d), dt, dev), *_opt_rows(residual, "residual", (T, d), dt, dev),
+            _opt(weight, "weight", (d,), dt, dev), *_opt_rows(h, "h", (T, d), dt, dev), *_opt_rows(y, "y", (T, d), dt, dev), codes,
+            scales)
+
+
+def btx_rms_norm_backward_workspace_size(desc):
+    sz = C.c_size_t(0)
+    s = lib().btx_rms_norm_backward_workspace_size(C.byref(desc), C.byref(sz))
+    if s != BTX_OK:
+        raise BtxError(s, "btx_rms_norm_backward_workspace_size")
+    return sz.value
+
+
+def btx_rms_norm_backward(desc, h, weight, dy, dx, dweight, workspace, dh=None, accumulate=False):
+    """Gradients of btx_rms_norm: dx in the tensors' type, dweight fp32 (None: not wanted); see btx.h."""
+    T, d, dt, dev = desc.T, desc.d_model, _DTYPE.get(desc.dtype), _device(h)
+    ws, ws_bytes = _workspace(workspace, dev)
+    _launch("btx_rms_norm_backward", dev, C.byref(desc), *_rows(h, "h", (T, d), dt, dev), _opt(weight, "weight", (d,), dt, dev),
+            *_rows(dy, "dy", (T, d), dt, dev), *_opt_rows(dh, "dh", (T, d), dt, dev), *_rows(dx, "dx", (T, d), dt, dev),
+            _opt(dweight, "dweight", (d,), _F32, dev), int(accumulate), ws, ws_bytes)
 
 
 def btx_selftest_wait_expiry(workspace):

@@ -1,0 +1,133 @@
+// Device code shared by the FP8 kernels: a lane's piece of a row, its largest magnitude, its cast and where scales lie.
+#pragma once
+
+#include <cuda_fp8.h>
+
+#include "btx_fp8.cuh"
+#include "btx_route_dev.cuh"
+
+namespace btx {
+namespace fp8 {
+namespace {
+
+constexpr unsigned kAll = 0xffffffffu;
+
+// N elements of a lane as they were loaded, two of bf16 or one of fp32 per word.
+template <typename T, int N> struct Piece {
+  static constexpr int WORDS = N * (int)sizeof(T) / 4;
+  uint32_t w[WORDS];
+
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) w[i] = 0;
+  }
+  // the first n (any number) of N elements; vec: p is on a 16-byte boundary
+  __device__ __forceinline__ void load(const T* p, int n, bool vec) {
+    if (vec && n >= N) {
+#pragma unroll
+      for (int i = 0; i < WORDS; i += 4) {
+        const uint4 q = __ldcs(reinterpret_cast<const uint4*>(p) + i / 4);
+        w[i] = q.x; w[i + 1] = q.y; w[i + 2] = q.z; w[i + 3] = q.w;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) {
+        if (sizeof(T) == 4) {
+          w[i] = i < n ? __float_as_uint(to_f32(p[i])) : 0u;
+        } else {
+          const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
+          w[i] = (2 * i < n ? (uint32_t)h[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)h[2 * i + 1] << 16 : 0u);
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void store(T* p, int n, bool vec) const {
+    if (vec && n >= N) {
+#pragma unroll
+      for (int i = 0; i < WORDS; i += 4) __stcs(reinterpret_cast<uint4*>(p) + i / 4, make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) {
+        if (sizeof(T) == 4) {
+          if (i < n) reinterpret_cast<uint32_t*>(p)[i] = w[i];
+        } else {
+          uint16_t* h = reinterpret_cast<uint16_t*>(p);
+          if (2 * i < n) h[2 * i] = (uint16_t)w[i];
+          if (2 * i + 1 < n) h[2 * i + 1] = (uint16_t)(w[i] >> 16);
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void values(float (&v)[N]) const {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) {
+      if (sizeof(T) == 4) {
+        v[i] = __uint_as_float(w[i]);
+      } else {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      }
+    }
+  }
+  __device__ __forceinline__ void set(const float (&v)[N]) {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) {
+      if (sizeof(T) == 4) {
+        w[i] = __float_as_uint(v[i]);
+      } else {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&h);
+      }
+    }
+  }
+  // largest magnitude as the bits of a float (NaN and infinities compare above every number)
+  __device__ __forceinline__ uint32_t amax() const {
+    uint32_t m = 0;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) m = max(m, w[i] & 0x7fffffffu);
+      return m;
+    } else {
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
+      return max(m & 0xffff0000u, m << 16);
+    }
+  }
+};
+
+template <int N> __device__ __forceinline__ uint32_t amax_of(const float (&v)[N]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+  return m;
+}
+// the largest over groups of LANES neighbouring lanes
+template <int LANES> __device__ __forceinline__ uint32_t lanes_max(uint32_t m) {
+#pragma unroll
+  for (int o = 1; o < LANES; o <<= 1) m = max(m, __shfl_xor_sync(kAll, m, o));
+  return m;
+}
+
+// four codes; b == 255: a block that is not a number has codes 0
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float inv) {
+  return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a * inv, b * inv), __NV_SATFINITE, __NV_E4M3) |
+         (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(c * inv, d * inv), __NV_SATFINITE, __NV_E4M3) << 16;
+}
+// N codes of a lane's elements, whose block's scale byte is `byte`
+template <int N> __device__ __forceinline__ void cast_codes(const float (&v)[N], uint32_t byte, uint32_t inv_bits, uint32_t (&q)[N / 4]) {
+  const float inv = __uint_as_float(inv_bits);
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i) q[i] = byte == 255u ? 0u : codes4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], inv);
+}
+__device__ __forceinline__ float scale_value(uint32_t byte) {
+  return __uint_as_float(byte == 255u ? 0x7fffffffu : (byte == 0u ? 0x00400000u : byte << 23));
+}
+
+// byte of the scale of row `row` (of a matrix whose first row tile is tile0), elements `block` * 128 ..
+__device__ __forceinline__ size_t scale_offset(size_t tile0, int row, int kt, int block) {
+  return ((tile0 + row / kTileRows) * (size_t)kt + block / 4) * kTileBytes + (row & 31) * 16 + ((row >> 5) & 3) * 4 + (block & 3);
+}
+
+}  // namespace
+}  // namespace fp8
+}  // namespace btx
