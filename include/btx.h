@@ -350,6 +350,37 @@ btx_status btx_fp8_quantize(int32_t dtype, const void* src, int64_t row_stride, 
 btx_status btx_fp8_dequantize(int32_t dtype, const void* codes, const void* scales, int32_t batch, int32_t rows,
                               int32_t K, void* dst, void* stream);
 
+/* y[batch][M][N] (dtype, contiguous) = A B^T of A[batch][M][K] and B[batch][N][K], both FP8 of either block_rows: products of
+ * the values, fp32 accumulation, one rounding; accumulate = 1 (dtype F32 only) adds to the y that is there.  M, N and K are
+ * any sizes (M or batch 0: nothing to do).  A linear layer y = x W^T takes x by rows and W[N][K] by square blocks; its
+ * gradients are the same call: dx = dy W from dy by rows and the codes_t of W, dW = dy^T x from the codes_t of dy and of x
+ * (rows of 128 tokens' scales).  The workspace serves one call at a time.  Results repeat from run to run.  How many parts
+ * the contraction is split into, and so the order in which an element's fp32 sum is formed, depends on batch, M, N and K:
+ * rows of calls of other sizes agree within that rounding only. */
+btx_status btx_fp8_matmul_workspace_size(int32_t dtype, int32_t batch, int32_t M, int32_t N, int32_t K,
+                                         size_t* workspace_bytes);
+btx_status btx_fp8_matmul(int32_t dtype, int32_t batch, int32_t M, int32_t N, int32_t K, const void* a_codes,
+                          const void* a_scales, const void* b_codes, const void* b_scales, void* y, int32_t accumulate,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* The expert layer of btx_moe_forward (Section 3.2) on FP8 experts under a routing from elsewhere, e.g. btx_route's:
+ *   y_t = sum over slots j of gates[t,j] * W2_e a,  a = fp8(silu(W1_e fp8(x_t)) * W3_e fp8(x_t)),  e = topk_idx[t,j].
+ * Activations are cast by rows in front of both products, products are formed in fp32, silu in fp32 from the fast
+ * exponential (for x in fp32 too: within (4 + 1.2 |h|) 2^-23 of silu(h)), slots are added in fp32 in slot order, y is rounded once.
+ *   x[T,d] in dtype, or with x_scales the codes and scales of its FP8 form by rows (btx_rms_norm's, say; NULL: x is in
+ *   dtype); y[T,d] in dtype; topk_idx[T,k] int32 (an index outside 0..E-1 is an empty slot: it adds nothing); gates[T,k]
+ *   fp32; w13: E matrices of 2F rows of d, row 2i is row i of W1_e and row 2i + 1 row i of W3_e; w2: E matrices of d rows of F.
+ * d and F are multiples of 16, E <= 512, T may be 0.  E = 1 with one slot is the dense gated block.  Inference: there is no
+ * gradient.  Results repeat from run to run; as in btx_mx4_moe_forward a token's last bits may depend on the batch around it. */
+typedef struct {
+  int32_t T, d_model, d_ff, E, k;
+  int32_t dtype;              /* btx_dtype of x and y */
+} btx_fp8_moe_desc;
+btx_status btx_fp8_moe_workspace_size(const btx_fp8_moe_desc* desc, size_t* workspace_bytes);
+btx_status btx_fp8_moe_forward(const btx_fp8_moe_desc* desc, const void* x, const void* x_scales, const int32_t* topk_idx,
+                               const float* gates, const void* w13_codes, const void* w13_scales, const void* w2_codes,
+                               const void* w2_scales, void* y, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Root-mean-square norm in front of the sublayer, with the residual's addition:
  *   h = x + residual, rounded to dtype (residual NULL: h = x);   y = h / sqrt(mean(h^2) + eps) * weight,
  * formed in fp32 and rounded once.  weight[d] in dtype, NULL: ones.  Outputs, each NULL to skip, one at least: h and y in

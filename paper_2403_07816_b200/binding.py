@@ -60,6 +60,10 @@ class Mx4MoeDesc(C.Structure):
                 ("dtype", C.c_int32)]
 
 
+class Fp8MoeDesc(C.Structure):
+    _fields_ = Mx4MoeDesc._fields_
+
+
 class NormDesc(C.Structure):
     _fields_ = [("T", C.c_int32), ("d_model", C.c_int32), ("dtype", C.c_int32), ("eps", C.c_float)]
 
@@ -69,7 +73,8 @@ EXPORTS = ["btx_moe_sizes", "btx_moe_forward", "btx_moe_backward", "btx_moe_step
            "btx_route", "btx_route_backward",
            "btx_mx4_sizes", "btx_mx4_quantize", "btx_mx4_dequantize", "btx_mx4_matmul_workspace_size", "btx_mx4_matmul",
            "btx_mx4_moe_workspace_size", "btx_mx4_moe_forward",
-           "btx_fp8_sizes", "btx_fp8_quantize", "btx_fp8_dequantize",
+           "btx_fp8_sizes", "btx_fp8_quantize", "btx_fp8_dequantize", "btx_fp8_matmul_workspace_size", "btx_fp8_matmul",
+           "btx_fp8_moe_workspace_size", "btx_fp8_moe_forward",
            "btx_rms_norm", "btx_rms_norm_backward_workspace_size", "btx_rms_norm_backward",
            "btx_device_status", "btx_selftest_wait_expiry", "btx_selftest_separate_launches", "btx_set_stage_events", "btx_status_string", "btx_version"]
 
@@ -111,6 +116,10 @@ def lib():
         L.btx_fp8_sizes.argtypes = [i32, i32, i32, C.POINTER(sz), C.POINTER(sz)]
         L.btx_fp8_quantize.argtypes = [i32, vp, i64, i64] + [i32] * 7 + [vp] * 5
         L.btx_fp8_dequantize.argtypes = [i32, vp, vp, i32, i32, i32, vp, vp]
+        L.btx_fp8_matmul_workspace_size.argtypes = [i32, i32, i32, i32, i32, C.POINTER(sz)]
+        L.btx_fp8_matmul.argtypes = [i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, i32, vp, sz, vp]
+        L.btx_fp8_moe_workspace_size.argtypes = [C.POINTER(Fp8MoeDesc), C.POINTER(sz)]
+        L.btx_fp8_moe_forward.argtypes = [C.POINTER(Fp8MoeDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.btx_rms_norm.argtypes = [C.POINTER(NormDesc), vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, vp]
         L.btx_rms_norm_backward_workspace_size.argtypes = [C.POINTER(NormDesc), C.POINTER(sz)]
         L.btx_rms_norm_backward.argtypes = [C.POINTER(NormDesc), vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, i32, vp, sz, vp]
@@ -636,6 +645,59 @@ def btx_fp8_dequantize(q, dst):
     batch, rows, K, codes, scales = _fp8(q, "q", dev)
     shape = (rows, K) if batch == 1 and dst.dim() == 2 else (batch, rows, K)
     _launch("btx_fp8_dequantize", dev, _dtype_code(dst.dtype), codes, scales, batch, rows, K, _arg(dst, "dst", shape, dst.dtype, dev))
+
+
+def btx_fp8_matmul_workspace_size(M, N, K, dtype, batch=1):
+    sz = C.c_size_t(0)
+    s = lib().btx_fp8_matmul_workspace_size(_dtype_code(dtype), batch, M, N, K, C.byref(sz))
+    if s != BTX_OK:
+        raise BtxError(s, "btx_fp8_matmul_workspace_size")
+    return sz.value
+
+
+def btx_fp8_matmul(a, b, y, workspace, accumulate=False):
+    """y = a b^T (fp32 y: or added to y) of two Fp8 of the same batch and K; y is [batch, M, N], or [M, N] for one matrix."""
+    dev = _device(y)
+    batch, M, K, ac, asc = _fp8(a, "a", dev)
+    bb, N, bK, bc, bsc = _fp8(b, "b", dev)
+    if bb != batch or bK != K:
+        raise ValueError(f"btx: a is {a.shape}, b is {b.shape}")
+    shape = (M, N) if batch == 1 and y.dim() == 2 else (batch, M, N)
+    ws, ws_bytes = _workspace(workspace, dev)
+    _launch("btx_fp8_matmul", dev, _dtype_code(y.dtype), batch, M, N, K, ac, asc, bc, bsc, _arg(y, "y", shape, y.dtype, dev),
+            int(accumulate), ws, ws_bytes)
+
+
+def make_fp8_moe_desc(T, d_model, d_ff, E, k, dtype) -> Fp8MoeDesc:
+    return Fp8MoeDesc(T, d_model, d_ff, E, k, _dtype_code(dtype) if isinstance(dtype, torch.dtype) else int(dtype))
+
+
+def btx_fp8_moe_workspace_size(desc):
+    sz = C.c_size_t(0)
+    s = lib().btx_fp8_moe_workspace_size(C.byref(desc), C.byref(sz))
+    if s != BTX_OK:
+        raise BtxError(s, "btx_fp8_moe_workspace_size")
+    return sz.value
+
+
+def btx_fp8_moe_forward(desc, x, topk_idx, gates, w13, w2, y, workspace):
+    """The expert layer on FP8 experts under a given routing; x is a tensor or an Fp8 of its rows, w13 holds the rows of W1
+    and W3 in turn; see btx.h."""
+    T, d, F, E, k, dev = desc.T, desc.d_model, desc.d_ff, desc.E, desc.k, _device(y)
+    dt, x_scales = _DTYPE.get(desc.dtype), None
+    if isinstance(x, Fp8):
+        *sx, x, x_scales = _fp8(x, "x", dev)
+        if sx != [1, T, d]:
+            raise ValueError(f"btx: x is {tuple(sx)}; the layer has T, d_model = {T}, {d}")
+    else:
+        x = _arg(x, "x", (T, d), dt, dev)
+    *s13, c13, sc13 = _fp8(w13, "w13", dev)
+    *s2, c2, sc2 = _fp8(w2, "w2", dev)
+    if s13 != [E, 2 * F, d] or s2 != [E, d, F]:
+        raise ValueError(f"btx: w13 is {w13.shape}, w2 is {w2.shape}; the layer has E, d_ff, d_model = {E}, {F}, {d}")
+    ws, ws_bytes = _workspace(workspace, dev)
+    _launch("btx_fp8_moe_forward", dev, C.byref(desc), x, x_scales, _arg(topk_idx, "topk_idx", (T, k), _I32, dev),
+            _arg(gates, "gates", (T, k), _F32, dev), c13, sc13, c2, sc2, _arg(y, "y", (T, d), dt, dev), ws, ws_bytes)
 
 
 def make_norm_desc(T, d_model, dtype, eps=1e-5) -> NormDesc:

@@ -6,7 +6,9 @@
 //                   elements a thread), which gives the largest of its rows, of its columns or of all; x is read once
 //                   for both outputs.  Transposed codes turn through shared memory, 8 bytes (of 8 rows) at a time
 //   dequantize      the mapping of quantize_rows backwards
+//   dispatch_rows   quantize_rows of the expert layer's tokens, or a copy of their FP8 form, to the k rows of every token
 #include "btx_fp8_dev.cuh"
+#include "btx_fp8_gemm.cuh"
 
 namespace btx {
 namespace fp8 {
@@ -201,6 +203,61 @@ dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__
   }
 }
 
+// T: type of x, or uint8_t where x is FP8 already (its scales in tiles of their own).  d is a multiple of 16.
+template <typename T, typename I>
+__global__ void __launch_bounds__(kThreads)
+dispatch_rows_kernel(const mx4::Dispatch q, const T* __restrict__ x, const uint8_t* __restrict__ x_scales, uint8_t* __restrict__ codes,
+                     uint8_t* __restrict__ scales, I items, int groups) {
+  const int lane = threadIdx.x & 31;
+  const int kt = (int)scale_tiles_k(q.d);
+  allow_dependents();
+  grid_dependency_wait();
+  for (I w = ((I)blockIdx.x * kThreads + threadIdx.x) >> 5; w < items; w += (I)gridDim.x * (kThreads / 32)) {
+    const size_t t = (size_t)(w / (I)groups);
+    const int g = (int)(w - (I)t * (I)groups);
+    const int c0 = g * kUnroll * 256 + lane * 8;
+    const T* from = x + t * q.d + c0;
+    uint2 code[kUnroll];
+    uint32_t byte[kUnroll];
+    if constexpr (sizeof(T) == 1) {
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        code[u] = make_uint2(0, 0); byte[u] = 0;
+        if (c0 + u * 256 < q.d) {
+          code[u] = __ldcs(reinterpret_cast<const uint2*>(from + u * 256));
+          byte[u] = x_scales[scale_offset(0, (int)t, kt, (c0 + u * 256) / kBlock)];
+        }
+      }
+    } else {
+      Piece<T, 8> v[kUnroll];
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) v[u].load(from + u * 256, q.d - (c0 + u * 256), true);
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        uint32_t inv, out[2];
+        float f[8];
+        byte[u] = scale_byte(lanes_max<16>(v[u].amax()), inv);
+        v[u].values(f);
+        cast_codes(f, byte[u], inv, out);
+        code[u] = make_uint2(out[0], out[1]);
+      }
+    }
+    for (int j = 0; j < q.k; ++j) {
+      const int row = q.flat2row[t * q.k + j];
+      if (row < 0) continue;
+      uint8_t* to = codes + (size_t)row * q.d + c0;
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        const int c = c0 + u * 256;
+        if (c < q.d) {
+          *reinterpret_cast<uint2*>(to + u * 256) = code[u];
+          if ((lane & 15) == 0) scales[scale_offset(0, row, kt, c / kBlock)] = (uint8_t)byte[u];
+        }
+      }
+    }
+  }
+}
+
 int cast_blocks(long long items) {
   const long long want = (items + kThreads / 32 - 1) / (kThreads / 32), most = 32ll * sm_count();
   return (int)(want < most ? want : most);
@@ -239,7 +296,24 @@ cudaError_t dequantize(const uint8_t* codes, const uint8_t* scales, int batch, i
   });
 }
 
+template <typename T>
+cudaError_t dispatch_rows(const mx4::Dispatch& q, const T* x, const uint8_t* x_scales, uint8_t* codes, uint8_t* scales, cudaStream_t st) {
+  const int groups = cast_groups(q.d);
+  const long long items = (long long)q.T * groups;
+  return by_index(items, [&](auto n) {
+    return launch_after_predecessor(dispatch_rows_kernel<T, decltype(n)>, dim3(cast_blocks(items)), dim3(kThreads), 0, st, true, q, x,
+                                    x_scales, codes, scales, n, groups);
+  });
+}
+
 }  // namespace
+
+cudaError_t launch_dispatch_rows(const mx4::Dispatch& q, int dtype, const void* x, const uint8_t* x_scales, uint8_t* codes,
+                                 uint8_t* scales, cudaStream_t st) {
+  if (x_scales != nullptr) return dispatch_rows(q, (const uint8_t*)x, x_scales, codes, scales, st);
+  return dtype == BTX_BF16 ? dispatch_rows(q, (const __nv_bfloat16*)x, x_scales, codes, scales, st)
+                           : dispatch_rows(q, (const float*)x, x_scales, codes, scales, st);
+}
 
 cudaError_t launch_quantize(const CastParams& p, int dtype, cudaStream_t st) {
   return dtype == BTX_BF16 ? quantize<__nv_bfloat16>(p, st) : quantize<float>(p, st);

@@ -75,6 +75,39 @@ def test_norm_refusals(L):
     assert L.btx_rms_norm_backward_workspace_size(mk(), None) == 1
 
 
+def test_product_and_layer_refusals(L):
+    sz = C.c_size_t(0)
+    mm = lambda *a: L.btx_fp8_matmul(*a, None)
+    assert mm(0, 1, 8, 8, 48, A, A, A, A, A, 0, A, 64) == 3
+    for bad in ((2, 1, 8, 8, 64), (0, -1, 8, 8, 64), (0, 1, -1, 8, 64), (0, 1, 8, 0, 64), (0, 1, 8, 8, 0)):
+        assert mm(*bad, A, A, A, A, A, 0, A, 256) == 1 and L.btx_fp8_matmul_workspace_size(*bad, C.byref(sz)) == 1
+    for i in range(5):
+        for wrong in (None, OFF):
+            ptr = [A] * 5
+            ptr[i] = wrong
+            assert mm(0, 1, 8, 8, 64, *ptr, 0, A, 256) == 1
+    assert mm(0, 1, 8, 8, 64, A, A, A, A, A, 0, None, 256) == 1 and mm(0, 1, 8, 8, 64, A, A, A, A, A, 0, OFF, 256) == 1
+    assert mm(1, 1, 8, 8, 64, A, A, A, A, A, 1, A, 256) == 2                    # adding to bf16
+    assert mm(0, 1, 1 << 30, 1 << 30, 64, A, A, A, A, A, 0, A, 256) == 2
+    for M, N, K in ((BIG, 1, 32), (1, BIG, 32), (1, 1, BIG)):
+        assert mm(0, 1, M, N, K, A, A, A, A, A, 0, A, 256) == 2
+    assert mm(0, 1, 0, 8, 64, None, None, None, None, None, 0, None, 0) == 0
+    mk = lambda T=4, d=64, f=96, E=4, k=2, dt=torch.float32: C.byref(B.make_fp8_moe_desc(T, d, f, E, k, dt))
+    run = lambda desc, *ptr, n=1 << 40: L.btx_fp8_moe_forward(desc, *ptr, n, None)
+    good = [A, None, A, A, A, A, A, A, A, A]
+    for bad, status in ((mk(k=5), 1), (mk(d=24), 2), (mk(f=40), 2), (mk(E=513), 2), (mk(T=-1), 1), (mk(dt=9), 1), (mk(d=BIG + 16), 2),
+                        (mk(d=16, f=1 << 30), 2), (mk(T=1 << 28), 2), (mk(d=1 << 20, f=1 << 20, E=1, k=1), 2)):
+        assert L.btx_fp8_moe_workspace_size(bad, C.byref(sz)) == status and run(bad, *good) == status
+    assert run(mk(), *good, n=16) == 3
+    for i in range(10):
+        for wrong in (None, C.c_void_p(4098)):
+            ptr = list(good)
+            ptr[i] = wrong
+            if not (i == 1 and wrong is None):
+                assert run(mk(), *ptr) == 1, i
+    assert run(mk(T=0), *[None] * 10, n=0) == 0
+
+
 # ---- the statements ----
 @pytest.mark.parametrize("std", [1e-42, 1e-30, 0.02, 1.0, 3e37])
 def test_cast_is_the_nearest_value_of_the_blocks_grid(std):
