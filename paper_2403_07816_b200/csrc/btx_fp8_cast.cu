@@ -1,12 +1,16 @@
 // FP8 casts: one power-of-two scale for 128 elements of a row, or for a block of 128 x 128.
 //
-//   quantize_rows   a scale per row and 128 elements, as the rows stand: sixteen lanes share a block, eight elements each, the
-//                   maximum takes four shuffles
-//   quantize_tiles  square blocks and transposed outputs: a block of threads holds a 128 x 128 tile in registers (8 rows of 8
-//                   elements a thread), which gives the largest of its rows, of its columns or of all; x is read once
-//                   for both outputs.  Transposed codes turn through shared memory, 8 bytes (of 8 rows) at a time
+//   quantize_rows   a scale per row and 128 elements, as the rows stand: a warp takes 256 elements at a time
+//   quantize_tiles  square blocks and transposed outputs: a block of threads works on 128 x 128 tiles, eight neighbouring rows
+//                   of 16 bytes a thread, which gives the largest of its rows, of its columns or of all; x is read once for
+//                   both outputs.  The next tile is on its way meanwhile (cp.async into the thread's own places in shared
+//                   memory).  Transposed codes turn through shared memory, 8 bytes (of 8 rows) at a time
 //   dequantize      the mapping of quantize_rows backwards
 //   dispatch_rows   quantize_rows of the expert layer's tokens, or a copy of their FP8 form, to the k rows of every token
+//
+// VEC: rows start on 16-byte boundaries and hold whole vectors; otherwise they are read element by element, by the same lanes.
+#include <atomic>
+
 #include "btx_fp8_dev.cuh"
 #include "btx_fp8_gemm.cuh"
 
@@ -17,9 +21,10 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kUnroll = 4;                 // 256-element chunks a warp has in flight
 
-template <typename T, typename I>
+// A warp takes kUnroll chunks of 256 elements of one row at a time, eight neighbours a lane: sixteen lanes share a block.
+template <typename T, bool VEC, typename I>
 __global__ void __launch_bounds__(kThreads)
-quantize_rows_kernel(const CastParams p, int vec, I items, int groups) {
+quantize_rows_kernel(const __grid_constant__ CastParams p, I items, int groups) {
   const int lane = threadIdx.x & 31;
   const int kt = (int)scale_tiles_k(p.K), pitch = (int)row_pitch(p.K);
   const size_t tiles = (size_t)row_tiles(p.out_rows);
@@ -29,137 +34,218 @@ quantize_rows_kernel(const CastParams p, int vec, I items, int groups) {
     const I r = w / (I)groups;
     const int g = (int)(w - r * (I)groups);
     const int b = (int)(r / (I)p.rows), row = (int)(r - (I)b * (I)p.rows);
-    const T* src = (const T*)p.src + b * p.batch_stride + row * p.row_stride;
     const int out_row = p.first + row * p.step;
-    const int c0 = g * kUnroll * 256 + lane * 8;
+    const int c0 = g * kUnroll * 256 + lane * 8, left = p.K - c0;
+    const T* src = (const T*)p.src + b * p.batch_stride + row * p.row_stride + c0;
+    uint8_t* codes = p.codes + ((size_t)b * p.out_rows + out_row) * pitch + c0;
+    uint8_t* scales = p.scales + scale_offset(b * tiles, out_row, kt, g * kUnroll * 2);    // (two scale tiles, eight blocks)
     Piece<T, 8> x[kUnroll];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) x[u].load(src + c0 + u * 256, p.K - (c0 + u * 256), vec != 0);
-    uint8_t* codes = p.codes + ((size_t)b * p.out_rows + out_row) * pitch + c0;
+    for (int u = 0; u < kUnroll; ++u) {
+      if (u * 256 < left) x[u].load(src + u * 256, VEC ? 8 : left - u * 256, VEC);
+      else x[u].zero();
+    }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      const int c = c0 + u * 256;
       uint32_t inv, q[2];
       const uint32_t byte = scale_byte(lanes_max<16>(x[u].amax()), inv);
       float v[8];
       x[u].values(v);
       cast_codes(v, byte, inv, q);
-      if (c < pitch) *reinterpret_cast<uint2*>(codes + u * 256) = make_uint2(q[0], q[1]);
-      if ((lane & 15) == 0 && c < p.K) p.scales[scale_offset(b * tiles, out_row, kt, c / kBlock)] = (uint8_t)byte;
+      if (u * 256 < left + pitch - p.K) *reinterpret_cast<uint2*>(codes + u * 256) = make_uint2(q[0], q[1]);
+      if ((lane & 15) == 0 && u * 256 < left) scales[(u >> 1) * kTileBytes + (u & 1) * 2 + (lane >> 4)] = (uint8_t)byte;
     }
   }
 }
 
-// A thread's eight rows are neighbours: rows rg * 8 .. of its eight columns cg * 8 ..
-template <typename T>
-__global__ void __launch_bounds__(kThreads)
-quantize_tiles_kernel(const CastParams p, int vec, long long items, int col_tiles) {
-  __shared__ __align__(16) uint8_t turned[128 * 128];
-  __shared__ uint32_t part[8][128];        // largest of every column over a warp's 16 rows (square: [warp][0], of all)
+// Threads of a tile: 16 groups of eight rows, 16 bytes of a row each.
+template <typename T> struct Tile {
+  static constexpr int VN = 16 / (int)sizeof(T), LANES = 128 / VN, THREADS = 16 * LANES, STAGES = 2;
+  static constexpr int STAGE_BYTES = THREADS * 8 * 16, SMEM = STAGES * STAGE_BYTES + 128 * 128;
+};
+
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(Tile<T>::THREADS)
+quantize_tiles_kernel(const __grid_constant__ CastParams p, long long items, int col_tiles, int words) {
+  using G = Tile<T>;
+  constexpr int VN = G::VN, LANES = G::LANES, WARPS = G::THREADS / 32;
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ float part[WARPS][128];       // largest of every column over a warp's rows
+  __shared__ uint32_t whole[2][WARPS];     // of a square block, for tiles in turn
   __shared__ uint32_t inv_of[128];
-  __shared__ uint8_t byte_of[128];
+  __shared__ uint8_t byte_of[128], row_byte[128];
+  uint8_t* turned = smem + G::STAGES * G::STAGE_BYTES;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int cg = tid & 15, rg = tid >> 4;
+  const int cg = tid % LANES, rg = tid / LANES;
   const int kt = (int)scale_tiles_k(p.K), pitch = (int)row_pitch(p.K);
   const int kt_t = (int)scale_tiles_k(p.rows), pitch_t = (int)row_pitch(p.rows);
   const size_t tiles = (size_t)row_tiles(p.out_rows), tiles_t = (size_t)row_tiles(p.K);
   const long long per = (long long)col_tiles * row_tiles(p.rows);
+  const uint32_t places = (uint32_t)__cvta_generic_to_shared(smem) + tid * 16;
+  auto place = [&](int stage, int i) { return places + stage * G::STAGE_BYTES + i * G::THREADS * 16; };
   allow_dependents();
   grid_dependency_wait();
-  for (long long it = blockIdx.x; it < items; it += gridDim.x) {
-    const int b = (int)(it / per);
-    const int rt = (int)((it - b * per) / col_tiles), ct = (int)(it - b * per - (long long)rt * col_tiles);
-    const int r0 = rt * 128 + rg * 8, c0 = ct * 128 + cg * 8;
-    const T* src = (const T*)p.src + b * p.batch_stride + r0 * p.row_stride + c0;
-    Piece<T, 8> x[8];
+
+  auto locate = [&](long long it, int& b, int& rt, int& ct) {
+    b = (int)(it / per);
+    rt = (int)((it - b * per) / col_tiles);
+    ct = (int)(it - b * per - (long long)rt * col_tiles);
+  };
+  auto fetch = [&](int stage, long long it) {
+    if (it < items) {
+      int b, rt, ct;
+      locate(it, b, rt, ct);
+      const int r0 = rt * 128 + rg * 8, left = max(0, p.K - ct * 128 - cg * VN);       // elements of a row from here on
+      const T* src = (const T*)p.src + b * p.batch_stride + r0 * p.row_stride + ct * 128 + cg * VN;
+      if (VEC || words) {                    // copies of 16 or 4 bytes; nothing is read where the size is 0
+        const int bytes = min(16, left * (int)sizeof(T));
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (r0 + i < p.rows) x[i].load(src + i * p.row_stride, p.K - c0, vec != 0);
-      else x[i].zero();
+        for (int i = 0; i < 8; ++i) {
+          const int n = r0 + i < p.rows ? bytes : 0;
+          const uint8_t* from = n > 0 ? reinterpret_cast<const uint8_t*>(src + i * p.row_stride) : reinterpret_cast<const uint8_t*>(p.src);
+          if (VEC) {
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(place(stage, i)), "l"(from), "r"(n) : "memory");
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(place(stage, i) + 4 * k), "l"(4 * k < n ? from + 4 * k : from), "r"(4 * k < n ? 4 : 0) : "memory");
+          }
+        }
+      } else {
+        Piece<T, VN> q[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i].load(src + i * p.row_stride, r0 + i < p.rows ? left : 0, false);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(place(stage, i)), "r"(q[i].w[0]), "r"(q[i].w[1]), "r"(q[i].w[2]),
+                       "r"(q[i].w[3]) : "memory");
+      }
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  auto read = [&](int stage, int i, Piece<T, VN>& q) {
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(q.w[0]), "=r"(q.w[1]), "=r"(q.w[2]), "=r"(q.w[3]) : "r"(place(stage, i)) : "memory");
+  };
+
+  fetch(0, blockIdx.x);
+  int stage = 0;
+  for (long long it = blockIdx.x; it < items; it += gridDim.x, stage ^= 1) {
+    fetch(stage ^ 1, it + gridDim.x);
+    asm volatile("cp.async.wait_group %0;" ::"n"(G::STAGES - 1) : "memory");
+    int b, rt, ct;
+    locate(it, b, rt, ct);
+    const int r0 = rt * 128 + rg * 8, c0 = ct * 128;
     uint32_t byte = 0, inv = 0;              // square: of the tile
     if (p.square) {
       uint32_t m = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) m = max(m, x[i].amax());
+      for (int i = 0; i < 8; ++i) {
+        Piece<T, VN> x;
+        read(stage, i, x);
+        m = max(m, x.amax());
+      }
       m = __reduce_max_sync(kAll, m);
-      if (lane == 0) part[warp][0] = m;
+      if (lane == 0) whole[stage][warp] = m;
       __syncthreads();
-#pragma unroll
-      for (int i = 0; i < 8; ++i) m = max(m, part[i][0]);
+      m = __reduce_max_sync(kAll, whole[stage][lane % WARPS]);
       byte = scale_byte(m, inv);
     }
+    float most[VN];                          // of the thread's columns
+#pragma unroll
+    for (int j = 0; j < VN; ++j) most[j] = 0.f;
     if (p.codes != nullptr) {
+      uint8_t* to = p.codes + ((size_t)b * p.out_rows + p.first + (size_t)r0 * p.step) * pitch + c0 + cg * VN;
+      const size_t next = (size_t)p.step * pitch;
+      const int n = c0 + cg * VN < pitch ? p.rows - r0 : 0;                              // rows to write
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        uint32_t bi = byte, vi = inv, q[2];
-        if (!p.square) bi = scale_byte(lanes_max<16>(x[i].amax()), vi);
-        float v[8];
-        x[i].values(v);
-        cast_codes(v, bi, vi, q);
-        if (r0 + i < p.rows) {
-          const int row = p.first + (r0 + i) * p.step;
-          if (c0 < pitch) *reinterpret_cast<uint2*>(p.codes + ((size_t)b * p.out_rows + row) * pitch + c0) = make_uint2(q[0], q[1]);
-          if (cg == 0) p.scales[scale_offset(b * tiles, row, kt, ct)] = (uint8_t)bi;
+        Piece<T, VN> x;
+        float v[VN];
+        read(stage, i, x);
+        x.values(v);
+        uint32_t bi = byte, vi = inv, q[VN / 4];
+        if (!p.square) {
+#pragma unroll
+          for (int j = 0; j < VN; ++j) most[j] = max_abs(most[j], v[j]);
+          bi = scale_byte(lanes_max<LANES>(x.amax()), vi);
+          if (cg == 0) row_byte[rg * 8 + i] = (uint8_t)bi;
         }
+        cast_codes(v, bi, vi, q);
+        if (i < n) {
+          if constexpr (VN == 8) *reinterpret_cast<uint2*>(to + i * next) = make_uint2(q[0], q[1]);
+          else *reinterpret_cast<uint32_t*>(to + i * next) = q[0];
+        }
+      }
+    } else if (!p.square) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        Piece<T, VN> x;
+        float v[VN];
+        read(stage, i, x);
+        x.values(v);
+#pragma unroll
+        for (int j = 0; j < VN; ++j) most[j] = max_abs(most[j], v[j]);
       }
     }
-    if (p.codes_t != nullptr) {
-      float v[8][8];
+    if (!p.square) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i].values(v[i]);
-      if (!p.square) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          uint32_t m = 0;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i][j]) & 0x7fffffffu);
-          m = max(m, __shfl_xor_sync(kAll, m, 16));
-          if (lane < 16) part[warp][cg * 8 + j] = m;
-        }
-        __syncthreads();
-        if (tid < 128) {
-          uint32_t m = 0;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) m = max(m, part[i][tid]);
-          uint32_t iv;
-          byte_of[tid] = (uint8_t)scale_byte(m, iv);
-          inv_of[tid] = iv;
-        }
-        __syncthreads();
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int col = cg * 8 + j;
-        const uint32_t bj = p.square ? byte : byte_of[col], vj = p.square ? inv : inv_of[col];
-        float t[8];
-        uint32_t q[2];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) t[i] = v[i][j];
-        cast_codes(t, bj, vj, q);
-        // 8-byte slot rg of the column, moved about so that sixteen lanes meet sixteen different pairs of banks
-        *reinterpret_cast<uint2*>(turned + col * 128 + ((rg ^ cg) * 8)) = make_uint2(q[0], q[1]);
+      for (int j = 0; j < VN; ++j) {
+        if (LANES == 16) most[j] = max_abs(most[j], __shfl_xor_sync(kAll, most[j], 16));
+        if (lane < LANES) part[warp][cg * VN + j] = most[j];
       }
       __syncthreads();
+      if (tid < 128) {
+        float m = 0.f;
+#pragma unroll
+        for (int i = 0; i < WARPS; ++i) m = max_abs(m, part[i][tid]);
+        uint32_t iv;
+        byte_of[tid] = (uint8_t)scale_byte(__float_as_uint(m) & 0x7fffffffu, iv);
+        inv_of[tid] = iv;
+      }
+    }
+    if (p.codes != nullptr && tid < 128 && rt * 128 + tid < p.rows)
+      p.scales[scale_offset(b * tiles, p.first + (rt * 128 + tid) * p.step, kt, ct)] = p.square ? (uint8_t)byte : row_byte[tid];
+    if (p.codes_t == nullptr) continue;
+    if (!p.square) __syncthreads();
+    uint32_t q[VN][2];                       // eight rows of every column
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      float v[4][VN];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int col = i * 32 + (tid >> 3), k = tid & 7, s = col >> 3;   // slots 2k and 2k + 1 of the column
-        uint4 q = *reinterpret_cast<const uint4*>(turned + col * 128 + ((k ^ (s >> 1)) * 16));
-        if (s & 1) q = make_uint4(q.z, q.w, q.x, q.y);
-        const int row = ct * 128 + col;
-        if (row < p.K && rt * 128 + k * 16 < pitch_t)
-          *reinterpret_cast<uint4*>(p.codes_t + ((size_t)b * p.K + row) * pitch_t + rt * 128 + k * 16) = q;
+        Piece<T, VN> x;
+        read(stage, g * 4 + i, x);
+        x.values(v[i]);
       }
-      if (tid < 128 && ct * 128 + tid < p.K)
-        p.scales_t[scale_offset(b * tiles_t, ct * 128 + tid, kt_t, rt)] = (uint8_t)(p.square ? byte : byte_of[tid]);
+#pragma unroll
+      for (int j = 0; j < VN; ++j) {
+        const uint32_t bj = p.square ? byte : byte_of[cg * VN + j], vj = p.square ? inv : inv_of[cg * VN + j];
+        const float t[4] = {v[0][j], v[1][j], v[2][j], v[3][j]};
+        uint32_t word[1];
+        cast_codes(t, bj, vj, word);
+        q[j][g] = word[0];
+      }
     }
-    __syncthreads();                         // the next tile's maxima and codes go to the same places
+    // 8-byte slot rg of a column, moved about so that sixteen lanes meet sixteen different pairs of banks
+#pragma unroll
+    for (int j = 0; j < VN; ++j) *reinterpret_cast<uint2*>(turned + (cg * VN + j) * 128 + ((rg ^ (cg & 15)) * 8)) = make_uint2(q[j][0], q[j][1]);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 1024 / G::THREADS; ++i) {
+      const int c = (i * G::THREADS + tid) >> 3, k = tid & 7, s = c / VN & 15;   // slots 2k and 2k + 1 of the column
+      uint4 w = *reinterpret_cast<const uint4*>(turned + c * 128 + ((k ^ (s >> 1)) * 16));
+      if (s & 1) w = make_uint4(w.z, w.w, w.x, w.y);
+      if (c0 + c < p.K && rt * 128 + k * 16 < pitch_t)
+        *reinterpret_cast<uint4*>(p.codes_t + ((size_t)b * p.K + c0 + c) * pitch_t + rt * 128 + k * 16) = w;
+    }
+    if (tid < 128 && c0 + tid < p.K) p.scales_t[scale_offset(b * tiles_t, c0 + tid, kt_t, rt)] = (uint8_t)(p.square ? byte : byte_of[tid]);
+    if (p.square) __syncthreads();           // (otherwise the next tile's maxima come between)
   }
 }
 
-template <typename T, typename I>
+template <typename T, bool VEC, typename I>
 __global__ void __launch_bounds__(kThreads)
-dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int rows, int K, I items, int groups, int vec,
+dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int rows, int K, I items, int groups,
                   T* __restrict__ dst) {
   const int lane = threadIdx.x & 31;
   const int kt = (int)scale_tiles_k(K), pitch = (int)row_pitch(K);
@@ -170,35 +256,61 @@ dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__
     const I r = w / (I)groups;
     const int g = (int)(w - r * (I)groups);
     const size_t b = (size_t)(r / (I)rows);
-    const int row = (int)(r - (I)b * (I)rows);
-    uint2 q[kUnroll];
-    uint32_t byte[kUnroll];
+    const int row = (int)(r - (I)b * (I)rows), at = g * kUnroll * 256;
+    const uint8_t* from = codes + (size_t)r * pitch + at;
+    const uint8_t* sc = scales + scale_offset(b * tiles, row, kt, at / kBlock);
+    T* to = dst + (size_t)r * K + at;
+    auto value2 = [](uint32_t two) {
+      const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3);
+      return __half22float2(*reinterpret_cast<const __half2*>(&h));
+    };
+    if constexpr (VEC) {
+      const int c0 = lane * 8, left = K - at - c0;
+      uint2 q[kUnroll];
+      uint32_t byte[kUnroll];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int c = (g * kUnroll + u) * 256 + lane * 8;
-      q[u] = make_uint2(0, 0); byte[u] = 0;
-      if (c < K) {
-        q[u] = __ldcs(reinterpret_cast<const uint2*>(codes + (size_t)r * pitch + c));
-        byte[u] = scales[scale_offset(b * tiles, row, kt, c / kBlock)];
+      for (int u = 0; u < kUnroll; ++u) {
+        q[u] = make_uint2(0, 0); byte[u] = 0;
+        if (u * 256 < left) {
+          q[u] = __ldcs(reinterpret_cast<const uint2*>(from + c0 + u * 256));
+          byte[u] = sc[(u >> 1) * kTileBytes + (u & 1) * 2 + (lane >> 4)];
+        }
       }
-    }
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int c = (g * kUnroll + u) * 256 + lane * 8;
-      if (c >= K) break;
-      const float s = scale_value(byte[u]);
-      float v[8];
+      for (int u = 0; u < kUnroll; ++u) {
+        if (u * 256 >= left) break;
+        const float s = scale_value(byte[u]);
+        float v[8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t word = i < 2 ? q[u].x : q[u].y;
-        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(word >> (16 * (i & 1))), __NV_E4M3);
-        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-        v[2 * i] = f.x * s;                  // exact: four significant bits times a power of two
-        v[2 * i + 1] = f.y * s;
+        for (int i = 0; i < 4; ++i) {
+          const float2 f = value2((i < 2 ? q[u].x : q[u].y) >> (16 * (i & 1)));
+          v[2 * i] = f.x * s;                // exact: four significant bits times a power of two
+          v[2 * i + 1] = f.y * s;
+        }
+        Piece<T, 8> out;
+        out.set(v);
+        out.store(to + c0 + u * 256, 8, true);
       }
-      Piece<T, 8> out;
-      out.set(v);
-      out.store(dst + (size_t)r * K + c, K - c, vec != 0);
+    } else {
+      uint32_t q[kUnroll][8];
+      uint32_t byte[kUnroll][2];
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q[u][j] = at + u * 256 + j * 32 + lane < K ? __ldcs(from + u * 256 + j * 32 + lane) : 0u;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) byte[u][h] = at + u * 256 + h * 128 < K ? sc[(u >> 1) * kTileBytes + (u & 1) * 2 + h] : 0u;
+      }
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+          const float2 f = value2(q[u][j] | q[u][j + 1] << 8);
+          const float s = scale_value(byte[u][j / 4]);
+          const int c = u * 256 + j * 32 + lane;
+          if (at + c < K) to[c] = from_f32<T>(f.x * s);
+          if (at + c + 32 < K) to[c + 32] = from_f32<T>(f.y * s);
+        }
     }
   }
 }
@@ -258,6 +370,8 @@ dispatch_rows_kernel(const mx4::Dispatch q, const T* __restrict__ x, const uint8
   }
 }
 
+template <typename T> constexpr int kTileBlocks = sizeof(T) == 2 ? 2 : 1;       // resident on a multiprocessor
+
 int cast_blocks(long long items) {
   const long long want = (items + kThreads / 32 - 1) / (kThreads / 32), most = 32ll * sm_count();
   return (int)(want < most ? want : most);
@@ -269,30 +383,38 @@ template <typename F> cudaError_t by_index(long long items, F&& f) {
   return items < (1ll << 31) ? f((uint32_t)items) : f((uint64_t)items);
 }
 
-template <typename T> cudaError_t quantize(const CastParams& p, cudaStream_t st) {
-  const int vec = ((uintptr_t)p.src & 15) == 0 && p.row_stride * sizeof(T) % 16 == 0 && p.batch_stride * sizeof(T) % 16 == 0;
+template <typename T, bool VEC> cudaError_t quantize(const CastParams& p, int words, cudaStream_t st) {
   if (p.square || p.codes_t != nullptr) {
+    static std::atomic<uint64_t> done{0};
     const int col_tiles = (int)((p.K + 127ll) / 128);
-    const long long items = (long long)p.batch * row_tiles(p.rows) * col_tiles, most = 8ll * sm_count();
-    return launch_after_predecessor(quantize_tiles_kernel<T>, dim3((unsigned)(items < most ? items : most)), dim3(kThreads), 0, st, true,
-                                    p, vec, items, col_tiles);
+    const long long items = (long long)p.batch * row_tiles(p.rows) * col_tiles, most = kTileBlocks<T> * (long long)sm_count();
+    if (!allow_smem((const void*)quantize_tiles_kernel<T, VEC>, Tile<T>::SMEM, done)) return cudaErrorInvalidValue;
+    return launch_after_predecessor(quantize_tiles_kernel<T, VEC>, dim3((unsigned)(items < most ? items : most)), dim3(Tile<T>::THREADS),
+                                    Tile<T>::SMEM, st, true, p, items, col_tiles, words);
   }
   const int groups = cast_groups(p.K);
   const long long items = (long long)p.batch * p.rows * groups;
   return by_index(items, [&](auto n) {
-    return launch_after_predecessor(quantize_rows_kernel<T, decltype(n)>, dim3(cast_blocks(items)), dim3(kThreads), 0, st, true, p, vec,
-                                    n, groups);
+    return launch_after_predecessor(quantize_rows_kernel<T, VEC, decltype(n)>, dim3(cast_blocks(items)), dim3(kThreads), 0, st, true, p, n,
+                                    groups);
   });
+}
+template <typename T> cudaError_t quantize(const CastParams& p, cudaStream_t st) {
+  const size_t e = sizeof(T);
+  const bool vec = ((uintptr_t)p.src & 15) == 0 && p.K * e % 16 == 0 && p.K % 8 == 0 && p.row_stride * e % 16 == 0 && p.batch_stride * e % 16 == 0;
+  const int words = ((uintptr_t)p.src & 3) == 0 && p.K * e % 4 == 0 && p.row_stride * e % 4 == 0 && p.batch_stride * e % 4 == 0;
+  return vec ? quantize<T, true>(p, words, st) : quantize<T, false>(p, words, st);
 }
 
 template <typename T>
 cudaError_t dequantize(const uint8_t* codes, const uint8_t* scales, int batch, int rows, int K, T* dst, cudaStream_t st) {
   const int groups = cast_groups(K);
   const long long items = (long long)batch * rows * groups;
-  const int vec = K * sizeof(T) % 16 == 0;
   return by_index(items, [&](auto n) {
-    return launch_after_predecessor(dequantize_kernel<T, decltype(n)>, dim3(cast_blocks(items)), dim3(kThreads), 0, st, true, codes,
-                                    scales, rows, K, n, groups, vec, dst);
+    const dim3 grid(cast_blocks(items)), block(kThreads);
+    if (K % 8 == 0)
+      return launch_after_predecessor(dequantize_kernel<T, true, decltype(n)>, grid, block, 0, st, true, codes, scales, rows, K, n, groups, dst);
+    return launch_after_predecessor(dequantize_kernel<T, false, decltype(n)>, grid, block, 0, st, true, codes, scales, rows, K, n, groups, dst);
   });
 }
 

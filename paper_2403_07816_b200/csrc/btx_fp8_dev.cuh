@@ -3,6 +3,8 @@
 
 #include <cuda_fp8.h>
 
+#include <atomic>
+
 #include "btx_fp8.cuh"
 #include "btx_route_dev.cuh"
 
@@ -11,6 +13,30 @@ namespace fp8 {
 namespace {
 
 constexpr unsigned kAll = 0xffffffffu;
+
+// Two fp32 numbers in a pair of registers, and the instructions that work on both.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pack2(float a, float b) {
+  f32x2 d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(a), "f"(b));
+  return d;
+}
+__device__ __forceinline__ void unpack2(f32x2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
 
 // N elements of a lane as they were loaded, two of bf16 or one of fp32 per word.
 template <typename T, int N> struct Piece {
@@ -80,6 +106,18 @@ template <typename T, int N> struct Piece {
       }
     }
   }
+  __device__ __forceinline__ void pairs(f32x2 (&v)[N / 2]) const {
+    float f[N];
+    values(f);
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) v[i] = pack2(f[2 * i], f[2 * i + 1]);
+  }
+  __device__ __forceinline__ void set(const f32x2 (&v)[N / 2]) {
+    float f[N];
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) unpack2(v[i], f[2 * i], f[2 * i + 1]);
+    set(f);
+  }
   // largest magnitude as the bits of a float (NaN and infinities compare above every number)
   __device__ __forceinline__ uint32_t amax() const {
     uint32_t m = 0;
@@ -95,11 +133,20 @@ template <typename T, int N> struct Piece {
   }
 };
 
+__device__ __forceinline__ float max_abs(float a, float b) {       // NaN if either is
+  float d;
+  asm("{\n\t.reg .f32 x, y;\n\tabs.f32 x, %1;\n\tabs.f32 y, %2;\n\tmax.NaN.f32 %0, x, y;\n\t}" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
 template <int N> __device__ __forceinline__ uint32_t amax_of(const float (&v)[N]) {
-  uint32_t m = 0;
+  float m[N / 2];
 #pragma unroll
-  for (int i = 0; i < N; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
-  return m;
+  for (int i = 0; i < N / 2; ++i) m[i] = max_abs(v[2 * i], v[2 * i + 1]);
+#pragma unroll
+  for (int k = N / 4; k > 0; k /= 2)
+#pragma unroll
+    for (int i = 0; i < k; ++i) m[i] = max_abs(m[i], m[i + k]);
+  return __float_as_uint(m[0]) & 0x7fffffffu;
 }
 // the largest over groups of LANES neighbouring lanes
 template <int LANES> __device__ __forceinline__ uint32_t lanes_max(uint32_t m) {
@@ -126,6 +173,17 @@ __device__ __forceinline__ float scale_value(uint32_t byte) {
 // byte of the scale of row `row` (of a matrix whose first row tile is tile0), elements `block` * 128 ..
 __device__ __forceinline__ size_t scale_offset(size_t tile0, int row, int kt, int block) {
   return ((tile0 + row / kTileRows) * (size_t)kt + block / 4) * kTileBytes + (row & 31) * 16 + ((row >> 5) & 3) * 4 + (block & 3);
+}
+
+// once per device and kernel: the attribute outlives the call
+inline bool allow_smem(const void* kernel, int bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0ull;
+  if (bit != 0 && (done.load(std::memory_order_relaxed) & bit)) return true;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+  done.fetch_or(bit, std::memory_order_relaxed);
+  return true;
 }
 
 }  // namespace

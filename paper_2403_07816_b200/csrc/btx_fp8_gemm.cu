@@ -718,7 +718,7 @@ btx_status launch(const GemmArgs& g, Params p, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
   CUtensorMap a, b;
   if (!make_codes_map(&a, g.a_codes, g.K, g.M, g.batch, p.a_box) || !make_codes_map(&b, g.b_codes, g.K, g.N, g.experts, BN) ||
-      !mx4::allow_smem((const void*)fp8_gemm_kernel<MODE, SPLIT>, SMEM_BYTES, done))
+      !allow_smem((const void*)fp8_gemm_kernel<MODE, SPLIT>, SMEM_BYTES, done))
     return BTX_ERR_CUDA;
   if (MODE == GATE_UP) p.n_tiles = (p.n_tiles + 1) / 2;   // pairs of column tiles
   const long long tiles = (long long)p.m_tiles * p.n_tiles * p.batch, per = SPLIT ? p.split : MODE == GATE_UP ? 2 : 1;
@@ -753,7 +753,7 @@ btx_status launch_pair(const GemmArgs& g, Params p, cudaStream_t st) {
   if (!make_codes_map(&a, g.a_codes, g.K, g.M, g.batch, 128) || !make_codes_map(&b, g.b_codes, g.K, g.N, g.experts, 128) ||
       !make_scales_map(&sa, g.a_scales, p.kt, (long long)p.a_row_tiles * g.batch, 1) ||
       !make_scales_map(&sb, g.b_scales, p.kt, (long long)p.b_row_tiles * g.experts, 2) ||
-      !mx4::allow_smem((const void*)fp8_gemm_pair_kernel<MODE>, P_SMEM, done))
+      !allow_smem((const void*)fp8_gemm_pair_kernel<MODE>, P_SMEM, done))
     return BTX_ERR_CUDA;
   const long long items = (long long)p.m_tiles * p.n_tiles * p.batch;
   int pairs = sm_count() / 2;

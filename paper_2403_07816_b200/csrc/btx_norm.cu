@@ -1,5 +1,5 @@
 // Root-mean-square norm of the rows in front of a feed-forward sublayer, with the residual's addition and an FP8 output, and
-// its backward pass.  Both are bound by memory: a row stays in registers between the sum over it and its outputs.
+// its backward pass.  Both are bound by memory: a row stays on the chip between the sum over it and its outputs.
 //
 //   forward   h = round(x + residual), s = 1 / sqrt(sum h^2 / d + eps), y = h s w; y is rounded to the output's type, and cast to
 //             FP8 from its fp32 value
@@ -7,7 +7,10 @@
 //             from h in the pass that reads h anyway.  A block keeps its share of dw in registers over all of its rows; a
 //             second kernel adds the blocks' shares in order, so the result repeats
 //
-// A row is shared by the threads of a block (threadIdx.y: another row), V vectors of 16 bytes for each of them.
+// A row is shared by blockDim.x threads, V vectors of 16 bytes each; a block works on blockDim.y rows at a time.  Blocks are
+// resident and walk over the rows.  Every thread fetches its own vectors of the next rows into its own places in shared memory
+// (cp.async), so what is in flight does not depend on registers and nobody waits for another thread's copy.
+#include <atomic>
 #include <type_traits>
 
 #include "btx_fp8_dev.cuh"
@@ -16,6 +19,7 @@ namespace btx {
 namespace fp8 {
 namespace {
 
+constexpr int kSmem = 220 * 1024;          // shared memory of a multiprocessor that the rings of its blocks share
 
 // Sums over the threads of a row, in every one of them; `slot` alternates between calls.
 template <int N> __device__ __forceinline__ void row_sum(float (&a)[N], float (*part)[32][N], int slot) {
@@ -25,14 +29,14 @@ template <int N> __device__ __forceinline__ void row_sum(float (&a)[N], float (*
     for (int o = 16; o > 0; o >>= 1) a[i] += __shfl_xor_sync(kAll, a[i], o);
   const int warps = blockDim.x >> 5;
   if (warps == 1) return;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, first = threadIdx.y * warps;
   if (lane == 0)
 #pragma unroll
-    for (int i = 0; i < N; ++i) part[slot][warp][i] = a[i];
+    for (int i = 0; i < N; ++i) part[slot][first + warp][i] = a[i];
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    a[i] = lane < warps ? part[slot][lane][i] : 0.f;
+    a[i] = lane < warps ? part[slot][first + lane][i] : 0.f;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) a[i] += __shfl_xor_sync(kAll, a[i], o);
   }
@@ -40,196 +44,275 @@ template <int N> __device__ __forceinline__ void row_sum(float (&a)[N], float (*
 
 __device__ __forceinline__ float inv_rms(float sum, int d, float eps) { return 1.0f / sqrtf(sum / (float)d + eps); }
 
-// vec: bit 0 x, 1 residual, 2 w, 3 h, 4 y
-template <typename T, int V, int THREADS>
-__global__ void __launch_bounds__(THREADS)
-norm_kernel(const NormParams p, int vec) {
-  constexpr int VN = 16 / (int)sizeof(T);
+// A thread's columns and its places in shared memory: STAGES rows of each of ARRAYS tensors, V vectors a row.  VEC: every
+// vector of every tensor is whole and on a 16-byte boundary.
+template <typename T, int V, int ARRAYS, int STAGES, bool VEC> struct Rows {
+  static constexpr int VN = 16 / (int)sizeof(T);
+  int d, c0, dc;                           // elements of a row, first column, columns from one vector to the next
+  uint32_t base, step;                     // first place, bytes from one place to the next
+  const T* from[ARRAYS];                   // first column of the next row to fetch
+  long long ahead[ARRAYS];                 // elements to the row after it
+
+  __device__ __forceinline__ void init(uint8_t* smem, int d_) {
+    d = d_; c0 = threadIdx.x * VN; dc = blockDim.x * VN;
+    step = blockDim.x * blockDim.y * 16;
+    base = (uint32_t)__cvta_generic_to_shared(smem) + (threadIdx.y * blockDim.x + threadIdx.x) * 16;
+    // places behind the last column are never written again
+    for (int k = 0; k < STAGES * ARRAYS * V; ++k)
+      asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(base + k * step), "r"(0) : "memory");
+  }
+  __device__ __forceinline__ void source(int array, const void* p, long long stride, long long row, long long rows_ahead) {
+    from[array] = (const T*)p + row * stride + c0;
+    ahead[array] = rows_ahead * stride;
+  }
+  __device__ __forceinline__ int col(int i) const { return c0 + i * dc; }
+  __device__ __forceinline__ uint32_t place(int stage, int array, int i) const { return base + ((stage * ARRAYS + array) * V + i) * step; }
+  // the next row, if there is one, into a stage
+  __device__ __forceinline__ void fetch(int stage, bool in) {
+#pragma unroll
+    for (int a = 0; a < ARRAYS; ++a) {
+      if (in && VEC) {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          if (col(i) < d)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(place(stage, a, i)), "l"(from[a] + i * dc) : "memory");
+      } else if (in) {
+        Piece<T, VN> q[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) q[i].load(from[a] + i * dc, d - col(i), false);
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(place(stage, a, i)), "r"(q[i].w[0]), "r"(q[i].w[1]), "r"(q[i].w[2]),
+                       "r"(q[i].w[3]) : "memory");
+      }
+      from[a] += ahead[a];
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  // the row of the oldest fetch has landed
+  __device__ __forceinline__ void wait() const { asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory"); }
+  __device__ __forceinline__ void read(int stage, int array, int i, f32x2 (&v)[VN / 2]) const {
+    Piece<T, VN> q;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(q.w[0]), "=r"(q.w[1]), "=r"(q.w[2]), "=r"(q.w[3])
+                 : "r"(place(stage, array, i)) : "memory");
+    q.pairs(v);
+  }
+  __device__ __forceinline__ void write(T* row, int i, const Piece<T, VN>& q) const {
+    if (VEC) {
+      if (col(i) < d) q.store(row + i * dc, VN, true);
+    } else {
+      q.store(row + i * dc, d - col(i), false);
+    }
+  }
+  // this thread's weights, ones where there are none
+  __device__ __forceinline__ void weights(const void* w, f32x2 (&v)[V][VN / 2]) const {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      Piece<T, VN> q;
+      q.load((const T*)w + col(i), w == nullptr ? 0 : d - col(i), VEC);
+      q.pairs(v[i]);
+      if (w == nullptr)
+#pragma unroll
+        for (int j = 0; j < VN / 2; ++j) v[i][j] = pack2(1.f, 1.f);
+    }
+  }
+};
+
+// Threads of a multiprocessor that the registers are meant for.  What is in flight should be about 64 KB: with a residual (two
+// loads a vector) or in the backward pass 512 threads have that, with one tensor to read it takes 1024.
+constexpr int resident_threads(int v, int threads, int arrays) { return threads == 1024 || (arrays == 1 && v == 2) ? 1024 : 512; }
+
+template <typename T, int V, int THREADS, bool RESIDUAL, bool VEC>
+__global__ void __launch_bounds__(THREADS, resident_threads(V, THREADS, RESIDUAL ? 2 : 1) / THREADS)
+norm_kernel(const __grid_constant__ NormParams p) {
+  constexpr int VN = 16 / (int)sizeof(T), STAGES = THREADS == 1024 ? 1 : 2;
+  extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float part[2][32][1];
-  const int kt = (int)scale_tiles_k(p.d), pitch = (int)row_pitch(p.d);
+  const int pitch = (int)row_pitch(p.d), kt = (int)scale_tiles_k(p.d);
+  const int step = gridDim.x * blockDim.y;
+  long long t = (long long)blockIdx.x * blockDim.y + threadIdx.y;
+  Rows<T, V, RESIDUAL ? 2 : 1, STAGES, VEC> rows;
+  rows.init(smem, p.d);
+  rows.source(0, p.x, p.x_stride, t, step);
+  if (RESIDUAL) rows.source(RESIDUAL ? 1 : 0, p.residual, p.residual_stride, t, step);
   allow_dependents();
   grid_dependency_wait();
-  const int rows = blockDim.y;
+  if (STAGES > 1) rows.fetch(0, t < p.T);
+  f32x2 w[V][VN / 2];
+  rows.weights(p.w, w);
+  T *h = (T*)p.h + t * p.h_stride + rows.c0, *y = (T*)p.y + t * p.y_stride + rows.c0;
+  uint8_t* codes = p.codes + t * pitch + rows.c0;
   int slot = 0;
-  for (long long t0 = (long long)blockIdx.x * rows; t0 < p.T; t0 += (long long)gridDim.x * rows, slot ^= 1) {
-    const bool in = t0 + threadIdx.y < p.T;
-    const int t = (int)(in ? t0 + threadIdx.y : 0);
-    Piece<T, VN> x[V], r[V];
+  for (long long b = (long long)blockIdx.x * blockDim.y; b < p.T; b += step, t += step) {      // (the same for all rows of the block)
+    const bool in = t < p.T;
+    const int stage = STAGES > 1 ? slot : 0;
+    rows.fetch(STAGES > 1 ? slot ^ 1 : 0, t + (STAGES > 1 ? step : 0) < p.T);
+    rows.wait();
+    f32x2 v[V][VN / 2], sums = 0;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const int c = (i * blockDim.x + threadIdx.x) * VN, n = in ? p.d - c : 0;
-      x[i].load((const T*)p.x + t * p.x_stride + c, n, vec & 1);
-      if (p.residual != nullptr) r[i].load((const T*)p.residual + t * p.residual_stride + c, n, vec & 2);
-    }
-    float sum[1] = {0.f};
+      rows.read(stage, 0, i, v[i]);
+      Piece<T, VN> q;
+      if (RESIDUAL) {
+        f32x2 r[VN / 2];
+        rows.read(stage, RESIDUAL ? 1 : 0, i, r);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int c = (i * blockDim.x + threadIdx.x) * VN, n = in ? p.d - c : 0;
-      float v[VN];
-      x[i].values(v);
-      if (p.residual != nullptr) {
-        float a[VN];
-        r[i].values(a);
-#pragma unroll
-        for (int j = 0; j < VN; ++j) v[j] += a[j];
-        x[i].set(v);
-        x[i].values(v);
+        for (int j = 0; j < VN / 2; ++j) v[i][j] = add2(v[i][j], r[j]);
+        q.set(v[i]);
+        q.pairs(v[i]);
+      } else {
+        q.set(v[i]);
       }
-      if (p.h != nullptr) x[i].store((T*)p.h + t * p.h_stride + c, n, vec & 8);
+      if (p.h != nullptr && in) rows.write(h, i, q);
 #pragma unroll
-      for (int j = 0; j < VN; ++j) sum[0] = fmaf(v[j], v[j], sum[0]);
+      for (int j = 0; j < VN / 2; ++j) sums = fma2(v[i][j], v[i][j], sums);
     }
+    float sum[1], other;
+    unpack2(sums, sum[0], other);
+    sum[0] += other;
     row_sum(sum, part, slot);
     const float s = inv_rms(sum[0], p.d, p.eps);
+    const f32x2 s2 = pack2(s, s);
+    uint8_t* scales = p.scales + scale_offset(0, (int)t, kt, 0);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const int c = (i * blockDim.x + threadIdx.x) * VN, n = in ? p.d - c : 0;
-      float v[VN];
-      x[i].values(v);
-      Piece<T, VN> out;
-      if (p.w != nullptr) {
-        float w[VN];
-        const T* from = (const T*)p.w + c;
-        if ((vec & 4) && n >= VN) {
-          const uint4 q = *reinterpret_cast<const uint4*>(from);
-          out.w[0] = q.x; out.w[1] = q.y; out.w[2] = q.z; out.w[3] = q.w;
-        } else {
-          out.load(from, n, false);
-        }
-        out.values(w);
 #pragma unroll
-        for (int j = 0; j < VN; ++j) v[j] = v[j] * s * w[j];
-      } else {
-#pragma unroll
-        for (int j = 0; j < VN; ++j) v[j] *= s;
-      }
-      if (p.y != nullptr) {
-        out.set(v);
-        out.store((T*)p.y + t * p.y_stride + c, n, vec & 16);
+      for (int j = 0; j < VN / 2; ++j) v[i][j] = mul2(mul2(v[i][j], s2), w[i][j]);
+      if (p.y != nullptr && in) {
+        Piece<T, VN> q;
+        q.set(v[i]);
+        rows.write(y, i, q);
       }
       if (p.codes != nullptr) {
         constexpr int LANES = kBlock / VN;
+        const int c = rows.col(i);
+        float f[VN];
 #pragma unroll
-        for (int j = 0; j < VN; ++j)
-          if (j >= n) v[j] = 0.f;            // behind the last element (0 times an infinite s otherwise)
-        uint32_t inv, q[VN / 4];
-        const uint32_t byte = scale_byte(lanes_max<LANES>(amax_of(v)), inv);
-        cast_codes(v, byte, inv, q);
-        if (in && c < pitch) {
-          uint8_t* to = p.codes + (size_t)t * pitch + c;
-          if constexpr (VN == 8) *reinterpret_cast<uint2*>(to) = make_uint2(q[0], q[1]);
-          else *reinterpret_cast<uint32_t*>(to) = q[0];
+        for (int j = 0; j < VN / 2; ++j) unpack2(v[i][j], f[2 * j], f[2 * j + 1]);
+        if (c + VN > p.d) {                  // behind the last element (0 times an infinite s otherwise)
+#pragma unroll
+          for (int j = 0; j < VN; ++j)
+            if (c + j >= p.d) f[j] = 0.f;
         }
-        if (n > 0 && (threadIdx.x & (LANES - 1)) == 0) p.scales[scale_offset(0, t, kt, c / kBlock)] = (uint8_t)byte;
+        uint32_t inv, q[VN / 4];
+        const uint32_t byte = scale_byte(lanes_max<LANES>(amax_of(f)), inv);
+        cast_codes(f, byte, inv, q);
+        if (in && c < pitch) {
+          if constexpr (VN == 8) *reinterpret_cast<uint2*>(codes + i * rows.dc) = make_uint2(q[0], q[1]);
+          else *reinterpret_cast<uint32_t*>(codes + i * rows.dc) = q[0];
+          if ((threadIdx.x & (LANES - 1)) == 0 && c < p.d) scales[c / (4 * kBlock) * kTileBytes + c / kBlock % 4] = (uint8_t)byte;
+        }
       }
     }
+    h += step * p.h_stride;
+    y += step * p.y_stride;
+    codes += (long long)step * pitch;
+    slot ^= 1;
   }
 }
 
-// vec: bit 0 h, 1 w, 2 dy, 3 dh, 4 dx, 5 the shares of dw
-template <typename T, int V, int THREADS>
-__global__ void __launch_bounds__(THREADS)
-norm_grad_kernel(const NormGradParams p, int vec) {
-  constexpr int VN = 16 / (int)sizeof(T);
+// sum h^2 and, with u = dy w, sum u h; then dw += dy (h s) and dx = dh + s u - (s^2 m) h.
+template <typename T, int V, int THREADS, bool ADD, bool VEC>
+__global__ void __launch_bounds__(THREADS, resident_threads(V, THREADS, 3) / THREADS)
+norm_grad_kernel(const __grid_constant__ NormGradParams p) {
+  constexpr int VN = 16 / (int)sizeof(T), STAGES = THREADS == 1024 ? 1 : 2;
+  extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float part[2][32][2];
+  const int step = gridDim.x * blockDim.y;
+  long long t = (long long)blockIdx.x * blockDim.y + threadIdx.y;
+  Rows<T, V, ADD ? 3 : 2, STAGES, VEC> rows;
+  rows.init(smem, p.d);
+  rows.source(0, p.h, p.h_stride, t, step);
+  rows.source(1, p.dy, p.dy_stride, t, step);
+  if (ADD) rows.source(ADD ? 2 : 0, p.dh, p.dh_stride, t, step);
   allow_dependents();
   grid_dependency_wait();
   if (blockIdx.x == 0)
-    for (int i = threadIdx.x; i < kStatusWords; i += blockDim.x) p.status[i] = 0;
-  float dw[V][VN];
+    for (int i = threadIdx.y * blockDim.x + threadIdx.x; i < kStatusWords; i += blockDim.x * blockDim.y) p.status[i] = 0;
+  if (STAGES > 1) rows.fetch(0, t < p.T);
+  f32x2 w[V][VN / 2], dw[V][VN / 2];
+  rows.weights(p.w, w);
 #pragma unroll
   for (int i = 0; i < V; ++i)
 #pragma unroll
-    for (int j = 0; j < VN; ++j) dw[i][j] = 0.f;
+    for (int j = 0; j < VN / 2; ++j) dw[i][j] = 0;
+  T* dx = (T*)p.dx + t * p.dx_stride + rows.c0;
   int slot = 0;
-  for (int t = blockIdx.x; t < p.T; t += gridDim.x, slot ^= 1) {
-    Piece<T, VN> h[V], dy[V], dh[V];
+  for (long long b = (long long)blockIdx.x * blockDim.y; b < p.T; b += step, t += step) {
+    const int stage = STAGES > 1 ? slot : 0;
+    rows.fetch(STAGES > 1 ? slot ^ 1 : 0, t + (STAGES > 1 ? step : 0) < p.T);
+    rows.wait();
+    f32x2 h[V][VN / 2], dy[V][VN / 2], sums[2] = {0, 0};
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const int c = (i * blockDim.x + threadIdx.x) * VN, n = p.d - c;
-      h[i].load((const T*)p.h + t * p.h_stride + c, n, vec & 1);
-      dy[i].load((const T*)p.dy + t * p.dy_stride + c, n, vec & 4);
-      if (p.dh != nullptr) dh[i].load((const T*)p.dh + t * p.dh_stride + c, n, vec & 8);
+      rows.read(stage, 0, i, h[i]);
+      rows.read(stage, 1, i, dy[i]);
+#pragma unroll
+      for (int j = 0; j < VN / 2; ++j) {
+        sums[0] = fma2(h[i][j], h[i][j], sums[0]);
+        sums[1] = fma2(mul2(dy[i][j], w[i][j]), h[i][j], sums[1]);
+      }
     }
-    float sum[2] = {0.f, 0.f};
-    auto weights = [&](int i, float (&w)[VN]) {
-      const int c = (i * blockDim.x + threadIdx.x) * VN, n = p.d - c;
-      Piece<T, VN> q;
-      if ((vec & 2) && n >= VN) {
-        const uint4 u = *reinterpret_cast<const uint4*>((const T*)p.w + c);
-        q.w[0] = u.x; q.w[1] = u.y; q.w[2] = u.z; q.w[3] = u.w;
-      } else {
-        q.load((const T*)p.w + c, n, false);
-      }
-      q.values(w);
-    };
+    float sum[2], other;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      float a[VN], g[VN];
-      h[i].values(a);
-      dy[i].values(g);
-      if (p.w != nullptr) {
-        float w[VN];
-        weights(i, w);
-#pragma unroll
-        for (int j = 0; j < VN; ++j) g[j] *= w[j];
-      }
-#pragma unroll
-      for (int j = 0; j < VN; ++j) {
-        sum[0] = fmaf(a[j], a[j], sum[0]);
-        sum[1] = fmaf(g[j], a[j], sum[1]);
-      }
+    for (int i = 0; i < 2; ++i) {
+      unpack2(sums[i], sum[i], other);
+      sum[i] += other;
     }
     row_sum(sum, part, slot);
     const float s = inv_rms(sum[0], p.d, p.eps), m = sum[1] / (float)p.d * s;
+    const f32x2 s2 = pack2(s, s), m2 = pack2(-(s * m) * s, -(s * m) * s);
+    if (t < p.T) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int c = (i * blockDim.x + threadIdx.x) * VN, n = p.d - c;
-      float a[VN], g[VN];
-      h[i].values(a);
-      dy[i].values(g);
+      for (int i = 0; i < V; ++i) {
+        f32x2 g[VN / 2];
+        if (ADD) {
+          rows.read(stage, ADD ? 2 : 0, i, g);
+        } else {
 #pragma unroll
-      for (int j = 0; j < VN; ++j) {
-        a[j] *= s;
-        if (j < n) dw[i][j] = fmaf(g[j], a[j], dw[i][j]);
+          for (int j = 0; j < VN / 2; ++j) g[j] = 0;
+        }
+#pragma unroll
+        for (int j = 0; j < VN / 2; ++j) {
+          dw[i][j] = fma2(dy[i][j], mul2(h[i][j], s2), dw[i][j]);
+          g[j] = fma2(h[i][j], m2, fma2(mul2(dy[i][j], w[i][j]), s2, g[j]));
+        }
+        Piece<T, VN> q;
+        q.set(g);
+        rows.write(dx, i, q);
       }
-      if (p.w != nullptr) {
-        float w[VN];
-        weights(i, w);
-#pragma unroll
-        for (int j = 0; j < VN; ++j) g[j] *= w[j];
-      }
-#pragma unroll
-      for (int j = 0; j < VN; ++j) g[j] = s * (g[j] - a[j] * m);
-      if (p.dh != nullptr) {
-        float r[VN];
-        dh[i].values(r);
-#pragma unroll
-        for (int j = 0; j < VN; ++j) g[j] += r[j];
-      }
-      Piece<T, VN> out;
-      out.set(g);
-      out.store((T*)p.dx + t * p.dx_stride + c, n, vec & 16);
     }
+    dx += step * p.dx_stride;
+    slot ^= 1;
   }
-  if (p.dw != nullptr)
+  if (p.dw == nullptr) return;
+  if (blockDim.y > 1) {                      // the rows of the block, in order (its ring has room for a place per value)
+    f32x2* sh = reinterpret_cast<f32x2*>(smem);
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int c = (i * blockDim.x + threadIdx.x) * VN;
-      float* to = p.part + (size_t)blockIdx.x * p.d + c;
-      if ((vec & 32) && c + VN <= p.d) {
+    for (int i = 0; i < V; ++i)
 #pragma unroll
-        for (int j = 0; j < VN; j += 4) *reinterpret_cast<float4*>(to + j) = make_float4(dw[i][j], dw[i][j + 1], dw[i][j + 2], dw[i][j + 3]);
-      } else {
+      for (int j = 0; j < VN / 2; ++j) sh[((threadIdx.y * V + i) * (VN / 2) + j) * blockDim.x + threadIdx.x] = dw[i][j];
+    __syncthreads();
+    if (threadIdx.y > 0) return;
+    for (int r = 1; r < (int)blockDim.y; ++r)
 #pragma unroll
-        for (int j = 0; j < VN; ++j)
-          if (c + j < p.d) to[j] = dw[i][j];
-      }
-    }
+      for (int i = 0; i < V; ++i)
+#pragma unroll
+        for (int j = 0; j < VN / 2; ++j) dw[i][j] = add2(dw[i][j], sh[((r * V + i) * (VN / 2) + j) * blockDim.x + threadIdx.x]);
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int c = rows.col(i);
+    Piece<float, VN> out;
+    out.set(dw[i]);
+    out.store(p.part + (size_t)blockIdx.x * p.d + c, p.d - c, p.d % 4 == 0);
+  }
 }
 
-// dw[c] (+)= the sum of column c over `parts` rows: 32 columns a block, its 16 warps take every sixteenth row
-constexpr int kSumWarps = 16;
+// dw[c] (+)= the sum of column c over `parts` rows: 32 columns a block, its 32 warps take every 32nd row, eight of them at once
+constexpr int kSumWarps = 32, kSumAhead = 8;
 __global__ void __launch_bounds__(32 * kSumWarps)
 norm_sum_kernel(const float* part, int parts, int d, int accumulate, float* dw) {
   __shared__ float share[kSumWarps][32];
@@ -239,7 +322,16 @@ norm_sum_kernel(const float* part, int parts, int d, int accumulate, float* dw) 
   grid_dependency_wait();
   float a = 0.f;
   if (c < d)
-    for (int i = warp; i < parts; i += kSumWarps) a += __ldcs(part + (size_t)i * d + c);
+    for (int i0 = warp; i0 < parts; i0 += kSumWarps * kSumAhead) {
+      float v[kSumAhead];
+#pragma unroll
+      for (int u = 0; u < kSumAhead; ++u) {
+        const int i = i0 + u * kSumWarps;
+        v[u] = i < parts ? __ldcs(part + (size_t)i * d + c) : 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < kSumAhead; ++u) a += v[u];
+    }
   share[warp][lane] = a;
   __syncthreads();
   if (warp == 0 && c < d) {
@@ -250,48 +342,68 @@ norm_sum_kernel(const float* part, int parts, int d, int accumulate, float* dw) 
   }
 }
 
-// Vectors of 16 bytes a thread and threads of a row: few vectors, so that many rows are in flight; more than 512 threads
-// (which leaves 64 registers for each) only for rows of more than 32 KB.
-struct Shape { int v, threads; };
-Shape shape_of(int vecs) {
-  for (int v = 1; v < 4; v *= 2)
-    if (vecs <= v * (v == 1 ? 64 : 512)) return {v, (vecs + 32 * v - 1) / (32 * v) * 32};
-  return {4, (vecs + 127) / 128 * 32};
+// Vectors of 16 bytes a thread, threads of a row, rows of a block; blocks that a multiprocessor holds, bytes of their ring.
+// More than 512 threads (which leaves 64 registers for each and one stage) only for rows of more than 32 KB.
+struct Shape { int v, threads, rows, blocks, smem; };
+Shape shape_of(int vecs, int esize, int arrays) {
+  Shape s;
+  s.v = vecs <= 1024 ? 2 : 4;
+  s.threads = (vecs + 32 * s.v - 1) / (32 * s.v) * 32;
+  s.rows = s.threads < 256 ? 256 / s.threads : 1;
+  const int block = s.threads * s.rows, bound = s.threads <= 512 ? 512 : 1024;
+  s.blocks = resident_threads(s.v, bound, arrays) / block;
+  s.smem = (bound == 1024 ? 1 : 2) * block * s.v * 16 * arrays;
+  const int shares = s.rows > 1 ? block * s.v * (16 / esize) * 4 : 0;
+  if (s.smem < shares) s.smem = shares;
+  return s;
 }
-template <typename F> cudaError_t by_shape(const Shape& s, F&& f) {
-  using std::integral_constant;
-  if (s.v == 1) return f(integral_constant<int, 1>(), integral_constant<int, 256>());
-  if (s.v == 2) return f(integral_constant<int, 2>(), integral_constant<int, 512>());
-  if (s.threads <= 512) return f(integral_constant<int, 4>(), integral_constant<int, 512>());
-  return f(integral_constant<int, 4>(), integral_constant<int, 1024>());
+template <bool X> using Bool = std::integral_constant<bool, X>;
+template <int X> using Int = std::integral_constant<int, X>;
+template <typename F> cudaError_t by_shape(const Shape& s, bool more, bool vec, F&& f) {
+  auto with = [&](auto v, auto threads) {
+    if (more) return vec ? f(v, threads, Bool<true>(), Bool<true>()) : f(v, threads, Bool<true>(), Bool<false>());
+    return vec ? f(v, threads, Bool<false>(), Bool<true>()) : f(v, threads, Bool<false>(), Bool<false>());
+  };
+  if (s.v == 2) return with(Int<2>(), Int<512>());
+  return s.threads <= 512 ? with(Int<4>(), Int<512>()) : with(Int<4>(), Int<1024>());
 }
+int vectors(long long d, int esize) { return (int)((d * esize + 15) / 16); }
 
-template <typename T> int vectors(long long d) { return (int)((d + 16 / (int)sizeof(T) - 1) / (16 / (int)sizeof(T))); }
-
-bool rows16(const void* p, long long stride, int esize) { return ((uintptr_t)p & 15) == 0 && stride * esize % 16 == 0; }
+// (a tensor that is not there does no harm)
+bool rows16(const void* p, long long stride, int esize) { return p == nullptr || (((uintptr_t)p & 15) == 0 && stride * esize % 16 == 0); }
 
 template <typename T> cudaError_t norm(const NormParams& p, cudaStream_t st) {
-  const Shape s = shape_of(vectors<T>(p.codes != nullptr ? row_pitch(p.d) : p.d));
-  const int rows = s.threads == 32 ? 8 : 1;
   const int e = sizeof(T);
-  const int vec = rows16(p.x, p.x_stride, e) | rows16(p.residual, p.residual_stride, e) << 1 | rows16(p.w, 0, e) << 2 |
-                  rows16(p.h, p.h_stride, e) << 3 | rows16(p.y, p.y_stride, e) << 4;
-  const long long want = (p.T + rows - 1ll) / rows, most = 64ll * sm_count();
-  const dim3 grid((unsigned)(want < most ? want : most)), block(s.threads, rows);
-  return by_shape(s, [&](auto v, auto threads) {
-    return launch_after_predecessor(norm_kernel<T, decltype(v)::value, decltype(threads)::value>, grid, block, 0, st, true, p, vec);
+  const Shape s = shape_of(vectors(p.codes != nullptr ? row_pitch(p.d) : p.d, e), e, p.residual != nullptr ? 2 : 1);
+  const bool vec = p.d * e % 16 == 0 && rows16(p.x, p.x_stride, e) && rows16(p.residual, p.residual_stride, e) && rows16(p.w, 0, e) &&
+                   rows16(p.h, p.h_stride, e) && rows16(p.y, p.y_stride, e);
+  const long long want = (p.T + s.rows - 1ll) / s.rows, most = (long long)s.blocks * sm_count();
+  const dim3 grid((unsigned)(want < most ? want : most)), block(s.threads, s.rows);
+  return by_shape(s, p.residual != nullptr, vec, [&](auto v, auto threads, auto residual, auto whole) {
+    static std::atomic<uint64_t> done{0};
+    auto kernel = norm_kernel<T, decltype(v)::value, decltype(threads)::value, decltype(residual)::value, decltype(whole)::value>;
+    if (!allow_smem((const void*)kernel, kSmem, done)) return cudaErrorInvalidValue;
+    return launch_after_predecessor(kernel, grid, block, s.smem, st, true, p);
   });
 }
 
+int grad_parts(int T, const Shape& s) {
+  const long long want = (T + s.rows - 1ll) / s.rows, most = (long long)s.blocks * sm_count();
+  return (int)(want < most ? (want > 0 ? want : 1) : most);
+}
+
 template <typename T> cudaError_t norm_grad(const NormGradParams& p, cudaStream_t st) {
-  const Shape s = shape_of(vectors<T>(p.d));
   const int e = sizeof(T);
-  const int vec = rows16(p.h, p.h_stride, e) | rows16(p.w, 0, e) << 1 | rows16(p.dy, p.dy_stride, e) << 2 |
-                  rows16(p.dh, p.dh_stride, e) << 3 | rows16(p.dx, p.dx_stride, e) << 4 | (p.d % 4 == 0) << 5;
-  const int parts = norm_grad_parts(p.T, p.d, sizeof(T) == 2 ? BTX_BF16 : BTX_F32);
-  const dim3 grid((unsigned)parts), block(s.threads);
-  const cudaError_t r = by_shape(s, [&](auto v, auto threads) {
-    return launch_after_predecessor(norm_grad_kernel<T, decltype(v)::value, decltype(threads)::value>, grid, block, 0, st, true, p, vec);
+  const Shape s = shape_of(vectors(p.d, e), e, 3);
+  const bool vec = p.d * e % 16 == 0 && rows16(p.h, p.h_stride, e) && rows16(p.w, 0, e) && rows16(p.dy, p.dy_stride, e) &&
+                   rows16(p.dh, p.dh_stride, e) && rows16(p.dx, p.dx_stride, e);
+  const int parts = grad_parts(p.T, s);
+  const dim3 grid((unsigned)parts), block(s.threads, s.rows);
+  const cudaError_t r = by_shape(s, p.dh != nullptr, vec, [&](auto v, auto threads, auto add, auto whole) {
+    static std::atomic<uint64_t> done{0};
+    auto kernel = norm_grad_kernel<T, decltype(v)::value, decltype(threads)::value, decltype(add)::value, decltype(whole)::value>;
+    if (!allow_smem((const void*)kernel, kSmem, done)) return cudaErrorInvalidValue;
+    return launch_after_predecessor(kernel, grid, block, s.smem, st, true, p);
   });
   if (r != cudaSuccess || p.dw == nullptr) return r;
   return launch_after_predecessor(norm_sum_kernel, dim3((p.d + 31) / 32), dim3(32 * kSumWarps), 0, st, true, (const float*)p.part, parts,
@@ -300,11 +412,10 @@ template <typename T> cudaError_t norm_grad(const NormGradParams& p, cudaStream_
 
 }  // namespace
 
-// Blocks of the backward pass, each with a share of dw: about 1024 threads for every multiprocessor.
+// Blocks of the backward pass, each with a share of dw: as many as are resident at once.
 int norm_grad_parts(int T, int d, int dtype) {
-  const Shape s = shape_of(dtype == BTX_BF16 ? vectors<__nv_bfloat16>(d) : vectors<float>(d));
-  const long long most = (1024 / s.threads) * (long long)sm_count();
-  return (int)(T < most ? (T > 0 ? T : 1) : most);
+  const int e = dtype == BTX_BF16 ? 2 : 4;
+  return grad_parts(T, shape_of(vectors(d, e), e, 3));
 }
 
 cudaError_t launch_norm(const NormParams& p, int dtype, cudaStream_t st) {
