@@ -1,8 +1,8 @@
 // FP8 casts: one power-of-two scale for 128 elements of a row, or for a block of 128 x 128.
 //
 //   quantize_rows   a scale per row and 128 elements, as the rows stand: a warp takes 256 elements at a time
-//   quantize_tiles  square blocks and transposed outputs: a block of threads works on 128 x 128 tiles, eight neighbouring rows
-//                   of 16 bytes a thread, which gives the largest of its rows, of its columns or of all; x is read once for
+//   quantize_tiles  square blocks and transposed outputs: a block of threads works on 128 x 128 tiles, eight neighbouring rows of
+//                   16 bytes a thread, which gives the largest of its rows, of its columns or of all; x is read once for
 //                   both outputs.  The next tile is on its way meanwhile (cp.async into the thread's own places in shared
 //                   memory).  Transposed codes turn through shared memory, 8 bytes (of 8 rows) at a time
 //   dequantize      the mapping of quantize_rows backwards
@@ -60,21 +60,58 @@ quantize_rows_kernel(const __grid_constant__ CastParams p, I items, int groups) 
 
 // Threads of a tile: 16 groups of eight rows, 16 bytes of a row each.
 template <typename T> struct Tile {
-  static constexpr int VN = 16 / (int)sizeof(T), LANES = 128 / VN, THREADS = 16 * LANES, STAGES = 2;
-  static constexpr int STAGE_BYTES = THREADS * 8 * 16, SMEM = STAGES * STAGE_BYTES + 128 * 128;
+  static constexpr int VN = 16 / (int)sizeof(T), LANES = 128 / VN, THREADS = 16 * LANES;
+  static constexpr int ROWS_BYTES = THREADS * 8 * 16, SMEM = ROWS_BYTES + 128 * 128;
+  static constexpr int BLOCKS = sizeof(T) == 2 ? 3 : 2;       // resident on a multiprocessor
 };
+// magnitudes of the elements of a word, and the larger ones of two words (as integers: NaN and infinities are above all numbers)
+template <typename T> __device__ __forceinline__ uint32_t word_abs(uint32_t w) { return w & (sizeof(T) == 2 ? 0x7fff7fffu : 0x7fffffffu); }
+template <typename T> __device__ __forceinline__ uint32_t word_max(uint32_t a, uint32_t b) { return sizeof(T) == 2 ? __vmaxu2(a, b) : max(a, b); }
+
+// Largest magnitudes of eight rows over the LANES lanes that share them, from m[i], the lane's words of row i.  Lanes hand each
+// other half of what is left to reduce, so a lane ends up with one row (bf16: two in a word); their scale bytes go to row_byte.
+template <typename T> __device__ __forceinline__ void rows_scales(const uint32_t (&m)[8], int cg, uint8_t* row_byte) {
+  if constexpr (sizeof(T) == 2) {
+    uint32_t r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = __vmaxu2(__byte_perm(m[2 * i], m[2 * i + 1], 0x5410), __byte_perm(m[2 * i], m[2 * i + 1], 0x7632));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t got = __shfl_xor_sync(kAll, cg & 8 ? r[i] : r[i + 2], 8);
+      r[i] = __vmaxu2(cg & 8 ? r[i + 2] : r[i], got);
+    }
+    const uint32_t got = __shfl_xor_sync(kAll, cg & 4 ? r[0] : r[1], 4);
+    uint32_t a = __vmaxu2(cg & 4 ? r[1] : r[0], got);
+    a = __vmaxu2(a, __shfl_xor_sync(kAll, a, 2));
+    a = __vmaxu2(a, __shfl_xor_sync(kAll, a, 1));
+    uint32_t inv;
+    const uint32_t lo = scale_byte(a << 16, inv), hi = scale_byte(a & 0xffff0000u, inv);
+    if ((cg & 3) == 0) *reinterpret_cast<uint16_t*>(row_byte + (cg >> 2) * 2) = (uint16_t)(lo | hi << 8);
+  } else {
+    uint32_t r[4], t[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = max(cg & 16 ? m[i + 4] : m[i], __shfl_xor_sync(kAll, cg & 16 ? m[i] : m[i + 4], 16));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) t[i] = max(cg & 8 ? r[i + 2] : r[i], __shfl_xor_sync(kAll, cg & 8 ? r[i] : r[i + 2], 8));
+    uint32_t a = max(cg & 4 ? t[1] : t[0], __shfl_xor_sync(kAll, cg & 4 ? t[0] : t[1], 4)), inv;
+    a = max(a, __shfl_xor_sync(kAll, a, 2));
+    a = max(a, __shfl_xor_sync(kAll, a, 1));
+    if ((cg & 3) == 0) row_byte[cg >> 2] = (uint8_t)scale_byte(a, inv);
+  }
+}
 
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(Tile<T>::THREADS)
+__global__ void __launch_bounds__(Tile<T>::THREADS, Tile<T>::BLOCKS)
 quantize_tiles_kernel(const __grid_constant__ CastParams p, long long items, int col_tiles, int words) {
   using G = Tile<T>;
-  constexpr int VN = G::VN, LANES = G::LANES, WARPS = G::THREADS / 32;
+  constexpr int VN = G::VN, LANES = G::LANES, WARPS = G::THREADS / 32, PER = VN / 4;      // PER: elements of a word
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ float part[WARPS][128];       // largest of every column over a warp's rows
+  __shared__ uint32_t part[WARPS][128 / PER];       // largest of every column over a warp's rows
   __shared__ uint32_t whole[2][WARPS];     // of a square block, for tiles in turn
   __shared__ uint32_t inv_of[128];
-  __shared__ uint8_t byte_of[128], row_byte[128];
-  uint8_t* turned = smem + G::STAGES * G::STAGE_BYTES;
+  __shared__ uint8_t byte_of[128];
+  __shared__ __align__(8) uint8_t row_byte[128];
+  uint8_t* turned = smem + G::ROWS_BYTES;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int cg = tid % LANES, rg = tid / LANES;
   const int kt = (int)scale_tiles_k(p.K), pitch = (int)row_pitch(p.K);
@@ -82,7 +119,7 @@ quantize_tiles_kernel(const __grid_constant__ CastParams p, long long items, int
   const size_t tiles = (size_t)row_tiles(p.out_rows), tiles_t = (size_t)row_tiles(p.K);
   const long long per = (long long)col_tiles * row_tiles(p.rows);
   const uint32_t places = (uint32_t)__cvta_generic_to_shared(smem) + tid * 16;
-  auto place = [&](int stage, int i) { return places + stage * G::STAGE_BYTES + i * G::THREADS * 16; };
+  auto place = [&](int i) { return places + i * G::THREADS * 16; };
   allow_dependents();
   grid_dependency_wait();
 
@@ -91,7 +128,7 @@ quantize_tiles_kernel(const __grid_constant__ CastParams p, long long items, int
     rt = (int)((it - b * per) / col_tiles);
     ct = (int)(it - b * per - (long long)rt * col_tiles);
   };
-  auto fetch = [&](int stage, long long it) {
+  auto fetch = [&](long long it) {
     if (it < items) {
       int b, rt, ct;
       locate(it, b, rt, ct);
@@ -104,11 +141,11 @@ quantize_tiles_kernel(const __grid_constant__ CastParams p, long long items, int
           const int n = r0 + i < p.rows ? bytes : 0;
           const uint8_t* from = n > 0 ? reinterpret_cast<const uint8_t*>(src + i * p.row_stride) : reinterpret_cast<const uint8_t*>(p.src);
           if (VEC) {
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(place(stage, i)), "l"(from), "r"(n) : "memory");
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(place(i)), "l"(from), "r"(n) : "memory");
           } else {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(place(stage, i) + 4 * k), "l"(4 * k < n ? from + 4 * k : from), "r"(4 * k < n ? 4 : 0) : "memory");
+              asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(place(i) + 4 * k), "l"(4 * k < n ? from + 4 * k : from), "r"(4 * k < n ? 4 : 0) : "memory");
           }
         }
       } else {
@@ -117,90 +154,85 @@ quantize_tiles_kernel(const __grid_constant__ CastParams p, long long items, int
         for (int i = 0; i < 8; ++i) q[i].load(src + i * p.row_stride, r0 + i < p.rows ? left : 0, false);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(place(stage, i)), "r"(q[i].w[0]), "r"(q[i].w[1]), "r"(q[i].w[2]),
+          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(place(i)), "r"(q[i].w[0]), "r"(q[i].w[1]), "r"(q[i].w[2]),
                        "r"(q[i].w[3]) : "memory");
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  auto read = [&](int stage, int i, Piece<T, VN>& q) {
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(q.w[0]), "=r"(q.w[1]), "=r"(q.w[2]), "=r"(q.w[3]) : "r"(place(stage, i)) : "memory");
-  };
 
-  fetch(0, blockIdx.x);
-  int stage = 0;
-  for (long long it = blockIdx.x; it < items; it += gridDim.x, stage ^= 1) {
-    fetch(stage ^ 1, it + gridDim.x);
-    asm volatile("cp.async.wait_group %0;" ::"n"(G::STAGES - 1) : "memory");
+  fetch(blockIdx.x);
+  int turn = 0;
+  for (long long it = blockIdx.x; it < items; it += gridDim.x, turn ^= 1) {
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
     int b, rt, ct;
     locate(it, b, rt, ct);
     const int r0 = rt * 128 + rg * 8, c0 = ct * 128;
+    Piece<T, VN> x[8];
+    uint32_t most[4], row_most[8];           // words of magnitudes: largest of the thread's columns, of its rows
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x[i].w[0]), "=r"(x[i].w[1]), "=r"(x[i].w[2]), "=r"(x[i].w[3]) : "r"(place(i)) : "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      uint32_t a[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        a[k] = word_abs<T>(x[i].w[k]);
+        most[k] = i == 0 ? a[k] : word_max<T>(most[k], a[k]);
+      }
+      row_most[i] = word_max<T>(word_max<T>(a[0], a[1]), word_max<T>(a[2], a[3]));
+    }
+    fetch(it + gridDim.x);                   // the places are free: this tile is in registers
     uint32_t byte = 0, inv = 0;              // square: of the tile
     if (p.square) {
-      uint32_t m = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        Piece<T, VN> x;
-        read(stage, i, x);
-        m = max(m, x.amax());
-      }
-      m = __reduce_max_sync(kAll, m);
-      if (lane == 0) whole[stage][warp] = m;
+      uint32_t m = word_max<T>(word_max<T>(most[0], most[1]), word_max<T>(most[2], most[3]));
+      m = __reduce_max_sync(kAll, PER == 2 ? max(m & 0xffff0000u, m << 16) : m);
+      if (lane == 0) whole[turn][warp] = m;
       __syncthreads();
-      m = __reduce_max_sync(kAll, whole[stage][lane % WARPS]);
-      byte = scale_byte(m, inv);
-    }
-    float most[VN];                          // of the thread's columns
+      byte = scale_byte(__reduce_max_sync(kAll, whole[turn][lane % WARPS]), inv);
+    } else if (p.codes_t != nullptr) {
 #pragma unroll
-    for (int j = 0; j < VN; ++j) most[j] = 0.f;
+      for (int k = 0; k < 4; ++k) {
+        if (LANES == 16) most[k] = word_max<T>(most[k], __shfl_xor_sync(kAll, most[k], 16));
+        if (lane < LANES) part[warp][cg * 4 + k] = most[k];
+      }
+    }
     if (p.codes != nullptr) {
       uint8_t* to = p.codes + ((size_t)b * p.out_rows + p.first + (size_t)r0 * p.step) * pitch + c0 + cg * VN;
       const size_t next = (size_t)p.step * pitch;
       const int n = c0 + cg * VN < pitch ? p.rows - r0 : 0;                              // rows to write
+      uint2 bytes = make_uint2(0, 0);
+      if (!p.square) {
+        rows_scales<T>(row_most, cg, row_byte + rg * 8);
+        __syncwarp();
+        bytes = *reinterpret_cast<const uint2*>(row_byte + rg * 8);
+      }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        Piece<T, VN> x;
-        float v[VN];
-        read(stage, i, x);
-        x.values(v);
         uint32_t bi = byte, vi = inv, q[VN / 4];
         if (!p.square) {
-#pragma unroll
-          for (int j = 0; j < VN; ++j) most[j] = max_abs(most[j], v[j]);
-          bi = scale_byte(lanes_max<LANES>(x.amax()), vi);
-          if (cg == 0) row_byte[rg * 8 + i] = (uint8_t)bi;
+          bi = (i < 4 ? bytes.x : bytes.y) >> (8 * (i & 3)) & 255u;
+          vi = (254u - bi) << 23;            // (of no use where the byte is 255)
         }
+        float v[VN];
+        x[i].values(v);
         cast_codes(v, bi, vi, q);
         if (i < n) {
           if constexpr (VN == 8) *reinterpret_cast<uint2*>(to + i * next) = make_uint2(q[0], q[1]);
           else *reinterpret_cast<uint32_t*>(to + i * next) = q[0];
         }
       }
-    } else if (!p.square) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        Piece<T, VN> x;
-        float v[VN];
-        read(stage, i, x);
-        x.values(v);
-#pragma unroll
-        for (int j = 0; j < VN; ++j) most[j] = max_abs(most[j], v[j]);
-      }
     }
     if (!p.square) {
-#pragma unroll
-      for (int j = 0; j < VN; ++j) {
-        if (LANES == 16) most[j] = max_abs(most[j], __shfl_xor_sync(kAll, most[j], 16));
-        if (lane < LANES) part[warp][cg * VN + j] = most[j];
-      }
       __syncthreads();
-      if (tid < 128) {
-        float m = 0.f;
+      if (p.codes_t != nullptr && tid < 128 / PER) {
+        uint32_t m = part[0][tid];
 #pragma unroll
-        for (int i = 0; i < WARPS; ++i) m = max_abs(m, part[i][tid]);
-        uint32_t iv;
-        byte_of[tid] = (uint8_t)scale_byte(__float_as_uint(m) & 0x7fffffffu, iv);
-        inv_of[tid] = iv;
+        for (int i = 1; i < WARPS; ++i) m = word_max<T>(m, part[i][tid]);
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+          byte_of[tid * PER + k] = (uint8_t)scale_byte(PER == 1 ? m : k == 0 ? m << 16 : m & 0xffff0000u, inv_of[tid * PER + k]);
       }
     }
     if (p.codes != nullptr && tid < 128 && rt * 128 + tid < p.rows)
@@ -212,11 +244,7 @@ quantize_tiles_kernel(const __grid_constant__ CastParams p, long long items, int
     for (int g = 0; g < 2; ++g) {
       float v[4][VN];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        Piece<T, VN> x;
-        read(stage, g * 4 + i, x);
-        x.values(v[i]);
-      }
+      for (int i = 0; i < 4; ++i) x[g * 4 + i].values(v[i]);
 #pragma unroll
       for (int j = 0; j < VN; ++j) {
         const uint32_t bj = p.square ? byte : byte_of[cg * VN + j], vj = p.square ? inv : inv_of[cg * VN + j];
@@ -370,8 +398,6 @@ dispatch_rows_kernel(const mx4::Dispatch q, const T* __restrict__ x, const uint8
   }
 }
 
-template <typename T> constexpr int kTileBlocks = sizeof(T) == 2 ? 2 : 1;       // resident on a multiprocessor
-
 int cast_blocks(long long items) {
   const long long want = (items + kThreads / 32 - 1) / (kThreads / 32), most = 32ll * sm_count();
   return (int)(want < most ? want : most);
@@ -387,7 +413,7 @@ template <typename T, bool VEC> cudaError_t quantize(const CastParams& p, int wo
   if (p.square || p.codes_t != nullptr) {
     static std::atomic<uint64_t> done{0};
     const int col_tiles = (int)((p.K + 127ll) / 128);
-    const long long items = (long long)p.batch * row_tiles(p.rows) * col_tiles, most = kTileBlocks<T> * (long long)sm_count();
+    const long long items = (long long)p.batch * row_tiles(p.rows) * col_tiles, most = Tile<T>::BLOCKS * (long long)sm_count();
     if (!allow_smem((const void*)quantize_tiles_kernel<T, VEC>, Tile<T>::SMEM, done)) return cudaErrorInvalidValue;
     return launch_after_predecessor(quantize_tiles_kernel<T, VEC>, dim3((unsigned)(items < most ? items : most)), dim3(Tile<T>::THREADS),
                                     Tile<T>::SMEM, st, true, p, items, col_tiles, words);

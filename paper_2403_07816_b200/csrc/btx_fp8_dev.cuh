@@ -155,16 +155,17 @@ template <int LANES> __device__ __forceinline__ uint32_t lanes_max(uint32_t m) {
   return m;
 }
 
-// four codes; b == 255: a block that is not a number has codes 0
-__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float inv) {
-  return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a * inv, b * inv), __NV_SATFINITE, __NV_E4M3) |
-         (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(c * inv, d * inv), __NV_SATFINITE, __NV_E4M3) << 16;
-}
-// N codes of a lane's elements, whose block's scale byte is `byte`
+__device__ __forceinline__ uint32_t codes2(float a, float b) { return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3); }
+// N codes of a lane's elements, whose block's scale byte is `byte` (255: a block that is not a number has codes 0)
 template <int N> __device__ __forceinline__ void cast_codes(const float (&v)[N], uint32_t byte, uint32_t inv_bits, uint32_t (&q)[N / 4]) {
-  const float inv = __uint_as_float(inv_bits);
+  const f32x2 inv = pack2(__uint_as_float(inv_bits), __uint_as_float(inv_bits));
 #pragma unroll
-  for (int i = 0; i < N / 4; ++i) q[i] = byte == 255u ? 0u : codes4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], inv);
+  for (int i = 0; i < N / 4; ++i) {
+    float a, b, c, d;
+    unpack2(mul2(pack2(v[4 * i], v[4 * i + 1]), inv), a, b);
+    unpack2(mul2(pack2(v[4 * i + 2], v[4 * i + 3]), inv), c, d);
+    q[i] = byte == 255u ? 0u : codes2(a, b) | codes2(c, d) << 16;
+  }
 }
 __device__ __forceinline__ float scale_value(uint32_t byte) {
   return __uint_as_float(byte == 255u ? 0x7fffffffu : (byte == 0u ? 0x00400000u : byte << 23));
