@@ -350,8 +350,8 @@ dispatch_rows_kernel(const mx4::Dispatch q, const T* __restrict__ x, const uint8
                      uint8_t* __restrict__ scales, I items, int groups) {
   const int lane = threadIdx.x & 31;
   const int kt = (int)scale_tiles_k(q.d);
-  allow_dependents();
   grid_dependency_wait();
+  allow_dependents();                        // in this order: the products start after the dispatch, see fp8_gemm_kernel
   for (I w = ((I)blockIdx.x * kThreads + threadIdx.x) >> 5; w < items; w += (I)gridDim.x * (kThreads / 32)) {
     const size_t t = (size_t)(w / (I)groups);
     const int g = (int)(w - (I)t * (I)groups);

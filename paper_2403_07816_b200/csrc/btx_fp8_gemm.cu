@@ -11,10 +11,10 @@
 //
 // fp8_gemm_kernel:
 //   warp 0, 10  TMA producers (one lane each) of A and of B: ring of stages of 128 contraction elements, a block (swizzled rows
-//               of 128 bytes).  Of A a stage holds only as many rows as a tile can have (a multiple of 32)
-//   warp 1      allocates tensor memory; one lane issues up to four MMAs per stage
-//   warp 15     TMA of the scales: a tile of A and one of B for every four stages
-//   warps 11-14 scales from shared memory into tensor memory, a warp per 32-lane quarter
+//               of 128 bytes), and in every fourth stage a scale tile of each.  Of A a stage holds only as many rows as a
+//               tile can have (a multiple of 32)
+//   warp 1      allocates tensor memory; copies scale tiles there (tcgen05.cp: two tiles for sixteen MMAs; warps that store them
+//               cost 0.7 us a tile, which was the time of four stages) and issues up to four MMAs per stage
 //   warps 2-9   epilogue: a row per thread, two warps per 32-lane quarter, each half of the columns
 // Persistent, two accumulators; or SPLIT: a cluster of 2 to 8 CTAs shares a tile's contraction, each leaves its
 // partial sums in its shared memory and then adds up a slice of the columns over the cluster, in CTA order.
@@ -26,6 +26,7 @@
 //   DOWN     gate-scaled fp32 rows scattered to t*k+slot
 // Every wait is bounded (tcx::mbar_wait); a wait that runs out leaves BTX_ERR_TIMEOUT in the status word.
 #include <cmath>
+#include <cstdlib>
 
 #include "btx_fp8_dev.cuh"
 #include "btx_fp8_gemm.cuh"
@@ -39,16 +40,12 @@ using namespace tcx;
 using mx4::arrive;
 using mx4::BM;
 using mx4::BN;
-using mx4::commit;
 using mx4::EPI_WARPS;
-using mx4::finish_chunk;
 using mx4::get_item;
 using mx4::Item;
-using mx4::ld_shared_v4;
 using mx4::load_3d;
 using mx4::load_bulk;
 using mx4::load_chunk;
-using mx4::store_turned;
 using mx4::TURN_BYTES;
 using mx4::warp_wait;
 using mx4::STORE;
@@ -61,31 +58,70 @@ constexpr int A_BYTES = BM * SKB, B_BYTES = BN * SKB;
 
 struct Params : mx4::Params {
   int accumulate;                                        // STORE: fp32 y is added to
+  int width;                                             // columns of a tile: 64 or 128 (pairs of CTAs: 256)
 };
 
-__device__ __forceinline__ void mma_mxf8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accum) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %6, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accum) : "memory");
+// The MMAs of a stage, `n` of 32 contraction elements each, issued by the lane whose `leader` is not 0; a, b: the low words of the
+// operands' descriptors.  The whole warp comes here: operands of an MMA are uniform registers, and in code for one lane
+// each of them is moved there first, which took longer than the MMAs (86 stages of 4 on a tile of 128 columns: 0.36 us a
+// stage, whatever the columns; 0.29 so).
+constexpr uint32_t kDescHigh = (1024u >> 4) | 1u << 14 | 2u << 29;       // of tcx::smem_desc, K-major
+__device__ __forceinline__ uint32_t desc_low(uint32_t addr) { return (addr & 0x3FFFFu) >> 4 | (16u >> 4) << 16; }
+#define BTX_FP8_MMA(GROUP, P, A, B, F) \
+  "@" P " tcgen05.mma.cta_group::" #GROUP ".kind::mxf8f6f4.block_scale.scale_vec::1X [%0], " A ", " B ", %3, [%4], [%5], " F ";\n\t"
+#define BTX_FP8_MMAS(GROUP)                                                                                                  \
+  if (n == 4) {                                                                                                              \
+    asm volatile(                                                                                                            \
+        "{\n\t.reg .pred l, f, t;\n\t.reg .b32 x;\n\t.reg .b64 a0, a1, a2, a3, b0, b1, b2, b3;\n\t"                          \
+        "setp.ne.b32 l, %7, 0;\n\tsetp.ne.b32 f, %6, 0;\n\tsetp.eq.b32 t, 0, 0;\n\t"                                         \
+        "mov.b64 a0, {%1, %8};\n\tmov.b64 b0, {%2, %8};\n\tadd.s32 x, %1, 2;\n\tmov.b64 a1, {x, %8};\n\t"                    \
+        "add.s32 x, %2, 2;\n\tmov.b64 b1, {x, %8};\n\tadd.s32 x, %1, 4;\n\tmov.b64 a2, {x, %8};\n\t"                         \
+        "add.s32 x, %2, 4;\n\tmov.b64 b2, {x, %8};\n\tadd.s32 x, %1, 6;\n\tmov.b64 a3, {x, %8};\n\t"                         \
+        "add.s32 x, %2, 6;\n\tmov.b64 b3, {x, %8};\n\t"                                                                      \
+        BTX_FP8_MMA(GROUP, "l", "a0", "b0", "f") BTX_FP8_MMA(GROUP, "l", "a1", "b1", "t")                                    \
+        BTX_FP8_MMA(GROUP, "l", "a2", "b2", "t") BTX_FP8_MMA(GROUP, "l", "a3", "b3", "t") "}"                                \
+        ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accum), "r"(leader), "r"(kDescHigh) : "memory");       \
+  } else {                                                                                                                   \
+    for (int j = 0; j < n; ++j)                                                                                              \
+      asm volatile("{\n\t.reg .pred l, f;\n\t.reg .b64 a0, b0;\n\tsetp.ne.b32 l, %7, 0;\n\tsetp.ne.b32 f, %6, 0;\n\t"         \
+                   "mov.b64 a0, {%1, %8};\n\tmov.b64 b0, {%2, %8};\n\t" BTX_FP8_MMA(GROUP, "l", "a0", "b0", "f") "}"         \
+                   ::"r"(d), "r"(a + 2 * j), "r"(b + 2 * j), "r"(idesc), "r"(sfa), "r"(sfb), "r"(j > 0 ? 1u : accum),        \
+                   "r"(leader), "r"(kDescHigh) : "memory");                                                                  \
+  }
+__device__ __forceinline__ void mma_stage(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accum,
+                                          uint32_t leader, int n) {
+  BTX_FP8_MMAS(1)
 }
-__device__ __forceinline__ void mma_mxf8_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
-                                              uint32_t accum) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %6, 0;\n\t"
-      "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accum) : "memory");
+__device__ __forceinline__ void mma_stage_pair(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                               uint32_t accum, uint32_t leader, int n) {
+  BTX_FP8_MMAS(2)
+}
+#undef BTX_FP8_MMAS
+#undef BTX_FP8_MMA
+__device__ __forceinline__ void commit_if(uint32_t bar, uint32_t leader) {
+  asm volatile("{\n\t.reg .pred l;\n\tsetp.ne.b32 l, %1, 0;\n\t"
+               "@l tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(leader) : "memory");
+}
+__device__ __forceinline__ void commit_pair_if(uint32_t bar, uint32_t leader) {
+  asm volatile("{\n\t.reg .pred l;\n\tsetp.ne.b32 l, %1, 0;\n\t"
+               "@l tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %2;\n\t}"
+               ::"r"(bar), "r"(leader), "h"((uint16_t)3) : "memory");
 }
 // e4m3 x e4m3 (type code 0), UE8M0 scales, both operands K-major; byte `id` of the words of scales
 __device__ __forceinline__ constexpr uint32_t instr(int m, int n, uint32_t id) {
   return ((uint32_t)(n >> 3) << 17) | (1u << 23) | ((uint32_t)(m >> 4) << 24) | (id << 4) | (id << 29);
 }
-// This lane's 16 bytes of one scale tile to four tensor-memory columns of the warp's 32-lane quarter
-__device__ __forceinline__ void store_scales4(uint32_t taddr, const uint4& q) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(q.x), "r"(q.y), "r"(q.z), "r"(q.w)
-               : "memory");
+// A scale tile (32 rows of 16 bytes: no swizzle, core matrices of eight rows 128 bytes apart) to four columns of tensor memory,
+// repeated in every 32-lane quarter; of a pair, in both CTAs, each from its own shared memory to its own tensor memory.
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint32_t smem, uint32_t leader) {
+  asm volatile("{\n\t.reg .pred l;\n\t.reg .b64 d;\n\tsetp.ne.b32 l, %3, 0;\n\tmov.b64 d, {%1, %2};\n\t"
+               "@l tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], d;\n\t}"
+               ::"r"(tmem), "r"((smem & 0x3FFFFu) >> 4 | (128u >> 4) << 16), "r"((128u >> 4) | 1u << 14), "r"(leader) : "memory");
+}
+__device__ __forceinline__ void copy_scales_pair(uint32_t tmem, uint32_t smem, uint32_t leader) {
+  asm volatile("{\n\t.reg .pred l;\n\t.reg .b64 d;\n\tsetp.ne.b32 l, %3, 0;\n\tmov.b64 d, {%1, %2};\n\t"
+               "@l tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], d;\n\t}"
+               ::"r"(tmem), "r"((smem & 0x3FFFFu) >> 4 | (128u >> 4) << 16), "r"((128u >> 4) | 1u << 14), "r"(leader) : "memory");
 }
 // A word into CTA `rank`'s shared memory at the offset of `slot`; four bytes complete on its barrier at the offset of `bar`.
 __device__ __forceinline__ void send_word(uint32_t slot, uint32_t bar, uint32_t rank, uint32_t value) {
@@ -125,42 +161,86 @@ __device__ __forceinline__ void store_units(const Params& p, const float* a, int
   }
 }
 
-// STORE with accumulate: what stands in 64 columns of a row of y is added to the sums
-__device__ __forceinline__ void add_old(const Params& p, const Item& it, float (&v)[64], int n0, int flat) {
-  if (!p.accumulate || flat < 0) return;
-  const float* y = (const float*)p.y + ((size_t)it.b * p.M + flat) * p.N + n0;
-  if (p.wide && n0 + 64 <= p.N) {
+// What becomes of 64 accumulator columns n0 .. of a row, of which those below n1 are the tile's.  flat: the row of y (STORE) or
+// its assignment, -1 for a row that nobody asked for.
+template <int MODE>
+__device__ __forceinline__ void put_chunk(const Params& p, const Item& it, float (&v)[64], int n0, int n1, int flat) {
+  if (flat < 0 || n0 >= n1) return;
+  const size_t o = (MODE == STORE ? ((size_t)it.b * p.M + flat) * p.N : (size_t)flat * p.N) + n0;
+  const bool whole = p.wide && n0 + 64 <= n1;
+  if (MODE == DOWN) {
+    const float g = p.gates[flat];
 #pragma unroll
-    for (int i = 0; i < 64; i += 4) {
-      const float4 o = *reinterpret_cast<const float4*>(y + i);
-      v[i] += o.x; v[i + 1] += o.y; v[i + 2] += o.z; v[i + 3] += o.w;
+    for (int i = 0; i < 64; ++i) v[i] *= g;
+  }
+  if (MODE == STORE && p.out_bf16) {
+    __nv_bfloat16* y = (__nv_bfloat16*)p.y + o;
+    if (whole) {
+#pragma unroll
+      for (int i = 0; i < 64; i += 16) st32(y + i, pack8(v + i), pack8(v + i + 8), true);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 64; ++i)
+        if (n0 + i < n1) y[i] = __float2bfloat16_rn(v[i]);
     }
+    return;
+  }
+  float* y = (float*)p.y + o;
+  if (whole) {
+    if (MODE == STORE && p.accumulate) {
+#pragma unroll
+      for (int i = 0; i < 64; i += 4) {
+        const float4 q = *reinterpret_cast<const float4*>(y + i);
+        v[i] += q.x; v[i + 1] += q.y; v[i + 2] += q.z; v[i + 3] += q.w;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 64; i += 8) st32(y + i, f4(v + i), f4(v + i + 4), true);
   } else {
 #pragma unroll
     for (int i = 0; i < 64; ++i)
-      if (n0 + i < p.N) v[i] += y[i];
+      if (n0 + i < n1) y[i] = MODE == STORE && p.accumulate ? v[i] + y[i] : v[i];
+  }
+}
+// STORE where rows of y do not start on 32-byte boundaries: a warp turns its 32 rows through shared memory
+__device__ __forceinline__ void put_turned(const Params& p, const Item& it, float (&v)[64], int n0, int n1, int m0, int lane, uint32_t* st) {
+  if (n0 >= n1) return;
+  const size_t o = ((size_t)it.b * p.M + m0) * p.N + n0;
+  const int rows = p.M - m0, cols = n1 - n0;
+  if (!p.out_bf16) {
+    if (p.accumulate && lane < rows) {
+      const float* y = (const float*)p.y + o + (size_t)lane * p.N;
+#pragma unroll
+      for (int i = 0; i < 64; ++i)
+        if (i < cols) v[i] += y[i];
+    }
+    mx4::turn_words<uint32_t, 1>((uint32_t*)p.y + o, p.N, rows, cols, lane, st, [&](int i) { return __float_as_uint(v[i]); });
+  } else if ((p.N & 1) == 0 && ((uintptr_t)p.y & 3) == 0) {
+    mx4::turn_words<uint32_t, 2>((uint32_t*)((__nv_bfloat16*)p.y + o), p.N, rows, cols, lane, st, [&](int i) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+      return *reinterpret_cast<const uint32_t*>(&h);
+    });
+  } else {
+    mx4::turn_words<uint16_t, 1>((uint16_t*)p.y + o, p.N, rows, cols, lane, st, [&](int i) {
+      return (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v[i]));
+    });
   }
 }
 
 // ---------------------------------------------------------------------------------------------
-// One CTA on a 128 x 128 tile
+// One CTA on a tile of 128 rows and up to 128 columns
 // ---------------------------------------------------------------------------------------------
-constexpr int THREADS = 512;
-constexpr int MAX_STAGES = 10, SF_SLOTS = 4;             // stages of codes; groups of scales, in shared and in tensor memory
-constexpr int SF_BYTES = 2 * kTileBytes, SF_COLS = 8, SF_COL0 = 2 * BN;
+constexpr int THREADS = 96 + EPI_WARPS * 32;
+constexpr int MAX_STAGES = 20;
+constexpr int SF_BYTES = 2 * kTileBytes;                 // of a stage: scale tiles of A and of B
+constexpr int SF_COLS = 8, SF_COL0 = 2 * BN, SF_SLOTS = 8;               // tensor memory: scale tiles of the last eight copies
 constexpr int XCH_BYTES = 2 * 4 * BM * 4;                // GATE_UP: two tiles' largest units, four for every row
-constexpr int RING_BYTES = 217 * 1024;
+constexpr int RING_BYTES = 219 * 1024;
 constexpr int CTL_BYTES = 384;
-constexpr int SMEM_BYTES = RING_BYTES + SF_SLOTS * SF_BYTES + XCH_BYTES + CTL_BYTES + 1024;
+constexpr int SMEM_BYTES = RING_BYTES + XCH_BYTES + CTL_BYTES + 1024;
 constexpr int PART_PITCH = BN + 4;                       // SPLIT: floats per row of a partial tile (a quad apart: no bank conflicts)
 static_assert(SMEM_BYTES <= 227 * 1024 && BM * PART_PITCH * 4 <= RING_BYTES && SF_COL0 + SF_SLOTS * SF_COLS <= 512, "memory");
-static_assert(MAX_STAGES * 16 + SF_SLOTS * 32 + 48 + 16 <= CTL_BYTES, "control block");
-
-inline __host__ __device__ int stage_bytes(int rows) { return rows * SKB + B_BYTES; }
-inline __host__ __device__ int stage_count(int rows, int ring_bytes) {
-  const int n = ring_bytes / stage_bytes(rows);
-  return n < MAX_STAGES ? n : MAX_STAGES;
-}
+static_assert(MAX_STAGES * 16 + 48 + 16 <= CTL_BYTES, "control block");
 
 template <int MODE, bool SPLIT>
 __global__ void __launch_bounds__(THREADS, 1)
@@ -168,26 +248,23 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t ring = (raw + 1023u) & ~1023u;
-  const uint32_t sf_ring = ring + RING_BYTES, xch = sf_ring + SF_SLOTS * SF_BYTES;
+  const uint32_t xch = ring + RING_BYTES;
   uint8_t* ctl = smem_raw + (xch + XCH_BYTES - raw);
   const uint32_t bar_full = smem_u32(ctl), bar_empty = bar_full + MAX_STAGES * 8;
-  const uint32_t bar_sfull = bar_empty + MAX_STAGES * 8, bar_sempty = bar_sfull + SF_SLOTS * 8;
-  const uint32_t bar_sready = bar_sempty + SF_SLOTS * 8, bar_sfree = bar_sready + SF_SLOTS * 8;
-  const uint32_t bar_tfull = bar_sfree + SF_SLOTS * 8, bar_tempty = bar_tfull + 16, bar_xch = bar_tempty + 16;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctl + MAX_STAGES * 16 + SF_SLOTS * 32 + 48);
+  const uint32_t bar_tfull = bar_empty + MAX_STAGES * 8, bar_tempty = bar_tfull + 16, bar_xch = bar_tempty + 16;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctl + MAX_STAGES * 16 + 48);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(kAll, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   constexpr bool TWIN = MODE == GATE_UP;                  // a cluster of two CTAs on neighbouring column tiles
   const bool turn = MODE == STORE && !SPLIT && !p.wide;   // a piece of the ring turns tiles around
   const int ring_bytes = RING_BYTES - (turn ? EPI_WARPS * TURN_BYTES : 0);
-  const int n_stages = stage_count(p.a_rows, ring_bytes), s_bytes = stage_bytes(p.a_rows);
+  // Codes of the stages (an MMA reads 128 rows of A, from the last one too: they come first), then their scales.
+  const int s_bytes = (p.a_rows + p.width) * SKB;
+  const int n_stages = min(MAX_STAGES, (ring_bytes - max(0, A_BYTES - s_bytes)) / (s_bytes + SF_BYTES));
+  const uint32_t scales = ring + n_stages * s_bytes;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < n_stages; ++s) { mbar_init(bar_full + s * 8, 2); mbar_init(bar_empty + s * 8, 1); }
-    for (int s = 0; s < SF_SLOTS; ++s) {
-      mbar_init(bar_sfull + s * 8, 1); mbar_init(bar_sempty + s * 8, 4);
-      mbar_init(bar_sready + s * 8, 4); mbar_init(bar_sfree + s * 8, 1);
-    }
     for (int a = 0; a < 2; ++a) { mbar_init(bar_tfull + a * 8, 1); mbar_init(bar_tempty + a * 8, EPI_WARPS); mbar_init(bar_xch + a * 8, 1); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -203,7 +280,9 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   allow_dependents();
-  grid_dependency_wait();
+  // The layer's weights, and what its dispatch wrote, do not come from the kernel before (which let this one start only after
+  // the dispatch was done): they are on their way while it runs.
+  if (MODE == STORE || warp != 10) grid_dependency_wait();
   // a product of its own clears its status word (a wait of another CTA cannot have run out yet)
   if (MODE == STORE && blockIdx.x == 0 && threadIdx.x < kStatusWords) p.status[threadIdx.x] = 0;
   const int m_tiles = p.grouped ? p.n_row_tiles[0] : p.m_tiles;
@@ -229,16 +308,21 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         const Item it = item(t);
         const int rows = min(p.grouped ? p.tile_rows[it.mt] : p.M - it.mt * BM, p.a_rows);
         const int boxes = (rows + p.a_box - 1) / p.a_box;
+        const uint8_t* sf = warp == 0 ? p.a_scales + it.b * p.a_scale_batch + (size_t)it.mt * p.kt * kTileBytes
+                                      : p.b_scales + it.e * p.b_scale_batch +
+                                            (size_t)min(it.nt * p.width / kTileRows, p.b_row_tiles - 1) * p.kt * kTileBytes;
         for (int kb = kb0; kb < kb1; ++kb) {
           if (!(ok = mbar_wait(bar_empty + stage * 8, phase ^ 1u, abort_flag, p.status))) break;
-          const uint32_t bar = bar_full + stage * 8, sA = ring + stage * s_bytes;
+          const uint32_t bar = bar_full + stage * 8, sA = ring + stage * s_bytes, sS = scales + stage * SF_BYTES;
+          const bool first = kb % SF_GROUP == 0 || kb == kb0;            // brings the scales of its group
           if (warp == 0) {
-            mbar_expect_tx(bar, boxes * p.a_box * SKB);
+            mbar_expect_tx(bar, boxes * p.a_box * SKB + (first ? kTileBytes : 0));
             for (int i = 0; i < boxes; ++i) load_3d(sA + i * p.a_box * SKB, &tmA, kb * SKB, it.mt * BM + i * p.a_box, it.b, bar);
           } else {
-            mbar_expect_tx(bar, B_BYTES);
-            load_3d(sA + p.a_rows * SKB, &tmB, kb * SKB, it.nt * BN, it.e, bar);
+            mbar_expect_tx(bar, p.width * SKB + (first ? kTileBytes : 0));
+            load_3d(sA + p.a_rows * SKB, &tmB, kb * SKB, it.nt * p.width, it.e, bar);
           }
+          if (first) load_bulk(warp == 0 ? sS : sS + kTileBytes, sf + (size_t)(kb / SF_GROUP) * kTileBytes, kTileBytes, bar);
           if (++stage == n_stages) { stage = 0; phase ^= 1u; }
         }
       }
@@ -248,81 +332,35 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
       }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      // The MMA reads 128 rows of A: those past the stage's A part (other bytes of the stage) give rows nobody reads.
-      uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0, slot = 0, slot_phase = 0;
-      bool ok = true;
-      for (int t = t0; t < n_total && ok; t += t_step) {
-        if (!(ok = mbar_wait(bar_tempty + acc * 8, acc_phase ^ 1u, abort_flag, p.status))) break;
-        tc_fence_after();
-        const uint32_t d = tmem + acc * BN;
-        for (int kb = kb0; kb < kb1; ++kb) {
-          const uint32_t id = kb % SF_GROUP;
-          if ((id == 0 || kb == kb0) && !(ok = mbar_wait(bar_sready + slot * 8, slot_phase, abort_flag, p.status))) break;
-          if (!(ok = mbar_wait(bar_full + stage * 8, phase, abort_flag, p.status))) break;
-          tc_fence_after();
-          const uint32_t sA = ring + stage * s_bytes, sB = sA + p.a_rows * SKB;
-          const uint32_t tA = tmem + SF_COL0 + slot * SF_COLS, tB = tA + 4;
-          const int k32 = min(SKB / 32, (p.K - kb * SKB + 31) / 32);      // MMAs that hold elements
-          const uint64_t da = smem_desc(sA, false), db = smem_desc(sB, false);
-#pragma unroll
-          for (int j = 0; j < SKB / 32; ++j)
-            if (j < k32) mma_mxf8(d, da + (uint64_t)(2 * j), db + (uint64_t)(2 * j), instr(BM, BN, id), tA, tB, (kb > kb0 || j > 0) ? 1u : 0u);
-          commit(bar_empty + stage * 8);
-          if (++stage == n_stages) { stage = 0; phase ^= 1u; }
-          if (id == SF_GROUP - 1 || kb == kb1 - 1) {
-            commit(bar_sfree + slot * 8);
-            if (++slot == SF_SLOTS) { slot = 0; slot_phase ^= 1u; }
-          }
-        }
-        if (!ok) break;
-        commit(bar_tfull + acc * 8);
-        acc ^= 1u;
-        if (acc == 0) acc_phase ^= 1u;
-      }
-    }
-  } else if (warp == 15) {
-    if (lane == 0) {
-      uint32_t slot = 0, phase = 0;
-      bool ok = true;
-      for (int t = t0; t < n_total && ok; t += t_step) {
-        const Item it = item(t);
-        const uint8_t* sfa = p.a_scales + it.b * p.a_scale_batch + (size_t)it.mt * p.kt * kTileBytes;
-        const uint8_t* sfb = p.b_scales + it.e * p.b_scale_batch + (size_t)min(it.nt, p.b_row_tiles - 1) * p.kt * kTileBytes;
-        for (int g = kb0 / SF_GROUP; g <= (kb1 - 1) / SF_GROUP; ++g) {
-          if (!(ok = mbar_wait(bar_sempty + slot * 8, phase ^ 1u, abort_flag, p.status))) break;
-          const uint32_t bar = bar_sfull + slot * 8, to = sf_ring + slot * SF_BYTES;
-          mbar_expect_tx(bar, SF_BYTES);
-          load_bulk(to, sfa + (size_t)g * kTileBytes, kTileBytes, bar);
-          load_bulk(to + kTileBytes, sfb + (size_t)g * kTileBytes, kTileBytes, bar);
-          if (++slot == SF_SLOTS) { slot = 0; phase ^= 1u; }
-        }
-      }
-      for (int i = 0; i < SF_SLOTS && ok; ++i) {          // every copy has landed and has been read
-        ok = mbar_wait(bar_sempty + slot * 8, phase ^ 1u, abort_flag, p.status);
-        if (++slot == SF_SLOTS) { slot = 0; phase ^= 1u; }
-      }
-    }
-  } else if (warp > 10) {
-    uint32_t slot = 0, phase = 0;
+    // The MMA reads 128 rows of A: those past the stage's A part (other bytes of the ring) give rows nobody reads.
+    const uint32_t leader = lane == 0;
+    uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0, slot = 0;
+    const uint32_t low_b = p.a_rows * SKB >> 4, idesc0 = instr(BM, p.width, 0);
+    const int tail = (p.K - (kb_all - 1) * SKB + 31) / 32;               // MMAs of the last stage that hold elements
     bool ok = true;
     for (int t = t0; t < n_total && ok; t += t_step) {
-      for (int g = kb0 / SF_GROUP; g <= (kb1 - 1) / SF_GROUP; ++g) {
-        if (!(ok = warp_wait(bar_sfull + slot * 8, phase, abort_flag, p.status))) break;
-        const uint32_t from = sf_ring + slot * SF_BYTES + lane * 16;
-        const uint4 a = ld_shared_v4(from), b = ld_shared_v4(from + kTileBytes);
-        // the MMAs that read this slot's last scales have retired
-        if (!(ok = warp_wait(bar_sfree + slot * 8, phase ^ 1u, abort_flag, p.status))) break;
+      const uint32_t b_col = 4 + item(t).nt * p.width % kTileRows / 32;  // of the tile's first column among those of the scales
+      if (!(ok = warp_wait(bar_tempty + acc * 8, acc_phase ^ 1u, abort_flag, p.status))) break;
+      const uint32_t d = tmem + acc * BN;
+      uint32_t tA = 0;
+      for (int kb = kb0; kb < kb1; ++kb) {
+        if (!(ok = warp_wait(bar_full + stage * 8, phase, abort_flag, p.status))) break;
         tc_fence_after();
-        mx4::store_scales(tmem + SF_COL0 + slot * SF_COLS + ((uint32_t)((warp & 3) * 32) << 16), a, b);
-        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-        tc_fence_before();
-        if (lane == 0) {
-          arrive(bar_sready + slot * 8);
-          arrive(bar_sempty + slot * 8);
+        const uint32_t id = kb % SF_GROUP, low = desc_low(ring + stage * s_bytes);
+        if (id == 0 || kb == kb0) {
+          tA = tmem + SF_COL0 + slot * SF_COLS;
+          slot = (slot + 1) % SF_SLOTS;
+          copy_scales(tA, scales + stage * SF_BYTES, leader);
+          copy_scales(tA + 4, scales + stage * SF_BYTES + kTileBytes, leader);
         }
-        if (++slot == SF_SLOTS) { slot = 0; phase ^= 1u; }
+        mma_stage(d, low, low + low_b, idesc0 | id << 4 | id << 29, tA, tA + b_col, kb > kb0, leader, kb == kb_all - 1 ? tail : SKB / 32);
+        commit_if(bar_empty + stage * 8, leader);
+        if (++stage == n_stages) { stage = 0; phase ^= 1u; }
       }
+      if (!ok) break;
+      commit_if(bar_tfull + acc * 8, leader);
+      acc ^= 1u;
+      if (acc == 0) acc_phase ^= 1u;
     }
   } else {
     const int q = warp & 3, half = (warp - 2) >> 2;
@@ -340,7 +378,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
       if (any) load_chunk(tmem + acc * BN + half * 64 + ((uint32_t)(q * 32) << 16), v);
       tc_fence_before();
       if (lane == 0) arrive(bar_tempty + acc * 8);        // the accumulator is read: the next tile may have it
-      const int n0 = it.nt * BN + half * 64;
+      const int n0 = it.nt * p.width + half * 64, n1 = min(p.N, (it.nt + 1) * p.width);
       if (MODE == GATE_UP) {
         // A tile's maxima take place acc of two: nobody writes to it again before everybody has passed the next tile's barrier.
         const int F = p.N / 2, f0 = n0 / 2;
@@ -370,12 +408,11 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                          "f"(v[i + 3]) : "memory");
         }
       } else if (any) {
-        if (MODE == STORE) add_old(p, it, v, n0, flat);
         if (turn)
-          store_turned(p, it, v, n0, it.mt * BM + q * 32, lane,
-                       reinterpret_cast<uint32_t*>(smem_raw + (ring - raw) + ring_bytes + (warp - 2) * TURN_BYTES));
+          put_turned(p, it, v, n0, n1, it.mt * BM + q * 32, lane,
+                     reinterpret_cast<uint32_t*>(smem_raw + (ring - raw) + ring_bytes + (warp - 2) * TURN_BYTES));
         else
-          finish_chunk<MODE == GATE_UP ? STORE : MODE>(p, it, v, n0, m, flat);
+          put_chunk<MODE>(p, it, v, n0, n1, flat);
       }
       acc ^= 1u;
       if (acc == 0) acc_phase ^= 1u;
@@ -393,8 +430,8 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     if (t0 < n_total && !*abort_flag) {
       const Item it = item(t0);
       const int rows = p.grouped ? p.tile_rows[it.mt] : min(BM, p.M - it.mt * BM);
-      const int width = BN / p.split, c0 = rank * width, n0 = it.nt * BN + c0;
-      const int cols = min(width, p.N - n0);
+      const int slice = (p.width / p.split + 3) / 4 * 4, c0 = rank * slice, n0 = it.nt * p.width + c0;
+      const int cols = min(min(slice, p.width - c0), p.N - n0);
       const int quads = (cols + 3) / 4;                   // (none where cols is negative: the slice lies past the last column)
       for (int i = threadIdx.x; i < rows * quads; i += THREADS) {
         const int r = i / quads, c = (i - r * quads) * 4;
@@ -445,19 +482,18 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
 // would fetch for the same products.  Tensor memory: an accumulator takes 256 of the 512 columns, so two do not fit beside
 // the scales whole.  They overlap in 128 columns: 0..255 and 128..383.  The epilogue reads the shared columns of a tile
 // into registers first and hands them over, so the next tile starts before anything is computed or stored.
-//   warp 0  TMA   warp 1  MMAs (one lane of the leader CTA)   warps 2-9  epilogue, two 64-column chunks each
-//   warps 10-13  scales   warp 14  TMA of the scales: a tile of A, one of each half of B for every four stages
+//   warp 0  TMA   warp 1  scale copies and MMAs (the leader CTA's)   warps 2-9  epilogue, two 64-column chunks each
 // GATE_UP: a tile's 256 columns are a block of 128 units; the two warps of a row hand each other the largest of theirs.
-constexpr int P_STAGES = 6, P_SLOTS = 4;
+constexpr int P_STAGES = 6, P_SLOTS = 8;
 constexpr int P_STAGE_BYTES = A_BYTES + B_BYTES;
-constexpr int P_SF_BYTES = 3 * kTileBytes, P_SF_COLS = 12;
+constexpr int P_SF_BYTES = 3 * kTileBytes, P_SF_COLS = 12;               // of a stage and CTA: a scale tile of A, one of each half of B
 constexpr int P_ACC1 = 128, P_SF0 = 384;
 constexpr int P_XCH_BYTES = 2 * 2 * BM * 4;
-constexpr int P_THREADS = 64 + EPI_WARPS * 32 + 160;
-constexpr int P_CTL_BYTES = 384;
-constexpr int P_SMEM = P_STAGES * P_STAGE_BYTES + P_SLOTS * P_SF_BYTES + EPI_WARPS * TURN_BYTES + P_XCH_BYTES + P_CTL_BYTES + 1024;
+constexpr int P_THREADS = 64 + EPI_WARPS * 32;
+constexpr int P_CTL_BYTES = 256;
+constexpr int P_SMEM = P_STAGES * (P_STAGE_BYTES + P_SF_BYTES) + EPI_WARPS * TURN_BYTES + P_XCH_BYTES + P_CTL_BYTES + 1024;
 static_assert(P_SF0 + P_SLOTS * P_SF_COLS <= 512 && P_ACC1 + 256 <= P_SF0, "tensor memory");
-static_assert(P_STAGES * 16 + P_SLOTS * 32 + 24 + 64 + 16 <= P_CTL_BYTES && P_SMEM <= 227 * 1024, "shared memory");
+static_assert(P_STAGES * 16 + 24 + 64 + 16 <= P_CTL_BYTES && P_SMEM <= 227 * 1024, "shared memory");
 
 template <int MODE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
@@ -466,26 +502,20 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t ring = (raw + 1023u) & ~1023u;
-  const uint32_t sf_ring = ring + P_STAGES * P_STAGE_BYTES, turned = sf_ring + P_SLOTS * P_SF_BYTES;
+  const uint32_t scales = ring + P_STAGES * P_STAGE_BYTES, turned = scales + P_STAGES * P_SF_BYTES;
   const uint32_t xch = turned + EPI_WARPS * TURN_BYTES;
   const bool turn = MODE == STORE && !p.wide;
   uint8_t* ctl = smem_raw + (xch + P_XCH_BYTES - raw);
   const uint32_t bar_full = smem_u32(ctl), bar_empty = bar_full + P_STAGES * 8;
-  const uint32_t bar_sfull = bar_empty + P_STAGES * 8, bar_sempty = bar_sfull + P_SLOTS * 8;
-  const uint32_t bar_sready = bar_sempty + P_SLOTS * 8, bar_sfree = bar_sready + P_SLOTS * 8;      // sready: used in the leader
-  const uint32_t bar_tfull = bar_sfree + P_SLOTS * 8, bar_handed = bar_tfull + 16, bar_xch = bar_handed + 8;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctl + P_STAGES * 16 + P_SLOTS * 32 + 24 + 64);
+  const uint32_t bar_tfull = bar_empty + P_STAGES * 8, bar_handed = bar_tfull + 16, bar_xch = bar_handed + 8;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctl + P_STAGES * 16 + 24 + 64);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(kAll, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < P_STAGES; ++s) { mbar_init(bar_full + s * 8, 1); mbar_init(bar_empty + s * 8, 1); }
-    for (int s = 0; s < P_SLOTS; ++s) {
-      mbar_init(bar_sfull + s * 8, 1); mbar_init(bar_sempty + s * 8, 4);
-      mbar_init(bar_sready + s * 8, 8); mbar_init(bar_sfree + s * 8, 1);
-    }
     for (int a = 0; a < 2; ++a) mbar_init(bar_tfull + a * 8, 1);
     mbar_init(bar_handed, 2 * EPI_WARPS);
     for (int a = 0; a < 8; ++a) mbar_init(bar_xch + a * 8, 2);
@@ -516,14 +546,20 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
       for (int t = pair; t < n_total && ok; t += n_pairs) {
         const Item it = get_item(p, m_tiles, t);
         const int row0 = it.mt * 256 + (int)rank * 128, col0 = it.nt * 256 + (int)rank * 128;
+        const int a_tile = it.b * p.a_row_tiles + it.mt * 2 + (int)rank, b_tile = it.e * p.b_row_tiles + it.nt * 2;
         for (int kb = 0; kb < kb_total; ++kb) {
           if (!(ok = mbar_wait(bar_empty + stage * 8, phase ^ 1u, abort_flag, p.status))) break;
           const uint32_t full_local = bar_full + stage * 8;
           const uint32_t full = map_to_cta(full_local, 0);
           const uint32_t sA = ring + stage * P_STAGE_BYTES, sB = sA + A_BYTES;
-          if (rank == 0) mbar_expect_tx(full_local, 2 * P_STAGE_BYTES);
+          const bool first = kb % SF_GROUP == 0;                         // brings the scales of its group
+          if (rank == 0) mbar_expect_tx(full_local, 2 * (P_STAGE_BYTES + (first ? P_SF_BYTES : 0)));
           tma_load_3d(sA, &tmA, kb * SKB, row0, it.b, full);
           tma_load_3d(sB, &tmB, kb * SKB, col0, it.e, full);
+          if (first) {                                                   // (tiles past the end of either matrix arrive as zeros)
+            tma_load_3d(scales + stage * P_SF_BYTES, &tmSA, 0, kb / SF_GROUP, a_tile, full);
+            tma_load_3d(scales + stage * P_SF_BYTES + kTileBytes, &tmSB, 0, kb / SF_GROUP, b_tile, full);
+          }
           if (++stage == P_STAGES) { stage = 0; phase ^= 1u; }
         }
       }
@@ -533,84 +569,35 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
       }
     }
   } else if (warp == 1) {
-    if (lane == 0 && rank == 0) {
-      uint32_t stage = 0, phase = 0, acc = 0, tile = 0, slot = 0, slot_phase = 0;
-      bool ok = true;
-      for (int t = pair; t < n_total && ok; t += n_pairs, ++tile) {
-        // the tile before has handed over the shared columns
-        if (tile > 0 && !(ok = mbar_wait(bar_handed, (tile - 1) & 1u, abort_flag, p.status))) break;
+    const uint32_t leader = lane == 0;
+    uint32_t stage = 0, phase = 0, acc = 0, tile = 0, slot = 0;
+    const uint32_t idesc0 = instr(256, 256, 0);
+    const int tail = (p.K - (kb_total - 1) * SKB + 31) / 32;             // MMAs of the last stage that hold elements
+    bool ok = rank == 0;
+    for (int t = pair; t < n_total && ok; t += n_pairs, ++tile) {
+      // the tile before has handed over the shared columns
+      if (tile > 0 && !(ok = warp_wait(bar_handed, (tile - 1) & 1u, abort_flag, p.status))) break;
+      const uint32_t d = tmem + (acc ? P_ACC1 : 0);
+      uint32_t tA = 0;
+      for (int kb = 0; kb < kb_total; ++kb) {
+        if (!(ok = warp_wait(bar_full + stage * 8, phase, abort_flag, p.status))) break;
         tc_fence_after();
-        const uint32_t d = tmem + (acc ? P_ACC1 : 0);
-        for (int kb = 0; kb < kb_total; ++kb) {
-          const uint32_t id = kb % SF_GROUP;
-          if (id == 0 && !(ok = mbar_wait(bar_sready + slot * 8, slot_phase, abort_flag, p.status))) break;
-          if (!(ok = mbar_wait(bar_full + stage * 8, phase, abort_flag, p.status))) break;
-          tc_fence_after();
-          const uint32_t sA = ring + stage * P_STAGE_BYTES, sB = sA + A_BYTES;
-          const uint32_t tA = tmem + P_SF0 + slot * P_SF_COLS, tB = tA + 4;
-          const int k32 = min(SKB / 32, (p.K - kb * SKB + 31) / 32);
-          const uint64_t da = smem_desc(sA, false), db = smem_desc(sB, false);
-#pragma unroll
-          for (int j = 0; j < SKB / 32; ++j)
-            if (j < k32) mma_mxf8_pair(d, da + (uint64_t)(2 * j), db + (uint64_t)(2 * j), instr(256, 256, id), tA, tB, (kb > 0 || j > 0) ? 1u : 0u);
-          tc_commit_pair(bar_empty + stage * 8);
-          if (++stage == P_STAGES) { stage = 0; phase ^= 1u; }
-          if (id == SF_GROUP - 1 || kb == kb_total - 1) {
-            tc_commit_pair(bar_sfree + slot * 8);
-            if (++slot == P_SLOTS) { slot = 0; slot_phase ^= 1u; }
-          }
+        const uint32_t id = kb % SF_GROUP, low = desc_low(ring + stage * P_STAGE_BYTES);
+        if (id == 0) {
+          const uint32_t from = scales + stage * P_SF_BYTES;
+          tA = tmem + P_SF0 + slot * P_SF_COLS;
+          slot = (slot + 1) % P_SLOTS;
+          copy_scales_pair(tA, from, leader);
+          copy_scales_pair(tA + 4, from + kTileBytes, leader);
+          copy_scales_pair(tA + 8, from + 2 * kTileBytes, leader);
         }
-        if (!ok) break;
-        tc_commit_pair(bar_tfull + acc * 8);
-        acc ^= 1u;
+        mma_stage_pair(d, low, low + (A_BYTES >> 4), idesc0 | id << 4 | id << 29, tA, tA + 4, kb > 0, leader, kb == kb_total - 1 ? tail : SKB / 32);
+        commit_pair_if(bar_empty + stage * 8, leader);
+        if (++stage == P_STAGES) { stage = 0; phase ^= 1u; }
       }
-    }
-  } else if (warp == 14) {
-    // ---- TMA of the scales; tiles past the end of either matrix arrive as zeros ----
-    if (lane == 0) {
-      uint32_t slot = 0, phase = 0;
-      bool ok = true;
-      for (int t = pair; t < n_total && ok; t += n_pairs) {
-        const Item it = get_item(p, m_tiles, t);
-        const int a_tile = it.b * p.a_row_tiles + it.mt * 2 + (int)rank, b_tile = it.e * p.b_row_tiles + it.nt * 2;
-        for (int g = 0; g < p.kt; ++g) {
-          if (!(ok = mbar_wait(bar_sempty + slot * 8, phase ^ 1u, abort_flag, p.status))) break;
-          const uint32_t bar = bar_sfull + slot * 8, to = sf_ring + slot * P_SF_BYTES;
-          mbar_expect_tx(bar, P_SF_BYTES);
-          load_3d(to, &tmSA, 0, g, a_tile, bar);
-          load_3d(to + kTileBytes, &tmSB, 0, g, b_tile, bar);
-          if (++slot == P_SLOTS) { slot = 0; phase ^= 1u; }
-        }
-      }
-      for (int i = 0; i < P_SLOTS && ok; ++i) {            // every copy has landed and has been read
-        ok = mbar_wait(bar_sempty + slot * 8, phase ^ 1u, abort_flag, p.status);
-        if (++slot == P_SLOTS) { slot = 0; phase ^= 1u; }
-      }
-    }
-  } else if (warp >= 2 + EPI_WARPS) {
-    // ---- scales: word c of a lane's 16 bytes is row c * 32 + lane of a tile, and column c of tensor memory ----
-    const uint32_t taddr = tmem + P_SF0 + ((uint32_t)((warp & 3) * 32) << 16);
-    const uint32_t ready = map_to_cta(bar_sready, 0);
-    uint32_t slot = 0, phase = 0;
-    bool ok = true;
-    for (int t = pair; t < n_total && ok; t += n_pairs) {
-      for (int g = 0; g < p.kt; ++g) {
-        if (!(ok = warp_wait(bar_sfull + slot * 8, phase, abort_flag, p.status))) break;
-        const uint32_t from = sf_ring + slot * P_SF_BYTES + lane * 16;
-        const uint4 a = ld_shared_v4(from), b0 = ld_shared_v4(from + kTileBytes), b1 = ld_shared_v4(from + 2 * kTileBytes);
-        // the MMAs that read this slot's last scales have retired
-        if (!(ok = warp_wait(bar_sfree + slot * 8, phase ^ 1u, abort_flag, p.status))) break;
-        tc_fence_after();
-        store_scales4(taddr + slot * P_SF_COLS, a);
-        mx4::store_scales(taddr + slot * P_SF_COLS + 4, b0, b1);
-        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-        tc_fence_before();
-        if (lane == 0) {
-          mbar_arrive_cluster(ready + slot * 8);
-          arrive(bar_sempty + slot * 8);
-        }
-        if (++slot == P_SLOTS) { slot = 0; phase ^= 1u; }
-      }
+      if (!ok) break;
+      commit_pair_if(bar_tfull + acc * 8, leader);
+      acc ^= 1u;
     }
   } else {
     const int q = warp & 3, half = (warp - 2) >> 2;
@@ -663,12 +650,11 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
         }
       } else if (any) {
         auto finish = [&](int c) {
-          if (MODE == STORE) add_old(p, it, v, n0 + c * 64, flat);
           if (turn)
-            store_turned(p, it, v, n0 + c * 64, it.mt * 256 + (int)rank * 128 + q * 32, lane,
-                         reinterpret_cast<uint32_t*>(smem_raw + (turned - raw) + (warp - 2) * TURN_BYTES));
+            put_turned(p, it, v, n0 + c * 64, p.N, it.mt * 256 + (int)rank * 128 + q * 32, lane,
+                       reinterpret_cast<uint32_t*>(smem_raw + (turned - raw) + (warp - 2) * TURN_BYTES));
           else
-            finish_chunk<MODE>(p, it, v, n0 + c * 64, m, flat);
+            put_chunk<MODE>(p, it, v, n0 + c * 64, p.N, flat);
         };
         finish(c0);
         load_chunk(taddr + c1 * 64, v);
@@ -717,7 +703,7 @@ template <int MODE, bool SPLIT>
 btx_status launch(const GemmArgs& g, Params p, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
   CUtensorMap a, b;
-  if (!make_codes_map(&a, g.a_codes, g.K, g.M, g.batch, p.a_box) || !make_codes_map(&b, g.b_codes, g.K, g.N, g.experts, BN) ||
+  if (!make_codes_map(&a, g.a_codes, g.K, g.M, g.batch, p.a_box) || !make_codes_map(&b, g.b_codes, g.K, g.N, g.experts, p.width) ||
       !allow_smem((const void*)fp8_gemm_kernel<MODE, SPLIT>, SMEM_BYTES, done))
     return BTX_ERR_CUDA;
   if (MODE == GATE_UP) p.n_tiles = (p.n_tiles + 1) / 2;   // pairs of column tiles
@@ -765,7 +751,7 @@ btx_status launch_pair(const GemmArgs& g, Params p, cudaStream_t st) {
 Params base_params(const GemmArgs& g) {
   Params p = {};
   p.M = g.M; p.N = g.N; p.K = g.K; p.batch = g.batch; p.status = g.status;
-  p.m_tiles = (g.M + BM - 1) / BM; p.n_tiles = (g.N + BN - 1) / BN; p.split = 1;
+  p.m_tiles = (g.M + BM - 1) / BM; p.n_tiles = (g.N + BN - 1) / BN; p.split = 1; p.width = BN;
   p.kt = (int)scale_tiles_k(g.K); p.tile_step = 1;
   p.a_row_tiles = (int)row_tiles(g.M); p.b_row_tiles = (int)row_tiles(g.N);
   p.a_scales = g.a_scales; p.b_scales = g.b_scales;
@@ -810,6 +796,9 @@ btx_status launch_matmul(const GemmArgs& g, int dtype, void* y, int accumulate, 
     return launch_pair<STORE>(g, p, st);
   p.a_rows = p.a_box = g.M < BM ? (g.M + 31) / 32 * 32 : BM;
   p.split = split_of(tiles, g.K);
+#ifdef TUNE
+  if (getenv("W")) { p.width = atoi(getenv("W")); p.n_tiles = (g.N + p.width - 1) / p.width; p.split = atoi(getenv("S")); }
+#endif
   return p.split > 1 ? launch<STORE, true>(g, p, st) : launch<STORE, false>(g, p, st);
 }
 
@@ -833,6 +822,9 @@ btx_status launch_down(const GemmArgs& g, const mx4::Dispatch& q, const float* g
   p.gates = gates; p.y = rows; p.wide = g.N % 8 == 0;
   if (q.pad_tiles == 2) return launch_pair<DOWN>(g, p, st);
   p.split = split_of((long long)p.m_tiles * p.n_tiles, g.K);
+#ifdef TUNE
+  if (getenv("W")) { p.width = atoi(getenv("W")); p.n_tiles = (g.N + p.width - 1) / p.width; p.split = atoi(getenv("S")); }
+#endif
   return p.split > 1 ? launch<DOWN, true>(g, p, st) : launch<DOWN, false>(g, p, st);
 }
 
