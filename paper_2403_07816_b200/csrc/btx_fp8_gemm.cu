@@ -26,7 +26,6 @@
 //   DOWN     gate-scaled fp32 rows scattered to t*k+slot
 // Every wait is bounded (tcx::mbar_wait); a wait that runs out leaves BTX_ERR_TIMEOUT in the status word.
 #include <cmath>
-#include <cstdlib>
 
 #include "btx_fp8_dev.cuh"
 #include "btx_fp8_gemm.cuh"
@@ -724,13 +723,6 @@ btx_status launch(const GemmArgs& g, Params p, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, fp8_gemm_kernel<MODE, SPLIT>, a, b, p) == cudaSuccess ? BTX_OK : BTX_ERR_CUDA;
 }
 
-// CTAs per tile: as many as keep every multiprocessor busy at most once, with two stages each at least
-int split_of(long long tiles, long long K) {
-  int s = 1;
-  while (s < 8 && 2 * s * tiles <= sm_count() && 4 * s <= (K + SKB - 1) / SKB) s *= 2;
-  return s;
-}
-
 template <int MODE>
 btx_status launch_pair(const GemmArgs& g, Params p, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
@@ -760,16 +752,32 @@ Params base_params(const GemmArgs& g) {
   return p;
 }
 
-// Which kernel a product takes: rounds of tiles over the multiprocessors times the time of a tile, in measured us: 0.38 a
-// stage of a 128 x 128 tile (its contraction split over a cluster where that keeps CTAs busy) and 0.47 of a 256 x 256 tile,
-// or the epilogue `epi` of the larger tile (the smaller one's takes half) where that is longer, and what a tile costs
-// beside them.
-double single_us(double tiles, long long K, double epi) {
-  const double split = split_of((long long)(tiles + 0.5), K), kb = (double)((K + SKB - 1) / SKB);
-  return ceil(tiles * split / sm_count()) * (fmax(ceil(kb / split) * 0.38, epi / 2) + 0.4);
+// How fp8_gemm_kernel goes about a product: columns of a tile, and the CTAs of a cluster that share its contraction.
+struct Plan1 { int width, split; double us; };
+
+// The cheapest of the plans by what was measured, in us: a launch 3.2; for a round of tiles 0.9, and a stage 0.27, or its bytes of B
+// at 6.1 TB/s over the CTAs at work where that is longer; sharing the contraction 1.6 and up to 1.4 more for full
+// tiles (their partial sums).  Clusters of 8 find room only up to about 64 CTAs.  E.g. one row: N = 4096, K = 4096: 8.0 us with
+// four CTAs a tile, 9.7 with two, 12.5 with one; N = 2048, K = 2048: 6.0 with four, 11.4 with eight; 200 x 700 x 900: 5.8 with
+// tiles of 64 columns, 6.5 with 128, 7.6 with four CTAs a tile.
+Plan1 plan_single(double row_tiles_, long long rows, long long N, long long K) {
+  Plan1 best = {BN, 1, 1e30};
+  const double kb = (double)((K + SKB - 1) / SKB);
+  const double a_rows = rows < BM ? (double)rows : BM;
+  for (int width = 64; width <= BN; width += 64)
+    for (int split = 1; split <= 8; split *= 2) {
+      const double ctas = row_tiles_ * (double)((N + width - 1) / width) * split;
+      if (split > 1 && (ctas > (split == 8 ? 64 : sm_count()) || kb < 2 * split)) break;
+      const double rounds = ceil(ctas / sm_count()), at_work = ctas < sm_count() ? ctas : sm_count();
+      const double stage = fmax(width == BN ? 0.27 : 0.25, width * SKB * at_work / 6.1e6);
+      const double us = 3.2 + rounds * (ceil(kb / split) * stage + 0.9) + (split > 1 ? 1.6 + 1.4 * a_rows / BM : 0.0);
+      if (us < best.us) best = {width, split, us};
+    }
+  return best;
 }
+// The same for fp8_gemm_pair_kernel: rounds of tiles, 0.45 us a stage or the epilogue `epi` where that is longer.
 double pair_us(double tiles, long long K, double epi) {
-  return ceil(tiles / (sm_count() / 2)) * (fmax((double)((K + SKB - 1) / SKB) * 0.47, epi) + 0.85);
+  return 3.5 + ceil(tiles / (sm_count() / 2)) * (fmax((double)((K + SKB - 1) / SKB) * 0.45, epi) + 0.85);
 }
 constexpr double kStoreUs = 2.0, kGateUpUs = 5.5, kDownUs = 3.5;       // epilogues of a 256 x 256 tile
 
@@ -781,24 +789,20 @@ bool pairs_fit(long long rows, long long experts, long long d, long long F) {
   if (rows == 0) return false;
   const double each = (double)rows / (double)experts;
   const double t1 = experts * fmax(1.0, each / 128 + 0.5), t2 = experts * fmax(1.0, each / 256 + 0.5);
-  const double n1 = (double)((2 * F + 127) / 128), m1 = (double)((d + 127) / 128);
   const double n2 = (double)((2 * F + 255) / 256), m2 = (double)((d + 255) / 256);
-  return pair_us(t2 * n2, d, kGateUpUs) + pair_us(t2 * m2, F, kDownUs) <
-         single_us(t1 * n1, d, kGateUpUs) + single_us(t1 * m1, F, kDownUs);
+  const double stages = (double)((d + SKB - 1) / SKB);
+  const double up = 3.2 + ceil(t1 * n2 * 2 / sm_count()) * (fmax(stages * 0.39, kGateUpUs / 2) + 0.4);      // twins of 128 x 128 tiles
+  return pair_us(t2 * n2, d, kGateUpUs) + pair_us(t2 * m2, F, kDownUs) < up + plan_single(t1, (long long)each + 1, d, F).us;
 }
 
 btx_status launch_matmul(const GemmArgs& g, int dtype, void* y, int accumulate, cudaStream_t st) {
   Params p = base_params(g);
   p.y = y; p.out_bf16 = dtype == BTX_BF16; p.accumulate = accumulate;
   p.wide = aligned32(y) && (size_t)g.N * (p.out_bf16 ? 2 : 4) % 32 == 0;
-  const long long tiles = (long long)p.m_tiles * p.n_tiles * p.batch;
-  if (pair_us((double)g.batch * ((g.M + 255) / 256) * ((g.N + 255) / 256), g.K, kStoreUs) < single_us((double)tiles, g.K, kStoreUs))
-    return launch_pair<STORE>(g, p, st);
+  const Plan1 plan = plan_single((double)p.m_tiles * p.batch, g.M, g.N, g.K);
+  if (pair_us((double)g.batch * ((g.M + 255) / 256) * ((g.N + 255) / 256), g.K, kStoreUs) < plan.us) return launch_pair<STORE>(g, p, st);
   p.a_rows = p.a_box = g.M < BM ? (g.M + 31) / 32 * 32 : BM;
-  p.split = split_of(tiles, g.K);
-#ifdef TUNE
-  if (getenv("W")) { p.width = atoi(getenv("W")); p.n_tiles = (g.N + p.width - 1) / p.width; p.split = atoi(getenv("S")); }
-#endif
+  p.split = plan.split; p.width = plan.width; p.n_tiles = (g.N + p.width - 1) / p.width;
   return p.split > 1 ? launch<STORE, true>(g, p, st) : launch<STORE, false>(g, p, st);
 }
 
@@ -821,10 +825,9 @@ btx_status launch_down(const GemmArgs& g, const mx4::Dispatch& q, const float* g
   Params p = grouped_params(g, q);
   p.gates = gates; p.y = rows; p.wide = g.N % 8 == 0;
   if (q.pad_tiles == 2) return launch_pair<DOWN>(g, p, st);
-  p.split = split_of((long long)p.m_tiles * p.n_tiles, g.K);
-#ifdef TUNE
-  if (getenv("W")) { p.width = atoi(getenv("W")); p.n_tiles = (g.N + p.width - 1) / p.width; p.split = atoi(getenv("S")); }
-#endif
+  // (m_tiles bounds the row tiles in use, and it is all that is known here)
+  const Plan1 plan = plan_single((double)p.m_tiles, q.R, g.N, g.K);
+  p.split = plan.split; p.width = plan.width; p.n_tiles = (g.N + p.width - 1) / p.width;
   return p.split > 1 ? launch<DOWN, true>(g, p, st) : launch<DOWN, false>(g, p, st);
 }
 
