@@ -114,15 +114,14 @@ def lib():
         L.btx_mx4_moe_workspace_size.argtypes = [C.POINTER(Mx4MoeDesc), C.POINTER(sz)]
         L.btx_mx4_moe_forward.argtypes = [C.POINTER(Mx4MoeDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.btx_fp8_sizes.argtypes = [i32, i32, i32, C.POINTER(sz), C.POINTER(sz)]
-        L.btx_fp8_quantize.argtypes = [i32, vp, i64, i64] + [i32] * 7 + [vp] * 5
-        L.btx_fp8_dequantize.argtypes = [i32, vp, vp, i32, i32, i32, vp, vp]
         L.btx_fp8_matmul_workspace_size.argtypes = [i32, i32, i32, i32, i32, C.POINTER(sz)]
-        L.btx_fp8_matmul.argtypes = [i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, i32, vp, sz, vp]
         L.btx_fp8_moe_workspace_size.argtypes = [C.POINTER(Fp8MoeDesc), C.POINTER(sz)]
-        L.btx_fp8_moe_forward.argtypes = [C.POINTER(Fp8MoeDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
-        L.btx_rms_norm.argtypes = [C.POINTER(NormDesc), vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, vp]
         L.btx_rms_norm_backward_workspace_size.argtypes = [C.POINTER(NormDesc), C.POINTER(sz)]
-        L.btx_rms_norm_backward.argtypes = [C.POINTER(NormDesc), vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, i32, vp, sz, vp]
+        # The calls that take a few microseconds on the device hand every argument (addresses, sizes, strides; no floats) over
+        # in a register or stack slot of 64 bits, as ctypes does fastest for pointers.
+        for name, n in (("btx_fp8_quantize", 16), ("btx_fp8_dequantize", 8), ("btx_fp8_matmul", 14), ("btx_fp8_moe_forward", 13),
+                        ("btx_rms_norm", 13), ("btx_rms_norm_backward", 15)):
+            getattr(L, name).argtypes = [vp] * n
         L.btx_device_status.argtypes = [vp, vp, C.POINTER(i32)]
         L.btx_status_string.argtypes = [i32]
         L.btx_status_string.restype = C.c_char_p
@@ -399,9 +398,10 @@ def _rows(t, name, shape, dtype, dev):
     if t.shape != shape or t.dtype is not dtype or t.get_device() != dev:
         _bad(t, name, shape, dtype, dev)
     rs, cs = t.stride()
-    if (cs != 1 and shape[1] > 1) or (rs < shape[1] and shape[0] > 1):
+    width = shape[1]
+    if (cs != 1 and width > 1) or (rs < width and shape[0] > 1):
         raise RuntimeError(f"btx: the rows of {name} must be contiguous and must not overlap")
-    return t.data_ptr(), max(rs, shape[1])
+    return t.data_ptr(), rs if rs > width else width
 
 
 def _device(t):
@@ -575,12 +575,17 @@ def btx_mx4_moe_forward(desc, x, topk_idx, gates, w13, w2, y, workspace):
             _arg(y, "y", (T, d), dt, dev), ws, ws_bytes)
 
 
-@dataclass
 class Fp8:
-    """A batch of matrices [batch, rows, K] held as FP8 codes and scale tiles (layout in btx.h)."""
-    codes: torch.Tensor
-    scales: torch.Tensor
-    K: int
+    """A batch of matrices [batch, rows, K] held as FP8 codes and scale tiles (layout in btx.h).  The tensors are checked here,
+    once, so that calls of a few microseconds need not: they keep their shapes from then on."""
+    __slots__ = ("codes", "scales", "K", "shape", "device")
+
+    def __init__(self, codes, scales, K):
+        dev = _device(codes)
+        batch, rows, _ = codes.shape
+        _arg(codes, "codes", (batch, rows, (K + 15) // 16 * 16), _U8, dev)
+        _arg(scales, "scales", (batch, (rows + 127) // 128, (K + 511) // 512, 512), _U8, dev)
+        self.codes, self.scales, self.K, self.shape, self.device = codes, scales, K, (batch, rows, K), dev
 
     @staticmethod
     def empty(batch, rows, K, device):
@@ -588,22 +593,12 @@ class Fp8:
         return Fp8(torch.empty((batch, rows, (K + 15) // 16 * 16), dtype=_U8, device=device),
                    torch.empty((batch, (rows + 127) // 128, (K + 511) // 512, 512), dtype=_U8, device=device), K)
 
-    @property
-    def shape(self):
-        b, r, _ = self.codes.shape
-        return b, r, self.K
 
-
-def _fp8(q, name, dev):
-    """Shape (batch, rows, K) and addresses of an Fp8 argument."""
-    codes, scales, K = q.codes, q.scales, q.K
-    batch, rows, pitch = codes.shape
-    if (pitch != (K + 15) // 16 * 16 or codes.dtype is not _U8 or codes.get_device() != dev or not codes.is_contiguous()
-            or scales.dtype is not _U8 or scales.get_device() != dev or not scales.is_contiguous()
-            or scales.shape != (batch, (rows + 127) // 128, (K + 511) // 512, 512)):
-        _arg(codes, name + ".codes", (batch, rows, (K + 15) // 16 * 16), _U8, dev)
-        _arg(scales, name + ".scales", (batch, (rows + 127) // 128, (K + 511) // 512, 512), _U8, dev)
-    return batch, rows, K, codes.data_ptr(), scales.data_ptr()
+def _fp8(q, name, shape, dev):
+    """Addresses of the codes and scales of an Fp8 argument of the given shape."""
+    if q.shape != shape or q.device != dev:
+        raise ValueError(f"btx: {name} must hold {shape} on device {dev}, not {q.shape} on device {q.device}")
+    return q.codes.data_ptr(), q.scales.data_ptr()
 
 
 def btx_fp8_sizes(batch, rows, K):
@@ -626,13 +621,10 @@ def btx_fp8_quantize(src, out, block_rows=1, row_first=0, row_step=1, out_t=None
         (batch, rows, K), (batch_stride, row_stride, col) = shape, stride
     out_rows, codes, scales, codes_t, scales_t = rows, None, None, None, None
     if out is not None:
-        ob, out_rows, oK, codes, scales = _fp8(out, "out", dev)
-        if ob != batch or oK != K:
-            raise ValueError(f"btx: src is {tuple(shape)}, out is {out.shape}")
+        out_rows = out.shape[1]
+        codes, scales = _fp8(out, "out", (batch, out_rows, K), dev)
     if out_t is not None:
-        *st, codes_t, scales_t = _fp8(out_t, "out_t", dev)
-        if st != [batch, K, rows]:
-            raise ValueError(f"btx: src is {tuple(shape)}, out_t is {out_t.shape}")
+        codes_t, scales_t = _fp8(out_t, "out_t", (batch, K, rows), dev)
     if col != 1 and K > 1:
         raise RuntimeError("btx: the rows of src must be contiguous")
     _launch("btx_fp8_quantize", dev, _dtype_code(src.dtype), src.data_ptr(), row_stride, batch_stride, batch, rows, K, block_rows,
@@ -642,9 +634,10 @@ def btx_fp8_quantize(src, out, block_rows=1, row_first=0, row_step=1, out_t=None
 def btx_fp8_dequantize(q, dst):
     """The values of the Fp8 `q` into dst (contiguous, [batch, rows, K] or [rows, K] for one matrix)."""
     dev = _device(dst)
-    batch, rows, K, codes, scales = _fp8(q, "q", dev)
-    shape = (rows, K) if batch == 1 and dst.dim() == 2 else (batch, rows, K)
-    _launch("btx_fp8_dequantize", dev, _dtype_code(dst.dtype), codes, scales, batch, rows, K, _arg(dst, "dst", shape, dst.dtype, dev))
+    batch, rows, K = q.shape
+    shape = (rows, K) if batch == 1 and dst.dim() == 2 else q.shape
+    _launch("btx_fp8_dequantize", dev, _dtype_code(dst.dtype), *_fp8(q, "q", q.shape, dev), batch, rows, K,
+            _arg(dst, "dst", shape, dst.dtype, dev))
 
 
 def btx_fp8_matmul_workspace_size(M, N, K, dtype, batch=1):
@@ -658,14 +651,11 @@ def btx_fp8_matmul_workspace_size(M, N, K, dtype, batch=1):
 def btx_fp8_matmul(a, b, y, workspace, accumulate=False):
     """y = a b^T (fp32 y: or added to y) of two Fp8 of the same batch and K; y is [batch, M, N], or [M, N] for one matrix."""
     dev = _device(y)
-    batch, M, K, ac, asc = _fp8(a, "a", dev)
-    bb, N, bK, bc, bsc = _fp8(b, "b", dev)
-    if bb != batch or bK != K:
-        raise ValueError(f"btx: a is {a.shape}, b is {b.shape}")
-    shape = (M, N) if batch == 1 and y.dim() == 2 else (batch, M, N)
-    ws, ws_bytes = _workspace(workspace, dev)
-    _launch("btx_fp8_matmul", dev, _dtype_code(y.dtype), batch, M, N, K, ac, asc, bc, bsc, _arg(y, "y", shape, y.dtype, dev),
-            int(accumulate), ws, ws_bytes)
+    batch, M, K = a.shape
+    N = b.shape[1]
+    _launch("btx_fp8_matmul", dev, _dtype_code(y.dtype), batch, M, N, K, *_fp8(a, "a", a.shape, dev), *_fp8(b, "b", (batch, N, K), dev),
+            _arg(y, "y", (M, N) if batch == 1 and y.dim() == 2 else (batch, M, N), y.dtype, dev), int(accumulate),
+            *_workspace(workspace, dev))
 
 
 def make_fp8_moe_desc(T, d_model, d_ff, E, k, dtype) -> Fp8MoeDesc:
@@ -686,18 +676,12 @@ def btx_fp8_moe_forward(desc, x, topk_idx, gates, w13, w2, y, workspace):
     T, d, F, E, k, dev = desc.T, desc.d_model, desc.d_ff, desc.E, desc.k, _device(y)
     dt, x_scales = _DTYPE.get(desc.dtype), None
     if isinstance(x, Fp8):
-        *sx, x, x_scales = _fp8(x, "x", dev)
-        if sx != [1, T, d]:
-            raise ValueError(f"btx: x is {tuple(sx)}; the layer has T, d_model = {T}, {d}")
+        x, x_scales = _fp8(x, "x", (1, T, d), dev)
     else:
         x = _arg(x, "x", (T, d), dt, dev)
-    *s13, c13, sc13 = _fp8(w13, "w13", dev)
-    *s2, c2, sc2 = _fp8(w2, "w2", dev)
-    if s13 != [E, 2 * F, d] or s2 != [E, d, F]:
-        raise ValueError(f"btx: w13 is {w13.shape}, w2 is {w2.shape}; the layer has E, d_ff, d_model = {E}, {F}, {d}")
-    ws, ws_bytes = _workspace(workspace, dev)
     _launch("btx_fp8_moe_forward", dev, C.byref(desc), x, x_scales, _arg(topk_idx, "topk_idx", (T, k), _I32, dev),
-            _arg(gates, "gates", (T, k), _F32, dev), c13, sc13, c2, sc2, _arg(y, "y", (T, d), dt, dev), ws, ws_bytes)
+            _arg(gates, "gates", (T, k), _F32, dev), *_fp8(w13, "w13", (E, 2 * F, d), dev), *_fp8(w2, "w2", (E, d, F), dev),
+            _arg(y, "y", (T, d), dt, dev), *_workspace(workspace, dev))
 
 
 def make_norm_desc(T, d_model, dtype, eps=1e-5) -> NormDesc:
@@ -710,15 +694,11 @@ def _opt_rows(t, name, shape, dtype, dev):
 
 def btx_rms_norm(desc, x, weight, residual=None, h=None, y=None, q=None):
     """h = x + residual and its norm, into y and the Fp8 `q` (each None to skip); rows may be strided; see btx.h."""
-    T, d, dt, dev = desc.T, desc.d_model, _DTYPE.get(desc.dtype), _device(x)
-    codes = scales = None
-    if q is not None:
-        *sq, codes, scales = _fp8(q, "q", dev)
-        if sq != [1, T, d]:
-            raise ValueError(f"btx: x is {tuple(x.shape)}, q is {q.shape}")
-    _launch("btx_rms_norm", dev, C.byref(desc), *_rows(x, "x", (T, d), dt, dev), *_opt_rows(residual, "residual", (T, d), dt, dev),
-            _opt(weight, "weight", (d,), dt, dev), *_opt_rows(h, "h", (T, d), dt, dev), *_opt_rows(y, "y", (T, d), dt, dev), codes,
-            scales)
+    d, dev = desc.d_model, _device(x)
+    dt, shape = _DTYPE.get(desc.dtype), (desc.T, d)
+    codes, scales = (None, None) if q is None else _fp8(q, "q", (1, *shape), dev)
+    _launch("btx_rms_norm", dev, C.byref(desc), *_rows(x, "x", shape, dt, dev), *_opt_rows(residual, "residual", shape, dt, dev),
+            _opt(weight, "weight", (d,), dt, dev), *_opt_rows(h, "h", shape, dt, dev), *_opt_rows(y, "y", shape, dt, dev), codes, scales)
 
 
 def btx_rms_norm_backward_workspace_size(desc):
@@ -731,11 +711,11 @@ def btx_rms_norm_backward_workspace_size(desc):
 
 def btx_rms_norm_backward(desc, h, weight, dy, dx, dweight, workspace, dh=None, accumulate=False):
     """Gradients of btx_rms_norm: dx in the tensors' type, dweight fp32 (None: not wanted); see btx.h."""
-    T, d, dt, dev = desc.T, desc.d_model, _DTYPE.get(desc.dtype), _device(h)
-    ws, ws_bytes = _workspace(workspace, dev)
-    _launch("btx_rms_norm_backward", dev, C.byref(desc), *_rows(h, "h", (T, d), dt, dev), _opt(weight, "weight", (d,), dt, dev),
-            *_rows(dy, "dy", (T, d), dt, dev), *_opt_rows(dh, "dh", (T, d), dt, dev), *_rows(dx, "dx", (T, d), dt, dev),
-            _opt(dweight, "dweight", (d,), _F32, dev), int(accumulate), ws, ws_bytes)
+    d, dev = desc.d_model, _device(h)
+    dt, shape = _DTYPE.get(desc.dtype), (desc.T, d)
+    _launch("btx_rms_norm_backward", dev, C.byref(desc), *_rows(h, "h", shape, dt, dev), _opt(weight, "weight", (d,), dt, dev),
+            *_rows(dy, "dy", shape, dt, dev), *_opt_rows(dh, "dh", shape, dt, dev), *_rows(dx, "dx", shape, dt, dev),
+            _opt(dweight, "dweight", (d,), _F32, dev), int(accumulate), *_workspace(workspace, dev))
 
 
 def btx_selftest_wait_expiry(workspace):

@@ -762,13 +762,14 @@ struct Plan1 { int width, split; double us; };
 // tiles of 64 columns, 6.5 with 128, 7.6 with four CTAs a tile.
 Plan1 plan_single(double row_tiles_, long long rows, long long N, long long K) {
   Plan1 best = {BN, 1, 1e30};
+  const int sms = sm_count();
   const double kb = (double)((K + SKB - 1) / SKB);
   const double a_rows = rows < BM ? (double)rows : BM;
   for (int width = 64; width <= BN; width += 64)
     for (int split = 1; split <= 8; split *= 2) {
       const double ctas = row_tiles_ * (double)((N + width - 1) / width) * split;
-      if (split > 1 && (ctas > (split == 8 ? 64 : sm_count()) || kb < 2 * split)) break;
-      const double rounds = ceil(ctas / sm_count()), at_work = ctas < sm_count() ? ctas : sm_count();
+      if (split > 1 && (ctas > (split == 8 ? 64 : sms) || kb < 2 * split)) break;
+      const double rounds = ceil(ctas / sms), at_work = ctas < sms ? ctas : sms;
       const double stage = fmax(width == BN ? 0.27 : 0.25, width * SKB * at_work / 6.1e6);
       const double us = 3.2 + rounds * (ceil(kb / split) * stage + 0.9) + (split > 1 ? 1.6 + 1.4 * a_rows / BM : 0.0);
       if (us < best.us) best = {width, split, us};

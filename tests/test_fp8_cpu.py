@@ -69,7 +69,7 @@ def test_norm_refusals(L):
     for bad in (dict(h=None), dict(dy=None), dict(dx=None), dict(hs=63), dict(dys=63), dict(dh=A, dhs=63), dict(dxs=63), dict(ws=None),
                 dict(ws=OFF), dict(dw=C.c_void_p(4098)), dict(w=ODD)):
         assert g(**bad) == 1, bad
-    assert g(n=1024) == 3
+    assert L.btx_rms_norm_backward_workspace_size(mk(), C.byref(sz)) == 0 and g(n=sz.value - 1) == 3
     assert f(desc=mk(T=0), x=None, y=None) == 0
     assert g(desc=mk(T=0), h=None, dy=None, dx=None, dw=None) == 0 and g(desc=mk(T=0), h=None, dy=None, dx=None, acc=1) == 0
     assert L.btx_rms_norm_backward_workspace_size(mk(), None) == 1
