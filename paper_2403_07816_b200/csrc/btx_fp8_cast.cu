@@ -319,6 +319,41 @@ dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__
         out.set(v);
         out.store(to + c0 + u * 256, 8, true);
       }
+    } else if constexpr (sizeof(T) == 2) {
+      // Two neighbours a lane, in a word of dst.  In a row that starts in the middle of a word they are the second of the lane's
+      // two codes and the first of the next lane's; the row's first element is by itself.
+      constexpr int PAIRS = kUnroll * 4, BLOCKS = kUnroll * 2;
+      const int off = (int)((uintptr_t)to >> 1 & 1), left = K - at;
+      uint32_t q[PAIRS + 1];
+      float scale[BLOCKS + 1];
+#pragma unroll
+      for (int j = 0; j < PAIRS; ++j) {
+        const int c = j * 64 + lane * 2;
+        q[j] = c < left ? (uint32_t)__ldcs(reinterpret_cast<const uint16_t*>(from + c)) : 0u;
+      }
+      q[PAIRS] = PAIRS * 64 < left ? from[PAIRS * 64] : 0u;
+#pragma unroll
+      for (int k = 0; k <= BLOCKS; ++k) scale[k] = k * kBlock < left ? scale_value(sc[(k >> 2) * kTileBytes + (k & 3)]) : 0.f;
+      if (off && g == 0 && lane == 0) to[0] = __float2bfloat16_rn(value2(q[0]).x * scale[0]);
+#pragma unroll
+      for (int j = 0; j < PAIRS; ++j) {
+        const int c = j * 64 + lane * 2 + off;
+        uint32_t two = q[j];
+        float s = scale[j / 2];
+        if (off) {
+          uint32_t next = __shfl_down_sync(kAll, q[j], 1);
+          const uint32_t first = __shfl_sync(kAll, q[j + 1], 0);
+          if (lane == 31) {
+            next = first;
+            if (j & 1) s = scale[j / 2 + 1];
+          }
+          two = two >> 8 | next << 8;
+        }
+        const float2 f = value2(two & 0xffffu);
+        const __nv_bfloat162 h = __floats2bfloat162_rn(f.x * scale[j / 2], f.y * s);
+        if (c + 1 < left) *reinterpret_cast<__nv_bfloat162*>(to + c) = h;
+        else if (c < left) to[c] = __low2bfloat16(h);
+      }
     } else {
       uint32_t q[kUnroll][8];
       uint32_t byte[kUnroll][2];

@@ -46,17 +46,28 @@ __device__ __forceinline__ float inv_rms(float sum, int d, float eps) { return 1
 
 // A thread's columns and its places in shared memory: STAGES rows of each of ARRAYS tensors, V vectors a row.  VEC: every
 // vector of every tensor is whole and on a 16-byte boundary.
+//
+// Otherwise rows go by words of 4 bytes.  A row of bf16 that starts in the middle of a word is kept and written as the words that
+// hold it: word k of a vector has elements 2k - 1 and 2k, element 7 is in the next lane's word 0, which the warp's last lane
+// fetches for itself.  Words that reach over an end of the row are put together from single elements.
 template <typename T, int V, int ARRAYS, int STAGES, bool VEC> struct Rows {
   static constexpr int VN = 16 / (int)sizeof(T);
+  static constexpr bool HALVES = !VEC && sizeof(T) == 2;
   int d, c0, dc;                           // elements of a row, first column, columns from one vector to the next
   uint32_t base, step;                     // first place, bytes from one place to the next
+  uint32_t more;                           // HALVES: the last lane's places of single words
+  uint32_t odd;                            // HALVES: bit stage * ARRAYS + array: that row starts in the middle of a word
   const T* from[ARRAYS];                   // first column of the next row to fetch
   long long ahead[ARRAYS];                 // elements to the row after it
 
   __device__ __forceinline__ void init(uint8_t* smem, int d_) {
     d = d_; c0 = threadIdx.x * VN; dc = blockDim.x * VN;
-    step = blockDim.x * blockDim.y * 16;
-    base = (uint32_t)__cvta_generic_to_shared(smem) + (threadIdx.y * blockDim.x + threadIdx.x) * 16;
+    const int threads = blockDim.x * blockDim.y, me = threadIdx.y * blockDim.x + threadIdx.x;
+    step = threads * 16;
+    const uint32_t first = (uint32_t)__cvta_generic_to_shared(smem);
+    base = first + me * 16;
+    more = first + STAGES * ARRAYS * V * step + (me >> 5) * (STAGES * ARRAYS * V * 4);
+    odd = 0;
     // places behind the last column are never written again
     for (int k = 0; k < STAGES * ARRAYS * V; ++k)
       asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(base + k * step), "r"(0) : "memory");
@@ -67,23 +78,45 @@ template <typename T, int V, int ARRAYS, int STAGES, bool VEC> struct Rows {
   }
   __device__ __forceinline__ int col(int i) const { return c0 + i * dc; }
   __device__ __forceinline__ uint32_t place(int stage, int array, int i) const { return base + ((stage * ARRAYS + array) * V + i) * step; }
+  // word with elements e and e + 1 of the row, of which the vector at `at` begins with element c
+  __device__ __forceinline__ void fetch_word(uint32_t to, const T* at, int c, int e) const {
+    if (e >= 0 && e + 1 < d) {
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(at + (e - c)) : "memory");
+    } else {
+      const uint16_t* h = reinterpret_cast<const uint16_t*>(at) + (e - c);
+      const uint32_t w = (e >= 0 && e < d ? (uint32_t)h[0] : 0u) | (e + 1 < d ? (uint32_t)h[1] << 16 : 0u);
+      asm volatile("st.shared.u32 [%0], %1;" ::"r"(to), "r"(w) : "memory");
+    }
+  }
   // the next row, if there is one, into a stage
   __device__ __forceinline__ void fetch(int stage, bool in) {
 #pragma unroll
     for (int a = 0; a < ARRAYS; ++a) {
-      if (in && VEC) {
+      if (in) {
+        int off = 0;
+        if constexpr (HALVES) {
+          const uint32_t bit = 1u << (stage * ARRAYS + a);
+          off = (int)((uintptr_t)from[a] >> 1 & 1);
+          odd = off ? odd | bit : odd & ~bit;
+        }
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-          if (col(i) < d)
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(place(stage, a, i)), "l"(from[a] + i * dc) : "memory");
-      } else if (in) {
-        Piece<T, VN> q[V];
+        for (int i = 0; i < V; ++i) {
+          const uint32_t to = place(stage, a, i);
+          const T* at = from[a] + i * dc;
+          if constexpr (VEC) {
+            if (col(i) < d) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(at) : "memory");
+          } else if constexpr (HALVES) {
+            if (col(i) <= d) {               // (the vector behind the last one may hold its last element)
 #pragma unroll
-        for (int i = 0; i < V; ++i) q[i].load(from[a] + i * dc, d - col(i), false);
+              for (int k = 0; k < 4; ++k) fetch_word(to + 4 * k, at, col(i), col(i) + 2 * k - off);
+            }
+            if (off && (threadIdx.x & 31) == 31) fetch_word(more + ((stage * ARRAYS + a) * V + i) * 4, at, col(i), col(i) + 7);
+          } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(place(stage, a, i)), "r"(q[i].w[0]), "r"(q[i].w[1]), "r"(q[i].w[2]),
-                       "r"(q[i].w[3]) : "memory");
+            for (int k = 0; k < 4; ++k)
+              if (col(i) + k < d) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to + 4 * k), "l"(at + k) : "memory");
+          }
+        }
       }
       from[a] += ahead[a];
     }
@@ -95,13 +128,42 @@ template <typename T, int V, int ARRAYS, int STAGES, bool VEC> struct Rows {
     Piece<T, VN> q;
     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(q.w[0]), "=r"(q.w[1]), "=r"(q.w[2]), "=r"(q.w[3])
                  : "r"(place(stage, array, i)) : "memory");
+    if constexpr (HALVES) {
+      if (odd >> (stage * ARRAYS + array) & 1) {         // (the same for the whole warp)
+        uint32_t next = __shfl_down_sync(kAll, q.w[0], 1);
+        if ((threadIdx.x & 31) == 31)
+          asm volatile("ld.shared.u32 %0, [%1];" : "=r"(next) : "r"(more + ((stage * ARRAYS + array) * V + i) * 4) : "memory");
+#pragma unroll
+        for (int k = 0; k < 4; ++k) q.w[k] = __funnelshift_r(q.w[k], k < 3 ? q.w[k + 1 < 4 ? k + 1 : 3] : next, 16);
+      }
+    }
     q.pairs(v);
   }
+  // (called by whole warps)
   __device__ __forceinline__ void write(T* row, int i, const Piece<T, VN>& q) const {
-    if (VEC) {
-      if (col(i) < d) q.store(row + i * dc, VN, true);
+    T* at = row + i * dc;
+    if constexpr (VEC) {
+      if (col(i) < d) q.store(at, VN, true);
+    } else if constexpr (HALVES) {
+      const int lane = threadIdx.x & 31, off = (int)((uintptr_t)at >> 1 & 1), n = d - col(i);
+      uint16_t* h = reinterpret_cast<uint16_t*>(at);
+      uint32_t w[4];
+      const uint32_t before = __shfl_up_sync(kAll, q.w[3], 1);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[k] = off ? __funnelshift_r(k > 0 ? q.w[k > 0 ? k - 1 : 0] : before, q.w[k], 16) : q.w[k];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int e = 2 * k - off;           // (element -1: the lane's before, which leaves it to this one)
+        if (e + 1 < n && (e >= 0 || lane > 0)) {
+          *reinterpret_cast<uint32_t*>(h + e) = w[k];
+        } else {
+          if (e < n && (e >= 0 || lane > 0)) h[e] = (uint16_t)w[k];
+          if (e + 1 < n) h[e + 1] = (uint16_t)(w[k] >> 16);
+        }
+      }
+      if (off && lane == 31 && 7 < n) h[7] = (uint16_t)(q.w[3] >> 16);
     } else {
-      q.store(row + i * dc, d - col(i), false);
+      q.store(at, d - col(i), false);
     }
   }
   // this thread's weights, ones where there are none
@@ -352,7 +414,7 @@ Shape shape_of(int vecs, int esize, int arrays) {
   s.rows = s.threads < 256 ? 256 / s.threads : 1;
   const int block = s.threads * s.rows, bound = s.threads <= 512 ? 512 : 1024;
   s.blocks = resident_threads(s.v, bound, arrays) / block;
-  s.smem = (bound == 1024 ? 1 : 2) * block * s.v * 16 * arrays;
+  s.smem = (bound == 1024 ? 1 : 2) * s.v * arrays * (block * 16 + block / 32 * 4);       // places, and words of last lanes
   const int shares = s.rows > 1 ? block * s.v * (16 / esize) * 4 : 0;
   if (s.smem < shares) s.smem = shares;
   return s;
