@@ -21,7 +21,8 @@ namespace {
 
 constexpr int kSmem = 220 * 1024;          // shared memory of a multiprocessor that the rings of its blocks share
 
-// Sums over the threads of a row, in every one of them; `slot` alternates between calls.
+// Sums over the threads of a row, in every one of them; `slot` alternates between calls.  Rows of a block wait for themselves
+// only (a named barrier each).
 template <int N> __device__ __forceinline__ void row_sum(float (&a)[N], float (*part)[32][N], int slot) {
 #pragma unroll
   for (int i = 0; i < N; ++i)
@@ -33,7 +34,7 @@ template <int N> __device__ __forceinline__ void row_sum(float (&a)[N], float (*
   if (lane == 0)
 #pragma unroll
     for (int i = 0; i < N; ++i) part[slot][first + warp][i] = a[i];
-  __syncthreads();
+  asm volatile("bar.sync %0, %1;" ::"r"(1 + threadIdx.y), "r"(blockDim.x) : "memory");
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     a[i] = lane < warps ? part[slot][first + lane][i] : 0.f;
@@ -407,11 +408,14 @@ norm_sum_kernel(const float* part, int parts, int d, int accumulate, float* dw) 
 // Vectors of 16 bytes a thread, threads of a row, rows of a block; blocks that a multiprocessor holds, bytes of their ring.
 // More than 512 threads (which leaves 64 registers for each and one stage) only for rows of more than 32 KB.
 struct Shape { int v, threads, rows, blocks, smem; };
-Shape shape_of(int vecs, int esize, int arrays) {
+Shape shape_of(int T, int vecs, int esize, int arrays) {
   Shape s;
   s.v = vecs <= 1024 ? 2 : 4;
   s.threads = (vecs + 32 * s.v - 1) / (32 * s.v) * 32;
-  s.rows = s.threads < 256 ? 256 / s.threads : 1;
+  // as many rows as make 512 threads (few blocks leave few shares of dw to add up), as long as every multiprocessor has some
+  const int fill = T / sm_count();
+  s.rows = s.threads < 512 ? 512 / s.threads : 1;
+  if (s.rows > fill) s.rows = fill > 0 ? fill : 1;
   const int block = s.threads * s.rows, bound = s.threads <= 512 ? 512 : 1024;
   s.blocks = resident_threads(s.v, bound, arrays) / block;
   s.smem = (bound == 1024 ? 1 : 2) * s.v * arrays * (block * 16 + block / 32 * 4);       // places, and words of last lanes
@@ -436,7 +440,7 @@ bool rows16(const void* p, long long stride, int esize) { return p == nullptr ||
 
 template <typename T> cudaError_t norm(const NormParams& p, cudaStream_t st) {
   const int e = sizeof(T);
-  const Shape s = shape_of(vectors(p.codes != nullptr ? row_pitch(p.d) : p.d, e), e, p.residual != nullptr ? 2 : 1);
+  const Shape s = shape_of(p.T, vectors(p.codes != nullptr ? row_pitch(p.d) : p.d, e), e, p.residual != nullptr ? 2 : 1);
   const bool vec = p.d * e % 16 == 0 && rows16(p.x, p.x_stride, e) && rows16(p.residual, p.residual_stride, e) && rows16(p.w, 0, e) &&
                    rows16(p.h, p.h_stride, e) && rows16(p.y, p.y_stride, e);
   const long long want = (p.T + s.rows - 1ll) / s.rows, most = (long long)s.blocks * sm_count();
@@ -456,7 +460,7 @@ int grad_parts(int T, const Shape& s) {
 
 template <typename T> cudaError_t norm_grad(const NormGradParams& p, cudaStream_t st) {
   const int e = sizeof(T);
-  const Shape s = shape_of(vectors(p.d, e), e, 3);
+  const Shape s = shape_of(p.T, vectors(p.d, e), e, 3);
   const bool vec = p.d * e % 16 == 0 && rows16(p.h, p.h_stride, e) && rows16(p.w, 0, e) && rows16(p.dy, p.dy_stride, e) &&
                    rows16(p.dh, p.dh_stride, e) && rows16(p.dx, p.dx_stride, e);
   const int parts = grad_parts(p.T, s);
@@ -477,7 +481,7 @@ template <typename T> cudaError_t norm_grad(const NormGradParams& p, cudaStream_
 // Blocks of the backward pass, each with a share of dw: as many as are resident at once.
 int norm_grad_parts(int T, int d, int dtype) {
   const int e = dtype == BTX_BF16 ? 2 : 4;
-  return grad_parts(T, shape_of(vectors(d, e), e, 3));
+  return grad_parts(T, shape_of(T, vectors(d, e), e, 3));
 }
 
 cudaError_t launch_norm(const NormParams& p, int dtype, cudaStream_t st) {
