@@ -230,6 +230,66 @@ def test_norm_route_and_layer_on_a_stream_and_in_a_graph():
         assert torch.equal(y, ref.roll(shift, 0))
 
 
+def test_weights_written_right_before_the_layer_and_the_product():
+    # kernels start before the one in front has ended, and the layer's weights are read early: not before they are written
+    T, d, F, E, k = 40, 512, 2048, 4, 2
+    x = randn(T, d, seed=1, dtype=BF16)
+    idx, gates = random_routing(T, E, k, 2)
+    sets = [tuple(randn(E, *s, seed=10 * i + j, std=0.1) for j, s in enumerate([(F, d), (F, d), (d, F)])) for i in range(2)]
+    refs = [moe(x, idx, gates, *w)[0].clone() for w in sets]
+    w13, w2q, _ = experts(*sets[0])
+    desc = B.make_fp8_moe_desc(T, d, F, E, k, BF16)
+    ws, y = torch.empty(B.btx_fp8_moe_workspace_size(desc), dtype=torch.uint8, device=DEV), torch.empty_like(x)
+    big = [randn(4096, d, seed=30 + i) for i in range(2)]
+    xq, wq, z = B.Fp8.empty(1, T, d, DEV), B.Fp8.empty(1, 4096, d, DEV), torch.empty(T, 4096, device=DEV)
+    B.btx_fp8_quantize(x, xq)
+    products = []
+    for w in big:
+        B.btx_fp8_quantize(w, wq)
+        torch.cuda.synchronize()
+        B.btx_fp8_matmul(xq, wq, z, ws)
+        products.append(z.clone())
+    outs = []
+    torch.cuda.synchronize()
+    for i in range(30):
+        w1, w3, w2 = sets[i % 2]
+        B.btx_fp8_quantize(w2, w2q, block_rows=128)
+        B.btx_fp8_quantize(w1, w13, block_rows=128, row_first=0, row_step=2)
+        B.btx_fp8_quantize(w3, w13, block_rows=128, row_first=1, row_step=2)
+        B.btx_fp8_moe_forward(desc, x, idx, gates, w13, w2q, y, ws)
+        B.btx_fp8_quantize(big[i % 2], wq)
+        B.btx_fp8_matmul(xq, wq, z, ws)
+        outs.append((y.clone(), z.clone()))
+    torch.cuda.synchronize()
+    for i, (a, b) in enumerate(outs):
+        assert torch.equal(a, refs[i % 2]) and torch.equal(b, products[i % 2]), i
+
+
+def test_two_captured_layers_with_a_workspace_each():
+    T, d, F, E, k = 24, 256, 512, 6, 2
+    w = weights_of(E, F, d, 0.1)
+    w13, w2q, _ = experts(*w)
+    desc = B.make_fp8_moe_desc(T, d, F, E, k, BF16)
+    runs = []
+    for i in range(2):
+        x = randn(T, d, seed=40 + i, dtype=BF16)
+        idx, gates = random_routing(T, E, k, 50 + i)
+        ref = moe(x, idx, gates, *w)[0]
+        ws, y = torch.empty(B.btx_fp8_moe_workspace_size(desc), dtype=torch.uint8, device=DEV), torch.empty_like(x)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            B.btx_fp8_moe_forward(desc, x, idx, gates, w13, w2q, y, ws)
+        runs.append((graph, y, ref, torch.cuda.Stream(), x, idx, gates, ws))
+    for _ in range(10):
+        for graph, y, _, stream, *_ in runs:
+            with torch.cuda.stream(stream):
+                graph.replay()
+    torch.cuda.synchronize()
+    for _, y, ref, *_ in runs:
+        assert torch.equal(y, ref)
+
+
 def test_layers_on_two_streams_at_once():
     T, d, F, E, k = 24, 512, 1024, 6, 2
     w = weights_of(E, F, d, 0.1)
