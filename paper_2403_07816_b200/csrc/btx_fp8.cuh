@@ -1,5 +1,5 @@
 // Shared declarations of the FP8 path: the format, the launchers of its kernels and of the norm in front of it
-// (btx_fp8_cast.cu, btx_norm.cu, btx_fp8_api.cu).
+// (btx_fp8_cast.cu, btx_norm.cu; called by btx_fp8_api.cu).
 //
 // Format (include/btx.h): e4m3 codes, a byte each, rows of `pitch` bytes (K rounded up to 16, zeros behind K); one scale
 // byte (2^(b-127)) per row and 128 elements, in tiles of 128 rows x 4 blocks = 512 bytes, [row tile][ceil(K/512)][512], byte

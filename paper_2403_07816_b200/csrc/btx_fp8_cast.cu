@@ -9,6 +9,11 @@
 //   dispatch_rows   quantize_rows of the expert layer's tokens, or a copy of their FP8 form, to the k rows of every token
 //
 // VEC: rows start on 16-byte boundaries and hold whole vectors; otherwise they are read element by element, by the same lanes.
+//
+// All are bound by memory and by the instructions of the casts.  Measured on one B200 (replayed; the floor is the bytes at the
+// 6561 GB/s of a copy): 16384 x 4096 bf16 as rows 29.7 us (30.7), as rows and transposed 54.4 (40.9), back to bf16 31.6 (30.7);
+// 2 x 11008 x 4096 fp32 in square blocks, both ways, 101 (82.5), back 42.3 (41.3).  quantize_tiles is at 69 % of the issue slots.
+// Rows off 16-byte boundaries: rows 60, both ways 110, back 64.
 #include <atomic>
 
 #include "btx_fp8_dev.cuh"

@@ -10,6 +10,10 @@
 // A row is shared by blockDim.x threads, V vectors of 16 bytes each; a block works on blockDim.y rows at a time.  Blocks are
 // resident and walk over the rows.  Every thread fetches its own vectors of the next rows into its own places in shared memory
 // (cp.async), so what is in flight does not depend on registers and nobody waits for another thread's copy.
+//
+// Measured on one B200 (16384 x 4096, replayed; the floor is the bytes at the 6561 GB/s of a copy).  Forward, bf16: with
+// residual, h and y 84.2 us (81.8), and codes too 94.3 (92), y alone 44.2 (40.9); fp32 with codes 175 (174).  Backward, bf16: 82 us
+// (81.8), and 5 of these are the second kernel.  Issue slots are taken to 52-54 %.  One row of 4096: 2.4 us, a launch.
 #include <atomic>
 #include <type_traits>
 
@@ -50,7 +54,9 @@ __device__ __forceinline__ float inv_rms(float sum, int d, float eps) { return 1
 //
 // Otherwise rows go by words of 4 bytes.  A row of bf16 that starts in the middle of a word is kept and written as the words that
 // hold it: word k of a vector has elements 2k - 1 and 2k, element 7 is in the next lane's word 0, which the warp's last lane
-// fetches for itself.  Words that reach over an end of the row are put together from single elements.
+// fetches for itself.  Words that reach over an end of the row are put together from single elements.  Four times the requests
+// of whole vectors: 16384 x 4098 bf16 with residual and h 239-279 us, where 16384 x 4096 takes 84 (single elements took 403;
+// aligned 16-byte pieces and shifts were slower, as the pieces at a row's ends then have to be waited for).
 template <typename T, int V, int ARRAYS, int STAGES, bool VEC> struct Rows {
   static constexpr int VN = 16 / (int)sizeof(T);
   static constexpr bool HALVES = !VEC && sizeof(T) == 2;
@@ -182,7 +188,8 @@ template <typename T, int V, int ARRAYS, int STAGES, bool VEC> struct Rows {
 };
 
 // Threads of a multiprocessor that the registers are meant for.  What is in flight should be about 64 KB: with a residual (two
-// loads a vector) or in the backward pass 512 threads have that, with one tensor to read it takes 1024.
+// loads a vector) or in the backward pass 512 threads have that, with one tensor to read it takes 1024
+// (16384 x 4096 without a residual: bf16 44.2 us, with 512 threads 52.2; fp32 82.1 and 104.6).
 constexpr int resident_threads(int v, int threads, int arrays) { return threads == 1024 || (arrays == 1 && v == 2) ? 1024 : 512; }
 
 template <typename T, int V, int THREADS, bool RESIDUAL, bool VEC>
@@ -406,7 +413,8 @@ norm_sum_kernel(const float* part, int parts, int d, int accumulate, float* dw) 
 }
 
 // Vectors of 16 bytes a thread, threads of a row, rows of a block; blocks that a multiprocessor holds, bytes of their ring.
-// More than 512 threads (which leaves 64 registers for each and one stage) only for rows of more than 32 KB.
+// More than 512 threads (which leaves 64 registers for each and one stage) only for rows of more than 32 KB.  The backward pass of
+// rows of bf16 over 16 KB has 64 floats of dw a thread and spills: 2048 x 16384 81 us, with a floor of 41.
 struct Shape { int v, threads, rows, blocks, smem; };
 Shape shape_of(int T, int vecs, int esize, int arrays) {
   Shape s;
