@@ -325,7 +325,7 @@ btx_status btx_mx4_moe_forward(const btx_mx4_moe_desc* desc, const void* x, cons
 /* FP8 (OCP e4m3: a sign, four bits of exponent, three of significand, at most 448, no infinities) with one power-of-two
  * scale for 128 elements: activations, gradients and 8-bit weights of the products below.  A matrix of `rows` rows of K elements
  * (any numbers), or a batch of them, is held as
- *   codes   [batch][rows][P] bytes, P = K rounded up to a multiple of 16; those past K are 0;
+ *   codes   [batch][rows][P] bytes, P = K rounded up to a multiple of 32; those past K are 0;
  *   scales  [batch][ceil(rows/128)][ceil(K/512)][512] bytes: byte (r % 32) * 16 + (r / 32 % 4) * 4 + j of a tile is the
  *           scale 2^(b - 127) of elements 128 (4c + j) .. of row r (255: the block is NaN).  Square blocks (below) repeat
  *           theirs in each of their rows.  Bytes past the last row and the last block are not read.

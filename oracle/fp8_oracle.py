@@ -64,8 +64,8 @@ def round_rows(x, rows=1):
 
 
 def stored_codes(codes):
-    """Codes with the zeros that fill a row to a multiple of 16 bytes."""
-    return np.pad(codes, ((0, 0), (0, -codes.shape[1] % 16)))
+    """Codes with the zeros that fill a row to a multiple of 32 bytes."""
+    return np.pad(codes, ((0, 0), (0, -codes.shape[1] % 32)))
 
 
 def stored_scales(scales, fill):

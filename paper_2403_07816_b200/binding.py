@@ -583,14 +583,14 @@ class Fp8:
     def __init__(self, codes, scales, K):
         dev = _device(codes)
         batch, rows, _ = codes.shape
-        _arg(codes, "codes", (batch, rows, (K + 15) // 16 * 16), _U8, dev)
+        _arg(codes, "codes", (batch, rows, (K + 31) // 32 * 32), _U8, dev)
         _arg(scales, "scales", (batch, (rows + 127) // 128, (K + 511) // 512, 512), _U8, dev)
         self.codes, self.scales, self.K, self.shape, self.device = codes, scales, K, (batch, rows, K), dev
 
     @staticmethod
     def empty(batch, rows, K, device):
         btx_fp8_sizes(batch, rows, K)
-        return Fp8(torch.empty((batch, rows, (K + 15) // 16 * 16), dtype=_U8, device=device),
+        return Fp8(torch.empty((batch, rows, (K + 31) // 32 * 32), dtype=_U8, device=device),
                    torch.empty((batch, (rows + 127) // 128, (K + 511) // 512, 512), dtype=_U8, device=device), K)
 
 

@@ -1,7 +1,7 @@
 // Shared declarations of the FP8 path: the format, the launchers of its kernels and of the norm in front of it
 // (btx_fp8_cast.cu, btx_norm.cu; called by btx_fp8_api.cu).
 //
-// Format (include/btx.h): e4m3 codes, a byte each, rows of `pitch` bytes (K rounded up to 16, zeros behind K); one scale
+// Format (include/btx.h): e4m3 codes, a byte each, rows of `pitch` bytes (K rounded up to 32, zeros behind K); one scale
 // byte (2^(b-127)) per row and 128 elements, in tiles of 128 rows x 4 blocks = 512 bytes, [row tile][ceil(K/512)][512], byte
 // (r % 32) * 16 + (r / 32 % 4) * 4 + j for block 4c + j of row r.  These are the tiles of the MXFP4 path with wider
 // blocks: a word of tensor memory holds the scales of four neighbouring blocks of a row, and an MMA names the byte it takes.
@@ -17,7 +17,9 @@ constexpr int kTileRows = 128;             // rows of a scale tile
 constexpr int kTileBytes = 512;
 constexpr int kTileK = 512;                // elements of a row whose scales lie in one tile
 
-inline __host__ __device__ long long row_pitch(long long K) { return (K + 15) / 16 * 16; }
+// Whole sectors of 32 bytes: a box of 128 bytes of a row at any multiple of 16 touches five of them (8192 x 4096 x 4080: 116 us with
+// rows of 4080 bytes, 102 with rows of 4096; rows of 4064 and 4032 bytes are no slower than those).
+inline __host__ __device__ long long row_pitch(long long K) { return (K + 31) / 32 * 32; }
 inline __host__ __device__ long long scale_tiles_k(long long K) { return (K + kTileK - 1) / kTileK; }
 inline __host__ __device__ long long row_tiles(long long rows) { return (rows + kTileRows - 1) / kTileRows; }
 

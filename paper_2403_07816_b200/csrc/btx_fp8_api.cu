@@ -60,8 +60,9 @@ btx_status make_moe_plan(const btx_fp8_moe_desc* d, MoePlan* pl) {
   const int pad_tiles = pairs_fit(R, used, d->d_model, d->d_ff) ? 2 : 1;
   const long long unit = pad_tiles * kTileRows;
   const long long tiles = (R + used * (unit - 1)) / unit * pad_tiles;
-  const long long wide = d->d_model > d->d_ff ? d->d_model : d->d_ff;       // codes of the rows, of W1 and W3, of W2
-  if (tiles * kTileRows * wide >= kMaxCodes || 2 * (long long)d->d_ff * d->d_model >= kMaxCodes) return BTX_ERR_UNSUPPORTED;
+  const long long d_pitch = row_pitch(d->d_model), f_pitch = row_pitch(d->d_ff);
+  const long long wide = d_pitch > f_pitch ? d_pitch : f_pitch;             // codes of the rows, of W1 and W3, of W2
+  if (tiles * kTileRows * wide >= kMaxCodes || 2 * (long long)d->d_ff * d_pitch >= kMaxCodes || d->d_model * f_pitch >= kMaxCodes) return BTX_ERR_UNSUPPORTED;
   const long long widest = d->d_model > 2 * (long long)d->d_ff ? d->d_model : 2 * (long long)d->d_ff;
   if (tiles * (row_tiles(widest) + 1) > kMaxItems) return BTX_ERR_UNSUPPORTED;
   *pl = MoePlan();
@@ -82,9 +83,9 @@ btx_status make_moe_plan(const btx_fp8_moe_desc* d, MoePlan* pl) {
   pl->w_n_tiles = take(4);
   pl->w_block_counts = take((size_t)q.blocks * d->E * 4);
   pl->w_pad_offsets = take((size_t)(d->E + 1) * 4);
-  pl->w_xs = take(rp * d->d_model);
+  pl->w_xs = take(rp * d_pitch);
   pl->w_xs_scales = take((size_t)tiles * scale_tiles_k(d->d_model) * kTileBytes);
-  pl->w_act = take(rp * d->d_ff);
+  pl->w_act = take(rp * f_pitch);
   pl->w_act_scales = take((size_t)tiles * scale_tiles_k(d->d_ff) * kTileBytes);
   pl->w_rows = take((size_t)R * d->d_model * 4);
   pl->bytes = o;

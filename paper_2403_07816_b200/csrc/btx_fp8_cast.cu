@@ -389,14 +389,14 @@ __global__ void __launch_bounds__(kThreads)
 dispatch_rows_kernel(const mx4::Dispatch q, const T* __restrict__ x, const uint8_t* __restrict__ x_scales, uint8_t* __restrict__ codes,
                      uint8_t* __restrict__ scales, I items, int groups) {
   const int lane = threadIdx.x & 31;
-  const int kt = (int)scale_tiles_k(q.d);
+  const int kt = (int)scale_tiles_k(q.d), pitch = (int)row_pitch(q.d);
   grid_dependency_wait();
   allow_dependents();                        // in this order: the products start after the dispatch, see fp8_gemm_kernel
   for (I w = ((I)blockIdx.x * kThreads + threadIdx.x) >> 5; w < items; w += (I)gridDim.x * (kThreads / 32)) {
     const size_t t = (size_t)(w / (I)groups);
     const int g = (int)(w - (I)t * (I)groups);
     const int c0 = g * kUnroll * 256 + lane * 8;
-    const T* from = x + t * q.d + c0;
+    const T* from = x + t * (sizeof(T) == 1 ? pitch : q.d) + c0;
     uint2 code[kUnroll];
     uint32_t byte[kUnroll];
     if constexpr (sizeof(T) == 1) {
@@ -425,7 +425,7 @@ dispatch_rows_kernel(const mx4::Dispatch q, const T* __restrict__ x, const uint8
     for (int j = 0; j < q.k; ++j) {
       const int row = q.flat2row[t * q.k + j];
       if (row < 0) continue;
-      uint8_t* to = codes + (size_t)row * q.d + c0;
+      uint8_t* to = codes + (size_t)row * pitch + c0;
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
         const int c = c0 + u * 256;

@@ -154,6 +154,7 @@ __device__ __forceinline__ void units(const float (&v)[N], int f0, int F, float*
 }
 // 32 units f0 .. of row m of the activations (F is a multiple of 16)
 __device__ __forceinline__ void store_units(const Params& p, const float* a, int f0, int F, int m, uint32_t byte, uint32_t inv_bits) {
+  uint8_t* to = p.act_codes + (size_t)m * row_pitch(F) + f0;
 #pragma unroll
   for (int h = 0; h < 32; h += 16) {
     if (f0 + h >= F) break;
@@ -162,7 +163,7 @@ __device__ __forceinline__ void store_units(const Params& p, const float* a, int
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = a[h + i];
     cast_codes(v, byte, inv_bits, q);
-    *reinterpret_cast<uint4*>(p.act_codes + (size_t)m * F + f0 + h) = make_uint4(q[0], q[1], q[2], q[3]);
+    *reinterpret_cast<uint4*>(to + h) = make_uint4(q[0], q[1], q[2], q[3]);
   }
 }
 

@@ -24,7 +24,7 @@ BIG = (1 << 31) - 32
 
 def test_cast_refusals(L):
     sz = C.c_size_t(0)
-    assert L.btx_fp8_sizes(2, 130, 513, C.byref(sz), None) == 0 and sz.value == 2 * 130 * 528
+    assert L.btx_fp8_sizes(2, 130, 513, C.byref(sz), None) == 0 and sz.value == 2 * 130 * 544
     assert L.btx_fp8_sizes(2, 130, 513, None, C.byref(sz)) == 0 and sz.value == 2 * 2 * 2 * 512
     for batch, rows, K, status in ((-1, 8, 64, 1), (1, -1, 64, 1), (1, 8, 0, 1), (1, BIG, 64, 2), (1, 8, BIG, 2), (1, 1 << 30, 1 << 30, 2),
                                    (1 << 30, 1 << 20, 1 << 19, 2)):

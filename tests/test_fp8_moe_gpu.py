@@ -25,7 +25,7 @@ def np64(t):
 
 def guarded_fp8(batch, rows, K, fill=0xFF):
     """Unwritten scale bytes read as NaN."""
-    bufs = {"codes": Guarded((batch, rows, (K + 15) // 16 * 16), torch.uint8, DEV, fill=fill),
+    bufs = {"codes": Guarded((batch, rows, (K + 31) // 32 * 32), torch.uint8, DEV, fill=fill),
             "scales": Guarded((batch, (rows + 127) // 128, (K + 511) // 512, 512), torch.uint8, DEV, fill=fill)}
     return B.Fp8(bufs["codes"].t, bufs["scales"].t, K), bufs
 

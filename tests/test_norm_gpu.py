@@ -62,7 +62,7 @@ def norm(x, w, residual, dtype, fp8=True):
     bufs = {"h": Guarded((T, d), dtype, DEV), "y": Guarded((T, d), dtype, DEV)}
     q = None
     if fp8:
-        bufs["codes"] = Guarded((1, T, (d + 15) // 16 * 16), torch.uint8, DEV, fill=0xEE)
+        bufs["codes"] = Guarded((1, T, (d + 31) // 32 * 32), torch.uint8, DEV, fill=0xEE)
         bufs["scales"] = Guarded((1, (T + 127) // 128, (d + 511) // 512, 512), torch.uint8, DEV, fill=0xEE)
         q = B.Fp8(bufs["codes"].t, bufs["scales"].t, d)
     B.btx_rms_norm(desc, x, w, residual=residual, h=bufs["h"].t, y=bufs["y"].t, q=q)
