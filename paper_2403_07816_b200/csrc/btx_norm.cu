@@ -47,7 +47,14 @@ template <int N> __device__ __forceinline__ void row_sum(float (&a)[N], float (*
   }
 }
 
-__device__ __forceinline__ float inv_rms(float sum, int d, float eps) { return 1.0f / sqrtf(sum / (float)d + eps); }
+// 1 / sqrt(m), m = sum / d + eps, and a step of Newton's method on it (with the product m s in two words), which leaves about half
+// an ulp of its two roundings: a row's elements share this error, and those near the middle between two FP8 values show it.
+__device__ __forceinline__ float inv_rms(float sum, int d, float eps) {
+  const float m = sum / (float)d + eps, s = 1.0f / sqrtf(m);
+  if (!(m > 0.f && m < INFINITY)) return s;
+  const float t = m * s, low = fmaf(m, s, -t);
+  return fmaf(0.5f * s, fmaf(-t, s, 1.0f) - low * s, s);
+}
 
 // A thread's columns and its places in shared memory: STAGES rows of each of ARRAYS tensors, V vectors a row.  VEC: every
 // vector of every tensor is whole and on a 16-byte boundary.
@@ -247,7 +254,8 @@ norm_kernel(const __grid_constant__ NormParams p) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
 #pragma unroll
-      for (int j = 0; j < VN / 2; ++j) v[i][j] = mul2(mul2(v[i][j], s2), w[i][j]);
+      for (int j = 0; j < VN / 2; ++j)           // h w of two bf16 is exact: one rounding
+        v[i][j] = sizeof(T) == 2 ? mul2(mul2(v[i][j], w[i][j]), s2) : mul2(mul2(v[i][j], s2), w[i][j]);
       if (p.y != nullptr && in) {
         Piece<T, VN> q;
         q.set(v[i]);

@@ -155,7 +155,7 @@ def test_layer_step_on_a_stream_and_in_a_graph():
     x, w, dy = randn(M, K, seed=1, dtype=BF16), randn(N, K, seed=2, std=0.05, dtype=BF16), randn(M, N, seed=3, std=0.1, dtype=BF16)
     e = lambda *s: B.Fp8.empty(1, *s, DEV)
     wq, wt, xq, xt, gq, gt = e(N, K), e(K, N), e(M, K), e(K, M), e(M, N), e(N, M)
-    ws = torch.empty(256, dtype=torch.uint8, device=DEV)
+    ws = torch.empty(max(B.btx_fp8_matmul_workspace_size(*s, BF16) for s in ((M, N, K), (M, K, N), (N, K, M))), dtype=torch.uint8, device=DEV)
     y, dx, dw = torch.empty(M, N, dtype=BF16, device=DEV), torch.empty(M, K, dtype=BF16, device=DEV), torch.empty(N, K, device=DEV)
 
     def step():
@@ -193,7 +193,8 @@ def test_offsets_past_32_bits():
     B.btx_fp8_quantize(x, q)
     B.btx_fp8_quantize(tail, qt)
     B.btx_fp8_quantize(randn(N, K, seed=2, dtype=BF16), w, block_rows=128)
-    ws, small = torch.empty(256, dtype=torch.uint8, device=DEV), torch.empty(200, N, dtype=BF16, device=DEV)
+    ws = torch.empty(max(B.btx_fp8_matmul_workspace_size(m, N, K, BF16) for m in (200, M)), dtype=torch.uint8, device=DEV)
+    small = torch.empty(200, N, dtype=BF16, device=DEV)
     B.btx_fp8_matmul(qt, w, small, ws)
     B.btx_fp8_matmul(q, w, x, ws)
     # sums of another split of the contraction: within the error of K products in fp32
