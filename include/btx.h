@@ -388,8 +388,8 @@ btx_status btx_fp8_moe_forward(const btx_fp8_moe_desc* desc, const void* x, cons
  * Rows are `*_stride` elements apart (at least d_model, the elements of a row contiguous) and need the alignment of their
  * elements; rows on 16-byte boundaries are moved fastest.  h may be x or residual itself (same address and stride: the
  * residual stream is updated in place), y may be x where h is not.  A row has at most 64 KB (32768 elements in BF16, 16384
- * in F32); eps >= 0, T may be 0.  No workspace.  A row whose sum of squares passes the largest fp32 number has y = 0; rows
- * do not affect one another. */
+ * in F32); eps >= 0, T may be 0.  No workspace.  A row whose sum of squares passes the largest fp32 number has y = 0; a row's
+ * results do not depend on the rows around it. */
 typedef struct {
   int32_t T, d_model;
   int32_t dtype;              /* btx_dtype */

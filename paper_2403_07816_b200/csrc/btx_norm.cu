@@ -12,8 +12,9 @@
 // (cp.async), so what is in flight does not depend on registers and nobody waits for another thread's copy.
 //
 // Measured on one B200 (16384 x 4096, replayed; the floor is the bytes at the 6561 GB/s of a copy).  Forward, bf16: with
-// residual, h and y 84.2 us (81.8), and codes too 94.3 (92), y alone 44.2 (40.9); fp32 with codes 175 (174).  Backward, bf16: 82 us
+// residual, h and y 84.2 us (81.8), and codes too 94-95 (92), y alone 48 (40.9); fp32 with codes 175 (174).  Backward, bf16: 82 us
 // (81.8), and 5 of these are the second kernel.  Issue slots are taken to 52-54 %.  One row of 4096: 2.4 us, a launch.
+#include <algorithm>
 #include <atomic>
 #include <type_traits>
 
@@ -61,14 +62,17 @@ __device__ __forceinline__ float inv_rms(float sum, int d, float eps) {
 //
 // Otherwise rows go by words of 4 bytes.  A row of bf16 that starts in the middle of a word is kept and written as the words that
 // hold it: word k of a vector has elements 2k - 1 and 2k, element 7 is in the next lane's word 0, which the warp's last lane
-// fetches for itself.  Words that reach over an end of the row are put together from single elements.  Four times the requests
-// of whole vectors: 16384 x 4098 bf16 with residual and h 239-279 us, where 16384 x 4096 takes 84 (single elements took 403;
+// fetches for itself.  Words that reach over an end of the row are put together from single elements.  Words of fp32 (TURNED) are
+// fetched and written 32 neighbours at a time and change hands in shared memory (16384 x 4097, gradients: 279 to 256 us; bf16, where
+// half words change hands too, does not gain).  Latency of the longer way of a row bounds these (32-39 % of the issue slots, 28 % of
+// the shared memory's): 16384 x 4098 bf16 with residual and h 195 us, 4099 226, where 4096 takes 84 (single elements took 403;
 // aligned 16-byte pieces and shifts were slower, as the pieces at a row's ends then have to be waited for).
 template <typename T, int V, int ARRAYS, int STAGES, bool VEC> struct Rows {
   static constexpr int VN = 16 / (int)sizeof(T);
-  static constexpr bool HALVES = !VEC && sizeof(T) == 2;
+  static constexpr bool HALVES = !VEC && sizeof(T) == 2, TURNED = !VEC && sizeof(T) == 4;
   int d, c0, dc;                           // elements of a row, first column, columns from one vector to the next
   uint32_t base, step;                     // first place, bytes from one place to the next
+  uint32_t turned;                         // words: the warp's vectors on their way out
   uint32_t more;                           // HALVES: the last lane's places of single words
   uint32_t odd;                            // HALVES: bit stage * ARRAYS + array: that row starts in the middle of a word
   const T* from[ARRAYS];                   // first column of the next row to fetch
@@ -80,7 +84,8 @@ template <typename T, int V, int ARRAYS, int STAGES, bool VEC> struct Rows {
     step = threads * 16;
     const uint32_t first = (uint32_t)__cvta_generic_to_shared(smem);
     base = first + me * 16;
-    more = first + STAGES * ARRAYS * V * step + (me >> 5) * (STAGES * ARRAYS * V * 4);
+    turned = first + STAGES * ARRAYS * V * step + (me >> 5) * 512;
+    more = first + (STAGES * ARRAYS * V + 1) * step + (me >> 5) * (STAGES * ARRAYS * V * 4);
     odd = 0;
     // places behind the last column are never written again
     for (int k = 0; k < STAGES * ARRAYS * V; ++k)
@@ -104,6 +109,7 @@ template <typename T, int V, int ARRAYS, int STAGES, bool VEC> struct Rows {
   }
   // the next row, if there is one, into a stage
   __device__ __forceinline__ void fetch(int stage, bool in) {
+    if (TURNED) __syncwarp();              // all lanes have read what was here
 #pragma unroll
     for (int a = 0; a < ARRAYS; ++a) {
       if (in) {
@@ -128,7 +134,8 @@ template <typename T, int V, int ARRAYS, int STAGES, bool VEC> struct Rows {
           } else {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              if (col(i) + k < d) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to + 4 * k), "l"(at + k) : "memory");
+              if (col(i) + word(k) < d)
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to + 4 * word(k)), "l"(at + word(k)) : "memory");
           }
         }
       }
@@ -136,8 +143,13 @@ template <typename T, int V, int ARRAYS, int STAGES, bool VEC> struct Rows {
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   }
+  // word `k`, `lane` of the warp's 32 vectors, counted from the lane's own
+  __device__ __forceinline__ static int word(int k) { return k * 32 - 3 * (int)(threadIdx.x & 31); }
   // the row of the oldest fetch has landed
-  __device__ __forceinline__ void wait() const { asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory"); }
+  __device__ __forceinline__ void wait() const {
+    asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+    if (TURNED) __syncwarp();
+  }
   __device__ __forceinline__ void read(int stage, int array, int i, f32x2 (&v)[VN / 2]) const {
     Piece<T, VN> q;
     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(q.w[0]), "=r"(q.w[1]), "=r"(q.w[2]), "=r"(q.w[3])
@@ -177,7 +189,16 @@ template <typename T, int V, int ARRAYS, int STAGES, bool VEC> struct Rows {
       }
       if (off && lane == 31 && 7 < n) h[7] = (uint16_t)(q.w[3] >> 16);
     } else {
-      q.store(at, d - col(i), false);
+      const int lane = threadIdx.x & 31, n = d - col(i);
+      __syncwarp();                        // (the vector before has been read)
+      asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(turned + lane * 16), "r"(q.w[0]), "r"(q.w[1]), "r"(q.w[2]), "r"(q.w[3]) : "memory");
+      __syncwarp();
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint32_t w;
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(turned + (k * 32 + lane) * 4) : "memory");
+        if (word(k) < n) reinterpret_cast<uint32_t*>(at)[word(k)] = w;
+      }
     }
   }
   // this thread's weights, ones where there are none
@@ -196,7 +217,7 @@ template <typename T, int V, int ARRAYS, int STAGES, bool VEC> struct Rows {
 
 // Threads of a multiprocessor that the registers are meant for.  What is in flight should be about 64 KB: with a residual (two
 // loads a vector) or in the backward pass 512 threads have that, with one tensor to read it takes 1024
-// (16384 x 4096 without a residual: bf16 44.2 us, with 512 threads 52.2; fp32 82.1 and 104.6).
+// (16384 x 4096 without a residual: bf16 44 us, with 512 threads 52; fp32 82 and 105).
 constexpr int resident_threads(int v, int threads, int arrays) { return threads == 1024 || (arrays == 1 && v == 2) ? 1024 : 512; }
 
 template <typename T, int V, int THREADS, bool RESIDUAL, bool VEC>
@@ -250,12 +271,18 @@ norm_kernel(const __grid_constant__ NormParams p) {
     row_sum(sum, part, slot);
     const float s = inv_rms(sum[0], p.d, p.eps);
     const f32x2 s2 = pack2(s, s);
+    // h w of two bf16 is exact, which leaves one rounding; not where it could leave fp32 and h s would not
+    const bool weight_first = sizeof(T) == 2 && s > 0x1p-30f && s < 0x1p30f;
     uint8_t* scales = p.scales + scale_offset(0, (int)t, kt, 0);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
+      if (weight_first) {
 #pragma unroll
-      for (int j = 0; j < VN / 2; ++j)           // h w of two bf16 is exact: one rounding
-        v[i][j] = sizeof(T) == 2 ? mul2(mul2(v[i][j], w[i][j]), s2) : mul2(mul2(v[i][j], s2), w[i][j]);
+        for (int j = 0; j < VN / 2; ++j) v[i][j] = mul2(mul2(v[i][j], w[i][j]), s2);
+      } else {
+#pragma unroll
+        for (int j = 0; j < VN / 2; ++j) v[i][j] = mul2(mul2(v[i][j], s2), w[i][j]);
+      }
       if (p.y != nullptr && in) {
         Piece<T, VN> q;
         q.set(v[i]);
@@ -424,13 +451,25 @@ norm_sum_kernel(const float* part, int parts, int d, int accumulate, float* dw) 
 // More than 512 threads (which leaves 64 registers for each and one stage) only for rows of more than 32 KB.  The backward pass of
 // rows of bf16 over 16 KB has 64 floats of dw a thread and spills: 2048 x 16384 81 us, with a floor of 41.
 struct Shape { int v, threads, rows, blocks, smem; };
-Shape shape_of(int T, int vecs, int esize, int arrays) {
+Shape shape_of(int T, int vecs, int esize, int arrays, int v0 = 0) {
   Shape s;
-  s.v = vecs <= 1024 ? 2 : 4;
-  s.threads = (vecs + 32 * s.v - 1) / (32 * s.v) * 32;
-  // as many rows as make 512 threads (few blocks leave few shares of dw to add up), as long as every multiprocessor has some
+  // as many rows as make 512 threads (few blocks leave few shares of dw to add up)
+  auto with = [&](int v) {
+    s.v = v;
+    s.threads = (vecs + 32 * v - 1) / (32 * v) * 32;
+    s.rows = s.threads < 512 ? 512 / s.threads : 1;
+    return s.threads <= 512 || v == 4 ? s.rows * vecs : 0;
+  };
+  // The fewest vectors a thread with which 700 are at work, or the most there can be: 16384 x 5120 bf16 (640 of them) with codes 120 us
+  // with two rows of 224 threads, 142 with one of 320; 16384 x 4099 262 and 413.  (By the row's length alone, so that its sums
+  // do not depend on the rows around it.)
+  if (v0 == 0) {
+    const int most = std::max(with(2), std::max(with(3), with(4)));
+    for (v0 = 2; with(v0) < (most < 700 ? most : 700); ++v0) {}
+  }
+  with(v0);
+  // as long as every multiprocessor has some
   const int fill = T / sm_count();
-  s.rows = s.threads < 512 ? 512 / s.threads : 1;
   if (s.rows > fill) s.rows = fill > 0 ? fill : 1;
   const int block = s.threads * s.rows, bound = s.threads <= 512 ? 512 : 1024;
   s.blocks = resident_threads(s.v, bound, arrays) / block;
@@ -447,6 +486,7 @@ template <typename F> cudaError_t by_shape(const Shape& s, bool more, bool vec, 
     return vec ? f(v, threads, Bool<false>(), Bool<true>()) : f(v, threads, Bool<false>(), Bool<false>());
   };
   if (s.v == 2) return with(Int<2>(), Int<512>());
+  if (s.v == 3) return with(Int<3>(), Int<512>());
   return s.threads <= 512 ? with(Int<4>(), Int<512>()) : with(Int<4>(), Int<1024>());
 }
 int vectors(long long d, int esize) { return (int)((d * esize + 15) / 16); }
@@ -456,19 +496,26 @@ bool rows16(const void* p, long long stride, int esize) { return p == nullptr ||
 
 template <typename T> cudaError_t norm(const NormParams& p, cudaStream_t st) {
   const int e = sizeof(T);
-  const Shape s = shape_of(p.T, vectors(p.codes != nullptr ? row_pitch(p.d) : p.d, e), e, p.residual != nullptr ? 2 : 1);
+  const Shape s = shape_of(p.T, vectors(row_pitch(p.d), e), e, p.residual != nullptr ? 2 : 1);
   const bool vec = p.d * e % 16 == 0 && rows16(p.x, p.x_stride, e) && rows16(p.residual, p.residual_stride, e) && rows16(p.w, 0, e) &&
                    rows16(p.h, p.h_stride, e) && rows16(p.y, p.y_stride, e);
   const long long want = (p.T + s.rows - 1ll) / s.rows, most = (long long)s.blocks * sm_count();
   const dim3 grid((unsigned)(want < most ? want : most)), block(s.threads, s.rows);
+  const int smem = s.smem + (vec ? 0 : s.threads * s.rows * 16);
   return by_shape(s, p.residual != nullptr, vec, [&](auto v, auto threads, auto residual, auto whole) {
     static std::atomic<uint64_t> done{0};
     auto kernel = norm_kernel<T, decltype(v)::value, decltype(threads)::value, decltype(residual)::value, decltype(whole)::value>;
     if (!allow_smem((const void*)kernel, kSmem, done)) return cudaErrorInvalidValue;
-    return launch_after_predecessor(kernel, grid, block, s.smem, st, true, p);
+    return launch_after_predecessor(kernel, grid, block, smem, st, true, p);
   });
 }
 
+// bf16: three vectors a thread spill here, which costs more than few threads where the rest is fast (16384 x 5120 136 us, 120 with two;
+// 16384 x 4099 369, 468 with two).
+Shape grad_shape(int T, int d, int esize) {
+  const int vecs = vectors(d, esize);
+  return shape_of(T, vecs, esize, 3, esize == 2 && d % 8 == 0 && vecs <= 1024 ? 2 : 0);
+}
 int grad_parts(int T, const Shape& s) {
   const long long want = (T + s.rows - 1ll) / s.rows, most = (long long)s.blocks * sm_count();
   return (int)(want < most ? (want > 0 ? want : 1) : most);
@@ -476,16 +523,17 @@ int grad_parts(int T, const Shape& s) {
 
 template <typename T> cudaError_t norm_grad(const NormGradParams& p, cudaStream_t st) {
   const int e = sizeof(T);
-  const Shape s = shape_of(p.T, vectors(p.d, e), e, 3);
+  const Shape s = grad_shape(p.T, p.d, e);
   const bool vec = p.d * e % 16 == 0 && rows16(p.h, p.h_stride, e) && rows16(p.w, 0, e) && rows16(p.dy, p.dy_stride, e) &&
                    rows16(p.dh, p.dh_stride, e) && rows16(p.dx, p.dx_stride, e);
   const int parts = grad_parts(p.T, s);
   const dim3 grid((unsigned)parts), block(s.threads, s.rows);
+  const int smem = s.smem + (vec ? 0 : s.threads * s.rows * 16);
   const cudaError_t r = by_shape(s, p.dh != nullptr, vec, [&](auto v, auto threads, auto add, auto whole) {
     static std::atomic<uint64_t> done{0};
     auto kernel = norm_grad_kernel<T, decltype(v)::value, decltype(threads)::value, decltype(add)::value, decltype(whole)::value>;
     if (!allow_smem((const void*)kernel, kSmem, done)) return cudaErrorInvalidValue;
-    return launch_after_predecessor(kernel, grid, block, s.smem, st, true, p);
+    return launch_after_predecessor(kernel, grid, block, smem, st, true, p);
   });
   if (r != cudaSuccess || p.dw == nullptr) return r;
   return launch_after_predecessor(norm_sum_kernel, dim3((p.d + 31) / 32), dim3(32 * kSumWarps), 0, st, true, (const float*)p.part, parts,
@@ -497,7 +545,7 @@ template <typename T> cudaError_t norm_grad(const NormGradParams& p, cudaStream_
 // Blocks of the backward pass, each with a share of dw: as many as are resident at once.
 int norm_grad_parts(int T, int d, int dtype) {
   const int e = dtype == BTX_BF16 ? 2 : 4;
-  return grad_parts(T, shape_of(T, vectors(d, e), e, 3));
+  return grad_parts(T, grad_shape(T, d, e));
 }
 
 cudaError_t launch_norm(const NormParams& p, int dtype, cudaStream_t st) {

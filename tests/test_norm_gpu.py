@@ -321,3 +321,38 @@ def test_binding_refuses_wrong_tensors():
     with pytest.raises(B.BtxError) as ei:
         B.btx_rms_norm_backward(d, x, None, x, x, None, ws[:256])
     assert ei.value.status == 3
+
+
+# rows that take three vectors a thread, on and off 16-byte boundaries, one and several rows of a block; four for the longer ones
+@both
+@pytest.mark.parametrize("shape", [(600, 4104), (601, 4107), (310, 5120), (299, 2051), (450, 9001), (20, 5606), (7, 12291)], ids=lambda s: "x".join(map(str, s)))
+def test_rows_a_little_longer_than_a_power_of_two(shape, dtype):
+    T, d = shape
+    x, w, r = randn(T, d, seed=d, dtype=dtype), (1 + randn(d, seed=2, std=0.3)).to(dtype), randn(T, d, seed=3, dtype=dtype)
+    h, y, q = norm(x, w, r, dtype)
+    check_forward(x, w, r, h, y, q)
+    check_backward(T, d, dtype, True, True)
+    for a, b in ((0, 1), (3, 7)):                                          # whatever rows there are beside them, the same bits
+        h1, y1, _ = norm(x[a:b].contiguous(), w, r[a:b].contiguous(), dtype)
+        assert torch.equal(h1, h[a:b]) and torch.equal(y1, y[a:b])
+    alone, y2 = norm(h, w, None, dtype)[1], torch.empty_like(h)
+    assert torch.equal(alone, y)
+    B.btx_rms_norm(B.make_norm_desc(T, d, dtype, EPS), h, w, y=y2)
+    assert torch.equal(y2, y)
+
+
+@both
+def test_rows_far_from_one_under_large_and_small_weights(dtype):
+    # every row's rms is 2^e; h w alone leaves fp32 for some of them, h s w for none
+    T, d = 9, 264
+    x = randn(T, d, seed=1, dtype=dtype)
+    x = (x.float() * torch.exp2(torch.tensor([-55.0, -50, -40, -20, 0, 20, 40, 50, 55], device=DEV))[:, None]).to(dtype)
+    x[4] = 1.5 * 2.0 ** 126                                                # the sum of squares is infinite
+    for e in (-80.0, 0.0, 80.0):
+        w = (randn(d, seed=2).abs() + 0.5).mul(2.0 ** e).to(dtype)
+        y = torch.empty_like(x)
+        B.btx_rms_norm(B.make_norm_desc(T, d, dtype, 0.0), x, w, y=y)
+        h64 = np64(x)
+        want = h64 / np.sqrt((h64 * h64).mean(1, keepdims=True)) * np64(w)
+        want[4] = 0.0
+        assert (np.abs(np64(y) - want) <= (half(dtype) + 2.0 ** -19) * np.abs(want) + 2.0 ** -140).all()
