@@ -365,8 +365,8 @@ btx_status btx_fp8_matmul(int32_t dtype, int32_t batch, int32_t M, int32_t N, in
 
 /* The expert layer of btx_moe_forward (Section 3.2) on FP8 experts under a routing from elsewhere, e.g. btx_route's:
  *   y_t = sum over slots j of gates[t,j] * W2_e a,  a = fp8(silu(W1_e fp8(x_t)) * W3_e fp8(x_t)),  e = topk_idx[t,j].
- * Activations are cast by rows in front of both products, products are formed in fp32, silu in fp32 from the fast
- * exponential (for x in fp32 too: within (4 + 1.2 |h|) 2^-23 of silu(h)), slots are added in fp32 in slot order, y is rounded once.
+ * Activations are cast by rows in front of both products, products are formed in fp32, silu(h1) h3 in fp32 within 9 * 2^-24 (h1
+ * below -87: within 2^-119 |h3|), slots are added in fp32 in slot order, y is rounded once.
  *   x[T,d] in dtype, or with x_scales the codes and scales of its FP8 form by rows (btx_rms_norm's, say; NULL: x is in
  *   dtype); y[T,d] in dtype; topk_idx[T,k] int32 (an index outside 0..E-1 is an empty slot: it adds nothing); gates[T,k]
  *   fp32; w13: E matrices of 2F rows of d, row 2i is row i of W1_e and row 2i + 1 row i of W3_e; w2: E matrices of d rows of F.

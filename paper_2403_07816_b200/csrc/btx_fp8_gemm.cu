@@ -142,13 +142,24 @@ __device__ __forceinline__ float4 ld_cluster_v4(uint32_t addr) {
   return v;
 }
 
+// silu(h1) h3 in fp32, within 9 * 2^-24: expf counts for two units of the last place, the reciprocal for one, and there are three
+// roundings (below h1 = -87, where 1 / (1 + e) is subnormal or 0, within 2^-119 |h3|).  The activations are cast to FP8, where
+// whatever passes a border moves by a whole step: not the place for the fast exponential, whose error grows with |h1|.  The
+// correctly rounded reciprocal has a branch that keeps the units of a thread one behind the other: T = 4096, 8 experts, d = 512,
+// F = 2048, top-2 121 us with it, 84 without; 64 experts, d = 2048, F = 1024, top-8 365 and 320.
+__device__ __forceinline__ float swiglu(float h1, float h3) {
+  float r;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(1.0f + expf(-h1)));       // (infinity: 0)
+  return h1 * r * h3;
+}
+
 // N/2 hidden units from N accumulator columns n0 .. (h1 and h3 in turn), 0 past the last unit, where the columns are those of
 // scales that nobody wrote; their largest magnitude joins `amax`.
 template <int N>
 __device__ __forceinline__ void units(const float (&v)[N], int f0, int F, float* a, uint32_t& amax) {
 #pragma unroll
   for (int i = 0; i < N / 2; ++i) {
-    a[i] = f0 + i < F ? fast_swiglu(v[2 * i], v[2 * i + 1]) : 0.f;
+    a[i] = f0 + i < F ? swiglu(v[2 * i], v[2 * i + 1]) : 0.f;
     amax = max(amax, __float_as_uint(a[i]) & 0x7fffffffu);
   }
 }
