@@ -270,18 +270,20 @@ norm_kernel(const __grid_constant__ NormParams p) {
     sum[0] += other;
     row_sum(sum, part, slot);
     const float s = inv_rms(sum[0], p.d, p.eps);
-    const f32x2 s2 = pack2(s, s);
-    // h w of two bf16 is exact, which leaves one rounding; not where it could leave fp32 and h s would not
-    const bool weight_first = sizeof(T) == 2 && s > 0x1p-30f && s < 0x1p30f;
+    // s in two factors, a power of two and a number from 1 to 2 (all of an s that is infinite or not a number in the first).  bf16:
+    // h 2^k is exact (in [2^-141, sqrt(d)]; smaller ones lose bits), and so is its product with w unless it leaves fp32, which y
+    // then does too: one rounding, whatever the sizes of h and w.
+    const uint32_t bits = __float_as_uint(s);
+    const float power = sizeof(T) == 4 || (bits & 0x7f800000u) == 0x7f800000u ? s : __uint_as_float(bits & 0x7f800000u);
+    const float rest = __uint_as_float((bits & 0x007fffffu) | 0x3f800000u);
+    const f32x2 first = pack2(power, power), second = pack2(rest, rest);
     uint8_t* scales = p.scales + scale_offset(0, (int)t, kt, 0);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      if (weight_first) {
 #pragma unroll
-        for (int j = 0; j < VN / 2; ++j) v[i][j] = mul2(mul2(v[i][j], w[i][j]), s2);
-      } else {
-#pragma unroll
-        for (int j = 0; j < VN / 2; ++j) v[i][j] = mul2(mul2(v[i][j], s2), w[i][j]);
+      for (int j = 0; j < VN / 2; ++j) {
+        v[i][j] = mul2(mul2(v[i][j], first), w[i][j]);
+        if (sizeof(T) == 2) v[i][j] = mul2(v[i][j], second);
       }
       if (p.y != nullptr && in) {
         Piece<T, VN> q;
