@@ -388,8 +388,9 @@ btx_status btx_fp8_moe_forward(const btx_fp8_moe_desc* desc, const void* x, cons
  * Rows are `*_stride` elements apart (at least d_model, the elements of a row contiguous) and need the alignment of their
  * elements; rows on 16-byte boundaries are moved fastest.  h may be x or residual itself (same address and stride: the
  * residual stream is updated in place), y may be x where h is not.  A row has at most 64 KB (32768 elements in BF16, 16384
- * in F32); eps >= 0, T may be 0.  No workspace.  A row whose sum of squares passes the largest fp32 number has y = 0; a row's
- * results do not depend on the rows around it. */
+ * in F32); eps >= 0, T may be 0.  No workspace.  A row's results do not depend on the rows around it.  The sum of squares is an
+ * fp32 number: a row where it passes the largest has y = 0, and with eps below 2^-100 a row of elements below 2^-60 is as
+ * inexact as their squares are.  The weights may be of any size. */
 typedef struct {
   int32_t T, d_model;
   int32_t dtype;              /* btx_dtype */
@@ -404,7 +405,9 @@ btx_status btx_rms_norm(const btx_norm_desc* desc, const void* x, int64_t x_stri
  *   dx[T,d] = dh + s (g - h s^2 mean(g h)), in dtype: the gradient of x and of residual alike;
  *   dweight[d] = sum over rows of dy * h * s, fp32 (NULL: not wanted); accumulate = 1 adds to it.
  * h is the h of the forward call (x where there was no residual).  Sums are fp32, in an order that repeats from run to
- * run.  dx may be dy, dh or h itself (same address and stride).  T = 0 leaves dweight 0 (accumulate: as it was). */
+ * run; g is an fp32 number, what is formed from it leaves fp32 only where dx does.  A row whose sum of squares passes the largest
+ * fp32 number has dx = dh and no part in dweight.  dx may be dy, dh or h itself (same address and stride).  T = 0 leaves
+ * dweight 0 (accumulate: as it was). */
 btx_status btx_rms_norm_backward_workspace_size(const btx_norm_desc* desc, size_t* workspace_bytes);
 btx_status btx_rms_norm_backward(const btx_norm_desc* desc, const void* h, int64_t h_stride, const void* weight,
                                  const void* dy, int64_t dy_stride, const void* dh, int64_t dh_stride, void* dx,

@@ -3,7 +3,7 @@
 //
 //   forward   h = round(x + residual), s = 1 / sqrt(sum h^2 / d + eps), y = h s w; y is rounded to the output's type, and cast to
 //             FP8 from its fp32 value
-//   backward  g = dy w, m = s sum(g h) / d: dx = dh + s (g - h s m), dw = sum over rows of dy h s.  s is formed again
+//   backward  g = dy w, m = sum(g h s) / d: dx = dh + s (g - h s m), dw = sum over rows of dy h s.  s is formed again
 //             from h in the pass that reads h anyway.  A block keeps its share of dw in registers over all of its rows; a
 //             second kernel adds the blocks' shares in order, so the result repeats
 //
@@ -318,13 +318,14 @@ norm_kernel(const __grid_constant__ NormParams p) {
   }
 }
 
-// sum h^2 and, with u = dy w, sum u h; then dw += dy (h s) and dx = dh + s u - (s^2 m) h.
+// sum h^2 and, with u = dy w, sum u h; then dw += dy (h s) and dx = dh + s (u - m (h s)), m = s sum(u h) / d.  With m h s in this order no product
+// leaves fp32 where dx does not.
 template <typename T, int V, int THREADS, bool ADD, bool VEC>
 __global__ void __launch_bounds__(THREADS, resident_threads(V, THREADS, 3) / THREADS)
 norm_grad_kernel(const __grid_constant__ NormGradParams p) {
   constexpr int VN = 16 / (int)sizeof(T), STAGES = THREADS == 1024 ? 1 : 2;
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ float part[2][32][2];
+  __shared__ float part[2][32][2], again[1][32][1];    // (between two uses of `again` lies a barrier of `part`'s)
   const int step = gridDim.x * blockDim.y;
   long long t = (long long)blockIdx.x * blockDim.y + threadIdx.y;
   Rows<T, V, ADD ? 3 : 2, STAGES, VEC> rows;
@@ -367,8 +368,24 @@ norm_grad_kernel(const __grid_constant__ NormGradParams p) {
       sum[i] += other;
     }
     row_sum(sum, part, slot);
-    const float s = inv_rms(sum[0], p.d, p.eps), m = sum[1] / (float)p.d * s;
-    const f32x2 s2 = pack2(s, s), m2 = pack2(-(s * m) * s, -(s * m) * s);
+    const float s = inv_rms(sum[0], p.d, p.eps);
+    const f32x2 s2 = pack2(s, s);
+    float m = sum[1] / (float)p.d * s;
+    // Products u h that may have left fp32 (their sum is infinite, not a number, or so small that they may have been below its normal
+    // numbers, which 2^15 of them at 2^-60 were not): once more with h s.
+    if (!(fabsf(sum[1]) >= 0x1p-60f && fabsf(sum[1]) < INFINITY)) {
+      f32x2 pairs = 0;
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+#pragma unroll
+        for (int j = 0; j < VN / 2; ++j) pairs = fma2(mul2(dy[i][j], w[i][j]), mul2(h[i][j], s2), pairs);
+      float a[1];
+      unpack2(pairs, a[0], other);
+      a[0] += other;
+      row_sum(a, again, 0);
+      m = a[0] / (float)p.d;
+    }
+    const f32x2 m2 = pack2(-m, -m);
     if (t < p.T) {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
@@ -381,8 +398,9 @@ norm_grad_kernel(const __grid_constant__ NormGradParams p) {
         }
 #pragma unroll
         for (int j = 0; j < VN / 2; ++j) {
-          dw[i][j] = fma2(dy[i][j], mul2(h[i][j], s2), dw[i][j]);
-          g[j] = fma2(h[i][j], m2, fma2(mul2(dy[i][j], w[i][j]), s2, g[j]));
+          const f32x2 unit = mul2(h[i][j], s2);
+          dw[i][j] = fma2(dy[i][j], unit, dw[i][j]);
+          g[j] = fma2(fma2(unit, m2, mul2(dy[i][j], w[i][j])), s2, g[j]);
         }
         Piece<T, VN> q;
         q.set(g);
