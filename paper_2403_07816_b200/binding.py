@@ -576,16 +576,25 @@ def btx_mx4_moe_forward(desc, x, topk_idx, gates, w13, w2, y, workspace):
 
 
 class Fp8:
-    """A batch of matrices [batch, rows, K] held as FP8 codes and scale tiles (layout in btx.h).  The tensors are checked here,
-    once, so that calls of a few microseconds need not: they keep their shapes from then on."""
-    __slots__ = ("codes", "scales", "K", "shape", "device")
+    """A batch of matrices [batch, rows, K] held as FP8 codes and scale tiles (layout in btx.h).  The tensors are checked here, once,
+    and the attributes are read-only, so that calls of a few microseconds need only see that nobody has resized them."""
+    __slots__ = ("codes", "scales", "K", "shape", "device", "sizes")
 
     def __init__(self, codes, scales, K):
         dev = _device(codes)
         batch, rows, _ = codes.shape
         _arg(codes, "codes", (batch, rows, (K + 31) // 32 * 32), _U8, dev)
         _arg(scales, "scales", (batch, (rows + 127) // 128, (K + 511) // 512, 512), _U8, dev)
-        self.codes, self.scales, self.K, self.shape, self.device = codes, scales, K, (batch, rows, K), dev
+        for name, value in zip(self.__slots__, (codes, scales, K, (batch, rows, K), dev, (codes.numel(), scales.numel()))):
+            object.__setattr__(self, name, value)
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"btx: the {name} of an Fp8 cannot be changed: make another one of its tensors")
+
+    __delattr__ = lambda self, name: self.__setattr__(name, None)
+
+    def __reduce__(self):
+        return Fp8, (self.codes, self.scales, self.K)
 
     @staticmethod
     def empty(batch, rows, K, device):
@@ -598,7 +607,10 @@ def _fp8(q, name, shape, dev):
     """Addresses of the codes and scales of an Fp8 argument of the given shape."""
     if q.shape != shape or q.device != dev:
         raise ValueError(f"btx: {name} must hold {shape} on device {dev}, not {q.shape} on device {q.device}")
-    return q.codes.data_ptr(), q.scales.data_ptr()
+    codes, scales = q.codes, q.scales
+    if (codes.numel(), scales.numel()) != q.sizes:
+        raise ValueError(f"btx: the tensors of {name} have been resized since it was made")
+    return codes.data_ptr(), scales.data_ptr()
 
 
 def btx_fp8_sizes(batch, rows, K):

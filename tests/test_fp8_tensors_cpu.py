@@ -1,0 +1,51 @@
+"""An Fp8 is checked when it is made: what was checked cannot be changed under the calls that rely on it."""
+import copy
+
+import pytest
+import torch
+
+from paper_2403_07816_b200 import binding as B
+from paper_2403_07816_b200 import build as builder
+
+
+@pytest.fixture
+def fp8(monkeypatch):
+    builder.build()
+    monkeypatch.setattr(B, "_device", lambda t: t.get_device())          # (-1: the host's tensors pass the checks, no call is made)
+    return lambda: B.Fp8.empty(2, 130, 200, "cpu")
+
+
+@pytest.mark.parametrize("name", ["codes", "scales", "K", "shape", "device", "sizes"])
+def test_attributes_are_read_only(fp8, name):
+    q = fp8()
+    was = getattr(q, name)
+    with pytest.raises(AttributeError):
+        setattr(q, name, was)
+    with pytest.raises(AttributeError):
+        delattr(q, name)
+    with pytest.raises(AttributeError):
+        q.another = 1
+    assert getattr(q, name) is was
+
+
+@pytest.mark.parametrize("name", ["codes", "scales"])
+def test_tensors_resized_since_are_refused(fp8, name):
+    q = fp8()
+    shape = (2, 130, 200)
+    assert B._fp8(q, "q", shape, -1) == (q.codes.data_ptr(), q.scales.data_ptr())
+    getattr(q, name).resize_(1, 1, 32)
+    with pytest.raises(ValueError, match="resized"):
+        B._fp8(q, "q", shape, -1)
+    q = fp8()
+    getattr(q, name).data = torch.empty(64, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="resized"):
+        B._fp8(q, "q", shape, -1)
+
+
+def test_copies_are_checked_again(fp8):
+    q = fp8()
+    same, own = copy.copy(q), copy.deepcopy(q)
+    assert same.codes is q.codes and own.codes is not q.codes and torch.equal(own.codes, q.codes) and own.shape == q.shape
+    q.scales.resize_(512)
+    with pytest.raises(ValueError):
+        copy.copy(q)
