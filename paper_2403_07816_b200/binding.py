@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
+from operator import index
 
 import torch
 
@@ -581,7 +582,7 @@ class Fp8:
     __slots__ = ("codes", "scales", "K", "shape", "device", "sizes")
 
     def __init__(self, codes, scales, K):
-        dev = _device(codes)
+        dev, K = _device(codes), index(K)
         batch, rows, _ = codes.shape
         _arg(codes, "codes", (batch, rows, (K + 31) // 32 * 32), _U8, dev)
         _arg(scales, "scales", (batch, (rows + 127) // 128, (K + 511) // 512, 512), _U8, dev)
@@ -639,6 +640,7 @@ def btx_fp8_quantize(src, out, block_rows=1, row_first=0, row_step=1, out_t=None
         codes_t, scales_t = _fp8(out_t, "out_t", (batch, K, rows), dev)
     if col != 1 and K > 1:
         raise RuntimeError("btx: the rows of src must be contiguous")
+    block_rows, row_first, row_step = index(block_rows), index(row_first), index(row_step)
     _launch("btx_fp8_quantize", dev, _dtype_code(src.dtype), src.data_ptr(), row_stride, batch_stride, batch, rows, K, block_rows,
             out_rows, row_first, row_step, codes, scales, codes_t, scales_t)
 

@@ -1,6 +1,8 @@
-"""An Fp8 is checked when it is made: what was checked cannot be changed under the calls that rely on it."""
+"""An Fp8 is checked when it is made: what was checked cannot be changed under the calls that rely on it.  And the numbers that go
+over to the library: of any integer type."""
 import copy
 
+import numpy as np
 import pytest
 import torch
 
@@ -49,3 +51,19 @@ def test_copies_are_checked_again(fp8):
     q.scales.resize_(512)
     with pytest.raises(ValueError):
         copy.copy(q)
+
+
+def test_integers_of_other_types_go_over(fp8, monkeypatch):
+    got = []
+    monkeypatch.setattr(B, "_launch", lambda name, dev, *args: got.append((name, args)))
+    one, dim = np.int64(1), torch.tensor(200)
+    q = B.Fp8(fp8().codes, fp8().scales, dim)
+    assert type(q.K) is int and q.shape == (2, 130, 200)
+    B.btx_fp8_quantize(torch.zeros(2, 65, 200), q, block_rows=np.int32(128), row_first=one, row_step=np.int64(2))
+    B.btx_fp8_dequantize(q, torch.zeros(2, 130, 200))
+    for name, args in got:
+        for value, kind in zip(args, getattr(B.lib(), name).argtypes):
+            kind.from_param(value)
+    assert got[0][1][7:11] == (128, 130, 1, 2)
+    with pytest.raises(TypeError):
+        B.btx_fp8_quantize(torch.zeros(2, 65, 200), q, row_step=2.0)
