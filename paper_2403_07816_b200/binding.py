@@ -586,6 +586,8 @@ class Fp8:
         batch, rows, _ = codes.shape
         _arg(codes, "codes", (batch, rows, (K + 31) // 32 * 32), _U8, dev)
         _arg(scales, "scales", (batch, (rows + 127) // 128, (K + 511) // 512, 512), _U8, dev)
+        if (batch | rows | K) >> 31:
+            raise ValueError("btx: the sizes of an Fp8 must fit 32 bits")
         for name, value in zip(self.__slots__, (codes, scales, K, (batch, rows, K), dev, (codes.numel(), scales.numel()))):
             object.__setattr__(self, name, value)
 
@@ -641,6 +643,8 @@ def btx_fp8_quantize(src, out, block_rows=1, row_first=0, row_step=1, out_t=None
     if col != 1 and K > 1:
         raise RuntimeError("btx: the rows of src must be contiguous")
     block_rows, row_first, row_step = index(block_rows), index(row_first), index(row_step)
+    if (batch | rows | K | block_rows | row_first | row_step) >> 31 not in (0, -1):      # (negative ones the library refuses)
+        raise ValueError("btx: the sizes of a cast must fit 32 bits")
     _launch("btx_fp8_quantize", dev, _dtype_code(src.dtype), src.data_ptr(), row_stride, batch_stride, batch, rows, K, block_rows,
             out_rows, row_first, row_step, codes, scales, codes_t, scales_t)
 

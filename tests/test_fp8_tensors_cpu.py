@@ -1,5 +1,5 @@
 """An Fp8 is checked when it is made: what was checked cannot be changed under the calls that rely on it.  And the numbers that go
-over to the library: of any integer type."""
+over to the library: of any integer type, none cut to 32 bits."""
 import copy
 
 import numpy as np
@@ -67,3 +67,16 @@ def test_integers_of_other_types_go_over(fp8, monkeypatch):
     assert got[0][1][7:11] == (128, 130, 1, 2)
     with pytest.raises(TypeError):
         B.btx_fp8_quantize(torch.zeros(2, 65, 200), q, row_step=2.0)
+
+
+def test_sizes_past_32_bits_are_refused(fp8, monkeypatch):
+    monkeypatch.setattr(B, "_launch", lambda *args: pytest.fail("the library would see other sizes"))
+    q, x = fp8(), torch.zeros(2, 130, 200)
+    for bad in (dict(row_first=1 << 32), dict(row_step=(1 << 32) + 1), dict(block_rows=(1 << 32) + 1), dict(row_first=-(1 << 32))):
+        with pytest.raises(ValueError, match="32 bits"):
+            B.btx_fp8_quantize(x, q, **bad)
+    with pytest.raises(ValueError, match="32 bits"):
+        B.btx_fp8_quantize(x[:, :1].expand(2, (1 << 32) + 130, 200), q)
+    rows = (1 << 32) + 5
+    with pytest.raises(ValueError, match="32 bits"):
+        B.Fp8(torch.empty(1, rows, 32, dtype=torch.uint8, device="meta"), torch.empty(1, (rows + 127) // 128, 1, 512, dtype=torch.uint8, device="meta"), 7)
