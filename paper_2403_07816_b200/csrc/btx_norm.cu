@@ -367,13 +367,22 @@ norm_grad_kernel(const __grid_constant__ NormGradParams p) {
       unpack2(sums[i], sum[i], other);
       sum[i] += other;
     }
+    // Products u h may leave fp32 where dx does not.  Too large, they make the sum infinite or not a number; too small (a thread's sum
+    // is below 2^-100, its products' smallest unit 2^-149), the thread makes it so itself unless its dy are 0, as they are in padded rows
+    // (16384 x 4096 bf16: 83 us, 90 where all dy are 0; 113 with a second sum for those).
+    if (!(fabsf(sum[1]) >= 0x1p-100f)) {
+      f32x2 any = 0;
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+#pragma unroll
+        for (int j = 0; j < VN / 2; ++j) any |= dy[i][j];
+      if ((any & 0x7fffffff7fffffffull) != 0) sum[1] = __uint_as_float(0x7fffffffu);
+    }
     row_sum(sum, part, slot);
     const float s = inv_rms(sum[0], p.d, p.eps);
     const f32x2 s2 = pack2(s, s);
     float m = sum[1] / (float)p.d * s;
-    // Products u h that may have left fp32 (their sum is infinite, not a number, or so small that they may have been below its normal
-    // numbers, which 2^15 of them at 2^-60 were not): once more with h s.
-    if (!(fabsf(sum[1]) >= 0x1p-60f && fabsf(sum[1]) < INFINITY)) {
+    if (!(fabsf(sum[1]) < INFINITY)) {       // once more, with h s
       f32x2 pairs = 0;
 #pragma unroll
       for (int i = 0; i < V; ++i)
