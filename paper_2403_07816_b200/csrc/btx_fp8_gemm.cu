@@ -1,6 +1,5 @@
 // Products of FP8 matrices on the 5th-generation tensor cores (tcgen05.mma kind::mxf8f6f4.block_scale): codes straight from
-// memory to shared memory by TMA, scales through shared memory and tcgen05.st into tensor memory, fp32 sums in tensor
-// memory.  y = A B^T with both operands K-major, per output element
+// memory to shared memory by TMA, scales through shared memory into tensor memory (tcgen05.cp), fp32 sums in tensor memory.  y = A B^T with both operands K-major, per output element
 //   sum over blocks of 128:  2^(sa - 127) 2^(sb - 127) sum a_i b_i.
 // An MMA covers 32 contraction elements and takes one scale per row for them; the four MMAs of a block name the same byte of
 // the row's word in tensor memory, the four blocks of a scale tile the four bytes in turn.  So one 512-byte tile of 128 rows
@@ -798,14 +797,15 @@ Plan1 plan_single(double row_tiles_, long long rows, long long N, long long K) {
 double pair_us(double tiles, long long K, double epi) {
   return 3.5 + ceil(tiles / (sm_count() / 2)) * (fmax((double)((K + SKB - 1) / SKB) * 0.45, epi) + 0.85);
 }
-constexpr double kStoreUs = 2.0, kGateUpUs = 5.5, kDownUs = 3.5;       // epilogues of a 256 x 256 tile
+// Epilogues of a 256 x 256 tile.  (kGateUpUs: T = 4096, d = 128, F = 11008, one expert, 19 rounds of tiles with one stage each, 114 us.)
+constexpr double kStoreUs = 2.0, kGateUpUs = 4.5, kDownUs = 3.5;
 
 }  // namespace
 
 // The expert layer's two products, for experts with about rows / experts rows each (a tile more than they fill for
-// every second).  Whole layers in us with tiles of 128 rows, and with pairs: 4 experts, d = 4096, F = 11008, top-2: 128 tokens 134, 135;
-// 256 174, 151; 512 278, 204; 1024 430, 293; 64 experts, d = 2048, F = 1024, top-8: 128 tokens 99, 156-177; 512 109, 121; 1024 147, 147;
-// 2048 235, 205.
+// every second).  Whole layers in us with tiles of 128 rows, and with pairs: 4 experts, d = 4096, F = 11008, top-2: 128 tokens 133, 133;
+// 256 192, 136; 512 300, 196; 64 experts, d = 2048, F = 1024, top-8: 128 tokens 116, 118; 512 109, 123; 1024 162, 147; 2048 243, 209;
+// 8 experts, d = 1024, F = 4096, top-2: 512 tokens 56, 59; 1024 91, 67.
 bool pairs_fit(long long rows, long long experts, long long d, long long F) {
   if (rows == 0) return false;
   const double each = (double)rows / (double)experts;

@@ -48,6 +48,15 @@ template <int N> __device__ __forceinline__ void row_sum(float (&a)[N], float (*
   }
 }
 
+// whether `yes` is true for any thread of a row
+__device__ __forceinline__ bool row_any(bool yes) {
+  if (blockDim.x == 32) return __any_sync(kAll, yes);
+  int any = yes;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.s32 p, %0, 0;\n\tbarrier.cta.red.or.pred q, %1, %2, p;\n\tselp.s32 %0, 1, 0, q;\n\t}"
+               : "+r"(any) : "r"(1 + threadIdx.y), "r"(blockDim.x) : "memory");
+  return any;
+}
+
 // 1 / sqrt(m), m = sum / d + eps, and a step of Newton's method on it (with the product m s in two words), which leaves about half
 // an ulp of its two roundings: a row's elements share this error, and those near the middle between two FP8 values show it.
 __device__ __forceinline__ float inv_rms(float sum, int d, float eps) {
@@ -324,8 +333,11 @@ template <typename T, int V, int THREADS, bool ADD, bool VEC>
 __global__ void __launch_bounds__(THREADS, resident_threads(V, THREADS, 3) / THREADS)
 norm_grad_kernel(const __grid_constant__ NormGradParams p) {
   constexpr int VN = 16 / (int)sizeof(T), STAGES = THREADS == 1024 ? 1 : 2;
+  // h and dy stay in registers for dx where these hold them, else they are read again: bf16 rows of three and four vectors a thread
+  // (2048 x 16384 80-84 us spilling, 50 so; 16384 x 4096 with two 83, 84 so).
+  constexpr bool KEEP = sizeof(T) == 4 || V == 2;
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ float part[2][32][2], again[1][32][1];    // (between two uses of `again` lies a barrier of `part`'s)
+  __shared__ float part[2][32][2], part_again[1][32][1];       // (between two uses of the second lies a barrier of the first's)
   const int step = gridDim.x * blockDim.y;
   long long t = (long long)blockIdx.x * blockDim.y + threadIdx.y;
   Rows<T, V, ADD ? 3 : 2, STAGES, VEC> rows;
@@ -350,15 +362,16 @@ norm_grad_kernel(const __grid_constant__ NormGradParams p) {
     const int stage = STAGES > 1 ? slot : 0;
     rows.fetch(STAGES > 1 ? slot ^ 1 : 0, t + (STAGES > 1 ? step : 0) < p.T);
     rows.wait();
-    f32x2 h[V][VN / 2], dy[V][VN / 2], sums[2] = {0, 0};
+    f32x2 h[KEEP ? V : 1][VN / 2], dy[KEEP ? V : 1][VN / 2], sums[2] = {0, 0};
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      rows.read(stage, 0, i, h[i]);
-      rows.read(stage, 1, i, dy[i]);
+      const int k = KEEP ? i : 0;
+      rows.read(stage, 0, i, h[k]);
+      rows.read(stage, 1, i, dy[k]);
 #pragma unroll
       for (int j = 0; j < VN / 2; ++j) {
-        sums[0] = fma2(h[i][j], h[i][j], sums[0]);
-        sums[1] = fma2(mul2(dy[i][j], w[i][j]), h[i][j], sums[1]);
+        sums[0] = fma2(h[k][j], h[k][j], sums[0]);
+        sums[1] = fma2(mul2(dy[k][j], w[i][j]), h[k][j], sums[1]);
       }
     }
     float sum[2], other;
@@ -367,38 +380,57 @@ norm_grad_kernel(const __grid_constant__ NormGradParams p) {
       unpack2(sums[i], sum[i], other);
       sum[i] += other;
     }
-    // Products u h may leave fp32 where dx does not.  Too large, they make the sum infinite or not a number; too small (a thread's sum
-    // is below 2^-100, its products' smallest unit 2^-149), the thread makes it so itself unless its dy are 0, as they are in padded rows
-    // (16384 x 4096 bf16: 83 us, 90 where all dy are 0; 113 with a second sum for those).
-    if (!(fabsf(sum[1]) >= 0x1p-100f)) {
-      f32x2 any = 0;
-#pragma unroll
-      for (int i = 0; i < V; ++i)
-#pragma unroll
-        for (int j = 0; j < VN / 2; ++j) any |= dy[i][j];
-      if ((any & 0x7fffffff7fffffffull) != 0) sum[1] = __uint_as_float(0x7fffffffu);
-    }
     row_sum(sum, part, slot);
     const float s = inv_rms(sum[0], p.d, p.eps);
     const f32x2 s2 = pack2(s, s);
     float m = sum[1] / (float)p.d * s;
-    if (!(fabsf(sum[1]) < INFINITY)) {       // once more, with h s
-      f32x2 pairs = 0;
+    // Products u h may leave fp32 where dx does not: their sum is infinite, not a number, or below 2^-60, of which 2^15 products
+    // below the normal numbers are no part.  Then with h s, unless all dy are 0, as in padded rows.
+    if (!(fabsf(sum[1]) >= 0x1p-60f && fabsf(sum[1]) < INFINITY)) {
+      f32x2 any = 0;
 #pragma unroll
-      for (int i = 0; i < V; ++i)
+      for (int i = 0; i < V; ++i) {
+        const int k = KEEP ? i : 0;
+        if (!KEEP) rows.read(stage, 1, i, dy[k]);
 #pragma unroll
-        for (int j = 0; j < VN / 2; ++j) pairs = fma2(mul2(dy[i][j], w[i][j]), mul2(h[i][j], s2), pairs);
-      float a[1];
-      unpack2(pairs, a[0], other);
-      a[0] += other;
-      row_sum(a, again, 0);
-      m = a[0] / (float)p.d;
+        for (int j = 0; j < VN / 2; ++j) any |= dy[k][j];
+      }
+      m = 0.f;
+      if (row_any((any & 0x7fffffff7fffffffull) != 0)) {
+        f32x2 units = 0;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          f32x2 hi[VN / 2], di[VN / 2];
+          if (!KEEP) {
+            rows.read(stage, 0, i, hi);
+            rows.read(stage, 1, i, di);
+          }
+#pragma unroll
+          for (int j = 0; j < VN / 2; ++j) {
+            if (KEEP) {                      // (copies that nothing of the way of other rows is computed from)
+              asm volatile("mov.b64 %0, %1;" : "=l"(hi[j]) : "l"(h[KEEP ? i : 0][j]));
+              asm volatile("mov.b64 %0, %1;" : "=l"(di[j]) : "l"(dy[KEEP ? i : 0][j]));
+            }
+            units = fma2(mul2(di[j], w[i][j]), mul2(hi[j], s2), units);
+          }
+        }
+        float again[1];
+        unpack2(units, again[0], other);
+        again[0] += other;
+        row_sum(again, part_again, 0);
+        m = again[0] / (float)p.d;
+      }
     }
     const f32x2 m2 = pack2(-m, -m);
     if (t < p.T) {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
+        const int k = KEEP ? i : 0;
         f32x2 g[VN / 2];
+        if (!KEEP) {
+          rows.read(stage, 0, i, h[k]);
+          rows.read(stage, 1, i, dy[k]);
+        }
         if (ADD) {
           rows.read(stage, ADD ? 2 : 0, i, g);
         } else {
@@ -407,9 +439,9 @@ norm_grad_kernel(const __grid_constant__ NormGradParams p) {
         }
 #pragma unroll
         for (int j = 0; j < VN / 2; ++j) {
-          const f32x2 unit = mul2(h[i][j], s2);
-          dw[i][j] = fma2(dy[i][j], unit, dw[i][j]);
-          g[j] = fma2(fma2(unit, m2, mul2(dy[i][j], w[i][j])), s2, g[j]);
+          const f32x2 unit = mul2(h[k][j], s2);
+          dw[i][j] = fma2(dy[k][j], unit, dw[i][j]);
+          g[j] = fma2(fma2(unit, m2, mul2(dy[k][j], w[i][j])), s2, g[j]);
         }
         Piece<T, VN> q;
         q.set(g);
@@ -477,10 +509,10 @@ norm_sum_kernel(const float* part, int parts, int d, int accumulate, float* dw) 
 }
 
 // Vectors of 16 bytes a thread, threads of a row, rows of a block; blocks that a multiprocessor holds, bytes of their ring.
-// More than 512 threads (which leaves 64 registers for each and one stage) only for rows of more than 32 KB.  The backward pass of
-// rows of bf16 over 16 KB has 64 floats of dw a thread and spills: 2048 x 16384 81 us, with a floor of 41.
+// More than 512 threads (which leaves 64 registers for each and one stage) only for rows of more than 32 KB; the backward pass, with
+// 32 floats of dw and of w in bf16, spills there: 2048 x 32768 159 us, with a floor of 82.
 struct Shape { int v, threads, rows, blocks, smem; };
-Shape shape_of(int T, int vecs, int esize, int arrays, int v0 = 0) {
+Shape shape_of(int T, int vecs, int esize, int arrays) {
   Shape s;
   // as many rows as make 512 threads (few blocks leave few shares of dw to add up)
   auto with = [&](int v) {
@@ -492,11 +524,8 @@ Shape shape_of(int T, int vecs, int esize, int arrays, int v0 = 0) {
   // The fewest vectors a thread with which 700 are at work, or the most there can be: 16384 x 5120 bf16 (640 of them) with codes 120 us
   // with two rows of 224 threads, 142 with one of 320; 16384 x 4099 262 and 413.  (By the row's length alone, so that its sums
   // do not depend on the rows around it.)
-  if (v0 == 0) {
-    const int most = std::max(with(2), std::max(with(3), with(4)));
-    for (v0 = 2; with(v0) < (most < 700 ? most : 700); ++v0) {}
-  }
-  with(v0);
+  const int most = std::max(with(2), std::max(with(3), with(4)));
+  for (int v = 2; with(v) < (most < 700 ? most : 700); ++v) {}
   // as long as every multiprocessor has some
   const int fill = T / sm_count();
   if (s.rows > fill) s.rows = fill > 0 ? fill : 1;
@@ -539,12 +568,6 @@ template <typename T> cudaError_t norm(const NormParams& p, cudaStream_t st) {
   });
 }
 
-// bf16: three vectors a thread spill here, which costs more than few threads where the rest is fast (16384 x 5120 136 us, 120 with two;
-// 16384 x 4099 369, 468 with two).
-Shape grad_shape(int T, int d, int esize) {
-  const int vecs = vectors(d, esize);
-  return shape_of(T, vecs, esize, 3, esize == 2 && d % 8 == 0 && vecs <= 1024 ? 2 : 0);
-}
 int grad_parts(int T, const Shape& s) {
   const long long want = (T + s.rows - 1ll) / s.rows, most = (long long)s.blocks * sm_count();
   return (int)(want < most ? (want > 0 ? want : 1) : most);
@@ -552,7 +575,7 @@ int grad_parts(int T, const Shape& s) {
 
 template <typename T> cudaError_t norm_grad(const NormGradParams& p, cudaStream_t st) {
   const int e = sizeof(T);
-  const Shape s = grad_shape(p.T, p.d, e);
+  const Shape s = shape_of(p.T, vectors(p.d, e), e, 3);
   const bool vec = p.d * e % 16 == 0 && rows16(p.h, p.h_stride, e) && rows16(p.w, 0, e) && rows16(p.dy, p.dy_stride, e) &&
                    rows16(p.dh, p.dh_stride, e) && rows16(p.dx, p.dx_stride, e);
   const int parts = grad_parts(p.T, s);
@@ -574,7 +597,7 @@ template <typename T> cudaError_t norm_grad(const NormGradParams& p, cudaStream_
 // Blocks of the backward pass, each with a share of dw: as many as are resident at once.
 int norm_grad_parts(int T, int d, int dtype) {
   const int e = dtype == BTX_BF16 ? 2 : 4;
-  return grad_parts(T, grad_shape(T, d, e));
+  return grad_parts(T, shape_of(T, vectors(d, e), e, 3));
 }
 
 cudaError_t launch_norm(const NormParams& p, int dtype, cudaStream_t st) {
