@@ -1,5 +1,6 @@
 // Products of FP8 matrices on the 5th-generation tensor cores (tcgen05.mma kind::mxf8f6f4.block_scale): codes straight from
-// memory to shared memory by TMA, scales through shared memory into tensor memory (tcgen05.cp), fp32 sums in tensor memory.  y = A B^T with both operands K-major, per output element
+// memory to shared memory by TMA, scales through shared memory into tensor memory (tcgen05.cp), fp32 sums in tensor memory.
+// y = A B^T with both operands K-major, per output element
 //   sum over blocks of 128:  2^(sa - 127) 2^(sb - 127) sum a_i b_i.
 // An MMA covers 32 contraction elements and takes one scale per row for them; the four MMAs of a block name the same byte of
 // the row's word in tensor memory, the four blocks of a scale tile the four bytes in turn.  So one 512-byte tile of 128 rows
@@ -8,10 +9,10 @@
 // Two kernels, as for MXFP4: fp8_gemm_kernel, a CTA per tile of 128 rows and 64 or 128 columns, for few rows (bound by reading B), and
 // fp8_gemm_pair_kernel, two CTAs per 256 x 256 tile, for many (bound by the tensor cores and their power).
 //
-// Measured on one B200 (replayed): 1 x 4096 x 11008 12.5-13.2 us (45 MB of B, 6.9 at the rate of a copy), 333 x 1001 x 2083 9.0,
-// 1024 x 4096 x 4096 16.4; 8192 x 11008 x 4096 258-267 us in short runs, 2.8 PFLOP/s, and 307 under the power limit, 2.4 PFLOP/s
+// Measured on one B200 (replayed): 1 x 4096 x 11008 12.5-13.3 us (45 MB of B, 6.9 at the rate of a copy), 333 x 1001 x 2083 9.0,
+// 1024 x 4096 x 4096 16.4-16.8; 8192 x 11008 x 4096 256-267 us in short runs, 2.8 PFLOP/s, and 307 under the power limit, 2.4 PFLOP/s
 // (a library product with one scale for each operand 301).  At 4001 x 4096 x 11008 256 tiles on 74 pairs are four
-// rounds where 3.46 would do: 163 us (143).  The tensor pipe is active 65-68 % of the time in the pair kernel; in the layer of 32
+// rounds where 3.46 would do: 163 us (143).  The tensor pipe is active 65-69 % of the time in the pair kernel; in the layer of 32
 // tokens gate_up reads its 361 MB at 5.3 TB/s.
 //
 // fp8_gemm_kernel:

@@ -11,9 +11,10 @@
 // resident and walk over the rows.  Every thread fetches its own vectors of the next rows into its own places in shared memory
 // (cp.async), so what is in flight does not depend on registers and nobody waits for another thread's copy.
 //
-// Measured on one B200 (16384 x 4096, replayed; the floor is the bytes at the 6561 GB/s of a copy).  Forward, bf16: with
-// residual, h and y 84.2 us (81.8), and codes too 94-95 (92), y alone 48 (40.9); fp32 with codes 175 (174).  Backward, bf16: 82 us
-// (81.8), and 5 of these are the second kernel.  Issue slots are taken to 52-54 %.  One row of 4096: 2.4 us, a launch.
+// Measured on one B200 (16384 x 4096, replayed; the floor is the bytes at the 6561 GB/s of a copy; a replay finds part of its data in
+// the L2).  Forward, bf16: with residual, h and y 83 us (81.8), and codes too 94-95 (92), y alone 47 (40.9); fp32 with codes 176 (174).
+// Backward with dh, bf16: 82.5 us (81.8), 3 of these for the second kernel, 93 from a cold L2; fp32 158.  Issue slots are taken to
+// 52-56 %.  One row of 4096: 2.3 us, a launch.
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -57,8 +58,8 @@ __device__ __forceinline__ bool row_any(bool yes) {
   return any;
 }
 
-// 1 / sqrt(m), m = sum / d + eps, and a step of Newton's method on it (with the product m s in two words), which leaves about half
-// an ulp of its two roundings: a row's elements share this error, and those near the middle between two FP8 values show it.
+// 1 / sqrt(m) of the fp32 m = sum / d + eps, and a step of Newton's method on it (with the product m s in two words), which leaves
+// about half an ulp of its two roundings: a row's elements share this error, and those near the middle between two FP8 values show it.
 __device__ __forceinline__ float inv_rms(float sum, int d, float eps) {
   const float m = sum / (float)d + eps, s = 1.0f / sqrtf(m);
   if (!(m > 0.f && m < INFINITY)) return s;
@@ -72,9 +73,9 @@ __device__ __forceinline__ float inv_rms(float sum, int d, float eps) {
 // Otherwise rows go by words of 4 bytes.  A row of bf16 that starts in the middle of a word is kept and written as the words that
 // hold it: word k of a vector has elements 2k - 1 and 2k, element 7 is in the next lane's word 0, which the warp's last lane
 // fetches for itself.  Words that reach over an end of the row are put together from single elements.  Words of fp32 (TURNED) are
-// fetched and written 32 neighbours at a time and change hands in shared memory (16384 x 4097, gradients: 279 to 256 us; bf16, where
+// fetched and written 32 neighbours at a time and change hands in shared memory (16384 x 4097, gradients: 246 us, 279 without; bf16, where
 // half words change hands too, does not gain).  Latency of the longer way of a row bounds these (32-39 % of the issue slots, 28 % of
-// the shared memory's): 16384 x 4098 bf16 with residual and h 195 us, 4099 226, where 4096 takes 84 (single elements took 403;
+// the shared memory's): 16384 x 4098 bf16 with residual, h and y 203 us, 4099 231, where 4096 takes 83 (single elements took 403;
 // aligned 16-byte pieces and shifts were slower, as the pieces at a row's ends then have to be waited for).
 template <typename T, int V, int ARRAYS, int STAGES, bool VEC> struct Rows {
   static constexpr int VN = 16 / (int)sizeof(T);
@@ -226,7 +227,7 @@ template <typename T, int V, int ARRAYS, int STAGES, bool VEC> struct Rows {
 
 // Threads of a multiprocessor that the registers are meant for.  What is in flight should be about 64 KB: with a residual (two
 // loads a vector) or in the backward pass 512 threads have that, with one tensor to read it takes 1024
-// (16384 x 4096 without a residual: bf16 44 us, with 512 threads 52; fp32 82 and 105).
+// (16384 x 4096 without a residual: bf16 47 us, with 512 threads 53; fp32 83 and 107).
 constexpr int resident_threads(int v, int threads, int arrays) { return threads == 1024 || (arrays == 1 && v == 2) ? 1024 : 512; }
 
 template <typename T, int V, int THREADS, bool RESIDUAL, bool VEC>
@@ -327,8 +328,8 @@ norm_kernel(const __grid_constant__ NormParams p) {
   }
 }
 
-// sum h^2 and, with u = dy w, sum u h; then dw += dy (h s) and dx = dh + s (u - m (h s)), m = s sum(u h) / d.  With m h s in this order no product
-// leaves fp32 where dx does not.
+// sum h^2 and, with u = dy w, sum u h; then dw += dy (h s) and dx = dh + s (u - m (h s)), m = s sum(u h) / d.  h s is of size 1, so
+// that s^2, which may leave fp32 where dx does not, is not formed.
 template <typename T, int V, int THREADS, bool ADD, bool VEC>
 __global__ void __launch_bounds__(THREADS, resident_threads(V, THREADS, 3) / THREADS)
 norm_grad_kernel(const __grid_constant__ NormGradParams p) {
@@ -522,7 +523,7 @@ Shape shape_of(int T, int vecs, int esize, int arrays) {
     return s.threads <= 512 || v == 4 ? s.rows * vecs : 0;
   };
   // The fewest vectors a thread with which 700 are at work, or the most there can be: 16384 x 5120 bf16 (640 of them) with codes 120 us
-  // with two rows of 224 threads, 142 with one of 320; 16384 x 4099 262 and 413.  (By the row's length alone, so that its sums
+  // with two rows of 224 threads, 142 with one of 320, gradients 101 and 124; 16384 x 4099 with codes 266 and 413.  (By the row's length alone, so that its sums
   // do not depend on the rows around it.)
   const int most = std::max(with(2), std::max(with(3), with(4)));
   for (int v = 2; with(v) < (most < 700 ? most : 700); ++v) {}
