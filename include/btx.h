@@ -406,8 +406,8 @@ btx_status btx_rms_norm(const btx_norm_desc* desc, const void* x, int64_t x_stri
  *   dweight[d] = sum over rows of dy * h * s, fp32 (NULL: not wanted); accumulate = 1 adds to it.
  * h is the h of the forward call (x where there was no residual).  Sums are fp32, in an order that repeats from run to
  * run.  g is an fp32 number; where those of a row are below 2^112 nothing formed from them leaves fp32 unless dx does.  A row whose
- * sum of squares passes the largest fp32 number has dx = dh and no part in dweight.  dx may be dy, dh or h itself (same address and stride).  T = 0 leaves
- * dweight 0 (accumulate: as it was). */
+ * sum of squares passes the largest fp32 number has dx = dh and no part in dweight.  dx may be dy, dh or h itself (same address
+ * and stride).  T = 0 leaves dweight 0 (accumulate: as it was). */
 btx_status btx_rms_norm_backward_workspace_size(const btx_norm_desc* desc, size_t* workspace_bytes);
 btx_status btx_rms_norm_backward(const btx_norm_desc* desc, const void* h, int64_t h_stride, const void* weight,
                                  const void* dy, int64_t dy_stride, const void* dh, int64_t dh_stride, void* dx,

@@ -798,7 +798,7 @@ Plan1 plan_single(double row_tiles_, long long rows, long long N, long long K) {
 double pair_us(double tiles, long long K, double epi) {
   return 3.5 + ceil(tiles / (sm_count() / 2)) * (fmax((double)((K + SKB - 1) / SKB) * 0.45, epi) + 0.85);
 }
-// Epilogues of a 256 x 256 tile.  (kGateUpUs: T = 4096, d = 128, F = 11008, one expert, 19 rounds of tiles with one stage each, 114 us.)
+// Epilogues of a 256 x 256 tile.  (kGateUpUs: T = 4096, d = 128, F = 11008, one expert, 19 rounds of tiles of one stage in about 106 us.)
 constexpr double kStoreUs = 2.0, kGateUpUs = 4.5, kDownUs = 3.5;
 
 }  // namespace

@@ -523,8 +523,8 @@ Shape shape_of(int T, int vecs, int esize, int arrays) {
     return s.threads <= 512 || v == 4 ? s.rows * vecs : 0;
   };
   // The fewest vectors a thread with which 700 are at work, or the most there can be: 16384 x 5120 bf16 (640 of them) with codes 120 us
-  // with two rows of 224 threads, 142 with one of 320, gradients 101 and 124; 16384 x 4099 with codes 266 and 413.  (By the row's length alone, so that its sums
-  // do not depend on the rows around it.)
+  // with two rows of 224 threads, 142 with one of 320, gradients 101 and 124; 16384 x 4099 with codes 266
+  // and 413.  (By the row's length alone, so that its sums do not depend on the rows around it.)
   const int most = std::max(with(2), std::max(with(3), with(4)));
   for (int v = 2; with(v) < (most < 700 ? most : 700); ++v) {}
   // as long as every multiprocessor has some
